@@ -514,6 +514,234 @@ AF1_API int af1_hisa_module_budgets(const double* phi_dir, const double* phi_mag
  * af1_rank_for_budget. Errors: INVALID_ARG. */
 AF1_API int af1_budget_to_rank(double b, int64_t m, int64_t n, int64_t* r_out);
 
+/* ---- the step around the linears: positions, cache, drafted tokens, scores ----
+ * What a decoder runs between its q | k | v projections and the output
+ * projection, and after the logits, for single tokens and for trees of drafted
+ * tokens. The paper has no counterpart. Values are FP16 or FP32 (AF1_F16,
+ * AF1_F32), as the linears write them; sums, softmax statistics and rotations
+ * are FP32. Strides are in elements; the last axis of every tensor has unit
+ * stride. A call with nothing to do (no tokens, no sequences) returns AF1_OK. */
+
+/* Rotary position tables. Pair i of the `dim` rotated entries turns by
+ * position * f_i, f_i = base^(-2i / dim), rescaled for contexts longer than
+ * the `original` one by one of
+ *   AF1_ROPE_LINEAR  f_i / factor
+ *   AF1_ROPE_BASE    base * factor^(dim / (dim - 2)) in place of base
+ *   AF1_ROPE_BANDS   by wavelength w = 2 pi / f_i: f_i where w < original / high,
+ *                    f_i / factor where w > original / low, in between
+ *                    (1 - g) f_i / factor + g f_i with g = (original / w - low) / (high - low)
+ *   AF1_ROPE_RAMP    by index: with e(beta) = dim ln(original / (2 pi beta)) / (2 ln base),
+ *                    i0 = max(0, floor e(high)), i1 = min(dim - 1, ceil e(low)) and
+ *                    g = clamp((i - i0) / (i1 - i0), 0, 1): (1 - g) f_i + g f_i / factor
+ * Every cos and sin is multiplied by `attention` (0: 1, or 0.1 ln(factor) + 1
+ * for AF1_ROPE_RAMP). The angles are FP64, the table is FP32. */
+#define AF1_ROPE_PLAIN 0
+#define AF1_ROPE_LINEAR 1
+#define AF1_ROPE_BASE 2
+#define AF1_ROPE_BANDS 3
+#define AF1_ROPE_RAMP 4
+typedef struct af1_rope_params {
+  int64_t length;    /* positions 0 .. length - 1, 1 .. 2^24 */
+  int32_t dim;       /* rotated entries of a head: even, 2 .. 256 */
+  int32_t scaling;   /* AF1_ROPE_* */
+  double base;       /* > 1 */
+  double factor;     /* >= 1 (ignored by AF1_ROPE_PLAIN) */
+  double low, high;  /* AF1_ROPE_BANDS: 0 < low < high; AF1_ROPE_RAMP: beta_slow < beta_fast */
+  double original;   /* > 0 for AF1_ROPE_BANDS and AF1_ROPE_RAMP */
+  double attention;  /* >= 0 */
+} af1_rope_params;
+
+/* The pairs' frequencies (dim / 2 doubles) and the factor of every cos and
+ * sin. Host-only. Errors: INVALID_ARG. */
+AF1_API int af1_rope_frequencies(const af1_rope_params* params, double* freq, double* attention);
+
+/* Fill table (device FP32 [length][dim / 2][2], cos then sin). Errors:
+ * INVALID_ARG, BAD_POINTER, MISALIGNED (8 bytes), CUDA. */
+AF1_API int af1_rope_table(const af1_rope_params* params, float* table, void* stream);
+
+/* Pairs are adjacent entries (2i, 2i + 1) instead of (i, i + dim / 2). */
+#define AF1_ROPE_INTERLEAVED 1
+/* The gradient with respect to the input: each pair turned back (times the
+ * table's factor), y = the transposed rotation of x. */
+#define AF1_ROPE_BACKWARD 2
+
+/* Rotate the first rope_dim entries of every head; the others are copied.
+ *   x, y: [tokens][heads][dim] of `dtype`, strides x_token, x_head, y_token,
+ *       y_head; y may be x (with equal strides), otherwise they may not
+ *       overlap. No result is rounded but the last: products and their sum
+ *       are FP32, each rounded on its own.
+ *   positions: device int32 [tokens]. A position outside 0 .. length - 1 makes
+ *       the token's rotated entries NaN.
+ *   table: device FP32 [length][rope_dim / 2][2], as af1_rope_table fills it.
+ * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
+typedef struct af1_rope_args {
+  const void* x;
+  void* y;
+  const int32_t* positions;
+  const float* table;
+  int64_t tokens, heads, dim, rope_dim, length;
+  int64_t x_token, x_head, y_token, y_head;
+  int32_t dtype; /* AF1_F16 or AF1_F32 */
+  int32_t flags; /* AF1_ROPE_INTERLEAVED, AF1_ROPE_BACKWARD */
+} af1_rope_args;
+AF1_API int af1_rope(const af1_rope_args* args, void* stream);
+
+/* A paged cache of keys and values over the caller's buffers. Slot p of a
+ * sequence lies in row p % page_size of page table[sequence][p / page_size].
+ *   k, v: [pages][kv_heads][page_size][row], row = head_dim entries:
+ *     AF1_KV_F16   FP16
+ *     AF1_KV_INT8  int8 codes, value = code * scale
+ *     AF1_KV_E4M3  8-bit floating point codes (4 exponent, 3 fraction bits), value = code * scale
+ *     AF1_KV_INT4  4-bit codes, entry 2i in the low half of byte i, value = code * scale + low
+ *   k_scale, v_scale: INT8 and E4M3: FP32 [pages][kv_heads][page_size], one per
+ *     vector; INT4: FP16 [pages][kv_heads][page_size][head_dim / 32][2], scale
+ *     and low of every 32 entries; F16: NULL.
+ * What is stored for a vector x (FP32 arithmetic, each step rounded on its own):
+ *   INT8  scale = max|x| * (1/127), code = clamp(rint(x * (1 / scale)), -127, 127)
+ *   E4M3  scale = max|x| * (1/448), code = x * (1 / scale), clamped to +-448, to nearest even
+ *   INT4  scale = FP16((max x - min x) * (1/15)), low = FP16(min x),
+ *         code = clamp(rint((x - low) * (1 / scale)), 0, 15)
+ * with 1 / scale read as 0 where scale is 0, or below 2^-120 for INT8 and
+ * E4M3 (scale is then stored as 0). Vectors (INT4: groups) that hold an
+ * infinity or a NaN, or whose scale or low is not finite, are stored with
+ * codes 0 and scale (and low) NaN. Buffers are 16-byte aligned. */
+#define AF1_KV_F16 0
+#define AF1_KV_INT8 1
+#define AF1_KV_E4M3 2
+#define AF1_KV_INT4 3
+typedef struct af1_kv_desc {
+  int64_t pages;     /* 1 .. 2^31 - 1 */
+  int32_t page_size; /* 16, 32, 64, 128 or 256 */
+  int32_t kv_heads;  /* 1 .. 1024 */
+  int32_t head_dim;  /* 64 or 128 */
+  int32_t kind;      /* AF1_KV_* */
+  void *k, *v, *k_scale, *v_scale;
+} af1_kv_desc;
+typedef struct af1_kv_cache af1_kv_cache; /* opaque: a checked description; the buffers stay the caller's */
+
+/* Check a description and keep it. Errors: INVALID_ARG, BAD_POINTER,
+ * MISALIGNED, CUDA. */
+AF1_API int af1_kv_create(const af1_kv_desc* desc, af1_kv_cache** out);
+/* Release a description (not the buffers). NULL is a no-op. */
+AF1_API void af1_kv_free(af1_kv_cache* cache);
+
+/* Write tokens to the cache, keys rotated on the way; optionally rotate the
+ * tokens' queries in the same launch.
+ *   k, v: [tokens][kv_heads][head_dim] of `dtype`, strides k_token, k_head, ...
+ *   seq, slot: device int32 [tokens]: where each token goes. A token whose
+ *       slot is negative is padding: nothing is stored and its rows of q_out,
+ *       k_out and v_out are zero. A token whose seq, slot or page lies outside
+ *       the table or the cache is not stored. No two tokens may share a slot.
+ *   pages: device int32 [sequences][page_columns], row stride pages_ld.
+ *   table, length, rope_dim, flags: rotation as in af1_rope (no BACKWARD);
+ *       table NULL: none. positions: device int32 [tokens], or NULL: the slots.
+ *   q, q_out: [tokens][q_heads][head_dim], q of `dtype`, q_out FP16; NULL: none.
+ *       q_out may be q (FP16, equal strides).
+ *   k_out, v_out: FP16 [tokens][kv_heads][head_dim] contiguous, the values
+ *       that the cache holds for the tokens, or NULL.
+ * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
+typedef struct af1_kv_append_args {
+  const void *k, *v;
+  int64_t k_token, k_head, v_token, v_head;
+  const int32_t *seq, *slot, *positions, *pages;
+  int64_t tokens, sequences, page_columns, pages_ld;
+  const float* table;
+  int64_t length, rope_dim;
+  const void* q;
+  void* q_out;
+  int64_t q_heads, q_token, q_head, qo_token, qo_head;
+  void *k_out, *v_out;
+  int32_t dtype; /* of q, k and v */
+  int32_t flags; /* AF1_ROPE_INTERLEAVED */
+} af1_kv_append_args;
+AF1_API int af1_kv_append(const af1_kv_cache* cache, const af1_kv_append_args* args, void* stream);
+
+/* Read slots first .. first + count - 1 of every sequence back.
+ *   lens: device int32 [sequences]: slots at lens and after, and slots whose
+ *       page lies outside the cache, give zeros.
+ *   k_out, v_out: [sequences][count][kv_heads][head_dim] of `dtype`, contiguous.
+ * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
+AF1_API int af1_kv_read(const af1_kv_cache* cache, const int32_t* pages, int64_t sequences, int64_t page_columns,
+                        int64_t pages_ld, const int32_t* lens, int64_t first, int64_t count, void* k_out,
+                        void* v_out, int dtype, void* stream);
+
+/* Mask words of trees: parents device int32 [sequences][nodes] (1 .. 64
+ * nodes), the index of each node's parent, or negative for the children of
+ * the last cached token. Bit j of mask[sequence][node][j / 32] is set where
+ * node j is the node itself or an ancestor of it, least significant bit
+ * first. A parent outside 0 .. nodes - 1 ends the walk up, and so do `nodes`
+ * steps. Errors: INVALID_ARG, BAD_POINTER, CUDA. */
+AF1_API int af1_tree_mask(const int32_t* parents, int64_t sequences, int64_t nodes, uint32_t* mask, void* stream);
+
+/* Attention of every sequence's drafted tokens (nodes) over its cache:
+ *   out = softmax(scale q k^T) v over the keys that a node sees: slots
+ *   0 .. lens - 1, and of the nodes' own slots lens .. lens + counts - 1 those
+ *   whose bit is set in its mask. One node with its own bit set is plain
+ *   decoding. A node that sees no key, and nodes at counts and after, give
+ *   zeros and lse -infinity.
+ *   q: FP16 [sequences][nodes][q_heads][head_dim], strides q_seq, q_node,
+ *       q_head (multiples of 8), 16-byte aligned; q_heads is a multiple of the
+ *       cache's kv_heads, head h reads cached head h / (q_heads / kv_heads).
+ *   lens: device int32 [sequences] (negative: 0). counts: device int32
+ *       [sequences] or NULL (all `nodes`). Slots beyond the table and slots
+ *       whose page lies outside the cache are not seen.
+ *   mask: uint32 [sequences][nodes][(nodes + 31) / 32], sequence stride
+ *       mask_seq words (0: one mask for all), or NULL: node i sees 0 .. i.
+ *   out: [sequences][nodes][q_heads][head_dim] of out_dtype, strides o_*
+ *       (multiples of 8 for FP16, 4 for FP32), 16-byte aligned.
+ *   lse: FP32 [sequences][nodes][q_heads] contiguous, the natural logarithm of
+ *       the softmax denominators, or NULL.
+ *   workspace: af1_tree_workspace_bytes bytes, with the rules of
+ *       af1_linear_forward (256-byte aligned, zero-filled before first use).
+ * An infinite or NaN key or value reaches the nodes that see it and no other.
+ * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, WORKSPACE, CUDA. */
+typedef struct af1_tree_args {
+  const void* q;
+  int64_t q_seq, q_node, q_head;
+  void* out;
+  int64_t o_seq, o_node, o_head;
+  float* lse;
+  const int32_t *pages, *lens, *counts;
+  const uint32_t* mask;
+  int64_t mask_seq;
+  int64_t sequences, nodes, q_heads, page_columns, pages_ld;
+  float scale;
+  int32_t out_dtype;
+} af1_tree_args;
+AF1_API int64_t af1_tree_workspace_bytes(const af1_kv_cache* cache, int64_t sequences, int64_t nodes,
+                                         int64_t q_heads);
+AF1_API int af1_tree_attention(const af1_kv_cache* cache, const af1_tree_args* args, void* workspace,
+                               int64_t workspace_bytes, void* stream);
+
+/* Scores of given tokens. For every row x of logits, divided by temperature:
+ *   logprobs[row][i] = x[tokens[row][i]] - log sum exp x (-infinity for a token
+ *       outside 0 .. vocab - 1),
+ *   entropy[row] = - sum p log p, p = softmax(x),
+ *   top_logprobs[row][j], top_ids[row][j]: the `top` largest entries in
+ *       descending order, equal ones by ascending index.
+ *   logits: [rows][vocab] of `dtype`, row stride ld; -infinity bans a token.
+ *   tokens: device int32 [rows][given], contiguous.
+ *   Outputs are FP32 and int32, contiguous. logprobs, entropy, and the two top_*
+ *   together, may be NULL (given 0, top 0).
+ * A row of -infinity alone has log-probabilities -infinity and entropy 0; one
+ * with a NaN or +infinity has NaN everywhere, its top_ids taken with NaN as
+ * the largest value. Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
+typedef struct af1_logprob_args {
+  const void* logits;
+  int64_t rows, vocab, ld;
+  const int32_t* tokens;
+  int64_t given;      /* 0 .. 1024 */
+  float* logprobs;
+  float* entropy;
+  float* top_logprobs;
+  int32_t* top_ids;
+  int32_t top;        /* 0 .. 32, at most vocab */
+  int32_t dtype;      /* AF1_F16 or AF1_F32 */
+  float temperature;  /* > 0 */
+  int32_t reserved;   /* must be 0 */
+} af1_logprob_args;
+AF1_API int af1_token_logprobs(const af1_logprob_args* args, void* stream);
+
 /* Message for the last error on the calling thread ("" if none). */
 AF1_API const char* af1_last_error(void);
 

@@ -20,6 +20,7 @@ import torch
 __all__ = [
     "AF1Error", "Layer", "Step", "rank_for_budget", "workspace_status", "static_status", "last_error", "version",
     "lib_path", "words_per_row", "set_wait_cycles", "get_wait_cycles", "AF1_F16", "AF1_F32",
+    "KVCache", "rope", "rope_table", "rope_frequencies", "tree_mask", "token_logprobs",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -639,3 +640,8 @@ class Step:
             self.destroy()
         except Exception:
             pass
+
+
+# -- the step around the linears -------------------------------------------------------
+
+from .attention import KVCache, rope, rope_frequencies, rope_table, token_logprobs, tree_mask  # noqa: E402

@@ -1,0 +1,867 @@
+// af1_kv.cu — rotary positions, and the paged cache of keys and values as it
+// is written and read back.
+//
+// All kernels here move data once and compute little, so device memory (or,
+// for a few tokens, the launch) bounds them: every thread holds 8 entries of
+// one head, 16 bytes of FP16, and neighbouring threads hold neighbouring
+// entries.
+//
+// The rotation of a pair is (a c - b s, b c + a s). Its products and sums are
+// rounded one by one (no fused multiply-add), as are the steps of the
+// quantiser, so that what a cache holds is a function of the inputs to the
+// bit, whichever launch wrote it.
+#include <cuda_fp8.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <type_traits>
+
+#include "af1_internal.h"
+#include "af1_kv.cuh"
+
+namespace af1 {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kTiny = 7.52316385e-37f;  // 2^-120: smaller scales are stored as 0
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+__device__ __forceinline__ void from_f32(float& y, float x) { y = x; }
+__device__ __forceinline__ void from_f32(__half& y, float x) { y = __float2half_rn(x); }
+
+// N entries at p: in 16-byte (or, for 4 FP16, 8-byte) accesses if VEC, else one by one.
+template <bool VEC, int N, typename T>
+__device__ __forceinline__ void load(float (&x)[N], const T* p) {
+  if constexpr (VEC) {
+    constexpr int B = N * (int)sizeof(T) >= 16 ? 16 : 8;
+    constexpr int E = B / (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < N / E; ++i) {
+      alignas(16) T t[E];
+      if constexpr (B == 16)
+        *reinterpret_cast<uint4*>(t) = reinterpret_cast<const uint4*>(p)[i];
+      else
+        *reinterpret_cast<uint2*>(t) = reinterpret_cast<const uint2*>(p)[i];
+#pragma unroll
+      for (int j = 0; j < E; ++j) x[i * E + j] = to_f32(t[j]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = to_f32(p[i]);
+  }
+}
+template <bool VEC, int N, typename T>
+__device__ __forceinline__ void store(T* p, const float (&x)[N]) {
+  if constexpr (VEC) {
+    constexpr int B = N * (int)sizeof(T) >= 16 ? 16 : 8;
+    constexpr int E = B / (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < N / E; ++i) {
+      alignas(16) T t[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) from_f32(t[j], x[i * E + j]);
+      if constexpr (B == 16)
+        reinterpret_cast<uint4*>(p)[i] = *reinterpret_cast<const uint4*>(t);
+      else
+        reinterpret_cast<uint2*>(p)[i] = *reinterpret_cast<const uint2*>(t);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) from_f32(p[i], x[i]);
+  }
+}
+
+// cos and sin of N consecutive pairs of a table row (NaN outside the table).
+template <bool VEC, int N>
+__device__ __forceinline__ void load_turn(float (&c)[N], float (&s)[N], const float* table, int64_t length, int half,
+                                          int pos, int pair) {
+  if (pos < 0 || pos >= length) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) c[i] = s[i] = __int_as_float(0x7fffffff);
+    return;
+  }
+  const float* p = table + ((int64_t)pos * half + pair) * 2;
+  if constexpr (VEC) {
+    float t[2 * N];
+    load<true>(t, p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) c[i] = t[2 * i], s[i] = t[2 * i + 1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float2 t = reinterpret_cast<const float2*>(p)[i];
+      c[i] = t.x, s[i] = t.y;
+    }
+  }
+}
+
+// ---- rope --------------------------------------------------------------------
+
+struct RopeProblem {
+  const void* x;
+  void* y;
+  const int32_t* positions;
+  const int32_t* slot;  // append: a negative slot zeroes the token's rows (nullptr: no padding)
+  const float* table;   // nullptr: copy
+  int64_t length, x_token, x_head, y_token, y_head;
+  int heads, half, units, pairs_units;  // units of a head: pairs_units of VP pairs, then copies of 2 VP entries
+  int64_t total;                        // tokens * heads * units
+  bool back;
+};
+
+// One unit: VP pairs of a head, or 2 VP entries that are only copied. A
+// thread owns both entries of its pairs, so that y may be x.
+template <typename TI, typename TO, int VP, bool IL>
+__device__ __forceinline__ void rope_unit(const RopeProblem& p, int64_t id) {
+  const int64_t row = id / p.units;
+  const int u = (int)(id - row * p.units);
+  const int64_t token = row / p.heads;
+  const int head = (int)(row - token * p.heads);
+  const TI* x = static_cast<const TI*>(p.x) + token * p.x_token + head * p.x_head;
+  TO* y = static_cast<TO*>(p.y) + token * p.y_token + head * p.y_head;
+  constexpr bool VEC = VP > 1;
+  const bool pad = p.slot != nullptr && p.slot[token] < 0;
+  if (u >= p.pairs_units) {
+    const int at = 2 * p.half + (u - p.pairs_units) * 2 * VP;
+    float a[2 * VP];
+    load<VEC>(a, x + at);
+    if (pad) {
+#pragma unroll
+      for (int i = 0; i < 2 * VP; ++i) a[i] = 0.f;
+    }
+    store<VEC>(y + at, a);
+    return;
+  }
+  float a[VP], b[VP], c[VP], s[VP];
+  if constexpr (IL) {
+    float t[2 * VP];
+    load<VEC>(t, x + u * 2 * VP);
+#pragma unroll
+    for (int i = 0; i < VP; ++i) a[i] = t[2 * i], b[i] = t[2 * i + 1];
+  } else {
+    load<VEC>(a, x + u * VP);
+    load<VEC>(b, x + p.half + u * VP);
+  }
+  load_turn<VEC>(c, s, p.table, p.length, p.half, pad ? 0 : p.positions[token], u * VP);
+  float ya[VP], yb[VP];
+#pragma unroll
+  for (int i = 0; i < VP; ++i) {
+    const float si = p.back ? -s[i] : s[i];
+    ya[i] = __fsub_rn(__fmul_rn(a[i], c[i]), __fmul_rn(b[i], si));
+    yb[i] = __fadd_rn(__fmul_rn(b[i], c[i]), __fmul_rn(a[i], si));
+    if (pad) ya[i] = yb[i] = 0.f;
+  }
+  if constexpr (IL) {
+    float t[2 * VP];
+#pragma unroll
+    for (int i = 0; i < VP; ++i) t[2 * i] = ya[i], t[2 * i + 1] = yb[i];
+    store<VEC>(y + u * 2 * VP, t);
+  } else {
+    store<VEC>(y + u * VP, ya);
+    store<VEC>(y + p.half + u * VP, yb);
+  }
+}
+
+template <typename T, int VP, bool IL>
+__global__ void __launch_bounds__(kThreads) rope_kernel(const RopeProblem p) {
+  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (id < p.total) rope_unit<T, T, VP, IL>(p, id);
+}
+
+// Units of a head, and whether 4 pairs to a thread fit the sizes, strides and
+// pointers (else one pair: any even rope_dim, any stride).
+bool plan_rope(RopeProblem& p, int64_t tokens, int dim, int rope_dim, size_t xs, size_t ys, bool il,
+               bool may = true) {
+  const int per = il ? 8 : 4;  // entries of one vector access
+  auto fits = [&](const void* q, int64_t a, int64_t b, size_t size) {
+    return (uintptr_t)q % std::min<size_t>(16, per * size) == 0 && a % 8 == 0 && b % 8 == 0;
+  };
+  const bool vec = may && dim % 8 == 0 && rope_dim % 8 == 0 && fits(p.x, p.x_token, p.x_head, xs) &&
+                   fits(p.y, p.y_token, p.y_head, ys) && (uintptr_t)p.x % 16 == 0 && (uintptr_t)p.y % 16 == 0 &&
+                   (uintptr_t)p.table % 16 == 0;
+  const int vp = vec ? 4 : 1;
+  p.half = rope_dim / 2;
+  p.pairs_units = p.half / vp;
+  p.units = p.pairs_units + (dim - rope_dim) / (2 * vp);
+  p.total = tokens * p.heads * p.units;
+  return vec;
+}
+
+// ---- the table -----------------------------------------------------------------
+
+struct RopeFreq {
+  double f[128];
+  double attention;
+  int64_t length;
+  int half;
+};
+
+__global__ void __launch_bounds__(kThreads) rope_table_kernel(const __grid_constant__ RopeFreq p, float2* table) {
+  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (id >= p.length * p.half) return;
+  const int64_t pos = id / p.half;
+  double s, c;
+  sincos((double)pos * p.f[id - pos * p.half], &s, &c);
+  table[id] = make_float2((float)(c * p.attention), (float)(s * p.attention));
+}
+
+// ---- quantisers ------------------------------------------------------------------
+
+// 8 entries of a vector that LANES neighbouring threads hold: their codes
+// (or FP16 values) to `row`, the vector's scale to `scale`, and the values
+// that the codes stand for to x.
+template <int KIND, int LANES>
+__device__ __forceinline__ void quantise(float (&x)[8], int lane, uint8_t* row, void* scale, bool keep) {
+  if constexpr (KIND == AF1_KV_F16) {
+    alignas(16) __half h[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = __float2half_rn(x[i]), x[i] = __half2float(h[i]);
+    if (keep) reinterpret_cast<uint4*>(row)[lane] = *reinterpret_cast<uint4*>(h);
+  } else if constexpr (KIND == AF1_KV_INT4) {
+    float lo = x[0], hi = x[0];
+    bool bad = !(fabsf(x[0]) < __int_as_float(0x7f800000));
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+      lo = fminf(lo, x[i]), hi = fmaxf(hi, x[i]);
+      bad |= !(fabsf(x[i]) < __int_as_float(0x7f800000));
+    }
+#pragma unroll
+    for (int m = 1; m < 4; m <<= 1) {  // a group of 32 entries: 4 threads
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, m));
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, m));
+      bad |= (bool)__shfl_xor_sync(0xffffffffu, (int)bad, m);
+    }
+    __half hs = __float2half_rn(__fmul_rn(__fsub_rn(hi, lo), (float)(1.0 / 15.0)));
+    __half hl = __float2half_rn(lo);
+    bad |= !(fabsf(__half2float(hs)) <= 65504.f) || !(fabsf(__half2float(hl)) <= 65504.f);
+    const __half nan = __ushort_as_half(0x7fff);
+    if (bad) hs = hl = nan;
+    const float s = __half2float(hs), l = __half2float(hl);
+    const float inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
+    uint32_t codes = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float q = bad ? 0.f : fminf(fmaxf(rintf(__fmul_rn(__fsub_rn(x[i], l), inv)), 0.f), 15.f);
+      codes |= (uint32_t)q << (4 * i);
+      x[i] = __fmaf_rn(q, s, l);
+    }
+    if (keep) {
+      reinterpret_cast<uint32_t*>(row)[lane] = codes;
+      if (lane % 4 == 0) static_cast<__half2*>(scale)[lane / 4] = __halves2half2(hs, hl);
+    }
+  } else {
+    float top = 0.f;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      top = fmaxf(top, fabsf(x[i]));
+      bad |= !(fabsf(x[i]) < __int_as_float(0x7f800000));
+    }
+#pragma unroll
+    for (int m = 1; m < LANES; m <<= 1) {
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+      bad |= (bool)__shfl_xor_sync(0xffffffffu, (int)bad, m);
+    }
+    float s = __fmul_rn(top, (float)(1.0 / (KIND == AF1_KV_INT8 ? 127.0 : 448.0)));
+    if (s < kTiny) s = 0.f;
+    const float inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
+    if (bad) s = __int_as_float(0x7fffffff);
+    alignas(8) uint8_t codes[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float q = bad ? 0.f : __fmul_rn(x[i], inv);
+      if constexpr (KIND == AF1_KV_INT8) {
+        const int c = (int)fminf(fmaxf(rintf(q), -127.f), 127.f);
+        codes[i] = (uint8_t)c;
+        x[i] = __fmul_rn((float)c, s);
+      } else {
+        const __nv_fp8_storage_t c = __nv_cvt_float_to_fp8(q, __NV_SATFINITE, __NV_E4M3);
+        codes[i] = c;
+        x[i] = __fmul_rn(__half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3))), s);
+      }
+    }
+    if (keep) {
+      reinterpret_cast<uint2*>(row)[lane] = *reinterpret_cast<uint2*>(codes);
+      if (lane == 0) *static_cast<float*>(scale) = s;
+    }
+  }
+}
+
+// 8 entries read back.
+template <int KIND>
+__device__ __forceinline__ void dequantise(float (&x)[8], int lane, const uint8_t* row, const void* scale) {
+  if constexpr (KIND == AF1_KV_F16) {
+    load<true>(x, reinterpret_cast<const __half*>(row) + 8 * lane);
+  } else if constexpr (KIND == AF1_KV_INT4) {
+    const uint32_t codes = reinterpret_cast<const uint32_t*>(row)[lane];
+    const float2 s = __half22float2(static_cast<const __half2*>(scale)[lane / 4]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __fmaf_rn((float)(codes >> (4 * i) & 15), s.x, s.y);
+  } else {
+    alignas(8) uint8_t c[8];
+    *reinterpret_cast<uint2*>(c) = reinterpret_cast<const uint2*>(row)[lane];
+    const float s = *static_cast<const float*>(scale);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      x[i] = __fmul_rn(KIND == AF1_KV_INT8 ? (float)(int8_t)c[i]
+                                           : __half2float(__half(__nv_cvt_fp8_to_halfraw(c[i], __NV_E4M3))),
+                       s);
+  }
+}
+
+// ---- append ------------------------------------------------------------------------
+
+struct AppendProblem {
+  KvView cache;
+  PageTable pages;
+  const void *k, *v;
+  int64_t k_token, k_head, v_token, v_head;
+  const int32_t *seq, *slot, *positions;
+  const float* table;
+  int64_t length;
+  __half *k_out, *v_out;
+  int half;
+  int64_t rows;       // 2 * tokens * heads vectors to store
+  int kv_blocks;      // blocks below store them, the others rotate q
+  RopeProblem q;
+};
+
+// Blocks of the cache part: DIM / 8 threads hold one vector, 8 entries each.
+// The entries that a key's own are paired with lie in another thread's part
+// (or, interleaved, in its own) and are read beside them: the second read
+// hits L1, and no exchange between threads depends on rope_dim.
+// 16 tokens x 8 heads x 128 with 32 query heads, INT8: see the table of
+// measurements in the design notes of the repository; the launch bounds it.
+template <int KIND, int DIM, typename T, bool VEC, bool IL>
+__global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendProblem p) {
+  if ((int)blockIdx.x >= p.kv_blocks) {
+    const int64_t id = (int64_t)(blockIdx.x - p.kv_blocks) * kThreads + threadIdx.x;
+    if (id < p.q.total) rope_unit<T, __half, VEC ? 4 : 1, IL>(p.q, id);
+    return;
+  }
+  constexpr int LANES = DIM / 8;
+  int64_t id = (int64_t)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
+  const bool real = id < p.rows;
+  if (!real) id = p.rows - 1;  // keeps every lane of the shuffles below
+  const int lane = threadIdx.x % LANES;
+  const int heads = p.cache.heads;
+  const int64_t token = id / (2 * heads);
+  int head = (int)(id - token * 2 * heads);
+  const bool is_v = head >= heads;
+  if (is_v) head -= heads;
+  const int slot = p.slot[token];
+  const T* src = is_v ? static_cast<const T*>(p.v) + token * p.v_token + head * p.v_head
+                      : static_cast<const T*>(p.k) + token * p.k_token + head * p.k_head;
+  const int at = 8 * lane;
+  float x[8];
+  load<VEC>(x, src + at);
+  if (!is_v && p.half > 0 && at < 2 * p.half) {
+    const int pos = p.positions != nullptr ? p.positions[token] : slot;
+    if constexpr (IL) {
+      float c[4], s[4];
+      if constexpr (VEC) load_turn<true>(c, s, p.table, p.length, p.half, pos, at / 2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (!VEC) {
+          if (at + 2 * i >= 2 * p.half) break;
+          float ci[1], si[1];
+          load_turn<false>(ci, si, p.table, p.length, p.half, pos, at / 2 + i);
+          c[i] = ci[0], s[i] = si[0];
+        }
+        const float a = x[2 * i], b = x[2 * i + 1];
+        x[2 * i] = __fsub_rn(__fmul_rn(a, c[i]), __fmul_rn(b, s[i]));
+        x[2 * i + 1] = __fadd_rn(__fmul_rn(b, c[i]), __fmul_rn(a, s[i]));
+      }
+    } else if (VEC) {  // half is a multiple of 8: the 8 entries lie in one half
+      const bool first = at < p.half;
+      float y[8], c[8], s[8];
+      load<VEC>(y, src + (first ? at + p.half : at - p.half));
+      load_turn<VEC>(c, s, p.table, p.length, p.half, pos, first ? at : at - p.half);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        x[i] = first ? __fsub_rn(__fmul_rn(x[i], c[i]), __fmul_rn(y[i], s[i]))
+                     : __fadd_rn(__fmul_rn(x[i], c[i]), __fmul_rn(y[i], s[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int e = at + i;
+        if (e >= 2 * p.half) break;
+        const bool first = e < p.half;
+        const float y = to_f32(src[first ? e + p.half : e - p.half]);
+        float c[1], s[1];
+        load_turn<false>(c, s, p.table, p.length, p.half, pos, first ? e : e - p.half);
+        x[i] = first ? __fsub_rn(__fmul_rn(x[i], c[0]), __fmul_rn(y, s[0]))
+                     : __fadd_rn(__fmul_rn(x[i], c[0]), __fmul_rn(y, s[0]));
+      }
+    }
+  }
+  const int64_t row = kv_row(p.cache, p.pages, p.seq[token], slot, head);
+  const int64_t safe = row < 0 ? 0 : row;
+  uint8_t* codes = (is_v ? p.cache.v : p.cache.k) + safe * kv_row_bytes(KIND, DIM);
+  uint8_t* scale = static_cast<uint8_t*>(is_v ? p.cache.vs : p.cache.ks) + safe * kv_scale_bytes(KIND, DIM);
+  quantise<KIND, LANES>(x, lane, codes, scale, real && row >= 0);
+  __half* out = is_v ? p.v_out : p.k_out;
+  if (real && out != nullptr) {
+    if (slot < 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = 0.f;
+    }
+    store<true>(out + (token * heads + head) * DIM + at, x);
+  }
+}
+
+// ---- read ---------------------------------------------------------------------------
+
+struct ReadProblem {
+  KvView cache;
+  PageTable pages;
+  const int32_t* lens;
+  int64_t first, count;
+  void *k_out, *v_out;
+};
+
+// A block reads one head of kThreads / (DIM / 8) * kReadRows neighbouring
+// slots, so that it reads whole runs of a page's rows.
+constexpr int kReadRows = 4;
+
+template <int KIND, int DIM, typename TO>
+__global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ ReadProblem p, int64_t tiles) {
+  constexpr int LANES = DIM / 8, ROWS = kThreads / LANES;
+  const int64_t tile = blockIdx.x % tiles;
+  const int seq = (int)(blockIdx.x / tiles);
+  const int heads = p.cache.heads;
+  const bool is_v = (int)blockIdx.y >= heads;
+  const int head = is_v ? blockIdx.y - heads : blockIdx.y;
+  const int lane = threadIdx.x % LANES;
+  const int len = p.lens[seq];
+  const uint8_t* codes = is_v ? p.cache.v : p.cache.k;
+  const uint8_t* scales = static_cast<const uint8_t*>(is_v ? p.cache.vs : p.cache.ks);
+  TO* out = static_cast<TO*>(is_v ? p.v_out : p.k_out);
+  float x[kReadRows][8];
+#pragma unroll
+  for (int i = 0; i < kReadRows; ++i) {
+    const int64_t at = tile * (ROWS * kReadRows) + i * ROWS + threadIdx.x / LANES;
+    const int64_t slot = p.first + at;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
+    if (at < p.count && slot < len) {
+      const int64_t row = kv_row(p.cache, p.pages, seq, (int)slot, head);
+      if (row >= 0)
+        dequantise<KIND>(x[i], lane, codes + row * kv_row_bytes(KIND, DIM), scales + row * kv_scale_bytes(KIND, DIM));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kReadRows; ++i) {
+    const int64_t at = tile * (ROWS * kReadRows) + i * ROWS + threadIdx.x / LANES;
+    if (at < p.count) store<true>(out + ((seq * p.count + at) * heads + head) * DIM + 8 * lane, x[i]);
+  }
+}
+
+// ---- tree masks -----------------------------------------------------------------------
+
+__global__ void __launch_bounds__(kThreads) tree_mask_kernel(const int32_t* parents, int64_t total, int nodes,
+                                                             uint32_t* mask) {
+  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (id >= total) return;
+  const int64_t seq = id / nodes;
+  int node = (int)(id - seq * nodes);
+  uint64_t bits = 0;
+  for (int step = 0; step < nodes && node >= 0 && node < nodes; ++step) {
+    bits |= 1ull << node;
+    node = parents[seq * nodes + node];
+  }
+  const int words = (nodes + 31) / 32;
+  for (int w = 0; w < words; ++w) mask[id * words + w] = (uint32_t)(bits >> (32 * w));
+}
+
+// ---- host ------------------------------------------------------------------------------
+
+int fail(int code, const char* who, const std::string& msg) { return set_error(code, std::string(who) + ": " + msg); }
+
+int launched(const char* who) {
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess)
+    return fail(AF1_ERR_CUDA, who, std::string(cudaGetErrorName(e)) + " (" + cudaGetErrorString(e) + ")");
+  set_error(AF1_OK, "");
+  return AF1_OK;
+}
+
+int current_device(const char* who, int* dev) {
+  const cudaError_t e = cudaGetDevice(dev);
+  if (e != cudaSuccess) return fail(AF1_ERR_CUDA, who, cudaGetErrorString(e));
+  return AF1_OK;
+}
+
+int check_table(const char* who, const float* table, int64_t length, int64_t rope_dim, int64_t dim, int dev) {
+  if (rope_dim < 2 || rope_dim % 2 != 0 || rope_dim > dim)
+    return fail(AF1_ERR_INVALID_ARG, who, "rope_dim must be even, at least 2 and at most the head's size");
+  if (length < 1 || length > (1 << 24)) return fail(AF1_ERR_INVALID_ARG, who, "length must be 1..2^24");
+  int rc = check_pointer(table, "table", dev);
+  if (rc == AF1_OK) rc = check_align(table, 8, "table");
+  return rc;
+}
+
+// Entries between the first and the last that a tensor's strides reach, as a bound for the 2^62 of its offsets.
+bool span_ok(int64_t n, int64_t stride) { return stride >= 0 && (n <= 1 || stride <= ((int64_t)1 << 60) / n); }
+
+template <typename F>
+int with_kind(int kind, F&& f) {
+  switch (kind) {
+    case AF1_KV_F16: return f(std::integral_constant<int, AF1_KV_F16>());
+    case AF1_KV_INT8: return f(std::integral_constant<int, AF1_KV_INT8>());
+    case AF1_KV_E4M3: return f(std::integral_constant<int, AF1_KV_E4M3>());
+    default: return f(std::integral_constant<int, AF1_KV_INT4>());
+  }
+}
+template <typename F>
+int with_bool(bool b, F&& f) {
+  return b ? f(std::true_type()) : f(std::false_type());
+}
+
+}  // namespace
+
+int check_pointer(const void* p, const char* name, int device) {
+  if (p == nullptr) return set_error(AF1_ERR_INVALID_ARG, std::string(name) + " is NULL");
+  cudaPointerAttributes at;
+  const cudaError_t e = cudaPointerGetAttributes(&at, p);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return set_error(AF1_ERR_BAD_POINTER, std::string(name) + " is not a CUDA pointer");
+  }
+  if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged)
+    return set_error(AF1_ERR_BAD_POINTER, std::string(name) + " is not device memory");
+  if (at.type == cudaMemoryTypeDevice && at.device != device)
+    return set_error(AF1_ERR_BAD_POINTER, std::string(name) + " lives on another device");
+  return AF1_OK;
+}
+
+int check_align(const void* p, int bytes, const char* name) {
+  if ((uintptr_t)p % bytes != 0)
+    return set_error(AF1_ERR_MISALIGNED, std::string(name) + " must be " + std::to_string(bytes) + "-byte aligned");
+  return AF1_OK;
+}
+
+KvView view_of(const af1_kv_desc& d) {
+  int shift = 0;
+  while ((1 << shift) < d.page_size) ++shift;
+  return {static_cast<uint8_t*>(d.k), static_cast<uint8_t*>(d.v), d.k_scale, d.v_scale, (int)d.pages, d.kv_heads, shift};
+}
+
+}  // namespace af1
+
+using namespace af1;
+
+int af1_rope_frequencies(const af1_rope_params* p, double* freq, double* attention) {
+  const char* who = "af1_rope_frequencies";
+  if (p == nullptr || freq == nullptr || attention == nullptr)
+    return fail(AF1_ERR_INVALID_ARG, who, "params, freq or attention is NULL");
+  if (p->length < 1 || p->length > (1 << 24)) return fail(AF1_ERR_INVALID_ARG, who, "length must be 1..2^24");
+  if (p->dim < 2 || p->dim > 256 || p->dim % 2 != 0)
+    return fail(AF1_ERR_INVALID_ARG, who, "dim must be even and 2..256");
+  if (p->scaling < AF1_ROPE_PLAIN || p->scaling > AF1_ROPE_RAMP) return fail(AF1_ERR_INVALID_ARG, who, "unknown scaling");
+  if (!(p->base > 1.0) || !std::isfinite(p->base)) return fail(AF1_ERR_INVALID_ARG, who, "base must be above 1");
+  const bool scaled = p->scaling != AF1_ROPE_PLAIN;
+  if (scaled && (!(p->factor >= 1.0) || !std::isfinite(p->factor)))
+    return fail(AF1_ERR_INVALID_ARG, who, "factor must be at least 1");
+  if (!(p->attention >= 0.0) || !std::isfinite(p->attention))
+    return fail(AF1_ERR_INVALID_ARG, who, "attention must be 0 or above");
+  if (p->scaling == AF1_ROPE_BANDS || p->scaling == AF1_ROPE_RAMP) {
+    if (!(p->original > 0.0) || !std::isfinite(p->original))
+      return fail(AF1_ERR_INVALID_ARG, who, "original must be positive");
+    if (!(p->low > 0.0) || !(p->high > p->low) || !std::isfinite(p->high))
+      return fail(AF1_ERR_INVALID_ARG, who, "need 0 < low < high");
+  }
+  if (p->scaling == AF1_ROPE_BASE && p->dim == 2)
+    return fail(AF1_ERR_INVALID_ARG, who, "AF1_ROPE_BASE needs dim above 2");
+  const double kPi = 3.14159265358979323846;
+  const int half = p->dim / 2;
+  double base = p->base;
+  if (p->scaling == AF1_ROPE_BASE) base *= std::pow(p->factor, (double)p->dim / (p->dim - 2));
+  double i0 = 0.0, i1 = 0.0;
+  if (p->scaling == AF1_ROPE_RAMP) {
+    auto e = [&](double beta) { return p->dim * std::log(p->original / (2.0 * kPi * beta)) / (2.0 * std::log(base)); };
+    i0 = std::fmax(0.0, std::floor(e(p->high)));
+    i1 = std::fmin(p->dim - 1.0, std::ceil(e(p->low)));
+  }
+  for (int i = 0; i < half; ++i) {
+    double f = std::pow(base, -2.0 * i / p->dim);
+    if (p->scaling == AF1_ROPE_LINEAR) {
+      f /= p->factor;
+    } else if (p->scaling == AF1_ROPE_BANDS) {
+      const double w = 2.0 * kPi / f;
+      if (w > p->original / p->low) {
+        f /= p->factor;
+      } else if (w >= p->original / p->high) {
+        const double g = (p->original / w - p->low) / (p->high - p->low);
+        f = (1.0 - g) * f / p->factor + g * f;
+      }
+    } else if (p->scaling == AF1_ROPE_RAMP) {
+      const double span = i1 > i0 ? i1 - i0 : 1e-3;
+      const double g = std::fmin(1.0, std::fmax(0.0, (i - i0) / span));
+      f = (1.0 - g) * f + g * f / p->factor;
+    }
+    freq[i] = f;
+  }
+  *attention = p->attention > 0.0 ? p->attention : p->scaling == AF1_ROPE_RAMP ? 0.1 * std::log(p->factor) + 1.0 : 1.0;
+  set_error(AF1_OK, "");
+  return AF1_OK;
+}
+
+int af1_rope_table(const af1_rope_params* params, float* table, void* stream) {
+  RopeFreq f = {};
+  int rc = af1_rope_frequencies(params, f.f, &f.attention);
+  if (rc != AF1_OK) return rc;
+  int dev;
+  if ((rc = current_device("af1_rope_table", &dev)) != AF1_OK) return rc;
+  if ((rc = check_pointer(table, "table", dev)) != AF1_OK || (rc = check_align(table, 8, "table")) != AF1_OK) return rc;
+  f.length = params->length;
+  f.half = params->dim / 2;
+  const int64_t blocks = (f.length * f.half + kThreads - 1) / kThreads;
+  rope_table_kernel<<<(unsigned)blocks, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(
+      f, reinterpret_cast<float2*>(table));
+  return launched("af1_rope_table");
+}
+
+int af1_rope(const af1_rope_args* a, void* stream) {
+  const char* who = "af1_rope";
+  if (a == nullptr) return fail(AF1_ERR_INVALID_ARG, who, "args is NULL");
+  if (a->tokens < 0 || a->heads < 1 || a->dim < 2 || a->dim > 1024 || a->dim % 2 != 0 || a->heads > 65536 ||
+      a->tokens > (1ll << 31))
+    return fail(AF1_ERR_INVALID_ARG, who, "need tokens 0..2^31, heads 1..65536, dim even and 2..1024");
+  if (a->dtype != AF1_F16 && a->dtype != AF1_F32) return fail(AF1_ERR_INVALID_ARG, who, "dtype must be AF1_F16 or AF1_F32");
+  if ((a->flags & ~(AF1_ROPE_INTERLEAVED | AF1_ROPE_BACKWARD)) != 0) return fail(AF1_ERR_INVALID_ARG, who, "unknown flags");
+  if (!span_ok(a->tokens, a->x_token) || !span_ok(a->heads, a->x_head) || !span_ok(a->tokens, a->y_token) ||
+      !span_ok(a->heads, a->y_head))
+    return fail(AF1_ERR_INVALID_ARG, who, "strides must not be negative");
+  if (a->x == a->y && (a->x_token != a->y_token || a->x_head != a->y_head))
+    return fail(AF1_ERR_INVALID_ARG, who, "in place, the strides of x and y must be equal");
+  if (a->tokens == 0) return AF1_OK;
+  int dev, rc;
+  if ((rc = current_device(who, &dev)) != AF1_OK) return rc;
+  if ((rc = check_table(who, a->table, a->length, a->rope_dim, a->dim, dev)) != AF1_OK) return rc;
+  if ((rc = check_pointer(a->x, "x", dev)) != AF1_OK || (rc = check_pointer(a->y, "y", dev)) != AF1_OK ||
+      (rc = check_pointer(a->positions, "positions", dev)) != AF1_OK)
+    return rc;
+  const size_t es = a->dtype == AF1_F16 ? 2 : 4;
+  if ((rc = check_align(a->x, (int)es, "x")) != AF1_OK || (rc = check_align(a->y, (int)es, "y")) != AF1_OK ||
+      (rc = check_align(a->positions, 4, "positions")) != AF1_OK)
+    return rc;
+  const bool il = (a->flags & AF1_ROPE_INTERLEAVED) != 0;
+  RopeProblem p = {a->x, a->y, a->positions, nullptr, a->table, a->length, a->x_token, a->x_head, a->y_token, a->y_head};
+  p.heads = (int)a->heads;
+  p.back = (a->flags & AF1_ROPE_BACKWARD) != 0;
+  const bool vec = plan_rope(p, a->tokens, (int)a->dim, (int)a->rope_dim, es, es, il);
+  const int64_t blocks = (p.total + kThreads - 1) / kThreads;
+  if (blocks > 0x7fffffff) return fail(AF1_ERR_INVALID_ARG, who, "too many entries for one call");
+  return with_bool(vec, [&](auto v) {
+    return with_bool(il, [&](auto i) {
+      return with_bool(a->dtype == AF1_F16, [&](auto h) {
+        using T = std::conditional_t<decltype(h)::value, __half, float>;
+        rope_kernel<T, decltype(v)::value ? 4 : 1, decltype(i)::value>
+            <<<(unsigned)blocks, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
+        return launched(who);
+      });
+    });
+  });
+}
+
+int af1_kv_create(const af1_kv_desc* d, af1_kv_cache** out) {
+  const char* who = "af1_kv_create";
+  if (out == nullptr) return fail(AF1_ERR_INVALID_ARG, who, "out is NULL");
+  *out = nullptr;
+  if (d == nullptr) return fail(AF1_ERR_INVALID_ARG, who, "desc is NULL");
+  if (d->kind < AF1_KV_F16 || d->kind > AF1_KV_INT4) return fail(AF1_ERR_INVALID_ARG, who, "unknown kind");
+  if (d->pages < 1 || d->pages > 0x7fffffff) return fail(AF1_ERR_INVALID_ARG, who, "pages must be 1..2^31 - 1");
+  if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1)) != 0)
+    return fail(AF1_ERR_INVALID_ARG, who, "page_size must be 16, 32, 64, 128 or 256");
+  if (d->kv_heads < 1 || d->kv_heads > 1024) return fail(AF1_ERR_INVALID_ARG, who, "kv_heads must be 1..1024");
+  if (d->head_dim != 64 && d->head_dim != 128) return fail(AF1_ERR_INVALID_ARG, who, "head_dim must be 64 or 128");
+  const bool scaled = d->kind != AF1_KV_F16;
+  if (scaled != (d->k_scale != nullptr) || scaled != (d->v_scale != nullptr))
+    return fail(AF1_ERR_INVALID_ARG, who, "k_scale and v_scale go with INT8, E4M3 and INT4, and only with these");
+  int dev, rc;
+  if ((rc = current_device(who, &dev)) != AF1_OK) return rc;
+  const void* ptrs[4] = {d->k, d->v, d->k_scale, d->v_scale};
+  const char* names[4] = {"k", "v", "k_scale", "v_scale"};
+  for (int i = 0; i < (scaled ? 4 : 2); ++i)
+    if ((rc = check_pointer(ptrs[i], names[i], dev)) != AF1_OK || (rc = check_align(ptrs[i], 16, names[i])) != AF1_OK)
+      return rc;
+  int sms = 0, smem = 0;
+  cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
+  if (e != cudaSuccess) return fail(AF1_ERR_CUDA, who, cudaGetErrorString(e));
+  af1_kv_cache* c = new (std::nothrow) af1_kv_cache();
+  if (c == nullptr) return fail(AF1_ERR_CUDA, who, "host allocation failed");
+  c->d = *d;
+  c->device = dev;
+  c->num_sms = sms;
+  c->max_smem = smem;
+  *out = c;
+  set_error(AF1_OK, "");
+  return AF1_OK;
+}
+
+void af1_kv_free(af1_kv_cache* cache) { delete cache; }
+
+namespace {
+
+int check_pages(const char* who, const af1_kv_cache* c, const int32_t* pages, int64_t sequences, int64_t columns,
+                int64_t ld, int dev) {
+  if (sequences > 65536 || columns < 1 || ld < columns || columns > ((int64_t)1 << 31) / c->d.page_size - 1 ||
+      !span_ok(sequences, ld))
+    return fail(AF1_ERR_INVALID_ARG, who,
+                "need at most 65536 sequences, page columns of fewer than 2^31 slots in all, pages_ld >= page_columns");
+  int rc = check_pointer(pages, "pages", dev);
+  if (rc == AF1_OK) rc = check_align(pages, 4, "pages");
+  return rc;
+}
+
+int check_cache(const char* who, const af1_kv_cache* c, int* dev) {
+  if (c == nullptr) return fail(AF1_ERR_INVALID_ARG, who, "cache is NULL");
+  int rc = current_device(who, dev);
+  if (rc != AF1_OK) return rc;
+  if (*dev != c->device) return fail(AF1_ERR_BAD_POINTER, who, "the current device is not the cache's device");
+  return AF1_OK;
+}
+
+}  // namespace
+
+int af1_kv_append(const af1_kv_cache* c, const af1_kv_append_args* a, void* stream) {
+  const char* who = "af1_kv_append";
+  int dev, rc;
+  if (a == nullptr) return fail(AF1_ERR_INVALID_ARG, who, "args is NULL");
+  if ((rc = check_cache(who, c, &dev)) != AF1_OK) return rc;
+  if (a->tokens < 0 || a->tokens > ((int64_t)1 << 31) || a->sequences < 0)
+    return fail(AF1_ERR_INVALID_ARG, who, "need tokens 0..2^31 and sequences >= 0");
+  if (a->dtype != AF1_F16 && a->dtype != AF1_F32) return fail(AF1_ERR_INVALID_ARG, who, "dtype must be AF1_F16 or AF1_F32");
+  if ((a->flags & ~AF1_ROPE_INTERLEAVED) != 0) return fail(AF1_ERR_INVALID_ARG, who, "unknown flags");
+  const int heads = c->d.kv_heads, dim = c->d.head_dim;
+  if (!span_ok(a->tokens, a->k_token) || !span_ok(heads, a->k_head) || !span_ok(a->tokens, a->v_token) ||
+      !span_ok(heads, a->v_head))
+    return fail(AF1_ERR_INVALID_ARG, who, "strides must not be negative");
+  if ((a->q == nullptr) != (a->q_out == nullptr)) return fail(AF1_ERR_INVALID_ARG, who, "q and q_out go together");
+  const bool has_q = a->q != nullptr;
+  if (has_q && (a->q_heads < 1 || a->q_heads > 65536 || !span_ok(a->tokens, a->q_token) ||
+                !span_ok(a->q_heads, a->q_head) || !span_ok(a->tokens, a->qo_token) || !span_ok(a->q_heads, a->qo_head)))
+    return fail(AF1_ERR_INVALID_ARG, who, "q_heads must be 1..65536 and strides not negative");
+  if (has_q && a->q == a->q_out &&
+      (a->dtype != AF1_F16 || a->q_token != a->qo_token || a->q_head != a->qo_head))
+    return fail(AF1_ERR_INVALID_ARG, who, "in place, q must be FP16 and the strides of q and q_out equal");
+  if (a->tokens == 0) return AF1_OK;
+  const bool rope = a->table != nullptr;
+  if (rope && (rc = check_table(who, a->table, a->length, a->rope_dim, dim, dev)) != AF1_OK) return rc;
+  if ((rc = check_pages(who, c, a->pages, a->sequences, a->page_columns, a->pages_ld, dev)) != AF1_OK) return rc;
+  const int es = a->dtype == AF1_F16 ? 2 : 4;
+  struct {
+    const void* p;
+    const char* name;
+    int align;
+    bool need;
+  } ptrs[] = {{a->k, "k", es, true},          {a->v, "v", es, true},
+              {a->seq, "seq", 4, true},       {a->slot, "slot", 4, true},
+              {a->positions, "positions", 4, false}, {a->q, "q", es, false},
+              {a->q_out, "q_out", 2, false},  {a->k_out, "k_out", 16, false},
+              {a->v_out, "v_out", 16, false}};
+  for (const auto& t : ptrs) {
+    if (t.p == nullptr && !t.need) continue;
+    if ((rc = check_pointer(t.p, t.name, dev)) != AF1_OK || (rc = check_align(t.p, t.align, t.name)) != AF1_OK) return rc;
+  }
+  const bool il = (a->flags & AF1_ROPE_INTERLEAVED) != 0;
+  AppendProblem p = {};
+  p.cache = view_of(c->d);
+  p.pages = {a->pages, a->pages_ld, (int)a->sequences, (int)a->page_columns};
+  p.k = a->k, p.v = a->v;
+  p.k_token = a->k_token, p.k_head = a->k_head, p.v_token = a->v_token, p.v_head = a->v_head;
+  p.seq = a->seq, p.slot = a->slot, p.positions = a->positions;
+  p.table = a->table, p.length = a->length;
+  p.k_out = static_cast<__half*>(a->k_out), p.v_out = static_cast<__half*>(a->v_out);
+  p.half = rope ? (int)a->rope_dim / 2 : 0;
+  p.rows = 2 * a->tokens * heads;
+  const int per_block = kThreads / (dim / 8);
+  const int64_t kv_blocks = (p.rows + per_block - 1) / per_block;
+  int64_t q_blocks = 0;
+  // 16-byte reads of k and v, and of their pairs and turns, where sizes and
+  // addresses allow them (for q too, as one variant serves both).
+  auto fits = [&](const void* q, int64_t s, int64_t t) {
+    return (uintptr_t)q % 16 == 0 && s * es % 16 == 0 && t * es % 16 == 0;
+  };
+  bool vec = fits(a->k, a->k_token, a->k_head) && fits(a->v, a->v_token, a->v_head) &&
+             (!rope || ((uintptr_t)a->table % 16 == 0 && a->rope_dim % 16 == 0));
+  if (has_q) {
+    p.q.x = a->q, p.q.y = a->q_out;
+    p.q.positions = a->positions != nullptr ? a->positions : a->slot;
+    p.q.slot = a->slot;
+    p.q.table = a->table, p.q.length = a->length;
+    p.q.x_token = a->q_token, p.q.x_head = a->q_head, p.q.y_token = a->qo_token, p.q.y_head = a->qo_head;
+    p.q.heads = (int)a->q_heads;
+    vec = plan_rope(p.q, a->tokens, dim, 2 * p.half, es, 2, il, vec);
+    q_blocks = (p.q.total + kThreads - 1) / kThreads;
+  }
+  if (kv_blocks + q_blocks > 0x7fffffff) return fail(AF1_ERR_INVALID_ARG, who, "too many entries for one call");
+  p.kv_blocks = (int)kv_blocks;
+  return with_kind(c->d.kind, [&](auto kind) {
+    return with_bool(dim == 128, [&](auto wide) {
+      return with_bool(a->dtype == AF1_F16, [&](auto h) {
+        return with_bool(vec, [&](auto v) {
+          return with_bool(il, [&](auto i) {
+            using T = std::conditional_t<decltype(h)::value, __half, float>;
+            append_kernel<decltype(kind)::value, decltype(wide)::value ? 128 : 64, T, decltype(v)::value,
+                          decltype(i)::value>
+                <<<(unsigned)(kv_blocks + q_blocks), kThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
+            return launched(who);
+          });
+        });
+      });
+    });
+  });
+}
+
+int af1_kv_read(const af1_kv_cache* c, const int32_t* pages, int64_t sequences, int64_t page_columns, int64_t pages_ld,
+                const int32_t* lens, int64_t first, int64_t count, void* k_out, void* v_out, int dtype, void* stream) {
+  const char* who = "af1_kv_read";
+  int dev, rc;
+  if ((rc = check_cache(who, c, &dev)) != AF1_OK) return rc;
+  if (sequences < 0 || first < 0 || count < 0 || first > 0x7fffffff || count > 0x7fffffff)
+    return fail(AF1_ERR_INVALID_ARG, who, "need sequences, first and count from 0 to 2^31 - 1");
+  if (dtype != AF1_F16 && dtype != AF1_F32) return fail(AF1_ERR_INVALID_ARG, who, "dtype must be AF1_F16 or AF1_F32");
+  if (sequences == 0 || count == 0) return AF1_OK;
+  if ((rc = check_pages(who, c, pages, sequences, page_columns, pages_ld, dev)) != AF1_OK) return rc;
+  if ((rc = check_pointer(lens, "lens", dev)) != AF1_OK || (rc = check_align(lens, 4, "lens")) != AF1_OK ||
+      (rc = check_pointer(k_out, "k_out", dev)) != AF1_OK || (rc = check_align(k_out, 16, "k_out")) != AF1_OK ||
+      (rc = check_pointer(v_out, "v_out", dev)) != AF1_OK || (rc = check_align(v_out, 16, "v_out")) != AF1_OK)
+    return rc;
+  const int dim = c->d.head_dim;
+  const int64_t tile = (int64_t)kThreads / (dim / 8) * kReadRows;
+  const int64_t tiles = (count + tile - 1) / tile;
+  if (tiles * sequences > 0x7fffffff) return fail(AF1_ERR_INVALID_ARG, who, "too many slots for one call");
+  ReadProblem p = {view_of(c->d), {pages, pages_ld, (int)sequences, (int)page_columns}, lens, first, count, k_out, v_out};
+  const dim3 grid((unsigned)(tiles * sequences), 2 * c->d.kv_heads);
+  return with_kind(c->d.kind, [&](auto kind) {
+    return with_bool(dim == 128, [&](auto wide) {
+      return with_bool(dtype == AF1_F16, [&](auto h) {
+        using T = std::conditional_t<decltype(h)::value, __half, float>;
+        read_kernel<decltype(kind)::value, decltype(wide)::value ? 128 : 64, T>
+            <<<grid, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(p, tiles);
+        return launched(who);
+      });
+    });
+  });
+}
+
+int af1_tree_mask(const int32_t* parents, int64_t sequences, int64_t nodes, uint32_t* mask, void* stream) {
+  const char* who = "af1_tree_mask";
+  if (nodes < 1 || nodes > 64 || sequences < 0 || sequences > 65536)
+    return fail(AF1_ERR_INVALID_ARG, who, "need 1..64 nodes and 0..65536 sequences");
+  if (sequences == 0) return AF1_OK;
+  int dev, rc;
+  if ((rc = current_device(who, &dev)) != AF1_OK || (rc = check_pointer(parents, "parents", dev)) != AF1_OK ||
+      (rc = check_align(parents, 4, "parents")) != AF1_OK || (rc = check_pointer(mask, "mask", dev)) != AF1_OK ||
+      (rc = check_align(mask, 4, "mask")) != AF1_OK)
+    return rc;
+  const int64_t total = sequences * nodes;
+  tree_mask_kernel<<<(unsigned)((total + kThreads - 1) / kThreads), kThreads, 0, static_cast<cudaStream_t>(stream)>>>(
+      parents, total, (int)nodes, mask);
+  return launched(who);
+}
