@@ -604,7 +604,8 @@ AF1_API int af1_rope(const af1_rope_args* args, void* stream);
  * with 1 / scale read as 0 where scale is 0, or below 2^-120 for INT8 and
  * E4M3 (scale is then stored as 0). Vectors (INT4: groups) that hold an
  * infinity or a NaN, or whose scale or low is not finite, are stored with
- * codes 0 and scale (and low) NaN. Buffers are 16-byte aligned. */
+ * codes 0 and scale (and low) NaN. Buffers are 16-byte aligned, and hold fewer
+ * than 2^31 vectors. */
 #define AF1_KV_F16 0
 #define AF1_KV_INT8 1
 #define AF1_KV_E4M3 2

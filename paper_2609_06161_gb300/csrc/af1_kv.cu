@@ -10,6 +10,7 @@
 // rounded one by one (no fused multiply-add), as are the steps of the
 // quantiser, so that what a cache holds is a function of the inputs to the
 // bit, whichever launch wrote it.
+#include <cudaTypedefs.h>
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -506,6 +507,28 @@ int check_table(const char* who, const float* table, int64_t length, int64_t rop
 // Entries between the first and the last that a tensor's strides reach, as a bound for the 2^62 of its offsets.
 bool span_ok(int64_t n, int64_t stride) { return stride >= 0 && (n <= 1 || stride <= ((int64_t)1 << 60) / n); }
 
+// Tensor map of `rows` rows of row_bytes bytes: boxes of `box` rows by up to
+// 128 bytes, swizzled by the box's width.
+bool make_row_map(CUtensorMap* map, void* base, int64_t rows, int row_bytes, int box) {
+  static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    return static_cast<PFN_cuTensorMapEncodeTiled_v12000>(nullptr);
+  }();
+  if (fn == nullptr) return false;
+  const int span = std::min(row_bytes, 128);
+  const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)row_bytes};
+  const cuuint32_t boxes[2] = {(cuuint32_t)span, (cuuint32_t)box}, steps[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            span == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+            : span == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                         : CU_TENSOR_MAP_SWIZZLE_32B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename F>
 int with_kind(int kind, F&& f) {
   switch (kind) {
@@ -688,16 +711,24 @@ int af1_kv_create(const af1_kv_desc* d, af1_kv_cache** out) {
   for (int i = 0; i < (scaled ? 4 : 2); ++i)
     if ((rc = check_pointer(ptrs[i], names[i], dev)) != AF1_OK || (rc = check_align(ptrs[i], 16, names[i])) != AF1_OK)
       return rc;
-  int sms = 0, smem = 0;
+  const int64_t rows = d->pages * d->kv_heads * d->page_size;
+  if (rows > 0x7fffffff) return fail(AF1_ERR_INVALID_ARG, who, "pages * kv_heads * page_size must be below 2^31");
+  int sms = 0;
   cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
   if (e != cudaSuccess) return fail(AF1_ERR_CUDA, who, cudaGetErrorString(e));
   af1_kv_cache* c = new (std::nothrow) af1_kv_cache();
   if (c == nullptr) return fail(AF1_ERR_CUDA, who, "host allocation failed");
   c->d = *d;
   c->device = dev;
   c->num_sms = sms;
-  c->max_smem = smem;
+  const int row_bytes = kv_row_bytes(d->kind, d->head_dim);
+  bool ok = make_row_map(&c->k16, d->k, rows, row_bytes, 16) && make_row_map(&c->v16, d->v, rows, row_bytes, 16);
+  if (d->page_size >= 32)
+    ok = ok && make_row_map(&c->k32, d->k, rows, row_bytes, 32) && make_row_map(&c->v32, d->v, rows, row_bytes, 32);
+  if (!ok) {
+    delete c;
+    return fail(AF1_ERR_CUDA, who, "cuTensorMapEncodeTiled failed");
+  }
   *out = c;
   set_error(AF1_OK, "");
   return AF1_OK;

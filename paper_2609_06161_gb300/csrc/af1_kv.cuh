@@ -2,6 +2,7 @@
 // the entry points of the step around the linears share.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -14,7 +15,9 @@ struct af1_kv_cache {
   af1_kv_desc d;
   int device = 0;
   int num_sms = 0;
-  int max_smem = 0;  // opt-in shared memory per block
+  // Tensor maps of k and v as rows of codes, boxes of 16 rows, and of 32
+  // where a page holds as many.
+  CUtensorMap k16, v16, k32, v32;
 };
 
 namespace af1 {

@@ -7,23 +7,39 @@
 // nodes that share a cached head are the rows of one product, so that the
 // cache is read once for all of them.
 //
-// Split. An item is one sequence, one cached head and one block of 16 MT
-// rows; its keys are cut into units, and every CTA takes an equal run of the
-// units of all items (ragged lengths balance by themselves). Inside a CTA
-// each warp takes every eighth step of KW keys of a run, with a ring of its
-// own in shared memory, its own running maximum m and sum l, and an
-// accumulator in registers; warps meet once a run, to join (m, l, o). Where
-// an item spans CTAs, each leaves its part in the workspace and the last one
-// to arrive joins them in order, so that results do not depend on timing.
+// Split. An item is one sequence, one cached head and one block of 8 NT rows;
+// its keys are cut into units of kUnit, and every CTA takes an equal run of
+// the units of all items (ragged lengths balance by themselves). Inside a
+// CTA each warp takes every W-th step of KW keys of a run, with a ring of its
+// own in shared memory that TMA fills, its own running maximum m and sum l,
+// and an accumulator in registers; warps meet once a run, to join (m, l, o).
+// Where an item spans CTAs, each leaves its part in the workspace and the
+// last one to arrive joins them in order, so that results do not depend on
+// timing.
 //
-// Codes become exact FP16 values in registers and go to m16n8k16 products
-// (FP32 accumulators). A contraction may run in any order, so the entries of
-// a key go to the product's k index in the order in which one lane's 16-byte
-// reads give them, and q is laid out to match. The scale of an 8-bit key
-// multiplies the scores, that of an 8-bit value the weights p (relative to
-// the largest one so far, kept apart); 4-bit codes become scale * code + low,
-// rounded once to FP16. p is rounded to FP16 (2^14 times its value, so that
-// weights down to 2^-28 keep 11 bits); m, l, scores and outputs are FP32.
+// Products. Few rows and many keys: the keys are the 16 rows of the products
+// S^T = K Q^T, the entries of a value those of O^T = V^T P^T (m16n8k16, FP32
+// accumulators), and 8 rows of q a column block, so that nothing is computed
+// for rows that do not exist beyond a block of 8. A contraction may run in any
+// order: the entries of a key go to the product's k index in the order in
+// which one lane's reads give them, and q is laid out to match.
+//
+// Codes become exact FP16 values in registers. Those of the keys of INT4 and
+// INT8 (plus 128) go in as the fraction bits of FP16 subnormals, 2^-24 times
+// the code, at one mask or byte permutation for two entries; the 128 and the
+// 2^24 are taken back in the FP32 scores, where 128 sum q is a constant of the
+// row. (A value's 128 would have to be taken back from a sum over all keys, in
+// which it is far larger than the result, so values of INT8 are made signed.)
+// Scales stay in FP32: a key's multiplies its scores (INT4: those of each
+// group of 32 entries, whose lows are contracted with the sums of q over the
+// groups), so that no entry of a key is rounded; a value's multiplies the
+// weights p. Only INT4's values, code * scale + low, are rounded to FP16: with
+// p times the scale in place of p, errors of the two terms would not cancel
+// where they do.
+// p is rounded to FP16, times 2^kShift, relative to a maximum that is moved
+// only when a score passes it by 2^kSlack, and to the largest value scale so
+// far; m, l, scores and outputs are FP32.
+#include <cuda.h>
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -36,15 +52,19 @@
 namespace af1 {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
+constexpr int kUnit = 64;                         // keys of a unit
+constexpr int kMinRun = 256;                      // keys of a CTA, at least (where there are so many)
 constexpr int kMaxCtas = 1024;                    // counters of the workspace
 constexpr int64_t kCounterOffset = 256;           // behind the status word's line
 constexpr int64_t kPartOffset = kCounterOffset + 4 * kMaxCtas;
-constexpr float kShift = 14.f;                    // weights are stored times 2^14
+// Weights are at most 2^(kShift + kSlack) = 2^15 (half of FP16's range), and
+// keep 11 bits down to 2^(-14 - kShift - kSlack) of the largest.
+constexpr float kShift = 7.f, kSlack = 8.f;
 constexpr float kInf = __builtin_huge_valf();
+constexpr float kCode = 16777216.f;               // 2^24: codes as subnormals
 
 struct TreeProblem {
+  CUtensorMap k_map, v_map;
   const __half* q;
   int64_t q_seq, q_node, q_head;
   void* out;
@@ -59,8 +79,10 @@ struct TreeProblem {
   int row_tiles;
   float scale_log2;         // scale * log2(e)
   bool out_f32;
+  unsigned* status;
   unsigned* counters;
   float* parts;
+  long long wait_cycles;
 };
 
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t s) { return __byte_perm(a, b, s); }
@@ -84,6 +106,10 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
 }
+__device__ __forceinline__ float low_float(uint32_t h2) { return __half2float(__ushort_as_half((unsigned short)h2)); }
+__device__ __forceinline__ float high_float(uint32_t h2) {
+  return __half2float(__ushort_as_half((unsigned short)(h2 >> 16)));
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -94,121 +120,121 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t d;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
+  return d;
+}
 __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                : "r"(addr)
                : "memory");
 }
-// 16 bytes of global memory to shared memory, the last 16 - bytes of them zeros.
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+// Bounded wait for a phase of a barrier: false where it gave up.
+__device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, long long budget) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity))
+    if (clock64() - t0 > budget) return false;
+  return true;
 }
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int x, int row, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+          dst),
+      "l"(map), "r"(x), "r"(row), "r"(smem_u32(bar))
+      : "memory");
 }
 
-// What the kernel knows of a kind of cache at compile time.
+// What the kernel knows of a kind of cache at compile time. Shared memory
+// holds the rows of a step as TMA writes them: slices of up to 128 bytes of a
+// row, each slice's rows in order, 16-byte chunks swizzled so that eight
+// neighbouring rows' chunks at one place lie in different banks.
 template <int KIND, int DIM>
 struct Kv {
   static constexpr int RB = kv_row_bytes(KIND, DIM);    // bytes of a row
   static constexpr int SB = kv_scale_bytes(KIND, DIM);  // bytes of its scales
-  static constexpr int CH = RB / 16;                    // 16-byte chunks of a row
-  static constexpr int KW = KIND == AF1_KV_F16 ? 16 : 32;  // keys of a warp's step
+  static constexpr int SPAN = RB < 128 ? RB : 128;      // bytes of a row in one slice
+  static constexpr int SLICES = RB / SPAN;
   static constexpr int KS = DIM / 16;                   // products along a key
-  static constexpr int WORDS = RB / 16;                 // 32-bit words of a key that one lane holds
-  static constexpr int STAGE = 2 * KW * (RB + SB);      // bytes of a step: k, v, k scales, v scales
-  // Byte offset of a chunk of a row in a step's k or v: the chunks of eight
-  // neighbouring rows at one place lie in different banks, and so do those
-  // that eight neighbouring lanes read of a key.
+  static constexpr int MT = DIM / 16;                   // 16-entry blocks of a value
+  static constexpr int GROUPS = KIND == AF1_KV_INT4 ? DIM / 32 : 1;
+  static constexpr bool SCALED8 = KIND == AF1_KV_INT8 || KIND == AF1_KV_E4M3;
+  // Byte offset of a chunk of a row in a step's k or v of KW rows.
+  template <int KW>
   static __device__ __forceinline__ int at(int row, int chunk) {
-    if constexpr (CH >= 8) return row * RB + ((chunk ^ ((row & 1) << 2 | (row >> 1 & 3))) << 4);
-    else if constexpr (CH == 4) return row * RB + ((chunk ^ (row >> 1 & 3)) << 4);
-    else return row * RB + ((chunk ^ (row >> 2 & 1)) << 4);
+    if constexpr (SPAN == 128)
+      return (chunk >> 3) * (KW * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+    else if constexpr (SPAN == 64)
+      return row * 64 + ((chunk ^ (row >> 1 & 3)) << 4);
+    else
+      return row * 32 + ((chunk ^ (row >> 2 & 1)) << 4);
   }
-  // Entry of a key that stands at k index pair (e >> 1), place (e & 1), of
-  // product ks in the lanes with lane % 4 == t.
+  // Entry of a key at place e (0, 1: the low k indices of the lanes with
+  // lane % 4 == t, 2, 3: the high ones) of product ks.
   static __device__ __forceinline__ int entry(int t, int ks, int e) {
-    if constexpr (KIND == AF1_KV_F16) {
-      const int w = 2 * ks + (e >> 1);
-      return 8 * (4 * (w / 4) + t) + 2 * (w % 4) + (e & 1);
-    } else if constexpr (KIND == AF1_KV_INT4) {
-      return (DIM / 4) * t + 8 * (ks >> 1) + 2 * (ks & 1) + (e >> 1) + 4 * (e & 1);
-    } else {
-      return 16 * (4 * (ks / 4) + t) + 4 * (ks % 4) + e;
-    }
+    if constexpr (KIND == AF1_KV_F16) return 64 * (ks >> 2) + 8 * (2 * t + (ks >> 1 & 1)) + 4 * (ks & 1) + e;
+    else if constexpr (KIND == AF1_KV_INT4) return 32 * (ks >> 1) + 8 * t + (ks & 1) + 2 * (e >> 1) + 4 * (e & 1);
+    else if constexpr (DIM == 128) return 16 * (2 * t + (ks >> 2)) + 4 * (ks & 3) + e;
+    else return 16 * t + 4 * ks + e;
   }
-  // Entry of a value that stands in column 2 t + i of output block n.
-  static __device__ __forceinline__ int column(int t, int n, int i) {
-    if constexpr (KIND == AF1_KV_F16) return 8 * n + 2 * t + i;
-    else if constexpr (KIND == AF1_KV_INT4) return 32 * (n / 4) + 8 * t + 4 * i + n % 4;
-    else return 16 * (n / 2) + 4 * t + 2 * i + n % 2;
+  // Entry of a value in row g (hi: g + 8) of its block m.
+  static __device__ __forceinline__ int row_entry(int m, int g, int hi) {
+    if constexpr (KIND == AF1_KV_F16) return 16 * m + g + 8 * hi;
+    else if constexpr (KIND == AF1_KV_INT4) return 32 * (m >> 1) + 4 * g + (m & 1) + 2 * hi;
+    else return 16 * m + 2 * g + hi;
   }
 };
 
-// The words of one key that a lane holds.
-template <typename C>
-__device__ __forceinline__ void load_key(uint32_t (&w)[C::WORDS], const uint8_t* k, int row, int t) {
-  if constexpr (C::CH >= 4) {
-#pragma unroll
-    for (int j = 0; j < C::CH / 4; ++j)
-      *reinterpret_cast<uint4*>(&w[4 * j]) = *reinterpret_cast<const uint4*>(k + C::at(row, 4 * j + t));
-  } else {
-    *reinterpret_cast<uint2*>(&w[0]) = *reinterpret_cast<const uint2*>(k + C::at(row, t / 2) + 8 * (t % 2));
-  }
-}
-
-// b operand of product ks from a lane's words; s2, m2: scale and low of an
-// INT4 group, twice.
+// The a operand of product ks, from the words of keys g and g + 8.
 template <int KIND, int N>
-__device__ __forceinline__ void key_operand(uint32_t& b0, uint32_t& b1, const uint32_t (&w)[N], int ks, uint32_t s2,
-                                            uint32_t m2) {
-  if constexpr (KIND == AF1_KV_F16) {
-    b0 = w[2 * ks], b1 = w[2 * ks + 1];
-  } else if constexpr (KIND == AF1_KV_INT8) {
-    const uint32_t u = w[ks] ^ 0x80808080u;
-    b0 = hsub2(prmt(u, 0x64646464u, 0x4140), 0x64806480u);
-    b1 = hsub2(prmt(u, 0x64646464u, 0x4342), 0x64806480u);
-  } else if constexpr (KIND == AF1_KV_E4M3) {
-    b0 = e4m3x2(w[ks]);
-    b1 = e4m3x2(w[ks] >> 16);
-  } else {
-    const uint32_t u = w[ks >> 1] >> (8 * (ks & 1));
-    b0 = hfma2(hsub2((u & 0x000f000fu) | 0x64006400u, 0x64006400u), s2, m2);
-    b1 = hfma2(hsub2((u >> 4 & 0x000f000fu) | 0x64006400u, 0x64006400u), s2, m2);
+__device__ __forceinline__ void key_operand(uint32_t (&a)[4], const uint32_t (&w)[2][N], int ks) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if constexpr (KIND == AF1_KV_F16) {
+      a[h] = w[h][2 * ks], a[2 + h] = w[h][2 * ks + 1];
+    } else if constexpr (KIND == AF1_KV_INT8) {
+      const uint32_t u = w[h][ks] ^ 0x80808080u;
+      a[h] = prmt(u, 0, 0x4140), a[2 + h] = prmt(u, 0, 0x4342);
+    } else if constexpr (KIND == AF1_KV_E4M3) {
+      a[h] = e4m3x2(w[h][ks]), a[2 + h] = e4m3x2(w[h][ks] >> 16);
+    } else {
+      const uint32_t u = w[h][ks >> 1];
+      const int b = 4 * (ks & 1);
+      a[h] = u >> b & 0x000f000fu, a[2 + h] = u >> (8 + b) & 0x000f000fu;
+    }
   }
 }
 
-// b operand of output block i of a chunk, from a transposed 16-bit word of
-// two keys; s2, m2: scale and low of the two keys (INT4).
-template <int KIND>
-__device__ __forceinline__ uint32_t value_operand(uint32_t r, int i, uint32_t s2, uint32_t m2) {
-  if constexpr (KIND == AF1_KV_F16) {
-    return r;
-  } else if constexpr (KIND == AF1_KV_INT8) {
-    return hsub2(prmt(r ^ 0x80808080u, 0x64646464u, i == 0 ? 0x4240 : 0x4341), 0x64806480u);
-  } else if constexpr (KIND == AF1_KV_E4M3) {
-    return e4m3x2(prmt(r, r, i == 0 ? 0x0020 : 0x0031));
+// The words of one key that a lane holds.
+template <typename C, int KIND, int KW, int N>
+__device__ __forceinline__ void load_key(uint32_t (&w)[N], const uint8_t* k, int row, int t) {
+  if constexpr (KIND == AF1_KV_INT4) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) w[c] = *reinterpret_cast<const uint32_t*>(k + C::template at<KW>(row, c) + 4 * t);
   } else {
-    return hfma2(hsub2((r >> (4 * i) & 0x000f000fu) | 0x64006400u, 0x64006400u), s2, m2);
+    constexpr int J = C::SPAN / 64;  // chunks of a slice that a lane holds
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+      *reinterpret_cast<uint4*>(&w[4 * i]) =
+          *reinterpret_cast<const uint4*>(k + C::template at<KW>(row, 8 * (i / J) + J * t + i % J));
   }
 }
 
-// One entry of a value in a step's buffers (scaled by its own scale for
-// INT4, as the code alone for INT8 and E4M3).
-template <int KIND, int DIM>
+// One entry of a value in a step's buffers (scaled for INT4, the code alone
+// for INT8 and E4M3).
+template <int KIND, int DIM, int KW>
 __device__ __forceinline__ float value_entry(const uint8_t* v, const uint8_t* vs, int row, int e) {
   using C = Kv<KIND, DIM>;
   if constexpr (KIND == AF1_KV_F16) {
-    return __half2float(*reinterpret_cast<const __half*>(v + C::at(row, e / 8) + 2 * (e % 8)));
+    return __half2float(*reinterpret_cast<const __half*>(v + C::template at<KW>(row, e / 8) + 2 * (e % 8)));
   } else if constexpr (KIND == AF1_KV_INT4) {
-    const uint8_t byte = v[C::at(row, e / 32) + (e % 32) / 2];
-    const __half2 s = reinterpret_cast<const __half2*>(vs)[row * (DIM / 32) + e / 32];
-    return __half2float(__hfma(__int2half_rn(e % 2 ? byte >> 4 : byte & 15), __low2half(s), __high2half(s)));
+    const uint8_t byte = v[C::template at<KW>(row, e / 32) + (e % 32) / 2];
+    const uint32_t s = reinterpret_cast<const uint32_t*>(vs)[row * (DIM / 32) + e / 32];
+    return fmaf((float)(e % 2 ? byte >> 4 : byte & 15), low_float(s), high_float(s));
   } else {
-    const uint8_t byte = v[C::at(row, e / 16) + e % 16];
+    const uint8_t byte = v[C::template at<KW>(row, e / 16) + e % 16];
     if constexpr (KIND == AF1_KV_INT8) return (float)(int8_t)byte;
     else return __half2float(__half(__nv_cvt_fp8_to_halfraw(byte, __NV_E4M3)));
   }
@@ -216,18 +242,18 @@ __device__ __forceinline__ float value_entry(const uint8_t* v, const uint8_t* vs
 
 // Whether part `part` of `parts` of a value's row holds an infinity or a NaN
 // (its 8-bit scale apart).
-template <int KIND, int DIM>
+template <int KIND, int DIM, int KW>
 __device__ __forceinline__ bool value_bad(const uint8_t* v, const uint8_t* vs, int row, int part, int parts) {
   using C = Kv<KIND, DIM>;
   bool bad = false;
   if constexpr (KIND == AF1_KV_INT4) {
     for (int i = part; i < DIM / 32; i += parts) {
       const uint32_t s = reinterpret_cast<const uint32_t*>(vs)[row * (DIM / 32) + i];
-      bad |= (s & 0x7c00u) == 0x7c00u || (s & 0x7c000000u) == 0x7c000000u;
+      bad |= !(15.f * fabsf(low_float(s)) + fabsf(high_float(s)) <= 65504.f);
     }
   } else if constexpr (KIND != AF1_KV_INT8) {
-    for (int i = part; i < C::CH; i += parts) {
-      const uint4 c = *reinterpret_cast<const uint4*>(v + C::at(row, i));
+    for (int i = part; i < C::RB / 16; i += parts) {
+      const uint4 c = *reinterpret_cast<const uint4*>(v + C::template at<KW>(row, i));
       const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -241,283 +267,350 @@ __device__ __forceinline__ bool value_bad(const uint8_t* v, const uint8_t* vs, i
   return bad;
 }
 
-struct Run {  // a CTA's run of units within one item
-  int seq, head, tile;
-  int u0, u1, units;  // units u0 .. u1 - 1 of the item's `units`
-  int len, keys;      // cached tokens, and keys with the nodes'
-  int64_t first;      // the item's first unit in the order of all items
+// 32 sequences at a time, one to a lane: their lengths, and their units (of
+// one cached head and row block) summed up. An item without keys has one
+// unit, that writes its zeros.
+struct Sequences {
+  int first;      // of the 32
+  int64_t before; // units of the sequences before them
+  int len, keys, units, sum;
+
+  __device__ __forceinline__ void load(const TreeProblem& p, int at, int64_t units_before) {
+    const int lane = threadIdx.x % 32, i = at + lane;
+    first = at;
+    before = units_before;
+    len = keys = units = 0;
+    if (i < p.pages.seqs) {
+      len = max(p.lens[i], 0);
+      const int count = p.counts == nullptr ? p.nodes : min(max(p.counts[i], 0), p.nodes);
+      keys = (int)min((int64_t)len + count, (int64_t)p.pages.columns << p.cache.shift);
+      units = max(1, (keys + kUnit - 1) / kUnit);
+    }
+    sum = units;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int other = __shfl_up_sync(0xffffffffu, sum, d);
+      if (lane >= d) sum += other;
+    }
+  }
+  __device__ __forceinline__ int64_t after() const { return before + __shfl_sync(0xffffffffu, sum, 31); }
 };
 
-__device__ __forceinline__ int node_count(const TreeProblem& p, int seq) {
-  return p.counts == nullptr ? p.nodes : min(max(p.counts[seq], 0), p.nodes);
-}
-
-// Prefix sums over sequences of units (of one cached head and row tile), by
-// the whole CTA. An item without keys has one unit, that writes its zeros.
-__device__ __forceinline__ int64_t scan_units(const TreeProblem& p, int unit, int64_t* prefix, int64_t* scratch) {
-  const int per = (p.pages.seqs + kThreads - 1) / kThreads;
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const int first = threadIdx.x * per;
-  const int cap = p.pages.columns << p.cache.shift;
-  int64_t sum = 0;
-  for (int i = first; i < min(first + per, p.pages.seqs); ++i) {
-    const int keys = (int)min((int64_t)max(p.lens[i], 0) + node_count(p, i), (int64_t)cap);
-    sum += max(1, (keys + unit - 1) / unit);
-    prefix[i + 1] = sum;
-  }
-  int64_t up = sum;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int64_t other = __shfl_up_sync(0xffffffffu, up, d);
-    if (lane >= d) up += other;
-  }
-  if (lane == 31) scratch[warp] = up;
-  __syncthreads();
-  int64_t before = up - sum, total = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before += scratch[w];
-    total += scratch[w];
-  }
-  for (int i = first; i < min(first + per, p.pages.seqs); ++i) prefix[i + 1] += before;
-  if (threadIdx.x == 0) prefix[0] = 0;
-  __syncthreads();
-  return total;
-}
-
-template <int KIND, int DIM, int MT, int STAGES>
-__global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant__ TreeProblem p) {
+template <int KIND, int DIM, int NT, int W, int KW, int STAGES>
+struct Shape {
   using C = Kv<KIND, DIM>;
-  constexpr int KW = C::KW, NB = KW / 8, KS = C::KS, ON = DIM / 8, ROWS = 16 * MT;
-  constexpr int PART = ROWS * (DIM + 2);  // floats of a part: o, m, l
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int64_t scratch[kWarps];
-  __shared__ uint8_t bad_pages[kWarps][STAGES];
-  __shared__ float join_m[kWarps][ROWS], join_l[kWarps][ROWS];
+  static constexpr int ROWS = 8 * NT;
+  static constexpr int RING = W * STAGES * 2 * KW * C::RB;    // k and v of every stage of every warp
+  static constexpr int SCALES = W * STAGES * 2 * KW * C::SB;
+  static constexpr int JOIN = W * ROWS * DIM * 4;             // the warps' o, over the ring
+  static constexpr int QS = NT > 2 ? NT * C::KS * 32 * 8 : 0;  // q's operands where registers do not hold them
+  static constexpr int SMEM = RING + SCALES + QS + 1024;
+  static constexpr int PART = ROWS * (DIM + 2);               // floats of a part: o, m, l
+  static_assert(JOIN <= RING, "the warps' outputs are joined over their rings");
+  static_assert((KW * C::RB) % 512 == 0, "a stage keeps the swizzle's alignment");
+};
+
+template <int KIND, int DIM, int NT, int W, int KW, int STAGES>
+__global__ void __launch_bounds__(32 * W, 1) tree_kernel(const __grid_constant__ TreeProblem p) {
+  using C = Kv<KIND, DIM>;
+  using S = Shape<KIND, DIM, NT, W, KW, STAGES>;
+  constexpr int KS = C::KS, MT = C::MT, MB = KW / 16, ROWS = S::ROWS, GROUPS = C::GROUPS;
+  constexpr int WORDS = C::RB / 16;        // 32-bit words of a key that one lane holds
+  constexpr int STAGE = 2 * KW * C::RB;    // bytes of a step's k and v
+  constexpr bool INT4 = KIND == AF1_KV_INT4;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t bars[W][STAGES];
+  __shared__ float join_m[W][ROWS], join_l[W][ROWS];
   __shared__ bool last_shared;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int g = lane / 4, t = lane % 4;
-  uint8_t* ring = smem + warp * (STAGES * C::STAGE);
-  const uint32_t ring_u32 = smem_u32(ring);
-  uint32_t* qs = reinterpret_cast<uint32_t*>(smem + kWarps * STAGES * C::STAGE);  // MT > 1: q's operands
-  int64_t* prefix = reinterpret_cast<int64_t*>(smem + kWarps * STAGES * C::STAGE + (MT > 1 ? MT * KS * 512 : 0));
-  float* join = reinterpret_cast<float*>(smem);  // after a run: the warps' o
+  uint8_t* ring = smem + warp * (STAGES * STAGE);
+  uint8_t* ring_scales = smem + S::RING + warp * (STAGES * 2 * KW * C::SB);
+  uint2* qs = reinterpret_cast<uint2*>(smem + S::RING + S::SCALES);
+  float* join = reinterpret_cast<float*>(smem);
 
-  // Units of 8 steps, or fewer where that would leave CTAs without work.
-  int unit = KW * kWarps;
-  const int64_t lanes = (int64_t)p.cache.heads * p.row_tiles;
-  int64_t per_head = scan_units(p, unit, prefix, scratch);
-  while (per_head * lanes < gridDim.x && unit > 2 * KW) {
-    unit /= 2;
-    per_head = scan_units(p, unit, prefix, scratch);
+  if (lane == 0) {
+    for (int i = 0; i < STAGES; ++i) mbar_init(&bars[warp][i], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  const int64_t total = per_head * lanes;
-  const int64_t ctas = min((int64_t)gridDim.x, total);  // each has a unit at least
+  __syncwarp();
+
+  // This CTA's units: begin .. end - 1 of all items'.
+  const int64_t lanes = (int64_t)p.cache.heads * p.row_tiles;
+  Sequences sq;
+  sq.load(p, 0, 0);
+  int64_t total = sq.after();
+  for (int at = 32; at < p.pages.seqs; at += 32) {
+    sq.load(p, at, total);
+    total = sq.after();
+  }
+  if (p.pages.seqs > 32) sq.load(p, 0, 0);
+  total *= lanes;
+  int64_t ctas = min((int64_t)gridDim.x, (total * kUnit + kMinRun - 1) / kMinRun);
+  ctas = min(ctas, total);  // each has a unit at least
   if (blockIdx.x >= ctas) return;
   const int64_t begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
 
-  int64_t pos = begin;
-  int seq = 0;
-  {
-    int hi = p.pages.seqs;  // the last sequence whose first unit is not after pos
-    while (hi - seq > 1) {
-      const int mid = (seq + hi) / 2;
-      if (prefix[mid] * lanes <= pos) seq = mid;
-      else hi = mid;
-    }
-  }
-  while (pos < end) {
-    while (prefix[seq + 1] * lanes <= pos) ++seq;
-    Run r;
-    r.seq = seq;
-    r.units = (int)(prefix[seq + 1] - prefix[seq]);
-    const int64_t local = pos - prefix[seq] * lanes;
-    const int item = (int)(local / r.units);
-    r.u0 = (int)(local - (int64_t)item * r.units);
-    r.u1 = (int)min((int64_t)r.units, r.u0 + (end - pos));
-    r.first = pos - r.u0;
-    r.head = item / p.row_tiles;
-    r.tile = item - r.head * p.row_tiles;
-    r.len = max(p.lens[seq], 0);
-    const int count = node_count(p, seq);
-    r.keys = (int)min((int64_t)r.len + count, (int64_t)p.pages.columns << p.cache.shift);
-    const int rows = min(ROWS, p.nodes * p.group - r.tile * ROWS);
-    const int k_begin = r.u0 * unit, k_end = min(r.u1 * unit, r.keys);
+  uint32_t phases = 0;   // of the warp's barriers
+  bool alive = true;     // no wait has given up
+  for (int64_t pos = begin; pos < end;) {
+    while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after());
+    const int which = __popc(__ballot_sync(0xffffffffu, (sq.before + sq.sum) * lanes <= pos));
+    const int seq = sq.first + which;
+    const int units = __shfl_sync(0xffffffffu, sq.units, which);
+    const int len = __shfl_sync(0xffffffffu, sq.len, which), keys = __shfl_sync(0xffffffffu, sq.keys, which);
+    const int64_t seq_first = (sq.before + __shfl_sync(0xffffffffu, sq.sum, which) - units) * lanes;
+    const int item = (int)((pos - seq_first) / units);
+    const int64_t first = seq_first + (int64_t)item * units;  // the item's first unit
+    const int u0 = (int)(pos - first), u1 = (int)min((int64_t)units, u0 + (end - pos));
+    const int head = item / p.row_tiles, tile = item - head * p.row_tiles;
+    const int rows = min(ROWS, p.nodes * p.group - tile * ROWS);
+    const int k_begin = u0 * kUnit, k_end = min(u1 * kUnit, keys);
 
     // -- copies -------------------------------------------------------------
+    constexpr int STRIDE = W * KW;
+    const int key0 = k_begin + warp * KW;  // this warp's steps: key0, key0 + STRIDE, ...
     const int32_t* page_row = p.pages.pages + seq * p.pages.ld;
-    int next_page[KW / 16];
+    const bool one_box = KW == 16 || p.cache.shift >= 5;  // a step lies in one page
+    int next_page[MB];
     auto fetch_pages = [&](int key) {
 #pragma unroll
-      for (int i = 0; i < KW / 16; ++i) {
+      for (int i = 0; i < MB; ++i) {
         const int k = key + 16 * i;
-        next_page[i] = k < k_end ? page_row[k >> p.cache.shift] : -1;
+        next_page[i] = (i == 0 || !one_box) && k < k_end ? page_row[k >> p.cache.shift] : -1;
       }
     };
+    uint32_t bad_pages = 0;  // two bits a stage: 16 keys each whose page is missing
     auto issue = [&](int key, int slot) {  // the step of KW keys at `key`, whose pages were fetched
-      const uint32_t dst = ring_u32 + slot * C::STAGE;
-      int64_t base[KW / 16];
       uint32_t bad = 0;
+      const int boxes = one_box ? 1 : MB;
 #pragma unroll
-      for (int i = 0; i < KW / 16; ++i) {
-        const int k = key + 16 * i;
+      for (int i = 0; i < MB; ++i) {
         const bool ok = next_page[i] >= 0 && next_page[i] < p.cache.pages;
-        if (!ok && k < k_end) bad |= 1u << i;
-        base[i] = ok ? (((int64_t)next_page[i] * p.cache.heads + r.head) << p.cache.shift) +
-                           (k & ((1 << p.cache.shift) - 1))
-                     : -1;
+        if (i < boxes && !ok && key + 16 * i < k_end) bad |= one_box ? 3u : 1u << i;
       }
+      bad_pages = (bad_pages & ~(3u << (2 * slot))) | bad << (2 * slot);
+      if (lane == 0) {
+        uint64_t* bar = &bars[warp][slot];
+        const int box = KW / boxes;
+        int have = 0;
 #pragma unroll
-      for (int i = 0; i < KW * C::CH / 32; ++i) {
-        const int row = (i * 32 + lane) / C::CH, ch = lane % C::CH;
-        const int64_t b = base[(i * 32) / C::CH / 16];  // 32 lanes stay within 16 rows
-        const bool ok = b >= 0 && key + row < k_end;
-        const int64_t off = ok ? (b + row % 16) * C::RB + ch * 16 : 0;
-        copy16(dst + C::at(row, ch), p.cache.k + off, ok ? 16 : 0);
-        copy16(dst + KW * C::RB + C::at(row, ch), p.cache.v + off, ok ? 16 : 0);
-      }
-      if constexpr (C::SB > 0) {
-        constexpr int KEYS = 16 / C::SB;  // keys of a 16-byte piece of scales
-        constexpr int PIECES = KW / KEYS;
+        for (int i = 0; i < MB; ++i) have += i < boxes && next_page[i] >= 0 && next_page[i] < p.cache.pages;
+        mbar_expect_tx(bar, have * box * 2 * (C::RB + C::SB));
+        uint8_t* to = ring + slot * STAGE;
+        uint8_t* scales = ring_scales + slot * (2 * KW * C::SB);
 #pragma unroll
-        for (int i = 0; i < 2 * PIECES; i += 32) {
-          const int id = i + lane;
-          if (id < 2 * PIECES) {
-            const bool is_v = id >= PIECES;
-            const int row = (id - (is_v ? PIECES : 0)) * KEYS;
-            const int64_t b = KW == 16 || row < 16 ? base[0] : base[KW / 16 - 1];
-            const int have = b >= 0 ? min(max(k_end - key - row, 0), KEYS) * C::SB : 0;
-            const uint8_t* src = static_cast<const uint8_t*>(is_v ? p.cache.vs : p.cache.ks);
-            copy16(dst + 2 * KW * C::RB + (is_v ? KW * C::SB : 0) + row * C::SB,
-                   src + (have > 0 ? (b + row % 16) * C::SB : 0), have);
+        for (int i = 0; i < MB; ++i) {
+          if (i >= boxes || next_page[i] < 0 || next_page[i] >= p.cache.pages) continue;
+          const int64_t row = (((int64_t)next_page[i] * p.cache.heads + head) << p.cache.shift) +
+                              ((key + 16 * i) & ((1 << p.cache.shift) - 1));
+#pragma unroll
+          for (int s = 0; s < C::SLICES; ++s) {
+            const int off = s * (KW * 128) + i * 16 * C::SPAN;
+            tma_rows(smem_u32(to + off), &p.k_map, s * 128, (int)row, bar);
+            tma_rows(smem_u32(to + KW * C::RB + off), &p.v_map, s * 128, (int)row, bar);
+          }
+          if constexpr (C::SB > 0) {
+            bulk_g2s(scales + i * 16 * C::SB, static_cast<const uint8_t*>(p.cache.ks) + row * C::SB, box * C::SB, bar);
+            bulk_g2s(scales + (KW + i * 16) * C::SB, static_cast<const uint8_t*>(p.cache.vs) + row * C::SB,
+                     box * C::SB, bar);
           }
         }
       }
-      if (lane == 0) bad_pages[warp][slot] = (uint8_t)bad;
     };
-
-    const int key0 = k_begin + warp * KW;  // this warp's steps: key0, key0 + kWarps KW, ...
-    constexpr int STRIDE = kWarps * KW;
+    int issued = 0;  // steps of this run
     fetch_pages(key0);
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) {
-      if (key0 + s * STRIDE < k_end) {
-        issue(key0 + s * STRIDE, s);
-        fetch_pages(key0 + (s + 1) * STRIDE);
+      const int key = key0 + s * STRIDE;
+      if (key < k_end && alive) {
+        issue(key, s);
+        ++issued;
+        fetch_pages(key + STRIDE);
       }
-      copy_commit();
     }
 
-    // -- q, laid out for the products ------------------------------------------
-    auto q_operand = [&](int mt, int ks, uint32_t (&a)[4]) {
+    // -- q: the b operands, and its sums over the entries of a group -----------
+    uint32_t qf[NT <= 2 ? NT : 1][KS][2];
+    float q128[NT][2];           // INT8: 128 sum q of rows 2 t and 2 t + 1
+    uint32_t q_sums[INT4 ? NT : 1];  // INT4: sum q / 32 over group t of row g, in two parts
+    auto load_q = [&](int nt, uint32_t (&b)[KS][2]) {
+      const int lr = nt * 8 + g, gr = tile * ROWS + lr, node = gr / p.group;
+      const __half* row = p.q + seq * p.q_seq + node * p.q_node + (int64_t)(head * p.group + gr - node * p.group) * p.q_head;
+      float sum[GROUPS];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int lr = mt * 16 + g + 8 * (i & 1);
-        uint32_t v = 0;
-        if (lr < rows) {
-          const int gr = r.tile * ROWS + lr, node = gr / p.group;
-          const __half* row = p.q + seq * p.q_seq + node * p.q_node + (int64_t)(r.head * p.group + gr % p.group) * p.q_head;
-          const int e0 = C::entry(t, ks, 2 * (i >> 1));
-          if constexpr (KIND == AF1_KV_INT4)
-            v = (uint32_t)__half_as_ushort(row[e0]) | (uint32_t)__half_as_ushort(row[e0 + 4]) << 16;
-          else
-            v = *reinterpret_cast<const uint32_t*>(row + e0);
+      for (int c = 0; c < GROUPS; ++c) sum[c] = 0.f;
+      auto add = [&](int c, uint32_t w) { sum[c] += low_float(w) + high_float(w); };
+      if constexpr (INT4) {
+#pragma unroll
+        for (int c = 0; c < GROUPS; ++c) {
+          const uint4 w = lr < rows ? *reinterpret_cast<const uint4*>(row + 32 * c + 8 * t) : make_uint4(0, 0, 0, 0);
+          b[2 * c][0] = prmt(w.x, w.z, 0x5410), b[2 * c][1] = prmt(w.y, w.w, 0x5410);
+          b[2 * c + 1][0] = prmt(w.x, w.z, 0x7632), b[2 * c + 1][1] = prmt(w.y, w.w, 0x7632);
+          add(c, w.x), add(c, w.y), add(c, w.z), add(c, w.w);
         }
-        a[i] = v;
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const uint2 w = lr < rows ? *reinterpret_cast<const uint2*>(row + C::entry(t, ks, 0)) : make_uint2(0, 0);
+          b[ks][0] = w.x, b[ks][1] = w.y;
+          if constexpr (KIND == AF1_KV_INT8) add(0, w.x), add(0, w.y);
+        }
+      }
+      if constexpr (INT4 || KIND == AF1_KV_INT8) {
+#pragma unroll
+        for (int c = 0; c < GROUPS; ++c) {
+          sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 1);
+          sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 2);
+        }
+      }
+      if constexpr (KIND == AF1_KV_INT8) {
+        q128[nt][0] = 128.f * __shfl_sync(0xffffffffu, sum[0], 8 * t);
+        q128[nt][1] = 128.f * __shfl_sync(0xffffffffu, sum[0], 8 * t + 4);
+      }
+      if constexpr (INT4) {
+        float mine = 0.f;
+#pragma unroll
+        for (int c = 0; c < GROUPS; ++c)
+          if (c == t) mine = sum[c] * (1.f / 32.f);
+        const float hi = __half2float(__float2half_rn(mine));
+        q_sums[nt] = pack_half2(hi, mine - hi);
       }
     };
-    uint32_t qf[MT == 1 ? KS : 1][4];
-    if constexpr (MT == 1) {
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) q_operand(0, ks, qf[ks]);
-    } else {
-      for (int i = warp; i < MT * KS; i += kWarps) {
-        uint32_t a[4];
-        q_operand(i / KS, i % KS, a);
-        reinterpret_cast<uint4*>(qs)[i * 32 + lane] = make_uint4(a[0], a[1], a[2], a[3]);
+    for (int nt = 0; nt < NT; ++nt) {
+      if constexpr (NT <= 2) {
+        load_q(nt, qf[nt]);
+      } else {
+        uint32_t b[KS][2];
+        load_q(nt, b);
+        if (warp == nt % W) {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) qs[(nt * KS + ks) * 32 + lane] = make_uint2(b[ks][0], b[ks][1]);
+        }
       }
-      __syncthreads();
     }
+    if constexpr (NT > 2) __syncthreads();
 
-    float o[MT][ON][4], m[MT][2], l[MT][2], vref = 0.f;
+    // o^T: block m, column block nt: entries row_entry(m, g, i / 2) of rows 2 t + i % 2.
+    float o[MT][NT][4], m[NT][2], l[NT][2], vref = 0.f;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-      for (int n = 0; n < ON; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
-      m[mt][0] = m[mt][1] = -kInf, l[mt][0] = l[mt][1] = 0.f;
+      for (int mt = 0; mt < MT; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
+      m[nt][0] = m[nt][1] = -kInf, l[nt][0] = l[nt][1] = 0.f;
     }
 
     // -- steps ---------------------------------------------------------------------
-    int slot = 0;
-    for (int key = key0; key < k_end; key += STRIDE) {
-      copy_wait<STAGES - 2>();
-      __syncwarp();
+    int slot = 0, waited = 0;
+    for (int key = key0; key < k_end && alive; key += STRIDE) {
       {
         const int ahead = key + (STAGES - 1) * STRIDE;
         int to = slot + STAGES - 1;
         if (to >= STAGES) to -= STAGES;
         if (ahead < k_end) {
           issue(ahead, to);
+          ++issued;
           fetch_pages(ahead + STRIDE);
         }
-        copy_commit();
       }
-      const uint8_t* kb = ring + slot * C::STAGE;
+      alive = __all_sync(0xffffffffu, wait_phase(&bars[warp][slot], phases >> slot & 1, p.wait_cycles));
+      if (!alive) break;
+      phases ^= 1u << slot;
+      ++waited;
+      const uint8_t* kb = ring + slot * STAGE;
       const uint8_t* vb = kb + KW * C::RB;
-      const uint8_t* ksb = kb + 2 * KW * C::RB;
+      const uint8_t* ksb = ring_scales + slot * (2 * KW * C::SB);
       const uint8_t* vsb = ksb + KW * C::SB;
-      const uint32_t bad = bad_pages[warp][slot];
+      const uint32_t bad = bad_pages >> (2 * slot) & 3u;
 
-      float s[MT][NB][4];
+      // Scores of keys mb 16 + g + 8 (i / 2), rows 2 t + i % 2.
+      float s[MB][NT][4];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        uint32_t w[C::WORDS];
-        load_key<C>(w, kb, nb * 8 + g, t);
-        uint32_t s2 = 0, m2 = 0;
-        if constexpr (KIND == AF1_KV_INT4) {
-          const uint32_t sm = reinterpret_cast<const uint32_t*>(ksb)[(nb * 8 + g) * (DIM / 32) + t * (DIM / 32) / 4];
-          s2 = prmt(sm, sm, 0x1010), m2 = prmt(sm, sm, 0x3232);
-        }
+      for (int mb = 0; mb < MB; ++mb) {
+        uint32_t w[2][WORDS];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) s[mt][nb][0] = s[mt][nb][1] = s[mt][nb][2] = s[mt][nb][3] = 0.f;
+        for (int h = 0; h < 2; ++h) load_key<C, KIND, KW>(w[h], kb, mb * 16 + 8 * h + g, t);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          uint32_t b0, b1;
-          key_operand<KIND>(b0, b1, w, ks, s2, m2);
+        for (int nt = 0; nt < NT; ++nt) s[mb][nt][0] = s[mb][nt][1] = s[mb][nt][2] = s[mb][nt][3] = 0.f;
+        auto q_of = [&](int nt, int ks) {
+          if constexpr (NT <= 2) return make_uint2(qf[nt][ks][0], qf[nt][ks][1]);
+          else return qs[(nt * KS + ks) * 32 + lane];
+        };
+        if constexpr (INT4) {
+          const uint32_t* sc = reinterpret_cast<const uint32_t*>(ksb);
+          uint32_t a[4] = {0, 0, 0, 0};
+          float key_scale[2][GROUPS];
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            if constexpr (MT == 1) {
-              mma(s[mt][nb], qf[ks], b0, b1);
-            } else {
-              uint4 a = reinterpret_cast<const uint4*>(qs)[(mt * KS + ks) * 32 + lane];
-              const uint32_t aa[4] = {a.x, a.y, a.z, a.w};
-              mma(s[mt][nb], aa, b0, b1);
+          for (int h = 0; h < 2; ++h) {
+            const int at = (mb * 16 + 8 * h + g) * GROUPS;
+            const uint32_t low = GROUPS == 4 || t < GROUPS ? sc[at + (GROUPS == 4 ? t : t & 1)] : 0;
+            a[h] = prmt(low, low, 0x3232);
+#pragma unroll
+            for (int c = 0; c < GROUPS; ++c) key_scale[h][c] = low_float(sc[at + c]) * (kCode / 32.f);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma(s[mb][nt], a, q_sums[nt], 0);
+#pragma unroll
+          for (int c = 0; c < GROUPS; ++c) {
+            uint32_t a0[4], a1[4];
+            key_operand<KIND>(a0, w, 2 * c);
+            key_operand<KIND>(a1, w, 2 * c + 1);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              float acc[4] = {0.f, 0.f, 0.f, 0.f};
+              const uint2 b0 = q_of(nt, 2 * c), b1 = q_of(nt, 2 * c + 1);
+              mma(acc, a0, b0.x, b0.y);
+              mma(acc, a1, b1.x, b1.y);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[mb][nt][i] = fmaf(acc[i], key_scale[i / 2][c], s[mb][nt][i]);
             }
           }
-        }
-        float c0 = p.scale_log2, c1 = p.scale_log2;
-        if constexpr (KIND == AF1_KV_INT8 || KIND == AF1_KV_E4M3) {
-          const float2 sc = *reinterpret_cast<const float2*>(ksb + (nb * 8 + 2 * t) * 4);
-          c0 *= sc.x, c1 *= sc.y;
-        }
+          const float f = 32.f * p.scale_log2;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          s[mt][nb][0] *= c0, s[mt][nb][1] *= c1;
-          s[mt][nb][2] *= c0, s[mt][nb][3] *= c1;
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[mb][nt][i] *= f;
+        } else {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            uint32_t a[4];
+            key_operand<KIND>(a, w, ks);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const uint2 b = q_of(nt, ks);
+              mma(s[mb][nt], a, b.x, b.y);
+            }
+          }
+          float f[2] = {p.scale_log2, p.scale_log2};
+          if constexpr (C::SCALED8) {
+            f[0] *= reinterpret_cast<const float*>(ksb)[mb * 16 + g];
+            f[1] *= reinterpret_cast<const float*>(ksb)[mb * 16 + 8 + g];
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float x = s[mb][nt][i];
+              if constexpr (KIND == AF1_KV_INT8) x = fmaf(x, kCode, -q128[nt][i % 2]);
+              s[mb][nt][i] = x * f[i / 2];
+            }
         }
       }
 
       // Steps with nodes, with keys past the end or with missing pages.
-      const bool masked = key + KW > min(r.len, k_end) || bad != 0;
+      const bool masked = key + KW > min(len, k_end) || bad != 0;
       if (masked) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const int lr = mt * 16 + g + 8 * hf;
+          for (int i = 0; i < 2; ++i) {
+            const int lr = nt * 8 + 2 * t + i;
             uint64_t bits = 0;
             if (lr < rows) {
-              const int node = (r.tile * ROWS + lr) / p.group;
+              const int node = (tile * ROWS + lr) / p.group;
               if (p.mask == nullptr) {
                 bits = (2ull << node) - 1;
               } else {
@@ -526,197 +619,251 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
               }
             }
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+            for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const int at = nb * 8 + 2 * t + i, k = key + at;
-                const bool sees = k < k_end && !(bad >> (at / 16) & 1) && (k < r.len || (bits >> (k - r.len) & 1));
-                if (!sees) s[mt][nb][2 * hf + i] = -kInf;
+              for (int h = 0; h < 2; ++h) {
+                const int k = key + mb * 16 + 8 * h + g;
+                const bool sees = k < k_end && !(bad >> mb & 1) && (k < len || (bits >> (k - len) & 1));
+                if (!sees) s[mb][nt][2 * h + i] = -kInf;
               }
           }
       }
 
-      // Running maximum; o and l follow it.
-      float alpha[MT][2], ref[MT][2];
-      bool moved = false;
+      // The maximum moves where a score is kSlack above it.
+      bool grow = false;
+      float top[NT][2];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          float top = fmaxf(s[mt][0][2 * hf], s[mt][0][2 * hf + 1]);
+        for (int i = 0; i < 2; ++i) {
+          float x = fmaxf(s[0][nt][i], s[0][nt][2 + i]);
 #pragma unroll
-          for (int nb = 1; nb < NB; ++nb) top = fmaxf(top, fmaxf(s[mt][nb][2 * hf], s[mt][nb][2 * hf + 1]));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          const float now = fmaxf(m[mt][hf], top);
-          moved |= now > m[mt][hf];
-          const float zero = now == -kInf ? 0.f : now;
-          alpha[mt][hf] = ex2(m[mt][hf] - zero);
-          m[mt][hf] = now;
-          ref[mt][hf] = zero - kShift;
+          for (int mb = 1; mb < MB; ++mb) x = fmaxf(x, fmaxf(s[mb][nt][i], s[mb][nt][2 + i]));
+          top[nt][i] = x;
+          grow |= x > m[nt][i] + kSlack;
         }
+      if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float x = top[nt][i];
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+            const float now = fmaxf(m[nt][i], x);
+            const float alpha = ex2(m[nt][i] - (now == -kInf ? 0.f : now));
+            m[nt][i] = now;
+            l[nt][i] *= alpha;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) o[mt][nt][i] *= alpha, o[mt][nt][2 + i] *= alpha;
+          }
+      }
+      // So does the largest scale of a value, with room to twice what it was.
       float vinv = 0.f;
-      if constexpr (KIND == AF1_KV_INT8 || KIND == AF1_KV_E4M3) {
-        const float vs = reinterpret_cast<const float*>(vsb)[lane];
+      if constexpr (C::SCALED8) {
+        const int row = lane % KW;
+        const bool real = !masked || (key + row < k_end && !(bad >> (row / 16) & 1));
+        float x = fabsf(reinterpret_cast<const float*>(vsb)[row]);
+        x = x < kInf ? x : 0.f;
         // Non-negative floats order as their bits.
-        const uint32_t top = __reduce_max_sync(0xffffffffu, fabsf(vs) < kInf ? __float_as_uint(fabsf(vs)) : 0u);
-        const float now = fmaxf(vref, __uint_as_float(top));
-        if (now > vref) {
-          const float f = vref / now;
+        const float most = __uint_as_float(__reduce_max_sync(0xffffffffu, real ? __float_as_uint(x) : 0u));
+        if (most > vref) {
+          const float now = 2.f * most, f = vref / now;
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int n = 0; n < ON; ++n)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) o[mt][n][i] *= f;
+              for (int i = 0; i < 4; ++i) o[mt][nt][i] *= f;
           vref = now;
         }
         vinv = vref > 0.f ? 1.f / vref : 0.f;
       }
-      if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) l[mt][hf] *= alpha[mt][hf];
-#pragma unroll
-          for (int n = 0; n < ON; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[mt][n][i] *= alpha[mt][i / 2];
-        }
-      }
 
       // Weights.
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        float2 vsc = make_float2(1.f, 1.f);
-        if constexpr (KIND == AF1_KV_INT8 || KIND == AF1_KV_E4M3) {
-          vsc = *reinterpret_cast<const float2*>(vsb + (nb * 8 + 2 * t) * 4);
-          vsc.x *= vinv, vsc.y *= vinv;
-        }
+      for (int nt = 0; nt < NT; ++nt) {
+        float ref[2];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int i = 0; i < 2; ++i) ref[i] = (m[nt][i] == -kInf ? 0.f : m[nt][i]) - kShift;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float w = ex2(s[mt][nb][i] - ref[mt][i / 2]);
-            l[mt][i / 2] += w;
-            if constexpr (KIND == AF1_KV_INT8 || KIND == AF1_KV_E4M3)
-              s[mt][nb][i] = masked && !(w > 0.f) ? 0.f : w * (i % 2 ? vsc.y : vsc.x);
-            else
-              s[mt][nb][i] = w;
+            const float x = ex2(s[mb][nt][i] - ref[i % 2]);
+            l[nt][i % 2] += x;
+            s[mb][nt][i] = x;
           }
       }
 
       // A node's infinite or NaN value must not reach the rows that do not
       // see it, as 0 times it would: such steps sum entry by entry.
       bool slow = false;
-      if (masked) {
-        constexpr int PARTS = 32 / KW;
-        slow = __any_sync(0xffffffffu, value_bad<KIND, DIM>(vb, vsb, lane % KW, lane / KW, PARTS));
-      }
+      if (masked) slow = __any_sync(0xffffffffu, value_bad<KIND, DIM, KW>(vb, vsb, lane % KW, lane / KW, 32 / KW));
       if (slow) {
         for (int j = 0; j < KW; ++j) {
-          const int from = (lane & ~3) | (j % 8) / 2;
+          const int from = (j % 8) * 4 + t;
+          float vs = 1.f;
+          if constexpr (C::SCALED8) vs = reinterpret_cast<const float*>(vsb)[j] * vinv;
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            float w[2];
+          for (int nt = 0; nt < NT; ++nt) {
+            float x[2];
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
+            for (int i = 0; i < 2; ++i) {
               float mine = 0.f;
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb)
+              for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                  if (nb == j / 8 && i == j % 2) mine = s[mt][nb][2 * hf + i];
-              w[hf] = __shfl_sync(0xffffffffu, mine, from);
+                for (int h = 0; h < 2; ++h)
+                  if (j / 8 == 2 * mb + h) mine = s[mb][nt][2 * h + i];
+              x[i] = __shfl_sync(0xffffffffu, mine, from);
             }
 #pragma unroll
-            for (int n = 0; n < ON; ++n)
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const float v = value_entry<KIND, DIM>(vb, vsb, j, C::column(t, n, i));
+              for (int h = 0; h < 2; ++h) {
+                const float v = value_entry<KIND, DIM, KW>(vb, vsb, j, C::row_entry(mt, g, h)) * vs;
 #pragma unroll
-                for (int hf = 0; hf < 2; ++hf)
-                  if (w[hf] != 0.f) o[mt][n][2 * hf + i] += w[hf] * v;
+                for (int i = 0; i < 2; ++i)
+                  if (x[i] != 0.f) o[mt][nt][2 * h + i] += x[i] * v;
               }
           }
         }
       } else {
 #pragma unroll
-        for (int kk = 0; kk < KW / 16; ++kk) {
-          uint32_t a[MT][4];
+        for (int mb = 0; mb < MB; ++mb) {
+          const uint32_t v_addr = smem_u32(vb);
+          const int row = mb * 16 + (lane & 15), hi = lane >> 4;
+          // Weights of the 16 keys, times c of each key, as b operands.
+          auto weights = [&](int nt, float c0, float c1, uint32_t (&b)[2]) {
+            const float x[4] = {s[mb][nt][0] * c0, s[mb][nt][1] * c0, s[mb][nt][2] * c1, s[mb][nt][3] * c1};
+            // 0 times a missing key's scale is 0.
+            auto ok = [&](int i) { return masked && !(s[mb][nt][i] > 0.f) ? 0.f : x[i]; };
+            b[0] = transpose8(pack_half2(ok(0), ok(1)));
+            b[1] = transpose8(pack_half2(ok(2), ok(3)));
+          };
+          if constexpr (INT4) {
+            const uint32_t* sc = reinterpret_cast<const uint32_t*>(vsb) + mb * 16 * GROUPS;
+            uint32_t b[NT][2];
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            a[mt][0] = pack_half2(s[mt][2 * kk][0], s[mt][2 * kk][1]);
-            a[mt][1] = pack_half2(s[mt][2 * kk][2], s[mt][2 * kk][3]);
-            a[mt][2] = pack_half2(s[mt][2 * kk + 1][0], s[mt][2 * kk + 1][1]);
-            a[mt][3] = pack_half2(s[mt][2 * kk + 1][2], s[mt][2 * kk + 1][3]);
-          }
-          const int row = kk * 16 + (lane & 15);
+            for (int nt = 0; nt < NT; ++nt) weights(nt, 1.f, 1.f, b[nt]);
 #pragma unroll
-          for (int c = 0; c < C::CH; c += 2) {
-            uint32_t v[4];
-            ldmatrix_x4_trans(v, smem_u32(vb) + C::at(row, c + (lane >> 4)));
+            for (int c = 0; c < GROUPS; c += 2) {
+              uint32_t v[4];
+              ldmatrix_x4_trans(v, v_addr + C::template at<KW>(row, c + hi));
 #pragma unroll
-            for (int cc = 0; cc < 2; ++cc) {
-              uint32_t s2[2] = {0, 0}, m2[2] = {0, 0};
-              if constexpr (KIND == AF1_KV_INT4) {
-                const uint32_t* sm = reinterpret_cast<const uint32_t*>(vsb) + (kk * 16 + 2 * t) * (DIM / 32) + c + cc;
+              for (int cc = 0; cc < 2; ++cc) {
+                uint32_t s2[2], low2[2];  // of keys 2 t and 2 t + 1, and of those 8 on
 #pragma unroll
-                for (int hf = 0; hf < 2; ++hf) {
-                  const uint32_t x = sm[hf * 8 * (DIM / 32)], y = sm[(hf * 8 + 1) * (DIM / 32)];
-                  s2[hf] = prmt(x, y, 0x5410), m2[hf] = prmt(x, y, 0x7632);
+                for (int h = 0; h < 2; ++h) {
+                  const uint32_t x = sc[(2 * t + 8 * h) * GROUPS + c + cc], y = sc[(2 * t + 1 + 8 * h) * GROUPS + c + cc];
+                  s2[h] = prmt(x, y, 0x5410), low2[h] = prmt(x, y, 0x7632);
+                }
+#pragma unroll
+                for (int odd = 0; odd < 2; ++odd) {
+                  uint32_t a[4];
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    const uint32_t code = v[2 * cc + i / 2] >> (4 * odd + 8 * (i % 2)) & 0x000f000fu;
+                    a[i] = hfma2(hsub2(code | 0x64006400u, 0x64006400u), s2[i / 2], low2[i / 2]);
+                  }
+#pragma unroll
+                  for (int nt = 0; nt < NT; ++nt) mma(o[2 * (c + cc) + odd][nt], a, b[nt][0], b[nt][1]);
                 }
               }
-              constexpr int BLOCKS = ON / C::CH;  // output blocks of a chunk
+            }
+          } else {
+            float c0 = 1.f, c1 = 1.f;
+            if constexpr (C::SCALED8) {
+              c0 = reinterpret_cast<const float*>(vsb)[mb * 16 + g] * vinv;
+              c1 = reinterpret_cast<const float*>(vsb)[mb * 16 + 8 + g] * vinv;
+            }
+            uint32_t b[NT][2];
 #pragma unroll
-              for (int i = 0; i < BLOCKS; ++i) {
-                const uint32_t b0 = value_operand<KIND>(v[2 * cc], i, s2[0], m2[0]);
-                const uint32_t b1 = value_operand<KIND>(v[2 * cc + 1], i, s2[1], m2[1]);
+            for (int nt = 0; nt < NT; ++nt) weights(nt, c0, c1, b[nt]);
+            constexpr int PER = KIND == AF1_KV_F16 ? 1 : 2;  // 16-entry blocks of two chunks
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) mma(o[mt][(c + cc) * BLOCKS + i], a[mt], b0, b1);
+            for (int mt = 0; mt < MT; mt += PER) {
+              uint32_t v[4];
+              ldmatrix_x4_trans(v, v_addr + C::template at<KW>(row, (KIND == AF1_KV_F16 ? 2 * mt : mt) + hi));
+#pragma unroll
+              for (int cc = 0; cc < PER; ++cc) {
+                uint32_t a[4];
+                if constexpr (KIND == AF1_KV_F16) {
+                  a[0] = v[0], a[1] = v[2], a[2] = v[1], a[3] = v[3];
+                } else {
+#pragma unroll
+                  for (int h = 0; h < 2; ++h) {
+                    if constexpr (KIND == AF1_KV_INT8) {
+                      const uint32_t u = v[2 * cc + h] ^ 0x80808080u;
+                      a[2 * h] = hsub2(prmt(u, 0x64646464u, 0x4240), 0x64806480u);
+                      a[2 * h + 1] = hsub2(prmt(u, 0x64646464u, 0x4341), 0x64806480u);
+                    } else {
+                      const uint32_t u = prmt(v[2 * cc + h], 0, 0x3120);
+                      a[2 * h] = e4m3x2(u);
+                      a[2 * h + 1] = e4m3x2(u >> 16);
+                    }
+                  }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma(o[mt + cc][nt], a, b[nt][0], b[nt][1]);
               }
             }
           }
         }
       }
       if (++slot == STAGES) slot = 0;
-      __syncwarp();
+      __syncwarp();  // the slot is free again
     }
-    copy_wait<0>();
+    if (!alive) {
+      // A wait gave up: let the copies in flight land (with the same limit)
+      // before shared memory changes hands, and report it.
+      for (; waited < issued; ++waited) {
+        if (wait_phase(&bars[warp][slot], phases >> slot & 1, p.wait_cycles)) phases ^= 1u << slot;
+        if (++slot == STAGES) slot = 0;
+      }
+      if (lane == 0) atomicOr(p.status, kStatusTimeout);
+    }
     __syncthreads();  // every warp is done with its ring
 
     // -- join the warps' parts -------------------------------------------------------
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        float sum = l[mt][hf];
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        const int lr = mt * 16 + g + 8 * hf;
-        if (t == 0) join_m[warp][lr] = m[mt][hf], join_l[warp][lr] = sum;
-        if (lr < rows) {
-          float* to = join + (warp * ROWS + lr) * DIM;
-          const float f = KIND == AF1_KV_INT8 || KIND == AF1_KV_E4M3 ? vref : 1.f;
+      for (int i = 0; i < 2; ++i) {
+        float sum = l[nt][i];
 #pragma unroll
-          for (int n = 0; n < ON; ++n) {
-            to[C::column(t, n, 0)] = o[mt][n][2 * hf] * f;
-            to[C::column(t, n, 1)] = o[mt][n][2 * hf + 1] * f;
+        for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        const int lr = nt * 8 + 2 * t + i;
+        if (g == 0) join_m[warp][lr] = m[nt][i], join_l[warp][lr] = sum;
+        float* to = join + (warp * ROWS + lr) * DIM;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          const float f = C::SCALED8 ? vref : 1.f;
+          if (lr < rows) {
+            to[C::row_entry(mt, g, 0)] = o[mt][nt][i] * f;
+            to[C::row_entry(mt, g, 1)] = o[mt][nt][2 + i] * f;
           }
         }
       }
     __syncthreads();
-    const bool whole = r.u0 == 0 && r.u1 == r.units;
-    // This run's place in the workspace: a CTA has at most two runs of parts,
-    // its first and its last.
-    auto part_of = [&](int cta) {
-      const int64_t from = total * cta / ctas;
-      return p.parts + (int64_t)(2 * cta + (from >= r.first ? 0 : 1)) * PART;
+    const bool whole = u0 == 0 && u1 == units;
+    // Parts of an item: a CTA leaves at most two, of its first run and of its
+    // last one. CTAs c0 .. c1 hold the item's units; all but c0 begin inside it.
+    auto holder = [&](int64_t u) {
+      int64_t c = u * ctas / total;
+      while (total * (c + 1) / ctas <= u) ++c;
+      return (int)c;
     };
-    float* part = whole ? nullptr : part_of(blockIdx.x);
+    int c0 = 0, c1 = 0;
+    if (!whole) c0 = holder(first), c1 = holder(first + units - 1);
+    const int c0_place = whole || total * c0 / ctas == first ? 0 : 1;
+    auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? c0_place : 0)) * S::PART; };
+    float* part = part_of(blockIdx.x);
+    const int live_nodes = p.counts == nullptr ? p.nodes : min(max(p.counts[seq], 0), p.nodes);
     auto finish = [&](int lr, int e, float mx, float sum, float acc) {
-      const int gr = r.tile * ROWS + lr, node = gr / p.group, h = r.head * p.group + gr % p.group;
-      const bool live = node < count && sum != 0.f;
+      const int gr = tile * ROWS + lr, node = gr / p.group, h = head * p.group + gr - node * p.group;
+      const bool live = node < live_nodes && sum != 0.f;
       const float y = live ? acc / sum : 0.f;
       const int64_t at = seq * p.o_seq + node * p.o_node + h * p.o_head + e;
       if (p.out_f32) static_cast<float*>(p.out)[at] = y;
@@ -725,15 +872,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         p.lse[((int64_t)seq * p.nodes + node) * p.cache.heads * p.group + h] =
             live ? (mx - kShift + log2f(sum)) * 0.69314718056f : -kInf;
     };
-    for (int i = threadIdx.x; i < rows * DIM; i += kThreads) {
+    for (int i = threadIdx.x; i < rows * DIM; i += 32 * W) {
       const int lr = i / DIM, e = i % DIM;
       float mx = -kInf;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, join_m[w][lr]);
+      for (int w = 0; w < W; ++w) mx = fmaxf(mx, join_m[w][lr]);
       const float zero = mx == -kInf ? 0.f : mx;
       float sum = 0.f, acc = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float f = ex2(join_m[w][lr] - zero);
         sum += f * join_l[w][lr];
         acc += f * join[(w * ROWS + lr) * DIM + e];
@@ -746,14 +893,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       }
     }
     if (!whole) {
-      // CTAs first .. last hold the item's units; the last to arrive joins.
-      const int64_t item_end = r.first + r.units;
-      auto holder = [&](int64_t u) {
-        int64_t c = u * ctas / total;
-        while (total * (c + 1) / ctas <= u) ++c;
-        return (int)c;
-      };
-      const int c0 = holder(r.first), c1 = holder(item_end - 1);
       __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
@@ -764,49 +903,49 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       __syncthreads();
       if (last_shared) {
         __threadfence();
-        for (int i = threadIdx.x; i < rows * DIM; i += kThreads) {
+        for (int i = threadIdx.x; i < rows * DIM; i += 32 * W) {
           const int lr = i / DIM, e = i % DIM;
           float mx = -kInf, sum = 0.f, acc = 0.f;
+#pragma unroll 4
           for (int c = c0; c <= c1; ++c) {
             const float* from = part_of(c);
-            const float pm = __ldcg(from + ROWS * DIM + lr);
+            const float pm = __ldcg(from + ROWS * DIM + lr), pl = __ldcg(from + ROWS * DIM + ROWS + lr);
+            const float po = __ldcg(from + lr * DIM + e);
             const float now = fmaxf(mx, pm);
             const float zero = now == -kInf ? 0.f : now;
             const float fa = ex2(mx - zero), fb = ex2(pm - zero);
-            sum = sum * fa + __ldcg(from + ROWS * DIM + ROWS + lr) * fb;
-            acc = acc * fa + __ldcg(from + lr * DIM + e) * fb;
+            sum = sum * fa + pl * fb;
+            acc = acc * fa + po * fb;
             mx = now;
           }
           finish(lr, e, mx, sum, acc);
         }
       }
     }
-    __syncthreads();  // join, join_m and qs are free again
-    pos += r.u1 - r.u0;
+    // The rings, written through the generic proxy above, go back to TMA.
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    pos += u1 - u0;
   }
 }
 
 int fail(int code, const std::string& msg) { return set_error(code, "af1_tree_attention: " + msg); }
 
-// Rows (of every query head and node that share a cached head) of a CTA.
-int row_blocks(int64_t rows) { return rows <= 16 ? 1 : 2; }
+// Blocks of 8 rows (of every query head and node that share a cached head) of a CTA.
+int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
 
 int64_t workspace_bytes(const af1_kv_cache& c, int64_t rows) {
   const int64_t ctas = std::min(c.num_sms, kMaxCtas);
-  return kPartOffset + 2 * ctas * (16 * row_blocks(rows)) * (c.d.head_dim + 2) * 4;
+  return kPartOffset + 2 * ctas * (8 * row_blocks(rows)) * (c.d.head_dim + 2) * 4;
 }
 
-template <int KIND, int DIM, int MT>
-int launch(const TreeProblem& p, int ctas, int max_smem, cudaStream_t st) {
-  using C = Kv<KIND, DIM>;
-  constexpr int STAGES = C::STAGE * kWarps * 4 <= 200 * 1024 ? 4 : 3;
-  static_assert(STAGES * C::STAGE >= 16 * MT * DIM * 4, "the warps' outputs are joined in their rings");
-  const int smem = kWarps * STAGES * C::STAGE + (MT > 1 ? MT * C::KS * 512 : 0) + 8 * (p.pages.seqs + 1);
-  auto kernel = tree_kernel<KIND, DIM, MT, STAGES>;
-  cudaError_t e = smem <= max_smem ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)
-                                   : cudaErrorInvalidValue;
+template <int KIND, int DIM, int NT, int W, int KW, int STAGES>
+int launch(const TreeProblem& p, int ctas, cudaStream_t st) {
+  constexpr int smem = Shape<KIND, DIM, NT, W, KW, STAGES>::SMEM;
+  auto kernel = tree_kernel<KIND, DIM, NT, W, KW, STAGES>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e == cudaSuccess) {
-    kernel<<<ctas, kThreads, smem, st>>>(p);
+    kernel<<<ctas, 32 * W, smem, st>>>(p);
     e = cudaGetLastError();
   }
   if (e != cudaSuccess) return fail(AF1_ERR_CUDA, std::string(cudaGetErrorName(e)) + " (" + cudaGetErrorString(e) + ")");
@@ -814,10 +953,31 @@ int launch(const TreeProblem& p, int ctas, int max_smem, cudaStream_t st) {
   return AF1_OK;
 }
 
+// Warps, keys of a step and stages of a kind: what fills the shared memory.
+template <int KIND, int DIM, int NT>
+int launch_rows(TreeProblem& p, const af1_kv_cache& c, int ctas, cudaStream_t st) {
+  constexpr int RB = kv_row_bytes(KIND, DIM);
+  constexpr int KW = RB >= 256 ? 16 : 32;
+  constexpr int W = NT == 4 ? 8 : 12;
+  constexpr int BYTES = 2 * KW * (RB + kv_scale_bytes(KIND, DIM)) * W;
+  constexpr int FIT = 215 * 1024 / BYTES;
+  constexpr int STAGES = FIT > 4 ? 4 : FIT;
+  static_assert(STAGES >= 2, "");
+  const int box = std::min(c.d.page_size, KW);
+  p.k_map = box == 16 ? c.k16 : c.k32;
+  p.v_map = box == 16 ? c.v16 : c.v32;
+  return launch<KIND, DIM, NT, W, KW, STAGES>(p, ctas, st);
+}
+
 template <int KIND>
-int launch_kind(const TreeProblem& p, int dim, int mt, int ctas, int max_smem, cudaStream_t st) {
-  if (dim == 128) return mt == 1 ? launch<KIND, 128, 1>(p, ctas, max_smem, st) : launch<KIND, 128, 2>(p, ctas, max_smem, st);
-  return mt == 1 ? launch<KIND, 64, 1>(p, ctas, max_smem, st) : launch<KIND, 64, 2>(p, ctas, max_smem, st);
+int launch_kind(TreeProblem& p, const af1_kv_cache& c, int nt, int ctas, cudaStream_t st) {
+  if (c.d.head_dim == 128)
+    return nt == 1   ? launch_rows<KIND, 128, 1>(p, c, ctas, st)
+           : nt == 2 ? launch_rows<KIND, 128, 2>(p, c, ctas, st)
+                     : launch_rows<KIND, 128, 4>(p, c, ctas, st);
+  return nt == 1   ? launch_rows<KIND, 64, 1>(p, c, ctas, st)
+         : nt == 2 ? launch_rows<KIND, 64, 2>(p, c, ctas, st)
+                   : launch_rows<KIND, 64, 4>(p, c, ctas, st);
 }
 
 bool sizes_ok(const af1_kv_cache* c, int64_t sequences, int64_t nodes, int64_t q_heads) {
@@ -877,7 +1037,7 @@ int af1_tree_attention(const af1_kv_cache* c, const af1_tree_args* a, void* work
     return fail(AF1_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
                                        std::to_string(workspace_bytes(*c, rows)) + " bytes");
   if (check_pointer(workspace, "workspace", dev) != AF1_OK) return fail(AF1_ERR_WORKSPACE, "workspace is not device memory");
-  const int mt = row_blocks(rows);
+  const int nt = row_blocks(rows);
   TreeProblem p = {};
   p.q = static_cast<const __half*>(a->q);
   p.q_seq = a->q_seq, p.q_node = a->q_node, p.q_head = a->q_head;
@@ -888,17 +1048,19 @@ int af1_tree_attention(const af1_kv_cache* c, const af1_tree_args* a, void* work
   p.pages = {a->pages, a->pages_ld, (int)a->sequences, (int)a->page_columns};
   p.lens = a->lens, p.counts = a->counts, p.mask = a->mask, p.mask_seq = a->mask_seq;
   p.nodes = (int)a->nodes, p.group = group, p.words = (int)(a->nodes + 31) / 32;
-  p.row_tiles = (int)((rows + 16 * mt - 1) / (16 * mt));
+  p.row_tiles = (int)((rows + 8 * nt - 1) / (8 * nt));
   p.scale_log2 = a->scale * 1.4426950408889634f;
   p.out_f32 = a->out_dtype == AF1_F32;
   p.counters = reinterpret_cast<unsigned*>(static_cast<uint8_t*>(workspace) + kCounterOffset);
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kPartOffset);
   const int ctas = std::min(c->num_sms, kMaxCtas);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  p.status = static_cast<unsigned*>(workspace);
+  p.wait_cycles = wait_budget();
   switch (c->d.kind) {
-    case AF1_KV_F16: return launch_kind<AF1_KV_F16>(p, c->d.head_dim, mt, ctas, c->max_smem, st);
-    case AF1_KV_INT8: return launch_kind<AF1_KV_INT8>(p, c->d.head_dim, mt, ctas, c->max_smem, st);
-    case AF1_KV_E4M3: return launch_kind<AF1_KV_E4M3>(p, c->d.head_dim, mt, ctas, c->max_smem, st);
-    default: return launch_kind<AF1_KV_INT4>(p, c->d.head_dim, mt, ctas, c->max_smem, st);
+    case AF1_KV_F16: return launch_kind<AF1_KV_F16>(p, *c, nt, ctas, st);
+    case AF1_KV_INT8: return launch_kind<AF1_KV_INT8>(p, *c, nt, ctas, st);
+    case AF1_KV_E4M3: return launch_kind<AF1_KV_E4M3>(p, *c, nt, ctas, st);
+    default: return launch_kind<AF1_KV_INT4>(p, *c, nt, ctas, st);
   }
 }
