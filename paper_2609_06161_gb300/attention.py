@@ -14,7 +14,7 @@ import math
 
 import torch
 
-from . import AF1_F16, AF1_F32, AF1Error, _check, _i64, _lib, _ptr, _stream_handle, _vp, last_error
+from . import AF1_F16, AF1_F32, AF1Error, _check, _i64, _lib, _ptr, _vp, last_error
 
 _i32 = ctypes.c_int32
 _f32 = ctypes.c_float
@@ -81,6 +81,13 @@ _tree_mask = _declare("af1_tree_mask", _vp, _i64, _i64, _vp, _vp)
 _tree_workspace = _declare("af1_tree_workspace_bytes", _vp, _i64, _i64, _i64, restype=_i64)
 _tree_attention = _declare("af1_tree_attention", _vp, _P(_TreeArgs), _vp, _i64, _vp)
 _token_logprobs = _declare("af1_token_logprobs", _P(_LogprobArgs), _vp)
+
+
+def _stream_handle(stream) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    # What torch.cuda.current_stream().cuda_stream gives, without building the stream object (3 us of a call's 14).
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:

@@ -9,8 +9,10 @@
 //
 // Split. An item is one sequence, one cached head and one block of 8 NT rows;
 // its keys are cut into units of kUnit, and every CTA takes an equal run of
-// the units of all items (ragged lengths balance by themselves). Inside a
-// CTA each warp takes every W-th step of KW keys of a run, with a ring of its
+// the units of all items (ragged lengths balance by themselves; each item
+// counts kSetup units more, for what a run costs whatever its length: with
+// short items uncounted, the CTA that had eight of them ran 102 us where the
+// others ran 70). Inside a CTA each warp takes every W-th step of KW keys of a run, with a ring of its
 // own in shared memory that TMA fills, its own running maximum m and sum l,
 // and an accumulator in registers; warps meet once a run, to join (m, l, o).
 // Where an item spans CTAs, each leaves its part in the workspace and the
@@ -54,6 +56,7 @@ namespace {
 
 constexpr int kUnit = 64;                         // keys of a unit
 constexpr int kMinRun = 256;                      // keys of a CTA, at least (where there are so many)
+constexpr int kSetup = 4;                         // units that a run's beginning and end are worth
 constexpr int kMaxCtas = 1024;                    // counters of the workspace
 constexpr int64_t kCounterOffset = 256;           // behind the status word's line
 constexpr int64_t kPartOffset = kCounterOffset + 4 * kMaxCtas;
@@ -268,8 +271,8 @@ __device__ __forceinline__ bool value_bad(const uint8_t* v, const uint8_t* vs, i
 }
 
 // 32 sequences at a time, one to a lane: their lengths, and their units (of
-// one cached head and row block) summed up. An item without keys has one
-// unit, that writes its zeros.
+// one cached head and row block) summed up, kSetup of them before the first
+// key of an item.
 struct Sequences {
   int first;      // of the 32
   int64_t before; // units of the sequences before them
@@ -284,7 +287,7 @@ struct Sequences {
       len = max(p.lens[i], 0);
       const int count = p.counts == nullptr ? p.nodes : min(max(p.counts[i], 0), p.nodes);
       keys = (int)min((int64_t)len + count, (int64_t)p.pages.columns << p.cache.shift);
-      units = max(1, (keys + kUnit - 1) / kUnit);
+      units = kSetup + (keys + kUnit - 1) / kUnit;
     }
     sum = units;
 #pragma unroll
@@ -310,8 +313,8 @@ struct Shape {
   static_assert((KW * C::RB) % 512 == 0, "a stage keeps the swizzle's alignment");
 };
 
-template <int KIND, int DIM, int NT, int W, int KW, int STAGES>
-__global__ void __launch_bounds__(32 * W, 1) tree_kernel(const __grid_constant__ TreeProblem p) {
+template <int KIND, int DIM, int NT, int W, int KW, int STAGES, int CTAS>
+__global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constant__ TreeProblem p) {
   using C = Kv<KIND, DIM>;
   using S = Shape<KIND, DIM, NT, W, KW, STAGES>;
   constexpr int KS = C::KS, MT = C::MT, MB = KW / 16, ROWS = S::ROWS, GROUPS = C::GROUPS;
@@ -351,7 +354,10 @@ __global__ void __launch_bounds__(32 * W, 1) tree_kernel(const __grid_constant__
   int64_t ctas = min((int64_t)gridDim.x, (total * kUnit + kMinRun - 1) / kMinRun);
   ctas = min(ctas, total);  // each has a unit at least
   if (blockIdx.x >= ctas) return;
-  const int64_t begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
+  // The first `more` CTAs have one unit more than the others.
+  const int64_t per = total / ctas, more = total - per * ctas;
+  const int64_t begin = per * blockIdx.x + min((int64_t)blockIdx.x, more);
+  const int64_t end = begin + per + (blockIdx.x < more ? 1 : 0);
 
   uint32_t phases = 0;   // of the warp's barriers
   bool alive = true;     // no wait has given up
@@ -364,10 +370,25 @@ __global__ void __launch_bounds__(32 * W, 1) tree_kernel(const __grid_constant__
     const int64_t seq_first = (sq.before + __shfl_sync(0xffffffffu, sq.sum, which) - units) * lanes;
     const int item = (int)((pos - seq_first) / units);
     const int64_t first = seq_first + (int64_t)item * units;  // the item's first unit
-    const int u0 = (int)(pos - first), u1 = (int)min((int64_t)units, u0 + (end - pos));
+    const int from = (int)(pos - first), to = (int)min((int64_t)units, from + (end - pos));
+    const int u0 = max(from - kSetup, 0), u1 = to - kSetup;  // units of keys
+    pos += to - from;
     const int head = item / p.row_tiles, tile = item - head * p.row_tiles;
     const int rows = min(ROWS, p.nodes * p.group - tile * ROWS);
     const int k_begin = u0 * kUnit, k_end = min(u1 * kUnit, keys);
+
+    if (keys == 0 && from == 0) {  // nothing to see: the item's first CTA writes its zeros
+      for (int i = threadIdx.x; i < rows * DIM; i += 32 * W) {
+        const int lr = i / DIM, e = i % DIM, gr = tile * ROWS + lr, node = gr / p.group;
+        const int h = head * p.group + gr - node * p.group;
+        const int64_t at = seq * p.o_seq + node * p.o_node + h * p.o_head + e;
+        if (p.out_f32) static_cast<float*>(p.out)[at] = 0.f;
+        else static_cast<__half*>(p.out)[at] = __ushort_as_half(0);
+        if (e == 0 && p.lse != nullptr)
+          p.lse[((int64_t)seq * p.nodes + node) * p.cache.heads * p.group + h] = -kInf;
+      }
+    }
+    if (u1 <= 0) continue;
 
     // -- copies -------------------------------------------------------------
     constexpr int STRIDE = W * KW;
@@ -420,17 +441,7 @@ __global__ void __launch_bounds__(32 * W, 1) tree_kernel(const __grid_constant__
         }
       }
     };
-    int issued = 0;  // steps of this run
     fetch_pages(key0);
-#pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) {
-      const int key = key0 + s * STRIDE;
-      if (key < k_end && alive) {
-        issue(key, s);
-        ++issued;
-        fetch_pages(key + STRIDE);
-      }
-    }
 
     // -- q: the b operands, and its sums over the entries of a group -----------
     uint32_t qf[NT <= 2 ? NT : 1][KS][2];
@@ -492,7 +503,18 @@ __global__ void __launch_bounds__(32 * W, 1) tree_kernel(const __grid_constant__
         }
       }
     }
-    if constexpr (NT > 2) __syncthreads();
+
+    int issued = 0;  // steps of this run
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+      const int key = key0 + s * STRIDE;
+      if (key < k_end && alive) {
+        issue(key, s);
+        ++issued;
+        fetch_pages(key + STRIDE);
+      }
+    }
+    if constexpr (NT > 2) __syncthreads();  // qs
 
     // o^T: block m, column block nt: entries row_entry(m, g, i / 2) of rows 2 t + i % 2.
     float o[MT][NT][4], m[NT][2], l[NT][2], vref = 0.f;
@@ -827,6 +849,8 @@ __global__ void __launch_bounds__(32 * W, 1) tree_kernel(const __grid_constant__
     __syncthreads();  // every warp is done with its ring
 
     // -- join the warps' parts -------------------------------------------------------
+    // Entry e of row lr is kept at e ^ 8 (lr / 2 % 4): the lanes of a store
+    // then write different banks.
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -836,86 +860,114 @@ __global__ void __launch_bounds__(32 * W, 1) tree_kernel(const __grid_constant__
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int lr = nt * 8 + 2 * t + i;
         if (g == 0) join_m[warp][lr] = m[nt][i], join_l[warp][lr] = sum;
-        float* to = join + (warp * ROWS + lr) * DIM;
+        if (lr >= rows) continue;
+        float* to_row = join + (warp * ROWS + lr) * DIM;
+        const float f = C::SCALED8 ? vref : 1.f;
+        if constexpr (KIND == AF1_KV_F16) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          const float f = C::SCALED8 ? vref : 1.f;
-          if (lr < rows) {
-            to[C::row_entry(mt, g, 0)] = o[mt][nt][i] * f;
-            to[C::row_entry(mt, g, 1)] = o[mt][nt][2 + i] * f;
+          for (int mt = 0; mt < MT; ++mt) {
+            to_row[C::row_entry(mt, g, 0) ^ (8 * t)] = o[mt][nt][i];
+            to_row[C::row_entry(mt, g, 1) ^ (8 * t)] = o[mt][nt][2 + i];
           }
+        } else if constexpr (INT4) {
+#pragma unroll
+          for (int mt = 0; mt < MT; mt += 2)
+            *reinterpret_cast<float4*>(to_row + (C::row_entry(mt, g, 0) ^ (8 * t))) =
+                make_float4(o[mt][nt][i], o[mt + 1][nt][i], o[mt][nt][2 + i], o[mt + 1][nt][2 + i]);
+        } else {
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+            *reinterpret_cast<float2*>(to_row + (C::row_entry(mt, g, 0) ^ (8 * t))) =
+                make_float2(o[mt][nt][i] * f, o[mt][nt][2 + i] * f);
         }
       }
     __syncthreads();
-    const bool whole = u0 == 0 && u1 == units;
-    // Parts of an item: a CTA leaves at most two, of its first run and of its
-    // last one. CTAs c0 .. c1 hold the item's units; all but c0 begin inside it.
+    const bool whole = u0 == 0 && to == units;
+    // Parts of an item: CTAs c0 .. c1 hold its units of keys. A CTA leaves at
+    // most two, in its first run (of an item that began before) and in its
+    // last one (of an item that it is the first to hold).
     auto holder = [&](int64_t u) {
-      int64_t c = u * ctas / total;
-      while (total * (c + 1) / ctas <= u) ++c;
-      return (int)c;
+      const int64_t large = more * (per + 1);
+      return (int)(u < large ? u / (per + 1) : more + (u - large) / per);
     };
     int c0 = 0, c1 = 0;
-    if (!whole) c0 = holder(first), c1 = holder(first + units - 1);
-    const int c0_place = whole || total * c0 / ctas == first ? 0 : 1;
-    auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? c0_place : 0)) * S::PART; };
+    if (!whole) c0 = holder(first + kSetup), c1 = holder(first + units - 1);
+    auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * S::PART; };
     float* part = part_of(blockIdx.x);
     const int live_nodes = p.counts == nullptr ? p.nodes : min(max(p.counts[seq], 0), p.nodes);
-    auto finish = [&](int lr, int e, float mx, float sum, float acc) {
+    auto finish = [&](int lr, int e, float mx, float sum, float4 acc) {
       const int gr = tile * ROWS + lr, node = gr / p.group, h = head * p.group + gr - node * p.group;
       const bool live = node < live_nodes && sum != 0.f;
-      const float y = live ? acc / sum : 0.f;
+      const float f = live ? 1.f / sum : 0.f;
+      const float4 y = live ? make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f) : make_float4(0.f, 0.f, 0.f, 0.f);
       const int64_t at = seq * p.o_seq + node * p.o_node + h * p.o_head + e;
-      if (p.out_f32) static_cast<float*>(p.out)[at] = y;
-      else static_cast<__half*>(p.out)[at] = __float2half_rn(y);
+      if (p.out_f32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = y;
+      else
+        *reinterpret_cast<uint2*>(static_cast<__half*>(p.out) + at) =
+            make_uint2(pack_half2(y.x, y.y), pack_half2(y.z, y.w));
       if (e == 0 && p.lse != nullptr)
         p.lse[((int64_t)seq * p.nodes + node) * p.cache.heads * p.group + h] =
             live ? (mx - kShift + log2f(sum)) * 0.69314718056f : -kInf;
     };
-    for (int i = threadIdx.x; i < rows * DIM; i += 32 * W) {
-      const int lr = i / DIM, e = i % DIM;
+    auto add = [](float4& acc, float f, const float4& x) {
+      acc.x = fmaf(f, x.x, acc.x), acc.y = fmaf(f, x.y, acc.y), acc.z = fmaf(f, x.z, acc.z), acc.w = fmaf(f, x.w, acc.w);
+    };
+    for (int i = threadIdx.x; i < rows * (DIM / 4); i += 32 * W) {
+      const int lr = i / (DIM / 4), e = i % (DIM / 4) * 4;
       float mx = -kInf;
 #pragma unroll
       for (int w = 0; w < W; ++w) mx = fmaxf(mx, join_m[w][lr]);
       const float zero = mx == -kInf ? 0.f : mx;
-      float sum = 0.f, acc = 0.f;
+      float sum = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < W; ++w) {
         const float f = ex2(join_m[w][lr] - zero);
-        sum += f * join_l[w][lr];
-        acc += f * join[(w * ROWS + lr) * DIM + e];
+        sum = fmaf(f, join_l[w][lr], sum);
+        add(acc, f, *reinterpret_cast<const float4*>(join + (w * ROWS + lr) * DIM + (e ^ (8 * (lr / 2 % 4)))));
       }
       if (whole) {
         finish(lr, e, mx, sum, acc);
       } else {
-        part[lr * DIM + e] = acc;
-        if (e == 0) part[ROWS * DIM + lr] = mx, part[ROWS * DIM + ROWS + lr] = sum;
+        *reinterpret_cast<float4*>(part + lr * DIM + e) = acc;
+        if (e == 0) *reinterpret_cast<float2*>(part + ROWS * DIM + 2 * lr) = make_float2(mx, sum);
       }
     }
     if (!whole) {
-      __threadfence();
       __syncthreads();
-      if (threadIdx.x == 0) {
+      if (threadIdx.x == 0) {  // the CTA's writes above are released with it
         const unsigned arrived = atom_add_acq_rel_gpu(&p.counters[c0], 1u);
         last_shared = arrived == (unsigned)(c1 - c0);
         if (last_shared) p.counters[c0] = 0;  // as the next call finds it
       }
       __syncthreads();
       if (last_shared) {
-        __threadfence();
-        for (int i = threadIdx.x; i < rows * DIM; i += 32 * W) {
-          const int lr = i / DIM, e = i % DIM;
-          float mx = -kInf, sum = 0.f, acc = 0.f;
-#pragma unroll 4
-          for (int c = c0; c <= c1; ++c) {
-            const float* from = part_of(c);
-            const float pm = __ldcg(from + ROWS * DIM + lr), pl = __ldcg(from + ROWS * DIM + ROWS + lr);
-            const float po = __ldcg(from + lr * DIM + e);
-            const float now = fmaxf(mx, pm);
+        for (int i = threadIdx.x; i < rows * (DIM / 4); i += 32 * W) {
+          const int lr = i / (DIM / 4), e = i % (DIM / 4) * 4;
+          float mx = -kInf, sum = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int c = c0; c <= c1; c += 4) {  // four parts' loads in flight
+            float2 ml[4];
+            float4 x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float* from = part_of(min(c + j, c1));
+              ml[j] = __ldcg(reinterpret_cast<const float2*>(from + ROWS * DIM + 2 * lr));
+              x[j] = __ldcg(reinterpret_cast<const float4*>(from + lr * DIM + e));
+            }
+            float now = mx;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) now = fmaxf(now, ml[j].x);
             const float zero = now == -kInf ? 0.f : now;
-            const float fa = ex2(mx - zero), fb = ex2(pm - zero);
-            sum = sum * fa + pl * fb;
-            acc = acc * fa + po * fb;
+            const float f = ex2(mx - zero);
+            sum *= f, acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (c + j > c1) continue;
+              const float fj = ex2(ml[j].x - zero);
+              sum = fmaf(fj, ml[j].y, sum);
+              add(acc, fj, x[j]);
+            }
             mx = now;
           }
           finish(lr, e, mx, sum, acc);
@@ -925,7 +977,6 @@ __global__ void __launch_bounds__(32 * W, 1) tree_kernel(const __grid_constant__
     // The rings, written through the generic proxy above, go back to TMA.
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
-    pos += u1 - u0;
   }
 }
 
@@ -935,17 +986,17 @@ int fail(int code, const std::string& msg) { return set_error(code, "af1_tree_at
 int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
 
 int64_t workspace_bytes(const af1_kv_cache& c, int64_t rows) {
-  const int64_t ctas = std::min(c.num_sms, kMaxCtas);
+  const int64_t ctas = std::min(3 * c.num_sms, kMaxCtas);  // at most three CTAs to an SM
   return kPartOffset + 2 * ctas * (8 * row_blocks(rows)) * (c.d.head_dim + 2) * 4;
 }
 
-template <int KIND, int DIM, int NT, int W, int KW, int STAGES>
-int launch(const TreeProblem& p, int ctas, cudaStream_t st) {
+template <int KIND, int DIM, int NT, int W, int KW, int STAGES, int CTAS>
+int launch(const TreeProblem& p, int sms, cudaStream_t st) {
   constexpr int smem = Shape<KIND, DIM, NT, W, KW, STAGES>::SMEM;
-  auto kernel = tree_kernel<KIND, DIM, NT, W, KW, STAGES>;
+  auto kernel = tree_kernel<KIND, DIM, NT, W, KW, STAGES, CTAS>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e == cudaSuccess) {
-    kernel<<<ctas, 32 * W, smem, st>>>(p);
+    kernel<<<std::min(sms * CTAS, kMaxCtas), 32 * W, smem, st>>>(p);
     e = cudaGetLastError();
   }
   if (e != cudaSuccess) return fail(AF1_ERR_CUDA, std::string(cudaGetErrorName(e)) + " (" + cudaGetErrorString(e) + ")");
@@ -955,29 +1006,30 @@ int launch(const TreeProblem& p, int ctas, cudaStream_t st) {
 
 // Warps, keys of a step and stages of a kind: what fills the shared memory.
 template <int KIND, int DIM, int NT>
-int launch_rows(TreeProblem& p, const af1_kv_cache& c, int ctas, cudaStream_t st) {
+int launch_rows(TreeProblem& p, const af1_kv_cache& c, cudaStream_t st) {
   constexpr int RB = kv_row_bytes(KIND, DIM);
   constexpr int KW = RB >= 256 ? 16 : 32;
-  constexpr int W = NT == 4 ? 8 : 12;
+  constexpr int W = NT == 4 ? 8 : 4;
+  constexpr int CTAS = NT == 4 ? 1 : 3;
   constexpr int BYTES = 2 * KW * (RB + kv_scale_bytes(KIND, DIM)) * W;
-  constexpr int FIT = 215 * 1024 / BYTES;
+  constexpr int FIT = (222 * 1024 / CTAS - 4096) / BYTES;
   constexpr int STAGES = FIT > 4 ? 4 : FIT;
   static_assert(STAGES >= 2, "");
   const int box = std::min(c.d.page_size, KW);
   p.k_map = box == 16 ? c.k16 : c.k32;
   p.v_map = box == 16 ? c.v16 : c.v32;
-  return launch<KIND, DIM, NT, W, KW, STAGES>(p, ctas, st);
+  return launch<KIND, DIM, NT, W, KW, STAGES, CTAS>(p, c.num_sms, st);
 }
 
 template <int KIND>
-int launch_kind(TreeProblem& p, const af1_kv_cache& c, int nt, int ctas, cudaStream_t st) {
+int launch_kind(TreeProblem& p, const af1_kv_cache& c, int nt, cudaStream_t st) {
   if (c.d.head_dim == 128)
-    return nt == 1   ? launch_rows<KIND, 128, 1>(p, c, ctas, st)
-           : nt == 2 ? launch_rows<KIND, 128, 2>(p, c, ctas, st)
-                     : launch_rows<KIND, 128, 4>(p, c, ctas, st);
-  return nt == 1   ? launch_rows<KIND, 64, 1>(p, c, ctas, st)
-         : nt == 2 ? launch_rows<KIND, 64, 2>(p, c, ctas, st)
-                   : launch_rows<KIND, 64, 4>(p, c, ctas, st);
+    return nt == 1   ? launch_rows<KIND, 128, 1>(p, c, st)
+           : nt == 2 ? launch_rows<KIND, 128, 2>(p, c, st)
+                     : launch_rows<KIND, 128, 4>(p, c, st);
+  return nt == 1   ? launch_rows<KIND, 64, 1>(p, c, st)
+         : nt == 2 ? launch_rows<KIND, 64, 2>(p, c, st)
+                   : launch_rows<KIND, 64, 4>(p, c, st);
 }
 
 bool sizes_ok(const af1_kv_cache* c, int64_t sequences, int64_t nodes, int64_t q_heads) {
@@ -1053,14 +1105,13 @@ int af1_tree_attention(const af1_kv_cache* c, const af1_tree_args* a, void* work
   p.out_f32 = a->out_dtype == AF1_F32;
   p.counters = reinterpret_cast<unsigned*>(static_cast<uint8_t*>(workspace) + kCounterOffset);
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kPartOffset);
-  const int ctas = std::min(c->num_sms, kMaxCtas);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   p.status = static_cast<unsigned*>(workspace);
   p.wait_cycles = wait_budget();
   switch (c->d.kind) {
-    case AF1_KV_F16: return launch_kind<AF1_KV_F16>(p, *c, nt, ctas, st);
-    case AF1_KV_INT8: return launch_kind<AF1_KV_INT8>(p, *c, nt, ctas, st);
-    case AF1_KV_E4M3: return launch_kind<AF1_KV_E4M3>(p, *c, nt, ctas, st);
-    default: return launch_kind<AF1_KV_INT4>(p, *c, nt, ctas, st);
+    case AF1_KV_F16: return launch_kind<AF1_KV_F16>(p, *c, nt, st);
+    case AF1_KV_INT8: return launch_kind<AF1_KV_INT8>(p, *c, nt, st);
+    case AF1_KV_E4M3: return launch_kind<AF1_KV_E4M3>(p, *c, nt, st);
+    default: return launch_kind<AF1_KV_INT4>(p, *c, nt, st);
   }
 }
