@@ -738,7 +738,7 @@ typedef struct af1_logprob_args {
   int32_t* top_ids;
   int32_t top;        /* 0 .. 32, at most vocab */
   int32_t dtype;      /* AF1_F16 or AF1_F32 */
-  float temperature;  /* > 0 */
+  float temperature;  /* 1e-30 .. 1e30 */
   int32_t reserved;   /* must be 0 */
 } af1_logprob_args;
 AF1_API int af1_token_logprobs(const af1_logprob_args* args, void* stream);

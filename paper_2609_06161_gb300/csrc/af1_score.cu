@@ -1,22 +1,28 @@
 // af1_score.cu — log-probabilities of given tokens, entropy and the largest
 // alternatives of rows of logits, in one pass over the logits.
 //
-// With y = x / temperature, a thread keeps m = max x, S = sum 2^d and
-// T = sum 2^d d over its entries, d = (x - m) log2(e) / temperature, and
-// follows a new maximum by S' = f S, T' = f (T + S delta). Then
+// With y = x log2(e) / temperature, a thread keeps a reference r (y of the
+// largest x so far), S = sum 2^d and T = sum 2^d d over its entries, d = y - r,
+// and follows a new maximum by S' = f S, T' = f (T + S delta). Then
 //   log p = (d - log2 S) ln 2,   entropy = (log2 S - T / S) ln 2.
+// For FP16, d is one fused multiply-add of x, and r the rounded y; FP32 logits
+// may be so large that y overflows, so there r is x itself and d the scaled
+// difference.
 //
 // The largest entries: each warp keeps its 32 largest so far, one to a lane,
 // in order. Keys of 64 bits (the value as an ordered integer, then the index,
 // inverted) make the order total, so that equal values go by index and the
 // result does not depend on which thread saw what first. An entry is looked
-// at again only where it may be among the `top`: not below the `top`-th of
-// any warp of its CTA, which the warps share.
+// at again only where it may be among the `top`: it is not below the `top`-th
+// of its warp, nor below what all warps of the CTA have ceil(top / warps) of
+// (then `top` entries are as large). A warp's first bound is the `top`-th
+// largest of its lanes' maxima.
 //
-// A cluster of CTAs takes a row (one where there are rows enough to fill the
-// GPU), and its first CTA joins their statistics and lists through
-// distributed shared memory. Device memory bounds large calls: one exponent
-// and about eight instructions an entry.
+// A cluster of CTAs takes a row (one CTA where there are rows enough to fill
+// the GPU), and its first CTA joins their statistics and lists through
+// distributed shared memory. Device memory bounds large calls: an entry costs
+// one exponent and about five instructions (pairs of entries share FP32
+// additions and multiply-adds).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -31,7 +37,7 @@ namespace cg = cooperative_groups;
 namespace af1 {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxCluster = 8;
 constexpr float kInf = __builtin_huge_valf();
@@ -45,7 +51,6 @@ struct ScoreProblem {
   int32_t* top_ids;
   int top;
   float c;      // log2(e) / temperature
-  float inv_t;  // 1 / temperature
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -53,24 +58,63 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Two FP32 operations in one instruction.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return d;
+}
 
+constexpr float kLeast = -1e4f;  // 2^d is 0 from far above on; d itself may be -infinity
+
+// r is -infinity where nothing is summed (or NaN alone).
 struct Stats {
-  float m = -kInf, s = 0.f, t = 0.f;
+  float r = -kInf, s = 0.f, t = 0.f;
 };
+// The reference of a value, and the distance of two references.
+template <typename T>
+__device__ __forceinline__ float reference(float x, float c) {
+  return sizeof(T) == 2 ? x * c : x;
+}
+template <typename T>
+__device__ __forceinline__ float distance(float a, float b, float c) {
+  return sizeof(T) == 2 ? a - b : (a - b) * c;
+}
+template <typename T>
+__device__ __forceinline__ float depth(float x, float r, float c) {  // d of a value
+  return sizeof(T) == 2 ? fmaf(x, c, -r) : (x - r) * c;
+}
 
 // The two sets of entries together.
+template <typename T>
 __device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float c) {
-  Stats r;
-  r.m = fmaxf(a.m, b.m);
-  if (r.m == -kInf) {
-    r.s = a.s + b.s, r.t = 0.f;  // nothing, or NaN
-    return r;
+  Stats o;
+  o.r = fmaxf(a.r, b.r);
+  if (o.r == -kInf) {
+    o.s = a.s + b.s, o.t = 0.f;  // nothing, or NaN
+    return o;
   }
-  const float da = fmaxf((a.m - r.m) * c, -1e4f), db = fmaxf((b.m - r.m) * c, -1e4f);
+  const float da = fmaxf(distance<T>(a.r, o.r, c), kLeast), db = fmaxf(distance<T>(b.r, o.r, c), kLeast);
   const float fa = ex2(da), fb = ex2(db);
-  r.s = a.s * fa + b.s * fb;
-  r.t = fa * (a.t + a.s * da) + fb * (b.t + b.s * db);
-  return r;
+  o.s = a.s * fa + b.s * fb;
+  o.t = fa * (a.t + a.s * da) + fb * (b.t + b.s * db);
+  return o;
 }
 
 // Larger for larger values (NaN largest, -0 as 0), then for smaller indices; never 0.
@@ -83,8 +127,21 @@ __device__ __forceinline__ float key_value(uint64_t key) {
   const uint32_t k = (uint32_t)(key >> 32);
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
-__device__ __forceinline__ float key_bound(uint64_t key) {  // entries below it cannot matter
-  return key == 0 ? -kInf : key_value(key);
+// Entries below it cannot come before the key (-infinity for NaN or no key: none is).
+__device__ __forceinline__ float key_bound(uint64_t key) {
+  const float v = key_value(key);
+  return key == 0 || v != v ? -kInf : v;
+}
+__device__ __forceinline__ float sort_descending(float x, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+    for (int d = size / 2; d > 0; d >>= 1) {
+      const float other = __shfl_xor_sync(0xffffffffu, x, d);
+      const bool down = size == 32 || (lane & size) == 0;
+      x = ((lane & d) == 0) == down ? fmaxf(x, other) : fminf(x, other);
+    }
+  return x;
 }
 
 // One key to a lane: descending.
@@ -110,12 +167,14 @@ __device__ __forceinline__ uint64_t merge_lists(uint64_t a, uint64_t b, int lane
 }
 
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__ ScoreProblem p) {
+__global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constant__ ScoreProblem p) {
   constexpr int E = 16 / (int)sizeof(T);  // entries of a 16-byte access
-  constexpr int U = 16 / E;               // accesses of a batch: 16 entries to a lane
+  constexpr int U = 4;                    // accesses of a batch: 16 or 32 entries to a lane
+  constexpr bool HALF = sizeof(T) == 2;
   __shared__ Stats stats[kWarps];
   __shared__ uint64_t lists[kWarps][32];
-  __shared__ int bound_shared;  // largest `top`-th entry of a warp, as an ordered integer
+  __shared__ uint4 stage[TOP ? kWarps : 1][U][32];  // a batch whose entries are looked at again
+  __shared__ volatile float share[kWarps];  // the ceil(top / kWarps)-th entry of each warp
   cg::cluster_group cluster = cg::this_cluster();
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -128,20 +187,39 @@ __global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__
   const int head = (int)min((int64_t)((16 - (uintptr_t)x % 16) % 16 / sizeof(T)), p.vocab);
   const int64_t nvec = (p.vocab - head) / E;
   const uint4* body = reinterpret_cast<const uint4*>(x + head);
-
-  if (threadIdx.x == 0) bound_shared = (int)0x80000000;
-  __syncthreads();
+  auto load = [&](uint4 (&w)[U], int64_t batch) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = batch * (32 * U) + u * 32 + lane;
+      if (i < nvec) w[u] = __ldcs(body + i);
+    }
+  };
+  const int64_t batches = (nvec + 32 * U - 1) / (32 * U);
+  const int64_t first = rank * kWarps + warp, step = (int64_t)cs * kWarps;
+  uint4 next[2][U];  // two batches ahead
+  load(next[0], first);
+  load(next[1], first + step);
+  // The first given tokens' logits, for the end.
+  float given = -kInf;
+  if (rank == 0 && warp == 0 && lane < p.given) {
+    const int id = p.tokens[row * p.given + lane];
+    if (id >= 0 && id < p.vocab) given = (float)x[id];
+  }
+  if constexpr (TOP) {
+    if (lane == 0) share[warp] = -kInf;
+    __syncthreads();
+  }
 
   Stats st;
-  uint64_t mine = 0;             // this lane's entry of the warp's list
-  uint64_t kth = 0;              // its `top`-th
-  float bound = -kInf;           // entries below it cannot be among the `top`
+  uint64_t mine = 0;    // this lane's entry of the warp's list
+  uint64_t kth = 0;     // its `top`-th
+  float bound = -kInf;  // entries below it cannot be among the `top`
   auto consider = [&](float v, bool real, uint32_t index) {
-    const bool maybe = real && !(v < bound);
-    const uint64_t key = maybe ? order_key(v, index) : 0;
+    if (__ballot_sync(0xffffffffu, real && !(v < bound)) == 0) return;
+    const uint64_t key = real && !(v < bound) ? order_key(v, index) : 0;
     unsigned want = __ballot_sync(0xffffffffu, key > kth);
     if (want == 0) return;
-    if (__popc(want) > 6) {
+    if (__popc(want) > 8) {
       mine = merge_lists(mine, warp_sort(key, lane), lane);
     } else {
       while (want != 0) {
@@ -157,65 +235,100 @@ __global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__
     bound = fmaxf(bound, key_bound(kth));
   };
 
-  auto load = [&](uint4 (&w)[U], int64_t batch) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t i = batch * (32 * U) + u * 32 + lane;
-      if (i < nvec) w[u] = __ldcs(body + i);
-    }
-  };
-  const int64_t batches = (nvec + 32 * U - 1) / (32 * U);
-  const int64_t first = rank * kWarps + warp, step = (int64_t)cs * kWarps;
-  uint4 next[U];
-  load(next, first);
-  for (int64_t b = first; b < batches; b += step) {
+  auto pass = [&](int64_t b, uint4 (&ahead)[U]) {
     uint4 w[U];
+    const int64_t left = nvec - b * (32 * U) - lane;  // accesses of this lane: those u with 32 u < left
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = next[u];
-    if (b + step < batches) load(next, b + step);
-    float v[16];
+    for (int u = 0; u < U; ++u) w[u] = ahead[u];
+    load(ahead, b + 2 * step);
+    if ((b + 1) * (32 * U) > nvec) {  // the last, in part: -infinity changes nothing
+      const uint32_t none = HALF ? 0xfc00fc00u : 0xff800000u;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const T* e = reinterpret_cast<const T*>(&w[u]);
-      const bool real = b * (32 * U) + u * 32 + lane < nvec;
-#pragma unroll
-      for (int i = 0; i < E; ++i) v[u * E + i] = real ? (float)e[i] : -kInf;
+      for (int u = 0; u < U; ++u)
+        if (32 * u >= left) w[u] = make_uint4(none, none, none, none);
     }
-    float top = v[0];
+    float top;
+    if constexpr (HALF) {
+      __half2 most = __half2half2(__ushort_as_half(0xfc00));
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, v[i]);
-    if (top > st.m) {
-      const float d = fmaxf((st.m - top) * c, -1e4f), f = ex2(d);
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = __hmax2(most, reinterpret_cast<const __half2*>(&w[u])[i]);
+      top = fmaxf(__low2float(most), __high2float(most));
+    } else {
+      top = -kInf;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, reinterpret_cast<const float*>(&w[u])[i]);
+    }
+    const float r = reference<T>(top, c);
+    if (r > st.r) {
+      const float d = fmaxf(distance<T>(st.r, r, c), kLeast), f = ex2(d);
       st.t = f * (st.t + st.s * d);
       st.s *= f;
-      st.m = top;
+      st.r = r;
     }
-    const float mx = st.m == -kInf ? 0.f : st.m;
+    const float minus = st.r == -kInf ? 0.f : -st.r;
+    float2 s2 = make_float2(st.s, 0.f), t2 = make_float2(st.t, 0.f);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      // The difference first: the products alone may overflow.
-      const float d = (v[i] - mx) * c, e = ex2(d);
-      st.s += e;
-      st.t = fmaf(e, fmaxf(d, -1e4f), st.t);
-    }
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) {
+        const float2 v = HALF ? __half22float2(reinterpret_cast<const __half2*>(&w[u])[i])
+                              : reinterpret_cast<const float2*>(&w[u])[i];
+        const float2 d = HALF ? fma2(v, make_float2(c, c), make_float2(minus, minus))
+                              : mul2(add2(v, make_float2(minus, minus)), make_float2(c, c));
+        const float2 e = make_float2(ex2(d.x), ex2(d.y));
+        s2 = add2(s2, e);
+        t2 = fma2(e, make_float2(fmaxf(d.x, kLeast), fmaxf(d.y, kLeast)), t2);
+      }
+    st.s = s2.x + s2.y;
+    st.t = t2.x + t2.y;
     if constexpr (TOP) {
-      const int shared = *static_cast<volatile int*>(&bound_shared);
-      bound = fmaxf(bound, __int_as_float(shared < 0 ? shared ^ 0x7fffffff : shared));
-      bool any = false;  // also where a NaN hides the maximum
+      if (b == first) {
+        const float sorted = sort_descending(top, lane);
+        bound = fmaxf(bound, __shfl_sync(0xffffffffu, sorted, p.top - 1));
+      }
+      // A NaN hides from the maximum, and shows in the sum.
+      if (__any_sync(0xffffffffu, !(top < bound) || st.s != st.s)) {
+        float least = lane < kWarps ? (float)share[lane] : kInf;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) any |= !(v[i] < bound);
-      if (__any_sync(0xffffffffu, any)) {
+        for (int d = 1; d < kWarps; d <<= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, d));
+        bound = fmaxf(bound, __shfl_sync(0xffffffffu, least, 0));
+        if (__any_sync(0xffffffffu, !(top < bound) || st.s != st.s)) {
+          // Bit 16 h + i: entry h of pair i; entry by entry from shared memory.
+          uint32_t maybe = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int64_t vec = b * (32 * U) + (i / E) * 32 + lane;
-          consider(v[i], vec < nvec, (uint32_t)(head + vec * E + i % E));
-        }
-        if (lane == 0) {
-          const int o = __float_as_int(bound);
-          atomicMax(&bound_shared, o < 0 ? o ^ 0x7fffffff : o);
+          for (int u = 0; u < U; ++u) {
+            stage[warp][u][lane] = w[u];
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+              const int at = u * (E / 2) + i;
+              if constexpr (HALF) {
+                const uint32_t below = __hlt2_mask(reinterpret_cast<const __half2*>(&w[u])[i], __float2half2_rn(bound));
+                maybe |= (~below & 0x00010001u) << at;
+              } else {
+                const float2 v = reinterpret_cast<const float2*>(&w[u])[i];
+                maybe |= (v.x < bound ? 0u : 1u << at) | (v.y < bound ? 0u : 0x10000u << at);
+              }
+            }
+          }
+          while (__any_sync(0xffffffffu, maybe != 0)) {
+            const int bit = maybe != 0 ? __ffs(maybe) - 1 : 0, u = (bit % 16) / (E / 2), i = 2 * (bit % (E / 2)) + bit / 16;
+            const float v = (float)reinterpret_cast<const T*>(&stage[warp][u][lane])[i];
+            consider(v, maybe != 0 && 32 * u < left, (uint32_t)(head + (b * (32 * U) + u * 32 + lane) * E + i));
+            maybe &= maybe - 1;
+          }
+          const uint64_t part = __shfl_sync(0xffffffffu, mine, (p.top + kWarps - 1) / kWarps - 1);
+          if (lane == 0) share[warp] = key_bound(part);
         }
       }
     }
+  };
+  for (int64_t b = first; b < batches; b += 2 * step) {
+    pass(b, next[0]);
+    if (b + step < batches) pass(b + step, next[1]);
   }
   if (rank == 0 && warp == 0) {  // the ends: fewer than 2 E entries
     const int64_t tail = p.vocab - head - nvec * E;
@@ -223,8 +336,8 @@ __global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__
     const bool real = lane < head + tail;
     const float v = real ? (float)x[i] : -kInf;
     Stats one;
-    if (real) one.m = v, one.s = v == -kInf ? 0.f : ex2((v - v) * c);
-    st = join(st, one, c);
+    if (real) one.r = reference<T>(v, c), one.s = v == -kInf ? 0.f : ex2(v - v);
+    st = join<T>(st, one, c);
     if constexpr (TOP) consider(v, real, (uint32_t)i);
   }
 
@@ -232,10 +345,10 @@ __global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) {
     Stats other;
-    other.m = __shfl_xor_sync(0xffffffffu, st.m, d);
+    other.r = __shfl_xor_sync(0xffffffffu, st.r, d);
     other.s = __shfl_xor_sync(0xffffffffu, st.s, d);
     other.t = __shfl_xor_sync(0xffffffffu, st.t, d);
-    st = join(st, other, c);
+    st = join<T>(st, other, c);
   }
   if (lane == 0) stats[warp] = st;
   if constexpr (TOP) lists[warp][lane] = mine;
@@ -252,7 +365,8 @@ __global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__
   }
   if (warp == 0) {
     st = stats[0];
-    for (int w = 1; w < kWarps; ++w) st = join(st, stats[w], c);
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) st = join<T>(st, stats[w], c);
     if (cs > 1) {
       __syncwarp();
       if (lane == 0) stats[0] = st;
@@ -262,9 +376,19 @@ __global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__
   if (cs > 1) {
     cluster.sync();
     if (rank == 0 && warp == 0) {
-      for (int r = 1; r < cs; ++r) {
-        st = join(st, *cluster.map_shared_rank(&stats[0], r), c);
-        if constexpr (TOP) mine = merge_lists(mine, cluster.map_shared_rank(&lists[0][0], r)[lane], lane);
+      Stats far[kMaxCluster - 1];
+      uint64_t far_list[kMaxCluster - 1];
+#pragma unroll
+      for (int i = 0; i < kMaxCluster - 1; ++i) {
+        if (i + 1 >= cs) break;
+        far[i] = *cluster.map_shared_rank(&stats[0], i + 1);
+        if constexpr (TOP) far_list[i] = cluster.map_shared_rank(&lists[0][0], i + 1)[lane];
+      }
+#pragma unroll
+      for (int i = 0; i < kMaxCluster - 1; ++i) {
+        if (i + 1 >= cs) break;
+        st = join<T>(st, far[i], c);
+        if constexpr (TOP) mine = merge_lists(mine, far_list[i], lane);
       }
     }
     cluster.sync();  // the other CTAs' shared memory is read until here
@@ -272,12 +396,20 @@ __global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__
   if (rank != 0 || warp != 0) return;
   const float ln2 = 0.6931471805599453f;
   const float log_s = st.s > 0.f || st.s != st.s ? log2f(st.s) : -kInf;
-  auto logprob = [&](float v) { return v == -kInf && st.s == st.s ? -kInf : fmaf(v - st.m, p.inv_t, -log_s * ln2); };
+  const float none = -kInf;
+  auto logprob = [&](float v) {
+    if (v == none && st.s == st.s) return none;
+    // FP32: the difference over the temperature, which does not overflow where its multiple by log2(e) would.
+    return HALF ? (depth<T>(v, st.r, c) - log_s) * ln2 : fmaf(v - st.r, c * ln2, -log_s * ln2);
+  };
   if (lane == 0 && p.entropy != nullptr)
-    p.entropy[row] = st.m == -kInf && st.s == st.s ? 0.f : (log_s - st.t / st.s) * ln2;
+    p.entropy[row] = st.r == -kInf && st.s == st.s ? 0.f : (log_s - st.t / st.s) * ln2;
   for (int i = lane; i < p.given; i += 32) {
-    const int id = p.tokens[row * p.given + i];
-    const float v = id >= 0 && id < p.vocab ? (float)x[id] : -kInf;
+    float v = given;
+    if (i >= 32) {
+      const int id = p.tokens[row * p.given + i];
+      v = id >= 0 && id < p.vocab ? (float)x[id] : -kInf;
+    }
     p.logprobs[row * p.given + i] = logprob(v);
   }
   if constexpr (TOP) {
@@ -318,8 +450,8 @@ int af1_token_logprobs(const af1_logprob_args* a, void* stream) {
     return fail(AF1_ERR_INVALID_ARG, "need rows 0..2^24, vocab 1..2^31 - 1, vocab <= ld <= 2^36");
   if (a->dtype != AF1_F16 && a->dtype != AF1_F32) return fail(AF1_ERR_INVALID_ARG, "dtype must be AF1_F16 or AF1_F32");
   if (a->reserved != 0) return fail(AF1_ERR_INVALID_ARG, "reserved must be 0");
-  if (!(a->temperature > 0.f) || !(a->temperature < kInf) || !(1.f / a->temperature < kInf))
-    return fail(AF1_ERR_INVALID_ARG, "temperature must be positive and finite");
+  if (!(a->temperature >= 1e-30f) || !(a->temperature <= 1e30f))
+    return fail(AF1_ERR_INVALID_ARG, "temperature must be 1e-30..1e30");
   if (a->rows == 0) return AF1_OK;
   if (a->given < 0 || a->given > 1024 || (a->given > 0) != (a->logprobs != nullptr) ||
       (a->given > 0) != (a->tokens != nullptr))
@@ -346,13 +478,12 @@ int af1_token_logprobs(const af1_logprob_args* a, void* stream) {
       return rc;
   }
   ScoreProblem p = {a->logits,  a->vocab,   a->ld,           a->tokens,  (int)a->given, a->logprobs,
-                    a->entropy, a->top_logprobs, a->top_ids, a->top,     1.4426950408889634f / a->temperature,
-                    1.f / a->temperature};
-  // CTAs of a row: enough to give every SM four, while a CTA keeps a batch for
-  // each warp.
-  const int64_t batches = a->vocab / (kThreads * 16) + 1;
+                    a->entropy, a->top_logprobs, a->top_ids, a->top,     1.4426950408889634f / a->temperature};
+  // CTAs of a row: as many as five to an SM allow, while each of their warps
+  // has a batch.
+  const int64_t batches = a->vocab / (kThreads * (a->dtype == AF1_F16 ? 32 : 16)) + 1;
   int cluster = 1;
-  while (cluster < kMaxCluster && a->rows * cluster < 4 * sms && 2 * cluster <= batches) cluster *= 2;
+  while (cluster < kMaxCluster && a->rows * cluster * 2 <= 5 * sms && 2 * cluster <= batches) cluster *= 2;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (a->dtype == AF1_F16)
     e = a->top > 0 ? launch<__half, true>(p, a->rows, cluster, st) : launch<__half, false>(p, a->rows, cluster, st);
