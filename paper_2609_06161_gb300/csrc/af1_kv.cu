@@ -25,6 +25,9 @@ namespace af1 {
 namespace {
 
 constexpr int kThreads = 256;
+// Added to |x| < 2^22, it rounds x to a whole number (to nearest even), which
+// then stands in the low bits: a conversion at the rate of an addition.
+constexpr float kRound = 12582912.f;  // 1.5 * 2^23
 constexpr float kTiny = 7.52316385e-37f;  // 2^-120: smaller scales are stored as 0
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
@@ -244,9 +247,10 @@ __device__ __forceinline__ void quantise(float (&x)[8], int lane, uint8_t* row, 
     uint32_t codes = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float q = bad ? 0.f : fminf(fmaxf(rintf(__fmul_rn(__fsub_rn(x[i], l), inv)), 0.f), 15.f);
-      codes |= (uint32_t)q << (4 * i);
-      x[i] = __fmaf_rn(q, s, l);
+      const float q = fminf(fmaxf(__fmul_rn(__fsub_rn(x[i], l), inv), 0.f), 15.f);
+      const float r = __fadd_rn(bad ? 0.f : q, kRound);
+      codes |= (__float_as_uint(r) & 15u) << (4 * i);
+      x[i] = __fmaf_rn(__fsub_rn(r, kRound), s, l);
     }
     if (keep) {
       reinterpret_cast<uint32_t*>(row)[lane] = codes;
@@ -271,16 +275,18 @@ __device__ __forceinline__ void quantise(float (&x)[8], int lane, uint8_t* row, 
     if (bad) s = __int_as_float(0x7fffffff);
     alignas(8) uint8_t codes[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float q = bad ? 0.f : __fmul_rn(x[i], inv);
+    for (int i = 0; i < 8; i += 2) {
+      const float q0 = bad ? 0.f : __fmul_rn(x[i], inv), q1 = bad ? 0.f : __fmul_rn(x[i + 1], inv);
       if constexpr (KIND == AF1_KV_INT8) {
-        const int c = (int)fminf(fmaxf(rintf(q), -127.f), 127.f);
-        codes[i] = (uint8_t)c;
-        x[i] = __fmul_rn((float)c, s);
+        const float r0 = __fadd_rn(fminf(fmaxf(q0, -127.f), 127.f), kRound);
+        const float r1 = __fadd_rn(fminf(fmaxf(q1, -127.f), 127.f), kRound);
+        codes[i] = (uint8_t)__float_as_uint(r0), codes[i + 1] = (uint8_t)__float_as_uint(r1);
+        x[i] = __fmul_rn(__fsub_rn(r0, kRound), s), x[i + 1] = __fmul_rn(__fsub_rn(r1, kRound), s);
       } else {
-        const __nv_fp8_storage_t c = __nv_cvt_float_to_fp8(q, __NV_SATFINITE, __NV_E4M3);
-        codes[i] = c;
-        x[i] = __fmul_rn(__half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3))), s);
+        const __nv_fp8x2_storage_t c = __nv_cvt_float2_to_fp8x2(make_float2(q0, q1), __NV_SATFINITE, __NV_E4M3);
+        *reinterpret_cast<__nv_fp8x2_storage_t*>(codes + i) = c;
+        const float2 y = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(c, __NV_E4M3)));
+        x[i] = __fmul_rn(y.x, s), x[i + 1] = __fmul_rn(y.y, s);
       }
     }
     if (keep) {
@@ -324,92 +330,115 @@ struct AppendProblem {
   int64_t length;
   __half *k_out, *v_out;
   int half;
-  int64_t rows;       // 2 * tokens * heads vectors to store
-  int kv_blocks;      // blocks below store them, the others rotate q
+  int64_t tokens;
+  int parts;          // threads of a token's lane: each takes every parts-th head
+  int k_blocks, kv_blocks;  // blocks below store keys, or values, and the others rotate q
   RopeProblem q;
 };
 
-// Blocks of the cache part: DIM / 8 threads hold one vector, 8 entries each.
-// The entries that a key's own are paired with lie in another thread's part
-// (or, interleaved, in its own) and are read beside them: the second read
-// hits L1, and no exchange between threads depends on rope_dim.
-// 16 tokens x 8 heads x 128 with 32 query heads, INT8: see the table of
-// measurements in the design notes of the repository; the launch bounds it.
+// Blocks of the cache part: DIM / 8 threads hold one vector, 8 entries each,
+// and each takes `parts`-th heads of its token, with the token's turns in
+// registers. The entries that a key's own are paired with
+// lie in another thread's part (or, interleaved, in its own) and are read
+// beside them: the second read hits L1, and no exchange between threads
+// depends on rope_dim.
 template <int KIND, int DIM, typename T, bool VEC, bool IL>
-__global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendProblem p) {
+__global__ void __launch_bounds__(kThreads, 4) append_kernel(const __grid_constant__ AppendProblem p) {
   if ((int)blockIdx.x >= p.kv_blocks) {
     const int64_t id = (int64_t)(blockIdx.x - p.kv_blocks) * kThreads + threadIdx.x;
     if (id < p.q.total) rope_unit<T, __half, VEC ? 4 : 1, IL>(p.q, id);
     return;
   }
   constexpr int LANES = DIM / 8;
-  int64_t id = (int64_t)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
-  const bool real = id < p.rows;
-  if (!real) id = p.rows - 1;  // keeps every lane of the shuffles below
+  const bool is_v = (int)blockIdx.x >= p.k_blocks;
+  int64_t id = (int64_t)(blockIdx.x - (is_v ? p.k_blocks : 0)) * (kThreads / LANES) + threadIdx.x / LANES;
+  const bool real = id < p.tokens * p.parts;
+  if (!real) id = 0;  // keeps every lane of the shuffles below
   const int lane = threadIdx.x % LANES;
   const int heads = p.cache.heads;
-  const int64_t token = id / (2 * heads);
-  int head = (int)(id - token * 2 * heads);
-  const bool is_v = head >= heads;
-  if (is_v) head -= heads;
-  const int slot = p.slot[token];
-  const T* src = is_v ? static_cast<const T*>(p.v) + token * p.v_token + head * p.v_head
-                      : static_cast<const T*>(p.k) + token * p.k_token + head * p.k_head;
-  const int at = 8 * lane;
-  float x[8];
-  load<VEC>(x, src + at);
-  if (!is_v && p.half > 0 && at < 2 * p.half) {
-    const int pos = p.positions != nullptr ? p.positions[token] : slot;
-    if constexpr (IL) {
-      float c[4], s[4];
-      if constexpr (VEC) load_turn<true>(c, s, p.table, p.length, p.half, pos, at / 2);
+  const int64_t token = id / p.parts;
+  const int part = (int)(id - token * p.parts);
+  const int slot = p.slot[token], seq = p.seq[token];
+  const int at = 8 * lane, half = p.half;
+  const bool turns = !is_v && at < 2 * half;
+  const int pos = p.positions != nullptr ? p.positions[token] : slot;
+  const bool first = at < half;  // VEC, not interleaved: half is a multiple of 8, the 8 entries lie in one half
+  float c[8], s[8];
+  if (turns) {
+    if constexpr (VEC && IL) {
+      float c4[4], s4[4];
+      load_turn<true>(c4, s4, p.table, p.length, half, pos, at / 2);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (!VEC) {
-          if (at + 2 * i >= 2 * p.half) break;
-          float ci[1], si[1];
-          load_turn<false>(ci, si, p.table, p.length, p.half, pos, at / 2 + i);
-          c[i] = ci[0], s[i] = si[0];
-        }
-        const float a = x[2 * i], b = x[2 * i + 1];
-        x[2 * i] = __fsub_rn(__fmul_rn(a, c[i]), __fmul_rn(b, s[i]));
-        x[2 * i + 1] = __fadd_rn(__fmul_rn(b, c[i]), __fmul_rn(a, s[i]));
-      }
-    } else if (VEC) {  // half is a multiple of 8: the 8 entries lie in one half
-      const bool first = at < p.half;
-      float y[8], c[8], s[8];
-      load<VEC>(y, src + (first ? at + p.half : at - p.half));
-      load_turn<VEC>(c, s, p.table, p.length, p.half, pos, first ? at : at - p.half);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        x[i] = first ? __fsub_rn(__fmul_rn(x[i], c[i]), __fmul_rn(y[i], s[i]))
-                     : __fadd_rn(__fmul_rn(x[i], c[i]), __fmul_rn(y[i], s[i]));
+      for (int i = 0; i < 4; ++i) c[i] = c4[i], s[i] = s4[i];
+    } else if constexpr (VEC) {
+      load_turn<true>(c, s, p.table, p.length, half, pos, first ? at : at - half);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int e = at + i;
-        if (e >= 2 * p.half) break;
-        const bool first = e < p.half;
-        const float y = to_f32(src[first ? e + p.half : e - p.half]);
-        float c[1], s[1];
-        load_turn<false>(c, s, p.table, p.length, p.half, pos, first ? e : e - p.half);
-        x[i] = first ? __fsub_rn(__fmul_rn(x[i], c[0]), __fmul_rn(y, s[0]))
-                     : __fadd_rn(__fmul_rn(x[i], c[0]), __fmul_rn(y, s[0]));
+      for (int i = 0; i < (IL ? 4 : 8); ++i) {
+        const int e = IL ? at / 2 + i : at + i;  // pair, or entry
+        float ci[1] = {1.f}, si[1] = {0.f};
+        if (IL ? e < half : e < 2 * half)
+          load_turn<false>(ci, si, p.table, p.length, half, pos, IL || e < half ? e : e - half);
+        c[i] = ci[0], s[i] = si[0];
       }
     }
   }
-  const int64_t row = kv_row(p.cache, p.pages, p.seq[token], slot, head);
-  const int64_t safe = row < 0 ? 0 : row;
-  uint8_t* codes = (is_v ? p.cache.v : p.cache.k) + safe * kv_row_bytes(KIND, DIM);
-  uint8_t* scale = static_cast<uint8_t*>(is_v ? p.cache.vs : p.cache.ks) + safe * kv_scale_bytes(KIND, DIM);
-  quantise<KIND, LANES>(x, lane, codes, scale, real && row >= 0);
+  const int64_t row0 = kv_row(p.cache, p.pages, seq, slot, 0);
+  const bool keep = real && row0 >= 0;
+  uint8_t* codes = is_v ? p.cache.v : p.cache.k;
+  uint8_t* scales = static_cast<uint8_t*>(is_v ? p.cache.vs : p.cache.ks);
   __half* out = is_v ? p.v_out : p.k_out;
-  if (real && out != nullptr) {
-    if (slot < 0) {
+  const T* token_src = is_v ? static_cast<const T*>(p.v) + token * p.v_token : static_cast<const T*>(p.k) + token * p.k_token;
+  const int64_t head_step = is_v ? p.v_head : p.k_head;
+  // Every thread of a block runs the same number of rounds: the shuffles need all lanes.
+  for (int round = 0; round * p.parts < heads; ++round) {
+    const int want = round * p.parts + part;
+    const bool there = want < heads;
+    const int head = there ? want : heads - 1;  // its lanes write the same values again
+    const T* src = token_src + head * head_step;
+    float x[8], y[8];
+    load<VEC>(x, src + at);
+    if constexpr (!IL) {
+      if (turns) {
+        if constexpr (VEC) {
+          load<VEC>(y, src + (first ? at + half : at - half));
+        } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = 0.f;
+          for (int i = 0; i < 8; ++i) {
+            const int e = at + i;
+            y[i] = e < 2 * half ? to_f32(src[e < half ? e + half : e - half]) : 0.f;
+          }
+        }
+      }
     }
-    store<true>(out + (token * heads + head) * DIM + at, x);
+    if (turns) {
+      if constexpr (IL) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (!VEC && at + 2 * i >= 2 * half) break;
+          const float a = x[2 * i], b = x[2 * i + 1];
+          x[2 * i] = __fsub_rn(__fmul_rn(a, c[i]), __fmul_rn(b, s[i]));
+          x[2 * i + 1] = __fadd_rn(__fmul_rn(b, c[i]), __fmul_rn(a, s[i]));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (!VEC && at + i >= 2 * half) break;
+          const bool low = VEC ? first : at + i < half;
+          x[i] = low ? __fsub_rn(__fmul_rn(x[i], c[i]), __fmul_rn(y[i], s[i]))
+                     : __fadd_rn(__fmul_rn(x[i], c[i]), __fmul_rn(y[i], s[i]));
+        }
+      }
+    }
+    const int64_t row = row0 < 0 ? 0 : row0 + ((int64_t)head << p.cache.shift);
+    quantise<KIND, LANES>(x, lane, codes + row * kv_row_bytes(KIND, DIM), scales + row * kv_scale_bytes(KIND, DIM), keep);
+    if (real && out != nullptr) {
+      if (slot < 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+      }
+      store<true>(out + (token * heads + head) * DIM + at, x);
+    }
   }
 }
 
@@ -423,9 +452,11 @@ struct ReadProblem {
   void *k_out, *v_out;
 };
 
-// A block reads one head of kThreads / (DIM / 8) * kReadRows neighbouring
-// slots, so that it reads whole runs of a page's rows.
-constexpr int kReadRows = 4;
+// A block reads kThreads / (DIM / 8) neighbouring slots, all heads of them one
+// after another, so that it reads runs of a page's rows and writes one stretch
+// of the output. (Blocks of one head each wrote 128-byte pieces a slot apart:
+// 103 us where this takes 54, 16 sequences of up to 8190 INT4 tokens of 8 x 64.)
+constexpr int kReadRows = 4;  // heads in flight
 
 template <int KIND, int DIM, typename TO>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ ReadProblem p, int64_t tiles) {
@@ -433,30 +464,38 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ 
   const int64_t tile = blockIdx.x % tiles;
   const int seq = (int)(blockIdx.x / tiles);
   const int heads = p.cache.heads;
-  const bool is_v = (int)blockIdx.y >= heads;
-  const int head = is_v ? blockIdx.y - heads : blockIdx.y;
+  const bool is_v = blockIdx.y != 0;
   const int lane = threadIdx.x % LANES;
-  const int len = p.lens[seq];
+  const int64_t at = tile * ROWS + threadIdx.x / LANES, slot = p.first + at;
+  if (at >= p.count) return;
+  const int64_t row0 = slot < p.lens[seq] ? kv_row(p.cache, p.pages, seq, (int)slot, 0) : -1;
   const uint8_t* codes = is_v ? p.cache.v : p.cache.k;
   const uint8_t* scales = static_cast<const uint8_t*>(is_v ? p.cache.vs : p.cache.ks);
-  TO* out = static_cast<TO*>(is_v ? p.v_out : p.k_out);
-  float x[kReadRows][8];
+  TO* out = static_cast<TO*>(is_v ? p.v_out : p.k_out) + (seq * p.count + at) * heads * DIM + 8 * lane;
+  const int64_t step_codes = (int64_t)kv_row_bytes(KIND, DIM) << p.cache.shift;
+  const int64_t step_scales = (int64_t)kv_scale_bytes(KIND, DIM) << p.cache.shift;
+  codes += (row0 < 0 ? 0 : row0) * kv_row_bytes(KIND, DIM);
+  scales += (row0 < 0 ? 0 : row0) * kv_scale_bytes(KIND, DIM);
+  int head = 0;
+  for (; head + kReadRows <= heads; head += kReadRows) {
+    float x[kReadRows][8];
+    if (row0 >= 0) {
 #pragma unroll
-  for (int i = 0; i < kReadRows; ++i) {
-    const int64_t at = tile * (ROWS * kReadRows) + i * ROWS + threadIdx.x / LANES;
-    const int64_t slot = p.first + at;
+      for (int i = 0; i < kReadRows; ++i)
+        dequantise<KIND>(x[i], lane, codes + (head + i) * step_codes, scales + (head + i) * step_scales);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
-    if (at < p.count && slot < len) {
-      const int64_t row = kv_row(p.cache, p.pages, seq, (int)slot, head);
-      if (row >= 0)
-        dequantise<KIND>(x[i], lane, codes + row * kv_row_bytes(KIND, DIM), scales + row * kv_scale_bytes(KIND, DIM));
+      for (int i = 0; i < kReadRows; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
     }
-  }
 #pragma unroll
-  for (int i = 0; i < kReadRows; ++i) {
-    const int64_t at = tile * (ROWS * kReadRows) + i * ROWS + threadIdx.x / LANES;
-    if (at < p.count) store<true>(out + ((seq * p.count + at) * heads + head) * DIM + 8 * lane, x[i]);
+    for (int i = 0; i < kReadRows; ++i) store<true>(out + (head + i) * DIM, x[i]);
+  }
+  for (; head < heads; ++head) {
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (row0 >= 0) dequantise<KIND>(x, lane, codes + head * step_codes, scales + head * step_scales);
+    store<true>(out + head * DIM, x);
   }
 }
 
@@ -809,9 +848,12 @@ int af1_kv_append(const af1_kv_cache* c, const af1_kv_append_args* a, void* stre
   p.table = a->table, p.length = a->length;
   p.k_out = static_cast<__half*>(a->k_out), p.v_out = static_cast<__half*>(a->v_out);
   p.half = rope ? (int)a->rope_dim / 2 : 0;
-  p.rows = 2 * a->tokens * heads;
+  p.tokens = a->tokens;
+  // Where tokens alone fill the GPU (1024 threads to an SM), a thread takes
+  // four heads; else one.
+  p.parts = a->tokens * (dim / 8) >= 1024 * c->num_sms / 2 ? (heads + 3) / 4 : heads;
   const int per_block = kThreads / (dim / 8);
-  const int64_t kv_blocks = (p.rows + per_block - 1) / per_block;
+  const int64_t kv_blocks = 2 * ((a->tokens * p.parts + per_block - 1) / per_block);
   int64_t q_blocks = 0;
   // 16-byte reads of k and v, and of their pairs and turns, where sizes and
   // addresses allow them (for q too, as one variant serves both).
@@ -831,7 +873,7 @@ int af1_kv_append(const af1_kv_cache* c, const af1_kv_append_args* a, void* stre
     q_blocks = (p.q.total + kThreads - 1) / kThreads;
   }
   if (kv_blocks + q_blocks > 0x7fffffff) return fail(AF1_ERR_INVALID_ARG, who, "too many entries for one call");
-  p.kv_blocks = (int)kv_blocks;
+  p.k_blocks = (int)(kv_blocks / 2), p.kv_blocks = (int)kv_blocks;
   return with_kind(c->d.kind, [&](auto kind) {
     return with_bool(dim == 128, [&](auto wide) {
       return with_bool(a->dtype == AF1_F16, [&](auto h) {
@@ -864,11 +906,11 @@ int af1_kv_read(const af1_kv_cache* c, const int32_t* pages, int64_t sequences, 
       (rc = check_pointer(v_out, "v_out", dev)) != AF1_OK || (rc = check_align(v_out, 16, "v_out")) != AF1_OK)
     return rc;
   const int dim = c->d.head_dim;
-  const int64_t tile = (int64_t)kThreads / (dim / 8) * kReadRows;
+  const int64_t tile = (int64_t)kThreads / (dim / 8);
   const int64_t tiles = (count + tile - 1) / tile;
   if (tiles * sequences > 0x7fffffff) return fail(AF1_ERR_INVALID_ARG, who, "too many slots for one call");
   ReadProblem p = {view_of(c->d), {pages, pages_ld, (int)sequences, (int)page_columns}, lens, first, count, k_out, v_out};
-  const dim3 grid((unsigned)(tiles * sequences), 2 * c->d.kv_heads);
+  const dim3 grid((unsigned)(tiles * sequences), 2);
   return with_kind(c->d.kind, [&](auto kind) {
     return with_bool(dim == 128, [&](auto wide) {
       return with_bool(dtype == AF1_F16, [&](auto h) {
