@@ -1,0 +1,843 @@
+// af1_tree_wide.cu — attention of drafted tokens over the paged cache where
+// more than 16 rows (nodes times query heads) share a cached head: the same
+// operator as af1_tree.cu, with tcgen05 products of 128 rows.
+//
+// An item is one sequence, one cached head and a block of 128 rows; its keys
+// are cut into tiles of 128, and every CTA (one to an SM) takes an equal run
+// of the tiles of all items, as in af1_tree.cu. The tiles of a run alternate
+// between two streams, each with its own scores, maximum, sum and output, so
+// that one stream's products run under the other's exponents; the streams are
+// joined at the end of a run. For one tile
+//   S = Q K^T   (128 x 128, FP32, tensor memory)
+//   P = 2^(S f - m + kShift) as FP16, over S
+//   O += P V    (P from tensor memory, V from shared memory)
+// Roles of the 16 warps:
+//   0-3, 4-7  softmax of stream 0 and 1: a thread has one row. The scores are
+//             read twice (maximum, weights): held between the passes they
+//             would need 128 registers. The maximum moves, and O with it, only
+//             when a score passes it by 2^kSlack;
+//   8-11      decode: thread i turns key or value i of a tile from codes into
+//             FP16 in the 128-byte-swizzled operand tile (keys K-major, values
+//             with their entries along N). INT8 and E4M3 stay codes, exact in
+//             FP16; a key's scale multiplies the scores, a value's the weights
+//             (relative to a power of two that bounds the scales so far, which
+//             the exponents take in). INT4, which has a scale for each group
+//             of 32 entries, is rounded once to FP16, keys too: a score is off
+//             by about 2^-12 sqrt(sum (q k)^2). FP16 tiles arrive by TMA and
+//             are only looked at where a sequence ends;
+//   12        one TMA copy for 16 or 32 rows of a page, into the ring of codes;
+//   13, 14    one thread each issues a stream's products.
+// Operand tiles pass through four slots in the order K0 K1 V0 K2 V1 K3 ..., in
+// which the products use them.
+//
+// Infinities and NaN: the values of slots past the end are zeros, a node's
+// value that is not finite is left out of the product (0 times it would reach
+// the rows that do not see it) and added to the rows that see it at the end.
+//
+// Bound: with all 128 rows in use, exponents (16 a cycle, 1024 cycles a tile)
+// and the instructions around them; the products need 512 cycles.
+// All waits are bounded; a wait that gives up sets the status word, and what
+// depends on it is skipped.
+#include "af1_tree.cuh"
+
+namespace af1 {
+namespace {
+
+constexpr int BK = 128;        // keys of a tile
+constexpr int kThreads = 512;
+constexpr int kSetupTiles = 2; // tiles that a run's beginning and end are worth
+constexpr int kRows = 128;
+constexpr int kSlots = 4;
+constexpr float kLeastScale = -60.f;  // of a value's scale's exponent: smaller ones count as 2^-60
+
+template <int KIND, int DIM>
+struct Wide {
+  using C = Kv<KIND, DIM>;
+  static constexpr bool F16 = KIND == AF1_KV_F16;
+  static constexpr int OP = BK * DIM * 2;                    // bytes of an operand tile
+  static constexpr int CODES = BK * C::RB;
+  static constexpr int SCALES = (C::SCALED8 ? 2 : 1) * BK * C::SB;  // 8 bits: of keys and values, with the keys
+  static constexpr int STAGES = F16 ? kSlots : C::RB >= 128 ? 3 : 4;  // ring of codes (FP16: the slots themselves)
+  static constexpr int SMEM = (kSlots + 1) * OP + (F16 ? 0 : STAGES * (CODES + SCALES)) + 8 * BK * 4 + 1024;
+  static constexpr int PART = kRows * (DIM + 2);  // floats: o, m, l, each along the rows
+};
+
+struct Barriers {
+  uint64_t op_ready[kSlots], op_empty[kSlots], code_full[kSlots], code_empty[kSlots];
+  uint64_t s_full[2], p_ready[2], pv_done[2], q_ready, other_done, joined;
+  uint32_t tmem;
+  volatile int gave_up;
+  uint32_t code_bad[kSlots], tile_bad[4];   // bits: 16 keys each whose page is missing
+  uint32_t nodes_bad[4][2];                 // by run: nodes whose value is not finite
+  float m[kRows], l[kRows];                 // stream 1's
+  float value_top[4][4];                    // by tile and warp: power of two above the values' scales
+  bool last;
+};
+
+// The runs of this CTA, one after another, known to every warp.
+struct Runs {
+  Sequences<BK, kSetupTiles> sq;
+  int64_t lanes, total, ctas, per, more, pos, end;
+  int seq, head, tile, rows, len, keys, units, from, to, k_begin, k_end, tiles;
+  int64_t first;
+
+  __device__ __forceinline__ bool begin(const TreeProblem& p) {
+    lanes = (int64_t)p.cache.heads * p.row_tiles;
+    sq.load(p, 0, 0);
+    total = sq.after();
+    for (int at = 32; at < p.pages.seqs; at += 32) {
+      sq.load(p, at, total);
+      total = sq.after();
+    }
+    if (p.pages.seqs > 32) sq.load(p, 0, 0);
+    total *= lanes;
+    ctas = min((int64_t)gridDim.x, total);
+    if (blockIdx.x >= ctas) return false;
+    per = total / ctas, more = total - per * ctas;
+    pos = per * blockIdx.x + min((int64_t)blockIdx.x, more);
+    end = pos + per + (blockIdx.x < more ? 1 : 0);
+    return true;
+  }
+  // The next run; tiles is 0 where it has no keys of its own.
+  __device__ __forceinline__ bool next(const TreeProblem& p) {
+    if (pos >= end) return false;
+    while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after());
+    const int which = __popc(__ballot_sync(0xffffffffu, (sq.before + sq.sum) * lanes <= pos));
+    seq = sq.first + which;
+    units = __shfl_sync(0xffffffffu, sq.units, which);
+    len = __shfl_sync(0xffffffffu, sq.len, which);
+    keys = __shfl_sync(0xffffffffu, sq.keys, which);
+    const int64_t seq_first = (sq.before + __shfl_sync(0xffffffffu, sq.sum, which) - units) * lanes;
+    const int item = (int)((pos - seq_first) / units);
+    first = seq_first + (int64_t)item * units;
+    from = (int)(pos - first);
+    to = (int)min((int64_t)units, from + (end - pos));
+    pos += to - from;
+    head = item / p.row_tiles;
+    tile = item - head * p.row_tiles;
+    rows = min(kRows, p.nodes * p.group - tile * kRows);
+    const int u0 = max(from - kSetupTiles, 0), u1 = to - kSetupTiles;
+    k_begin = u0 * BK, k_end = min(u1 * BK, keys);
+    tiles = max(u1 - u0, 0);
+    return true;
+  }
+  __device__ __forceinline__ int holder(int64_t u) const {  // the CTA that has unit u
+    const int64_t large = more * (per + 1);
+    return (int)(u < large ? u / (per + 1) : more + (u - large) / per);
+  }
+};
+
+// Operand i of a run of n tiles: K0 K1 V0 K2 V1 ... V(n-2) V(n-1).
+__device__ __forceinline__ void operand(int i, int n, bool& is_v, int& j) {
+  is_v = i == 2 * n - 1 || (i >= 2 && i % 2 == 0);
+  j = i == 2 * n - 1 ? n - 1 : i == 0 ? 0 : is_v ? (i - 2) / 2 : (i + 1) / 2;
+}
+__device__ __forceinline__ int k_index(int j) { return j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ int v_index(int j, int n) { return j == n - 1 ? 2 * n - 1 : 2 * j + 2; }
+
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+               : "memory");
+}
+// Shared-memory matrix: 128-byte swizzle, 8 rows 1024 bytes apart; `lead`: bytes
+// between 64-entry groups where the entries run along M or N.
+__device__ __forceinline__ uint64_t matrix(uint32_t addr, int lead) {
+  return (uint64_t)((addr >> 4) & 0x3fffu) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+         (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
+      : "memory");
+}
+// 32 columns of this thread's row.
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&x)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+      "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
+          addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Where entry pair and group places stand: INT4's decode takes 4 apart nibbles
+// at once, so place 2 i + h of every 8 is entry i + 4 h. q is laid out alike,
+// and the outputs are put back.
+template <int KIND>
+__device__ __forceinline__ constexpr int place_entry(int place) {
+  return KIND == AF1_KV_INT4 ? (place & ~7) | ((place & 7) >> 1) | (place & 1) << 2 : place;
+}
+
+template <int KIND, int DIM>
+__global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant__ TreeProblem p) {
+  using C = Kv<KIND, DIM>;
+  using S = Wide<KIND, DIM>;
+  constexpr bool F16 = S::F16, INT4 = KIND == AF1_KV_INT4;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Barriers bar;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* ops = smem;
+  uint8_t* qt = smem + kSlots * S::OP;
+  uint8_t* codes = qt + S::OP;
+  uint8_t* scales = codes + S::STAGES * S::CODES;
+  float* key_scale = reinterpret_cast<float*>(qt + S::OP + (F16 ? 0 : S::STAGES * (S::CODES + S::SCALES)));
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+
+  Runs run;
+  if (!run.begin(p)) return;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(&bar.op_ready[i], 4);
+      mbar_init(&bar.op_empty[i], 1);
+      mbar_init(&bar.code_full[i], 1);
+      mbar_init(&bar.code_empty[i], 4);
+      bar.nodes_bad[i][0] = bar.nodes_bad[i][1] = 0;
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bar.s_full[i], 1);
+      mbar_init(&bar.p_ready[i], 4);
+      mbar_init(&bar.pv_done[i], 1);
+    }
+    mbar_init(&bar.q_ready, 4);
+    mbar_init(&bar.other_done, 5);
+    mbar_init(&bar.joined, 4);
+    bar.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async();
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bar.tmem)),
+                 "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = bar.tmem;
+  float* value_scale = key_scale + 4 * BK;
+
+  // Bounded wait; once one has given up, all return at once.
+  auto wait = [&](uint64_t* b, uint32_t parity) {
+    if (mbar_try_wait(b, parity)) return true;
+    const long long t0 = clock64();
+    while (!mbar_try_wait(b, parity)) {
+      if (bar.gave_up) return false;
+      if (clock64() - t0 > p.wait_cycles) {
+        bar.gave_up = 1;
+        return false;
+      }
+    }
+    return true;
+  };
+
+  int ops_done = 0, tiles_done = 0, runs_done = 0;  // before this run
+  if (warp == 12) {
+    // ---- copies ------------------------------------------------------------------
+    const int box = p.cache.shift >= 5 ? 32 : 16;
+    uint32_t issued_stages = 0;
+    for (; run.next(p); ++runs_done) {
+      const int32_t* page_row = p.pages.pages + run.seq * p.pages.ld;
+      const int n = run.tiles;
+      auto page_of = [&](int i) {
+        bool is_v;
+        int j;
+        operand(i, n, is_v, j);
+        const int k = run.k_begin + j * BK + lane * box;
+        return lane < BK / box && k < run.k_end ? page_row[k >> p.cache.shift] : -1;
+      };
+      int page = n > 0 ? page_of(0) : -1;
+      for (int i = 0; i < 2 * n; ++i) {
+        bool is_v;
+        int j;
+        operand(i, n, is_v, j);
+        const int op = ops_done + i, st = op % S::STAGES;
+        const int k = run.k_begin + j * BK + lane * box;
+        const bool there = page >= 0 && page < p.cache.pages;
+        const unsigned have = __ballot_sync(0xffffffffu, there);
+        const unsigned lack = __ballot_sync(0xffffffffu, !there && lane < BK / box && k < run.k_end);
+        const int64_t row =
+            (((int64_t)page * p.cache.heads + run.head) << p.cache.shift) + (k & ((1 << p.cache.shift) - 1));
+        if (i + 1 < 2 * n) page = page_of(i + 1);
+        const bool ok = wait(F16 ? &bar.op_empty[st] : &bar.code_empty[st], (op / S::STAGES & 1) ^ 1);
+        if (!__all_sync(0xffffffffu, ok)) continue;
+        if (lane == 0) {
+          uint32_t bad = lack;
+          if (box == 32) {  // a bit for each 16 keys
+            bad = 0;
+            for (int b = 0; b < 4; ++b)
+              if (lack >> b & 1) bad |= 3u << (2 * b);
+          }
+          bar.code_bad[st] = bad;
+          const int per_key = C::RB + (C::SCALED8 ? (is_v ? 0 : 2 * C::SB) : C::SB);
+          mbar_expect_tx(&bar.code_full[st], __popc(have) * box * per_key);
+          issued_stages = op + 1;
+        }
+        __syncwarp();
+        if (there) {
+          uint8_t* to = (F16 ? ops + st * S::OP : codes + st * S::CODES) + lane * box * C::SPAN;
+#pragma unroll
+          for (int s = 0; s < C::SLICES; ++s)
+            tma_rows(smem_u32(to + s * (BK * 128)), is_v ? &p.v_map : &p.k_map, s * 128, (int)row, &bar.code_full[st]);
+          if constexpr (C::SB > 0) {
+            uint8_t* to_scales = scales + st * S::SCALES + lane * box * C::SB;
+            if (!C::SCALED8 || !is_v)
+              bulk_g2s(to_scales, static_cast<const uint8_t*>(is_v ? p.cache.vs : p.cache.ks) + row * C::SB, box * C::SB,
+                       &bar.code_full[st]);
+            if (C::SCALED8 && !is_v)
+              bulk_g2s(to_scales + BK * C::SB, static_cast<const uint8_t*>(p.cache.vs) + row * C::SB, box * C::SB,
+                       &bar.code_full[st]);
+          }
+        }
+      }
+      ops_done += 2 * n;
+    }
+    // After a wait that gave up, copies may still be on their way.
+    if (bar.gave_up && lane == 0) {
+      for (int back = 0; back < S::STAGES && back < (int)issued_stages; ++back) {
+        const int op = (int)issued_stages - 1 - back;
+        const long long t0 = clock64();
+        while (!mbar_try_wait(&bar.code_full[op % S::STAGES], op / S::STAGES & 1) && clock64() - t0 < p.wait_cycles) {
+        }
+      }
+    }
+  } else if (warp >= 8 && warp < 12) {
+    // ---- decode ---------------------------------------------------------------------
+    const int row = threadIdx.x - 256;
+    for (; run.next(p); ++runs_done) {
+      const int n = run.tiles;
+      for (int i = 0; i < 2 * n; ++i) {
+        bool is_v;
+        int j;
+        operand(i, n, is_v, j);
+        const int op = ops_done + i, st = op % S::STAGES, slot = op % kSlots;
+        bool ok = wait(&bar.code_full[st], op / S::STAGES & 1);
+        if constexpr (!F16) ok = wait(&bar.op_empty[slot], (op / kSlots & 1) ^ 1) && ok;
+        ok = __all_sync(0xffffffffu, ok);
+        const int key = run.k_begin + j * BK + row;
+        const uint32_t bad = bar.code_bad[st];
+        const bool gone = key >= run.k_end || (bad >> (row / 16) & 1);
+        const bool node = key >= run.len;
+        uint8_t* to = ops + slot * S::OP + row * 128;
+        auto place = [&](int c) { return to + (c >> 3) * (BK * 128) + (((c & 7) ^ (row & 7)) << 4); };
+        bool odd_value = false;  // a value that is not finite, of a node
+        if (ok) {
+          if constexpr (F16) {
+            if (is_v && (gone || node)) {
+#pragma unroll 4
+              for (int c = 0; c < DIM / 8; ++c) {
+                uint4 v = *reinterpret_cast<uint4*>(place(c));
+                uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  if ((w[e] & 0x7c00u) == 0x7c00u) w[e] &= 0xffff0000u, odd_value = true;
+                  if ((w[e] & 0x7c000000u) == 0x7c000000u) w[e] &= 0x0000ffffu, odd_value = true;
+                  if (gone) w[e] = 0;
+                }
+                *reinterpret_cast<uint4*>(place(c)) = v;
+              }
+            }
+          } else {
+            const uint8_t* from = codes + st * S::CODES;
+            const uint8_t* sc = scales + st * S::SCALES;
+            uint32_t scale2 = 0;
+            if constexpr (C::SCALED8) {
+              if (!is_v) {
+                const int at = (tiles_done + j) % 4;
+                const float vs = reinterpret_cast<const float*>(sc)[BK + row];
+                key_scale[at * BK + row] = reinterpret_cast<const float*>(sc)[row] * fabsf(p.scale_log2);
+                value_scale[at * BK + row] = vs;
+                // Non-negative floats order as their bits.
+                const uint32_t most =
+                    __reduce_max_sync(0xffffffffu, !gone && fabsf(vs) < kInf ? __float_as_uint(fabsf(vs)) : 0u);
+                if (lane == 0) bar.value_top[at][warp % 4] = fmaxf((float)((int)(most >> 23) - 126), kLeastScale);
+              }
+            }
+#pragma unroll 2
+            for (int c = 0; c < C::RB / 16; ++c) {
+              const uint4 x = *reinterpret_cast<const uint4*>(from + C::template at<BK>(row, c));
+              const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+              uint32_t low2 = 0;
+              if constexpr (INT4) {
+                const uint32_t s = reinterpret_cast<const uint32_t*>(sc)[row * C::GROUPS + c];
+                scale2 = prmt(s, s, 0x1010), low2 = prmt(s, s, 0x3232);
+              }
+              constexpr int OUT = INT4 ? 4 : 2;  // 16-byte pieces of FP16
+#pragma unroll
+              for (int q = 0; q < OUT; ++q) {
+                uint32_t h[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  if constexpr (INT4) {
+                    h[e] = hfma2(hsub2((w[q] >> (4 * e) & 0x000f000fu) | 0x64006400u, 0x64006400u), scale2, low2);
+                  } else {
+                    const uint32_t u = w[2 * q + e / 2];
+                    if constexpr (KIND == AF1_KV_INT8)
+                      h[e] = hsub2(prmt(u ^ 0x80808080u, 0x64646464u, e % 2 ? 0x4342 : 0x4140), 0x64806480u);
+                    else
+                      h[e] = e4m3x2(e % 2 ? u >> 16 : u);
+                  }
+                }
+                if (is_v && (gone || node)) {
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    if ((h[e] & 0x7c00u) == 0x7c00u) h[e] &= 0xffff0000u, odd_value = true;
+                    if ((h[e] & 0x7c000000u) == 0x7c000000u) h[e] &= 0x0000ffffu, odd_value = true;
+                    if (gone) h[e] = 0;
+                  }
+                }
+                *reinterpret_cast<uint4*>(place(c * OUT + q)) = make_uint4(h[0], h[1], h[2], h[3]);
+              }
+            }
+          }
+          if (odd_value && !gone) {
+            const int at = key - run.len;
+            atomicOr(&bar.nodes_bad[runs_done % 4][at / 32], 1u << (at % 32));
+          }
+          if (!is_v && row == 0) bar.tile_bad[(tiles_done + j) % 4] = bad;
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (!F16) mbar_arrive(&bar.code_empty[st]);
+          mbar_arrive(&bar.op_ready[slot]);
+        }
+      }
+      ops_done += 2 * n, tiles_done += n;
+    }
+  } else if (warp == 13 || warp == 14) {
+    // ---- products ---------------------------------------------------------------------
+    const int s = warp - 13;
+    const uint32_t base = tmem + s * 256;
+    constexpr uint32_t kScores = 1u << 4 | (uint32_t)(BK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+    constexpr uint32_t kOutput = 1u << 4 | 1u << 16 | (uint32_t)(DIM >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+    int done = 0;  // tiles of this stream
+    int q_runs = 0;
+    for (; run.next(p); ++runs_done) {
+      const int n = run.tiles;
+      if (n > 0) {
+        bool ok = true;
+        if (lane == 0) {
+          ok = wait(&bar.q_ready, q_runs & 1);
+          if (s == 1) mbar_arrive(&bar.other_done);  // q_ready is not two phases ahead of this thread
+        }
+        ++q_runs;
+        for (int j = s; j < n && lane == 0; j += 2, ++done) {
+          const int ko = ops_done + k_index(j), vo = ops_done + v_index(j, n);
+          ok = wait(&bar.op_ready[ko % kSlots], ko / kSlots & 1) && ok;
+          fence_after();
+          if (ok) {
+            const uint32_t a = smem_u32(qt), b = smem_u32(ops + ko % kSlots * S::OP);
+#pragma unroll
+            for (int ks = 0; ks < DIM / 16; ++ks) {
+              const int off = (ks / 4) * (BK * 128) + (ks % 4) * 32;
+              mma_ss(base, matrix(a + off, 16), matrix(b + off, 16), kScores, ks > 0);
+            }
+          }
+          commit(&bar.op_empty[ko % kSlots]);
+          commit(&bar.s_full[s]);
+          ok = wait(&bar.op_ready[vo % kSlots], vo / kSlots & 1) && ok;
+          ok = wait(&bar.p_ready[s], done & 1) && ok;
+          fence_after();
+          if (ok) {
+            const uint32_t b = smem_u32(ops + vo % kSlots * S::OP);
+#pragma unroll
+            for (int ks = 0; ks < BK / 16; ++ks)
+              mma_ts(base + 128, base + ks * 8, matrix(b + ks * 2048, BK * 128), kOutput, j > s || ks > 0);
+          }
+          commit(&bar.op_empty[vo % kSlots]);
+          commit(&bar.pv_done[s]);
+        }
+        __syncwarp();
+      }
+      ops_done += 2 * n;
+    }
+  } else if (warp < 8) {
+    // ---- softmax, and the ends of the runs ------------------------------------------------
+    const int s = warp / 4;
+    const int row = threadIdx.x % 128;
+    const uint32_t base = tmem + s * 256 + ((uint32_t)(warp % 4 * 32) << 16);
+    const float f16_scale = fabsf(p.scale_log2);
+    int done = 0, live_runs = 0;
+    for (; run.next(p); ++runs_done) {
+      const int n = run.tiles, rows = run.rows;
+      const int gr = run.tile * kRows + row, node = gr / p.group, head = run.head * p.group + gr - node * p.group;
+      const bool real = row < rows;
+      const int live_nodes = node_count(p, run.seq);
+      __half* out16 = static_cast<__half*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
+      float* out32 = static_cast<float*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
+      const int64_t lse_at = ((int64_t)run.seq * p.nodes + node) * p.cache.heads * p.group + head;
+      if (run.keys == 0 && run.from == 0 && s == 0 && real) {  // nothing to see: the item's first CTA writes its zeros
+        for (int e = 0; e < DIM; e += 8) {
+          if (p.out_f32) {
+            reinterpret_cast<float4*>(out32 + e)[0] = make_float4(0.f, 0.f, 0.f, 0.f);
+            reinterpret_cast<float4*>(out32 + e)[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+          } else {
+            *reinterpret_cast<uint4*>(out16 + e) = make_uint4(0, 0, 0, 0);
+          }
+        }
+        if (p.lse != nullptr) p.lse[lse_at] = -kInf;
+      }
+      if (n == 0) continue;
+      if (s == 0) {
+        // q of this run (the products of the run before are done); a negative
+        // scale turns its signs.
+        const __half* q = p.q + run.seq * p.q_seq + node * p.q_node + (int64_t)head * p.q_head;
+        const uint32_t sign = p.scale_log2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll 4
+        for (int c = 0; c < DIM / 8; ++c) {
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (real) v = *reinterpret_cast<const uint4*>(q + 8 * c);
+          if constexpr (INT4)
+            v = make_uint4(prmt(v.x, v.z, 0x5410), prmt(v.x, v.z, 0x7632), prmt(v.y, v.w, 0x5410),
+                           prmt(v.y, v.w, 0x7632));
+          v.x ^= sign, v.y ^= sign, v.z ^= sign, v.w ^= sign;
+          *reinterpret_cast<uint4*>(qt + (c >> 3) * (BK * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar.q_ready);
+      }
+      uint64_t bits = 0;
+      if (real) {
+        if (p.mask == nullptr) {
+          bits = (2ull << node) - 1;
+        } else {
+          const uint32_t* w = p.mask + run.seq * p.mask_seq + node * p.words;
+          bits = w[0] | (p.words > 1 ? (uint64_t)w[1] << 32 : 0);
+        }
+      }
+      const bool warp_real = (warp % 4) * 32 < rows;
+      // Weights are 2^(score - m - ev + kShift), times a value's scale, which is below 2^ev.
+      float m = -kInf, l = 0.f, ev = C::SCALED8 ? kLeastScale : 0.f;
+      bool ok = true;
+      // Stream 1's output of the run before is read until then.
+      if (s == 1 && live_runs > 0) ok = wait(&bar.joined, (live_runs - 1) & 1);
+      for (int j = s; j < n; j += 2, ++done) {
+        const int key = run.k_begin + j * BK;
+        ok = wait(&bar.s_full[s], done & 1) && ok;
+        fence_after();
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok && warp_real) {
+          const int at_tile = (tiles_done + j) % 4;
+          const float* ks = key_scale + at_tile * BK;
+          const float* vs = value_scale + at_tile * BK;
+          const uint32_t bad = bar.tile_bad[at_tile];
+          float ev_now = ev;
+          if constexpr (C::SCALED8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ev_now = fmaxf(ev_now, bar.value_top[at_tile][i]);
+          }
+          const bool masked = key + BK > min(run.len, run.k_end) || bad != 0;
+          // Columns c .. c + 31 as scores: scaled, and -infinity where the row does not see.
+          auto scores = [&](int c, float (&x)[32]) {
+            tmem_load(base + c, x);
+            if constexpr (C::SCALED8) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                const float4 f = *reinterpret_cast<const float4*>(ks + c + i);
+                x[i] *= f.x, x[i + 1] *= f.y, x[i + 2] *= f.z, x[i + 3] *= f.w;
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] *= f16_scale;
+            }
+            if (masked) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const int at = c + i, k = key + at;
+                const bool sees =
+                    k < run.k_end && !(bad >> (at / 16) & 1) && (k < run.len || (bits >> (k - run.len) & 1));
+                if (!sees) x[i] = -kInf;
+              }
+            }
+          };
+          float top = -kInf;
+#pragma unroll 1
+          for (int c = 0; c < BK; c += 32) {
+            float x[32];
+            scores(c, x);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i]);
+          }
+          if (__any_sync(0xffffffffu, top > m + kSlack || ev_now > ev)) {
+            const float now = fmaxf(m, top);
+            const float alpha = ex2(m - (now == -kInf ? 0.f : now) + (ev - ev_now));
+            m = now, ev = ev_now;
+            l *= alpha;
+            if (j > s) {
+              ok = wait(&bar.pv_done[s], (done - 1) & 1);
+              ok = __all_sync(0xffffffffu, ok);
+              fence_after();
+#pragma unroll 1
+              for (int c = 0; c < DIM; c += 32) {
+                float x[32];
+                tmem_load(base + 128 + c, x);
+                uint32_t r[16];
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(x[16 * hf + i] * alpha);
+                  tmem_store16(base + 128 + c + 16 * hf, r);
+                }
+              }
+            }
+          }
+          const float ref = (m == -kInf ? 0.f : m) + ev - kShift;
+#pragma unroll 1
+          for (int c = 0; c < BK; c += 32) {
+            float x[32];
+            scores(c, x);
+            uint32_t r[16];
+            float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              float a[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) a[e] = ex2(x[2 * i + e] - ref);
+              sum0 += a[0], sum1 += a[1], sum0 += a[2], sum1 += a[3];
+              if constexpr (C::SCALED8) {
+                const float4 f = *reinterpret_cast<const float4*>(vs + c + 2 * i);
+                const float y[4] = {a[0] * f.x, a[1] * f.y, a[2] * f.z, a[3] * f.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a[e] = masked && a[e] == 0.f ? 0.f : y[e];  // 0 times any scale is 0
+              }
+              r[i] = pack_half2(a[0], a[1]), r[i + 1] = pack_half2(a[2], a[3]);
+            }
+            l += sum0 + sum1;
+            tmem_store16(base + c / 2, r);
+          }
+          tmem_wait_store();
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar.p_ready[s]);
+      }
+      m += ev;  // the reference that sums and outputs share
+      // -- the run's end ------------------------------------------------------------------
+      const int mine = (n - s + 1) / 2;  // tiles of this stream
+      if (mine > 0) {
+        ok = wait(&bar.pv_done[s], (done - 1) & 1) && ok;
+        fence_after();
+      }
+      if (s == 1) {
+        bar.m[row] = m, bar.l[row] = l;
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar.other_done);
+      } else {
+        ok = wait(&bar.other_done, live_runs & 1) && ok;
+        fence_after();
+        ok = __all_sync(0xffffffffu, ok);
+        const float m1 = bar.m[row], l1 = bar.l[row];
+        const bool two = n > 1;
+        const float mx = two ? fmaxf(m, m1) : m, zero = mx == -kInf ? 0.f : mx;
+        const float f0 = ex2(m - zero), f1 = two ? ex2(m1 - zero) : 0.f;
+        const float sum = two ? l * f0 + l1 * f1 : l * f0;
+        const bool whole = run.from <= kSetupTiles && run.to == run.units;
+        int c0 = 0, c1 = 0;
+        if (!whole) c0 = run.holder(run.first + kSetupTiles), c1 = run.holder(run.first + run.units - 1);
+        auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * S::PART; };
+        float* part = part_of(blockIdx.x);
+        const uint32_t* odd = bar.nodes_bad[runs_done % 4];
+        const uint64_t poison = (odd[0] | (uint64_t)odd[1] << 32) & bits;
+        const bool live = node < live_nodes;
+        auto write = [&](int place, float inv, const float (&x)[8]) {  // 8 places of the row
+          float y[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[place_entry<KIND>(i)] = inv == 0.f ? 0.f : x[i] * inv;
+          if (p.out_f32) {
+            reinterpret_cast<float4*>(out32 + place)[0] = make_float4(y[0], y[1], y[2], y[3]);
+            reinterpret_cast<float4*>(out32 + place)[1] = make_float4(y[4], y[5], y[6], y[7]);
+          } else {
+            *reinterpret_cast<uint4*>(out16 + place) = make_uint4(pack_half2(y[0], y[1]), pack_half2(y[2], y[3]),
+                                                                  pack_half2(y[4], y[5]), pack_half2(y[6], y[7]));
+          }
+        };
+        auto inverse = [&](float total) { return live && total != 0.f ? 1.f / total : 0.f; };
+        if (ok && warp_real) {
+#pragma unroll 1
+          for (int c = 0; c < DIM; c += 32) {
+            float x[32];
+            tmem_load(base + 128 + c, x);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] *= f0;
+            if (two) {
+              float y[32];
+              tmem_load(base + 256 + 128 + c, y);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] = fmaf(y[i], f1, x[i]);
+            }
+            if (poison != 0) {  // infinite and NaN values of nodes that this row sees
+              for (uint64_t left = poison; left != 0; left &= left - 1) {
+                const int slot = run.len + __ffsll((long long)left) - 1;
+                if (slot < run.k_begin || slot >= run.k_end) continue;
+                const int64_t at = kv_row(p.cache, p.pages, run.seq, slot, run.head);
+                if (at < 0) continue;
+                const uint8_t* v = p.cache.v + at * C::RB;
+                const uint8_t* vs = static_cast<const uint8_t*>(p.cache.vs) + at * C::SB;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                  const int e = place_entry<KIND>(c + i);
+                  float y;
+                  if constexpr (F16) {
+                    y = __half2float(reinterpret_cast<const __half*>(v)[e]);
+                  } else if constexpr (INT4) {
+                    const uint32_t sc = reinterpret_cast<const uint32_t*>(vs)[e / 32];
+                    y = fmaf((float)(v[e / 2] >> (e % 2 * 4) & 15), low_float(sc), high_float(sc));
+                  } else {
+                    y = KIND == AF1_KV_INT8 ? (float)(int8_t)v[e]
+                                            : __half2float(__half(__nv_cvt_fp8_to_halfraw(v[e], __NV_E4M3)));
+                  }
+                  y = __half2float(__float2half_rn(y));
+                  if (!(fabsf(y) <= 65504.f)) x[i] += y;
+                }
+              }
+            }
+            if (!real) continue;
+            if (whole) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 8) {
+                const float y[8] = {x[i], x[i + 1], x[i + 2], x[i + 3], x[i + 4], x[i + 5], x[i + 6], x[i + 7]};
+                write(c + i, inverse(sum), y);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) part[(c + i) * kRows + row] = x[i];
+            }
+          }
+          auto write_lse = [&](float top, float total) {
+            if (p.lse != nullptr)
+              p.lse[lse_at] = live && total != 0.f ? (top - kShift + log2f(total)) * 0.69314718056f : -kInf;
+          };
+          if (real && whole) write_lse(mx, sum);
+          if (real && !whole) part[DIM * kRows + row] = mx, part[(DIM + 1) * kRows + row] = sum;
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar.joined);  // both streams' outputs may be overwritten
+        named_sync(1, 128);
+        if (threadIdx.x == 0) bar.nodes_bad[runs_done % 4][0] = bar.nodes_bad[runs_done % 4][1] = 0;
+        if (!whole) {
+          if (threadIdx.x == 0) {  // the group's writes above are released with it
+            const unsigned arrived = atom_add_acq_rel_gpu(&p.counters[c0], 1u);
+            bar.last = arrived == (unsigned)(c1 - c0);
+            if (bar.last) p.counters[c0] = 0;  // as the next call finds it
+          }
+          named_sync(1, 128);
+          if (bar.last && real) {
+            float top = -kInf;
+            for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(part_of(c) + DIM * kRows + row));
+            const float none = top == -kInf ? 0.f : top;
+            float total = 0.f;
+            for (int c = c0; c <= c1; ++c)
+              total += ex2(__ldcg(part_of(c) + DIM * kRows + row) - none) * __ldcg(part_of(c) + (DIM + 1) * kRows + row);
+            const float inv = inverse(total);
+#pragma unroll 1
+            for (int e = 0; e < DIM; e += 16) {
+              float acc[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+              for (int c = c0; c <= c1; ++c) {
+                const float* from = part_of(c);
+                const float f = ex2(__ldcg(from + DIM * kRows + row) - none);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[i] = fmaf(f, __ldcg(from + (e + i) * kRows + row), acc[i]);
+              }
+#pragma unroll
+              for (int i = 0; i < 16; i += 8) {
+                const float y[8] = {acc[i],     acc[i + 1], acc[i + 2], acc[i + 3],
+                                    acc[i + 4], acc[i + 5], acc[i + 6], acc[i + 7]};
+                write(e + i, inv, y);
+              }
+            }
+            if (p.lse != nullptr)
+              p.lse[lse_at] = live && total != 0.f ? (top - kShift + log2f(total)) * 0.69314718056f : -kInf;
+          }
+          named_sync(1, 128);  // bar.last is read
+        }
+      }
+      ++live_runs;
+      tiles_done += n;
+    }
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (bar.gave_up && threadIdx.x == 0) atomicOr(p.status, kStatusTimeout);
+  if (warp == 12) {
+    if (bar.gave_up) {  // products may still be on their way: let them end before their memory goes
+      if (lane == 0) {
+        commit(&bar.q_ready);
+        const long long t0 = clock64();
+        while (clock64() - t0 < 1000000) {
+        }
+      }
+      __syncwarp();
+    }
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+template <int KIND, int DIM>
+cudaError_t launch(const TreeProblem& p, int sms, cudaStream_t st) {
+  constexpr int smem = Wide<KIND, DIM>::SMEM;
+  auto kernel = wide_kernel<KIND, DIM>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  kernel<<<std::min(sms, kMaxCtas), kThreads, smem, st>>>(p);
+  return cudaGetLastError();
+}
+
+template <int KIND>
+cudaError_t launch_kind(const TreeProblem& p, const af1_kv_cache& c, cudaStream_t st) {
+  return c.d.head_dim == 128 ? launch<KIND, 128>(p, c.num_sms, st) : launch<KIND, 64>(p, c.num_sms, st);
+}
+
+}  // namespace
+
+int64_t tree_wide_part_bytes(const af1_kv_cache& c) {
+  return 2 * (int64_t)std::min(c.num_sms, kMaxCtas) * kRows * (c.d.head_dim + 2) * 4;
+}
+
+cudaError_t launch_tree_wide(TreeProblem& p, const af1_kv_cache& c, int rows, cudaStream_t st) {
+  p.row_tiles = (rows + kRows - 1) / kRows;
+  p.k_map = c.d.page_size >= 32 ? c.k32 : c.k16;
+  p.v_map = c.d.page_size >= 32 ? c.v32 : c.v16;
+  switch (c.d.kind) {
+    case AF1_KV_F16: return launch_kind<AF1_KV_F16>(p, c, st);
+    case AF1_KV_INT8: return launch_kind<AF1_KV_INT8>(p, c, st);
+    case AF1_KV_E4M3: return launch_kind<AF1_KV_E4M3>(p, c, st);
+    default: return launch_kind<AF1_KV_INT4>(p, c, st);
+  }
+}
+
+}  // namespace af1
