@@ -11,13 +11,13 @@
 //   S = Q K^T   (128 x 128, FP32, tensor memory)
 //   P = 2^(S f - m + kShift) as FP16, over S
 //   O += P V    (P from tensor memory, V from shared memory)
-// Roles of the 16 warps:
+// Roles of the 19 warps:
 //   0-3, 4-7  softmax of stream 0 and 1: a thread has one row. The scores are
 //             read twice (maximum, weights): held between the passes they
 //             would need 128 registers. The maximum moves, and O with it, only
 //             when a score passes it by 2^kSlack;
-//   8-11      decode: thread i turns key or value i of a tile from codes into
-//             FP16 in the 128-byte-swizzled operand tile (keys K-major, values
+//   8-11, 12-15  decode keys, and values: thread i turns vector i of a tile
+//             from codes into FP16 in the 128-byte-swizzled operand tile (keys K-major, values
 //             with their entries along N). INT8 and E4M3 stay codes, exact in
 //             FP16; a key's scale multiplies the scores, a value's the weights
 //             (relative to a power of two that bounds the scales so far, which
@@ -25,8 +25,8 @@
 //             of 32 entries, is rounded once to FP16, keys too: a score is off
 //             by about 2^-12 sqrt(sum (q k)^2). FP16 tiles arrive by TMA and
 //             are only looked at where a sequence ends;
-//   12        one TMA copy for 16 or 32 rows of a page, into the ring of codes;
-//   13, 14    one thread each issues a stream's products.
+//   16        one TMA copy for 16 or 32 rows of a page, into the ring of codes;
+//   17, 18    one thread each issues a stream's products.
 // Operand tiles pass through four slots in the order K0 K1 V0 K2 V1 K3 ..., in
 // which the products use them.
 //
@@ -44,10 +44,11 @@ namespace af1 {
 namespace {
 
 constexpr int BK = 128;        // keys of a tile
-constexpr int kThreads = 512;
+constexpr int kThreads = 608;
 constexpr int kSetupTiles = 2; // tiles that a run's beginning and end are worth
 constexpr int kRows = 128;
 constexpr int kSlots = 4;
+constexpr int kNotes = 8;      // tiles whose scales and page bits are kept: the decoders run ahead
 constexpr float kLeastScale = -60.f;  // of a value's scale's exponent: smaller ones count as 2^-60
 
 template <int KIND, int DIM>
@@ -58,7 +59,7 @@ struct Wide {
   static constexpr int CODES = BK * C::RB;
   static constexpr int SCALES = (C::SCALED8 ? 2 : 1) * BK * C::SB;  // 8 bits: of keys and values, with the keys
   static constexpr int STAGES = F16 ? kSlots : C::RB >= 128 ? 3 : 4;  // ring of codes (FP16: the slots themselves)
-  static constexpr int SMEM = (kSlots + 1) * OP + (F16 ? 0 : STAGES * (CODES + SCALES)) + 8 * BK * 4 + 1024;
+  static constexpr int SMEM = (kSlots + 1) * OP + (F16 ? 0 : STAGES * (CODES + SCALES)) + 2 * kNotes * BK * 4 + 1024;
   static constexpr int PART = kRows * (DIM + 2);  // floats: o, m, l, each along the rows
 };
 
@@ -67,10 +68,15 @@ struct Barriers {
   uint64_t s_full[2], p_ready[2], pv_done[2], q_ready, other_done, joined;
   uint32_t tmem;
   volatile int gave_up;
-  uint32_t code_bad[kSlots], tile_bad[4];   // bits: 16 keys each whose page is missing
+  uint32_t code_bad[kSlots], tile_bad[kNotes];   // bits: 16 keys each whose page is missing
   uint32_t nodes_bad[4][2];                 // by run: nodes whose value is not finite
   float m[kRows], l[kRows];                 // stream 1's
-  float value_top[4][4];                    // by tile and warp: power of two above the values' scales
+  float value_top[kNotes][4];                    // by tile and warp: power of two above the values' scales
+  // Parts of items that this CTA has left: of its first and of its last run.
+  struct {
+    int c0, c1, seq, head, tile, rows;
+  } part[2];
+  int parts;
   bool last;
 };
 
@@ -229,11 +235,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     mbar_init(&bar.q_ready, 4);
     mbar_init(&bar.other_done, 5);
     mbar_init(&bar.joined, 4);
-    bar.gave_up = 0;
+    bar.gave_up = 0, bar.parts = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
   }
-  if (warp == 12) {
+  if (warp == 16) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bar.tmem)),
                  "r"(512u)
                  : "memory");
@@ -243,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   __syncthreads();
   fence_after();
   const uint32_t tmem = bar.tmem;
-  float* value_scale = key_scale + 4 * BK;
+  float* value_scale = key_scale + kNotes * BK;
 
   // Bounded wait; once one has given up, all return at once.
   auto wait = [&](uint64_t* b, uint32_t parity) {
@@ -260,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   };
 
   int ops_done = 0, tiles_done = 0, runs_done = 0;  // before this run
-  if (warp == 12) {
+  if (warp == 16) {
     // ---- copies ------------------------------------------------------------------
     const int box = p.cache.shift >= 5 ? 32 : 16;
     uint32_t issued_stages = 0;
@@ -329,16 +335,14 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         }
       }
     }
-  } else if (warp >= 8 && warp < 12) {
+  } else if (warp >= 8 && warp < 16) {
     // ---- decode ---------------------------------------------------------------------
-    const int row = threadIdx.x - 256;
+    const int row = threadIdx.x % 128;
+    const bool is_v = warp >= 12;
     for (; run.next(p); ++runs_done) {
       const int n = run.tiles;
-      for (int i = 0; i < 2 * n; ++i) {
-        bool is_v;
-        int j;
-        operand(i, n, is_v, j);
-        const int op = ops_done + i, st = op % S::STAGES, slot = op % kSlots;
+      for (int j = 0; j < n; ++j) {
+        const int op = ops_done + (is_v ? v_index(j, n) : k_index(j)), st = op % S::STAGES, slot = op % kSlots;
         bool ok = wait(&bar.code_full[st], op / S::STAGES & 1);
         if constexpr (!F16) ok = wait(&bar.op_empty[slot], (op / kSlots & 1) ^ 1) && ok;
         ok = __all_sync(0xffffffffu, ok);
@@ -348,30 +352,13 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         const bool node = key >= run.len;
         uint8_t* to = ops + slot * S::OP + row * 128;
         auto place = [&](int c) { return to + (c >> 3) * (BK * 128) + (((c & 7) ^ (row & 7)) << 4); };
-        bool odd_value = false;  // a value that is not finite, of a node
         if (ok) {
-          if constexpr (F16) {
-            if (is_v && (gone || node)) {
-#pragma unroll 4
-              for (int c = 0; c < DIM / 8; ++c) {
-                uint4 v = *reinterpret_cast<uint4*>(place(c));
-                uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  if ((w[e] & 0x7c00u) == 0x7c00u) w[e] &= 0xffff0000u, odd_value = true;
-                  if ((w[e] & 0x7c000000u) == 0x7c000000u) w[e] &= 0x0000ffffu, odd_value = true;
-                  if (gone) w[e] = 0;
-                }
-                *reinterpret_cast<uint4*>(place(c)) = v;
-              }
-            }
-          } else {
+          if constexpr (!F16) {
             const uint8_t* from = codes + st * S::CODES;
             const uint8_t* sc = scales + st * S::SCALES;
-            uint32_t scale2 = 0;
             if constexpr (C::SCALED8) {
               if (!is_v) {
-                const int at = (tiles_done + j) % 4;
+                const int at = (tiles_done + j) % kNotes;
                 const float vs = reinterpret_cast<const float*>(sc)[BK + row];
                 key_scale[at * BK + row] = reinterpret_cast<const float*>(sc)[row] * fabsf(p.scale_log2);
                 value_scale[at * BK + row] = vs;
@@ -381,15 +368,17 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 if (lane == 0) bar.value_top[at][warp % 4] = fmaxf((float)((int)(most >> 23) - 126), kLeastScale);
               }
             }
-#pragma unroll 2
+            // A loop, not unrolled, with the next chunk read ahead: the roles of a
+            // scheduler share its instruction cache.
+            uint4 x = *reinterpret_cast<const uint4*>(from + C::template at<BK>(row, 0));
+            uint32_t group = INT4 ? reinterpret_cast<const uint32_t*>(sc)[row * C::GROUPS] : 0;
+#pragma unroll 1
             for (int c = 0; c < C::RB / 16; ++c) {
-              const uint4 x = *reinterpret_cast<const uint4*>(from + C::template at<BK>(row, c));
               const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-              uint32_t low2 = 0;
-              if constexpr (INT4) {
-                const uint32_t s = reinterpret_cast<const uint32_t*>(sc)[row * C::GROUPS + c];
-                scale2 = prmt(s, s, 0x1010), low2 = prmt(s, s, 0x3232);
-              }
+              const uint32_t scale2 = prmt(group, group, 0x1010), low2 = prmt(group, group, 0x3232);
+              const int ahead = c + 1 < C::RB / 16 ? c + 1 : c;
+              x = *reinterpret_cast<const uint4*>(from + C::template at<BK>(row, ahead));
+              if constexpr (INT4) group = reinterpret_cast<const uint32_t*>(sc)[row * C::GROUPS + ahead];
               constexpr int OUT = INT4 ? 4 : 2;  // 16-byte pieces of FP16
 #pragma unroll
               for (int q = 0; q < OUT; ++q) {
@@ -406,23 +395,30 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                       h[e] = e4m3x2(e % 2 ? u >> 16 : u);
                   }
                 }
-                if (is_v && (gone || node)) {
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) {
-                    if ((h[e] & 0x7c00u) == 0x7c00u) h[e] &= 0xffff0000u, odd_value = true;
-                    if ((h[e] & 0x7c000000u) == 0x7c000000u) h[e] &= 0x0000ffffu, odd_value = true;
-                    if (gone) h[e] = 0;
-                  }
-                }
                 *reinterpret_cast<uint4*>(place(c * OUT + q)) = make_uint4(h[0], h[1], h[2], h[3]);
               }
+            }
+          }
+          bool odd_value = false;  // a value that is not finite, of a node
+          if (is_v && (gone || node)) {
+#pragma unroll 1
+            for (int c = 0; c < DIM / 8; ++c) {
+              uint4 v = *reinterpret_cast<uint4*>(place(c));
+              uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if ((w[e] & 0x7c00u) == 0x7c00u) w[e] &= 0xffff0000u, odd_value = true;
+                if ((w[e] & 0x7c000000u) == 0x7c000000u) w[e] &= 0x0000ffffu, odd_value = true;
+                if (gone) w[e] = 0;
+              }
+              *reinterpret_cast<uint4*>(place(c)) = v;
             }
           }
           if (odd_value && !gone) {
             const int at = key - run.len;
             atomicOr(&bar.nodes_bad[runs_done % 4][at / 32], 1u << (at % 32));
           }
-          if (!is_v && row == 0) bar.tile_bad[(tiles_done + j) % 4] = bad;
+          if (!is_v && row == 0) bar.tile_bad[(tiles_done + j) % kNotes] = bad;
         }
         fence_async();
         __syncwarp();
@@ -433,9 +429,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       }
       ops_done += 2 * n, tiles_done += n;
     }
-  } else if (warp == 13 || warp == 14) {
+  } else if (warp == 17 || warp == 18) {
     // ---- products ---------------------------------------------------------------------
-    const int s = warp - 13;
+    const int s = warp - 17;
     const uint32_t base = tmem + s * 256;
     constexpr uint32_t kScores = 1u << 4 | (uint32_t)(BK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
     constexpr uint32_t kOutput = 1u << 4 | 1u << 16 | (uint32_t)(DIM >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
@@ -485,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     const int s = warp / 4;
     const int row = threadIdx.x % 128;
     const uint32_t base = tmem + s * 256 + ((uint32_t)(warp % 4 * 32) << 16);
-    const float f16_scale = fabsf(p.scale_log2);
+    const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);  // -infinity times it stays so
     int done = 0, live_runs = 0;
     for (; run.next(p); ++runs_done) {
       const int n = run.tiles, rows = run.rows;
@@ -547,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         fence_after();
         ok = __all_sync(0xffffffffu, ok);
         if (ok && warp_real) {
-          const int at_tile = (tiles_done + j) % 4;
+          const int at_tile = (tiles_done + j) % kNotes;
           const float* ks = key_scale + at_tile * BK;
           const float* vs = value_scale + at_tile * BK;
           const uint32_t bad = bar.tile_bad[at_tile];
@@ -557,37 +553,43 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             for (int i = 0; i < 4; ++i) ev_now = fmaxf(ev_now, bar.value_top[at_tile][i]);
           }
           const bool masked = key + BK > min(run.len, run.k_end) || bad != 0;
-          // Columns c .. c + 31 as scores: scaled, and -infinity where the row does not see.
-          auto scores = [&](int c, float (&x)[32]) {
-            tmem_load(base + c, x);
-            if constexpr (C::SCALED8) {
+          auto hide = [&](int c, float (&x)[32]) {  // -infinity where the row does not see
+            auto low = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; };  // n columns
+            const int d = key + c - run.len;  // the first column's node
+            uint32_t sees = low(-d);
+            if (d >= 0) sees |= d < 64 ? (uint32_t)(bits >> d) : 0u;
+            else if (d > -32) sees |= (uint32_t)(bits << -d);
+            sees &= low(run.k_end - key - c);
+            if (bad >> (c / 16) & 1) sees &= 0xffff0000u;
+            if (bad >> (c / 16) & 2) sees &= 0x0000ffffu;
 #pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                const float4 f = *reinterpret_cast<const float4*>(ks + c + i);
-                x[i] *= f.x, x[i + 1] *= f.y, x[i + 2] *= f.z, x[i + 3] *= f.w;
-              }
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] *= f16_scale;
-            }
-            if (masked) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const int at = c + i, k = key + at;
-                const bool sees =
-                    k < run.k_end && !(bad >> (at / 16) & 1) && (k < run.len || (bits >> (k - run.len) & 1));
-                if (!sees) x[i] = -kInf;
-              }
-            }
+            for (int i = 0; i < 32; ++i)
+              if (!(sees >> i & 1)) x[i] = -kInf;
+          };
+          auto factors = [&](int at) {  // of four columns' products
+            return C::SCALED8 ? *reinterpret_cast<const float4*>(ks + at) : make_float4(scale, scale, scale, scale);
           };
           float top = -kInf;
 #pragma unroll 1
           for (int c = 0; c < BK; c += 32) {
             float x[32];
-            scores(c, x);
+            tmem_load(base + c, x);
+            if constexpr (C::SCALED8) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i]);
+              for (int i = 0; i < 32; i += 4) {
+                const float4 f = factors(c + i);
+                const float2 a = mul2(make_float2(x[i], x[i + 1]), make_float2(f.x, f.y));
+                const float2 b = mul2(make_float2(x[i + 2], x[i + 3]), make_float2(f.z, f.w));
+                x[i] = a.x, x[i + 1] = a.y, x[i + 2] = b.x, x[i + 3] = b.y;
+              }
+            }
+            if (masked) hide(c, x);
+            float t0 = x[0], t1 = x[1];
+#pragma unroll
+            for (int i = 2; i < 32; i += 2) t0 = fmaxf(t0, x[i]), t1 = fmaxf(t1, x[i + 1]);
+            top = fmaxf(top, fmaxf(t0, t1));
           }
+          if constexpr (!C::SCALED8) top *= scale;
           if (__any_sync(0xffffffffu, top > m + kSlack || ev_now > ev)) {
             const float now = fmaxf(m, top);
             const float alpha = ex2(m - (now == -kInf ? 0.f : now) + (ev - ev_now));
@@ -615,24 +617,34 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
 #pragma unroll 1
           for (int c = 0; c < BK; c += 32) {
             float x[32];
-            scores(c, x);
-            uint32_t r[16];
-            float sum0 = 0.f, sum1 = 0.f;
+            tmem_load(base + c, x);
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              float a[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) a[e] = ex2(x[2 * i + e] - ref);
-              sum0 += a[0], sum1 += a[1], sum0 += a[2], sum1 += a[3];
-              if constexpr (C::SCALED8) {
-                const float4 f = *reinterpret_cast<const float4*>(vs + c + 2 * i);
-                const float y[4] = {a[0] * f.x, a[1] * f.y, a[2] * f.z, a[3] * f.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) a[e] = masked && a[e] == 0.f ? 0.f : y[e];  // 0 times any scale is 0
-              }
-              r[i] = pack_half2(a[0], a[1]), r[i + 1] = pack_half2(a[2], a[3]);
+            for (int i = 0; i < 32; i += 4) {
+              const float4 f = factors(c + i);
+              const float2 a = fma2(make_float2(x[i], x[i + 1]), make_float2(f.x, f.y), make_float2(-ref, -ref));
+              const float2 b = fma2(make_float2(x[i + 2], x[i + 3]), make_float2(f.z, f.w), make_float2(-ref, -ref));
+              x[i] = a.x, x[i + 1] = a.y, x[i + 2] = b.x, x[i + 3] = b.y;
             }
-            l += sum0 + sum1;
+            if (masked) hide(c, x);
+            uint32_t r[16];
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              float2 a = make_float2(ex2(x[i]), ex2(x[i + 1])), b = make_float2(ex2(x[i + 2]), ex2(x[i + 3]));
+              sum = add2(sum, add2(a, b));
+              if constexpr (C::SCALED8) {
+                const float4 f = *reinterpret_cast<const float4*>(vs + c + i);
+                const float2 wa = mul2(a, make_float2(f.x, f.y)), wb = mul2(b, make_float2(f.z, f.w));
+                if (masked) {  // 0 times any scale is 0
+                  a.x = a.x == 0.f ? 0.f : wa.x, a.y = a.y == 0.f ? 0.f : wa.y;
+                  b.x = b.x == 0.f ? 0.f : wb.x, b.y = b.y == 0.f ? 0.f : wb.y;
+                } else {
+                  a = wa, b = wb;
+                }
+              }
+              r[i / 2] = pack_half2(a.x, a.y), r[i / 2 + 1] = pack_half2(b.x, b.y);
+            }
+            l += sum.x + sum.y;
             tmem_store16(base + c / 2, r);
           }
           tmem_wait_store();
@@ -746,44 +758,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         if (lane == 0) mbar_arrive(&bar.joined);  // both streams' outputs may be overwritten
         named_sync(1, 128);
         if (threadIdx.x == 0) bar.nodes_bad[runs_done % 4][0] = bar.nodes_bad[runs_done % 4][1] = 0;
-        if (!whole) {
-          if (threadIdx.x == 0) {  // the group's writes above are released with it
-            const unsigned arrived = atom_add_acq_rel_gpu(&p.counters[c0], 1u);
-            bar.last = arrived == (unsigned)(c1 - c0);
-            if (bar.last) p.counters[c0] = 0;  // as the next call finds it
-          }
-          named_sync(1, 128);
-          if (bar.last && real) {
-            float top = -kInf;
-            for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(part_of(c) + DIM * kRows + row));
-            const float none = top == -kInf ? 0.f : top;
-            float total = 0.f;
-            for (int c = c0; c <= c1; ++c)
-              total += ex2(__ldcg(part_of(c) + DIM * kRows + row) - none) * __ldcg(part_of(c) + (DIM + 1) * kRows + row);
-            const float inv = inverse(total);
-#pragma unroll 1
-            for (int e = 0; e < DIM; e += 16) {
-              float acc[16];
-#pragma unroll
-              for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-              for (int c = c0; c <= c1; ++c) {
-                const float* from = part_of(c);
-                const float f = ex2(__ldcg(from + DIM * kRows + row) - none);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[i] = fmaf(f, __ldcg(from + (e + i) * kRows + row), acc[i]);
-              }
-#pragma unroll
-              for (int i = 0; i < 16; i += 8) {
-                const float y[8] = {acc[i],     acc[i + 1], acc[i + 2], acc[i + 3],
-                                    acc[i + 4], acc[i + 5], acc[i + 6], acc[i + 7]};
-                write(e + i, inv, y);
-              }
-            }
-            if (p.lse != nullptr)
-              p.lse[lse_at] = live && total != 0.f ? (top - kShift + log2f(total)) * 0.69314718056f : -kInf;
-          }
-          named_sync(1, 128);  // bar.last is read
-        }
+        if (!whole && threadIdx.x == 0) bar.part[bar.parts++] = {c0, c1, run.seq, run.head, run.tile, rows};
       }
       ++live_runs;
       tiles_done += n;
@@ -793,7 +768,75 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   __syncthreads();
   fence_after();
   if (bar.gave_up && threadIdx.x == 0) atomicOr(p.status, kStatusTimeout);
-  if (warp == 12) {
+  // ---- items that span CTAs: the last CTA to arrive joins the parts, in order, all its
+  // threads at it (128 threads with a row each read 64 KB parts at 11 GB/s: 40 us)
+  for (int i = 0; i < bar.parts; ++i) {
+    const int c0 = bar.part[i].c0, c1 = bar.part[i].c1;
+    if (threadIdx.x == 0) {  // the CTA's parts are released with it
+      const unsigned arrived = atom_add_acq_rel_gpu(&p.counters[c0], 1u);
+      bar.last = arrived == (unsigned)(c1 - c0);
+      if (bar.last) p.counters[c0] = 0;  // as the next call finds it
+    }
+    __syncthreads();
+    const int row0 = lane * 4, e0 = warp * 8;  // of this thread: 4 rows, 8 places
+    if (bar.last && e0 < DIM && row0 < bar.part[i].rows) {
+      auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * S::PART; };
+      auto four = [&](const float* from, int e) { return __ldcg(reinterpret_cast<const float4*>(from + e * kRows + row0)); };
+      float top[4], total[4] = {0.f, 0.f, 0.f, 0.f}, acc[8][4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        top[r] = -kInf;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e][r] = 0.f;
+      }
+      for (int c = c0; c <= c1; ++c) {
+        const float4 m = four(part_of(c), DIM);
+        top[0] = fmaxf(top[0], m.x), top[1] = fmaxf(top[1], m.y), top[2] = fmaxf(top[2], m.z), top[3] = fmaxf(top[3], m.w);
+      }
+#pragma unroll 2
+      for (int c = c0; c <= c1; ++c) {
+        const float* from = part_of(c);
+        const float4 m = four(from, DIM), l = four(from, DIM + 1);
+        float4 x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = four(from, e0 + e);
+        const float mr[4] = {m.x, m.y, m.z, m.w}, lr[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float f = ex2(mr[r] - (top[r] == -kInf ? 0.f : top[r]));
+          total[r] = fmaf(f, lr[r], total[r]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            acc[e][r] = fmaf(f, r == 0 ? x[e].x : r == 1 ? x[e].y : r == 2 ? x[e].z : x[e].w, acc[e][r]);
+        }
+      }
+      const int seq = bar.part[i].seq, live_nodes = node_count(p, seq);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (row0 + r >= bar.part[i].rows) break;
+        const int gr = bar.part[i].tile * kRows + row0 + r, node = gr / p.group;
+        const int head = bar.part[i].head * p.group + gr - node * p.group;
+        const bool live = node < live_nodes && total[r] != 0.f;
+        const float inv = live ? 1.f / total[r] : 0.f;
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[place_entry<KIND>(e)] = live ? acc[e][r] * inv : 0.f;
+        const int64_t at = seq * p.o_seq + node * p.o_node + head * p.o_head + e0;
+        if (p.out_f32) {
+          reinterpret_cast<float4*>(static_cast<float*>(p.out) + at)[0] = make_float4(y[0], y[1], y[2], y[3]);
+          reinterpret_cast<float4*>(static_cast<float*>(p.out) + at)[1] = make_float4(y[4], y[5], y[6], y[7]);
+        } else {
+          *reinterpret_cast<uint4*>(static_cast<__half*>(p.out) + at) = make_uint4(
+              pack_half2(y[0], y[1]), pack_half2(y[2], y[3]), pack_half2(y[4], y[5]), pack_half2(y[6], y[7]));
+        }
+        if (warp == 0 && p.lse != nullptr)
+          p.lse[((int64_t)seq * p.nodes + node) * p.cache.heads * p.group + head] =
+              live ? (top[r] - kShift + log2f(total[r])) * 0.69314718056f : -kInf;
+      }
+    }
+    __syncthreads();  // bar.last is read
+  }
+  if (warp == 16) {
     if (bar.gave_up) {  // products may still be on their way: let them end before their memory goes
       if (lane == 0) {
         commit(&bar.q_ready);
