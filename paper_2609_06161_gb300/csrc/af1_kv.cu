@@ -764,6 +764,8 @@ int af1_kv_create(const af1_kv_desc* d, af1_kv_cache** out) {
   bool ok = make_row_map(&c->k16, d->k, rows, row_bytes, 16) && make_row_map(&c->v16, d->v, rows, row_bytes, 16);
   if (d->page_size >= 32)
     ok = ok && make_row_map(&c->k32, d->k, rows, row_bytes, 32) && make_row_map(&c->v32, d->v, rows, row_bytes, 32);
+  const int most = std::min(d->page_size, 128);
+  ok = ok && make_row_map(&c->k128, d->k, rows, row_bytes, most) && make_row_map(&c->v128, d->v, rows, row_bytes, most);
   if (!ok) {
     delete c;
     return fail(AF1_ERR_CUDA, who, "cuTensorMapEncodeTiled failed");

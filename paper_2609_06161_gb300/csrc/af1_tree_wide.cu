@@ -25,7 +25,7 @@
 //             of 32 entries, is rounded once to FP16, keys too: a score is off
 //             by about 2^-12 sqrt(sum (q k)^2). FP16 tiles arrive by TMA and
 //             are only looked at where a sequence ends;
-//   16        one TMA copy for 16 or 32 rows of a page, into the ring of codes;
+//   16        TMA copies, one for up to 128 rows of a page, into the ring of codes;
 //   17, 18    one thread each issues a stream's products.
 // Operand tiles pass through four slots in the order K0 K1 V0 K2 V1 K3 ..., in
 // which the products use them.
@@ -148,25 +148,37 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
                : "memory");
 }
-// Shared-memory matrix: 128-byte swizzle, 8 rows 1024 bytes apart; `lead`: bytes
-// between 64-entry groups where the entries run along M or N.
-__device__ __forceinline__ uint64_t matrix(uint32_t addr, int lead) {
-  return (uint64_t)((addr >> 4) & 0x3fffu) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
-         (uint64_t)1 << 46 | (uint64_t)2 << 61;
+// Shared-memory matrices: 128-byte swizzle, 8 rows 1024 bytes apart; `lead`: bytes
+// between 64-entry groups where the entries run along M or N. The upper half of
+// the description is a constant.
+constexpr uint32_t kMatrixHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t matrix(uint32_t addr, int lead) {
+  return ((addr >> 4) & 0x3fffu) | (uint32_t)(lead >> 4) << 16;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(accumulate ? 1u : 0u), "n"(kMatrixHigh)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
+      "{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.b32 p, %4, 0;\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(accumulate ? 1u : 0u), "n"(kMatrixHigh)
       : "memory");
+}
+// True in one lane of the warp.
+__device__ __forceinline__ bool elect() {
+  uint32_t one;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+  return one != 0;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 // 32 columns of this thread's row.
 __device__ __forceinline__ void tmem_load(uint32_t addr, float (&x)[32]) {
@@ -268,40 +280,41 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   int ops_done = 0, tiles_done = 0, runs_done = 0;  // before this run
   if (warp == 16) {
     // ---- copies ------------------------------------------------------------------
-    const int box = p.cache.shift >= 5 ? 32 : 16;
+    const int box = min(1 << p.cache.shift, BK), boxes = BK / box, group = 32 / boxes;  // tiles whose pages the lanes hold
     uint32_t issued_stages = 0;
     for (; run.next(p); ++runs_done) {
       const int32_t* page_row = p.pages.pages + run.seq * p.pages.ld;
       const int n = run.tiles;
-      auto page_of = [&](int i) {
-        bool is_v;
-        int j;
-        operand(i, n, is_v, j);
-        const int k = run.k_begin + j * BK + lane * box;
-        return lane < BK / box && k < run.k_end ? page_row[k >> p.cache.shift] : -1;
+      auto pages_of = [&](int b) {  // lane l: box l % boxes of tile b group + l / boxes
+        const int k = run.k_begin + (b * 32 + lane) * box;
+        return k < run.k_end ? page_row[k >> p.cache.shift] : -1;
       };
-      int page = n > 0 ? page_of(0) : -1;
+      // Groups of the latest key tile, the one before (values lag by a tile) and the next one.
+      int before = -1, now = n > 0 ? pages_of(0) : -1, next = n > 0 ? pages_of(1) : -1, held = 0;
       for (int i = 0; i < 2 * n; ++i) {
         bool is_v;
         int j;
         operand(i, n, is_v, j);
         const int op = ops_done + i, st = op % S::STAGES;
+        const int b = j / group;
+        if (b > held) {
+          before = now, now = next, ++held;
+          next = pages_of(held + 1);
+        }
+        const int page = __shfl_sync(0xffffffffu, b == held ? now : before, ((j % group) * boxes + lane) & 31);
         const int k = run.k_begin + j * BK + lane * box;
-        const bool there = page >= 0 && page < p.cache.pages;
+        const bool mine = lane < boxes && k < run.k_end;
+        const bool there = mine && page >= 0 && page < p.cache.pages;
         const unsigned have = __ballot_sync(0xffffffffu, there);
-        const unsigned lack = __ballot_sync(0xffffffffu, !there && lane < BK / box && k < run.k_end);
+        const unsigned lack = __ballot_sync(0xffffffffu, mine && !there);
         const int64_t row =
             (((int64_t)page * p.cache.heads + run.head) << p.cache.shift) + (k & ((1 << p.cache.shift) - 1));
-        if (i + 1 < 2 * n) page = page_of(i + 1);
         const bool ok = wait(F16 ? &bar.op_empty[st] : &bar.code_empty[st], (op / S::STAGES & 1) ^ 1);
         if (!__all_sync(0xffffffffu, ok)) continue;
         if (lane == 0) {
-          uint32_t bad = lack;
-          if (box == 32) {  // a bit for each 16 keys
-            bad = 0;
-            for (int b = 0; b < 4; ++b)
-              if (lack >> b & 1) bad |= 3u << (2 * b);
-          }
+          uint32_t bad = 0;  // a bit for each 16 keys
+          for (unsigned left = lack; left != 0; left &= left - 1)
+            bad |= ((1u << (box / 16)) - 1) << ((__ffs(left) - 1) * (box / 16));
           bar.code_bad[st] = bad;
           const int per_key = C::RB + (C::SCALED8 ? (is_v ? 0 : 2 * C::SB) : C::SB);
           mbar_expect_tx(&bar.code_full[st], __popc(have) * box * per_key);
@@ -386,7 +399,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   if constexpr (INT4) {
-                    h[e] = hfma2(hsub2((w[q] >> (4 * e) & 0x000f000fu) | 0x64006400u, 0x64006400u), scale2, low2);
+                    // As fraction bits of 1024 + code, or, 4 bits up, of 64 + code.
+                    const uint32_t u = e < 2 ? w[q] : w[q] >> 8;
+                    h[e] = e % 2 ? hsub2((u & 0x00f000f0u) | 0x54005400u, 0x54005400u)
+                                 : hsub2((u & 0x000f000fu) | 0x64006400u, 0x64006400u);
+                    h[e] = hfma2(h[e], scale2, low2);
                   } else {
                     const uint32_t u = w[2 * q + e / 2];
                     if constexpr (KIND == AF1_KV_INT8)
@@ -431,48 +448,58 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     }
   } else if (warp == 17 || warp == 18) {
     // ---- products ---------------------------------------------------------------------
-    const int s = warp - 17;
-    const uint32_t base = tmem + s * 256;
+    // The whole warp runs the loop and one elected lane issues: values that the
+    // compiler knows to be alike in all lanes (read from lane 0) stay in the
+    // registers that the instruction takes.
+    const int s = __shfl_sync(0xffffffffu, warp - 17, 0);
+    const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0) + s * 256;
+    const uint32_t q_matrix = matrix(smem_u32(qt), 16), op_matrix = matrix(smem_u32(ops), 16);
+    constexpr uint32_t kLead = (uint32_t)(BK * 128 - 16) >> 4 << 16;  // values: 64 entries in a group
     constexpr uint32_t kScores = 1u << 4 | (uint32_t)(BK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
     constexpr uint32_t kOutput = 1u << 4 | 1u << 16 | (uint32_t)(DIM >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
     int done = 0;  // tiles of this stream
     int q_runs = 0;
     for (; run.next(p); ++runs_done) {
-      const int n = run.tiles;
+      const int n = __shfl_sync(0xffffffffu, run.tiles, 0);
       if (n > 0) {
-        bool ok = true;
-        if (lane == 0) {
-          ok = wait(&bar.q_ready, q_runs & 1);
-          if (s == 1) mbar_arrive(&bar.other_done);  // q_ready is not two phases ahead of this thread
-        }
+        bool ok = wait(&bar.q_ready, q_runs & 1);
+        __syncwarp();
+        if (s == 1 && lane == 0) mbar_arrive(&bar.other_done);  // q_ready is not two phases ahead of this warp
         ++q_runs;
-        for (int j = s; j < n && lane == 0; j += 2, ++done) {
+        for (int j = s; j < n; j += 2, ++done) {
           const int ko = ops_done + k_index(j), vo = ops_done + v_index(j, n);
           ok = wait(&bar.op_ready[ko % kSlots], ko / kSlots & 1) && ok;
+          ok = __all_sync(0xffffffffu, ok);
           fence_after();
-          if (ok) {
-            const uint32_t a = smem_u32(qt), b = smem_u32(ops + ko % kSlots * S::OP);
+          if (elect()) {
+            if (ok) {
+              const uint32_t b = op_matrix + ko % kSlots * (S::OP >> 4);
 #pragma unroll
-            for (int ks = 0; ks < DIM / 16; ++ks) {
-              const int off = (ks / 4) * (BK * 128) + (ks % 4) * 32;
-              mma_ss(base, matrix(a + off, 16), matrix(b + off, 16), kScores, ks > 0);
+              for (int ks = 0; ks < DIM / 16; ++ks) {
+                const int off = ((ks / 4) * (BK * 128) + (ks % 4) * 32) >> 4;
+                mma_ss(base, q_matrix + off, b + off, kScores, ks > 0);
+              }
             }
+            commit(&bar.s_full[s]);
+            commit(&bar.op_empty[ko % kSlots]);
           }
-          commit(&bar.op_empty[ko % kSlots]);
-          commit(&bar.s_full[s]);
+          __syncwarp();
           ok = wait(&bar.op_ready[vo % kSlots], vo / kSlots & 1) && ok;
           ok = wait(&bar.p_ready[s], done & 1) && ok;
+          ok = __all_sync(0xffffffffu, ok);
           fence_after();
-          if (ok) {
-            const uint32_t b = smem_u32(ops + vo % kSlots * S::OP);
+          if (elect()) {
+            if (ok) {
+              const uint32_t b = op_matrix + kLead + vo % kSlots * (S::OP >> 4);
 #pragma unroll
-            for (int ks = 0; ks < BK / 16; ++ks)
-              mma_ts(base + 128, base + ks * 8, matrix(b + ks * 2048, BK * 128), kOutput, j > s || ks > 0);
+              for (int ks = 0; ks < BK / 16; ++ks)
+                mma_ts(base + 128, base + ks * 8, b + (ks * 2048 >> 4), kOutput, j > s || ks > 0);
+            }
+            commit(&bar.pv_done[s]);
+            commit(&bar.op_empty[vo % kSlots]);
           }
-          commit(&bar.op_empty[vo % kSlots]);
-          commit(&bar.pv_done[s]);
+          __syncwarp();
         }
-        __syncwarp();
       }
       ops_done += 2 * n;
     }
@@ -586,8 +613,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             if (masked) hide(c, x);
             float t0 = x[0], t1 = x[1];
 #pragma unroll
-            for (int i = 2; i < 32; i += 2) t0 = fmaxf(t0, x[i]), t1 = fmaxf(t1, x[i + 1]);
-            top = fmaxf(top, fmaxf(t0, t1));
+            for (int i = 2; i < 30; i += 4) t0 = max3(t0, x[i], x[i + 1]), t1 = max3(t1, x[i + 2], x[i + 3]);
+            top = max3(top, max3(t0, x[30], x[31]), t1);
           }
           if constexpr (!C::SCALED8) top *= scale;
           if (__any_sync(0xffffffffu, top > m + kSlack || ev_now > ev)) {
@@ -873,8 +900,7 @@ int64_t tree_wide_part_bytes(const af1_kv_cache& c) {
 
 cudaError_t launch_tree_wide(TreeProblem& p, const af1_kv_cache& c, int rows, cudaStream_t st) {
   p.row_tiles = (rows + kRows - 1) / kRows;
-  p.k_map = c.d.page_size >= 32 ? c.k32 : c.k16;
-  p.v_map = c.d.page_size >= 32 ? c.v32 : c.v16;
+  p.k_map = c.k128, p.v_map = c.v128;
   switch (c.d.kind) {
     case AF1_KV_F16: return launch_kind<AF1_KV_F16>(p, c, st);
     case AF1_KV_INT8: return launch_kind<AF1_KV_INT8>(p, c, st);
