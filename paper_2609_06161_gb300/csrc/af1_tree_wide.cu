@@ -4,18 +4,20 @@
 //
 // An item is one sequence, one cached head and a block of 128 rows; its keys
 // are cut into tiles of 128, and every CTA (one to an SM) takes an equal run
-// of the tiles of all items, as in af1_tree.cu. The tiles of a run alternate
-// between two streams, each with its own scores, maximum, sum and output, so
-// that one stream's products run under the other's exponents; the streams are
-// joined at the end of a run. For one tile
+// of the tiles of all items, as in af1_tree.cu. For one tile
 //   S = Q K^T   (128 x 128, FP32, tensor memory)
-//   P = 2^(S f - m + kShift) as FP16, over S
+//   P = 2^(S f - m + kShift) as FP16, tensor memory
 //   O += P V    (P from tensor memory, V from shared memory)
+// S and P have two buffers, so that the products of one tile run under the
+// exponents of another. (Two streams of tiles, each with scores, weights and
+// output of its own, waited for one another's latencies: 115 us for trees of
+// 64 over 32768 INT4 tokens.)
 // Roles of the 19 warps:
-//   0-3, 4-7  softmax of stream 0 and 1: a thread has one row. The scores are
-//             read twice (maximum, weights): held between the passes they
-//             would need 128 registers. The maximum moves, and O with it, only
-//             when a score passes it by 2^kSlack;
+//   0-3, 4-7  softmax of the tile's first and second 64 keys: a thread has one
+//             row. The scores are read twice (maximum, weights): held between
+//             the passes they would need 64 registers more. The maximum of
+//             both halves moves, and O with it, only when a score passes it by
+//             2^kSlack;
 //   8-11, 12-15  decode keys, and values: thread i turns vector i of a tile
 //             from codes into FP16 in the 128-byte-swizzled operand tile (keys K-major, values
 //             with their entries along N). INT8 and E4M3 stay codes, exact in
@@ -26,7 +28,7 @@
 //             by about 2^-12 sqrt(sum (q k)^2). FP16 tiles arrive by TMA and
 //             are only looked at where a sequence ends;
 //   16        TMA copies, one for up to 128 rows of a page, into the ring of codes;
-//   17, 18    one thread each issues a stream's products.
+//   17, 18    one lane each issues Q K^T, and P V.
 // Operand tiles pass through four slots in the order K0 K1 V0 K2 V1 K3 ..., in
 // which the products use them.
 //
@@ -47,6 +49,7 @@ constexpr int BK = 128;        // keys of a tile
 constexpr int kThreads = 608;
 constexpr int kSetupTiles = 2; // tiles that a run's beginning and end are worth
 constexpr int kRows = 128;
+constexpr int kOutAt = 2 * BK, kWeightsAt = 3 * BK;  // columns of tensor memory, behind two tiles of scores
 constexpr int kSlots = 4;
 constexpr int kNotes = 8;      // tiles whose scales and page bits are kept: the decoders run ahead
 constexpr float kLeastScale = -60.f;  // of a value's scale's exponent: smaller ones count as 2^-60
@@ -65,12 +68,12 @@ struct Wide {
 
 struct Barriers {
   uint64_t op_ready[kSlots], op_empty[kSlots], code_full[kSlots], code_empty[kSlots];
-  uint64_t s_full[2], p_ready[2], pv_done[2], q_ready, other_done, joined;
+  uint64_t s_full[2], p_ready[2], pv_done[2], q_ready;  // by tile
   uint32_t tmem;
   volatile int gave_up;
   uint32_t code_bad[kSlots], tile_bad[kNotes];   // bits: 16 keys each whose page is missing
   uint32_t nodes_bad[4][2];                 // by run: nodes whose value is not finite
-  float m[kRows], l[kRows];                 // stream 1's
+  float top[2][2][kRows], sum[2][kRows];    // of the halves of a tile (by tile), and of a run
   float value_top[kNotes][4];                    // by tile and warp: power of two above the values' scales
   // Parts of items that this CTA has left: of its first and of its last run.
   struct {
@@ -241,12 +244,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bar.s_full[i], 1);
-      mbar_init(&bar.p_ready[i], 4);
+      mbar_init(&bar.p_ready[i], 8);
       mbar_init(&bar.pv_done[i], 1);
     }
-    mbar_init(&bar.q_ready, 4);
-    mbar_init(&bar.other_done, 5);
-    mbar_init(&bar.joined, 4);
+    mbar_init(&bar.q_ready, 8);
     bar.gave_up = 0, bar.parts = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
@@ -451,65 +452,57 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     // The whole warp runs the loop and one elected lane issues: values that the
     // compiler knows to be alike in all lanes (read from lane 0) stay in the
     // registers that the instruction takes.
-    const int s = __shfl_sync(0xffffffffu, warp - 17, 0);
-    const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0) + s * 256;
+    const bool second = __shfl_sync(0xffffffffu, warp, 0) == 18;
+    const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0);
     const uint32_t q_matrix = matrix(smem_u32(qt), 16), op_matrix = matrix(smem_u32(ops), 16);
     constexpr uint32_t kLead = (uint32_t)(BK * 128 - 16) >> 4 << 16;  // values: 64 entries in a group
     constexpr uint32_t kScores = 1u << 4 | (uint32_t)(BK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
     constexpr uint32_t kOutput = 1u << 4 | 1u << 16 | (uint32_t)(DIM >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
-    int done = 0;  // tiles of this stream
-    int q_runs = 0;
+    int live_runs = 0;
     for (; run.next(p); ++runs_done) {
       const int n = __shfl_sync(0xffffffffu, run.tiles, 0);
-      if (n > 0) {
-        bool ok = wait(&bar.q_ready, q_runs & 1);
-        __syncwarp();
-        if (s == 1 && lane == 0) mbar_arrive(&bar.other_done);  // q_ready is not two phases ahead of this warp
-        ++q_runs;
-        for (int j = s; j < n; j += 2, ++done) {
-          const int ko = ops_done + k_index(j), vo = ops_done + v_index(j, n);
-          ok = wait(&bar.op_ready[ko % kSlots], ko / kSlots & 1) && ok;
-          ok = __all_sync(0xffffffffu, ok);
-          fence_after();
-          if (elect()) {
-            if (ok) {
-              const uint32_t b = op_matrix + ko % kSlots * (S::OP >> 4);
+      if (n == 0) continue;
+      bool ok = true;
+      if (!second) ok = wait(&bar.q_ready, live_runs & 1);
+      ++live_runs;
+      for (int j = 0; j < n; ++j) {
+        const int at = tiles_done + j, buf = at & 1;
+        const int op = ops_done + (second ? v_index(j, n) : k_index(j)), slot = op % kSlots;
+        ok = wait(&bar.op_ready[slot], op / kSlots & 1) && ok;
+        // The tile's weights, or those of the tile whose scores were there before.
+        if (second) ok = wait(&bar.p_ready[buf], at >> 1 & 1) && ok;
+        else if (at >= 2) ok = wait(&bar.p_ready[buf], (at - 2) >> 1 & 1) && ok;
+        ok = __all_sync(0xffffffffu, ok);
+        fence_after();
+        if (elect()) {
+          if (ok && !second) {
+            const uint32_t b = op_matrix + slot * (S::OP >> 4);
 #pragma unroll
-              for (int ks = 0; ks < DIM / 16; ++ks) {
-                const int off = ((ks / 4) * (BK * 128) + (ks % 4) * 32) >> 4;
-                mma_ss(base, q_matrix + off, b + off, kScores, ks > 0);
-              }
+            for (int ks = 0; ks < DIM / 16; ++ks) {
+              const int off = ((ks / 4) * (BK * 128) + (ks % 4) * 32) >> 4;
+              mma_ss(base + buf * BK, q_matrix + off, b + off, kScores, ks > 0);
             }
-            commit(&bar.s_full[s]);
-            commit(&bar.op_empty[ko % kSlots]);
-          }
-          __syncwarp();
-          ok = wait(&bar.op_ready[vo % kSlots], vo / kSlots & 1) && ok;
-          ok = wait(&bar.p_ready[s], done & 1) && ok;
-          ok = __all_sync(0xffffffffu, ok);
-          fence_after();
-          if (elect()) {
-            if (ok) {
-              const uint32_t b = op_matrix + kLead + vo % kSlots * (S::OP >> 4);
+          } else if (ok) {
+            const uint32_t b = op_matrix + kLead + slot * (S::OP >> 4);
 #pragma unroll
-              for (int ks = 0; ks < BK / 16; ++ks)
-                mma_ts(base + 128, base + ks * 8, b + (ks * 2048 >> 4), kOutput, j > s || ks > 0);
-            }
-            commit(&bar.pv_done[s]);
-            commit(&bar.op_empty[vo % kSlots]);
+            for (int ks = 0; ks < BK / 16; ++ks)
+              mma_ts(base + kOutAt, base + kWeightsAt + buf * (BK / 2) + ks * 8, b + (ks * 2048 >> 4), kOutput,
+                     j > 0 || ks > 0);
           }
-          __syncwarp();
+          commit(second ? &bar.pv_done[buf] : &bar.s_full[buf]);
+          commit(&bar.op_empty[slot]);
         }
+        __syncwarp();
       }
-      ops_done += 2 * n;
+      ops_done += 2 * n, tiles_done += n;
     }
   } else if (warp < 8) {
     // ---- softmax, and the ends of the runs ------------------------------------------------
-    const int s = warp / 4;
+    const int half = warp / 4;  // of a tile's keys, and of the output's entries
     const int row = threadIdx.x % 128;
-    const uint32_t base = tmem + s * 256 + ((uint32_t)(warp % 4 * 32) << 16);
+    const uint32_t base = tmem + ((uint32_t)(warp % 4 * 32) << 16);
     const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);  // -infinity times it stays so
-    int done = 0, live_runs = 0;
+    const int e0 = half * (DIM / 2);
     for (; run.next(p); ++runs_done) {
       const int n = run.tiles, rows = run.rows;
       const int gr = run.tile * kRows + row, node = gr / p.group, head = run.head * p.group + gr - node * p.group;
@@ -518,7 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       __half* out16 = static_cast<__half*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
       float* out32 = static_cast<float*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
       const int64_t lse_at = ((int64_t)run.seq * p.nodes + node) * p.cache.heads * p.group + head;
-      if (run.keys == 0 && run.from == 0 && s == 0 && real) {  // nothing to see: the item's first CTA writes its zeros
+      if (run.keys == 0 && run.from == 0 && half == 0 && real) {  // nothing to see: the item's first CTA writes its zeros
         for (int e = 0; e < DIM; e += 8) {
           if (p.out_f32) {
             reinterpret_cast<float4*>(out32 + e)[0] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -530,13 +523,13 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         if (p.lse != nullptr) p.lse[lse_at] = -kInf;
       }
       if (n == 0) continue;
-      if (s == 0) {
-        // q of this run (the products of the run before are done); a negative
+      {
+        // q of this run (the products with the one before are done); a negative
         // scale turns its signs.
         const __half* q = p.q + run.seq * p.q_seq + node * p.q_node + (int64_t)head * p.q_head;
         const uint32_t sign = p.scale_log2 < 0.f ? 0x80008000u : 0u;
 #pragma unroll 4
-        for (int c = 0; c < DIM / 8; ++c) {
+        for (int c = half * (DIM / 16); c < (half + 1) * (DIM / 16); ++c) {
           uint4 v = make_uint4(0, 0, 0, 0);
           if (real) v = *reinterpret_cast<const uint4*>(q + 8 * c);
           if constexpr (INT4)
@@ -562,45 +555,42 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       // Weights are 2^(score - m - ev + kShift), times a value's scale, which is below 2^ev.
       float m = -kInf, l = 0.f, ev = C::SCALED8 ? kLeastScale : 0.f;
       bool ok = true;
-      // Stream 1's output of the run before is read until then.
-      if (s == 1 && live_runs > 0) ok = wait(&bar.joined, (live_runs - 1) & 1);
-      for (int j = s; j < n; j += 2, ++done) {
-        const int key = run.k_begin + j * BK;
-        ok = wait(&bar.s_full[s], done & 1) && ok;
+      for (int j = 0; j < n; ++j) {
+        const int key = run.k_begin + j * BK, at = tiles_done + j, buf = at & 1;
+        ok = wait(&bar.s_full[buf], at >> 1 & 1) && ok;
+        if (at >= 2) ok = wait(&bar.pv_done[buf], (at - 2) >> 1 & 1) && ok;  // these weights' place
         fence_after();
         ok = __all_sync(0xffffffffu, ok);
-        if (ok && warp_real) {
-          const int at_tile = (tiles_done + j) % kNotes;
-          const float* ks = key_scale + at_tile * BK;
-          const float* vs = value_scale + at_tile * BK;
-          const uint32_t bad = bar.tile_bad[at_tile];
-          float ev_now = ev;
-          if constexpr (C::SCALED8) {
+        const uint32_t scores = base + buf * BK + half * (BK / 2);
+        const int c_first = half * (BK / 2);  // column of the tile
+        const int at_tile = at % kNotes;
+        const bool work = ok && warp_real;
+        const uint32_t bad = bar.tile_bad[at_tile];
+        const bool masked = key + BK > min(run.len, run.k_end) || bad != 0;
+        const float* ks = key_scale + at_tile * BK + c_first;
+        const float* vs = value_scale + at_tile * BK + c_first;
+        float top = -kInf;
+        auto hide = [&](int c, float (&x)[32]) {  // -infinity where the row does not see
+          auto low = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; };  // n columns
+          const int k0 = key + c_first + c, d = k0 - run.len;  // the first column's key, and node
+          uint32_t sees = low(-d);
+          if (d >= 0) sees |= d < 64 ? (uint32_t)(bits >> d) : 0u;
+          else if (d > -32) sees |= (uint32_t)(bits << -d);
+          sees &= low(run.k_end - k0);
+          if (bad >> ((c_first + c) / 16) & 1) sees &= 0xffff0000u;
+          if (bad >> ((c_first + c) / 16) & 2) sees &= 0x0000ffffu;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ev_now = fmaxf(ev_now, bar.value_top[at_tile][i]);
-          }
-          const bool masked = key + BK > min(run.len, run.k_end) || bad != 0;
-          auto hide = [&](int c, float (&x)[32]) {  // -infinity where the row does not see
-            auto low = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; };  // n columns
-            const int d = key + c - run.len;  // the first column's node
-            uint32_t sees = low(-d);
-            if (d >= 0) sees |= d < 64 ? (uint32_t)(bits >> d) : 0u;
-            else if (d > -32) sees |= (uint32_t)(bits << -d);
-            sees &= low(run.k_end - key - c);
-            if (bad >> (c / 16) & 1) sees &= 0xffff0000u;
-            if (bad >> (c / 16) & 2) sees &= 0x0000ffffu;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!(sees >> i & 1)) x[i] = -kInf;
-          };
-          auto factors = [&](int at) {  // of four columns' products
-            return C::SCALED8 ? *reinterpret_cast<const float4*>(ks + at) : make_float4(scale, scale, scale, scale);
-          };
-          float top = -kInf;
+          for (int i = 0; i < 32; ++i)
+            if (!(sees >> i & 1)) x[i] = -kInf;
+        };
+        auto factors = [&](int at) {  // of four columns' products
+          return C::SCALED8 ? *reinterpret_cast<const float4*>(ks + at) : make_float4(scale, scale, scale, scale);
+        };
+        if (work) {
 #pragma unroll 1
-          for (int c = 0; c < BK; c += 32) {
+          for (int c = 0; c < BK / 2; c += 32) {
             float x[32];
-            tmem_load(base + c, x);
+            tmem_load(scores + c, x);
             if constexpr (C::SCALED8) {
 #pragma unroll
               for (int i = 0; i < 32; i += 4) {
@@ -617,34 +607,45 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             top = max3(top, max3(t0, x[30], x[31]), t1);
           }
           if constexpr (!C::SCALED8) top *= scale;
+        }
+        // Both halves' maximum.
+        bar.top[buf][half][row] = top;
+        named_sync(2, 256);
+        top = fmaxf(top, bar.top[buf][half ^ 1][row]);
+        if (work) {
+          float ev_now = ev;
+          if constexpr (C::SCALED8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ev_now = fmaxf(ev_now, bar.value_top[at_tile][i]);
+          }
           if (__any_sync(0xffffffffu, top > m + kSlack || ev_now > ev)) {
             const float now = fmaxf(m, top);
             const float alpha = ex2(m - (now == -kInf ? 0.f : now) + (ev - ev_now));
             m = now, ev = ev_now;
             l *= alpha;
-            if (j > s) {
-              ok = wait(&bar.pv_done[s], (done - 1) & 1);
+            if (j > 0) {
+              ok = wait(&bar.pv_done[buf ^ 1], (at - 1) >> 1 & 1);
               ok = __all_sync(0xffffffffu, ok);
               fence_after();
 #pragma unroll 1
-              for (int c = 0; c < DIM; c += 32) {
+              for (int c = e0; c < e0 + DIM / 2; c += 32) {
                 float x[32];
-                tmem_load(base + 128 + c, x);
+                tmem_load(base + kOutAt + c, x);
                 uint32_t r[16];
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf) {
 #pragma unroll
                   for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(x[16 * hf + i] * alpha);
-                  tmem_store16(base + 128 + c + 16 * hf, r);
+                  tmem_store16(base + kOutAt + c + 16 * hf, r);
                 }
               }
             }
           }
           const float ref = (m == -kInf ? 0.f : m) + ev - kShift;
 #pragma unroll 1
-          for (int c = 0; c < BK; c += 32) {
+          for (int c = 0; c < BK / 2; c += 32) {
             float x[32];
-            tmem_load(base + c, x);
+            tmem_load(scores + c, x);
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
               const float4 f = factors(c + i);
@@ -672,42 +673,32 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
               r[i / 2] = pack_half2(a.x, a.y), r[i / 2 + 1] = pack_half2(b.x, b.y);
             }
             l += sum.x + sum.y;
-            tmem_store16(base + c / 2, r);
+            tmem_store16(base + kWeightsAt + buf * (BK / 2) + (c_first + c) / 2, r);
           }
           tmem_wait_store();
         }
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bar.p_ready[s]);
+        if (lane == 0) mbar_arrive(&bar.p_ready[buf]);
       }
       m += ev;  // the reference that sums and outputs share
       // -- the run's end ------------------------------------------------------------------
-      const int mine = (n - s + 1) / 2;  // tiles of this stream
-      if (mine > 0) {
-        ok = wait(&bar.pv_done[s], (done - 1) & 1) && ok;
-        fence_after();
-      }
-      if (s == 1) {
-        bar.m[row] = m, bar.l[row] = l;
-        fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar.other_done);
-      } else {
-        ok = wait(&bar.other_done, live_runs & 1) && ok;
+      {
+        const int last = tiles_done + n - 1;
+        bar.sum[half][row] = l;
+        ok = wait(&bar.pv_done[last & 1], last >> 1 & 1) && ok;
         fence_after();
         ok = __all_sync(0xffffffffu, ok);
-        const float m1 = bar.m[row], l1 = bar.l[row];
-        const bool two = n > 1;
-        const float mx = two ? fmaxf(m, m1) : m, zero = mx == -kInf ? 0.f : mx;
-        const float f0 = ex2(m - zero), f1 = two ? ex2(m1 - zero) : 0.f;
-        const float sum = two ? l * f0 + l1 * f1 : l * f0;
+        const uint32_t* odd = bar.nodes_bad[runs_done % 4];
+        const uint64_t poison = (odd[0] | (uint64_t)odd[1] << 32) & bits;
+        named_sync(2, 256);
+        if (threadIdx.x == 0) bar.nodes_bad[runs_done % 4][0] = bar.nodes_bad[runs_done % 4][1] = 0;
+        const float sum = l + bar.sum[half ^ 1][row];
         const bool whole = run.from <= kSetupTiles && run.to == run.units;
         int c0 = 0, c1 = 0;
         if (!whole) c0 = run.holder(run.first + kSetupTiles), c1 = run.holder(run.first + run.units - 1);
         auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * S::PART; };
         float* part = part_of(blockIdx.x);
-        const uint32_t* odd = bar.nodes_bad[runs_done % 4];
-        const uint64_t poison = (odd[0] | (uint64_t)odd[1] << 32) & bits;
         const bool live = node < live_nodes;
         auto write = [&](int place, float inv, const float (&x)[8]) {  // 8 places of the row
           float y[8];
@@ -724,17 +715,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         auto inverse = [&](float total) { return live && total != 0.f ? 1.f / total : 0.f; };
         if (ok && warp_real) {
 #pragma unroll 1
-          for (int c = 0; c < DIM; c += 32) {
+          for (int c = e0; c < e0 + DIM / 2; c += 32) {
             float x[32];
-            tmem_load(base + 128 + c, x);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] *= f0;
-            if (two) {
-              float y[32];
-              tmem_load(base + 256 + 128 + c, y);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] = fmaf(y[i], f1, x[i]);
-            }
+            tmem_load(base + kOutAt + c, x);
             if (poison != 0) {  // infinite and NaN values of nodes that this row sees
               for (uint64_t left = poison; left != 0; left &= left - 1) {
                 const int slot = run.len + __ffsll((long long)left) - 1;
@@ -761,33 +744,25 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 }
               }
             }
-            if (!real) continue;
-            if (whole) {
+            if (real && whole) {
 #pragma unroll
               for (int i = 0; i < 32; i += 8) {
                 const float y[8] = {x[i], x[i + 1], x[i + 2], x[i + 3], x[i + 4], x[i + 5], x[i + 6], x[i + 7]};
                 write(c + i, inverse(sum), y);
               }
-            } else {
+            } else if (real) {
 #pragma unroll
               for (int i = 0; i < 32; ++i) part[(c + i) * kRows + row] = x[i];
             }
           }
-          auto write_lse = [&](float top, float total) {
-            if (p.lse != nullptr)
-              p.lse[lse_at] = live && total != 0.f ? (top - kShift + log2f(total)) * 0.69314718056f : -kInf;
-          };
-          if (real && whole) write_lse(mx, sum);
-          if (real && !whole) part[DIM * kRows + row] = mx, part[(DIM + 1) * kRows + row] = sum;
+          if (real && half == 0) {
+            if (!whole) part[DIM * kRows + row] = m, part[(DIM + 1) * kRows + row] = sum;
+            else if (p.lse != nullptr)
+              p.lse[lse_at] = live && sum != 0.f ? (m - kShift + log2f(sum)) * 0.69314718056f : -kInf;
+          }
         }
-        fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar.joined);  // both streams' outputs may be overwritten
-        named_sync(1, 128);
-        if (threadIdx.x == 0) bar.nodes_bad[runs_done % 4][0] = bar.nodes_bad[runs_done % 4][1] = 0;
         if (!whole && threadIdx.x == 0) bar.part[bar.parts++] = {c0, c1, run.seq, run.head, run.tile, rows};
       }
-      ++live_runs;
       tiles_done += n;
     }
   }
