@@ -66,7 +66,12 @@ struct Wide {
   static constexpr int PART = kRows * (DIM + 2);  // floats: o, m, l, each along the rows
 };
 
+struct Plan {
+  int64_t per, more, end;  // units of a CTA, the CTAs with one more, and where this one's end
+};
+
 struct Barriers {
+  Plan plan;
   uint64_t op_ready[kSlots], op_empty[kSlots], code_full[kSlots], code_empty[kSlots];
   uint64_t s_full[2], p_ready[2], pv_done[2], q_ready;  // by tile
   uint32_t tmem;
@@ -83,33 +88,35 @@ struct Barriers {
   bool last;
 };
 
-// The runs of this CTA, one after another, known to every warp.
+// The runs of this CTA, one after another, known to every warp. What stays the
+// same lies in shared memory: every thread of the softmax needs its registers.
 struct Runs {
   Sequences<BK, kSetupTiles> sq;
-  int64_t lanes, total, ctas, per, more, pos, end;
-  int seq, head, tile, rows, len, keys, units, from, to, k_begin, k_end, tiles;
-  int64_t first;
+  int64_t pos, first;
+  int seq, head, tile, len, keys, units, from, to, k_begin, k_end, tiles;
 
-  __device__ __forceinline__ bool begin(const TreeProblem& p) {
-    lanes = (int64_t)p.cache.heads * p.row_tiles;
+  __device__ __forceinline__ bool begin(const TreeProblem& p, Plan& plan) {
+    const int64_t lanes = (int64_t)p.cache.heads * p.row_tiles;
     sq.load(p, 0, 0);
-    total = sq.after();
+    int64_t total = sq.after();
     for (int at = 32; at < p.pages.seqs; at += 32) {
       sq.load(p, at, total);
       total = sq.after();
     }
     if (p.pages.seqs > 32) sq.load(p, 0, 0);
     total *= lanes;
-    ctas = min((int64_t)gridDim.x, total);
+    const int64_t ctas = min((int64_t)gridDim.x, total);
     if (blockIdx.x >= ctas) return false;
-    per = total / ctas, more = total - per * ctas;
+    const int64_t per = total / ctas, more = total - per * ctas;
     pos = per * blockIdx.x + min((int64_t)blockIdx.x, more);
-    end = pos + per + (blockIdx.x < more ? 1 : 0);
+    if (threadIdx.x == 0) plan.per = per, plan.more = more, plan.end = pos + per + (blockIdx.x < more ? 1 : 0);
     return true;
   }
   // The next run; tiles is 0 where it has no keys of its own.
-  __device__ __forceinline__ bool next(const TreeProblem& p) {
+  __device__ __forceinline__ bool next(const TreeProblem& p, const volatile Plan& plan) {
+    const int64_t end = plan.end;
     if (pos >= end) return false;
+    const int64_t lanes = (int64_t)p.cache.heads * p.row_tiles;
     while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after());
     const int which = __popc(__ballot_sync(0xffffffffu, (sq.before + sq.sum) * lanes <= pos));
     seq = sq.first + which;
@@ -124,17 +131,21 @@ struct Runs {
     pos += to - from;
     head = item / p.row_tiles;
     tile = item - head * p.row_tiles;
-    rows = min(kRows, p.nodes * p.group - tile * kRows);
     const int u0 = max(from - kSetupTiles, 0), u1 = to - kSetupTiles;
     k_begin = u0 * BK, k_end = min(u1 * BK, keys);
     tiles = max(u1 - u0, 0);
     return true;
   }
-  __device__ __forceinline__ int holder(int64_t u) const {  // the CTA that has unit u
-    const int64_t large = more * (per + 1);
-    return (int)(u < large ? u / (per + 1) : more + (u - large) / per);
+  __device__ __forceinline__ int rows(const TreeProblem& p) const {
+    return min(kRows, p.nodes * p.group - tile * kRows);
   }
 };
+
+// The CTA that has unit u.
+__device__ __forceinline__ int holder(const volatile Plan& plan, int64_t u) {
+  const int64_t per = plan.per, more = plan.more, large = more * (per + 1);
+  return (int)(u < large ? u / (per + 1) : more + (u - large) / per);
+}
 
 // Operand i of a run of n tiles: K0 K1 V0 K2 V1 ... V(n-2) V(n-1).
 __device__ __forceinline__ void operand(int i, int n, bool& is_v, int& j) {
@@ -233,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
 
   Runs run;
-  if (!run.begin(p)) return;
+  if (!run.begin(p, bar.plan)) return;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(&bar.op_ready[i], 4);
@@ -283,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     // ---- copies ------------------------------------------------------------------
     const int box = min(1 << p.cache.shift, BK), boxes = BK / box, group = 32 / boxes;  // tiles whose pages the lanes hold
     uint32_t issued_stages = 0;
-    for (; run.next(p); ++runs_done) {
+    for (; run.next(p, bar.plan); ++runs_done) {
       const int32_t* page_row = p.pages.pages + run.seq * p.pages.ld;
       const int n = run.tiles;
       auto pages_of = [&](int b) {  // lane l: box l % boxes of tile b group + l / boxes
@@ -353,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     // ---- decode ---------------------------------------------------------------------
     const int row = threadIdx.x % 128;
     const bool is_v = warp >= 12;
-    for (; run.next(p); ++runs_done) {
+    for (; run.next(p, bar.plan); ++runs_done) {
       const int n = run.tiles;
       for (int j = 0; j < n; ++j) {
         const int op = ops_done + (is_v ? v_index(j, n) : k_index(j)), st = op % S::STAGES, slot = op % kSlots;
@@ -459,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     constexpr uint32_t kScores = 1u << 4 | (uint32_t)(BK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
     constexpr uint32_t kOutput = 1u << 4 | 1u << 16 | (uint32_t)(DIM >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
     int live_runs = 0;
-    for (; run.next(p); ++runs_done) {
+    for (; run.next(p, bar.plan); ++runs_done) {
       const int n = __shfl_sync(0xffffffffu, run.tiles, 0);
       if (n == 0) continue;
       bool ok = true;
@@ -503,29 +514,36 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     const uint32_t base = tmem + ((uint32_t)(warp % 4 * 32) << 16);
     const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);  // -infinity times it stays so
     const int e0 = half * (DIM / 2);
-    for (; run.next(p); ++runs_done) {
-      const int n = run.tiles, rows = run.rows;
-      const int gr = run.tile * kRows + row, node = gr / p.group, head = run.head * p.group + gr - node * p.group;
+    for (; run.next(p, bar.plan); ++runs_done) {
+      const int n = run.tiles, rows = run.rows(p);
       const bool real = row < rows;
-      const int live_nodes = node_count(p, run.seq);
-      __half* out16 = static_cast<__half*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
-      float* out32 = static_cast<float*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
-      const int64_t lse_at = ((int64_t)run.seq * p.nodes + node) * p.cache.heads * p.group + head;
+      // Where this row's node and query head stand (found again where they are
+      // needed: between lie the steps, that need the registers).
+      auto place = [&](int& node, int& head) {
+        const int gr = run.tile * kRows + row;
+        node = gr / p.group, head = run.head * p.group + gr - node * p.group;
+      };
       if (run.keys == 0 && run.from == 0 && half == 0 && real) {  // nothing to see: the item's first CTA writes its zeros
+        int node, head;
+        place(node, head);
+        const int64_t at = run.seq * p.o_seq + node * p.o_node + head * p.o_head;
         for (int e = 0; e < DIM; e += 8) {
           if (p.out_f32) {
-            reinterpret_cast<float4*>(out32 + e)[0] = make_float4(0.f, 0.f, 0.f, 0.f);
-            reinterpret_cast<float4*>(out32 + e)[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            reinterpret_cast<float4*>(static_cast<float*>(p.out) + at + e)[0] = make_float4(0.f, 0.f, 0.f, 0.f);
+            reinterpret_cast<float4*>(static_cast<float*>(p.out) + at + e)[1] = make_float4(0.f, 0.f, 0.f, 0.f);
           } else {
-            *reinterpret_cast<uint4*>(out16 + e) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(static_cast<__half*>(p.out) + at + e) = make_uint4(0, 0, 0, 0);
           }
         }
-        if (p.lse != nullptr) p.lse[lse_at] = -kInf;
+        if (p.lse != nullptr) p.lse[((int64_t)run.seq * p.nodes + node) * p.cache.heads * p.group + head] = -kInf;
       }
       if (n == 0) continue;
+      uint64_t bits = 0;
       {
         // q of this run (the products with the one before are done); a negative
         // scale turns its signs.
+        int node, head;
+        place(node, head);
         const __half* q = p.q + run.seq * p.q_seq + node * p.q_node + (int64_t)head * p.q_head;
         const uint32_t sign = p.scale_log2 < 0.f ? 0x80008000u : 0u;
 #pragma unroll 4
@@ -541,14 +559,13 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         fence_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bar.q_ready);
-      }
-      uint64_t bits = 0;
-      if (real) {
-        if (p.mask == nullptr) {
-          bits = (2ull << node) - 1;
-        } else {
-          const uint32_t* w = p.mask + run.seq * p.mask_seq + node * p.words;
-          bits = w[0] | (p.words > 1 ? (uint64_t)w[1] << 32 : 0);
+        if (real) {
+          if (p.mask == nullptr) {
+            bits = (2ull << node) - 1;
+          } else {
+            const uint32_t* w = p.mask + run.seq * p.mask_seq + node * p.words;
+            bits = w[0] | (p.words > 1 ? (uint64_t)w[1] << 32 : 0);
+          }
         }
       }
       const bool warp_real = (warp % 4) * 32 < rows;
@@ -695,8 +712,13 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         if (threadIdx.x == 0) bar.nodes_bad[runs_done % 4][0] = bar.nodes_bad[runs_done % 4][1] = 0;
         const float sum = l + bar.sum[half ^ 1][row];
         const bool whole = run.from <= kSetupTiles && run.to == run.units;
-        int c0 = 0, c1 = 0;
-        if (!whole) c0 = run.holder(run.first + kSetupTiles), c1 = run.holder(run.first + run.units - 1);
+        int c0 = 0, c1 = 0, node, head;
+        if (!whole)
+          c0 = holder(bar.plan, run.first + kSetupTiles), c1 = holder(bar.plan, run.first + run.units - 1);
+        place(node, head);
+        __half* out16 = static_cast<__half*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
+        float* out32 = static_cast<float*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
+        const int live_nodes = node_count(p, run.seq);
         auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * S::PART; };
         float* part = part_of(blockIdx.x);
         const bool live = node < live_nodes;
@@ -758,7 +780,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           if (real && half == 0) {
             if (!whole) part[DIM * kRows + row] = m, part[(DIM + 1) * kRows + row] = sum;
             else if (p.lse != nullptr)
-              p.lse[lse_at] = live && sum != 0.f ? (m - kShift + log2f(sum)) * 0.69314718056f : -kInf;
+              p.lse[((int64_t)run.seq * p.nodes + node) * p.cache.heads * p.group + head] = live && sum != 0.f ? (m - kShift + log2f(sum)) * 0.69314718056f : -kInf;
           }
         }
         if (!whole && threadIdx.x == 0) bar.part[bar.parts++] = {c0, c1, run.seq, run.head, run.tile, rows};
