@@ -90,26 +90,32 @@ def _stream_handle(stream) -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+_F16, _F32, _I32 = torch.float16, torch.float32, torch.int32
+_KINDS_OF = {_F16: AF1_F16, _F32: AF1_F32}
+
+
 def _dtype(t: torch.Tensor, what: str) -> int:
-    if t.dtype == torch.float16:
-        return AF1_F16
-    if t.dtype == torch.float32:
-        return AF1_F32
-    raise ValueError(f"{what} must be float16 or float32")
+    kind = _KINDS_OF.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{what} must be float16 or float32")
+    return kind
 
 
 def _steps(t: torch.Tensor, what: str, dims: int):
-    """Strides of all axes but the last, 0 for axes of one entry."""
-    if t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+    """Strides of all axes; the last one is 1. Axes of one entry have stride 0."""
+    s = t.stride()
+    if len(s) != dims or (s[-1] != 1 and t.shape[-1] > 1):
         raise ValueError(f"{what} must be {dims}-D with unit stride along its last axis")
-    return [s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape)]
+    if 1 in t.shape:
+        s = tuple(a if n > 1 else 0 for a, n in zip(s, t.shape))
+    return s
 
 
 def _index(t, what: str, shape) -> int:
     """Pointer of a contiguous int32 tensor of this shape, 0 for None."""
     if t is None:
         return 0
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not _I32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous int32 tensor of shape {tuple(shape)}")
     return t.data_ptr()
 
@@ -122,10 +128,11 @@ def _empty(shape, dtype, device, stream) -> torch.Tensor:
 
 
 def _pages(t: torch.Tensor):
-    if t.dtype != torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    s = t.stride()
+    if t.dtype is not _I32 or len(s) != 2 or (s[1] != 1 and t.shape[1] > 1):
         raise ValueError("pages must be a 2-D int32 tensor with contiguous rows")
     rows, columns = t.shape
-    return t.data_ptr(), rows, columns, t.stride(0) if rows > 1 else columns
+    return t.data_ptr(), rows, columns, s[0] if rows > 1 else columns
 
 
 # -- rotary positions ----------------------------------------------------------------
@@ -159,9 +166,10 @@ def rope_table(length: int, dim: int, base: float = 10000.0, scaling=None, facto
 
 
 def _table(t: torch.Tensor):
-    if t.dtype != torch.float32 or t.dim() != 3 or t.shape[2] != 2 or not t.is_contiguous():
+    shape = t.shape
+    if t.dtype is not _F32 or len(shape) != 3 or shape[2] != 2 or not t.is_contiguous():
         raise ValueError("the rotary table must be a contiguous float32 tensor (length, pairs, 2)")
-    return t.data_ptr(), t.shape[0], 2 * t.shape[1]
+    return t.data_ptr(), shape[0], 2 * shape[1]
 
 
 def rope(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, out: torch.Tensor | None = None,
@@ -181,7 +189,7 @@ def rope(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, out: tor
     if heads == 0 or tokens == 0:
         return out
     a = _RopeArgs(x.data_ptr(), out.data_ptr(), _index(positions, "positions", (tokens,)), tp, tokens, heads, dim,
-                  rope_dim, length, *xs, *ys, dt, (_INTERLEAVED if interleaved else 0) | (_BACKWARD if backward else 0))
+                  rope_dim, length, xs[0], xs[1], ys[0], ys[1], dt, (_INTERLEAVED if interleaved else 0) | (_BACKWARD if backward else 0))
     _check(_rope(ctypes.byref(a), _stream_handle(stream)))
     return out
 
@@ -263,7 +271,7 @@ class KVCache:
         for t in (k_out, v_out):
             if t is not None and (t.shape != shape or t.dtype != torch.float16 or not t.is_contiguous()):
                 raise ValueError(f"k_out and v_out must be contiguous float16 tensors of shape {shape}")
-        heads, qs, qos = 0, (0, 0), (0, 0)
+        heads, qs, qos = 0, (0, 0, 1), (0, 0, 1)
         if q is not None:
             qs, heads = _steps(q, "q", 3), q.shape[1]
             if q.shape != (tokens, heads, self.head_dim) or q.dtype != k.dtype:
@@ -281,10 +289,11 @@ class KVCache:
             raise ValueError("q has no heads")
         tp, length, rope_dim = _table(rope) if rope is not None else (0, 0, 0)
         one = (tokens,)
-        a = _AppendArgs(k.data_ptr(), v.data_ptr(), *ks, *vs, _index(seq, "seq", one), _index(slot, "slot", one),
-                        _index(positions, "positions", one), *_append_pages(pages, tokens), tp, length, rope_dim,
-                        _ptr(q), _ptr(q_out), heads, *qs, *qos, _ptr(k_out), _ptr(v_out), dt,
-                        _INTERLEAVED if interleaved else 0)
+        pp, sequences, columns, ld = _pages(pages)
+        a = _AppendArgs(k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], _index(seq, "seq", one),
+                        _index(slot, "slot", one), _index(positions, "positions", one), pp, tokens, sequences,
+                        columns, ld, tp, length, rope_dim, _ptr(q), _ptr(q_out), heads, qs[0], qs[1], qos[0],
+                        qos[1], _ptr(k_out), _ptr(v_out), dt, _INTERLEAVED if interleaved else 0)
         _check(_kv_append(self._h, ctypes.byref(a), _stream_handle(stream)))
         return q_out
 
@@ -366,7 +375,7 @@ class KVCache:
             else:
                 with torch.cuda.stream(stream):
                     workspace = self.make_workspace(q)
-        a = _TreeArgs(q.data_ptr(), *qs, out.data_ptr(), *os, _ptr(lse), pp, _index(lens, "lens", (sequences,)),
+        a = _TreeArgs(q.data_ptr(), qs[0], qs[1], qs[2], out.data_ptr(), os[0], os[1], os[2], _ptr(lse), pp, _index(lens, "lens", (sequences,)),
                       _index(counts, "counts", (sequences,)), mp, mask_seq, sequences, nodes, heads, columns, ld,
                       1.0 / math.sqrt(dim) if scale is None else scale, _dtype(out, "out"))
         _check(_tree_attention(self._h, ctypes.byref(a), workspace.data_ptr(),
@@ -383,11 +392,6 @@ class KVCache:
             self.free()
         except Exception:
             pass
-
-
-def _append_pages(pages: torch.Tensor, tokens: int):
-    pp, sequences, columns, ld = _pages(pages)
-    return pp, tokens, sequences, columns, ld
 
 
 def tree_mask(parents: torch.Tensor, stream=None) -> torch.Tensor:
@@ -412,23 +416,22 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top
     or, with `top`, (logprobs, entropy, top_logprobs, top_ids)
     (af1_token_logprobs). tokens: int32 (rows, given), or None (logprobs is
     then (rows, 0))."""
-    (ld,) = _steps(logits, "logits", 2)
+    ld = _steps(logits, "logits", 2)[0]
     dt = _dtype(logits, "logits")
     rows, vocab = logits.shape
     if tokens is not None and (tokens.dim() != 2 or tokens.shape[0] != rows):
         raise ValueError("tokens must be (rows, given)")
     given = 0 if tokens is None else tokens.shape[1]
     device = logits.device
-    # One allocation holds the float32 outputs.
-    n = rows * given
-    flat = _empty((n + rows + rows * top,), torch.float32, device, stream)
-    logprobs, entropy = flat[:n].view(rows, given), flat[n: n + rows]
-    top_logprobs = flat[n + rows:].view(rows, top)
-    ids = _empty((rows, top), torch.int32, device, stream) if top else None
+    logprobs = _empty((rows, given), _F32, device, stream)
+    entropy = _empty((rows,), _F32, device, stream)
+    best = ids = None
+    if top:
+        best, ids = _empty((rows, top), _F32, device, stream), _empty((rows, top), _I32, device, stream)
     if rows > 0:
         a = _LogprobArgs(logits.data_ptr(), rows, vocab, ld if rows > 1 else vocab,
                          _index(tokens, "tokens", (rows, given)) if given else 0, given,
-                         logprobs.data_ptr() if given else 0, entropy.data_ptr(),
-                         top_logprobs.data_ptr() if top else 0, _ptr(ids), top, dt, temperature, 0)
+                         logprobs.data_ptr() if given else 0, entropy.data_ptr(), _ptr(best), _ptr(ids), top, dt,
+                         temperature, 0)
         _check(_token_logprobs(ctypes.byref(a), _stream_handle(stream)))
-    return (logprobs, entropy, top_logprobs, ids) if top else (logprobs, entropy)
+    return (logprobs, entropy, best, ids) if top else (logprobs, entropy)

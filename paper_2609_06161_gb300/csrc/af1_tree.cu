@@ -735,8 +735,13 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
 int fail(int code, const std::string& msg) { return set_error(code, "af1_tree_attention: " + msg); }
 
 // Blocks of 8 rows (of every query head and node that share a cached head) of
-// a CTA; 0: the tensor-core kernel.
-int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 0; }
+// a CTA; 0: the tensor-core kernel, whose products have 128 rows. Up to 32
+// rows it pays to go over the keys again for the second 16: 4 sequences of up
+// to 6001 tokens with 20 rows of E4M3 take 31 us here and 42 there, 32 rows of
+// INT8 33 and 38; 64 rows of E4M3 46 and 42, 256 rows of INT8 over 8000 tokens
+// 64 and 46. (Blocks of 32 rows, which leave an SM 8 warps, took 36, 41 and 56
+// for the first three.)
+int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 32 ? 2 : 0; }
 
 int64_t workspace_bytes(const af1_kv_cache& c, int64_t rows) {
   if (row_blocks(rows) == 0) return kPartOffset + tree_wide_part_bytes(c);

@@ -261,7 +261,7 @@ struct Sequences {
   __device__ __forceinline__ int64_t after() const { return before + __shfl_sync(0xffffffffu, sum, 31); }
 };
 
-// The tensor-core kernel for more than 16 rows to a cached head
+// The tensor-core kernel for more than 32 rows to a cached head
 // (af1_tree_wide.cu): its workspace bytes, and its launch.
 int64_t tree_wide_part_bytes(const af1_kv_cache& c);
 cudaError_t launch_tree_wide(TreeProblem& p, const af1_kv_cache& c, int rows, cudaStream_t st);

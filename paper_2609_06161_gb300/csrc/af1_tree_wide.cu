@@ -1,5 +1,5 @@
 // af1_tree_wide.cu — attention of drafted tokens over the paged cache where
-// more than 16 rows (nodes times query heads) share a cached head: the same
+// more than 32 rows (nodes times query heads) share a cached head: the same
 // operator as af1_tree.cu, with tcgen05 products of 128 rows.
 //
 // An item is one sequence, one cached head and a block of 128 rows; its keys
