@@ -106,8 +106,9 @@ def _steps(t: torch.Tensor, what: str, dims: int):
     s = t.stride()
     if len(s) != dims or (s[-1] != 1 and t.shape[-1] > 1):
         raise ValueError(f"{what} must be {dims}-D with unit stride along its last axis")
-    if 1 in t.shape:
-        s = tuple(a if n > 1 else 0 for a, n in zip(s, t.shape))
+    n = t.shape
+    if 1 in n:
+        return [0 if n[i] == 1 else s[i] for i in range(dims)]
     return s
 
 

@@ -761,11 +761,12 @@ int af1_kv_create(const af1_kv_desc* d, af1_kv_cache** out) {
   c->device = dev;
   c->num_sms = sms;
   const int row_bytes = kv_row_bytes(d->kind, d->head_dim);
-  bool ok = make_row_map(&c->k16, d->k, rows, row_bytes, 16) && make_row_map(&c->v16, d->v, rows, row_bytes, 16);
-  if (d->page_size >= 32)
-    ok = ok && make_row_map(&c->k32, d->k, rows, row_bytes, 32) && make_row_map(&c->v32, d->v, rows, row_bytes, 32);
-  const int most = std::min(d->page_size, 128);
-  ok = ok && make_row_map(&c->k128, d->k, rows, row_bytes, most) && make_row_map(&c->v128, d->v, rows, row_bytes, most);
+  // Boxes of a warp's step (16 rows for rows of 256 bytes), and of a tile.
+  const int step = std::min(d->page_size, row_bytes >= 256 ? 16 : 32), tile = std::min(d->page_size, 128);
+  bool ok = make_row_map(&c->k_step, d->k, rows, row_bytes, step) && make_row_map(&c->v_step, d->v, rows, row_bytes, step);
+  c->k_tile = c->k_step, c->v_tile = c->v_step;
+  if (tile != step)
+    ok = ok && make_row_map(&c->k_tile, d->k, rows, row_bytes, tile) && make_row_map(&c->v_tile, d->v, rows, row_bytes, tile);
   if (!ok) {
     delete c;
     return fail(AF1_ERR_CUDA, who, "cuTensorMapEncodeTiled failed");

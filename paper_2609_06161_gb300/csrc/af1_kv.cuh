@@ -15,9 +15,9 @@ struct af1_kv_cache {
   af1_kv_desc d;
   int device = 0;
   int num_sms = 0;
-  // Tensor maps of k and v as rows of codes: boxes of 16 rows, of 32 where a
-  // page holds as many, and of a page's rows up to 128.
-  CUtensorMap k16, v16, k32, v32, k128, v128;
+  // Tensor maps of k and v as rows of codes, in boxes of a page's rows up to
+  // those of a warp's step (af1_tree.cu), and of a tile (af1_tree_wide.cu).
+  CUtensorMap k_step, v_step, k_tile, v_tile;
 };
 
 namespace af1 {

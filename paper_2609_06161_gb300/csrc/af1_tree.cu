@@ -10,9 +10,9 @@
 // Split. An item is one sequence, one cached head and one block of 8 NT rows;
 // its keys are cut into units of kUnit, and every CTA takes an equal run of
 // the units of all items (ragged lengths balance by themselves; each item
-// counts kSetup units more, for what a run costs whatever its length: with
-// short items uncounted, the CTA that had eight of them ran 102 us where the
-// others ran 70). Inside a CTA each warp takes every W-th step of KW keys of a run, with a ring of its
+// counts some units more, for what a run costs whatever its length: without
+// them the CTA that had eight short items ran 102 us where the others ran 70).
+// Inside a CTA each warp takes every W-th step of KW keys of a run, with a ring of its
 // own in shared memory that TMA fills, its own running maximum m and sum l,
 // and an accumulator in registers; warps meet once a run, to join (m, l, o).
 // Where an item spans CTAs, each leaves its part in the workspace and the
@@ -48,7 +48,7 @@ namespace {
 
 constexpr int kUnit = 64;                         // keys of a unit
 constexpr int kMinRun = 256;                      // keys of a CTA, at least (where there are so many)
-constexpr int kSetup = 4;                         // units that a run's beginning and end are worth
+constexpr int kSetup = 12;                        // units that a run's beginning and end are worth, at most
 constexpr float kCode = 16777216.f;               // 2^24: codes as subnormals
 
 template <int KIND, int DIM, int NT, int W, int KW, int STAGES>
@@ -94,15 +94,9 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
 
   // This CTA's units: begin .. end - 1 of all items'.
   const int64_t lanes = (int64_t)p.cache.heads * p.row_tiles;
-  Sequences<kUnit, kSetup> sq;
-  sq.load(p, 0, 0);
-  int64_t total = sq.after();
-  for (int at = 32; at < p.pages.seqs; at += 32) {
-    sq.load(p, at, total);
-    total = sq.after();
-  }
-  if (p.pages.seqs > 32) sq.load(p, 0, 0);
-  total *= lanes;
+  Sequences<kUnit> sq;
+  int setup;
+  const int64_t total = sq.begin(p, lanes, kSetup / 3, kSetup, setup);
   int64_t ctas = min((int64_t)gridDim.x, (total * kUnit + kMinRun - 1) / kMinRun);
   ctas = min(ctas, total);  // each has a unit at least
   if (blockIdx.x >= ctas) return;
@@ -114,7 +108,7 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
   uint32_t phases = 0;   // of the warp's barriers
   bool alive = true;     // no wait has given up
   for (int64_t pos = begin; pos < end;) {
-    while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after());
+    while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after(), setup);
     const int which = __popc(__ballot_sync(0xffffffffu, (sq.before + sq.sum) * lanes <= pos));
     const int seq = sq.first + which;
     const int units = __shfl_sync(0xffffffffu, sq.units, which);
@@ -123,7 +117,7 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
     const int item = (int)((pos - seq_first) / units);
     const int64_t first = seq_first + (int64_t)item * units;  // the item's first unit
     const int from = (int)(pos - first), to = (int)min((int64_t)units, from + (end - pos));
-    const int u0 = max(from - kSetup, 0), u1 = to - kSetup;  // units of keys
+    const int u0 = max(from - setup, 0), u1 = to - setup;  // units of keys
     pos += to - from;
     const int head = item / p.row_tiles, tile = item - head * p.row_tiles;
     const int rows = min(ROWS, p.nodes * p.group - tile * ROWS);
@@ -643,7 +637,7 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
       return (int)(u < large ? u / (per + 1) : more + (u - large) / per);
     };
     int c0 = 0, c1 = 0;
-    if (!whole) c0 = holder(first + kSetup), c1 = holder(first + units - 1);
+    if (!whole) c0 = holder(first + setup), c1 = holder(first + units - 1);
     auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * S::PART; };
     float* part = part_of(blockIdx.x);
     const int live_nodes = node_count(p, seq);
@@ -774,9 +768,7 @@ int launch_rows(TreeProblem& p, const af1_kv_cache& c, cudaStream_t st) {
   constexpr int FIT = (222 * 1024 / CTAS - 4096) / BYTES;
   constexpr int STAGES = FIT > 4 ? 4 : FIT;
   static_assert(STAGES >= 2, "");
-  const int box = std::min(c.d.page_size, KW);
-  p.k_map = box == 16 ? c.k16 : c.k32;
-  p.v_map = box == 16 ? c.v16 : c.v32;
+  p.k_map = c.k_step, p.v_map = c.v_step;
   return launch<KIND, DIM, NT, W, KW, STAGES, CTAS>(p, c.num_sms, st);
 }
 

@@ -47,7 +47,7 @@ namespace {
 
 constexpr int BK = 128;        // keys of a tile
 constexpr int kThreads = 608;
-constexpr int kSetupTiles = 2; // tiles that a run's beginning and end are worth
+constexpr int kSetupTiles = 4; // tiles that a run's beginning and end are worth, at most
 constexpr int kRows = 128;
 constexpr int kOutAt = 2 * BK, kWeightsAt = 3 * BK;  // columns of tensor memory, behind two tiles of scores
 constexpr int kSlots = 4;
@@ -91,20 +91,14 @@ struct Barriers {
 // The runs of this CTA, one after another, known to every warp. What stays the
 // same lies in shared memory: every thread of the softmax needs its registers.
 struct Runs {
-  Sequences<BK, kSetupTiles> sq;
+  Sequences<BK> sq;
+  int setup;
   int64_t pos, first;
   int seq, head, tile, len, keys, units, from, to, k_begin, k_end, tiles;
 
   __device__ __forceinline__ bool begin(const TreeProblem& p, Plan& plan) {
     const int64_t lanes = (int64_t)p.cache.heads * p.row_tiles;
-    sq.load(p, 0, 0);
-    int64_t total = sq.after();
-    for (int at = 32; at < p.pages.seqs; at += 32) {
-      sq.load(p, at, total);
-      total = sq.after();
-    }
-    if (p.pages.seqs > 32) sq.load(p, 0, 0);
-    total *= lanes;
+    const int64_t total = sq.begin(p, lanes, kSetupTiles / 2, kSetupTiles, setup);
     const int64_t ctas = min((int64_t)gridDim.x, total);
     if (blockIdx.x >= ctas) return false;
     const int64_t per = total / ctas, more = total - per * ctas;
@@ -117,7 +111,7 @@ struct Runs {
     const int64_t end = plan.end;
     if (pos >= end) return false;
     const int64_t lanes = (int64_t)p.cache.heads * p.row_tiles;
-    while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after());
+    while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after(), setup);
     const int which = __popc(__ballot_sync(0xffffffffu, (sq.before + sq.sum) * lanes <= pos));
     seq = sq.first + which;
     units = __shfl_sync(0xffffffffu, sq.units, which);
@@ -131,7 +125,7 @@ struct Runs {
     pos += to - from;
     head = item / p.row_tiles;
     tile = item - head * p.row_tiles;
-    const int u0 = max(from - kSetupTiles, 0), u1 = to - kSetupTiles;
+    const int u0 = max(from - setup, 0), u1 = to - setup;
     k_begin = u0 * BK, k_end = min(u1 * BK, keys);
     tiles = max(u1 - u0, 0);
     return true;
@@ -711,10 +705,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         named_sync(2, 256);
         if (threadIdx.x == 0) bar.nodes_bad[runs_done % 4][0] = bar.nodes_bad[runs_done % 4][1] = 0;
         const float sum = l + bar.sum[half ^ 1][row];
-        const bool whole = run.from <= kSetupTiles && run.to == run.units;
+        const bool whole = run.from <= run.setup && run.to == run.units;
         int c0 = 0, c1 = 0, node, head;
         if (!whole)
-          c0 = holder(bar.plan, run.first + kSetupTiles), c1 = holder(bar.plan, run.first + run.units - 1);
+          c0 = holder(bar.plan, run.first + run.setup), c1 = holder(bar.plan, run.first + run.units - 1);
         place(node, head);
         __half* out16 = static_cast<__half*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
         float* out32 = static_cast<float*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
@@ -897,7 +891,7 @@ int64_t tree_wide_part_bytes(const af1_kv_cache& c) {
 
 cudaError_t launch_tree_wide(TreeProblem& p, const af1_kv_cache& c, int rows, cudaStream_t st) {
   p.row_tiles = (rows + kRows - 1) / kRows;
-  p.k_map = c.k128, p.v_map = c.v128;
+  p.k_map = c.k_tile, p.v_map = c.v_tile;
   switch (c.d.kind) {
     case AF1_KV_F16: return launch_kind<AF1_KV_F16>(p, c, st);
     case AF1_KV_INT8: return launch_kind<AF1_KV_INT8>(p, c, st);
