@@ -14,10 +14,9 @@
 // 64 over 32768 INT4 tokens.)
 // Roles of the 19 warps:
 //   0-3, 4-7  softmax of the tile's first and second 64 keys: a thread has one
-//             row. The scores are read twice (maximum, weights): held between
-//             the passes they would need 64 registers more. The maximum of
-//             both halves moves, and O with it, only when a score passes it by
-//             2^kSlack;
+//             row. The weights are formed relative to the maximum so far, and
+//             formed again (after O is scaled) only where a score of either
+//             half passes it by more than kSlack binary places;
 //   8-11, 12-15  decode keys, and values: thread i turns vector i of a tile
 //             from codes into FP16 in the 128-byte-swizzled operand tile (keys K-major, values
 //             with their entries along N). INT8 and E4M3 stay codes, exact in
@@ -149,6 +148,17 @@ __device__ __forceinline__ void operand(int i, int n, bool& is_v, int& j) {
 __device__ __forceinline__ int k_index(int j) { return j == 0 ? 0 : 2 * j - 1; }
 __device__ __forceinline__ int v_index(int j, int n) { return j == n - 1 ? 2 * n - 1 : 2 * j + 2; }
 
+// Suspends the thread for up to 20 us (a hint): a poll that came back at once
+// would take the schedulers' slots from the warps that work.
+__device__ __forceinline__ bool try_wait_long(uint64_t* bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(done)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return done != 0;
+}
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -271,9 +281,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
 
   // Bounded wait; once one has given up, all return at once.
   auto wait = [&](uint64_t* b, uint32_t parity) {
-    if (mbar_try_wait(b, parity)) return true;
+    if (try_wait_long(b, parity)) return true;
     const long long t0 = clock64();
-    while (!mbar_try_wait(b, parity)) {
+    while (!try_wait_long(b, parity)) {
       if (bar.gave_up) return false;
       if (clock64() - t0 > p.wait_cycles) {
         bar.gave_up = 1;
@@ -387,17 +397,24 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 if (lane == 0) bar.value_top[at][warp % 4] = fmaxf((float)((int)(most >> 23) - 126), kLeastScale);
               }
             }
-            // A loop, not unrolled, with the next chunk read ahead: the roles of a
-            // scheduler share its instruction cache.
-            uint4 x = *reinterpret_cast<const uint4*>(from + C::template at<BK>(row, 0));
-            uint32_t group = INT4 ? reinterpret_cast<const uint32_t*>(sc)[row * C::GROUPS] : 0;
-#pragma unroll 1
+            // Keys and values share this code: the roles of a scheduler share its
+            // instruction cache. All of the row is read before the first store:
+            // loads are not moved over stores.
+            uint4 in[C::RB / 16];
+            uint32_t group[4];
+#pragma unroll
+            for (int c = 0; c < C::RB / 16; ++c) in[c] = *reinterpret_cast<const uint4*>(from + C::template at<BK>(row, c));
+            if constexpr (INT4) {
+#pragma unroll
+              for (int c = 0; c < C::GROUPS; ++c)
+                group[c] = reinterpret_cast<const uint32_t*>(sc)[row * C::GROUPS + c];
+            }
+            const uint32_t swizzle = (uint32_t)(row & 7) << 4;
+#pragma unroll
             for (int c = 0; c < C::RB / 16; ++c) {
-              const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-              const uint32_t scale2 = prmt(group, group, 0x1010), low2 = prmt(group, group, 0x3232);
-              const int ahead = c + 1 < C::RB / 16 ? c + 1 : c;
-              x = *reinterpret_cast<const uint4*>(from + C::template at<BK>(row, ahead));
-              if constexpr (INT4) group = reinterpret_cast<const uint32_t*>(sc)[row * C::GROUPS + ahead];
+              const uint32_t w[4] = {in[c].x, in[c].y, in[c].z, in[c].w};
+              uint32_t scale2 = 0, low2 = 0;
+              if constexpr (INT4) scale2 = prmt(group[c], group[c], 0x1010), low2 = prmt(group[c], group[c], 0x3232);
               constexpr int OUT = INT4 ? 4 : 2;  // 16-byte pieces of FP16
 #pragma unroll
               for (int q = 0; q < OUT; ++q) {
@@ -418,7 +435,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                       h[e] = e4m3x2(e % 2 ? u >> 16 : u);
                   }
                 }
-                *reinterpret_cast<uint4*>(place(c * OUT + q)) = make_uint4(h[0], h[1], h[2], h[3]);
+                const int piece = c * OUT + q;
+                *reinterpret_cast<uint4*>(to + (piece >> 3) * (BK * 128) + (((piece & 7) << 4) ^ swizzle)) =
+                    make_uint4(h[0], h[1], h[2], h[3]);
               }
             }
           }
@@ -594,10 +613,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           for (int i = 0; i < 32; ++i)
             if (!(sees >> i & 1)) x[i] = -kInf;
         };
-        auto factors = [&](int at) {  // of four columns' products
-          return C::SCALED8 ? *reinterpret_cast<const float4*>(ks + at) : make_float4(scale, scale, scale, scale);
-        };
-        if (work) {
+        // The half's weights relative to `ref`, and its largest score.
+        float2 sum;
+        auto pass = [&](float ref) {
+          sum = make_float2(0.f, 0.f);
 #pragma unroll 1
           for (int c = 0; c < BK / 2; c += 32) {
             float x[32];
@@ -605,7 +624,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             if constexpr (C::SCALED8) {
 #pragma unroll
               for (int i = 0; i < 32; i += 4) {
-                const float4 f = factors(c + i);
+                const float4 f = *reinterpret_cast<const float4*>(ks + c + i);
                 const float2 a = mul2(make_float2(x[i], x[i + 1]), make_float2(f.x, f.y));
                 const float2 b = mul2(make_float2(x[i + 2], x[i + 3]), make_float2(f.z, f.w));
                 x[i] = a.x, x[i + 1] = a.y, x[i + 2] = b.x, x[i + 3] = b.y;
@@ -616,10 +635,38 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
 #pragma unroll
             for (int i = 2; i < 30; i += 4) t0 = max3(t0, x[i], x[i + 1]), t1 = max3(t1, x[i + 2], x[i + 3]);
             top = max3(top, max3(t0, x[30], x[31]), t1);
+            uint32_t r[16];
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              float2 a = make_float2(x[i], x[i + 1]), b = make_float2(x[i + 2], x[i + 3]);
+              const float2 minus = make_float2(-ref, -ref);
+              if constexpr (C::SCALED8) a = add2(a, minus), b = add2(b, minus);
+              else a = fma2(a, make_float2(scale, scale), minus), b = fma2(b, make_float2(scale, scale), minus);
+              a = make_float2(ex2(a.x), ex2(a.y)), b = make_float2(ex2(b.x), ex2(b.y));
+              sum = add2(sum, add2(a, b));
+              if constexpr (C::SCALED8) {
+                const float4 f = *reinterpret_cast<const float4*>(vs + c + i);
+                const float2 wa = mul2(a, make_float2(f.x, f.y)), wb = mul2(b, make_float2(f.z, f.w));
+                if (masked) {  // 0 times any scale is 0
+                  a.x = a.x == 0.f ? 0.f : wa.x, a.y = a.y == 0.f ? 0.f : wa.y;
+                  b.x = b.x == 0.f ? 0.f : wb.x, b.y = b.y == 0.f ? 0.f : wb.y;
+                } else {
+                  a = wa, b = wb;
+                }
+              }
+              r[i / 2] = pack_half2(a.x, a.y), r[i / 2 + 1] = pack_half2(b.x, b.y);
+            }
+            tmem_store16(base + kWeightsAt + buf * (BK / 2) + (c_first + c) / 2, r);
           }
+          tmem_wait_store();
+        };
+        // The weights relative to the maximum so far, which mostly holds; where a
+        // row's has to move (both halves agree on that), they are formed again.
+        auto reference = [&] { return (m == -kInf ? 0.f : m) + ev - kShift; };
+        if (work) {
+          pass(reference());
           if constexpr (!C::SCALED8) top *= scale;
         }
-        // Both halves' maximum.
         bar.top[buf][half][row] = top;
         named_sync(2, 256);
         top = fmaxf(top, bar.top[buf][half ^ 1][row]);
@@ -651,42 +698,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 }
               }
             }
+            pass(reference());
           }
-          const float ref = (m == -kInf ? 0.f : m) + ev - kShift;
-#pragma unroll 1
-          for (int c = 0; c < BK / 2; c += 32) {
-            float x[32];
-            tmem_load(scores + c, x);
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-              const float4 f = factors(c + i);
-              const float2 a = fma2(make_float2(x[i], x[i + 1]), make_float2(f.x, f.y), make_float2(-ref, -ref));
-              const float2 b = fma2(make_float2(x[i + 2], x[i + 3]), make_float2(f.z, f.w), make_float2(-ref, -ref));
-              x[i] = a.x, x[i + 1] = a.y, x[i + 2] = b.x, x[i + 3] = b.y;
-            }
-            if (masked) hide(c, x);
-            uint32_t r[16];
-            float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-              float2 a = make_float2(ex2(x[i]), ex2(x[i + 1])), b = make_float2(ex2(x[i + 2]), ex2(x[i + 3]));
-              sum = add2(sum, add2(a, b));
-              if constexpr (C::SCALED8) {
-                const float4 f = *reinterpret_cast<const float4*>(vs + c + i);
-                const float2 wa = mul2(a, make_float2(f.x, f.y)), wb = mul2(b, make_float2(f.z, f.w));
-                if (masked) {  // 0 times any scale is 0
-                  a.x = a.x == 0.f ? 0.f : wa.x, a.y = a.y == 0.f ? 0.f : wa.y;
-                  b.x = b.x == 0.f ? 0.f : wb.x, b.y = b.y == 0.f ? 0.f : wb.y;
-                } else {
-                  a = wa, b = wb;
-                }
-              }
-              r[i / 2] = pack_half2(a.x, a.y), r[i / 2 + 1] = pack_half2(b.x, b.y);
-            }
-            l += sum.x + sum.y;
-            tmem_store16(base + kWeightsAt + buf * (BK / 2) + (c_first + c) / 2, r);
-          }
-          tmem_wait_store();
+          l += sum.x + sum.y;
         }
         fence_before();
         __syncwarp();
