@@ -12,7 +12,7 @@
 // exponents of another. (Two streams of tiles, each with scores, weights and
 // output of its own, waited for one another's latencies: 115 us for trees of
 // 64 over 32768 INT4 tokens.)
-// Roles of the 19 warps:
+// Roles of the 20 warps:
 //   0-3, 4-7  softmax of the tile's first and second 64 keys: a thread has one
 //             row. The weights are formed relative to the maximum so far, and
 //             formed again (after O is scaled) only where a score of either
@@ -26,10 +26,13 @@
 //             of 32 entries, is rounded once to FP16, keys too: a score is off
 //             by about 2^-12 sqrt(sum (q k)^2). FP16 tiles arrive by TMA and
 //             are only looked at where a sequence ends;
-//   16        TMA copies, one for up to 128 rows of a page, into the ring of codes;
+//   16, 19    TMA copies of keys, and of values, one for up to 128 rows of a
+//             page, into the ring of codes (one warp for both took 0.65 us for
+//             each, which held up the decoders);
 //   17, 18    one lane each issues Q K^T, and P V.
-// Operand tiles pass through four slots in the order K0 K1 V0 K2 V1 K3 ..., in
-// which the products use them.
+// Keys and values each have a ring of codes and two operand tiles, with
+// barriers of their own: whoever waits on a barrier meets each of its phases in
+// turn, as a test of a phase's parity needs.
 //
 // Infinities and NaN: the values of slots past the end are zeros, a node's
 // value that is not finite is left out of the product (0 times it would reach
@@ -45,12 +48,12 @@ namespace af1 {
 namespace {
 
 constexpr int BK = 128;        // keys of a tile
-constexpr int kThreads = 608;
+constexpr int kThreads = 640;
 constexpr int kSetupTiles = 4; // tiles that a run's beginning and end are worth, at most
 constexpr int kRows = 128;
 constexpr int kOutAt = 2 * BK, kWeightsAt = 3 * BK;  // columns of tensor memory, behind two tiles of scores
-constexpr int kSlots = 4;
-constexpr int kNotes = 8;      // tiles whose scales and page bits are kept: the decoders run ahead
+constexpr int kSlots = 2;      // operand tiles of keys, and of values
+constexpr int kNotes = 4;      // tiles whose scales and page bits are kept: keys are decoded up to three tiles ahead
 constexpr float kLeastScale = -60.f;  // of a value's scale's exponent: smaller ones count as 2^-60
 
 template <int KIND, int DIM>
@@ -60,8 +63,12 @@ struct Wide {
   static constexpr int OP = BK * DIM * 2;                    // bytes of an operand tile
   static constexpr int CODES = BK * C::RB;
   static constexpr int SCALES = (C::SCALED8 ? 2 : 1) * BK * C::SB;  // 8 bits: of keys and values, with the keys
-  static constexpr int STAGES = F16 ? kSlots : C::RB >= 128 ? 3 : 4;  // ring of codes (FP16: the slots themselves)
-  static constexpr int SMEM = (kSlots + 1) * OP + (F16 ? 0 : STAGES * (CODES + SCALES)) + 2 * kNotes * BK * 4 + 1024;
+  // Rings of codes (FP16: the operand tiles themselves). Decoders hold a stage
+  // only while they read it; 8-bit values of 128 entries have room for one.
+  static constexpr int K_STAGES = 2, V_STAGES = C::SCALED8 && DIM == 128 ? 1 : 2;
+  static constexpr int K_BYTES = CODES + SCALES, V_BYTES = CODES + (C::SCALED8 ? 0 : SCALES);
+  static constexpr int RINGS = F16 ? 0 : K_STAGES * K_BYTES + V_STAGES * V_BYTES;
+  static constexpr int SMEM = (2 * kSlots + 1) * OP + RINGS + 2 * kNotes * BK * 4 + 1024;
   static constexpr int PART = kRows * (DIM + 2);  // floats: o, m, l, each along the rows
 };
 
@@ -71,11 +78,11 @@ struct Plan {
 
 struct Barriers {
   Plan plan;
-  uint64_t op_ready[kSlots], op_empty[kSlots], code_full[kSlots], code_empty[kSlots];
+  uint64_t op_ready[2][2], op_empty[2][2], code_full[2][2], code_empty[2][2];  // of keys and values
   uint64_t s_full[2], p_ready[2], pv_done[2], q_ready;  // by tile
   uint32_t tmem;
   volatile int gave_up;
-  uint32_t code_bad[kSlots], tile_bad[kNotes];   // bits: 16 keys each whose page is missing
+  uint32_t code_bad[2][2], tile_bad[kNotes];   // bits: 16 keys each whose page is missing
   uint32_t nodes_bad[4][2];                 // by run: nodes whose value is not finite
   float top[2][2][kRows], sum[2][kRows];    // of the halves of a tile (by tile), and of a run
   float value_top[kNotes][4];                    // by tile and warp: power of two above the values' scales
@@ -139,14 +146,6 @@ __device__ __forceinline__ int holder(const volatile Plan& plan, int64_t u) {
   const int64_t per = plan.per, more = plan.more, large = more * (per + 1);
   return (int)(u < large ? u / (per + 1) : more + (u - large) / per);
 }
-
-// Operand i of a run of n tiles: K0 K1 V0 K2 V1 ... V(n-2) V(n-1).
-__device__ __forceinline__ void operand(int i, int n, bool& is_v, int& j) {
-  is_v = i == 2 * n - 1 || (i >= 2 && i % 2 == 0);
-  j = i == 2 * n - 1 ? n - 1 : i == 0 ? 0 : is_v ? (i - 2) / 2 : (i + 1) / 2;
-}
-__device__ __forceinline__ int k_index(int j) { return j == 0 ? 0 : 2 * j - 1; }
-__device__ __forceinline__ int v_index(int j, int n) { return j == n - 1 ? 2 * n - 1 : 2 * j + 2; }
 
 // Suspends the thread for up to 20 us (a hint): a poll that came back at once
 // would take the schedulers' slots from the warps that work.
@@ -241,20 +240,29 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   __shared__ Barriers bar;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* ops = smem;
-  uint8_t* qt = smem + kSlots * S::OP;
+  uint8_t* qt = smem + 2 * kSlots * S::OP;
   uint8_t* codes = qt + S::OP;
-  uint8_t* scales = codes + S::STAGES * S::CODES;
-  float* key_scale = reinterpret_cast<float*>(qt + S::OP + (F16 ? 0 : S::STAGES * (S::CODES + S::SCALES)));
+  float* key_scale = reinterpret_cast<float*>(codes + S::RINGS);
+  // Tile `at` of the CTA's (keys or values): its operand tile, and its codes
+  // with the scales behind them.
+  auto op_tile = [&](bool is_v, int at) { return ops + ((is_v ? 2 : 0) + (at & 1)) * S::OP; };
+  auto code_stage = [&](bool is_v, int at) { return is_v ? at % S::V_STAGES : at % S::K_STAGES; };
+  auto code_turn = [&](bool is_v, int at) { return is_v ? at / S::V_STAGES : at / S::K_STAGES; };
+  auto code_tile = [&](bool is_v, int at) {
+    if constexpr (F16) return op_tile(is_v, at);
+    return codes + (is_v ? S::K_STAGES * S::K_BYTES + code_stage(true, at) * S::V_BYTES
+                         : code_stage(false, at) * S::K_BYTES);
+  };
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
 
   Runs run;
   if (!run.begin(p, bar.plan)) return;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kSlots; ++i) {
-      mbar_init(&bar.op_ready[i], 4);
-      mbar_init(&bar.op_empty[i], 1);
-      mbar_init(&bar.code_full[i], 1);
-      mbar_init(&bar.code_empty[i], 4);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&bar.op_ready[i / 2][i % 2], 4);
+      mbar_init(&bar.op_empty[i / 2][i % 2], 1);
+      mbar_init(&bar.code_full[i / 2][i % 2], 1);
+      mbar_init(&bar.code_empty[i / 2][i % 2], 4);
       bar.nodes_bad[i][0] = bar.nodes_bad[i][1] = 0;
     }
     for (int i = 0; i < 2; ++i) {
@@ -293,74 +301,76 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     return true;
   };
 
-  int ops_done = 0, tiles_done = 0, runs_done = 0;  // before this run
-  if (warp == 16) {
+  int tiles_done = 0, runs_done = 0;  // before this run
+  if (warp == 16 || warp == 19) {
     // ---- copies ------------------------------------------------------------------
-    const int box = min(1 << p.cache.shift, BK), boxes = BK / box, group = 32 / boxes;  // tiles whose pages the lanes hold
-    uint32_t issued_stages = 0;
+    const bool is_v = warp == 19;
+    const CUtensorMap* map = is_v ? &p.v_map : &p.k_map;
+    // A box is a page's rows, up to a tile's; the lanes hold the pages of `group` tiles.
+    const int box_shift = min(p.cache.shift, 7), box = 1 << box_shift, boxes = BK >> box_shift;
+    const int group_shift = box_shift - 2;  // 32 / boxes
+    const bool leads = lane < boxes;
+    int issued = -1;  // the last tile whose copies were
     for (; run.next(p, bar.plan); ++runs_done) {
       const int32_t* page_row = p.pages.pages + run.seq * p.pages.ld;
       const int n = run.tiles;
-      auto pages_of = [&](int b) {  // lane l: box l % boxes of tile b group + l / boxes
-        const int k = run.k_begin + (b * 32 + lane) * box;
+      auto pages_of = [&](int b) {  // lane l: box l % boxes of tile (b << group_shift) + l / boxes
+        const int k = run.k_begin + ((b * 32 + lane) << box_shift);
         return k < run.k_end ? page_row[k >> p.cache.shift] : -1;
       };
-      // Groups of the latest key tile, the one before (values lag by a tile) and the next one.
-      int before = -1, now = n > 0 ? pages_of(0) : -1, next = n > 0 ? pages_of(1) : -1, held = 0;
-      for (int i = 0; i < 2 * n; ++i) {
-        bool is_v;
-        int j;
-        operand(i, n, is_v, j);
-        const int op = ops_done + i, st = op % S::STAGES;
-        const int b = j / group;
-        if (b > held) {
-          before = now, now = next, ++held;
-          next = pages_of(held + 1);
+      int now = n > 0 ? pages_of(0) : -1, next = n > 0 ? pages_of(1) : -1;
+      for (int j = 0; j < n; ++j) {
+        const int in_group = j & ((1 << group_shift) - 1);
+        if (j > 0 && in_group == 0) {
+          now = next;
+          next = pages_of((j >> group_shift) + 1);
         }
-        const int page = __shfl_sync(0xffffffffu, b == held ? now : before, ((j % group) * boxes + lane) & 31);
-        const int k = run.k_begin + j * BK + lane * box;
-        const bool mine = lane < boxes && k < run.k_end;
+        const int page = __shfl_sync(0xffffffffu, now, (in_group * boxes + lane) & 31);
+        const int at = tiles_done + j, st = code_stage(is_v, at);
+        const int k = run.k_begin + j * BK + (lane << box_shift);
+        const bool mine = leads && k < run.k_end;
         const bool there = mine && page >= 0 && page < p.cache.pages;
         const unsigned have = __ballot_sync(0xffffffffu, there);
         const unsigned lack = __ballot_sync(0xffffffffu, mine && !there);
         const int64_t row =
             (((int64_t)page * p.cache.heads + run.head) << p.cache.shift) + (k & ((1 << p.cache.shift) - 1));
-        const bool ok = wait(F16 ? &bar.op_empty[st] : &bar.code_empty[st], (op / S::STAGES & 1) ^ 1);
+        const bool ok = wait(F16 ? &bar.op_empty[is_v][st] : &bar.code_empty[is_v][st], (code_turn(is_v, at) & 1) ^ 1);
         if (!__all_sync(0xffffffffu, ok)) continue;
         if (lane == 0) {
           uint32_t bad = 0;  // a bit for each 16 keys
           for (unsigned left = lack; left != 0; left &= left - 1)
             bad |= ((1u << (box / 16)) - 1) << ((__ffs(left) - 1) * (box / 16));
-          bar.code_bad[st] = bad;
+          bar.code_bad[is_v][st] = bad;
           const int per_key = C::RB + (C::SCALED8 ? (is_v ? 0 : 2 * C::SB) : C::SB);
-          mbar_expect_tx(&bar.code_full[st], __popc(have) * box * per_key);
-          issued_stages = op + 1;
+          mbar_expect_tx(&bar.code_full[is_v][st], __popc(have) * box * per_key);
         }
+        issued = at;
         __syncwarp();
         if (there) {
-          uint8_t* to = (F16 ? ops + st * S::OP : codes + st * S::CODES) + lane * box * C::SPAN;
+          uint8_t* to = code_tile(is_v, at) + lane * box * C::SPAN;
+          uint64_t* full = &bar.code_full[is_v][st];
 #pragma unroll
           for (int s = 0; s < C::SLICES; ++s)
-            tma_rows(smem_u32(to + s * (BK * 128)), is_v ? &p.v_map : &p.k_map, s * 128, (int)row, &bar.code_full[st]);
+            tma_rows(smem_u32(to + s * (BK * 128)), map, s * 128, (int)row, full);
           if constexpr (C::SB > 0) {
-            uint8_t* to_scales = scales + st * S::SCALES + lane * box * C::SB;
+            uint8_t* to_scales = code_tile(is_v, at) + S::CODES + lane * box * C::SB;
             if (!C::SCALED8 || !is_v)
               bulk_g2s(to_scales, static_cast<const uint8_t*>(is_v ? p.cache.vs : p.cache.ks) + row * C::SB, box * C::SB,
-                       &bar.code_full[st]);
+                       full);
             if (C::SCALED8 && !is_v)
               bulk_g2s(to_scales + BK * C::SB, static_cast<const uint8_t*>(p.cache.vs) + row * C::SB, box * C::SB,
-                       &bar.code_full[st]);
+                       full);
           }
         }
       }
-      ops_done += 2 * n;
+      tiles_done += n;
     }
     // After a wait that gave up, copies may still be on their way.
     if (bar.gave_up && lane == 0) {
-      for (int back = 0; back < S::STAGES && back < (int)issued_stages; ++back) {
-        const int op = (int)issued_stages - 1 - back;
+      for (int at = max(issued - 1, 0); at <= issued; ++at) {
         const long long t0 = clock64();
-        while (!mbar_try_wait(&bar.code_full[op % S::STAGES], op / S::STAGES & 1) && clock64() - t0 < p.wait_cycles) {
+        while (!mbar_try_wait(&bar.code_full[is_v][code_stage(is_v, at)], code_turn(is_v, at) & 1) &&
+               clock64() - t0 < p.wait_cycles) {
         }
       }
     }
@@ -371,30 +381,30 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     for (; run.next(p, bar.plan); ++runs_done) {
       const int n = run.tiles;
       for (int j = 0; j < n; ++j) {
-        const int op = ops_done + (is_v ? v_index(j, n) : k_index(j)), st = op % S::STAGES, slot = op % kSlots;
-        bool ok = wait(&bar.code_full[st], op / S::STAGES & 1);
-        if constexpr (!F16) ok = wait(&bar.op_empty[slot], (op / kSlots & 1) ^ 1) && ok;
+        const int at = tiles_done + j, st = code_stage(is_v, at), slot = at & 1;
+        bool ok = wait(&bar.code_full[is_v][st], code_turn(is_v, at) & 1);
+        if constexpr (!F16) ok = wait(&bar.op_empty[is_v][slot], (at >> 1 & 1) ^ 1) && ok;
         ok = __all_sync(0xffffffffu, ok);
         const int key = run.k_begin + j * BK + row;
-        const uint32_t bad = bar.code_bad[st];
+        const uint32_t bad = bar.code_bad[is_v][st];
         const bool gone = key >= run.k_end || (bad >> (row / 16) & 1);
         const bool node = key >= run.len;
-        uint8_t* to = ops + slot * S::OP + row * 128;
+        uint8_t* to = op_tile(is_v, at) + row * 128;
         auto place = [&](int c) { return to + (c >> 3) * (BK * 128) + (((c & 7) ^ (row & 7)) << 4); };
         if (ok) {
           if constexpr (!F16) {
-            const uint8_t* from = codes + st * S::CODES;
-            const uint8_t* sc = scales + st * S::SCALES;
+            const uint8_t* from = code_tile(is_v, at);
+            const uint8_t* sc = from + S::CODES;
             if constexpr (C::SCALED8) {
               if (!is_v) {
-                const int at = (tiles_done + j) % kNotes;
+                const int note = at % kNotes;
                 const float vs = reinterpret_cast<const float*>(sc)[BK + row];
-                key_scale[at * BK + row] = reinterpret_cast<const float*>(sc)[row] * fabsf(p.scale_log2);
-                value_scale[at * BK + row] = vs;
+                key_scale[note * BK + row] = reinterpret_cast<const float*>(sc)[row] * fabsf(p.scale_log2);
+                value_scale[note * BK + row] = vs;
                 // Non-negative floats order as their bits.
                 const uint32_t most =
                     __reduce_max_sync(0xffffffffu, !gone && fabsf(vs) < kInf ? __float_as_uint(fabsf(vs)) : 0u);
-                if (lane == 0) bar.value_top[at][warp % 4] = fmaxf((float)((int)(most >> 23) - 126), kLeastScale);
+                if (lane == 0) bar.value_top[note][warp % 4] = fmaxf((float)((int)(most >> 23) - 126), kLeastScale);
               }
             }
             // Keys and values share this code: the roles of a scheduler share its
@@ -409,6 +419,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
               for (int c = 0; c < C::GROUPS; ++c)
                 group[c] = reinterpret_cast<const uint32_t*>(sc)[row * C::GROUPS + c];
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.code_empty[is_v][st]);  // the stage is read
             const uint32_t swizzle = (uint32_t)(row & 7) << 4;
 #pragma unroll
             for (int c = 0; c < C::RB / 16; ++c) {
@@ -457,19 +469,19 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             }
           }
           if (odd_value && !gone) {
-            const int at = key - run.len;
-            atomicOr(&bar.nodes_bad[runs_done % 4][at / 32], 1u << (at % 32));
+            const int bit = key - run.len;
+            atomicOr(&bar.nodes_bad[runs_done % 4][bit / 32], 1u << (bit % 32));
           }
-          if (!is_v && row == 0) bar.tile_bad[(tiles_done + j) % kNotes] = bad;
+          if (!is_v && row == 0) bar.tile_bad[at % kNotes] = bad;
         }
         fence_async();
         __syncwarp();
         if (lane == 0) {
-          if constexpr (!F16) mbar_arrive(&bar.code_empty[st]);
-          mbar_arrive(&bar.op_ready[slot]);
+          if (!F16 && !ok) mbar_arrive(&bar.code_empty[is_v][st]);
+          mbar_arrive(&bar.op_ready[is_v][slot]);
         }
       }
-      ops_done += 2 * n, tiles_done += n;
+      tiles_done += n;
     }
   } else if (warp == 17 || warp == 18) {
     // ---- products ---------------------------------------------------------------------
@@ -491,8 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       ++live_runs;
       for (int j = 0; j < n; ++j) {
         const int at = tiles_done + j, buf = at & 1;
-        const int op = ops_done + (second ? v_index(j, n) : k_index(j)), slot = op % kSlots;
-        ok = wait(&bar.op_ready[slot], op / kSlots & 1) && ok;
+        ok = wait(&bar.op_ready[second][buf], at >> 1 & 1) && ok;
         // The tile's weights, or those of the tile whose scores were there before.
         if (second) ok = wait(&bar.p_ready[buf], at >> 1 & 1) && ok;
         else if (at >= 2) ok = wait(&bar.p_ready[buf], (at - 2) >> 1 & 1) && ok;
@@ -500,25 +511,25 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         fence_after();
         if (elect()) {
           if (ok && !second) {
-            const uint32_t b = op_matrix + slot * (S::OP >> 4);
+            const uint32_t b = op_matrix + buf * (S::OP >> 4);
 #pragma unroll
             for (int ks = 0; ks < DIM / 16; ++ks) {
               const int off = ((ks / 4) * (BK * 128) + (ks % 4) * 32) >> 4;
               mma_ss(base + buf * BK, q_matrix + off, b + off, kScores, ks > 0);
             }
           } else if (ok) {
-            const uint32_t b = op_matrix + kLead + slot * (S::OP >> 4);
+            const uint32_t b = op_matrix + kLead + (2 + buf) * (S::OP >> 4);
 #pragma unroll
             for (int ks = 0; ks < BK / 16; ++ks)
               mma_ts(base + kOutAt, base + kWeightsAt + buf * (BK / 2) + ks * 8, b + (ks * 2048 >> 4), kOutput,
                      j > 0 || ks > 0);
           }
           commit(second ? &bar.pv_done[buf] : &bar.s_full[buf]);
-          commit(&bar.op_empty[slot]);
+          commit(&bar.op_empty[second][buf]);
         }
         __syncwarp();
       }
-      ops_done += 2 * n, tiles_done += n;
+      tiles_done += n;
     }
   } else if (warp < 8) {
     // ---- softmax, and the ends of the runs ------------------------------------------------

@@ -445,6 +445,27 @@ def test_long_and_ragged(P, kind, nodes):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 64), (128, 256)])
+def test_many_rows_long_runs(P, kind, dim, page):
+    """The tensor-core kernel: long items, short and empty ones, several runs to a CTA, rows beyond one block."""
+    g = gen(dim + page)
+    seqs, nodes, group = 24, 35, 4  # 140 rows
+    lens = g.integers(0, 700, seqs).astype(np.int32)
+    lens[[0, 5, 9]] = 6500, 0, 4099
+    pool = Pool(P, kind, seqs, 6500 + nodes, 1, dim, page, seed=7)
+    q = (1.5 * g.standard_normal((seqs, nodes, group, dim))).astype(np.float16)
+    _, sees = random_tree(g, seqs, nodes)
+    counts = g.integers(0, nodes + 1, seqs).astype(np.int32)
+    workspace = pool.cache.make_workspace(dev(q))
+    a = check(P, pool, q, lens, words(sees), counts, rows_of(sees, counts), workspace=workspace)
+    for _ in range(3):  # the order of the sums does not depend on timing
+        b = pool.cache.tree_attention(dev(q), pool.pages, dev(lens), mask=dev(words(sees)), counts=dev(counts),
+                                      workspace=workspace)
+        np.testing.assert_array_equal(a, b.double().cpu().numpy())
+    P.workspace_status(workspace)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("nodes,group", [(6, 2), (40, 4)])
 def test_masked_places_hold_nan_and_infinity(P, kind, nodes, group):
     """Slots after a sequence's end, and nodes that a node does not see."""
