@@ -91,7 +91,7 @@ struct Barriers {
     int c0, c1, seq, head, tile, rows;
   } part[2];
   int parts;
-  bool last;
+  bool last[2];
 };
 
 // The runs of this CTA, one after another, known to every warp. What stays the
@@ -813,16 +813,18 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   if (bar.gave_up && threadIdx.x == 0) atomicOr(p.status, kStatusTimeout);
   // ---- items that span CTAs: the last CTA to arrive joins the parts, in order, all its
   // threads at it (128 threads with a row each read 64 KB parts at 11 GB/s: 40 us)
+  if ((int)threadIdx.x < bar.parts) {  // the CTA's parts are released with it
+    unsigned* counter = &p.counters[bar.part[threadIdx.x].c0];
+    const unsigned others = bar.part[threadIdx.x].c1 - bar.part[threadIdx.x].c0;
+    const bool last = atom_add_acq_rel_gpu(counter, 1u) == others;
+    bar.last[threadIdx.x] = last;
+    if (last) *counter = 0;  // as the next call finds it
+  }
+  __syncthreads();
   for (int i = 0; i < bar.parts; ++i) {
     const int c0 = bar.part[i].c0, c1 = bar.part[i].c1;
-    if (threadIdx.x == 0) {  // the CTA's parts are released with it
-      const unsigned arrived = atom_add_acq_rel_gpu(&p.counters[c0], 1u);
-      bar.last = arrived == (unsigned)(c1 - c0);
-      if (bar.last) p.counters[c0] = 0;  // as the next call finds it
-    }
-    __syncthreads();
     const int row0 = lane * 4, e0 = warp * 8;  // of this thread: 4 rows, 8 places
-    if (bar.last && e0 < DIM && row0 < bar.part[i].rows) {
+    if (bar.last[i] && e0 < DIM && row0 < bar.part[i].rows) {
       auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * S::PART; };
       auto four = [&](const float* from, int e) { return __ldcg(reinterpret_cast<const float4*>(from + e * kRows + row0)); };
       float top[4], total[4] = {0.f, 0.f, 0.f, 0.f}, acc[8][4];
@@ -832,9 +834,14 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e][r] = 0.f;
       }
-      for (int c = c0; c <= c1; ++c) {
-        const float4 m = four(part_of(c), DIM);
-        top[0] = fmaxf(top[0], m.x), top[1] = fmaxf(top[1], m.y), top[2] = fmaxf(top[2], m.z), top[3] = fmaxf(top[3], m.w);
+      for (int c = c0; c <= c1; c += 4) {  // four parts' loads in flight
+        float4 m[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m[k] = four(part_of(min(c + k, c1)), DIM);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          top[0] = fmaxf(top[0], m[k].x), top[1] = fmaxf(top[1], m[k].y), top[2] = fmaxf(top[2], m[k].z),
+          top[3] = fmaxf(top[3], m[k].w);
       }
 #pragma unroll 2
       for (int c = c0; c <= c1; ++c) {
@@ -877,7 +884,6 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
               live ? (top[r] - kShift + log2f(total[r])) * 0.69314718056f : -kInf;
       }
     }
-    __syncthreads();  // bar.last is read
   }
   if (warp == 16) {
     if (bar.gave_up) {  // products may still be on their way: let them end before their memory goes
