@@ -83,7 +83,8 @@ struct Barriers {
   uint32_t tmem;
   volatile int gave_up;
   uint32_t code_bad[2][2], tile_bad[kNotes];   // bits: 16 keys each whose page is missing
-  uint32_t nodes_bad[4][2];                 // by run: nodes whose value is not finite
+  uint32_t nodes_bad[4][2];                 // by run that has keys: nodes whose value is not finite (values are
+                                            // decoded at most two tiles, so two such runs, ahead of their use)
   float top[2][2][kRows], sum[2][kRows];    // of the halves of a tile (by tile), and of a run
   float value_top[kNotes][4];                    // by tile and warp: power of two above the values' scales
   // Parts of items that this CTA has left: of its first and of its last run.
@@ -301,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     return true;
   };
 
-  int tiles_done = 0, runs_done = 0;  // before this run
+  int tiles_done = 0, runs_done = 0;  // before this run (runs: those with keys)
   if (warp == 16 || warp == 19) {
     // ---- copies ------------------------------------------------------------------
     const bool is_v = warp == 19;
@@ -311,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     const int group_shift = box_shift - 2;  // 32 / boxes
     const bool leads = lane < boxes;
     int issued = -1;  // the last tile whose copies were
-    for (; run.next(p, bar.plan); ++runs_done) {
+    while (run.next(p, bar.plan)) {
       const int32_t* page_row = p.pages.pages + run.seq * p.pages.ld;
       const int n = run.tiles;
       auto pages_of = [&](int b) {  // lane l: box l % boxes of tile (b << group_shift) + l / boxes
@@ -378,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     // ---- decode ---------------------------------------------------------------------
     const int row = threadIdx.x % 128;
     const bool is_v = warp >= 12;
-    for (; run.next(p, bar.plan); ++runs_done) {
+    for (; run.next(p, bar.plan); runs_done += run.tiles > 0) {
       const int n = run.tiles;
       for (int j = 0; j < n; ++j) {
         const int at = tiles_done + j, st = code_stage(is_v, at), slot = at & 1;
@@ -494,13 +495,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     constexpr uint32_t kLead = (uint32_t)(BK * 128 - 16) >> 4 << 16;  // values: 64 entries in a group
     constexpr uint32_t kScores = 1u << 4 | (uint32_t)(BK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
     constexpr uint32_t kOutput = 1u << 4 | 1u << 16 | (uint32_t)(DIM >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
-    int live_runs = 0;
-    for (; run.next(p, bar.plan); ++runs_done) {
+    for (; run.next(p, bar.plan); runs_done += run.tiles > 0) {
       const int n = __shfl_sync(0xffffffffu, run.tiles, 0);
       if (n == 0) continue;
       bool ok = true;
-      if (!second) ok = wait(&bar.q_ready, live_runs & 1);
-      ++live_runs;
+      if (!second) ok = wait(&bar.q_ready, runs_done & 1);
       for (int j = 0; j < n; ++j) {
         const int at = tiles_done + j, buf = at & 1;
         ok = wait(&bar.op_ready[second][buf], at >> 1 & 1) && ok;
@@ -538,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     const uint32_t base = tmem + ((uint32_t)(warp % 4 * 32) << 16);
     const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);  // -infinity times it stays so
     const int e0 = half * (DIM / 2);
-    for (; run.next(p, bar.plan); ++runs_done) {
+    for (; run.next(p, bar.plan); runs_done += run.tiles > 0) {
       const int n = run.tiles, rows = run.rows(p);
       const bool real = row < rows;
       // Where this row's node and query head stand (found again where they are

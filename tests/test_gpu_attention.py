@@ -493,6 +493,23 @@ def test_masked_places_hold_nan_and_infinity(P, kind, nodes, group):
     assert not np.isfinite(y[2, 1, :, 7]).any() and np.isfinite(y[2, 0]).all()
 
 
+@pytest.mark.parametrize("kind", ["f16", "int8"])
+@pytest.mark.parametrize("nodes", [5, 33])
+def test_infinite_values_among_empty_sequences(P, kind, nodes):
+    """Many sequences to a CTA, most of them empty: each one's odd values are its own."""
+    g, seqs = gen(12), 1024
+    pool = Pool(P, kind, seqs, 48, 1, 64, 16, seed=6)
+    inf = g.standard_normal((1, 1, 1, 64)).astype(np.float32)
+    inf[..., 7] = np.inf
+    for b in range(4, seqs, 8):
+        pool.write("v", inf, [b], [0])
+    counts = np.where(np.arange(seqs) % 4 == 0, nodes, 0)
+    sees = np.repeat(np.eye(nodes, dtype=bool)[None], seqs, 0)
+    q = g.standard_normal((seqs, nodes, 1, 64)).astype(np.float16)
+    y = check(P, pool, q, np.zeros(seqs, np.int32), words(sees), counts, rows_of(sees, counts))
+    assert not np.isfinite(y[4::8, 0, :, 7]).any() and np.isfinite(y[0::8]).all() and np.isfinite(y[4::8, 1:]).all()
+
+
 def test_missing_pages_strides_masks_and_scales(P):
     g = gen(10)
     nodes, group, dim = 5, 3, 128
