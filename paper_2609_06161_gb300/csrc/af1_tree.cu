@@ -58,8 +58,7 @@ struct Shape {
   static constexpr int RING = W * STAGES * 2 * KW * C::RB;    // k and v of every stage of every warp
   static constexpr int SCALES = W * STAGES * 2 * KW * C::SB;
   static constexpr int JOIN = W * ROWS * DIM * 4;             // the warps' o, over the ring
-  static constexpr int QS = NT > 2 ? NT * C::KS * 32 * 8 : 0;  // q's operands where registers do not hold them
-  static constexpr int SMEM = RING + SCALES + QS + 1024;
+  static constexpr int SMEM = RING + SCALES + 1024;
   static constexpr int PART = ROWS * (DIM + 2);               // floats of a part: o, m, l
   static_assert(JOIN <= RING, "the warps' outputs are joined over their rings");
   static_assert((KW * C::RB) % 512 == 0, "a stage keeps the swizzle's alignment");
@@ -82,7 +81,6 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
   const int g = lane / 4, t = lane % 4;
   uint8_t* ring = smem + warp * (STAGES * STAGE);
   uint8_t* ring_scales = smem + S::RING + warp * (STAGES * 2 * KW * C::SB);
-  uint2* qs = reinterpret_cast<uint2*>(smem + S::RING + S::SCALES);
   float* join = reinterpret_cast<float*>(smem);
 
   if (lane == 0) {
@@ -190,7 +188,7 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
     fetch_pages(key0);
 
     // -- q: the b operands, and its sums over the entries of a group -----------
-    uint32_t qf[NT <= 2 ? NT : 1][KS][2];
+    uint32_t qf[NT][KS][2];
     float q128[NT][2];           // INT8: 128 sum q of rows 2 t and 2 t + 1
     uint32_t q_sums[INT4 ? NT : 1];  // INT4: sum q / 32 over group t of row g, in two parts
     auto load_q = [&](int nt, uint32_t (&b)[KS][2]) {
@@ -237,18 +235,7 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
       }
     };
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      if constexpr (NT <= 2) {
-        load_q(nt, qf[nt]);
-      } else {
-        uint32_t b[KS][2];
-        load_q(nt, b);
-        if (warp == nt % W) {
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) qs[(nt * KS + ks) * 32 + lane] = make_uint2(b[ks][0], b[ks][1]);
-        }
-      }
-    }
+    for (int nt = 0; nt < NT; ++nt) load_q(nt, qf[nt]);
 
     int issued = 0;  // steps of this run
 #pragma unroll
@@ -260,7 +247,6 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
         fetch_pages(key + STRIDE);
       }
     }
-    if constexpr (NT > 2) __syncthreads();  // qs
 
     // o^T: block m, column block nt: entries row_entry(m, g, i / 2) of rows 2 t + i % 2.
     float o[MT][NT][4], m[NT][2], l[NT][2], vref = 0.f;
@@ -303,10 +289,6 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
         for (int h = 0; h < 2; ++h) load_key<C, KIND, KW>(w[h], kb, mb * 16 + 8 * h + g, t);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) s[mb][nt][0] = s[mb][nt][1] = s[mb][nt][2] = s[mb][nt][3] = 0.f;
-        auto q_of = [&](int nt, int ks) {
-          if constexpr (NT <= 2) return make_uint2(qf[nt][ks][0], qf[nt][ks][1]);
-          else return qs[(nt * KS + ks) * 32 + lane];
-        };
         if constexpr (INT4) {
           const uint32_t* sc = reinterpret_cast<const uint32_t*>(ksb);
           uint32_t a[4] = {0, 0, 0, 0};
@@ -329,9 +311,8 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               float acc[4] = {0.f, 0.f, 0.f, 0.f};
-              const uint2 b0 = q_of(nt, 2 * c), b1 = q_of(nt, 2 * c + 1);
-              mma(acc, a0, b0.x, b0.y);
-              mma(acc, a1, b1.x, b1.y);
+              mma(acc, a0, qf[nt][2 * c][0], qf[nt][2 * c][1]);
+              mma(acc, a1, qf[nt][2 * c + 1][0], qf[nt][2 * c + 1][1]);
 #pragma unroll
               for (int i = 0; i < 4; ++i) s[mb][nt][i] = fmaf(acc[i], key_scale[i / 2][c], s[mb][nt][i]);
             }
@@ -347,10 +328,7 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
             uint32_t a[4];
             key_operand<KIND>(a, w, ks);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              const uint2 b = q_of(nt, ks);
-              mma(s[mb][nt], a, b.x, b.y);
-            }
+            for (int nt = 0; nt < NT; ++nt) mma(s[mb][nt], a, qf[nt][ks][0], qf[nt][ks][1]);
           }
           float f[2] = {p.scale_log2, p.scale_log2};
           if constexpr (C::SCALED8) {
