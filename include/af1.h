@@ -520,7 +520,8 @@ AF1_API int af1_budget_to_rank(double b, int64_t m, int64_t n, int64_t* r_out);
  * tokens. The paper has no counterpart. Values are FP16 or FP32 (AF1_F16,
  * AF1_F32), as the linears write them; sums, softmax statistics and rotations
  * are FP32. Strides are in elements; the last axis of every tensor has unit
- * stride. A call with nothing to do (no tokens, no sequences) returns AF1_OK. */
+ * stride. Outputs overlap no input and no other output unless an entry says
+ * so. A call with nothing to do (no tokens, no sequences) returns AF1_OK. */
 
 /* Rotary position tables. Pair i of the `dim` rotated entries turns by
  * position * f_i, f_i = base^(-2i / dim), rescaled for contexts longer than

@@ -12,9 +12,9 @@
 // the units of all items (ragged lengths balance by themselves; each item
 // counts some units more, for what a run costs whatever its length: without
 // them the CTA that had eight short items ran 102 us where the others ran 70).
-// Inside a CTA each warp takes every W-th step of KW keys of a run, with a ring of its
-// own in shared memory that TMA fills, its own running maximum m and sum l,
-// and an accumulator in registers; warps meet once a run, to join (m, l, o).
+// Inside a CTA each warp takes every W-th step of KW keys of a run, with a ring
+// of its own in shared memory that TMA fills, its own running maximum m and sum
+// l, and an accumulator in registers; warps meet once a run, to join (m, l, o).
 // Where an item spans CTAs, each leaves its part in the workspace and the
 // last one to arrive joins them in order, so that results do not depend on
 // timing.
@@ -41,6 +41,10 @@
 // p is rounded to FP16, times 2^kShift, relative to a maximum that is moved
 // only when a score passes it by 2^kSlack, and to the largest value scale so
 // far; m, l, scores and outputs are FP32.
+//
+// Bound: device memory where contexts are long (32 sequences of up to 8192 INT8
+// tokens, 8 heads of 128, 4 queries each: 71 us, 0.85 of the copy rate), latency
+// where they are short (1000 FP16 tokens: 9 us).
 #include "af1_tree.cuh"
 
 namespace af1 {
