@@ -9,22 +9,27 @@
 // may be so large that y overflows, so there r is x itself and d the scaled
 // difference.
 //
-// The largest entries: each warp keeps its 32 largest so far, one to a lane,
-// in order. Keys of 64 bits (the value as an ordered integer, then the index,
-// inverted) make the order total, so that equal values go by index and the
-// result does not depend on which thread saw what first. An entry is looked
-// at again only where it may be among the `top`: it is not below the `top`-th
-// of its warp, nor below what all warps of the CTA have ceil(top / warps) of
-// (then `top` entries are as large). A warp's first bound is the `top`-th
-// largest of its lanes' maxima.
+// The largest entries. Passing over the logits, a warp only keeps its lanes'
+// maxima of every batch (of 16 or 32 entries to a lane). Every kSegment batches
+// it looks back: if ceil(top / warps) lanes of every warp, or `top` lanes of
+// this one, have a maximum of at least some bound, `top` entries of the row
+// have, so only batches of lanes whose maximum is not below it are read again
+// (about 8 to a warp, for the 20 largest of 128001 in random order), and their entries
+// that are not below it are merged into the warp's list of its 32 largest, one
+// to a lane, in order. Keys of 64 bits (the value as an ordered integer, then
+// the index, inverted) make the order total, so that equal values go by index
+// and the result does not depend on which thread saw what first. (With entries
+// compared with the list as they came by, warps waited on their lists: 512 rows
+// of 128001 FP16 logits took 45 us with the 20 largest where 25 without.)
 //
 // A cluster of CTAs takes a row (one CTA where there are rows enough to fill
 // the GPU), and its first CTA joins their statistics and lists through
-// distributed shared memory. Issue slots bound large calls: an entry costs one
-// exponent and about five instructions (pairs of entries share FP32 additions
-// and multiply-adds); 512 rows of 128001 FP16 logits, 20 largest, take 45 us,
-// 2.9 TB/s. Small ones are bound by the latency of lists and joins: 5 rows of
-// 32000 FP32 logits take 8 us.
+// distributed shared memory. Logits come by asynchronous copies, three batches of a
+// warp in flight. Large calls are bound by device memory and the look back:
+// those 512 rows take 32.5 us (4.0 TB/s), 26 without the largest; the pass
+// itself costs one exponent and about five instructions an entry (pairs of
+// entries share FP32 additions and multiply-adds). Small calls are bound by the
+// latency of lists and joins: 5 rows of 32000 FP32 logits take 7 us.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -42,6 +47,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxCluster = 8;
+constexpr int kSegment = 32;  // batches
 constexpr float kInf = __builtin_huge_valf();
 
 struct ScoreProblem {
@@ -60,6 +66,12 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ __half max_nan(__half a, __half b) { return __hmax_nan(a, b); }
 constexpr float kLeast = -1e4f;  // 2^d is 0 from far above on; d itself may be -infinity
 
 // r is -infinity where nothing is summed (or NaN alone).
@@ -145,15 +157,23 @@ __device__ __forceinline__ uint64_t merge_lists(uint64_t a, uint64_t b, int lane
   return k;
 }
 
+// 16 bytes to shared memory, as part of the thread's next group of copies.
+__device__ __forceinline__ void copy16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constant__ ScoreProblem p) {
   constexpr int E = 16 / (int)sizeof(T);  // entries of a 16-byte access
   constexpr int U = 4;                    // accesses of a batch: 16 or 32 entries to a lane
   constexpr bool HALF = sizeof(T) == 2;
+  constexpr int STAGES = TOP && !HALF ? 3 : 4;  // batches of a warp's ring: 48 KB in all
+  __shared__ uint4 ring[kWarps][STAGES][U][32];  // each lane reads what it has copied itself
   __shared__ Stats stats[kWarps];
   __shared__ uint64_t lists[kWarps][32];
-  __shared__ uint4 stage[TOP ? kWarps : 1][U][32];  // a batch whose entries are looked at again
-  __shared__ volatile float share[kWarps];  // the ceil(top / kWarps)-th entry of each warp
+  __shared__ T tops[TOP ? kWarps : 1][kSegment][32];  // the lanes' maxima of a segment's batches
+  __shared__ uint64_t found[TOP ? kWarps : 1][64];    // keys on their way to the list
+  __shared__ volatile float share[kWarps];  // ceil(top / kWarps) entries of each warp are as large
   cg::cluster_group cluster = cg::this_cluster();
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -166,81 +186,68 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
   const int head = (int)min((int64_t)((16 - (uintptr_t)x % 16) % 16 / sizeof(T)), p.vocab);
   const int64_t nvec = (p.vocab - head) / E;
   const uint4* body = reinterpret_cast<const uint4*>(x + head);
-  auto load = [&](uint4 (&w)[U], int64_t batch) {
+  auto load = [&](int64_t batch, int slot) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t i = batch * (32 * U) + u * 32 + lane;
-      if (i < nvec) w[u] = __ldcs(body + i);
+      if (i < nvec) copy16(&ring[warp][slot][u][lane], body + i);
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
   const int64_t batches = (nvec + 32 * U - 1) / (32 * U);
   const int64_t first = rank * kWarps + warp, step = (int64_t)cs * kWarps;
-  uint4 next[2][U];  // two batches ahead
-  load(next[0], first);
-  load(next[1], first + step);
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) load(first + i * step, i);
+  int slot = 0;
   // The first given tokens' logits, for the end.
   float given = -kInf;
   if (rank == 0 && warp == 0 && lane < p.given) {
     const int id = p.tokens[row * p.given + lane];
     if (id >= 0 && id < p.vocab) given = (float)x[id];
   }
-  if constexpr (TOP) {
-    if (lane == 0) share[warp] = -kInf;
-    __syncthreads();
-  }
 
   Stats st;
   uint64_t mine = 0;    // this lane's entry of the warp's list
   uint64_t kth = 0;     // its `top`-th
   float bound = -kInf;  // entries below it cannot be among the `top`
-  auto consider = [&](float v, bool real, uint32_t index) {
-    if (__ballot_sync(0xffffffffu, real && !(v < bound)) == 0) return;
-    const uint64_t key = real && !(v < bound) ? order_key(v, index) : 0;
-    unsigned want = __ballot_sync(0xffffffffu, key > kth);
-    if (want == 0) return;
-    if (__popc(want) > 8) {
-      mine = merge_lists(mine, warp_sort(key, lane), lane);
-    } else {
-      while (want != 0) {
-        const int from = __ffs(want) - 1;
-        want &= want - 1;
-        const uint64_t k = __shfl_sync(0xffffffffu, key, from);
-        const int at = __popc(__ballot_sync(0xffffffffu, mine > k));
-        const uint64_t up = __shfl_up_sync(0xffffffffu, mine, 1);
-        mine = lane < at ? mine : lane == at ? k : up;
-      }
-    }
+  auto merge = [&](uint64_t key) {  // one to a lane, 0: none
+    mine = merge_lists(mine, warp_sort(key, lane), lane);
     kth = __shfl_sync(0xffffffffu, mine, p.top - 1);
     bound = fmaxf(bound, key_bound(kth));
   };
 
-  auto pass = [&](int64_t b, uint4 (&ahead)[U]) {
+  auto pass = [&](int64_t b) {  // the lane's maximum
     uint4 w[U];
     const int64_t left = nvec - b * (32 * U) - lane;  // accesses of this lane: those u with 32 u < left
+    // Into the slot that the batch before was read from.
+    load(b + (STAGES - 1) * step, slot == 0 ? STAGES - 1 : slot - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = ahead[u];
-    load(ahead, b + 2 * step);
+    for (int u = 0; u < U; ++u) w[u] = ring[warp][slot][u][lane];
+    if (++slot == STAGES) slot = 0;
     if ((b + 1) * (32 * U) > nvec) {  // the last, in part: -infinity changes nothing
       const uint32_t none = HALF ? 0xfc00fc00u : 0xff800000u;
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (32 * u >= left) w[u] = make_uint4(none, none, none, none);
     }
-    float top;
+    // NaN if there is one: the reference then stays, and the sums become NaN.
+    T lane_top;
     if constexpr (HALF) {
       __half2 most = __half2half2(__ushort_as_half(0xfc00));
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = __hmax2(most, reinterpret_cast<const __half2*>(&w[u])[i]);
-      top = fmaxf(__low2float(most), __high2float(most));
+        for (int i = 0; i < 4; ++i) most = __hmax2_nan(most, reinterpret_cast<const __half2*>(&w[u])[i]);
+      lane_top = __hmax_nan(__low2half(most), __high2half(most));
     } else {
-      top = -kInf;
+      lane_top = -kInf;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, reinterpret_cast<const float*>(&w[u])[i]);
+        for (int i = 0; i < 4; ++i) lane_top = max_nan(lane_top, reinterpret_cast<const float*>(&w[u])[i]);
     }
+    const float top = (float)lane_top;
     const float r = reference<T>(top, c);
     if (r > st.r) {
       const float d = fmaxf(distance<T>(st.r, r, c), kLeast), f = ex2(d);
@@ -264,50 +271,75 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
       }
     st.s = s2.x + s2.y;
     st.t = t2.x + t2.y;
-    if constexpr (TOP) {
-      if (b == first) {
-        const float sorted = sort_descending(top, lane);
-        bound = fmaxf(bound, __shfl_sync(0xffffffffu, sorted, p.top - 1));
+    return lane_top;
+  };
+  // Batches first + k step, k0 <= k < k0 + n, whose lanes' maxima are kept; the
+  // largest of them, seg_top, to a lane.
+  auto look_back = [&](int64_t k0, int n, float seg_top) {
+    const int part = (p.top + kWarps - 1) / kWarps - 1;
+    const float sorted = sort_descending(seg_top != seg_top ? kInf : seg_top, lane);
+    bound = fmaxf(bound, __shfl_sync(0xffffffffu, sorted, p.top - 1));
+    const float listed = key_bound(__shfl_sync(0xffffffffu, mine, part));
+    if (lane == part) share[warp] = fmaxf(sorted, listed);
+    __syncthreads();
+    float least = share[0];
+#pragma unroll
+    for (int i = 1; i < kWarps; ++i) least = fminf(least, share[i]);
+    bound = fmaxf(bound, least);
+    uint32_t mask = 0;  // of the lane's batches
+    for (int k = 0; k < n; ++k) mask |= (float)tops[warp][k][lane] < bound ? 0u : 1u << k;
+    auto next_one = [&] {  // a batch of a lane: 32 k + lane, or -1
+      const unsigned have = __ballot_sync(0xffffffffu, mask != 0);
+      if (have == 0) return -1;
+      const int from = __ffs(have) - 1, k = __shfl_sync(0xffffffffu, __ffs(mask) - 1, from);
+      if (lane == from) mask &= mask - 1;
+      return 32 * k + from;
+    };
+    constexpr int N = E * U, AT_ONCE = HALF ? 8 : 4;  // entries of such a batch, and batches (FP32: pairs of them) in flight
+    int count = 0;
+    while (__any_sync(0xffffffffu, mask != 0)) {
+      float v[AT_ONCE];
+      uint32_t index[AT_ONCE];  // below 2^31
+#pragma unroll
+      for (int s = 0; s < AT_ONCE; ++s) {
+        int one = next_one();
+        if constexpr (N < 32) {
+          const int second = next_one();
+          if (lane >= N) one = second;
+        }
+        const int64_t access = (first + (k0 + (one >> 5)) * step) * (32 * U) + lane % N / E * 32 + (one & 31);
+        index[s] = one >= 0 && access < nvec ? (uint32_t)(head + access * E + lane % E) : ~0u;
+        v[s] = index[s] != ~0u ? (float)x[index[s]] : -kInf;
       }
-      // A NaN hides from the maximum, and shows in the sum.
-      if (__any_sync(0xffffffffu, !(top < bound) || st.s != st.s)) {
-        float least = lane < kWarps ? (float)share[lane] : kInf;
 #pragma unroll
-        for (int d = 1; d < kWarps; d <<= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, d));
-        bound = fmaxf(bound, __shfl_sync(0xffffffffu, least, 0));
-        if (__any_sync(0xffffffffu, !(top < bound) || st.s != st.s)) {
-          // Bit 16 h + i: entry h of pair i; entry by entry from shared memory.
-          uint32_t maybe = 0;
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            stage[warp][u][lane] = w[u];
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-              const int at = u * (E / 2) + i;
-              if constexpr (HALF) {
-                const uint32_t below = __hlt2_mask(reinterpret_cast<const __half2*>(&w[u])[i], __float2half2_rn(bound));
-                maybe |= (~below & 0x00010001u) << at;
-              } else {
-                const float2 v = reinterpret_cast<const float2*>(&w[u])[i];
-                maybe |= (v.x < bound ? 0u : 1u << at) | (v.y < bound ? 0u : 0x10000u << at);
-              }
-            }
-          }
-          while (__any_sync(0xffffffffu, maybe != 0)) {
-            const int bit = maybe != 0 ? __ffs(maybe) - 1 : 0, u = (bit % 16) / (E / 2), i = 2 * (bit % (E / 2)) + bit / 16;
-            const float v = (float)reinterpret_cast<const T*>(&stage[warp][u][lane])[i];
-            consider(v, maybe != 0 && 32 * u < left, (uint32_t)(head + (b * (32 * U) + u * 32 + lane) * E + i));
-            maybe &= maybe - 1;
-          }
-          const uint64_t part = __shfl_sync(0xffffffffu, mine, (p.top + kWarps - 1) / kWarps - 1);
-          if (lane == 0) share[warp] = key_bound(part);
+      for (int s = 0; s < AT_ONCE; ++s) {
+        const uint64_t key = index[s] == ~0u || v[s] < bound ? 0 : order_key(v[s], index[s]);
+        const unsigned want = __ballot_sync(0xffffffffu, key > kth);
+        if (key > kth) found[warp][count + __popc(want & ((1u << lane) - 1))] = key;
+        count += __popc(want);
+        if (count >= 32) {
+          __syncwarp();
+          const uint64_t now = found[warp][lane], rest = found[warp][32 + lane];
+          __syncwarp();
+          found[warp][lane] = rest;
+          count -= 32;
+          merge(now);
         }
       }
     }
+    __syncwarp();
+    if (count > 0) merge(lane < count ? found[warp][lane] : 0);
+    __syncwarp();
   };
-  for (int64_t b = first; b < batches; b += 2 * step) {
-    pass(b, next[0]);
-    if (b + step < batches) pass(b + step, next[1]);
+  const int64_t rounds = (batches - rank * kWarps + step - 1) / step;  // of the CTA's first warp: the most
+  for (int64_t k0 = 0; k0 < rounds; k0 += kSegment) {
+    const int n = (int)min((int64_t)kSegment, (batches - first + step - 1) / step - k0);  // may be 0, or less
+    T most = (T)-kInf;
+    for (int k = 0; k < n; ++k) {
+      const T one = pass(first + (k0 + k) * step);
+      if constexpr (TOP) tops[warp][k][lane] = one, most = max_nan(most, one);
+    }
+    if constexpr (TOP) look_back(k0, n, (float)most);
   }
   if (rank == 0 && warp == 0) {  // the ends: fewer than 2 E entries
     const int64_t tail = p.vocab - head - nvec * E;
@@ -317,7 +349,10 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
     Stats one;
     if (real) one.r = reference<T>(v, c), one.s = v == -kInf ? 0.f : ex2(v - v);
     st = join<T>(st, one, c);
-    if constexpr (TOP) consider(v, real, (uint32_t)i);
+    if constexpr (TOP) {
+      const uint64_t key = real && !(v < bound) ? order_key(v, (uint32_t)i) : 0;
+      if (__any_sync(0xffffffffu, key > kth)) merge(key);
+    }
   }
 
   // -- join: lanes, warps, the cluster's CTAs ---------------------------------

@@ -681,6 +681,19 @@ def test_scores_of_hard_rows(P, dtype):
     score_check(P, x, None, 0)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_scores_of_long_rows(P, dtype):
+    """Rows that a thread passes over in several stretches, the largest entries in any of them."""
+    g, vocab = gen(22), 2200003
+    up = torch.arange(vocab, device="cuda") / 131072
+    r = dev(g.standard_normal((4, vocab)).astype(np.float32))
+    r[1, -5], r[2, : 20], r[2, 1500000:1500009] = float("nan"), 30.0, 30.0
+    x = torch.stack([up, -up, torch.zeros_like(up), *r]).to(dtype)
+    tokens = g.integers(0, vocab, (7, 2)).astype(np.int32)
+    score_check(P, x, tokens, 32)
+    score_check(P, x[3:], tokens[3:], 1)
+
+
 def test_scores_strides(P):
     g = gen(21)
     for dtype in (torch.float16, torch.float32):
