@@ -7,7 +7,7 @@
 // nodes that share a cached head are the rows of one product, so that the
 // cache is read once for all of them.
 //
-// Split. An item is one sequence, one cached head and one block of 8 NT rows;
+// Split. An item is one sequence and one cached head, with 8 NT rows at most;
 // its keys are cut into units of kUnit, and every CTA takes an equal run of
 // the units of all items (ragged lengths balance by themselves; each item
 // counts some units more, for what a run costs whatever its length: without
@@ -43,7 +43,7 @@
 // far; m, l, scores and outputs are FP32.
 //
 // Bound: device memory where contexts are long (32 sequences of up to 8192 INT8
-// tokens, 8 heads of 128, 4 queries each: 71 us, 0.85 of the copy rate), latency
+// tokens, 8 heads of 128, 4 queries each: 70 us, 0.86 of the copy rate), latency
 // where they are short (1000 FP16 tokens: 9 us).
 #include "af1_tree.cuh"
 
@@ -52,7 +52,9 @@ namespace {
 
 constexpr int kUnit = 64;                         // keys of a unit
 constexpr int kMinRun = 256;                      // keys of a CTA, at least (where there are so many)
-constexpr int kSetup = 12;                        // units that a run's beginning and end are worth, at most
+constexpr int kSetup = 10;                        // units that a run's beginning and end are worth (with 4, 4 trees
+                                                  // of 4 over 8000 E4M3 tokens took 33 us instead of 31; 16: 30,
+                                                  // but 32 long INT4 sequences 77 instead of 74)
 constexpr float kCode = 16777216.f;               // 2^24: codes as subnormals
 
 template <int KIND, int DIM, int NT, int W, int KW, int STAGES>
@@ -95,10 +97,9 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
   __syncwarp();
 
   // This CTA's units: begin .. end - 1 of all items'.
-  const int64_t lanes = (int64_t)p.cache.heads * p.row_tiles;
-  Sequences<kUnit> sq;
-  int setup;
-  const int64_t total = sq.begin(p, lanes, kSetup / 3, kSetup, setup);
+  const int64_t lanes = p.cache.heads;
+  Sequences<kUnit, kSetup> sq;
+  const int64_t total = sq.begin(p) * lanes;
   int64_t ctas = min((int64_t)gridDim.x, (total * kUnit + kMinRun - 1) / kMinRun);
   ctas = min(ctas, total);  // each has a unit at least
   if (blockIdx.x >= ctas) return;
@@ -107,28 +108,26 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
   const int64_t begin = per * blockIdx.x + min((int64_t)blockIdx.x, more);
   const int64_t end = begin + per + (blockIdx.x < more ? 1 : 0);
 
+  const int rows = p.nodes * p.group;
   uint32_t phases = 0;   // of the warp's barriers
   bool alive = true;     // no wait has given up
   for (int64_t pos = begin; pos < end;) {
-    while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after(), setup);
+    while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after());
     const int which = __popc(__ballot_sync(0xffffffffu, (sq.before + sq.sum) * lanes <= pos));
     const int seq = sq.first + which;
     const int units = __shfl_sync(0xffffffffu, sq.units, which);
     const int len = __shfl_sync(0xffffffffu, sq.len, which), keys = __shfl_sync(0xffffffffu, sq.keys, which);
     const int64_t seq_first = (sq.before + __shfl_sync(0xffffffffu, sq.sum, which) - units) * lanes;
-    const int item = (int)((pos - seq_first) / units);
-    const int64_t first = seq_first + (int64_t)item * units;  // the item's first unit
+    const int head = (int)((pos - seq_first) / units);
+    const int64_t first = seq_first + (int64_t)head * units;  // the item's first unit
     const int from = (int)(pos - first), to = (int)min((int64_t)units, from + (end - pos));
-    const int u0 = max(from - setup, 0), u1 = to - setup;  // units of keys
+    const int u0 = max(from - kSetup, 0), u1 = to - kSetup;  // units of keys
     pos += to - from;
-    const int head = item / p.row_tiles, tile = item - head * p.row_tiles;
-    const int rows = min(ROWS, p.nodes * p.group - tile * ROWS);
     const int k_begin = u0 * kUnit, k_end = min(u1 * kUnit, keys);
 
     if (keys == 0 && from == 0) {  // nothing to see: the item's first CTA writes its zeros
       for (int i = threadIdx.x; i < rows * DIM; i += 32 * W) {
-        const int lr = i / DIM, e = i % DIM, gr = tile * ROWS + lr, node = gr / p.group;
-        const int h = head * p.group + gr - node * p.group;
+        const int lr = i / DIM, e = i % DIM, node = lr / p.group, h = head * p.group + lr - node * p.group;
         const int64_t at = seq * p.o_seq + node * p.o_node + h * p.o_head + e;
         if (p.out_f32) static_cast<float*>(p.out)[at] = 0.f;
         else static_cast<__half*>(p.out)[at] = __ushort_as_half(0);
@@ -196,8 +195,8 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
     float q128[NT][2];           // INT8: 128 sum q of rows 2 t and 2 t + 1
     uint32_t q_sums[INT4 ? NT : 1];  // INT4: sum q / 32 over group t of row g, in two parts
     auto load_q = [&](int nt, uint32_t (&b)[KS][2]) {
-      const int lr = nt * 8 + g, gr = tile * ROWS + lr, node = gr / p.group;
-      const __half* row = p.q + seq * p.q_seq + node * p.q_node + (int64_t)(head * p.group + gr - node * p.group) * p.q_head;
+      const int lr = nt * 8 + g, node = lr / p.group;
+      const __half* row = p.q + seq * p.q_seq + node * p.q_node + (int64_t)(head * p.group + lr - node * p.group) * p.q_head;
       float sum[GROUPS];
 #pragma unroll
       for (int c = 0; c < GROUPS; ++c) sum[c] = 0.f;
@@ -360,7 +359,7 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
             const int lr = nt * 8 + 2 * t + i;
             uint64_t bits = 0;
             if (lr < rows) {
-              const int node = (tile * ROWS + lr) / p.group;
+              const int node = lr / p.group;
               if (p.mask == nullptr) {
                 bits = (2ull << node) - 1;
               } else {
@@ -619,12 +618,12 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
       return (int)(u < large ? u / (per + 1) : more + (u - large) / per);
     };
     int c0 = 0, c1 = 0;
-    if (!whole) c0 = holder(first + setup), c1 = holder(first + units - 1);
+    if (!whole) c0 = holder(first + kSetup), c1 = holder(first + units - 1);
     auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * S::PART; };
     float* part = part_of(blockIdx.x);
     const int live_nodes = node_count(p, seq);
     auto finish = [&](int lr, int e, float mx, float sum, float4 acc) {
-      const int gr = tile * ROWS + lr, node = gr / p.group, h = head * p.group + gr - node * p.group;
+      const int node = lr / p.group, h = head * p.group + lr - node * p.group;
       const bool live = node < live_nodes && sum != 0.f;
       const float f = live ? 1.f / sum : 0.f;
       const float4 y = live ? make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -710,14 +709,14 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
 
 int fail(int code, const std::string& msg) { return set_error(code, "af1_tree_attention: " + msg); }
 
-// Blocks of 8 rows (of every query head and node that share a cached head) of
-// a CTA; 0: the tensor-core kernel, whose products have 128 rows. Up to 32
-// rows it pays to go over the keys again for the second 16: 4 sequences of up
-// to 6001 tokens with 20 rows of E4M3 take 31 us here and 42 there, 32 rows of
-// INT8 33 and 38; 64 rows of E4M3 46 and 42, 256 rows of INT8 over 8000 tokens
-// 64 and 46. (Blocks of 32 rows, which leave an SM 8 warps, took 36, 41 and 56
-// for the first three.)
-int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 32 ? 2 : 0; }
+// Blocks of 8 rows (of every query head and node that share a cached head) that
+// a CTA has; 0: the tensor-core kernel, whose products have 128 rows. Going
+// over the keys again for 16 rows more did not pay: 4 sequences of up to 6001
+// tokens with 20 rows of E4M3 took 32 us and 31 there, 24 of INT4 32 and 26, 32
+// of FP16 33 and 28, of INT8 33 and 32; 64 of E4M3 47 and 33. (32 short
+// sequences of 32 rows of INT8 42 and 46.) Blocks of 32 rows, which leave an
+// SM 8 warps, were no better.
+int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 0; }
 
 int64_t workspace_bytes(const af1_kv_cache& c, int64_t rows) {
   if (row_blocks(rows) == 0) return kPartOffset + tree_wide_part_bytes(c);
@@ -829,7 +828,6 @@ int af1_tree_attention(const af1_kv_cache* c, const af1_tree_args* a, void* work
   p.pages = {a->pages, a->pages_ld, (int)a->sequences, (int)a->page_columns};
   p.lens = a->lens, p.counts = a->counts, p.mask = a->mask, p.mask_seq = a->mask_seq;
   p.nodes = (int)a->nodes, p.group = group, p.words = (int)(a->nodes + 31) / 32;
-  p.row_tiles = nt > 0 ? (int)((rows + 8 * nt - 1) / (8 * nt)) : 0;
   p.scale_log2 = a->scale * 1.4426950408889634f;
   p.out_f32 = a->out_dtype == AF1_F32;
   p.counters = reinterpret_cast<unsigned*>(static_cast<uint8_t*>(workspace) + kCounterOffset);

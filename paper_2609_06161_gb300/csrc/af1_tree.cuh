@@ -233,15 +233,15 @@ static __device__ __forceinline__ int node_count(const TreeProblem& p, int seq) 
 }
 
 // 32 sequences at a time, one to a lane: their lengths, and their units (of
-// one cached head and row block) summed up, `setup` of them before the first
-// key of an item.
-template <int UNIT>
+// one cached head and row block) summed up, SETUP of them before the first key
+// of an item: what a run of its keys costs whatever its length, in a CTA.
+template <int UNIT, int SETUP>
 struct Sequences {
   int first;      // of the 32
   int64_t before; // units of the sequences before them
   int len, keys, units, sum;
 
-  __device__ __forceinline__ void load(const TreeProblem& p, int at, int64_t units_before, int setup) {
+  __device__ __forceinline__ void load(const TreeProblem& p, int at, int64_t units_before) {
     const int lane = threadIdx.x % 32, i = at + lane;
     first = at;
     before = units_before;
@@ -249,7 +249,7 @@ struct Sequences {
     if (i < p.pages.seqs) {
       len = max(p.lens[i], 0);
       keys = (int)min((int64_t)len + node_count(p, i), (int64_t)p.pages.columns << p.cache.shift);
-      units = setup + (keys + UNIT - 1) / UNIT;
+      units = SETUP + (keys + UNIT - 1) / UNIT;
     }
     sum = units;
 #pragma unroll
@@ -260,30 +260,20 @@ struct Sequences {
   }
   __device__ __forceinline__ int64_t after() const { return before + __shfl_sync(0xffffffffu, sum, 31); }
 
-  // The first 32 sequences, and all items' units (for each sequence `lanes`
-  // items). An item's setup is what a run costs whatever its length, `most`
-  // units, where CTAs have several times that to do; where they have less it
-  // goes down to `least`, as the CTAs that would get nothing else are worth more.
-  __device__ __forceinline__ int64_t begin(const TreeProblem& p, int64_t lanes, int least, int most, int& setup) {
-    load(p, 0, 0, 0);
+  // The first 32 sequences, and the units of all.
+  __device__ __forceinline__ int64_t begin(const TreeProblem& p) {
+    load(p, 0, 0);
     int64_t total = after();
     for (int at = 32; at < p.pages.seqs; at += 32) {
-      load(p, at, total, 0);
+      load(p, at, total);
       total = after();
     }
-    setup = (int)max((int64_t)least, min((int64_t)most, total * lanes / (4 * (int64_t)gridDim.x)));
-    if (p.pages.seqs > 32) {
-      load(p, 0, 0, setup);
-    } else {
-      const int lane = threadIdx.x % 32;
-      if (lane < p.pages.seqs) units += setup;
-      sum += setup * min(lane + 1, p.pages.seqs);
-    }
-    return (total + (int64_t)setup * p.pages.seqs) * lanes;
+    if (p.pages.seqs > 32) load(p, 0, 0);
+    return total;
   }
 };
 
-// The tensor-core kernel for more than 32 rows to a cached head
+// The tensor-core kernel for more than 16 rows to a cached head
 // (af1_tree_wide.cu): its workspace bytes, and its launch.
 int64_t tree_wide_part_bytes(const af1_kv_cache& c);
 cudaError_t launch_tree_wide(TreeProblem& p, const af1_kv_cache& c, int rows, cudaStream_t st);

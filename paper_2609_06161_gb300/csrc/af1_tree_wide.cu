@@ -1,5 +1,5 @@
 // af1_tree_wide.cu — attention of drafted tokens over the paged cache where
-// more than 32 rows (nodes times query heads) share a cached head: the same
+// more than 16 rows (nodes times query heads) share a cached head: the same
 // operator as af1_tree.cu, with tcgen05 products of 128 rows.
 //
 // An item is one sequence, one cached head and a block of 128 rows; its keys
@@ -40,10 +40,11 @@
 //
 // Bound: issue slots. With all 128 rows in use a tile's exponents take 1024
 // cycles (16 a cycle), its products 512, its decoding and the five
-// instructions beside each exponent the rest: 1.45 us a tile, 95 us for a tree
-// of 64 nodes and 8 queries to a head over 32768 INT4 tokens of 8 heads (720
-// TFLOP/s). Few tiles to a CTA are bound by what a run costs once: 4 trees of 16
-// over 6001 E4M3 tokens take 41 us.
+// instructions beside each exponent the rest: 1.3 us a tile, 91 us for a tree
+// of 64 nodes and 8 queries to a head over 32768 INT4 tokens of 8 heads (755
+// TFLOP/s). Where CTAs have few tiles, it is what a run costs once (first pages,
+// keys and q 6 us, the first tile 2, join 5 to 10): 4 trees of 16 over 6001
+// E4M3 tokens take 32 us.
 // All waits are bounded; a wait that gives up sets the status word, and what
 // depends on it is skipped.
 #include "af1_tree.cuh"
@@ -53,7 +54,10 @@ namespace {
 
 constexpr int BK = 128;        // keys of a tile
 constexpr int kThreads = 640;
-constexpr int kSetupTiles = 4; // tiles that a run's beginning and end are worth, at most
+// Tiles that a run's beginning and end are worth. (With 2, 4 trees of 16 over
+// 6001 E4M3 tokens took 40 us instead of 32, one over 20000 tokens 63 instead of
+// 40; with 8, 33 and 40.)
+constexpr int kSetupTiles = 5;
 constexpr int kRows = 128;
 constexpr int kOutAt = 2 * BK, kWeightsAt = 3 * BK;  // columns of tensor memory, behind two tiles of scores
 constexpr int kSlots = 2;      // operand tiles of keys, and of values
@@ -73,8 +77,15 @@ struct Wide {
   static constexpr int K_BYTES = CODES + SCALES, V_BYTES = CODES + (C::SCALED8 ? 0 : SCALES);
   static constexpr int RINGS = F16 ? 0 : K_STAGES * K_BYTES + V_STAGES * V_BYTES;
   static constexpr int SMEM = (2 * kSlots + 1) * OP + RINGS + 2 * kNotes * BK * 4 + 1024;
-  static constexpr int PART = kRows * (DIM + 2);  // floats: o, m, l, each along the rows
+  static constexpr int PART = kRows * (DIM + 2);  // floats: o, m, l, each along the rows (to a multiple of 4 of them)
+  static constexpr int COPIES = 10 * DIM / 8 * 16;  // bytes of a part for 4 rows, as it is joined
+  static_assert(2 * COPIES * (kRows / 4) <= SMEM - 1024, "two parts are on their way");
 };
+
+// 16 bytes to shared memory, as part of the thread's next group of copies.
+__device__ __forceinline__ void copy16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
 
 struct Plan {
   int64_t per, more, end;  // units of a CTA, the CTAs with one more, and where this one's end
@@ -89,8 +100,8 @@ struct Barriers {
   uint32_t code_bad[2][2], tile_bad[kNotes];   // bits: 16 keys each whose page is missing
   uint32_t nodes_bad[4][2];                 // by run that has keys: nodes whose value is not finite (values are
                                             // decoded at most two tiles, so two such runs, ahead of their use)
-  float top[2][2][kRows], sum[2][kRows];    // of the halves of a tile (by tile), and of a run
-  float value_top[kNotes][4];                    // by tile and warp: power of two above the values' scales
+  alignas(16) float top[2][2][kRows], sum[2][kRows];    // of the halves of a tile (by tile), and of a run
+  alignas(16) float value_top[kNotes][4];        // by tile and warp: power of two above the values' scales
   // Parts of items that this CTA has left: of its first and of its last run.
   struct {
     int c0, c1, seq, head, tile, rows;
@@ -102,14 +113,13 @@ struct Barriers {
 // The runs of this CTA, one after another, known to every warp. What stays the
 // same lies in shared memory: every thread of the softmax needs its registers.
 struct Runs {
-  Sequences<BK> sq;
-  int setup;
+  Sequences<BK, kSetupTiles> sq;
   int64_t pos, first;
   int seq, head, tile, len, keys, units, from, to, k_begin, k_end, tiles;
 
   __device__ __forceinline__ bool begin(const TreeProblem& p, Plan& plan) {
     const int64_t lanes = (int64_t)p.cache.heads * p.row_tiles;
-    const int64_t total = sq.begin(p, lanes, kSetupTiles / 2, kSetupTiles, setup);
+    const int64_t total = sq.begin(p) * lanes;
     const int64_t ctas = min((int64_t)gridDim.x, total);
     if (blockIdx.x >= ctas) return false;
     const int64_t per = total / ctas, more = total - per * ctas;
@@ -122,7 +132,7 @@ struct Runs {
     const int64_t end = plan.end;
     if (pos >= end) return false;
     const int64_t lanes = (int64_t)p.cache.heads * p.row_tiles;
-    while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after(), setup);
+    while (sq.after() * lanes <= pos) sq.load(p, sq.first + 32, sq.after());
     const int which = __popc(__ballot_sync(0xffffffffu, (sq.before + sq.sum) * lanes <= pos));
     seq = sq.first + which;
     units = __shfl_sync(0xffffffffu, sq.units, which);
@@ -136,7 +146,7 @@ struct Runs {
     pos += to - from;
     head = item / p.row_tiles;
     tile = item - head * p.row_tiles;
-    const int u0 = max(from - setup, 0), u1 = to - setup;
+    const int u0 = max(from - kSetupTiles, 0), u1 = to - kSetupTiles;
     k_begin = u0 * BK, k_end = min(u1 * BK, keys);
     tiles = max(u1 - u0, 0);
     return true;
@@ -145,6 +155,8 @@ struct Runs {
     return min(kRows, p.nodes * p.group - tile * kRows);
   }
 };
+
+__device__ __forceinline__ int part_ld(int rows) { return (rows + 3) & ~3; }
 
 // The CTA that has unit u.
 __device__ __forceinline__ int holder(const volatile Plan& plan, int64_t u) {
@@ -202,8 +214,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// 32 columns of this thread's row.
-__device__ __forceinline__ void tmem_load(uint32_t addr, float (&x)[32]) {
+// 32 columns of this thread's row; `meanwhile` runs before they are waited for.
+template <typename F>
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&x)[32], F meanwhile) {
   uint32_t r[32];
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
@@ -214,17 +227,40 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, float (&x)[32]) {
         "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr)
       : "memory");
+  meanwhile();
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
   for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&x)[32]) {
+  tmem_load(addr, x, [] {});
+}
+template <typename F>
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&x)[16], F meanwhile) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr)
+      : "memory");
+  meanwhile();
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
           addr),
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -567,25 +603,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       if (n == 0) continue;
       uint64_t bits = 0;
       {
-        // q of this run (the products with the one before are done); a negative
-        // scale turns its signs.
         int node, head;
         place(node, head);
-        const __half* q = p.q + run.seq * p.q_seq + node * p.q_node + (int64_t)head * p.q_head;
-        const uint32_t sign = p.scale_log2 < 0.f ? 0x80008000u : 0u;
-#pragma unroll 4
-        for (int c = half * (DIM / 16); c < (half + 1) * (DIM / 16); ++c) {
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (real) v = *reinterpret_cast<const uint4*>(q + 8 * c);
-          if constexpr (INT4)
-            v = make_uint4(prmt(v.x, v.z, 0x5410), prmt(v.x, v.z, 0x7632), prmt(v.y, v.w, 0x5410),
-                           prmt(v.y, v.w, 0x7632));
-          v.x ^= sign, v.y ^= sign, v.z ^= sign, v.w ^= sign;
-          *reinterpret_cast<uint4*>(qt + (c >> 3) * (BK * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
-        }
-        fence_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar.q_ready);
         if (real) {
           if (p.mask == nullptr) {
             bits = (2ull << node) - 1;
@@ -594,6 +613,32 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             bits = w[0] | (p.words > 1 ? (uint64_t)w[1] << 32 : 0);
           }
         }
+        // q of this run (the products with the one before are done), whole rows at
+        // a time; a negative scale turns its signs.
+        constexpr int CHUNKS = DIM / 8, N = 16 * CHUNKS / 32;
+        const uint32_t sign = p.scale_log2 < 0.f ? 0x80008000u : 0u;
+        const int c = lane % CHUNKS, r0 = warp * 16 + lane / CHUNKS;
+        uint4 v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int r = r0 + i * (32 / CHUNKS), gr = run.tile * kRows + r, of = gr / p.group;
+          v[i] = make_uint4(0, 0, 0, 0);
+          if (r < rows)
+            v[i] = *reinterpret_cast<const uint4*>(p.q + run.seq * p.q_seq + of * p.q_node +
+                                                   (int64_t)(run.head * p.group + gr - of * p.group) * p.q_head + 8 * c);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int r = r0 + i * (32 / CHUNKS);
+          if constexpr (INT4)
+            v[i] = make_uint4(prmt(v[i].x, v[i].z, 0x5410), prmt(v[i].x, v[i].z, 0x7632),
+                              prmt(v[i].y, v[i].w, 0x5410), prmt(v[i].y, v[i].w, 0x7632));
+          v[i].x ^= sign, v[i].y ^= sign, v[i].z ^= sign, v[i].w ^= sign;
+          *reinterpret_cast<uint4*>(qt + (c >> 3) * (BK * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[i];
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar.q_ready);
       }
       const bool warp_real = (warp % 4) * 32 < rows;
       // Weights are 2^(score - m - ev + kShift), times a value's scale, which is below 2^ev.
@@ -607,6 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         ok = __all_sync(0xffffffffu, ok);
         const uint32_t scores = base + buf * BK + half * (BK / 2);
         const int c_first = half * (BK / 2);  // column of the tile
+        constexpr int COLS = C::SCALED8 ? 16 : 32;  // at a time: as many as the registers hold, with their scales
         const int at_tile = at % kNotes;
         const bool work = ok && warp_real;
         const uint32_t bad = bar.tile_bad[at_tile];
@@ -614,7 +660,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         const float* ks = key_scale + at_tile * BK + c_first;
         const float* vs = value_scale + at_tile * BK + c_first;
         float top = -kInf;
-        auto hide = [&](int c, float (&x)[32]) {  // -infinity where the row does not see
+        auto hide = [&](int c, float (&x)[COLS]) {  // -infinity where the row does not see
           auto low = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; };  // n columns
           const int k0 = key + c_first + c, d = k0 - run.len;  // the first column's key, and node
           uint32_t sees = low(-d);
@@ -624,7 +670,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           if (bad >> ((c_first + c) / 16) & 1) sees &= 0xffff0000u;
           if (bad >> ((c_first + c) / 16) & 2) sees &= 0x0000ffffu;
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
+          for (int i = 0; i < COLS; ++i)
             if (!(sees >> i & 1)) x[i] = -kInf;
         };
         // The half's weights relative to `ref`, and its largest score.
@@ -632,26 +678,35 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         auto pass = [&](float ref) {
           sum = make_float2(0.f, 0.f);
 #pragma unroll 1
-          for (int c = 0; c < BK / 2; c += 32) {
-            float x[32];
-            tmem_load(scores + c, x);
+          for (int c = 0; c < BK / 2; c += COLS) {
+            float x[COLS];
+            float4 f8[COLS / 4];
+            auto fetch = [&](const float* from) {  // here, not one by one where they are used
+              if constexpr (C::SCALED8) {
+#pragma unroll
+                for (int i = 0; i < COLS / 4; ++i) f8[i] = *reinterpret_cast<const float4*>(from + c + 4 * i);
+                asm volatile("" ::: "memory");
+              }
+            };
+            tmem_load(scores + c, x, [&] { fetch(ks); });
             if constexpr (C::SCALED8) {
 #pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                const float4 f = *reinterpret_cast<const float4*>(ks + c + i);
+              for (int i = 0; i < COLS; i += 4) {
+                const float4 f = f8[i / 4];
                 const float2 a = mul2(make_float2(x[i], x[i + 1]), make_float2(f.x, f.y));
                 const float2 b = mul2(make_float2(x[i + 2], x[i + 3]), make_float2(f.z, f.w));
                 x[i] = a.x, x[i + 1] = a.y, x[i + 2] = b.x, x[i + 3] = b.y;
               }
+              fetch(vs);
             }
             if (masked) hide(c, x);
             float t0 = x[0], t1 = x[1];
 #pragma unroll
-            for (int i = 2; i < 30; i += 4) t0 = max3(t0, x[i], x[i + 1]), t1 = max3(t1, x[i + 2], x[i + 3]);
-            top = max3(top, max3(t0, x[30], x[31]), t1);
-            uint32_t r[16];
+            for (int i = 2; i < COLS - 2; i += 4) t0 = max3(t0, x[i], x[i + 1]), t1 = max3(t1, x[i + 2], x[i + 3]);
+            top = max3(top, max3(t0, x[COLS - 2], x[COLS - 1]), t1);
+            uint32_t r[COLS / 2];
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
+            for (int i = 0; i < COLS; i += 4) {
               float2 a = make_float2(x[i], x[i + 1]), b = make_float2(x[i + 2], x[i + 3]);
               const float2 minus = make_float2(-ref, -ref);
               if constexpr (C::SCALED8) a = add2(a, minus), b = add2(b, minus);
@@ -659,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
               a = make_float2(ex2(a.x), ex2(a.y)), b = make_float2(ex2(b.x), ex2(b.y));
               sum = add2(sum, add2(a, b));
               if constexpr (C::SCALED8) {
-                const float4 f = *reinterpret_cast<const float4*>(vs + c + i);
+                const float4 f = f8[i / 4];
                 const float2 wa = mul2(a, make_float2(f.x, f.y)), wb = mul2(b, make_float2(f.z, f.w));
                 if (masked) {  // 0 times any scale is 0
                   a.x = a.x == 0.f ? 0.f : wa.x, a.y = a.y == 0.f ? 0.f : wa.y;
@@ -670,7 +725,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
               }
               r[i / 2] = pack_half2(a.x, a.y), r[i / 2 + 1] = pack_half2(b.x, b.y);
             }
-            tmem_store16(base + kWeightsAt + buf * (BK / 2) + (c_first + c) / 2, r);
+            tmem_store(base + kWeightsAt + buf * (BK / 2) + (c_first + c) / 2, r);
           }
           tmem_wait_store();
         };
@@ -681,16 +736,18 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           pass(reference());
           if constexpr (!C::SCALED8) top *= scale;
         }
+        float ev_now = ev;
+        if constexpr (C::SCALED8) {
+          const float4 most = *reinterpret_cast<const float4*>(bar.value_top[at_tile]);
+          const float tile_top = fmaxf(fmaxf(most.x, most.y), fmaxf(most.z, most.w));
+          if (tile_top > ev) ev_now = tile_top + 1.f;  // with room, as moving costs as much as a tile
+        }
+        // The two warps that have these rows agree.
         bar.top[buf][half][row] = top;
-        named_sync(2, 256);
+        named_sync(2 + warp % 4, 64);
         top = fmaxf(top, bar.top[buf][half ^ 1][row]);
-        if (work) {
-          float ev_now = ev;
-          if constexpr (C::SCALED8) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) ev_now = fmaxf(ev_now, bar.value_top[at_tile][i]);
-          }
-          if (__any_sync(0xffffffffu, top > m + kSlack || ev_now > ev)) {
+        if (__any_sync(0xffffffffu, work && (top > m + kSlack || ev_now > ev))) {
+          if (work) {
             const float now = fmaxf(m, top);
             const float alpha = ex2(m - (now == -kInf ? 0.f : now) + (ev - ev_now));
             m = now, ev = ev_now;
@@ -708,14 +765,14 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 for (int hf = 0; hf < 2; ++hf) {
 #pragma unroll
                   for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(x[16 * hf + i] * alpha);
-                  tmem_store16(base + kOutAt + c + 16 * hf, r);
+                  tmem_store(base + kOutAt + c + 16 * hf, r);
                 }
               }
             }
             pass(reference());
           }
-          l += sum.x + sum.y;
         }
+        if (work) l += sum.x + sum.y;
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bar.p_ready[buf]);
@@ -730,13 +787,13 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         ok = __all_sync(0xffffffffu, ok);
         const uint32_t* odd = bar.nodes_bad[runs_done % 4];
         const uint64_t poison = (odd[0] | (uint64_t)odd[1] << 32) & bits;
-        named_sync(2, 256);
+        named_sync(1, 256);
         if (threadIdx.x == 0) bar.nodes_bad[runs_done % 4][0] = bar.nodes_bad[runs_done % 4][1] = 0;
         const float sum = l + bar.sum[half ^ 1][row];
-        const bool whole = run.from <= run.setup && run.to == run.units;
+        const bool whole = run.from <= kSetupTiles && run.to == run.units;
         int c0 = 0, c1 = 0, node, head;
         if (!whole)
-          c0 = holder(bar.plan, run.first + run.setup), c1 = holder(bar.plan, run.first + run.units - 1);
+          c0 = holder(bar.plan, run.first + kSetupTiles), c1 = holder(bar.plan, run.first + run.units - 1);
         place(node, head);
         __half* out16 = static_cast<__half*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
         float* out32 = static_cast<float*>(p.out) + run.seq * p.o_seq + node * p.o_node + head * p.o_head;
@@ -796,11 +853,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
               }
             } else if (real) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) part[(c + i) * kRows + row] = x[i];
+              for (int i = 0; i < 32; ++i) part[(c + i) * part_ld(rows) + row] = x[i];
             }
           }
           if (real && half == 0) {
-            if (!whole) part[DIM * kRows + row] = m, part[(DIM + 1) * kRows + row] = sum;
+            if (!whole) part[DIM * part_ld(rows) + row] = m, part[(DIM + 1) * part_ld(rows) + row] = sum;
             else if (p.lse != nullptr)
               p.lse[((int64_t)run.seq * p.nodes + node) * p.cache.heads * p.group + head] = live && sum != 0.f ? (m - kShift + log2f(sum)) * 0.69314718056f : -kInf;
           }
@@ -814,8 +871,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   __syncthreads();
   fence_after();
   if (bar.gave_up && threadIdx.x == 0) atomicOr(p.status, kStatusTimeout);
-  // ---- items that span CTAs: the last CTA to arrive joins the parts, in order, all its
-  // threads at it (128 threads with a row each read 64 KB parts at 11 GB/s: 40 us)
+  // ---- items that span CTAs: the last CTA to arrive joins the parts, in order.
+  // A thread has 8 places of 4 rows, and copies them (and the rows' maxima and
+  // sums) to slots of its own in shared memory, whose tiles are used up, two or
+  // four parts ahead; the parts of this CTA's two items follow one another.
   if ((int)threadIdx.x < bar.parts) {  // the CTA's parts are released with it
     unsigned* counter = &p.counters[bar.part[threadIdx.x].c0];
     const unsigned others = bar.part[threadIdx.x].c1 - bar.part[threadIdx.x].c0;
@@ -824,53 +883,72 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     if (last) *counter = 0;  // as the next call finds it
   }
   __syncthreads();
+  int steps[2] = {0, 0}, quads[2] = {1, 1};
   for (int i = 0; i < bar.parts; ++i) {
-    const int c0 = bar.part[i].c0, c1 = bar.part[i].c1;
-    const int row0 = lane * 4, e0 = warp * 8;  // of this thread: 4 rows, 8 places
-    if (bar.last[i] && e0 < DIM && row0 < bar.part[i].rows) {
-      auto part_of = [&](int c) { return p.parts + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * S::PART; };
-      auto four = [&](const float* from, int e) { return __ldcg(reinterpret_cast<const float4*>(from + e * kRows + row0)); };
-      float top[4], total[4] = {0.f, 0.f, 0.f, 0.f}, acc[8][4];
+    if (bar.last[i]) steps[i] = bar.part[i].c1 - bar.part[i].c0 + 1;
+    quads[i] = part_ld(bar.part[i].rows) / 4;
+  }
+  const int most = steps[1] > 0 ? max(quads[0], quads[1]) : quads[0], ahead = most <= kRows / 8 ? 4 : 2;
+  auto slot = [&](int step, int which) {
+    return smem + ((step & (ahead - 1)) * 10 + which) * (DIM / 8 * 16 * most) + threadIdx.x * 16;
+  };
+  auto fetch = [&](int step) {
+    const int i = step >= steps[0], k = step - (i ? steps[0] : 0);
+    const int q = i ? quads[1] : quads[0], row0 = threadIdx.x % q * 4, e0 = threadIdx.x / q * 8;
+    if (k < (i ? steps[1] : steps[0]) && e0 < DIM) {
+      const float* from = p.parts + (int64_t)(2 * (bar.part[i].c0 + k) + (k == 0 ? 1 : 0)) * S::PART + row0;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        top[r] = -kInf;
+      for (int e = 0; e < 8; ++e) copy16(slot(step, e), from + (e0 + e) * (4 * q));
+      copy16(slot(step, 8), from + DIM * (4 * q));
+      copy16(slot(step, 9), from + (DIM + 1) * (4 * q));
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  for (int step = 0; step < (steps[0] + steps[1] > 0 ? ahead : 0); ++step) fetch(step);
+  for (int i = 0, step = 0; i < 2; ++i) {
+    const int q = i ? quads[1] : quads[0], row0 = threadIdx.x % q * 4, e0 = threadIdx.x / q * 8;
+    const int end = step + (i ? steps[1] : steps[0]);
+    if (step == end) continue;
+    float m[4], l[4], acc[8][4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e][r] = 0.f;
-      }
-      for (int c = c0; c <= c1; c += 4) {  // four parts' loads in flight
-        float4 m[4];
+    for (int r = 0; r < 4; ++r) {
+      m[r] = -kInf, l[r] = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) m[k] = four(part_of(min(c + k, c1)), DIM);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          top[0] = fmaxf(top[0], m[k].x), top[1] = fmaxf(top[1], m[k].y), top[2] = fmaxf(top[2], m[k].z),
-          top[3] = fmaxf(top[3], m[k].w);
-      }
-#pragma unroll 2
-      for (int c = c0; c <= c1; ++c) {
-        const float* from = part_of(c);
-        const float4 m = four(from, DIM), l = four(from, DIM + 1);
-        float4 x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = four(from, e0 + e);
-        const float mr[4] = {m.x, m.y, m.z, m.w}, lr[4] = {l.x, l.y, l.z, l.w};
+      for (int e = 0; e < 8; ++e) acc[e][r] = 0.f;
+    }
+    for (; step < end; ++step) {
+      if (ahead == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+      else asm volatile("cp.async.wait_group 1;" ::: "memory");
+      if (e0 < DIM) {
+        float part_m[4], part_l[4], a[4], b[4];
+        *reinterpret_cast<float4*>(part_m) = *reinterpret_cast<const float4*>(slot(step, 8));
+        *reinterpret_cast<float4*>(part_l) = *reinterpret_cast<const float4*>(slot(step, 9));
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float f = ex2(mr[r] - (top[r] == -kInf ? 0.f : top[r]));
-          total[r] = fmaf(f, lr[r], total[r]);
+          const float now = fmaxf(m[r], part_m[r]), zero = now == -kInf ? 0.f : now;
+          a[r] = ex2(m[r] - zero), b[r] = ex2(part_m[r] - zero);
+          l[r] = fmaf(b[r], part_l[r], l[r] * a[r]);
+          m[r] = now;
+        }
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            acc[e][r] = fmaf(f, r == 0 ? x[e].x : r == 1 ? x[e].y : r == 2 ? x[e].z : x[e].w, acc[e][r]);
+        for (int e = 0; e < 8; ++e) {
+          float y[4];
+          *reinterpret_cast<float4*>(y) = *reinterpret_cast<const float4*>(slot(step, e));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[e][r] = fmaf(b[r], y[r], acc[e][r] * a[r]);
         }
       }
+      fetch(step + ahead);
+    }
+    if (e0 < DIM) {
       const int seq = bar.part[i].seq, live_nodes = node_count(p, seq);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         if (row0 + r >= bar.part[i].rows) break;
         const int gr = bar.part[i].tile * kRows + row0 + r, node = gr / p.group;
         const int head = bar.part[i].head * p.group + gr - node * p.group;
-        const bool live = node < live_nodes && total[r] != 0.f;
-        const float inv = live ? 1.f / total[r] : 0.f;
+        const bool live = node < live_nodes && l[r] != 0.f;
+        const float inv = live ? 1.f / l[r] : 0.f;
         float y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[place_entry<KIND>(e)] = live ? acc[e][r] * inv : 0.f;
@@ -882,9 +960,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           *reinterpret_cast<uint4*>(static_cast<__half*>(p.out) + at) = make_uint4(
               pack_half2(y[0], y[1]), pack_half2(y[2], y[3]), pack_half2(y[4], y[5]), pack_half2(y[6], y[7]));
         }
-        if (warp == 0 && p.lse != nullptr)
+        if (e0 == 0 && p.lse != nullptr)
           p.lse[((int64_t)seq * p.nodes + node) * p.cache.heads * p.group + head] =
-              live ? (top[r] - kShift + log2f(total[r])) * 0.69314718056f : -kInf;
+              live ? (m[r] - kShift + log2f(l[r])) * 0.69314718056f : -kInf;
       }
     }
   }
