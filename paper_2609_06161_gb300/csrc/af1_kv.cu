@@ -9,7 +9,8 @@
 // The rotation of a pair is (a c - b s, b c + a s). Its products and sums are
 // rounded one by one (no fused multiply-add), as are the steps of the
 // quantiser, so that what a cache holds is a function of the inputs to the
-// bit, whichever launch wrote it.
+// bit, whichever launch wrote it. (Paired operations are used where no product
+// meets a sum: the assembler may fuse a paired product and sum.)
 #include <cudaTypedefs.h>
 #include <cuda_fp8.h>
 
@@ -20,6 +21,7 @@
 
 #include "af1_internal.h"
 #include "af1_kv.cuh"
+#include "af1_ptx.cuh"
 
 namespace af1 {
 namespace {
@@ -30,6 +32,17 @@ constexpr int kThreads = 256;
 constexpr float kRound = 12582912.f;  // 1.5 * 2^23
 constexpr float kTiny = 7.52316385e-37f;  // 2^-120: smaller scales are stored as 0
 
+// NaN if either is.
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float d;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ void from_f32(float& y, float x) { y = x; }
@@ -224,51 +237,48 @@ __device__ __forceinline__ void quantise(float (&x)[8], int lane, uint8_t* row, 
     for (int i = 0; i < 8; ++i) h[i] = __float2half_rn(x[i]), x[i] = __half2float(h[i]);
     if (keep) reinterpret_cast<uint4*>(row)[lane] = *reinterpret_cast<uint4*>(h);
   } else if constexpr (KIND == AF1_KV_INT4) {
+    // Infinities and NaN show in the extremes.
     float lo = x[0], hi = x[0];
-    bool bad = !(fabsf(x[0]) < __int_as_float(0x7f800000));
 #pragma unroll
-    for (int i = 1; i < 8; ++i) {
-      lo = fminf(lo, x[i]), hi = fmaxf(hi, x[i]);
-      bad |= !(fabsf(x[i]) < __int_as_float(0x7f800000));
-    }
+    for (int i = 1; i < 8; ++i) lo = min_nan(lo, x[i]), hi = max_nan(hi, x[i]);
 #pragma unroll
     for (int m = 1; m < 4; m <<= 1) {  // a group of 32 entries: 4 threads
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, m));
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, m));
-      bad |= (bool)__shfl_xor_sync(0xffffffffu, (int)bad, m);
+      lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, m));
+      hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, m));
     }
     __half hs = __float2half_rn(__fmul_rn(__fsub_rn(hi, lo), (float)(1.0 / 15.0)));
     __half hl = __float2half_rn(lo);
-    bad |= !(fabsf(__half2float(hs)) <= 65504.f) || !(fabsf(__half2float(hl)) <= 65504.f);
-    const __half nan = __ushort_as_half(0x7fff);
-    if (bad) hs = hl = nan;
+    const bool good = fabsf(__half2float(hs)) <= 65504.f && fabsf(__half2float(hl)) <= 65504.f;
+    if (!good) hs = hl = __ushort_as_half(0x7fff);
     const float s = __half2float(hs), l = __half2float(hl);
     const float inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
-    uint32_t codes = 0;
+    // A NaN scale makes every code 0: the maximum of NaN and 0 is 0.
+    float2 part[4];  // codes of entries 2 i and 2 i + 1
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float q = fminf(fmaxf(__fmul_rn(__fsub_rn(x[i], l), inv), 0.f), 15.f);
-      const float r = __fadd_rn(bad ? 0.f : q, kRound);
-      codes |= (__float_as_uint(r) & 15u) << (4 * i);
-      x[i] = __fmaf_rn(__fsub_rn(r, kRound), s, l);
+    for (int i = 0; i < 4; ++i) {
+      const float2 q = mul2(add2(make_float2(x[2 * i], x[2 * i + 1]), make_float2(-l, -l)), make_float2(inv, inv));
+      const float2 r = add2(make_float2(fminf(fmaxf(q.x, 0.f), 15.f), fminf(fmaxf(q.y, 0.f), 15.f)),
+                            make_float2(kRound, kRound));
+      part[i] = add2(r, make_float2(-kRound, -kRound));
+      const float2 y = fma2(part[i], make_float2(s, s), make_float2(l, l));
+      x[2 * i] = y.x, x[2 * i + 1] = y.y;
     }
+    // Four codes as one whole number, below 2^16.
+    auto four = [](const float2& a, const float2& b) {
+      return __float_as_uint(fmaf(b.y, 4096.f, fmaf(b.x, 256.f, fmaf(a.y, 16.f, a.x))) + kRound);
+    };
+    const uint32_t codes = __byte_perm(four(part[0], part[1]), four(part[2], part[3]), 0x5410);
     if (keep) {
       reinterpret_cast<uint32_t*>(row)[lane] = codes;
       if (lane % 4 == 0) static_cast<__half2*>(scale)[lane / 4] = __halves2half2(hs, hl);
     }
   } else {
-    float top = 0.f;
-    bool bad = false;
+    float top = 0.f;  // infinities and NaN show in it
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      top = fmaxf(top, fabsf(x[i]));
-      bad |= !(fabsf(x[i]) < __int_as_float(0x7f800000));
-    }
+    for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(x[i]));
 #pragma unroll
-    for (int m = 1; m < LANES; m <<= 1) {
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-      bad |= (bool)__shfl_xor_sync(0xffffffffu, (int)bad, m);
-    }
+    for (int m = 1; m < LANES; m <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, m));
+    const bool bad = !(top < __int_as_float(0x7f800000));
     float s = __fmul_rn(top, (float)(1.0 / (KIND == AF1_KV_INT8 ? 127.0 : 448.0)));
     if (s < kTiny) s = 0.f;
     const float inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
@@ -276,17 +286,19 @@ __device__ __forceinline__ void quantise(float (&x)[8], int lane, uint8_t* row, 
     alignas(8) uint8_t codes[8];
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      const float q0 = bad ? 0.f : __fmul_rn(x[i], inv), q1 = bad ? 0.f : __fmul_rn(x[i + 1], inv);
+      const float2 q = bad ? make_float2(0.f, 0.f) : make_float2(__fmul_rn(x[i], inv), __fmul_rn(x[i + 1], inv));
       if constexpr (KIND == AF1_KV_INT8) {
-        const float r0 = __fadd_rn(fminf(fmaxf(q0, -127.f), 127.f), kRound);
-        const float r1 = __fadd_rn(fminf(fmaxf(q1, -127.f), 127.f), kRound);
-        codes[i] = (uint8_t)__float_as_uint(r0), codes[i + 1] = (uint8_t)__float_as_uint(r1);
-        x[i] = __fmul_rn(__fsub_rn(r0, kRound), s), x[i + 1] = __fmul_rn(__fsub_rn(r1, kRound), s);
+        // |q| <= 127 (1 + 2^-22), which rounds to 127: no clamp.
+        const float2 r = add2(q, make_float2(kRound, kRound));
+        codes[i] = (uint8_t)__float_as_uint(r.x), codes[i + 1] = (uint8_t)__float_as_uint(r.y);
+        const float2 y = mul2(add2(r, make_float2(-kRound, -kRound)), make_float2(s, s));
+        x[i] = y.x, x[i + 1] = y.y;
       } else {
-        const __nv_fp8x2_storage_t c = __nv_cvt_float2_to_fp8x2(make_float2(q0, q1), __NV_SATFINITE, __NV_E4M3);
+        const __nv_fp8x2_storage_t c = __nv_cvt_float2_to_fp8x2(q, __NV_SATFINITE, __NV_E4M3);
         *reinterpret_cast<__nv_fp8x2_storage_t*>(codes + i) = c;
         const float2 y = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(c, __NV_E4M3)));
-        x[i] = __fmul_rn(y.x, s), x[i + 1] = __fmul_rn(y.y, s);
+        const float2 z = mul2(y, make_float2(s, s));
+        x[i] = z.x, x[i + 1] = z.y;
       }
     }
     if (keep) {
@@ -373,6 +385,10 @@ __global__ void __launch_bounds__(kThreads, 4) append_kernel(const __grid_consta
       for (int i = 0; i < 4; ++i) c[i] = c4[i], s[i] = s4[i];
     } else if constexpr (VEC) {
       load_turn<true>(c, s, p.table, p.length, half, pos, first ? at : at - half);
+      if (first) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = -s[i];
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < (IL ? 4 : 8); ++i) {
@@ -439,11 +455,14 @@ __global__ void __launch_bounds__(kThreads, 4) append_kernel(const __grid_consta
           x[2 * i] = __fsub_rn(__fmul_rn(a, c[i]), __fmul_rn(b, s[i]));
           x[2 * i + 1] = __fadd_rn(__fmul_rn(b, c[i]), __fmul_rn(a, s[i]));
         }
+      } else if constexpr (VEC) {  // s has the sign of its part
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __fadd_rn(__fmul_rn(x[i], c[i]), __fmul_rn(y[i], s[i]));
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if (!VEC && at + i >= 2 * half) break;
-          const bool low = VEC ? first : at + i < half;
+          if (at + i >= 2 * half) break;
+          const bool low = at + i < half;
           x[i] = low ? __fsub_rn(__fmul_rn(x[i], c[i]), __fmul_rn(y[i], s[i]))
                      : __fadd_rn(__fmul_rn(x[i], c[i]), __fmul_rn(y[i], s[i]));
         }
