@@ -124,72 +124,96 @@ struct RopeProblem {
   const float* table;   // nullptr: copy
   int64_t length, x_token, x_head, y_token, y_head;
   int heads, half, units, pairs_units;  // units of a head: pairs_units of VP pairs, then copies of 2 VP entries
-  int64_t total;                        // tokens * heads * units
+  int groups;                           // of heads that a thread takes together
+  int64_t total;                        // tokens * groups * units
   bool back;
 };
 
-// One unit: VP pairs of a head, or 2 VP entries that are only copied. A
-// thread owns both entries of its pairs, so that y may be x.
-template <typename TI, typename TO, int VP, bool IL>
+// One unit of TAKE heads of a token, which share its turns and whose entries
+// are on their way together: VP pairs of each, or 2 VP entries that are only
+// copied. A thread owns both entries of its pairs, so that y may be x. Beside
+// the keys and values of an append, which leave an SM 1024 threads, four heads
+// to a thread take 39 us where one takes 61 (8192 tokens, 32 heads of q, 8 of k
+// and v); alone, with twice the threads, one takes 13 us and four 15 (2048 tokens
+// x 32 x 128 FP32).
+constexpr int kAppendTake = 4;
+template <typename TI, typename TO, int VP, bool IL, int TAKE>
 __device__ __forceinline__ void rope_unit(const RopeProblem& p, int64_t id) {
   const int64_t row = id / p.units;
   const int u = (int)(id - row * p.units);
-  const int64_t token = row / p.heads;
-  const int head = (int)(row - token * p.heads);
+  const int64_t token = row / p.groups;
+  const int head = (int)(row - token * p.groups) * TAKE, heads = min(TAKE, p.heads - head);
   const TI* x = static_cast<const TI*>(p.x) + token * p.x_token + head * p.x_head;
   TO* y = static_cast<TO*>(p.y) + token * p.y_token + head * p.y_head;
   constexpr bool VEC = VP > 1;
   const bool pad = p.slot != nullptr && p.slot[token] < 0;
-  if (u >= p.pairs_units) {
-    const int at = 2 * p.half + (u - p.pairs_units) * 2 * VP;
-    float a[2 * VP];
-    load<VEC>(a, x + at);
+  const bool turns = u < p.pairs_units;
+  // The unit's entries, in two halves of VP.
+  const int at = turns ? (IL ? u * 2 * VP : u * VP) : 2 * p.half + (u - p.pairs_units) * 2 * VP;
+  const int second = turns && !IL ? p.half : VP;
+  // As they stand: a conversion would wait for them before the turns are read.
+  struct alignas(VP * sizeof(TI)) Raw {
+    TI at[VP];
+  } first_raw[TAKE], second_raw[TAKE];
+#pragma unroll
+  for (int h = 0; h < TAKE; ++h) {
+    if (h >= heads) continue;
+    first_raw[h] = *reinterpret_cast<const Raw*>(x + h * p.x_head + at);
+    second_raw[h] = *reinterpret_cast<const Raw*>(x + h * p.x_head + at + second);
+  }
+  float a[TAKE][VP], b[TAKE][VP], c[VP], s[VP];
+  if (turns) load_turn<VEC>(c, s, p.table, p.length, p.half, pad ? 0 : p.positions[token], u * VP);
+#pragma unroll
+  for (int h = 0; h < TAKE; ++h)
+#pragma unroll
+    for (int i = 0; i < VP; ++i) a[h][i] = to_f32(first_raw[h].at[i]), b[h][i] = to_f32(second_raw[h].at[i]);
+  if (turns) {
+    if (p.back) {
+#pragma unroll
+      for (int i = 0; i < VP; ++i) s[i] = -s[i];
+    }
+#pragma unroll
+    for (int h = 0; h < TAKE; ++h) {
+      auto turn = [](float& first, float& other, float c, float s) {
+        const float f = first, o = other;
+        first = __fsub_rn(__fmul_rn(f, c), __fmul_rn(o, s));
+        other = __fadd_rn(__fmul_rn(o, c), __fmul_rn(f, s));
+      };
+      if constexpr (!IL) {
+#pragma unroll
+        for (int i = 0; i < VP; ++i) turn(a[h][i], b[h][i], c[i], s[i]);
+      } else if constexpr (VP == 1) {
+        turn(a[h][0], b[h][0], c[0], s[0]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VP; i += 2) {
+          turn(a[h][i], a[h][i + 1], c[i / 2], s[i / 2]);
+          turn(b[h][i], b[h][i + 1], c[(VP + i) / 2], s[(VP + i) / 2]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < TAKE; ++h) {
+    if (h >= heads) continue;
     if (pad) {
 #pragma unroll
-      for (int i = 0; i < 2 * VP; ++i) a[i] = 0.f;
+      for (int i = 0; i < VP; ++i) a[h][i] = b[h][i] = 0.f;
     }
-    store<VEC>(y + at, a);
-    return;
-  }
-  float a[VP], b[VP], c[VP], s[VP];
-  if constexpr (IL) {
-    float t[2 * VP];
-    load<VEC>(t, x + u * 2 * VP);
-#pragma unroll
-    for (int i = 0; i < VP; ++i) a[i] = t[2 * i], b[i] = t[2 * i + 1];
-  } else {
-    load<VEC>(a, x + u * VP);
-    load<VEC>(b, x + p.half + u * VP);
-  }
-  load_turn<VEC>(c, s, p.table, p.length, p.half, pad ? 0 : p.positions[token], u * VP);
-  float ya[VP], yb[VP];
-#pragma unroll
-  for (int i = 0; i < VP; ++i) {
-    const float si = p.back ? -s[i] : s[i];
-    ya[i] = __fsub_rn(__fmul_rn(a[i], c[i]), __fmul_rn(b[i], si));
-    yb[i] = __fadd_rn(__fmul_rn(b[i], c[i]), __fmul_rn(a[i], si));
-    if (pad) ya[i] = yb[i] = 0.f;
-  }
-  if constexpr (IL) {
-    float t[2 * VP];
-#pragma unroll
-    for (int i = 0; i < VP; ++i) t[2 * i] = ya[i], t[2 * i + 1] = yb[i];
-    store<VEC>(y + u * 2 * VP, t);
-  } else {
-    store<VEC>(y + u * VP, ya);
-    store<VEC>(y + p.half + u * VP, yb);
+    store<VEC>(y + h * p.y_head + at, a[h]);
+    store<VEC>(y + h * p.y_head + at + second, b[h]);
   }
 }
 
 template <typename T, int VP, bool IL>
 __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeProblem p) {
   const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (id < p.total) rope_unit<T, T, VP, IL>(p, id);
+  if (id < p.total) rope_unit<T, T, VP, IL, 1>(p, id);
 }
 
 // Units of a head, and whether 4 pairs to a thread fit the sizes, strides and
 // pointers (else one pair: any even rope_dim, any stride).
-bool plan_rope(RopeProblem& p, int64_t tokens, int dim, int rope_dim, size_t xs, size_t ys, bool il,
+bool plan_rope(RopeProblem& p, int take, int64_t tokens, int dim, int rope_dim, size_t xs, size_t ys, bool il,
                bool may = true) {
   const int per = il ? 8 : 4;  // entries of one vector access
   auto fits = [&](const void* q, int64_t a, int64_t b, size_t size) {
@@ -202,7 +226,8 @@ bool plan_rope(RopeProblem& p, int64_t tokens, int dim, int rope_dim, size_t xs,
   p.half = rope_dim / 2;
   p.pairs_units = p.half / vp;
   p.units = p.pairs_units + (dim - rope_dim) / (2 * vp);
-  p.total = tokens * p.heads * p.units;
+  p.groups = (p.heads + take - 1) / take;
+  p.total = tokens * p.groups * p.units;
   return vec;
 }
 
@@ -353,13 +378,14 @@ struct AppendProblem {
 // registers. The entries that a key's own are paired with lie in another
 // thread's part (or, interleaved, in its own) and are read beside them: the
 // second read hits L1, and no exchange between threads depends on rope_dim.
-// Bytes in flight bound it, hence the read ahead: 8192 tokens of 8 x 128 to
-// INT4, with the values back, take 22 us (28 without), 3.7 TB/s.
+// Issue slots and bytes in flight bound it: 8192 tokens of 8 x 128 to INT4, with
+// the values back, take 20 us, 4.0 TB/s (without reading ahead 6 us more; ahead
+// by two rounds, with the pairs by shuffles, 4 more).
 template <int KIND, int DIM, typename T, bool VEC, bool IL>
 __global__ void __launch_bounds__(kThreads, 4) append_kernel(const __grid_constant__ AppendProblem p) {
   if ((int)blockIdx.x >= p.kv_blocks) {
     const int64_t id = (int64_t)(blockIdx.x - p.kv_blocks) * kThreads + threadIdx.x;
-    if (id < p.q.total) rope_unit<T, __half, VEC ? 4 : 1, IL>(p.q, id);
+    if (id < p.q.total) rope_unit<T, __half, VEC ? 4 : 1, IL, kAppendTake>(p.q, id);
     return;
   }
   constexpr int LANES = DIM / 8;
@@ -752,7 +778,7 @@ int af1_rope(const af1_rope_args* a, void* stream) {
   RopeProblem p = {a->x, a->y, a->positions, nullptr, a->table, a->length, a->x_token, a->x_head, a->y_token, a->y_head};
   p.heads = (int)a->heads;
   p.back = (a->flags & AF1_ROPE_BACKWARD) != 0;
-  const bool vec = plan_rope(p, a->tokens, (int)a->dim, (int)a->rope_dim, es, es, il);
+  const bool vec = plan_rope(p, 1, a->tokens, (int)a->dim, (int)a->rope_dim, es, es, il);
   const int64_t blocks = (p.total + kThreads - 1) / kThreads;
   if (blocks > 0x7fffffff) return fail(AF1_ERR_INVALID_ARG, who, "too many entries for one call");
   return with_bool(vec, [&](auto v) {
@@ -892,7 +918,7 @@ int af1_kv_append(const af1_kv_cache* c, const af1_kv_append_args* a, void* stre
   p.tokens = a->tokens;
   // A thread takes several heads of its token (one turn for all of them) where
   // there are tokens enough to give every SM 1024 threads all the same: 8192
-  // tokens of 8 x 128 as INT4 with their values take 37 us with one head to a
+  // tokens of 8 x 128 as INT4 with their values took 37 us with one head to a
   // thread, 27 with two, 23 with four and 22 with eight.
   const int64_t threads = 2 * a->tokens * (dim / 8) * heads;
   const int take = (int)std::max<int64_t>(1, std::min<int64_t>(8, threads / (1024 * (int64_t)c->num_sms)));
@@ -914,7 +940,7 @@ int af1_kv_append(const af1_kv_cache* c, const af1_kv_append_args* a, void* stre
     p.q.table = a->table, p.q.length = a->length;
     p.q.x_token = a->q_token, p.q.x_head = a->q_head, p.q.y_token = a->qo_token, p.q.y_head = a->qo_head;
     p.q.heads = (int)a->q_heads;
-    vec = plan_rope(p.q, a->tokens, dim, 2 * p.half, es, 2, il, vec);
+    vec = plan_rope(p.q, kAppendTake, a->tokens, dim, 2 * p.half, es, 2, il, vec);
     q_blocks = (p.q.total + kThreads - 1) / kThreads;
   }
   if (kv_blocks + q_blocks > 0x7fffffff) return fail(AF1_ERR_INVALID_ARG, who, "too many entries for one call");
