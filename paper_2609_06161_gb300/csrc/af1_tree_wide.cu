@@ -38,11 +38,12 @@
 // value that is not finite is left out of the product (0 times it would reach
 // the rows that do not see it) and added to the rows that see it at the end.
 //
-// Bound: issue slots. With all 128 rows in use a tile's exponents take 1024
-// cycles (16 a cycle), its products 512, its decoding and the five
-// instructions beside each exponent the rest: 1.3 us a tile, 91 us for a tree
-// of 64 nodes and 8 queries to a head over 32768 INT4 tokens of 8 heads (755
-// TFLOP/s). Where CTAs have few tiles, it is what a run costs once (first pages,
+// Bound: a softmax warp's chain of steps for a tile (wait, read, exponents,
+// agree, arrive), which queue in shared memory behind the decoders' stores and
+// the products' operands. With all 128 rows in use a tile's exponents take 1024
+// cycles (16 a cycle), its products 1024; the chain takes 2700, 1.3 us: 91 us
+// for a tree of 64 nodes and 8 queries to a head over 32768 INT4 tokens of 8
+// heads (755 TFLOP/s; 0.66 of the issue slots, 0.37 of the tensor pipe). Where CTAs have few tiles, it is what a run costs once (first pages,
 // keys and q 6 us, the first tile 2, join 5 to 10): 4 trees of 16 over 6001
 // E4M3 tokens take 32 us.
 // All waits are bounded; a wait that gives up sets the status word, and what
