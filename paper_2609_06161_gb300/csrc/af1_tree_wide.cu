@@ -12,7 +12,7 @@
 // exponents of another. (Two streams of tiles, each with scores, weights and
 // output of its own, waited for one another's latencies: 115 us for trees of
 // 64 over 32768 INT4 tokens.)
-// Roles of the 20 warps:
+// Roles of the 19 warps:
 //   0-3, 4-7  softmax of the tile's first and second 64 keys: a thread has one
 //             row. The weights are formed relative to the maximum so far, and
 //             formed again (after O is scaled) only where a score of either
@@ -26,10 +26,11 @@
 //             of 32 entries, is rounded once to FP16, keys too: a score is off
 //             by about 2^-12 sqrt(sum (q k)^2). FP16 tiles arrive by TMA and
 //             are only looked at where a sequence ends;
-//   16, 19    TMA copies of keys, and of values, one for up to 128 rows of a
+//   16, 18    TMA copies of keys, and of values, one for up to 128 rows of a
 //             page, into the ring of codes (one warp for both took 0.65 us for
 //             each, which held up the decoders);
-//   17, 18    one lane each issues Q K^T, and P V.
+//   17        one lane issues the products. (A lane each for Q K^T and P V, and a
+//             wait more for the softmax, took 2 % longer.)
 // Keys and values each have a ring of codes and two operand tiles, with
 // barriers of their own: whoever waits on a barrier meets each of its phases in
 // turn, as a test of a phase's parity needs.
@@ -41,9 +42,9 @@
 // Bound: a softmax warp's chain of steps for a tile (wait, read, exponents,
 // agree, arrive), which queue in shared memory behind the decoders' stores and
 // the products' operands. With all 128 rows in use a tile's exponents take 1024
-// cycles (16 a cycle), its products 1024; the chain takes 2700, 1.3 us: 91 us
+// cycles (16 a cycle), its products 1024; the chain takes 2700, 1.3 us: 90 us
 // for a tree of 64 nodes and 8 queries to a head over 32768 INT4 tokens of 8
-// heads (755 TFLOP/s; 0.66 of the issue slots, 0.37 of the tensor pipe). Where CTAs have few tiles, it is what a run costs once (first pages,
+// heads (765 TFLOP/s; 0.66 of the issue slots, 0.37 of the tensor pipe). Where CTAs have few tiles, it is what a run costs once (first pages,
 // keys and q 6 us, the first tile 2, join 5 to 10): 4 trees of 16 over 6001
 // E4M3 tokens take 32 us.
 // All waits are bounded; a wait that gives up sets the status word, and what
@@ -54,7 +55,7 @@ namespace af1 {
 namespace {
 
 constexpr int BK = 128;        // keys of a tile
-constexpr int kThreads = 640;
+constexpr int kThreads = 608;
 // Tiles that a run's beginning and end are worth. (With 2, 4 trees of 16 over
 // 6001 E4M3 tokens took 40 us instead of 32, one over 20000 tokens 63 instead of
 // 40; with 8, 33 and 40.)
@@ -344,9 +345,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   };
 
   int tiles_done = 0, runs_done = 0;  // before this run (runs: those with keys)
-  if (warp == 16 || warp == 19) {
+  if (warp == 16 || warp == 18) {
     // ---- copies ------------------------------------------------------------------
-    const bool is_v = warp == 19;
+    const bool is_v = warp == 18;
     const CUtensorMap* map = is_v ? &p.v_map : &p.k_map;
     // A box is a page's rows, up to a tile's; the lanes hold the pages of `group` tiles.
     const int box_shift = min(p.cache.shift, 7), box = 1 << box_shift, boxes = BK >> box_shift;
@@ -525,12 +526,13 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       }
       tiles_done += n;
     }
-  } else if (warp == 17 || warp == 18) {
+  } else if (warp == 17) {
     // ---- products ---------------------------------------------------------------------
     // The whole warp runs the loop and one elected lane issues: values that the
     // compiler knows to be alike in all lanes (read from lane 0) stay in the
-    // registers that the instruction takes.
-    const bool second = __shfl_sync(0xffffffffu, warp, 0) == 18;
+    // registers that the instruction takes. P V of a tile comes before Q K^T of
+    // the second tile after it, so that the arrival of those scores tells that
+    // the weights' place is free too.
     const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0);
     const uint32_t q_matrix = matrix(smem_u32(qt), 16), op_matrix = matrix(smem_u32(ops), 16);
     constexpr uint32_t kLead = (uint32_t)(BK * 128 - 16) >> 4 << 16;  // values: 64 entries in a group
@@ -539,33 +541,41 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     for (; run.next(p, bar.plan); runs_done += run.tiles > 0) {
       const int n = __shfl_sync(0xffffffffu, run.tiles, 0);
       if (n == 0) continue;
-      bool ok = true;
-      if (!second) ok = wait(&bar.q_ready, runs_done & 1);
-      for (int j = 0; j < n; ++j) {
-        const int at = tiles_done + j, buf = at & 1;
-        ok = wait(&bar.op_ready[second][buf], at >> 1 & 1) && ok;
-        // The tile's weights, or those of the tile whose scores were there before.
-        if (second) ok = wait(&bar.p_ready[buf], at >> 1 & 1) && ok;
-        else if (at >= 2) ok = wait(&bar.p_ready[buf], (at - 2) >> 1 & 1) && ok;
+      bool ok = wait(&bar.q_ready, runs_done & 1);
+      for (int j = 0; j < n + 2; ++j) {
+        const int at = tiles_done + j, buf = at & 1, turn = at >> 1 & 1;  // the tile two before: the same buffers
+        const bool first = j < n, second = j >= 2;
+        if (second) {
+          ok = wait(&bar.op_ready[1][buf], turn ^ 1) && ok;
+          ok = wait(&bar.p_ready[buf], turn ^ 1) && ok;
+        }
+        if (first) ok = wait(&bar.op_ready[0][buf], turn) && ok;
         ok = __all_sync(0xffffffffu, ok);
         fence_after();
         if (elect()) {
-          if (ok && !second) {
-            const uint32_t b = op_matrix + buf * (S::OP >> 4);
+          if (second) {
+            if (ok) {
+              const uint32_t b = op_matrix + kLead + (2 + buf) * (S::OP >> 4);
 #pragma unroll
-            for (int ks = 0; ks < DIM / 16; ++ks) {
-              const int off = ((ks / 4) * (BK * 128) + (ks % 4) * 32) >> 4;
-              mma_ss(base + buf * BK, q_matrix + off, b + off, kScores, ks > 0);
+              for (int ks = 0; ks < BK / 16; ++ks)
+                mma_ts(base + kOutAt, base + kWeightsAt + buf * (BK / 2) + ks * 8, b + (ks * 2048 >> 4), kOutput,
+                       j > 2 || ks > 0);
             }
-          } else if (ok) {
-            const uint32_t b = op_matrix + kLead + (2 + buf) * (S::OP >> 4);
-#pragma unroll
-            for (int ks = 0; ks < BK / 16; ++ks)
-              mma_ts(base + kOutAt, base + kWeightsAt + buf * (BK / 2) + ks * 8, b + (ks * 2048 >> 4), kOutput,
-                     j > 0 || ks > 0);
+            commit(&bar.pv_done[buf]);
+            commit(&bar.op_empty[1][buf]);
           }
-          commit(second ? &bar.pv_done[buf] : &bar.s_full[buf]);
-          commit(&bar.op_empty[second][buf]);
+          if (first) {
+            if (ok) {
+              const uint32_t b = op_matrix + buf * (S::OP >> 4);
+#pragma unroll
+              for (int ks = 0; ks < DIM / 16; ++ks) {
+                const int off = ((ks / 4) * (BK * 128) + (ks % 4) * 32) >> 4;
+                mma_ss(base + buf * BK, q_matrix + off, b + off, kScores, ks > 0);
+              }
+            }
+            commit(&bar.s_full[buf]);
+            commit(&bar.op_empty[0][buf]);
+          }
         }
         __syncwarp();
       }
@@ -647,8 +657,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       bool ok = true;
       for (int j = 0; j < n; ++j) {
         const int key = run.k_begin + j * BK, at = tiles_done + j, buf = at & 1;
-        ok = wait(&bar.s_full[buf], at >> 1 & 1) && ok;
-        if (at >= 2) ok = wait(&bar.pv_done[buf], (at - 2) >> 1 & 1) && ok;  // these weights' place
+        ok = wait(&bar.s_full[buf], at >> 1 & 1) && ok;  // and the weights of the tile two before are used
         fence_after();
         ok = __all_sync(0xffffffffu, ok);
         const uint32_t scores = base + buf * BK + half * (BK / 2);
