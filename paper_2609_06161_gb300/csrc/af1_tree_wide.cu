@@ -686,6 +686,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         // The half's weights relative to `ref`, and its largest score.
         float2 sum;
         auto pass = [&](float ref) {
+          float most = -kInf;
           sum = make_float2(0.f, 0.f);
 #pragma unroll 1
           for (int c = 0; c < BK / 2; c += COLS) {
@@ -699,29 +700,24 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
               }
             };
             tmem_load(scores + c, x, [&] { fetch(ks); });
-            if constexpr (C::SCALED8) {
 #pragma unroll
-              for (int i = 0; i < COLS; i += 4) {
-                const float4 f = f8[i / 4];
-                const float2 a = mul2(make_float2(x[i], x[i + 1]), make_float2(f.x, f.y));
-                const float2 b = mul2(make_float2(x[i + 2], x[i + 3]), make_float2(f.z, f.w));
-                x[i] = a.x, x[i + 1] = a.y, x[i + 2] = b.x, x[i + 3] = b.y;
-              }
-              fetch(vs);
+            for (int i = 0; i < COLS; i += 4) {  // exponents of the weights
+              float4 f = make_float4(scale, scale, scale, scale);
+              if constexpr (C::SCALED8) f = f8[i / 4];
+              const float2 a = fma2(make_float2(x[i], x[i + 1]), make_float2(f.x, f.y), make_float2(-ref, -ref));
+              const float2 b = fma2(make_float2(x[i + 2], x[i + 3]), make_float2(f.z, f.w), make_float2(-ref, -ref));
+              x[i] = a.x, x[i + 1] = a.y, x[i + 2] = b.x, x[i + 3] = b.y;
             }
+            fetch(vs);
             if (masked) hide(c, x);
             float t0 = x[0], t1 = x[1];
 #pragma unroll
             for (int i = 2; i < COLS - 2; i += 4) t0 = max3(t0, x[i], x[i + 1]), t1 = max3(t1, x[i + 2], x[i + 3]);
-            top = max3(top, max3(t0, x[COLS - 2], x[COLS - 1]), t1);
+            most = max3(most, max3(t0, x[COLS - 2], x[COLS - 1]), t1);
             uint32_t r[COLS / 2];
 #pragma unroll
             for (int i = 0; i < COLS; i += 4) {
-              float2 a = make_float2(x[i], x[i + 1]), b = make_float2(x[i + 2], x[i + 3]);
-              const float2 minus = make_float2(-ref, -ref);
-              if constexpr (C::SCALED8) a = add2(a, minus), b = add2(b, minus);
-              else a = fma2(a, make_float2(scale, scale), minus), b = fma2(b, make_float2(scale, scale), minus);
-              a = make_float2(ex2(a.x), ex2(a.y)), b = make_float2(ex2(b.x), ex2(b.y));
+              float2 a = make_float2(ex2(x[i]), ex2(x[i + 1])), b = make_float2(ex2(x[i + 2]), ex2(x[i + 3]));
               sum = add2(sum, add2(a, b));
               if constexpr (C::SCALED8) {
                 const float4 f = f8[i / 4];
@@ -737,15 +733,13 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             }
             tmem_store(base + kWeightsAt + buf * (BK / 2) + (c_first + c) / 2, r);
           }
+          top = most + ref;
           tmem_wait_store();
         };
         // The weights relative to the maximum so far, which mostly holds; where a
         // row's has to move (both halves agree on that), they are formed again.
         auto reference = [&] { return (m == -kInf ? 0.f : m) + ev - kShift; };
-        if (work) {
-          pass(reference());
-          if constexpr (!C::SCALED8) top *= scale;
-        }
+        if (work) pass(reference());
         float ev_now = ev;
         if constexpr (C::SCALED8) {
           const float4 most = *reinterpret_cast<const float4*>(bar.value_top[at_tile]);
