@@ -19,13 +19,13 @@
 //             half passes it by more than kSlack binary places;
 //   8-11, 12-15  decode keys, and values: thread i turns vector i of a tile
 //             from codes into FP16 in the 128-byte-swizzled operand tile (keys
-//             K-major, values with their entries along N). INT8 and E4M3 stay codes, exact in
-//             FP16; a key's scale multiplies the scores, a value's the weights
-//             (relative to a power of two that bounds the scales so far, which
-//             the exponents take in). INT4, which has a scale for each group
-//             of 32 entries, is rounded once to FP16, keys too: a score is off
-//             by about 2^-12 sqrt(sum (q k)^2). FP16 tiles arrive by TMA and
-//             are only looked at where a sequence ends;
+//             K-major, values with their entries along N). INT8 and E4M3 stay
+//             codes, exact in FP16; a key's scale multiplies the scores, a
+//             value's the weights (relative to a power of two that bounds the
+//             scales so far, which the exponents take in). INT4, which has a
+//             scale for each group of 32 entries, is rounded once to FP16, keys
+//             too: a score is off by about 2^-12 sqrt(sum (q k)^2). FP16 tiles
+//             arrive by TMA and are only looked at where a sequence ends;
 //   16, 18    TMA copies of keys, and of values, one for up to 128 rows of a
 //             page, into the ring of codes (one warp for both took 0.65 us for
 //             each, which held up the decoders);
@@ -33,7 +33,8 @@
 //             wait more for the softmax, took 2 % longer.)
 // Keys and values each have a ring of codes and two operand tiles, with
 // barriers of their own: whoever waits on a barrier meets each of its phases in
-// turn, as a test of a phase's parity needs.
+// turn, as a test of a phase's parity needs. (The softmax skips phases of P V,
+// as the scores that it waits for come after them.)
 //
 // Infinities and NaN: the values of slots past the end are zeros, a node's
 // value that is not finite is left out of the product (0 times it would reach
@@ -42,11 +43,11 @@
 // Bound: a softmax warp's chain of steps for a tile (wait, read, exponents,
 // agree, arrive), which queue in shared memory behind the decoders' stores and
 // the products' operands. With all 128 rows in use a tile's exponents take 1024
-// cycles (16 a cycle), its products 1024; the chain takes 2700, 1.3 us: 90 us
+// cycles (16 a cycle), its products 1024; the chain takes 2600, 1.3 us: 87 us
 // for a tree of 64 nodes and 8 queries to a head over 32768 INT4 tokens of 8
-// heads (765 TFLOP/s; 0.66 of the issue slots, 0.37 of the tensor pipe). Where CTAs have few tiles, it is what a run costs once (first pages,
-// keys and q 6 us, the first tile 2, join 5 to 10): 4 trees of 16 over 6001
-// E4M3 tokens take 32 us.
+// heads (790 TFLOP/s; 0.64 of the issue slots, 0.37 of the tensor pipe). Where
+// CTAs have few tiles, it is what a run costs once (first pages, keys and q 6 us,
+// the first tile 2, join 5 to 10): 4 trees of 16 over 6001 E4M3 tokens take 32 us.
 // All waits are bounded; a wait that gives up sets the status word, and what
 // depends on it is skipped.
 #include "af1_tree.cuh"
@@ -56,10 +57,10 @@ namespace {
 
 constexpr int BK = 128;        // keys of a tile
 constexpr int kThreads = 608;
-// Tiles that a run's beginning and end are worth. (With 2, 4 trees of 16 over
-// 6001 E4M3 tokens took 40 us instead of 32, one over 20000 tokens 63 instead of
-// 40; with 8, 33 and 40.)
-constexpr int kSetupTiles = 5;
+// Tiles that a run's beginning and end are worth. (4 trees of 16 over 6001 E4M3
+// tokens, 16 of them over 2000, one of 64 over 32768 INT4 tokens: 36, 40 and 91 us
+// with 4 tiles, 31, 40 and 89 with 5, 32, 38 and 87 with 8.)
+constexpr int kSetupTiles = 8;
 constexpr int kRows = 128;
 constexpr int kOutAt = 2 * BK, kWeightsAt = 3 * BK;  // columns of tensor memory, behind two tiles of scores
 constexpr int kSlots = 2;      // operand tiles of keys, and of values
