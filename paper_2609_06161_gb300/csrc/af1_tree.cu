@@ -565,10 +565,10 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
       __syncwarp();  // the slot is free again
     }
     if (!alive) {
-      // A wait gave up: let the copies in flight land (with the same limit)
+      // A wait gave up: let the copies in flight land (within a limit)
       // before shared memory changes hands, and report it.
       for (; waited < issued; ++waited) {
-        if (wait_phase(&bars[warp][slot], phases >> slot & 1, p.wait_cycles)) phases ^= 1u << slot;
+        if (wait_phase(&bars[warp][slot], phases >> slot & 1, max(p.wait_cycles, kLanding))) phases ^= 1u << slot;
         if (++slot == STAGES) slot = 0;
       }
       if (lane == 0) atomicOr(p.status, kStatusTimeout);

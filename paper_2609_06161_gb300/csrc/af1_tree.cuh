@@ -23,6 +23,10 @@ constexpr int64_t kPartOffset = kCounterOffset + 4 * kMaxCtas;
 constexpr float kShift = 7.f, kSlack = 8.f;
 constexpr float kInf = __builtin_huge_valf();
 
+// Cycles that copies in flight are given to land after a wait has given up,
+// however short the waits are: 10 ms.
+constexpr long long kLanding = 20000000;
+
 struct TreeProblem {
   CUtensorMap k_map, v_map;
   const __half* q;

@@ -414,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       for (int at = max(issued - 1, 0); at <= issued; ++at) {
         const long long t0 = clock64();
         while (!mbar_try_wait(&bar.code_full[is_v][code_stage(is_v, at)], code_turn(is_v, at) & 1) &&
-               clock64() - t0 < p.wait_cycles) {
+               clock64() - t0 < max(p.wait_cycles, kLanding)) {
         }
       }
     }
