@@ -1,13 +1,14 @@
 // af1_score.cu — log-probabilities of given tokens, entropy and the largest
 // alternatives of rows of logits, in one pass over the logits.
 //
-// With y = x log2(e) / temperature, a thread keeps a reference r (y of the
-// largest x so far), S = sum 2^d and T = sum 2^d d over its entries, d = y - r,
-// and follows a new maximum by S' = f S, T' = f (T + S delta). Then
+// With c = log2(e) / temperature, a thread keeps a reference r (the largest x
+// so far), S = sum 2^d and T = sum 2^d d over its entries, d = (x - r) c, and
+// follows a new maximum by S' = f S, T' = f (T + S delta). Then
 //   log p = (d - log2 S) ln 2,   entropy = (log2 S - T / S) ln 2.
-// For FP16, d is one fused multiply-add of x, and r the rounded y; FP32 logits
-// may be so large that y overflows, so there r is x itself and d the scaled
-// difference.
+// The difference comes before the factor at every temperature and for both
+// types: d of the largest entry is then 0, where x c less a rounded r c would
+// leave it half a unit in the last place of r c, which low temperatures raise
+// past every exponent; and x c itself may overflow where d does not.
 //
 // The largest entries. Passing over the logits, a warp only keeps its lanes'
 // maxima of every batch (of 16 or 32 entries to a lane). Every kSegment batches
@@ -78,22 +79,7 @@ constexpr float kLeast = -1e4f;  // 2^d is 0 from far above on; d itself may be 
 struct Stats {
   float r = -kInf, s = 0.f, t = 0.f;
 };
-// The reference of a value, and the distance of two references.
-template <typename T>
-__device__ __forceinline__ float reference(float x, float c) {
-  return sizeof(T) == 2 ? x * c : x;
-}
-template <typename T>
-__device__ __forceinline__ float distance(float a, float b, float c) {
-  return sizeof(T) == 2 ? a - b : (a - b) * c;
-}
-template <typename T>
-__device__ __forceinline__ float depth(float x, float r, float c) {  // d of a value
-  return sizeof(T) == 2 ? fmaf(x, c, -r) : (x - r) * c;
-}
-
 // The two sets of entries together.
-template <typename T>
 __device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float c) {
   Stats o;
   o.r = fmaxf(a.r, b.r);
@@ -101,7 +87,7 @@ __device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float c) {
     o.s = a.s + b.s, o.t = 0.f;  // nothing, or NaN
     return o;
   }
-  const float da = fmaxf(distance<T>(a.r, o.r, c), kLeast), db = fmaxf(distance<T>(b.r, o.r, c), kLeast);
+  const float da = fmaxf((a.r - o.r) * c, kLeast), db = fmaxf((b.r - o.r) * c, kLeast);
   const float fa = ex2(da), fb = ex2(db);
   o.s = a.s * fa + b.s * fb;
   o.t = fa * (a.t + a.s * da) + fb * (b.t + b.s * db);
@@ -248,12 +234,11 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
         for (int i = 0; i < 4; ++i) lane_top = max_nan(lane_top, reinterpret_cast<const float*>(&w[u])[i]);
     }
     const float top = (float)lane_top;
-    const float r = reference<T>(top, c);
-    if (r > st.r) {
-      const float d = fmaxf(distance<T>(st.r, r, c), kLeast), f = ex2(d);
+    if (top > st.r) {
+      const float d = fmaxf((st.r - top) * c, kLeast), f = ex2(d);
       st.t = f * (st.t + st.s * d);
       st.s *= f;
-      st.r = r;
+      st.r = top;
     }
     const float minus = st.r == -kInf ? 0.f : -st.r;
     float2 s2 = make_float2(st.s, 0.f), t2 = make_float2(st.t, 0.f);
@@ -263,8 +248,7 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
       for (int i = 0; i < E / 2; ++i) {
         const float2 v = HALF ? __half22float2(reinterpret_cast<const __half2*>(&w[u])[i])
                               : reinterpret_cast<const float2*>(&w[u])[i];
-        const float2 d = HALF ? fma2(v, make_float2(c, c), make_float2(minus, minus))
-                              : mul2(add2(v, make_float2(minus, minus)), make_float2(c, c));
+        const float2 d = mul2(add2(v, make_float2(minus, minus)), make_float2(c, c));
         const float2 e = make_float2(ex2(d.x), ex2(d.y));
         s2 = add2(s2, e);
         t2 = fma2(e, make_float2(fmaxf(d.x, kLeast), fmaxf(d.y, kLeast)), t2);
@@ -347,8 +331,8 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
     const bool real = lane < head + tail;
     const float v = real ? (float)x[i] : -kInf;
     Stats one;
-    if (real) one.r = reference<T>(v, c), one.s = v == -kInf ? 0.f : ex2(v - v);
-    st = join<T>(st, one, c);
+    if (real) one.r = v, one.s = v == -kInf ? 0.f : ex2(v - v);
+    st = join(st, one, c);
     if constexpr (TOP) {
       const uint64_t key = real && !(v < bound) ? order_key(v, (uint32_t)i) : 0;
       if (__any_sync(0xffffffffu, key > kth)) merge(key);
@@ -362,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
     other.r = __shfl_xor_sync(0xffffffffu, st.r, d);
     other.s = __shfl_xor_sync(0xffffffffu, st.s, d);
     other.t = __shfl_xor_sync(0xffffffffu, st.t, d);
-    st = join<T>(st, other, c);
+    st = join(st, other, c);
   }
   if (lane == 0) stats[warp] = st;
   if constexpr (TOP) lists[warp][lane] = mine;
@@ -380,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
   if (warp == 0) {
     st = stats[0];
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) st = join<T>(st, stats[w], c);
+    for (int w = 1; w < kWarps; ++w) st = join(st, stats[w], c);
     if (cs > 1) {
       __syncwarp();
       if (lane == 0) stats[0] = st;
@@ -401,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
 #pragma unroll
       for (int i = 0; i < kMaxCluster - 1; ++i) {
         if (i + 1 >= cs) break;
-        st = join<T>(st, far[i], c);
+        st = join(st, far[i], c);
         if constexpr (TOP) mine = merge_lists(mine, far_list[i], lane);
       }
     }
@@ -413,8 +397,8 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
   const float none = -kInf;
   auto logprob = [&](float v) {
     if (v == none && st.s == st.s) return none;
-    // FP32: the difference over the temperature, which does not overflow where its multiple by log2(e) would.
-    return HALF ? (depth<T>(v, st.r, c) - log_s) * ln2 : fmaf(v - st.r, c * ln2, -log_s * ln2);
+    // The difference over the temperature, which does not overflow where its multiple by log2(e) would.
+    return fmaf(v - st.r, c * ln2, -log_s * ln2);
   };
   if (lane == 0 && p.entropy != nullptr)
     p.entropy[row] = st.r == -kInf && st.s == st.s ? 0.f : (log_s - st.t / st.s) * ln2;

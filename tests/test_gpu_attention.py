@@ -694,6 +694,25 @@ def test_scores_of_long_rows(P, dtype):
     score_check(P, x[3:], tokens[3:], 1)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("temperature", [1e-30, 1e-10, 1e-8, 1e-6, 1e-4, 1e-2, 30.0, 1e30])
+def test_scores_at_any_temperature(P, dtype, temperature):
+    """The largest entry before the first 16-byte boundary, after the last one, and between; rows that are all ends."""
+    g = gen(23)
+    for vocab in (5, 33, 4099, 40003):
+        for first in (0, 3):
+            big = dev((3 * g.standard_normal((6, vocab + 11))).astype(np.float32)).to(dtype)
+            x = big[:, first: first + vocab]
+            at = [0, vocab - 1, vocab // 2, 1, max(0, vocab - 3), vocab // 3]
+            x[torch.arange(6), torch.tensor(at)] = 17.36
+            x[5, at[4]] = 17.36  # equal entries, one of them in an end
+            x[0, 2] = 17.34375  # next to the largest
+            tokens = g.integers(0, vocab, (6, 3)).astype(np.int32)
+            tokens[:, 0] = at
+            # The library is given the temperature in FP32.
+            score_check(P, x, tokens, min(vocab, 9), temperature=float(np.float32(temperature)))
+
+
 def test_scores_strides(P):
     g = gen(21)
     for dtype in (torch.float16, torch.float32):
