@@ -95,11 +95,23 @@ static __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint3
                : "r"(addr)
                : "memory");
 }
+// Budgets below this many cycles are waited for without suspending the thread,
+// which may take longer.
+constexpr long long kSuspend = 65536;
+static __device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(done)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return done != 0;
+}
 // Bounded wait for a phase of a barrier: false where it gave up.
 static __device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, long long budget) {
-  if (mbar_try_wait(bar, parity)) return true;
+  if (mbar_test_wait(bar, parity)) return true;
   const long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity))
+  while (!(budget < kSuspend ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)))
     if (clock64() - t0 > budget) return false;
   return true;
 }

@@ -49,7 +49,8 @@
 // CTAs have few tiles, it is what a run costs once (first pages, keys and q 6 us,
 // the first tile 2, join 5 to 10): 4 trees of 16 over 6001 E4M3 tokens take 32 us.
 // All waits are bounded; a wait that gives up sets the status word, and what
-// depends on it is skipped.
+// depends on it is skipped. Where one has, no copy is issued any more, and before
+// shared or tensor memory changes hands the copies and products in flight end.
 #include "af1_tree.cuh"
 
 namespace af1 {
@@ -98,8 +99,10 @@ struct Barriers {
   Plan plan;
   uint64_t op_ready[2][2], op_empty[2][2], code_full[2][2], code_empty[2][2];  // of keys and values
   uint64_t s_full[2], p_ready[2], pv_done[2], q_ready;  // by tile
+  uint64_t drained;                         // products, after a wait that gave up
   uint32_t tmem;
   volatile int gave_up;
+  int issued[2];                            // of keys and values: the last tile whose copies were
   uint32_t code_bad[2][2], tile_bad[kNotes];   // bits: 16 keys each whose page is missing
   uint32_t nodes_bad[4][2];                 // by run that has keys: nodes whose value is not finite (values are
                                             // decoded at most two tiles, so two such runs, ahead of their use)
@@ -315,7 +318,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       mbar_init(&bar.pv_done[i], 1);
     }
     mbar_init(&bar.q_ready, 8);
+    mbar_init(&bar.drained, 1);
     bar.gave_up = 0, bar.parts = 0;
+    bar.issued[0] = bar.issued[1] = -1;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
   }
@@ -354,7 +359,6 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     const int box_shift = min(p.cache.shift, 7), box = 1 << box_shift, boxes = BK >> box_shift;
     const int group_shift = box_shift - 2;  // 32 / boxes
     const bool leads = lane < boxes;
-    int issued = -1;  // the last tile whose copies were
     while (run.next(p, bar.plan)) {
       const int32_t* page_row = p.pages.pages + run.seq * p.pages.ld;
       const int n = run.tiles;
@@ -378,7 +382,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         const unsigned lack = __ballot_sync(0xffffffffu, mine && !there);
         const int64_t row =
             (((int64_t)page * p.cache.heads + run.head) << p.cache.shift) + (k & ((1 << p.cache.shift) - 1));
-        const bool ok = wait(F16 ? &bar.op_empty[is_v][st] : &bar.code_empty[is_v][st], (code_turn(is_v, at) & 1) ^ 1);
+        // Decoders free a stage whose copies they gave up on, too, but only after
+        // gave_up is set: nothing is issued into it.
+        const bool ok =
+            wait(F16 ? &bar.op_empty[is_v][st] : &bar.code_empty[is_v][st], (code_turn(is_v, at) & 1) ^ 1) && !bar.gave_up;
         if (!__all_sync(0xffffffffu, ok)) continue;
         if (lane == 0) {
           uint32_t bad = 0;  // a bit for each 16 keys
@@ -387,8 +394,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           bar.code_bad[is_v][st] = bad;
           const int per_key = C::RB + (C::SCALED8 ? (is_v ? 0 : 2 * C::SB) : C::SB);
           mbar_expect_tx(&bar.code_full[is_v][st], __popc(have) * box * per_key);
+          bar.issued[is_v] = at;
         }
-        issued = at;
         __syncwarp();
         if (there) {
           uint8_t* to = code_tile(is_v, at) + lane * box * C::SPAN;
@@ -409,15 +416,6 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       }
       tiles_done += n;
     }
-    // After a wait that gave up, copies may still be on their way.
-    if (bar.gave_up && lane == 0) {
-      for (int at = max(issued - 1, 0); at <= issued; ++at) {
-        const long long t0 = clock64();
-        while (!mbar_try_wait(&bar.code_full[is_v][code_stage(is_v, at)], code_turn(is_v, at) & 1) &&
-               clock64() - t0 < max(p.wait_cycles, kLanding)) {
-        }
-      }
-    }
   } else if (warp >= 8 && warp < 16) {
     // ---- decode ---------------------------------------------------------------------
     const int row = threadIdx.x % 128;
@@ -426,7 +424,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       const int n = run.tiles;
       for (int j = 0; j < n; ++j) {
         const int at = tiles_done + j, st = code_stage(is_v, at), slot = at & 1;
-        bool ok = wait(&bar.code_full[is_v][st], code_turn(is_v, at) & 1);
+        // Copies keep to budgets below a suspension, too. (Of the other waits, which
+        // are for warps of this CTA, that cost 4 us of 86.)
+        bool ok = true;
+        if (p.wait_cycles >= kSuspend) ok = wait(&bar.code_full[is_v][st], code_turn(is_v, at) & 1);
+        else if (!wait_phase(&bar.code_full[is_v][st], code_turn(is_v, at) & 1, p.wait_cycles)) bar.gave_up = 1, ok = false;
         if constexpr (!F16) ok = wait(&bar.op_empty[is_v][slot], (at >> 1 & 1) ^ 1) && ok;
         ok = __all_sync(0xffffffffu, ok);
         const int key = run.k_begin + j * BK + row;
@@ -875,7 +877,26 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   fence_before();
   __syncthreads();
   fence_after();
-  if (bar.gave_up && threadIdx.x == 0) atomicOr(p.status, kStatusTimeout);
+  if (bar.gave_up) {  // by any role: no role waits any more
+    // Copies and products may still be on their way. They end, within a limit,
+    // before the parts are joined over the tiles and tensor memory goes.
+    const long long t0 = clock64(), limit = max(p.wait_cycles, kLanding);
+    if ((warp == 16 || warp == 18) && lane == 0) {
+      const bool is_v = warp == 18;
+      const int issued = bar.issued[is_v];
+      for (int at = max(issued + 1 - (is_v ? S::V_STAGES : S::K_STAGES), 0); at <= issued; ++at)
+        while (!mbar_try_wait(&bar.code_full[is_v][code_stage(is_v, at)], code_turn(is_v, at) & 1) &&
+               clock64() - t0 < limit) {
+        }
+    }
+    if (warp == 17 && elect()) {  // the lane that issued the products
+      commit(&bar.drained);
+      while (!mbar_try_wait(&bar.drained, 0) && clock64() - t0 < limit) {
+      }
+    }
+    if (threadIdx.x == 0) atomicOr(p.status, kStatusTimeout);
+    __syncthreads();
+  }
   // ---- items that span CTAs: the last CTA to arrive joins the parts, in order.
   // A thread has 8 places of 4 rows, and copies them (and the rows' maxima and
   // sums) to slots of its own in shared memory, whose tiles are used up, two or
@@ -971,18 +992,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       }
     }
   }
-  if (warp == 16) {
-    if (bar.gave_up) {  // products may still be on their way: let them end before their memory goes
-      if (lane == 0) {
-        commit(&bar.q_ready);
-        const long long t0 = clock64();
-        while (clock64() - t0 < 1000000) {
-        }
-      }
-      __syncwarp();
-    }
+  if (warp == 16)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
-  }
 }
 
 template <int KIND, int DIM>

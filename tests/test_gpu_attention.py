@@ -578,6 +578,46 @@ def test_workspace_serves_other_shapes_streams_and_graphs(P):
     P.workspace_status(big)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("nodes,dim", [(2, 64), (2, 128), (40, 64), (40, 128)])
+def test_waits_that_give_up(P, kind, nodes, dim):
+    """A budget of one cycle, which waits for copies do not keep: the calls end and say so, the arrival counters are at
+    zero again, and the next calls on the cleared workspace give what they gave before."""
+    torch.manual_seed(14)
+    cache = P.KVCache.empty(400, 256, 8, dim, kind)  # enough to keep the memory busy
+    for t in (cache.k, cache.v):
+        if kind == "f16":
+            t.normal_()
+        else:  # E4M3: no NaN, at most 30
+            t.view(torch.uint8).random_().bitwise_and_(0xCF if kind == "e4m3" else 0xFF)
+    for t in (cache.k_scale, cache.v_scale):
+        if t is not None:
+            t.uniform_(0.001, 0.01)
+    pages = torch.randperm(400, device="cuda").to(torch.int32).view(16, 25)
+    lens = torch.randint(0, 6300, (16,), device="cuda").to(torch.int32)
+    q = torch.randn((16, nodes, 32, dim), device="cuda").half()
+    workspace = cache.make_workspace(q)
+    run = lambda: cache.tree_attention(q, pages, lens, workspace=workspace)  # noqa: E731
+    before = run()
+    P.workspace_status(workspace)
+    old = P.get_wait_cycles()
+    try:
+        P.set_wait_cycles(1)
+        for _ in range(8):
+            run()
+        torch.cuda.synchronize()
+    finally:
+        P.set_wait_cycles(old)
+    with pytest.raises(P.AF1Error) as e:
+        P.workspace_status(workspace)
+    assert e.value.code == -7
+    assert not workspace[256:4352].any()
+    workspace.zero_()
+    for _ in range(3):
+        assert torch.equal(run(), before)
+    P.workspace_status(workspace)
+
+
 def test_offsets_past_32_bits(P):
     """A cache of more than 2^32 bytes and 2^31 entries: its last pages."""
     g = gen(13)
