@@ -600,10 +600,12 @@ def test_waits_that_give_up(P, kind, nodes, dim):
     run = lambda: cache.tree_attention(q, pages, lens, workspace=workspace)  # noqa: E731
     before = run()
     P.workspace_status(workspace)
+    sweep = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")  # twice the L2: copies come from the memory
     old = P.get_wait_cycles()
     try:
         P.set_wait_cycles(1)
-        for _ in range(8):
+        for _ in range(40):
+            sweep.zero_()
             run()
         torch.cuda.synchronize()
     finally:
