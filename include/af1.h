@@ -209,8 +209,10 @@ AF1_API int af1_layer_get_desc(const af1_layer* layer, af1_layer_desc* desc);
 /* Device bytes the layer holds for its signs (row-block layout) and its scales. */
 AF1_API int af1_layer_device_bytes(const af1_layer* layer, int64_t* sign_bytes, int64_t* scale_bytes);
 
-/* Bytes of workspace one af1_linear_forward call with `tokens` rows needs
- * (>= 256). Returns a negative AF1_ERR_* code on bad arguments. */
+/* Bytes of workspace one af1_linear_forward call with `tokens` rows needs: a
+ * head of 65792 bytes (a status word and counters, the same for every call of
+ * every entry point but af1_step_run) and scratch. Returns a negative AF1_ERR_*
+ * code on bad arguments. */
 AF1_API int64_t af1_workspace_bytes(const af1_layer* layer, int64_t tokens);
 
 /* y = x . W_hat^T for `tokens` rows (AF1 Eq. final_reconstruction applied
@@ -221,11 +223,13 @@ AF1_API int64_t af1_workspace_bytes(const af1_layer* layer, int64_t tokens);
  *       AF1_F16 (ldy % 8 == 0) or AF1_F32 (ldy % 4 == 0). Only the first m
  *       entries of each row are written.
  *   workspace: device scratch of at least af1_workspace_bytes(layer, tokens)
- *       bytes, 256-byte aligned, owned by the caller. It must be zero-filled
- *       before its first use; every completed call leaves its bookkeeping
- *       words at zero again, so one workspace serves any sequence of calls
- *       on one stream, for any layer. Calls that may overlap on the GPU
- *       (different streams) need different workspaces.
+ *       bytes, 256-byte aligned, owned by the caller. Its first 65792 bytes
+ *       must be zero before its first use; every completed call leaves them
+ *       at zero again and has its scratch behind them, so one workspace
+ *       serves any sequence of calls on one stream, for any layer and length,
+ *       of this and every other entry point that takes one except
+ *       af1_step_run. Calls that may overlap on the GPU (different streams)
+ *       need different workspaces.
  * Asynchronous and stream-ordered: nothing is synchronized. tokens == 0 is a
  * no-op returning AF1_OK. Launch errors are returned at once; a device-side
  * wait that gave up is reported by af1_workspace_status. The layer is not
@@ -324,10 +328,11 @@ AF1_API int af1_linear_forward_multi(const af1_layer* const* layers, int count, 
  * Same arguments as af1_linear_forward minus the workspace: the scratch is a
  * 1 MiB array compiled into the library, present on every GPU that loads it
  * until the process exits. Nothing is allocated by this call. Calls whose
- * scratch need (af1_workspace_bytes(layer, tokens)) exceeds 1 MiB are
- * rejected with AF1_ERR_WORKSPACE: with up to 16 tokens every shape with
- * r <= 16256 fits; longer calls also hold min(tokens, 2048) x r FP16 rank
- * intermediates, so they fit only for short passes of small-rank layers.
+ * scratch need (af1_workspace_bytes(layer, tokens), less its counters, which
+ * these calls do without) exceeds 1 MiB are rejected with AF1_ERR_WORKSPACE:
+ * with up to 16 tokens every shape with r <= 16256 fits; longer calls also hold
+ * min(tokens, 2048) x r FP16 rank intermediates, so they fit only for short
+ * passes of small-rank layers.
  * Passes of 8-16 tokens over large sign matrices run here without the
  * prepared tensor-core operand that af1_linear_forward keeps in its
  * workspace (the CUDA-core kernel takes them), so they can be slower.
@@ -465,7 +470,8 @@ AF1_API int af1_step_info(const af1_step* step, int64_t* ctas, int64_t* tasks, i
  * launch is resident). workspace: device memory of af1_step_workspace_bytes,
  * 256-byte aligned, zero-filled before its first use; every completed run
  * leaves the header ready for the next one, so one workspace serves any
- * sequence of runs on one stream. Runs that may overlap on the GPU need
+ * sequence of runs on one stream (of af1_step_run alone: other calls'
+ * counters lie where a run has scratch). Runs that may overlap on the GPU need
  * different workspaces. A bounded wait that gave up is reported by
  * af1_workspace_status(workspace, stream) (the run's bookkeeping is closed
  * even then, so the workspace stays usable). Asynchronous; errors:
@@ -694,7 +700,8 @@ AF1_API int af1_tree_mask(const int32_t* parents, int64_t sequences, int64_t nod
  *   lse: FP32 [sequences][nodes][q_heads] contiguous, the natural logarithm of
  *       the softmax denominators, or NULL.
  *   workspace: af1_tree_workspace_bytes bytes, with the rules of
- *       af1_linear_forward (256-byte aligned, zero-filled before first use).
+ *       af1_linear_forward (256-byte aligned, the first 65792 bytes zero
+ *       before first use); one workspace serves both.
  * An infinite or NaN key or value reaches the nodes that see it and no other.
  * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, WORKSPACE, CUDA. */
 typedef struct af1_tree_args {

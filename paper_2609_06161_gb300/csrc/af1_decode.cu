@@ -1520,7 +1520,7 @@ Workspace plan_workspace(const af1_layer& L, int64_t tokens, bool prep, bool swi
   Workspace w;
   int64_t off = 0;
   w.status = off;
-  off += 256;
+  off += prep ? kScratchOffset : kStatusBytes;  // prep = false uses no counters
   const bool mid = mid_pass(L, tokens, prep);
   w.sbuf = off;
   off += align256((mid ? tokens : (int64_t)kMaxPassTokens) * decode_ldz(L) * 4);
@@ -1540,8 +1540,11 @@ Workspace plan_workspace(const af1_layer& L, int64_t tokens, bool prep, bool swi
     if (prep) {
       w.pbuf = off;
       off += align256(prefill_part_bytes(L, tokens));
-      w.pcnt = off;
-      off += align256(prefill_count_bytes(L, tokens));
+      w.pcnt = kStatusBytes;
+      if (prefill_count_bytes(L, tokens) > kCounterBytes) {
+        w.pcnt = off;
+        off += align256(prefill_count_bytes(L, tokens));
+      }
     }
   }
   if (swiglu) {
@@ -1629,7 +1632,14 @@ cudaError_t launch_forward(const af1_layer& L, const void* x, int64_t ldx, int64
     // Prefill: two tensor-core GEMMs per pass (af1_prefill.cu); the SwiGLU
     // input is formed first, one pass of tokens at a time.
     float* part = W.pbuf != 0 ? reinterpret_cast<float*>(wsb + W.pbuf) : nullptr;
-    unsigned* count = W.pcnt != 0 ? reinterpret_cast<unsigned*>(wsb + W.pcnt) : nullptr;
+    unsigned* count = nullptr;
+    if (W.pcnt == kStatusBytes) {
+      count = stat + kStatusBytes / 4;  // those of the workspace that the call reports to
+    } else if (W.pcnt != 0) {
+      count = reinterpret_cast<unsigned*>(wsb + W.pcnt);
+      const cudaError_t e = cudaMemsetAsync(count, 0, prefill_count_bytes(L, tokens), st);
+      if (e != cudaSuccess) return e;
+    }
     if (x2 == nullptr) return launch_prefill(L, x, ldx, tokens, y, ldy, y_dtype, wsb + W.hbuf, part, count, stat, st);
     for (int64_t t0 = 0; t0 < tokens; t0 += kPrefillPassTokens) {
       const int64_t T = (tokens - t0) < kPrefillPassTokens ? (tokens - t0) : kPrefillPassTokens;

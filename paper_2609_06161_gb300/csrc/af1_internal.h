@@ -38,6 +38,17 @@ constexpr int64_t kMidMaxTokens = 64;
 // SM count the planners assume when the caller passes none (a GB300 has 152).
 constexpr int kDefaultSms = 152;
 
+// Every workspace (but a step's) begins with the status word's line and then
+// counters that are zero between calls. Both are a region of their own, the
+// same for every layer, length and operator: no call has scratch there, so
+// that one workspace serves any sequence of them. (With the prefill's counters
+// behind its scratch, where other calls had theirs, tiles that CTAs share were
+// left unwritten.) 64 KB hold the prefill's counters of 8192 tiles: 131072 rows
+// at 2048 tokens.
+constexpr int64_t kStatusBytes = 256;
+constexpr int64_t kCounterBytes = 65536;
+constexpr int64_t kScratchOffset = kStatusBytes + kCounterBytes;
+
 // Workspace carve-up for one layer and one forward call of `tokens` tokens.
 struct Workspace {
   int64_t status = 0;  // uint32 status word
@@ -47,7 +58,8 @@ struct Workspace {
   int64_t hbuf = 0;    // FP16 [min(tokens, kPrefillPassTokens)][prefill_h_ld]: H (prefill)
   int64_t hx = 0;      // FP16 [min(tokens, kPrefillPassTokens)][swiglu_ld]: SwiGLU input h (0: none)
   int64_t pbuf = 0;    // FP32 partial tiles of the prefill GEMMs (0: none; one tile per CTA then)
-  int64_t pcnt = 0;    // uint32 per prefill tile: contributors arrived (zero between calls)
+  int64_t pcnt = 0;    // two uint32 per prefill tile: contributors arrived and stored; kStatusBytes, or, where they are
+                       // more than kCounterBytes, behind the scratch (then cleared by each call)
   int64_t total = 0;
 };
 // prep = false leaves out the prepared-B region and the prefill's partial

@@ -719,9 +719,9 @@ int fail(int code, const std::string& msg) { return set_error(code, "af1_tree_at
 int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 0; }
 
 int64_t workspace_bytes(const af1_kv_cache& c, int64_t rows) {
-  if (row_blocks(rows) == 0) return kPartOffset + tree_wide_part_bytes(c);
+  if (row_blocks(rows) == 0) return kScratchOffset + tree_wide_part_bytes(c);
   const int64_t ctas = std::min(3 * c.num_sms, kMaxCtas);  // at most three CTAs to an SM
-  return kPartOffset + 2 * ctas * (8 * row_blocks(rows)) * (c.d.head_dim + 2) * 4;
+  return kScratchOffset + 2 * ctas * (8 * row_blocks(rows)) * (c.d.head_dim + 2) * 4;
 }
 
 template <int KIND, int DIM, int NT, int W, int KW, int STAGES, int CTAS>
@@ -830,8 +830,8 @@ int af1_tree_attention(const af1_kv_cache* c, const af1_tree_args* a, void* work
   p.nodes = (int)a->nodes, p.group = group, p.words = (int)(a->nodes + 31) / 32;
   p.scale_log2 = a->scale * 1.4426950408889634f;
   p.out_f32 = a->out_dtype == AF1_F32;
-  p.counters = reinterpret_cast<unsigned*>(static_cast<uint8_t*>(workspace) + kCounterOffset);
-  p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kPartOffset);
+  p.counters = reinterpret_cast<unsigned*>(static_cast<uint8_t*>(workspace) + kStatusBytes);
+  p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kScratchOffset);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   p.status = static_cast<unsigned*>(workspace);
   p.wait_cycles = wait_budget();

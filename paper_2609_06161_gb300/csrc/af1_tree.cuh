@@ -15,9 +15,8 @@
 
 namespace af1 {
 
-constexpr int kMaxCtas = 1024;                    // counters of the workspace
-constexpr int64_t kCounterOffset = 256;           // behind the status word's line
-constexpr int64_t kPartOffset = kCounterOffset + 4 * kMaxCtas;
+constexpr int kMaxCtas = 1024;  // counters of the workspace
+static_assert(4 * kMaxCtas <= kCounterBytes, "the counters lie in the region of counters");
 // Weights are at most 2^(kShift + kSlack) = 2^15 (half of FP16's range), and
 // keep 11 bits down to 2^(-14 - kShift - kSlack) of the largest.
 constexpr float kShift = 7.f, kSlack = 8.f;
