@@ -620,6 +620,34 @@ def test_waits_that_give_up(P, kind, nodes, dim):
     P.workspace_status(workspace)
 
 
+@pytest.mark.parametrize("nodes,group", [(1, 4), (40, 4)])
+def test_default_workspace_clears_its_head_alone(P, nodes, group):
+    """What a workspace holds behind its head may be anything, and is left as it is."""
+    cache = P.KVCache.empty(8, 64, 2, 64, "f16")
+    cache.k.normal_(), cache.v.normal_()
+    q = torch.randn((1, nodes, 2 * group, 64), device="cuda").half()
+    size, head = cache.workspace_bytes(1, nodes, 2 * group), 65792
+    old = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    at = old.data_ptr()
+    del old
+    workspace = cache.make_workspace(q)
+    assert not workspace[:head].any()
+    if workspace.data_ptr() == at:  # the allocator gave the same memory
+        assert workspace[head:].eq(255).all()
+    else:
+        workspace[head:] = 255
+    pages, lens = torch.arange(8, device="cuda").to(torch.int32)[None], torch.tensor([500 - nodes], dtype=torch.int32,
+                                                                                     device="cuda")
+    with pytest.raises(P.AF1Error) as e:  # leaves no error behind
+        cache.tree_attention(q.cpu(), pages, lens)
+    assert e.value.code == -2 and not cache.make_workspace(q.cpu()).any()
+    zeros = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    a = cache.tree_attention(q, pages, lens, workspace=workspace)
+    assert torch.equal(a, cache.tree_attention(q, pages, lens, workspace=zeros))
+    assert torch.equal(a, cache.tree_attention(q, pages, lens))
+    assert not workspace[:head].any() and not zeros[:head].any()
+
+
 def test_offsets_past_32_bits(P):
     """A cache of more than 2^32 bytes and 2^31 entries: its last pages."""
     g = gen(13)
