@@ -335,7 +335,10 @@ class KVCache:
 
     def make_workspace(self, q: torch.Tensor, pages: torch.Tensor | None = None) -> torch.Tensor:
         """A workspace for tree_attention calls with queries of q's shape, or
-        with fewer rows for each cached head; what has to be zero is."""
+        with fewer rows for each cached head; what has to be zero is. pages:
+        the table of these calls, only checked against q."""
+        if pages is not None and _pages(pages)[1] != q.shape[0]:
+            raise ValueError("pages must have one row for each sequence")
         size = self.workspace_bytes(q.shape[0], q.shape[1], q.shape[2])
         if not q.is_cuda:
             return torch.zeros(size, dtype=torch.uint8, device=q.device)

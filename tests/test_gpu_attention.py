@@ -648,6 +648,15 @@ def test_default_workspace_clears_its_head_alone(P, nodes, group):
     assert not workspace[:head].any() and not zeros[:head].any()
 
 
+def test_workspace_checks_the_table(P):
+    cache = P.KVCache.empty(4, 16, 2, 64, "int8")
+    q, table = torch.zeros((2, 3, 4, 64), dtype=torch.float16, device="cuda"), torch.zeros((2, 2), device="cuda")
+    assert cache.make_workspace(q, table.int()).numel() == cache.make_workspace(q).numel()
+    for bad in (table, table.int()[:1], table.int()[0], table.int().t()):
+        with pytest.raises(ValueError):
+            cache.make_workspace(q, bad)
+
+
 def test_offsets_past_32_bits(P):
     """A cache of more than 2^32 bytes and 2^31 entries: its last pages."""
     g = gen(13)
