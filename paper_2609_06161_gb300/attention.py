@@ -147,23 +147,27 @@ def _pages(t: torch.Tensor):
 def _params(length, dim, base, scaling, factor, low, high, original, attention):
     if scaling not in SCALINGS:
         raise ValueError(f"scaling must be one of {list(SCALINGS)}")
+    low = 1.0 if low is None else low
+    high = (32.0 if scaling == "ramp" else 4.0) if high is None else high
     return _RopeParams(length, dim, SCALINGS[scaling], base, factor, low, high, original, attention)
 
 
-def rope_frequencies(dim: int, base: float = 10000.0, scaling=None, factor: float = 1.0, low: float = 1.0,
-                     high: float = 4.0, original: float = 0.0, attention: float = 0.0):
-    """(list of dim / 2 frequencies, factor of cos and sin): af1_rope_frequencies, on the host."""
+def rope_frequencies(dim: int, base: float = 10000.0, scaling=None, factor: float = 1.0, low: float | None = None,
+                     high: float | None = None, original: float = 0.0, attention: float = 0.0):
+    """(list of dim / 2 frequencies, factor of cos and sin): af1_rope_frequencies, on the host.
+    low, high: by default 1 and 4 for "bands", 1 and 32 for "ramp"."""
     p = _params(1, dim, base, scaling, factor, low, high, original, attention)
     freq, att = (_f64 * 128)(), _f64()
     _check(_rope_frequencies(ctypes.byref(p), freq, ctypes.byref(att)))
     return list(freq)[: dim // 2], att.value
 
 
-def rope_table(length: int, dim: int, base: float = 10000.0, scaling=None, factor: float = 1.0, low: float = 1.0,
-               high: float = 4.0, original: float = 0.0, attention: float = 0.0, device=None,
-               stream=None) -> torch.Tensor:
+def rope_table(length: int, dim: int, base: float = 10000.0, scaling=None, factor: float = 1.0,
+               low: float | None = None, high: float | None = None, original: float = 0.0, attention: float = 0.0,
+               device=None, stream=None) -> torch.Tensor:
     """cos and sin of positions 0 .. length - 1, float32 (length, dim / 2, 2)
-    (af1_rope_table). scaling: None, "linear", "base", "bands" or "ramp"."""
+    (af1_rope_table). scaling: None, "linear", "base", "bands" or "ramp";
+    low, high: by default 1 and 4 for "bands", 1 and 32 for "ramp"."""
     p = _params(length, dim, base, scaling, factor, low, high, original, attention)
     table = _empty((max(length, 0), max(dim, 0) // 2, 2), torch.float32,
                    device or torch.device("cuda", torch.cuda.current_device()), stream)

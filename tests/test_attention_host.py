@@ -49,6 +49,17 @@ def test_frequencies(P, dim, scaling):
     assert P.rope_frequencies(dim, base, scaling, factor, low, high, original, attention=0.75)[1] == 0.75
 
 
+def test_default_bounds(P):
+    """Of each scaling its own: what is between the bounds, and what not."""
+    kw = dict(base=10000.0, factor=4.0, original=4096.0)
+    for scaling, low, high in (("bands", 1.0, 4.0), ("ramp", 1.0, 32.0)):
+        default, _ = P.rope_frequencies(128, scaling=scaling, **kw)
+        assert default == P.rope_frequencies(128, scaling=scaling, low=low, high=high, **kw)[0]
+        turns = 4096.0 * 10000.0 ** (-2.0 * np.arange(64) / 128) / (2 * math.pi)
+        kept = np.isclose(default, 10000.0 ** (-2.0 * np.arange(64) / 128), rtol=1e-12)
+        assert kept[turns > high * 1.3].all() and not kept[turns < high / 1.3].any()
+
+
 def test_refusals(P):
     for kw in (dict(dim=0), dict(dim=3), dict(dim=258), dict(dim=64, base=1.0), dict(dim=64, base=float("nan")),
                dict(dim=64, scaling="linear", factor=0.5), dict(dim=64, scaling="bands", original=0.0),
