@@ -539,7 +539,8 @@ AF1_API int af1_budget_to_rank(double b, int64_t m, int64_t n, int64_t* r_out);
  *                    (1 - g) f_i / factor + g f_i with g = (original / w - low) / (high - low)
  *   AF1_ROPE_RAMP    by index: with e(beta) = dim ln(original / (2 pi beta)) / (2 ln base),
  *                    i0 = max(0, floor e(high)), i1 = min(dim - 1, ceil e(low)) and
- *                    g = clamp((i - i0) / (i1 - i0), 0, 1): (1 - g) f_i + g f_i / factor
+ *                    g = clamp((i - i0) / (i1 - i0), 0, 1): (1 - g) f_i + g f_i / factor;
+ *                    i1 - i0 counts as 1/1000 where it is not positive: a step behind i0
  * Every cos and sin is multiplied by `attention` (0: 1, or 0.1 ln(factor) + 1
  * for AF1_ROPE_RAMP). The angles are FP64, the table is FP32. */
 #define AF1_ROPE_PLAIN 0
@@ -553,7 +554,8 @@ typedef struct af1_rope_params {
   int32_t scaling;   /* AF1_ROPE_* */
   double base;       /* > 1 */
   double factor;     /* >= 1 (ignored by AF1_ROPE_PLAIN) */
-  double low, high;  /* AF1_ROPE_BANDS: 0 < low < high; AF1_ROPE_RAMP: beta_slow < beta_fast */
+  double low, high;  /* 0 < low < high, turns within the original context: AF1_ROPE_BANDS (usually 1 and 4)
+                        divides below low and keeps above high; so does AF1_ROPE_RAMP (usually 1 and 32), by index */
   double original;   /* > 0 for AF1_ROPE_BANDS and AF1_ROPE_RAMP */
   double attention;  /* >= 0 */
 } af1_rope_params;

@@ -60,6 +60,14 @@ def test_default_bounds(P):
         assert kept[turns > high * 1.3].all() and not kept[turns < high / 1.3].any()
 
 
+def test_ramp_without_a_span(P):
+    """Both bounds at one index: a step behind it."""
+    for original, keeps in ((2 * math.pi * 0.01, 1), (2 * math.pi * 1e9, 32)):  # before the first index, after the last
+        got, _ = P.rope_frequencies(64, 10000.0, "ramp", 8.0, 1.0, 2.0, original)
+        f = 10000.0 ** (-2.0 * np.arange(32) / 64)
+        np.testing.assert_allclose(got, np.where(np.arange(32) < keeps, f, f / 8), rtol=1e-12)
+
+
 def test_refusals(P):
     for kw in (dict(dim=0), dict(dim=3), dict(dim=258), dict(dim=64, base=1.0), dict(dim=64, base=float("nan")),
                dict(dim=64, scaling="linear", factor=0.5), dict(dim=64, scaling="bands", original=0.0),
