@@ -716,8 +716,8 @@ typedef struct af1_tree_args {
   const uint32_t* mask;
   int64_t mask_seq;
   int64_t sequences, nodes, q_heads, page_columns, pages_ld;
-  float scale;
-  int32_t out_dtype;
+  float scale;       /* -1e30 .. 1e30 */
+  int32_t out_dtype; /* AF1_F16 or AF1_F32 */
 } af1_tree_args;
 AF1_API int64_t af1_tree_workspace_bytes(const af1_kv_cache* cache, int64_t sequences, int64_t nodes,
                                          int64_t q_heads);

@@ -785,7 +785,8 @@ int af1_tree_attention(const af1_kv_cache* c, const af1_tree_args* a, void* work
   if (!sizes_ok(c, a->sequences, a->nodes, a->q_heads)) return fail(AF1_ERR_INVALID_ARG, kSizes);
   if (a->out_dtype != AF1_F16 && a->out_dtype != AF1_F32)
     return fail(AF1_ERR_INVALID_ARG, "out_dtype must be AF1_F16 or AF1_F32");
-  if (!(std::abs(a->scale) <= 3e38f)) return fail(AF1_ERR_INVALID_ARG, "scale must be finite");
+  // With log2(e), a code's 2^24 and a key's scale it has to stay finite, as 0 times it is 0.
+  if (!(std::abs(a->scale) <= 1e30f)) return fail(AF1_ERR_INVALID_ARG, "scale must be -1e30..1e30");
   if (a->page_columns < 1 || a->pages_ld < a->page_columns || a->pages_ld > ((int64_t)1 << 40) ||
       a->page_columns > ((int64_t)1 << 30) / c->d.page_size)
     return fail(AF1_ERR_INVALID_ARG, "need page columns of at most 2^30 slots in all and pages_ld >= page_columns");

@@ -648,6 +648,22 @@ def test_default_workspace_clears_its_head_alone(P, nodes, group):
     assert not workspace[:head].any() and not zeros[:head].any()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("nodes", [1, 40])
+def test_largest_scale(P, kind, nodes):
+    """Scores of 0 stay 0 at the largest scale; larger ones, whose multiple by log2(e) is infinite, are refused."""
+    pool = Pool(P, kind, 2, 100, 1, 64, 16, seed=1)
+    q = np.zeros((2, nodes, 1, 64), np.float16)
+    sees = np.repeat(np.tril(np.ones((nodes, nodes), bool))[None], 2, 0)
+    lens = np.array([60, 7], np.int32)
+    for scale in (1e30, -1e30, 0.0):
+        check(P, pool, q, lens, None, None, rows_of(sees, [nodes] * 2), scale=scale)
+    for scale in (3e38, -3e38):
+        with pytest.raises(P.AF1Error) as e:
+            pool.cache.tree_attention(dev(q), pool.pages, dev(lens), scale=scale)
+        assert e.value.code == -1
+
+
 def test_workspace_checks_the_table(P):
     cache = P.KVCache.empty(4, 16, 2, 64, "int8")
     q, table = torch.zeros((2, 3, 4, 64), dtype=torch.float16, device="cuda"), torch.zeros((2, 2), device="cuda")
