@@ -588,7 +588,7 @@ typedef struct af1_rope_args {
   void* y;
   const int32_t* positions;
   const float* table;
-  int64_t tokens, heads, dim, rope_dim, length;
+  int64_t tokens, heads, dim, rope_dim, length; /* 0 .. 2^31, 1 .. 65536, even 2 .. 1024, even 2 .. dim, 1 .. 2^24 */
   int64_t x_token, x_head, y_token, y_head;
   int32_t dtype; /* AF1_F16 or AF1_F32 */
   int32_t flags; /* AF1_ROPE_INTERLEAVED, AF1_ROPE_BACKWARD */
@@ -642,7 +642,9 @@ AF1_API void af1_kv_free(af1_kv_cache* cache);
  *       slot is negative is padding: nothing is stored and its rows of q_out,
  *       k_out and v_out are zero. A token whose seq, slot or page lies outside
  *       the table or the cache is not stored. No two tokens may share a slot.
- *   pages: device int32 [sequences][page_columns], row stride pages_ld.
+ *   pages: device int32 [sequences][page_columns], row stride pages_ld; up to
+ *       65536 sequences and columns of fewer than 2^31 slots.
+ *   tokens: 0 .. 2^31; q_heads: 1 .. 65536.
  *   table, length, rope_dim, flags: rotation as in af1_rope (no BACKWARD);
  *       table NULL: none. positions: device int32 [tokens], or NULL: the slots.
  *   q, q_out: [tokens][q_heads][head_dim], q of `dtype`, q_out FP16; NULL: none.
@@ -667,6 +669,7 @@ typedef struct af1_kv_append_args {
 AF1_API int af1_kv_append(const af1_kv_cache* cache, const af1_kv_append_args* args, void* stream);
 
 /* Read slots first .. first + count - 1 of every sequence back.
+ *   pages: as in af1_kv_append. first, count: 0 .. 2^31 - 1.
  *   lens: device int32 [sequences]: slots at lens and after, and slots whose
  *       page lies outside the cache, give zeros.
  *   k_out, v_out: [sequences][count][kv_heads][head_dim] of `dtype`, contiguous.
@@ -692,6 +695,9 @@ AF1_API int af1_tree_mask(const int32_t* parents, int64_t sequences, int64_t nod
  *   q: FP16 [sequences][nodes][q_heads][head_dim], strides q_seq, q_node,
  *       q_head (multiples of 8), 16-byte aligned; q_heads is a multiple of the
  *       cache's kv_heads, head h reads cached head h / (q_heads / kv_heads).
+ *   sequences: 0 .. 1024 (append and read take more: attend to them in parts,
+ *       each with its rows of the table); nodes: 1 .. 64; q_heads: up to 65536;
+ *       the columns of the table: up to 2^30 slots.
  *   lens: device int32 [sequences] (negative: 0). counts: device int32
  *       [sequences] or NULL (all `nodes`). Slots beyond the table and slots
  *       whose page lies outside the cache are not seen.
@@ -739,7 +745,7 @@ AF1_API int af1_tree_attention(const af1_kv_cache* cache, const af1_tree_args* a
  * the largest value. Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
 typedef struct af1_logprob_args {
   const void* logits;
-  int64_t rows, vocab, ld;
+  int64_t rows, vocab, ld; /* 0 .. 2^24, 1 .. 2^31 - 1, vocab .. 2^36 */
   const int32_t* tokens;
   int64_t given;      /* 0 .. 1024 */
   float* logprobs;

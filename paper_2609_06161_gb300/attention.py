@@ -359,7 +359,8 @@ class KVCache:
         float16, over slots 0 .. lens - 1 and over the nodes' own slots as
         `mask` says (af1_tree_attention). mask: int32 (sequences or 1, nodes,
         words) from tree_mask, or None: each node sees the nodes up to itself.
-        counts: nodes of each sequence's tree. scale: default
+        At most 1024 sequences and 64 nodes. counts: nodes of each sequence's
+        tree. scale: default
         1 / sqrt(head_dim). out: float16 (default) or float32, the shape of q.
         lse: float32 (sequences, nodes, heads), optional."""
         qs = _steps(q, "q", 4)

@@ -664,6 +664,21 @@ def test_largest_scale(P, kind, nodes):
         assert e.value.code == -1
 
 
+def test_limits_of_sequences_nodes_and_heads(P):
+    """The largest of what the header allows, and the next."""
+    cache = P.KVCache.empty(1, 16, 1, 64, "int8")
+
+    def call(sequences=1, nodes=1, heads=1):
+        q = torch.zeros((sequences, nodes, heads, 64), dtype=torch.float16, device="cuda")
+        return cache.tree_attention(q, torch.zeros((sequences, 1), dtype=torch.int32, device="cuda"),
+                                    torch.zeros(sequences, dtype=torch.int32, device="cuda"))
+    assert not any(call(**most).any() for most in (dict(sequences=1024), dict(nodes=64), dict(heads=65536)))
+    for bad in (dict(sequences=1025), dict(nodes=65), dict(heads=65537)):
+        with pytest.raises(P.AF1Error) as e:
+            call(**bad)
+        assert e.value.code == -1
+
+
 def test_workspace_checks_the_table(P):
     cache = P.KVCache.empty(4, 16, 2, 64, "int8")
     q, table = torch.zeros((2, 3, 4, 64), dtype=torch.float16, device="cuda"), torch.zeros((2, 2), device="cuda")
