@@ -664,6 +664,68 @@ def test_largest_scale(P, kind, nodes):
         assert e.value.code == -1
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("nodes,group", [(5, 3), (40, 4)])  # either kernel
+@pytest.mark.parametrize("page", [16, 64, 256])
+def test_forms_of_both_kernels(P, kind, nodes, group, page):
+    """One mask for all sequences, scales of either sign and 0, strided queries and outputs, pages that do not exist (in
+    the prefix, below nodes, a whole tile of keys), slots beyond the table, negative lengths."""
+    g = gen(nodes + page)
+    seqs, heads, dim = 3, 2, 128
+    pool = Pool(P, kind, seqs, 700, heads, dim, page, seed=3)
+    slots = pool.columns * page
+    lens = np.array([300, 513, 640], np.int32)
+    _, sees = random_tree(g, 1, nodes)
+    mask = words(sees)
+    q = g.standard_normal((seqs, nodes, heads * group, dim)).astype(np.float16)
+    allowed = rows_of(np.repeat(sees, seqs, 0), [nodes] * seqs)
+    check(P, pool, q, lens, mask, None, allowed, scale=0.3)
+    check(P, pool, q, lens, mask, None, allowed, scale=0.0)
+    # A negative scale is the positive one of the opposite queries.
+    want, _, tol = attention(pool, -q, lens, allowed, 0.2)
+    out = pool.cache.tree_attention(dev(q), pool.pages, dev(lens), mask=dev(mask), scale=-0.2,
+                                    out=torch.empty(q.shape, device="cuda"))
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol)
+    # Strided queries and outputs.
+    ref, ref_lse, tol = attention(pool, q, lens, allowed, dim ** -0.5)
+    wide_q, wide_o = dev(np.zeros((seqs, nodes, heads * group, 256), np.float16)), torch.zeros(
+        (nodes, seqs, heads * group, 136), device="cuda")
+    wide_q[..., 128:] = dev(q)
+    out = wide_o.transpose(0, 1)[..., :128]
+    pool.cache.tree_attention(wide_q[..., 128:], pool.pages, dev(lens), mask=dev(mask), out=out)
+    assert np.all(np.abs(out.double().cpu().numpy() - ref) <= tol)
+    assert not wide_o[..., 128:].any()
+    # Pages that do not exist: what is there is as if it were outside every mask.
+    gone = pool.table.copy()
+    keep = np.ones((seqs, slots), bool)
+    lost = [(0, 0), (0, 290 // page), (1, 513 // page), (2, 128 // page), (2, 255 // page), (2, 655 // page)]
+    for n, (b, col) in enumerate(lost):
+        gone[b, col] = (-1, 10 ** 6, -(2 ** 31))[n % 3]
+        keep[b, page * col: page * col + page] = False
+    out = pool.cache.tree_attention(dev(q), dev(gone), dev(lens), mask=dev(mask), out=torch.empty(q.shape, device="cuda"))
+    for b in range(seqs):
+        for i in range(nodes):
+            see = keep[b].copy()
+            see[lens[b]:] = False
+            new = sees[0, i][: slots - lens[b]]
+            see[lens[b]: lens[b] + nodes][: len(new)] = new & keep[b, lens[b]: lens[b] + nodes]
+            for h in range(heads * group):
+                k, v = pool.k[b, see, h // group].astype(float), pool.v[b, see, h // group].astype(float)
+                x = q[b, i, h].astype(float)
+                e = k @ x * dim ** -0.5
+                w = np.exp(e - e.max()) if e.size else e
+                want = w @ v / w.sum() if e.size else np.zeros(dim)
+                four = kind == "int4"
+                far = dim ** -0.5 * (np.abs(k) @ np.abs(x)).max() if e.size else 0.0
+                ds = (U if four else 0.0) * far + 2 * E * dim * far + 4 * E * np.abs(e).max(initial=0)
+                a = w @ np.abs(v) / w.sum() if e.size else np.zeros(dim)
+                assert np.all(np.abs(out[b, i, h].double().cpu().numpy() - want) <=
+                              (U * (2 if four else 1) + 2 * ds + 2.0 ** -20) * a)
+    # Slots beyond the table are not there; negative lengths are 0.
+    short = np.array([slots, slots - 2, -3], np.int32)
+    check(P, pool, q, short, mask, None, allowed)
+
+
 def test_limits_of_sequences_nodes_and_heads(P):
     """The largest of what the header allows, and the next."""
     cache = P.KVCache.empty(1, 16, 1, 64, "int8")
