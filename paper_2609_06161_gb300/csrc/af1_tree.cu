@@ -429,6 +429,28 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
         vinv = vref > 0.f ? 1.f / vref : 0.f;
       }
 
+      // A node's infinite or NaN value (or scale of it) must reach the rows that
+      // see it, however small their weight, and no other, as 0 times it would:
+      // such steps sum entry by entry, with weights of at least 2^-120.
+      bool slow = false;
+      if (masked) {
+        bool odd = value_bad<KIND, DIM, KW>(vb, vsb, lane % KW, lane / KW, 32 / KW);
+        if constexpr (C::SCALED8) {  // scales past the end are never used
+          const int row = lane % KW;
+          odd |= key + row < k_end && !(bad >> (row / 16) & 1) && !(fabsf(reinterpret_cast<const float*>(vsb)[row]) < kInf);
+        }
+        slow = __any_sync(0xffffffffu, odd);
+        if (__builtin_expect(slow, 0)) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (s[mb][nt][i] > -kInf) s[mb][nt][i] = fmaxf(s[mb][nt][i], m[nt][i % 2] - kShift - 120.f);
+        }
+      }
+
       // Weights.
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -445,11 +467,7 @@ __global__ void __launch_bounds__(32 * W, CTAS) tree_kernel(const __grid_constan
           }
       }
 
-      // A node's infinite or NaN value must not reach the rows that do not
-      // see it, as 0 times it would: such steps sum entry by entry.
-      bool slow = false;
-      if (masked) slow = __any_sync(0xffffffffu, value_bad<KIND, DIM, KW>(vb, vsb, lane % KW, lane / KW, 32 / KW));
-      if (slow) {
+      if (__builtin_expect(slow, 0)) {
         for (int j = 0; j < KW; ++j) {
           const int from = (j % 8) * 4 + t;
           float vs = 1.f;

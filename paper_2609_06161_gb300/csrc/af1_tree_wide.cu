@@ -37,8 +37,9 @@
 // as the scores that it waits for come after them.)
 //
 // Infinities and NaN: the values of slots past the end are zeros, a node's
-// value that is not finite is left out of the product (0 times it would reach
-// the rows that do not see it) and added to the rows that see it at the end.
+// value that is not finite (or its scale) is left out of the product (0 times it
+// would reach the rows that do not see it) and added to the rows that see it at
+// the end.
 //
 // Bound: a softmax warp's chain of steps for a tile (wait, read, exponents,
 // agree, arrive), which queue in shared memory behind the decoders' stores and
@@ -105,7 +106,8 @@ struct Barriers {
   int issued[2];                            // of keys and values: the last tile whose copies were
   uint32_t code_bad[2][2], tile_bad[kNotes];   // bits: 16 keys each whose page is missing
   uint32_t nodes_bad[4][2];                 // by run that has keys: nodes whose value is not finite (values are
-                                            // decoded at most two tiles, so two such runs, ahead of their use)
+                                            // decoded at most two tiles, their scales, which come with the keys,
+                                            // three, so three such runs, ahead of their use)
   alignas(16) float top[2][2][kRows], sum[2][kRows];    // of the halves of a tile (by tile), and of a run
   alignas(16) float value_top[kNotes][4];        // by tile and warp: power of two above the values' scales
   // Parts of items that this CTA has left: of its first and of its last run.
@@ -444,7 +446,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             if constexpr (C::SCALED8) {
               if (!is_v) {
                 const int note = at % kNotes;
-                const float vs = reinterpret_cast<const float*>(sc)[BK + row];
+                float vs = reinterpret_cast<const float*>(sc)[BK + row];
+                if ((gone || node) && !(fabsf(vs) < kInf)) {
+                  if (!gone) atomicOr(&bar.nodes_bad[runs_done % 4][(key - run.len) / 32], 1u << ((key - run.len) % 32));
+                  vs = 0.f;
+                }
                 key_scale[note * BK + row] = reinterpret_cast<const float*>(sc)[row] * fabsf(p.scale_log2);
                 value_scale[note * BK + row] = vs;
                 // Non-negative floats order as their bits.
@@ -724,13 +730,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
               sum = add2(sum, add2(a, b));
               if constexpr (C::SCALED8) {
                 const float4 f = f8[i / 4];
-                const float2 wa = mul2(a, make_float2(f.x, f.y)), wb = mul2(b, make_float2(f.z, f.w));
-                if (masked) {  // 0 times any scale is 0
-                  a.x = a.x == 0.f ? 0.f : wa.x, a.y = a.y == 0.f ? 0.f : wa.y;
-                  b.x = b.x == 0.f ? 0.f : wb.x, b.y = b.y == 0.f ? 0.f : wb.y;
-                } else {
-                  a = wa, b = wb;
-                }
+                a = mul2(a, make_float2(f.x, f.y)), b = mul2(b, make_float2(f.z, f.w));
               }
               r[i / 2] = pack_half2(a.x, a.y), r[i / 2 + 1] = pack_half2(b.x, b.y);
             }
@@ -843,9 +843,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                   } else if constexpr (INT4) {
                     const uint32_t sc = reinterpret_cast<const uint32_t*>(vs)[e / 32];
                     y = fmaf((float)(v[e / 2] >> (e % 2 * 4) & 15), low_float(sc), high_float(sc));
-                  } else {
+                  } else {  // times a scale that is not finite, or, of a finite one, by code alone
+                    const float scale = *reinterpret_cast<const float*>(vs);
                     y = KIND == AF1_KV_INT8 ? (float)(int8_t)v[e]
                                             : __half2float(__half(__nv_cvt_fp8_to_halfraw(v[e], __NV_E4M3)));
+                    if (!(fabsf(scale) < kInf)) y *= scale;
                   }
                   y = __half2float(__float2half_rn(y));
                   if (!(fabsf(y) <= 65504.f)) x[i] += y;

@@ -493,6 +493,27 @@ def test_masked_places_hold_nan_and_infinity(P, kind, nodes, group):
     assert not np.isfinite(y[2, 1, :, 7]).any() and np.isfinite(y[2, 0]).all()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("nodes", [4, 40])
+def test_nan_values_of_the_least_weight(P, kind, nodes):
+    """A node's NaN or infinite value whose weight is e^-362: it still reaches the rows that see it, and no other."""
+    g = gen(15)
+    pool = Pool(P, kind, 2, 100, 1, 128, 16, seed=4)
+    lens = np.array([50, 35], np.int32)
+    odd = g.standard_normal((1, 1, 1, 128)).astype(np.float32)
+    odd[..., 9] = np.nan
+    for b in range(2):
+        pool.write("k", np.full((1, 1, 1, 128), -8, np.float32), [b], [lens[b] + 1])
+        pool.write("v", odd, [b], [lens[b] + 1])
+        odd[..., 9] = np.inf
+    q = np.full((2, nodes, 1, 128), 4, np.float16)
+    sees = np.repeat(np.tril(np.ones((nodes, nodes), bool))[None], 2, 0)
+    sees[:, 2:, 1] = False  # node 1 sees itself; so does one node more
+    sees[:, 3, 1] = True
+    y = check(P, pool, q, lens, words(sees), None, rows_of(sees, [nodes] * 2), want_lse=False)
+    assert not np.isfinite(y[:, [1, 3], 0, 9]).any() and np.isfinite(np.delete(y, [1, 3], 1)).all()
+
+
 @pytest.mark.parametrize("kind", ["f16", "int8"])
 @pytest.mark.parametrize("nodes", [5, 33])
 def test_infinite_values_among_empty_sequences(P, kind, nodes):
