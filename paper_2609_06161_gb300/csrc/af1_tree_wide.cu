@@ -22,10 +22,9 @@
 //             K-major, values with their entries along N). INT8 and E4M3 stay
 //             codes, exact in FP16; a key's scale multiplies the scores, a
 //             value's the weights (relative to a power of two that bounds the
-//             scales so far, which the exponents take in). INT4, which has a
-//             scale for each group of 32 entries, is rounded once to FP16, keys
-//             too: a score is off by about 2^-12 sqrt(sum (q k)^2). FP16 tiles
-//             arrive by TMA and are only looked at where a sequence ends;
+//             scales so far, which the exponents take in). INT4 has a scale and a
+//             low for each group of 32 entries: see below. FP16 tiles arrive by
+//             TMA and are only looked at where a sequence ends;
 //   16, 18    TMA copies of keys, and of values, one for up to 128 rows of a
 //             page, into the ring of codes (one warp for both took 0.65 us for
 //             each, which held up the decoders);
@@ -36,6 +35,20 @@
 // turn, as a test of a phase's parity needs. (The softmax skips phases of P V,
 // as the scores that it waits for come after them.)
 //
+// INT4. Values, code * scale + low, are rounded to FP16 once. Keys are not: with
+// scale = high + rest, high its first seven significant bits, (code - 7.5) high and
+// (code - 7.5) rest are FP16 numbers, and two products sum both; one product more
+// of 16 entries adds (low + 7.5 scale) times the sum of q over each group, that sum
+// and 7.5 times it in two FP16 parts each. So a score has the precision that
+// af1_tree.cu gives it (rounded keys made the outputs' error 7.8e-4 of the norm
+// where it is 3.2e-4, FP16 outputs alone 2.1e-4). The second part of the keys costs a third of the tensor time and of
+// shared memory, which for entries of 128 leaves values one operand tile and each
+// ring of codes one stage: 100 us for the tree of 64 below where rounded keys took 86,
+// 85 for 79 with entries of 64. (Keys in one operand tile of two parts, values in
+// two: 132 us; its halves in turn: 112; halves in a ring of three: 127; halves by
+// all eight warps: 120. A thread's fixed costs, waits and fences, are half of what
+// a tile takes it.)
+//
 // Infinities and NaN: the values of slots past the end are zeros, a node's
 // value that is not finite (or its scale) is left out of the product (0 times it
 // would reach the rows that do not see it) and added to the rows that see it at
@@ -44,9 +57,10 @@
 // Bound: a softmax warp's chain of steps for a tile (wait, read, exponents,
 // agree, arrive), which queue in shared memory behind the decoders' stores and
 // the products' operands. With all 128 rows in use a tile's exponents take 1024
-// cycles (16 a cycle), its products 1024; the chain takes 2600, 1.3 us: 87 us
-// for a tree of 64 nodes and 8 queries to a head over 32768 INT4 tokens of 8
-// heads (790 TFLOP/s; 0.64 of the issue slots, 0.37 of the tensor pipe). Where
+// cycles (16 a cycle), its products 1024, or 1600 of INT4; the chain takes 2200.
+// INT4 with entries of 128 is bound by the decoders of keys, 2500 and their waits:
+// 100 us for a tree of 64 nodes and 8 queries to a head over 32768 tokens of 8
+// heads (690 TFLOP/s of the attention's own operations). Where
 // CTAs have few tiles, it is what a run costs once (first pages, keys and q 6 us,
 // the first tile 2, join 5 to 10): 4 trees of 16 over 6001 E4M3 tokens take 32 us.
 // All waits are bounded; a wait that gives up sets the status word, and what
@@ -65,7 +79,6 @@ constexpr int kThreads = 608;
 constexpr int kSetupTiles = 8;
 constexpr int kRows = 128;
 constexpr int kOutAt = 2 * BK, kWeightsAt = 3 * BK;  // columns of tensor memory, behind two tiles of scores
-constexpr int kSlots = 2;      // operand tiles of keys, and of values
 constexpr int kNotes = 4;      // tiles whose scales and page bits are kept: keys are decoded up to three tiles ahead
 constexpr float kLeastScale = -60.f;  // of a value's scale's exponent: smaller ones count as 2^-60
 
@@ -76,12 +89,19 @@ struct Wide {
   static constexpr int OP = BK * DIM * 2;                    // bytes of an operand tile
   static constexpr int CODES = BK * C::RB;
   static constexpr int SCALES = (C::SCALED8 ? 2 : 1) * BK * C::SB;  // 8 bits: of keys and values, with the keys
+  // Operand tiles: two of keys, which of INT4 have two parts, then two of values
+  // (one where there is no room for two), then q.
+  static constexpr bool SPLIT = KIND == AF1_KV_INT4;
+  static constexpr int V_TILE = SPLIT ? 4 : 2, V_SLOTS = SPLIT && DIM == 128 ? 1 : 2;
   // Rings of codes (FP16: the operand tiles themselves). Decoders hold a stage
-  // only while they read it; 8-bit values of 128 entries have room for one.
-  static constexpr int K_STAGES = 2, V_STAGES = C::SCALED8 && DIM == 128 ? 1 : 2;
+  // only while they read it; where the room is short there is one.
+  static constexpr int K_STAGES = SPLIT && DIM == 128 ? 1 : 2, V_STAGES = !F16 && DIM == 128 ? 1 : 2;
   static constexpr int K_BYTES = CODES + SCALES, V_BYTES = CODES + (C::SCALED8 ? 0 : SCALES);
   static constexpr int RINGS = F16 ? 0 : K_STAGES * K_BYTES + V_STAGES * V_BYTES;
-  static constexpr int SMEM = (2 * kSlots + 1) * OP + RINGS + 2 * kNotes * BK * 4 + 1024;
+  // INT4: sums of q over the groups, and the groups' scales and lows.
+  static constexpr int GROUP_BYTES = SPLIT ? 2 * BK * 32 : 0;
+  static constexpr int SMEM =
+      (V_TILE + V_SLOTS + 1) * OP + GROUP_BYTES + RINGS + (C::SCALED8 ? 2 * kNotes * BK * 4 : 0) + 1024;
   static constexpr int PART = kRows * (DIM + 2);  // floats: o, m, l, each along the rows (to a multiple of 4 of them)
   static constexpr int COPIES = 10 * DIM / 8 * 16;  // bytes of a part for 4 rows, as it is joined
   static_assert(2 * COPIES * (kRows / 4) <= SMEM - 1024, "two parts are on their way");
@@ -100,6 +120,7 @@ struct Barriers {
   Plan plan;
   uint64_t op_ready[2][2], op_empty[2][2], code_full[2][2], code_empty[2][2];  // of keys and values
   uint64_t s_full[2], p_ready[2], pv_done[2], q_ready;  // by tile
+  uint64_t groups_empty;                    // INT4: the tile of the keys' groups
   uint64_t drained;                         // products, after a wait that gave up
   uint32_t tmem;
   volatile int gave_up;
@@ -109,6 +130,7 @@ struct Barriers {
                                             // decoded at most two tiles, their scales, which come with the keys,
                                             // three, so three such runs, ahead of their use)
   alignas(16) float top[2][2][kRows], sum[2][kRows];    // of the halves of a tile (by tile), and of a run
+  float q_scale[kRows];                     // INT4: what the rows of q were divided by
   alignas(16) float value_top[kNotes][4];        // by tile and warp: power of two above the values' scales
   // Parts of items that this CTA has left: of its first and of its last run.
   struct {
@@ -194,14 +216,17 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
 // between 64-entry groups where the entries run along M or N. The upper half of
 // the description is a constant.
 constexpr uint32_t kMatrixHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
+// Rows of 32 bytes, with a 32-byte swizzle, 8 of them 256 bytes apart.
+constexpr uint32_t kGroupsHigh = (256 >> 4) | 1u << 14 | 6u << 29;
 __device__ __forceinline__ uint32_t matrix(uint32_t addr, int lead) {
   return ((addr >> 4) & 0x3fffu) | (uint32_t)(lead >> 4) << 16;
 }
+template <uint32_t HIGH = kMatrixHigh>
 __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
   asm volatile(
       "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
       " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d),
-      "r"(a), "r"(b), "r"(idesc), "r"(accumulate ? 1u : 0u), "n"(kMatrixHigh)
+      "r"(a), "r"(b), "r"(idesc), "r"(accumulate ? 1u : 0u), "n"(HIGH)
       : "memory");
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
@@ -289,12 +314,17 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   __shared__ Barriers bar;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* ops = smem;
-  uint8_t* qt = smem + 2 * kSlots * S::OP;
-  uint8_t* codes = qt + S::OP;
+  uint8_t* qt = smem + (S::V_TILE + S::V_SLOTS) * S::OP;
+  uint8_t* groups_q = qt + S::OP;
+  uint8_t* groups_k = groups_q + S::GROUP_BYTES / 2;
+  uint8_t* codes = qt + S::OP + S::GROUP_BYTES;
   float* key_scale = reinterpret_cast<float*>(codes + S::RINGS);
   // Tile `at` of the CTA's (keys or values): its operand tile, and its codes
   // with the scales behind them.
-  auto op_tile = [&](bool is_v, int at) { return ops + ((is_v ? 2 : 0) + (at & 1)) * S::OP; };
+  auto op_slot = [&](bool is_v, int at) { return S::V_SLOTS == 1 && is_v ? 0 : at & 1; };
+  auto op_turn = [&](bool is_v, int at) { return S::V_SLOTS == 1 && is_v ? at : at >> 1; };
+  auto op_place = [&](bool is_v, int at) { return is_v ? S::V_TILE + op_slot(true, at) : (S::SPLIT ? 2 : 1) * (at & 1); };
+  auto op_tile = [&](bool is_v, int at) { return ops + op_place(is_v, at) * S::OP; };
   auto code_stage = [&](bool is_v, int at) { return is_v ? at % S::V_STAGES : at % S::K_STAGES; };
   auto code_turn = [&](bool is_v, int at) { return is_v ? at / S::V_STAGES : at / S::K_STAGES; };
   auto code_tile = [&](bool is_v, int at) {
@@ -321,6 +351,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     }
     mbar_init(&bar.q_ready, 8);
     mbar_init(&bar.drained, 1);
+    mbar_init(&bar.groups_empty, 1);
     bar.gave_up = 0, bar.parts = 0;
     bar.issued[0] = bar.issued[1] = -1;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -425,14 +456,15 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     for (; run.next(p, bar.plan); runs_done += run.tiles > 0) {
       const int n = run.tiles;
       for (int j = 0; j < n; ++j) {
-        const int at = tiles_done + j, st = code_stage(is_v, at), slot = at & 1;
+        const int at = tiles_done + j, st = code_stage(is_v, at), slot = op_slot(is_v, at);
         // Copies keep to budgets below a suspension, too. (Of the other waits, which
         // are for warps of this CTA, that cost 4 us of 86.)
         bool ok = true;
         if (p.wait_cycles >= kSuspend) ok = wait(&bar.code_full[is_v][st], code_turn(is_v, at) & 1);
         else if (!wait_phase(&bar.code_full[is_v][st], code_turn(is_v, at) & 1, p.wait_cycles)) bar.gave_up = 1, ok = false;
-        if constexpr (!F16) ok = wait(&bar.op_empty[is_v][slot], (at >> 1 & 1) ^ 1) && ok;
+        if (!F16 && S::V_SLOTS > 1) ok = wait(&bar.op_empty[is_v][slot], (op_turn(is_v, at) & 1) ^ 1) && ok;
         ok = __all_sync(0xffffffffu, ok);
+        const bool started = ok;
         const int key = run.k_begin + j * BK + row;
         const uint32_t bad = bar.code_bad[is_v][st];
         const bool gone = key >= run.k_end || (bad >> (row / 16) & 1);
@@ -473,7 +505,43 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&bar.code_empty[is_v][st]);  // the stage is read
+            if (S::V_SLOTS == 1)  // what it waits for, decoding does too: not before the row is read
+              ok = __all_sync(0xffffffffu, wait(&bar.op_empty[is_v][slot], (op_turn(is_v, at) & 1) ^ 1));
             const uint32_t swizzle = (uint32_t)(row & 7) << 4;
+            if (INT4 && !is_v) {
+#pragma unroll
+              for (int c = 0; c < C::GROUPS; ++c) {
+                const uint32_t scale2 = prmt(group[c], group[c], 0x1010), high2 = scale2 & 0xfff0fff0u;
+                const uint32_t rest2 = hsub2(scale2, high2);
+                const uint32_t w[4] = {in[c].x, in[c].y, in[c].z, in[c].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                  uint32_t h[4], r[4];
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    // As fraction bits of 64 + code, less 71.5.
+                    const uint32_t u = e == 0 ? w[q] << 4 : w[q] >> (4 * e - 4);
+                    const uint32_t code = hsub2((u & 0x00f000f0u) | 0x54005400u, 0x54785478u);
+                    h[e] = hmul2(code, high2), r[e] = hmul2(code, rest2);
+                  }
+                  uint8_t* at16 = to + (c >> 1) * (BK * 128) + ((((4 * c + q) & 7) << 4) ^ swizzle);
+                  *reinterpret_cast<uint4*>(at16) = make_uint4(h[0], h[1], h[2], h[3]);
+                  *reinterpret_cast<uint4*>(at16 + S::OP) = make_uint4(r[0], r[1], r[2], r[3]);
+                }
+              }
+              // Twice the low and twice the scale of each group; one tile of these.
+              ok = __all_sync(0xffffffffu, wait(&bar.groups_empty, (at & 1) ^ 1)) && ok;
+              if (ok) {
+#pragma unroll
+                for (int c = 0; c < 4; c += 2) {
+                  uint4 of = make_uint4(0, 0, 0, 0);
+                  if (c < C::GROUPS)
+                    of = make_uint4(prmt(group[c], group[c], 0x3232), prmt(group[c], group[c], 0x1010),
+                                    prmt(group[c + 1], group[c + 1], 0x3232), prmt(group[c + 1], group[c + 1], 0x1010));
+                  reinterpret_cast<uint4*>(groups_k + row * 32)[c / 2 ^ (row >> 2 & 1)] = of;
+                }
+              }
+            } else
 #pragma unroll
             for (int c = 0; c < C::RB / 16; ++c) {
               const uint32_t w[4] = {in[c].x, in[c].y, in[c].z, in[c].w};
@@ -529,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         fence_async();
         __syncwarp();
         if (lane == 0) {
-          if (!F16 && !ok) mbar_arrive(&bar.code_empty[is_v][st]);
+          if (!F16 && !started) mbar_arrive(&bar.code_empty[is_v][st]);
           mbar_arrive(&bar.op_ready[is_v][slot]);
         }
       }
@@ -544,6 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     // the weights' place is free too.
     const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0);
     const uint32_t q_matrix = matrix(smem_u32(qt), 16), op_matrix = matrix(smem_u32(ops), 16);
+    const uint32_t q_groups = matrix(smem_u32(groups_q), 16), k_groups = matrix(smem_u32(groups_k), 16);
     constexpr uint32_t kLead = (uint32_t)(BK * 128 - 16) >> 4 << 16;  // values: 64 entries in a group
     constexpr uint32_t kScores = 1u << 4 | (uint32_t)(BK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
     constexpr uint32_t kOutput = 1u << 4 | 1u << 16 | (uint32_t)(DIM >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
@@ -554,36 +623,47 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       for (int j = 0; j < n + 2; ++j) {
         const int at = tiles_done + j, buf = at & 1, turn = at >> 1 & 1;  // the tile two before: the same buffers
         const bool first = j < n, second = j >= 2;
+        auto output = [&] {
+          if (ok) {
+            const uint32_t b = op_matrix + kLead + op_place(true, at) * (S::OP >> 4);
+#pragma unroll
+            for (int ks = 0; ks < BK / 16; ++ks)
+              mma_ts(base + kOutAt, base + kWeightsAt + buf * (BK / 2) + ks * 8, b + (ks * 2048 >> 4), kOutput,
+                     j > 2 || ks > 0);
+          }
+          commit(&bar.pv_done[buf]);
+          commit(&bar.op_empty[1][op_slot(true, at)]);
+        };
         if (second) {
-          ok = wait(&bar.op_ready[1][buf], turn ^ 1) && ok;
+          ok = wait(&bar.op_ready[1][op_slot(true, at)], op_turn(true, at - 2) & 1) && ok;
           ok = wait(&bar.p_ready[buf], turn ^ 1) && ok;
+        }
+        if (S::V_SLOTS == 1) {  // the output's products free the one tile of values: at once
+          ok = __all_sync(0xffffffffu, ok);
+          fence_after();
+          if (second && elect()) output();
+          __syncwarp();
         }
         if (first) ok = wait(&bar.op_ready[0][buf], turn) && ok;
         ok = __all_sync(0xffffffffu, ok);
         fence_after();
         if (elect()) {
-          if (second) {
-            if (ok) {
-              const uint32_t b = op_matrix + kLead + (2 + buf) * (S::OP >> 4);
-#pragma unroll
-              for (int ks = 0; ks < BK / 16; ++ks)
-                mma_ts(base + kOutAt, base + kWeightsAt + buf * (BK / 2) + ks * 8, b + (ks * 2048 >> 4), kOutput,
-                       j > 2 || ks > 0);
-            }
-            commit(&bar.pv_done[buf]);
-            commit(&bar.op_empty[1][buf]);
-          }
+          if (S::V_SLOTS > 1 && second) output();
           if (first) {
             if (ok) {
-              const uint32_t b = op_matrix + buf * (S::OP >> 4);
+              const uint32_t b = op_matrix + op_place(false, at) * (S::OP >> 4);
 #pragma unroll
-              for (int ks = 0; ks < DIM / 16; ++ks) {
-                const int off = ((ks / 4) * (BK * 128) + (ks % 4) * 32) >> 4;
-                mma_ss(base + buf * BK, q_matrix + off, b + off, kScores, ks > 0);
-              }
+              for (int part = 0; part < (INT4 ? 2 : 1); ++part)
+#pragma unroll
+                for (int ks = 0; ks < DIM / 16; ++ks) {
+                  const int off = ((ks / 4) * (BK * 128) + (ks % 4) * 32) >> 4;
+                  mma_ss(base + buf * BK, q_matrix + off, b + part * (S::OP >> 4) + off, kScores, part + ks > 0);
+                }
+              if constexpr (INT4) mma_ss<kGroupsHigh>(base + buf * BK, q_groups, k_groups, kScores, true);
             }
             commit(&bar.s_full[buf]);
             commit(&bar.op_empty[0][buf]);
+            if constexpr (INT4) commit(&bar.groups_empty);
           }
         }
         __syncwarp();
@@ -595,7 +675,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     const int half = warp / 4;  // of a tile's keys, and of the output's entries
     const int row = threadIdx.x % 128;
     const uint32_t base = tmem + ((uint32_t)(warp % 4 * 32) << 16);
-    const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);  // -infinity times it stays so
+    float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);  // -infinity times it stays so
     const int e0 = half * (DIM / 2);
     for (; run.next(p, bar.plan); runs_done += run.tiles > 0) {
       const int n = run.tiles, rows = run.rows(p);
@@ -654,11 +734,44 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             v[i] = make_uint4(prmt(v[i].x, v[i].z, 0x5410), prmt(v[i].x, v[i].z, 0x7632),
                               prmt(v[i].y, v[i].w, 0x5410), prmt(v[i].y, v[i].w, 0x7632));
           v[i].x ^= sign, v[i].y ^= sign, v[i].z ^= sign, v[i].w ^= sign;
+          if constexpr (INT4) {
+            // The sum over each group of 32 entries (four lanes), in two FP16 parts, and
+            // 7.5 times it. Rows whose sums are too large for that are divided by 256,
+            // below which their largest entry stays above 1.
+            auto both = [](uint32_t h2) { return low_float(h2) + high_float(h2); };
+            float sum = (both(v[i].x) + both(v[i].y)) + (both(v[i].z) + both(v[i].w));
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            float most = fabsf(sum);
+#pragma unroll
+            for (int d = 4; d < CHUNKS; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            const bool large = most > 8192.f;
+            if (large) {
+              const uint32_t down = 0x1c001c00u;  // 1 / 256
+              v[i] = make_uint4(hmul2(v[i].x, down), hmul2(v[i].y, down), hmul2(v[i].z, down), hmul2(v[i].w, down));
+              sum *= 1.f / 256.f;
+            }
+            if (c == 0) bar.q_scale[r] = large ? 256.f : 1.f;
+            auto parts = [](float x) {
+              const float hi = __half2float(__float2half_rn(x));
+              return pack_half2(hi, x - hi);
+            };
+            const int at16 = (c / 8) ^ (r >> 2 & 1);
+            if (c % 4 == 0)
+              *reinterpret_cast<uint2*>(groups_q + r * 32 + at16 * 16 + c / 4 % 2 * 8) =
+                  make_uint2(parts(sum), parts(7.5f * sum));
+            if (C::GROUPS == 2 && c == 1)
+              *reinterpret_cast<uint4*>(groups_q + r * 32 + (at16 ^ 1) * 16) = make_uint4(0, 0, 0, 0);
+          }
           *reinterpret_cast<uint4*>(qt + (c >> 3) * (BK * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[i];
         }
         fence_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bar.q_ready);
+        if constexpr (INT4) {
+          named_sync(1, 256);
+          scale = fmaxf(fabsf(p.scale_log2), 1e-30f) * bar.q_scale[row];
+        }
       }
       const bool warp_real = (warp % 4) * 32 < rows;
       // Weights are 2^(score - m - ev + kShift), times a value's scale, which is below 2^ev.

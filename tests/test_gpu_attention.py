@@ -493,6 +493,45 @@ def test_masked_places_hold_nan_and_infinity(P, kind, nodes, group):
     assert not np.isfinite(y[2, 1, :, 7]).any() and np.isfinite(y[2, 0]).all()
 
 
+def exact_attention(pool, q, lens, scale):
+    """Causal attention of the nodes in 64 bits, as tensors on the GPU."""
+    k, v, x = (torch.from_numpy(t).cuda().double() for t in (pool.k, pool.v, q))
+    seqs, nodes, heads, _ = q.shape
+    out = torch.zeros(q.shape, dtype=torch.float64, device="cuda")
+    for b in range(seqs):
+        n = int(lens[b]) + nodes
+        hide = torch.ones((nodes, n), dtype=torch.bool, device="cuda").triu(1 + int(lens[b]))
+        for h in range(heads):
+            e = scale * (x[b, :, h] @ k[b, :n, h * k.shape[2] // heads].T)
+            out[b, :, h] = torch.softmax(e.masked_fill(hide, -math.inf), -1) @ v[b, :n, h * k.shape[2] // heads]
+    return out
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nodes", [3, 40, 64])
+@pytest.mark.parametrize("big", [1.0, 600.0, -2.0])
+def test_four_bit_keys_are_exact(P, dim, nodes, big):
+    """Scores of INT4 keys take the scale, low and code of each group as they are, whichever kernel a call takes.
+
+    What is left are the roundings to FP16 of each weight and each value, both of at most U and independent: of sums of
+    random terms sqrt(2 / 3) U of the norm. Rounded keys, with a few channels of six times the others, make that twice
+    as much. Queries of 600 have sums over a group that are beyond FP16; the scale undoes them."""
+    g = gen(16 + nodes)
+    pool = Pool(P, "int4", 1, 4000 + nodes, 2, dim, 64, seed=9)
+    k = pool.k * np.where(g.random((1, 1, 2, dim)) < 0.05, 6, 1).astype(np.float32)
+    k[..., :32] += 3  # a group off zero
+    pool.write("k", k)
+    q = (1.5 * g.standard_normal((1, nodes, 8, dim))).astype(np.float32)
+    if big == 600.0:
+        q = np.abs(q)  # sums of 32 entries above 8192, FP16 ends at 65504
+    q = (abs(big) * q).astype(np.float16)
+    scale = dim ** -0.5 / big
+    lens = np.array([4000], np.int32)
+    out = pool.cache.tree_attention(dev(q), pool.pages, dev(lens), scale=scale, out=torch.empty(q.shape, device="cuda"))
+    want = exact_attention(pool, q, lens, scale)
+    assert (out - want).norm() <= U * want.norm(), float((out - want).norm() / want.norm())
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("nodes", [4, 40])
 def test_nan_values_of_the_least_weight(P, kind, nodes):
