@@ -85,11 +85,17 @@ _token_logprobs = _declare("af1_token_logprobs", _P(_LogprobArgs), _vp)
 _memset = _declare("cudaMemsetAsync", _vp, ctypes.c_int, ctypes.c_size_t, _vp)
 
 
+# What torch.cuda.current_stream().cuda_stream gives, without building the stream object (3 us of a call's 14); a
+# torch without these functions takes the public way.
+_raw_stream, _raw_device = (getattr(torch._C, f, None) for f in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+
+
 def _stream_handle(stream) -> int:
     if stream is not None:
         return stream.cuda_stream
-    # What torch.cuda.current_stream().cuda_stream gives, without building the stream object (3 us of a call's 14).
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    if _raw_stream is None or _raw_device is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_raw_device())
 
 
 # Bytes at the front of a workspace that are zero between calls.

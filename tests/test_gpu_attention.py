@@ -786,6 +786,19 @@ def test_forms_of_both_kernels(P, kind, nodes, group, page):
     check(P, pool, q, short, mask, None, allowed)
 
 
+def test_stream_handles(P, monkeypatch):
+    """The current stream, also without torch's private functions."""
+    from paper_2609_06161_gb300 import attention as A
+    side = torch.cuda.Stream()
+    for missing in ((), ("_raw_stream",), ("_raw_stream", "_raw_device")):
+        for name in missing:
+            monkeypatch.setattr(A, name, None)
+        assert A._stream_handle(None) == torch.cuda.current_stream().cuda_stream
+        assert A._stream_handle(side) == side.cuda_stream
+        with torch.cuda.stream(side):
+            assert A._stream_handle(None) == side.cuda_stream
+
+
 def test_limits_of_sequences_nodes_and_heads(P):
     """The largest of what the header allows, and the next."""
     cache = P.KVCache.empty(1, 16, 1, 64, "int8")
