@@ -710,6 +710,12 @@ AF1_API int af1_tree_mask(const int32_t* parents, int64_t sequences, int64_t nod
  *   workspace: af1_tree_workspace_bytes bytes, with the rules of
  *       af1_linear_forward (256-byte aligned, the first 65792 bytes zero
  *       before first use); one workspace serves both.
+ * Precision: scores are FP32 sums of q and the values that the cache holds for
+ * keys. Weights are rounded to FP16 relative to the largest so far (11 bits down
+ * to 2^-28 of it), values of AF1_KV_INT4 to FP16. Of AF1_KV_INT8 and AF1_KV_E4M3 the
+ * weights are relative to the largest scale of a value so far, too: values whose
+ * scale is below 2^-20 of that, or in products of 128 rows below 2^-60, add fewer
+ * bits. Sums, maxima and outputs before their own rounding are FP32.
  * An infinite or NaN key or value reaches the nodes that see it and no other.
  * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, WORKSPACE, CUDA. */
 typedef struct af1_tree_args {

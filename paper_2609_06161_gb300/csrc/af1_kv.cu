@@ -379,8 +379,8 @@ struct AppendProblem {
 // thread's part (or, interleaved, in its own) and are read beside them: the
 // second read hits L1, and no exchange between threads depends on rope_dim.
 // Issue slots and bytes in flight bound it: 8192 tokens of 8 x 128 to INT4, with
-// the values back, take 20 us, 4.0 TB/s (without reading ahead 6 us more; ahead
-// by two rounds, with the pairs by shuffles, 4 more).
+// the values back, take 20.9 us, 3.9 TB/s (without reading ahead 6 us more; ahead
+// by two rounds, with the pairs by shuffles, 3 more).
 template <int KIND, int DIM, typename T, bool VEC, bool IL>
 __global__ void __launch_bounds__(kThreads, 4) append_kernel(const __grid_constant__ AppendProblem p) {
   if ((int)blockIdx.x >= p.kv_blocks) {
@@ -918,8 +918,8 @@ int af1_kv_append(const af1_kv_cache* c, const af1_kv_append_args* a, void* stre
   p.tokens = a->tokens;
   // A thread takes several heads of its token (one turn for all of them) where
   // there are tokens enough to give every SM 1024 threads all the same: 8192
-  // tokens of 8 x 128 as INT4 with their values took 37 us with one head to a
-  // thread, 27 with two, 23 with four and 22 with eight.
+  // tokens of 8 x 128 as INT4 with their values take 35 us with one head to a
+  // thread, 26 with two, 22.5 with four and 20.9 with eight.
   const int64_t threads = 2 * a->tokens * (dim / 8) * heads;
   const int take = (int)std::max<int64_t>(1, std::min<int64_t>(8, threads / (1024 * (int64_t)c->num_sms)));
   p.parts = (heads + take - 1) / take;

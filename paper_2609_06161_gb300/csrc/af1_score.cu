@@ -27,10 +27,11 @@
 // the GPU), and its first CTA joins their statistics and lists through
 // distributed shared memory. Logits come by asynchronous copies, three batches of a
 // warp in flight. Large calls are bound by device memory and the look back:
-// those 512 rows take 32.5 us (4.0 TB/s), 26 without the largest; the pass
+// those 512 rows take 33.4 us (3.9 TB/s), 27 without the largest; the pass
 // itself costs one exponent and about five instructions an entry (pairs of
-// entries share FP32 additions and multiply-adds). Small calls are bound by the
-// latency of lists and joins: 5 rows of 32000 FP32 logits take 7 us.
+// entries share FP32 additions, products and multiply-adds). Small launches are bound
+// by the latency of lists and joins: 5 rows of 32000 FP32 logits take 7.5 us on the
+// GPU (a call from Python, which allocates four outputs, 20).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, 5) score_kernel(const __grid_constan
   constexpr int E = 16 / (int)sizeof(T);  // entries of a 16-byte access
   constexpr int U = 4;                    // accesses of a batch: 16 or 32 entries to a lane
   constexpr bool HALF = sizeof(T) == 2;
-  constexpr int STAGES = TOP && !HALF ? 3 : 4;  // batches of a warp's ring: 48 KB in all
+  constexpr int STAGES = TOP && !HALF ? 3 : 4;  // batches of a warp's ring: 24 or 32 KB for the CTA's
   __shared__ uint4 ring[kWarps][STAGES][U][32];  // each lane reads what it has copied itself
   __shared__ Stats stats[kWarps];
   __shared__ uint64_t lists[kWarps][32];

@@ -730,10 +730,10 @@ int fail(int code, const std::string& msg) { return set_error(code, "af1_tree_at
 // Blocks of 8 rows (of every query head and node that share a cached head) that
 // a CTA has; 0: the tensor-core kernel, whose products have 128 rows. Going
 // over the keys again for 16 rows more did not pay: 4 sequences of up to 6001
-// tokens with 20 rows of E4M3 took 32 us and 31 there, 24 of INT4 32 and 26, 32
-// of FP16 33 and 28, of INT8 33 and 32; 64 of E4M3 47 and 33. (32 short
-// sequences of 32 rows of INT8 42 and 46.) Blocks of 32 rows, which leave an
-// SM 8 warps, were no better.
+// tokens with 20 rows of E4M3 took 32 us where 30 are taken there, 24 of INT4 32
+// and 31, 32 of FP16 33 and 30, of INT8 33 and 31; 64 of E4M3 47 and 31. (It was a
+// tenth faster for 32 short sequences of 32 rows of INT8.) Blocks of 32 rows, which
+// leave an SM 8 warps, were no better.
 int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 0; }
 
 int64_t workspace_bytes(const af1_kv_cache& c, int64_t rows) {

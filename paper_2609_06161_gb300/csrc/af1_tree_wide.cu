@@ -30,8 +30,8 @@
 //             each, which held up the decoders);
 //   17        one lane issues the products. (A lane each for Q K^T and P V, and a
 //             wait more for the softmax, took 2 % longer.)
-// Keys and values each have a ring of codes and two operand tiles, with
-// barriers of their own: whoever waits on a barrier meets each of its phases in
+// Keys and values each have a ring of codes and two operand tiles (but as said
+// below), with barriers of their own: whoever waits on a barrier meets each of its phases in
 // turn, as a test of a phase's parity needs. (The softmax skips phases of P V,
 // as the scores that it waits for come after them.)
 //
@@ -41,13 +41,14 @@
 // of 16 entries adds (low + 7.5 scale) times the sum of q over each group, that sum
 // and 7.5 times it in two FP16 parts each. So a score has the precision that
 // af1_tree.cu gives it (rounded keys made the outputs' error 7.8e-4 of the norm
-// where it is 3.2e-4, FP16 outputs alone 2.1e-4). The second part of the keys costs a third of the tensor time and of
-// shared memory, which for entries of 128 leaves values one operand tile and each
-// ring of codes one stage: 100 us for the tree of 64 below where rounded keys took 86,
-// 85 for 79 with entries of 64. (Keys in one operand tile of two parts, values in
-// two: 132 us; its halves in turn: 112; halves in a ring of three: 127; halves by
-// all eight warps: 120. A thread's fixed costs, waits and fences, are half of what
-// a tile takes it.)
+// where it is 3.2e-4, FP16 outputs alone 2.1e-4; where products with the rest are
+// subnormal, for scales below 2^-13, each is off by 2^-25). The second part costs a
+// third of the tensor time and of shared memory, which for entries of 128 leaves
+// values one operand tile and each ring of codes one stage: 100 us for the tree of
+// 64 below where rounded keys took 87, 79 with entries of 64 for 71. (Keys in
+// one operand tile of two parts, values in two: 132 us; its halves in turn: 112;
+// halves in a ring of three: 127; halves by all eight warps: 120. A thread's fixed
+// costs, waits and fences, are half of what a tile takes it.)
 //
 // Infinities and NaN: the values of slots past the end are zeros, a node's
 // value that is not finite (or its scale) is left out of the product (0 times it
@@ -57,12 +58,13 @@
 // Bound: a softmax warp's chain of steps for a tile (wait, read, exponents,
 // agree, arrive), which queue in shared memory behind the decoders' stores and
 // the products' operands. With all 128 rows in use a tile's exponents take 1024
-// cycles (16 a cycle), its products 1024, or 1600 of INT4; the chain takes 2200.
-// INT4 with entries of 128 is bound by the decoders of keys, 2500 and their waits:
-// 100 us for a tree of 64 nodes and 8 queries to a head over 32768 tokens of 8
-// heads (690 TFLOP/s of the attention's own operations). Where
-// CTAs have few tiles, it is what a run costs once (first pages, keys and q 6 us,
-// the first tile 2, join 5 to 10): 4 trees of 16 over 6001 E4M3 tokens take 32 us.
+// cycles (16 a cycle), its products 1024, or 1600 of INT4; the chain takes 2200:
+// 91 us for a tree of 64 nodes and 8 queries to a head over 32768 FP16 tokens of 8
+// heads (760 TFLOP/s), 98 of E4M3, 101 of INT8, whose scales every row reads. INT4
+// with entries of 128 is bound by the decoders of keys, 2500 cycles and their waits
+// (100 us; 0.58 of the issue slots, 0.48 of the tensor pipe). Where CTAs have few
+// tiles, it is what a run costs once (first pages, keys and q 6 us, the first tile
+// 2, join 5 to 10): 4 trees of 16 over 6001 E4M3 tokens take 31 us.
 // All waits are bounded; a wait that gives up sets the status word, and what
 // depends on it is skipped. Where one has, no copy is issued any more, and before
 // shared or tensor memory changes hands the copies and products in flight end.
@@ -74,8 +76,8 @@ namespace {
 constexpr int BK = 128;        // keys of a tile
 constexpr int kThreads = 608;
 // Tiles that a run's beginning and end are worth. (4 trees of 16 over 6001 E4M3
-// tokens, 16 of them over 2000, one of 64 over 32768 INT4 tokens: 36, 40 and 91 us
-// with 4 tiles, 31, 40 and 89 with 5, 32, 38 and 87 with 8.)
+// tokens, 16 of them over 2000, one of 64 over 32768 INT4 tokens: 35, 38 and 107 us
+// with 4 tiles, 30, 38 and 105 with 5, 31, 37 and 100 with 8.)
 constexpr int kSetupTiles = 8;
 constexpr int kRows = 128;
 constexpr int kOutAt = 2 * BK, kWeightsAt = 3 * BK;  // columns of tensor memory, behind two tiles of scores
