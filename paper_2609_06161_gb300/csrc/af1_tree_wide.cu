@@ -40,9 +40,12 @@
 // (code - 7.5) rest are FP16 numbers, and two products sum both; one product more
 // of 16 entries adds (low + 7.5 scale) times the sum of q over each group, that sum
 // and 7.5 times it in two FP16 parts each. So a score has the precision that
-// af1_tree.cu gives it (rounded keys made the outputs' error 7.8e-4 of the norm
-// where it is 3.2e-4, FP16 outputs alone 2.1e-4; where products with the rest are
-// subnormal, for scales below 2^-13, each is off by 2^-25). The second part costs a
+// af1_tree.cu gives it; where products with the rest are subnormal, for scales
+// below 2^-13, each is off by 2^-25. What is left are roundings of weights and
+// values; of the largest weight of every 32 what rounding adds is added to the
+// divisor, too, where it cancels most of what it adds to the output. (Rounded keys made
+// the outputs' error 7.8e-4 of the norm, weights as if not rounded 3.2e-4; it is
+// 3.0e-4, FP16 outputs alone 2.1e-4.) The second part costs a
 // third of the tensor time and of shared memory, which for entries of 128 leaves
 // values one operand tile and each ring of codes one stage: 100 us for the tree of
 // 64 below where rounded keys took 87, 79 with entries of 64 for 71. (Keys in
@@ -132,6 +135,7 @@ struct Barriers {
                                             // decoded at most two tiles, their scales, which come with the keys,
                                             // three, so three such runs, ahead of their use)
   alignas(16) float top[2][2][kRows], sum[2][kRows];    // of the halves of a tile (by tile), and of a run
+  float over[2][kRows];                     // INT4: what rounding has added to the largest weights
   float q_scale[kRows];                     // INT4: what the rows of q were divided by
   alignas(16) float value_top[kNotes][4];        // by tile and warp: power of two above the values' scales
   // Parts of items that this CTA has left: of its first and of its last run.
@@ -777,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       }
       const bool warp_real = (warp % 4) * 32 < rows;
       // Weights are 2^(score - m - ev + kShift), times a value's scale, which is below 2^ev.
-      float m = -kInf, l = 0.f, ev = C::SCALED8 ? kLeastScale : 0.f;
+      float m = -kInf, l = 0.f, l_over = 0.f, ev = C::SCALED8 ? kLeastScale : 0.f;
       bool ok = true;
       for (int j = 0; j < n; ++j) {
         const int key = run.k_begin + j * BK, at = tiles_done + j, buf = at & 1;
@@ -809,9 +813,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         };
         // The half's weights relative to `ref`, and its largest score.
         float2 sum;
+        float over;
         auto pass = [&](float ref) {
           float most = -kInf;
-          sum = make_float2(0.f, 0.f);
+          sum = make_float2(0.f, 0.f), over = 0.f;
 #pragma unroll 1
           for (int c = 0; c < BK / 2; c += COLS) {
             float x[COLS];
@@ -837,7 +842,12 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             float t0 = x[0], t1 = x[1];
 #pragma unroll
             for (int i = 2; i < COLS - 2; i += 4) t0 = max3(t0, x[i], x[i + 1]), t1 = max3(t1, x[i + 2], x[i + 3]);
-            most = max3(most, max3(t0, x[COLS - 2], x[COLS - 1]), t1);
+            t0 = max3(t0, x[COLS - 2], x[COLS - 1]);
+            most = max3(most, t0, t1);
+            if constexpr (INT4) {  // the largest weight, as above
+              const float w = ex2(fmaxf(t0, t1));
+              over += __half2float(__float2half_rn(w)) - w;
+            }
             uint32_t r[COLS / 2];
 #pragma unroll
             for (int i = 0; i < COLS; i += 4) {
@@ -873,7 +883,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             const float now = fmaxf(m, top);
             const float alpha = ex2(m - (now == -kInf ? 0.f : now) + (ev - ev_now));
             m = now, ev = ev_now;
-            l *= alpha;
+            l *= alpha, l_over *= alpha;
             if (j > 0) {
               ok = wait(&bar.pv_done[buf ^ 1], (at - 1) >> 1 & 1);
               ok = __all_sync(0xffffffffu, ok);
@@ -894,7 +904,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             pass(reference());
           }
         }
-        if (work) l += sum.x + sum.y;
+        if (work) l += sum.x + sum.y, l_over += over;
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bar.p_ready[buf]);
@@ -904,6 +914,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       {
         const int last = tiles_done + n - 1;
         bar.sum[half][row] = l;
+        if constexpr (INT4) bar.over[half][row] = l_over;
         ok = wait(&bar.pv_done[last & 1], last >> 1 & 1) && ok;
         fence_after();
         ok = __all_sync(0xffffffffu, ok);
@@ -912,6 +923,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         named_sync(1, 256);
         if (threadIdx.x == 0) bar.nodes_bad[runs_done % 4][0] = bar.nodes_bad[runs_done % 4][1] = 0;
         const float sum = l + bar.sum[half ^ 1][row];
+        // What rounding adds to the largest weights, and so to the output, it adds to the
+        // divisor, too (of the output: lse takes the sum of what they were before).
+        const float even = INT4 && sum > 0.f ? sum / (sum + (l_over + bar.over[half ^ 1][row])) : 1.f;
         const bool whole = run.from <= kSetupTiles && run.to == run.units;
         int c0 = 0, c1 = 0, node, head;
         if (!whole)
@@ -941,6 +955,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           for (int c = e0; c < e0 + DIM / 2; c += 32) {
             float x[32];
             tmem_load(base + kOutAt + c, x);
+            if constexpr (INT4) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] *= even;
+            }
             if (poison != 0) {  // infinite and NaN values of nodes that this row sees
               for (uint64_t left = poison; left != 0; left &= left - 1) {
                 const int slot = run.len + __ffsll((long long)left) - 1;
