@@ -93,3 +93,9 @@ def test_linears_and_tree_attention(P):
     shared(P, [linear(layer, 8192, t) for t in (1, 16, 150, 2048)] +
               [attention(P, "int8", 1, 4, [4000, 30, 0, 1777]), attention(P, "f16", 3, 4, [4090, 3000]),
                attention(P, "int4", 33, 4, [4000, 30, 0, 1777]), attention(P, "e4m3", 64, 8, [2500, 4000])])
+
+
+def test_more_counters_than_the_head_holds(P):
+    """131400 rows: 8216 tiles at 2000 tokens, whose counters lie behind the scratch, where others have theirs."""
+    big, c = make(P, 36, 131400, 8192, 64), make(P, 34, 256, 256, 9000)
+    shared(P, [linear(big, 8192, 2000), linear(big, 8192, 2), linear(c, 256, 2048), linear(c, 256, 1200)])
