@@ -47,8 +47,8 @@
 // the outputs' error 7.8e-4 of the norm, weights as if not rounded 3.2e-4; it is
 // 3.0e-4, FP16 outputs alone 2.1e-4.) The second part costs a
 // third of the tensor time and of shared memory, which for entries of 128 leaves
-// values one operand tile and each ring of codes one stage: 100 us for the tree of
-// 64 below where rounded keys took 87, 79 with entries of 64 for 71. (Keys in
+// values one operand tile and each ring of codes one stage: 99 us for the tree of
+// 64 below where rounded keys took 87, 78 with entries of 64 for 71. (Keys in
 // one operand tile of two parts, values in two: 132 us; its halves in turn: 112;
 // halves in a ring of three: 127; halves by all eight warps: 120. A thread's fixed
 // costs, waits and fences, are half of what a tile takes it.)
@@ -65,7 +65,7 @@
 // 91 us for a tree of 64 nodes and 8 queries to a head over 32768 FP16 tokens of 8
 // heads (760 TFLOP/s), 98 of E4M3, 101 of INT8, whose scales every row reads. INT4
 // with entries of 128 is bound by the decoders of keys, 2500 cycles and their waits
-// (100 us; 0.58 of the issue slots, 0.48 of the tensor pipe). Where CTAs have few
+// (99 us; 0.58 of the issue slots, 0.48 of the tensor pipe). Where CTAs have few
 // tiles, it is what a run costs once (first pages, keys and q 6 us, the first tile
 // 2, join 5 to 10): 4 trees of 16 over 6001 E4M3 tokens take 31 us.
 // All waits are bounded; a wait that gives up sets the status word, and what
@@ -80,7 +80,7 @@ constexpr int BK = 128;        // keys of a tile
 constexpr int kThreads = 608;
 // Tiles that a run's beginning and end are worth. (4 trees of 16 over 6001 E4M3
 // tokens, 16 of them over 2000, one of 64 over 32768 INT4 tokens: 35, 38 and 107 us
-// with 4 tiles, 30, 38 and 105 with 5, 31, 37 and 100 with 8.)
+// with 4 tiles, 30, 38 and 105 with 5, 31, 37 and 99 with 8.)
 constexpr int kSetupTiles = 8;
 constexpr int kRows = 128;
 constexpr int kOutAt = 2 * BK, kWeightsAt = 3 * BK;  // columns of tensor memory, behind two tiles of scores
@@ -656,6 +656,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         if (elect()) {
           if (S::V_SLOTS > 1 && second) output();
           if (first) {
+            if constexpr (INT4) {  // first: the decoders wait for the one tile of groups
+              if (ok) mma_ss<kGroupsHigh>(base + buf * BK, q_groups, k_groups, kScores, false);
+              commit(&bar.groups_empty);
+            }
             if (ok) {
               const uint32_t b = op_matrix + op_place(false, at) * (S::OP >> 4);
 #pragma unroll
@@ -663,13 +667,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
 #pragma unroll
                 for (int ks = 0; ks < DIM / 16; ++ks) {
                   const int off = ((ks / 4) * (BK * 128) + (ks % 4) * 32) >> 4;
-                  mma_ss(base + buf * BK, q_matrix + off, b + part * (S::OP >> 4) + off, kScores, part + ks > 0);
+                  mma_ss(base + buf * BK, q_matrix + off, b + part * (S::OP >> 4) + off, kScores, INT4 || ks > 0);
                 }
-              if constexpr (INT4) mma_ss<kGroupsHigh>(base + buf * BK, q_groups, k_groups, kScores, true);
             }
             commit(&bar.s_full[buf]);
             commit(&bar.op_empty[0][buf]);
-            if constexpr (INT4) commit(&bar.groups_empty);
           }
         }
         __syncwarp();
