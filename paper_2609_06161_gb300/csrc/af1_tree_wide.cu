@@ -43,15 +43,16 @@
 // af1_tree.cu gives it; where products with the rest are subnormal, for scales
 // below 2^-13, each is off by 2^-25. What is left are roundings of weights and
 // values; of the largest weight of every 32 what rounding adds is added to the
-// divisor, too, where it cancels most of what it adds to the output. (Rounded keys made
-// the outputs' error 7.8e-4 of the norm, weights as if not rounded 3.2e-4; it is
-// 3.0e-4, FP16 outputs alone 2.1e-4.) The second part costs a
-// third of the tensor time and of shared memory, which for entries of 128 leaves
-// values one operand tile and each ring of codes one stage: 99 us for the tree of
-// 64 below where rounded keys took 87, 78 with entries of 64 for 71. (Keys in
-// one operand tile of two parts, values in two: 132 us; its halves in turn: 112;
-// halves in a ring of three: 127; halves by all eight warps: 120. A thread's fixed
-// costs, waits and fences, are half of what a tile takes it.)
+// divisor, too, where it cancels most of what it adds to the output. (Rounded
+// keys made the outputs' error 7.8e-4 of the norm, weights as if not rounded 3.2e-4;
+// it is 3.0e-4, FP16 outputs alone 2.1e-4. All weights as rounded in the divisor:
+// 3.0e-4 and a tenth slower; the same for 8 bits: 2.3e-4 for 2.9e-4, but 118 us for
+// 101.) The second part costs a third of the tensor time and of shared memory, which
+// for entries of 128 leaves values one operand tile and each ring of codes one
+// stage: 99 us for the tree of 64 below where rounded keys took 87, 78 with entries
+// of 64 for 71. (Keys in one operand tile of two parts, values in two: 132 us; its
+// halves in turn: 112; halves in a ring of three: 127; halves by all eight warps:
+// 120. A thread's fixed costs, waits and fences, are half of what a tile takes it.)
 //
 // Infinities and NaN: the values of slots past the end are zeros, a node's
 // value that is not finite (or its scale) is left out of the product (0 times it
@@ -64,8 +65,9 @@
 // cycles (16 a cycle), its products 1024, or 1600 of INT4; the chain takes 2200:
 // 91 us for a tree of 64 nodes and 8 queries to a head over 32768 FP16 tokens of 8
 // heads (760 TFLOP/s), 98 of E4M3, 101 of INT8, whose scales every row reads. INT4
-// with entries of 128 is bound by the decoders of keys, 2500 cycles and their waits
-// (99 us; 0.58 of the issue slots, 0.48 of the tensor pipe). Where CTAs have few
+// with entries of 128 is bound by the decoders: of keys, 2500 cycles and their waits,
+// and of values, which wait for the products with those before (2700; together 99
+// us, 0.58 of the issue slots, 0.48 of the tensor pipe). Where CTAs have few
 // tiles, it is what a run costs once (first pages, keys and q 6 us, the first tile
 // 2, join 5 to 10): 4 trees of 16 over 6001 E4M3 tokens take 31 us.
 // All waits are bounded; a wait that gives up sets the status word, and what
