@@ -173,7 +173,8 @@ def _randint(g, lo, hi, *shape):
 def _logits(g, rows, vocab):
     """Most entries unlikely, a few that the model thinks likely."""
     x = _randn(g, rows, vocab).mul_(2.5)
-    top = torch.randint(0, vocab, (rows, 6), generator=g, device=DEVICE)
+    part = vocab // 6  # each in a part of its own: no place is written twice
+    top = torch.arange(6, device=DEVICE) * part + torch.randint(0, part, (rows, 6), generator=g, device=DEVICE)
     return x.scatter_(1, top, 11 + 2 * _randn(g, rows, 6))
 
 
