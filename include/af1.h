@@ -765,6 +765,156 @@ typedef struct af1_logprob_args {
 } af1_logprob_args;
 AF1_API int af1_token_logprobs(const af1_logprob_args* args, void* stream);
 
+/* Probabilities of rows of logits, as sampling takes them:
+ *   p_i = e^((x_i - M) / T) / S for the entries that are kept, 0 for the others;
+ *   M = max x, S the sum of the kept e^((x_i - M) / T).
+ * Kept are the top_k largest (equal ones by ascending index; top_k below 1 or
+ * at least vocab: all) that are at least min_p times as likely as the largest:
+ * x_i >= M + T ln(min_p), compared in FP64; min_p is taken as 0 .. 1 (NaN: 0).
+ * T below 1e-30 (or NaN) is greedy: 1 for the first largest entry; T above 1e30
+ * counts as 1e30.
+ *   logits: [rows][vocab] of `dtype`, row stride ld; -infinity bans a token.
+ *   temperature, top_k, min_p: device [rows], each row's own, or NULL: the
+ *       scalar beside it for all rows.
+ *   probs: FP32 [rows][vocab], row stride probs_ld.
+ * A row of -infinity alone gives zeros, one with a NaN or +infinity NaN
+ * everywhere. Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
+typedef struct af1_probs_args {
+  const void* logits;
+  int64_t rows, vocab, ld; /* 0 .. 2^24, 1 .. 2^31 - 1, vocab .. 2^36 */
+  float* probs;
+  int64_t probs_ld;        /* vocab .. 2^36 */
+  const float* temperature;
+  const int32_t* top_k;
+  const float* min_p;
+  float all_temperature;
+  int32_t all_top_k;
+  float all_min_p;
+  int32_t dtype;           /* AF1_F16 or AF1_F32 */
+} af1_probs_args;
+AF1_API int af1_token_probs(const af1_probs_args* args, void* stream);
+
+/* Drafted tokens verified against the target's probabilities with given random
+ * numbers, so that what comes out is distributed as the target's own samples.
+ * Node 0 of a sequence's tree is its last token, which needs no verification;
+ * the walk begins there. At a node `at`, with P = probs[at], Q = draft[at], c = 0,
+ * Z = Z' = 1 and nothing rejected, its children (the nodes whose parent it is)
+ * are looked at in ascending order. A child of token x and number u is
+ * accepted, and the walk goes on there, if
+ *     u Q(x) Z < r Z',   r = max(P(x) - c Q(x), 0), 0 if x was rejected here.
+ * Otherwise x is rejected here: c += Z / Z'; with AF1_VERIFY_DISTINCT Z' -= Q(x)
+ * (siblings drawn from Q without repetition; otherwise each is a draw of its
+ * own); Z = sum of R, R(v) = max(P(v) - c Q(v), 0) and 0 for the rejected.
+ * Without a draft the children are guesses: accepted if u Z < r, r = P(x) or 0
+ * if x was rejected here; otherwise Z -= r.
+ * Where no child is accepted the walk ends, and the token that follows is drawn
+ * from R: the first v for which R(0) + .. + R(v) exceeds uniforms[0] times the
+ * sum of R. (Of P where R has no mass; -1 where P has none, and where a tree has no node.)
+ *   probs, draft: FP32 [sequences][nodes][vocab] with strides, rows that sum to 1;
+ *       entries count as 0 .. 1 (NaN: 0). draft NULL: guesses. Rows of nodes that
+ *       the walk does not come to are not read.
+ *   tokens, parents: device int32 [sequences][nodes]; node 0's own are not
+ *       read, nor are nodes at counts and after. A node whose parent is no node, or
+ *       whose token is outside the vocabulary, is never looked at, nor, with
+ *       AF1_VERIFY_DISTINCT, one whose token was rejected here or where Z' is not above 0.
+ *   counts: device int32 [sequences], or NULL (all `nodes`).
+ *   uniforms: FP32 [sequences][nodes], at least 0 and below 1: number 0 draws the
+ *       token that follows, number i decides node i.
+ *   path: int32 [sequences][nodes], the accepted nodes from node 0 on, then -1;
+ *       lengths: int32 [sequences], how many they are; following: int32 [sequences].
+ * Precision: c Q is an FP32 product of c rounded to FP32, P - c Q an FP32 difference; R is
+ * summed as whole multiples of 2^-40 (to nearest even), the bound of the draw is
+ * rounded down to one; all else is FP64. So the result is a function of the inputs to the bit.
+ * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
+#define AF1_VERIFY_DISTINCT 1
+typedef struct af1_verify_args {
+  const float* probs;
+  int64_t probs_seq, probs_node;
+  const float* draft;
+  int64_t draft_seq, draft_node;
+  const int32_t *tokens, *parents, *counts;
+  const float* uniforms;
+  int32_t *path, *lengths, *following;
+  int64_t sequences, nodes, vocab; /* 0 .. 65536, 1 .. 64, 1 .. 2^22 */
+  int32_t flags;                   /* AF1_VERIFY_DISTINCT */
+  int32_t reserved;                /* must be 0 */
+} af1_verify_args;
+AF1_API int af1_verify_tree(const af1_verify_args* args, void* stream);
+
+/* ---- between two steps of drafted tokens: accepted slots, copied pages, the page table ----
+ * Several caches (a model's layers) share one table of pages: `caches` has
+ * `count` of them (1 .. 256), with one page size and no buffer twice; kinds,
+ * heads and numbers of pages may differ. A call moves the rows of all of them,
+ * codes and scales as they are. */
+
+/* Move slots of every sequence: slot first[s] + index[s][j] to first[s] + j for
+ * j < counts[s], all read before any is written (so that an accepted path of a
+ * tree comes to lie behind the prefix). Keys keep their rotation: a path's j-th
+ * node has position first + j already.
+ *   pages: as in af1_kv_append; up to 65536 sequences.
+ *   first, counts: device int32 [sequences]; index: device int32
+ *       [sequences][nodes], contiguous, nodes 1 .. 64. counts above nodes count as
+ *       nodes, negative ones as 0.
+ *   A slot is not moved where it, or the one that it goes to, is negative, or
+ *       lies outside the table or in a page outside the cache. Slots that are
+ *       written are of no other sequence's: no page that two sequences hold.
+ * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
+AF1_API int af1_kv_compact(const af1_kv_cache* const* caches, int64_t count, const int32_t* pages, int64_t sequences,
+                           int64_t page_columns, int64_t pages_ld, const int32_t* first, const int32_t* index,
+                           int64_t nodes, const int32_t* counts, void* stream);
+
+/* Copy the first rows of pages.
+ *   copies: device int32 [entries][3], contiguous: source page, target page,
+ *       rows (above the page size: all). An entry with a page outside a cache
+ *       copies nothing there, one with rows below 1 nothing at all. entries: 0 ..
+ *       2^20. A target is no other entry's target and no entry's source but its own.
+ * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
+AF1_API int af1_kv_copy(const af1_kv_cache* const* caches, int64_t count, const int32_t* copies, int64_t entries,
+                        void* stream);
+
+/* The table of pages and how many of its entries hold each page.
+ *   table: device int32 [sequences][columns], row stride ld. An entry outside 0 ..
+ *       pages - 1 holds no page.
+ *   refs: device int32 [pages]: the entries that hold the page, plus what the
+ *       caller adds to keep it; 0: free. */
+typedef struct af1_page_table {
+  int32_t* table;
+  int32_t* refs;
+  int64_t sequences, columns, ld; /* 0 .. 1024, 1 .. 2^20 (columns of fewer than 2^31 slots), columns .. 2^36 */
+  int64_t pages;                  /* 1 .. 2^31 - 1 */
+  int32_t page_size;              /* 16, 32, 64, 128 or 256 */
+  int32_t reserved;               /* must be 0 */
+} af1_page_table;
+
+/* Row s becomes what row parents[s] was; a row whose parent lies outside 0 ..
+ * sequences - 1 gives up its pages (-1). Pages are shared, not copied, and
+ * refs follow. parents: device int32 [sequences]. Errors: INVALID_ARG,
+ * BAD_POINTER, MISALIGNED, CUDA. */
+AF1_API int af1_pages_fork(const af1_page_table* table, const int32_t* parents, void* stream);
+
+/* Give every sequence pages of its own for slots first[s] .. first[s] +
+ * counts[s] - 1 (none where first is negative or counts below 1; slots behind
+ * the table's columns have no page).
+ * Taken in order of sequences and columns: an entry that holds no page gets one,
+ * and so does one whose page other entries hold too, but for the last of these
+ * if all of them are given pages in this call. New pages are the lowest free ones,
+ * in the same order. If they do not suffice, no page changes hands.
+ *   copies: device int32 [sequences][3]: the copy that af1_kv_copy is to make
+ *       before new tokens are written, of the rows before first[s] in a page that was
+ *       replaced; -1 three times where there is none.
+ *   lacking: device int32 [1]: pages that were lacking (0: done).
+ *   workspace: af1_pages_workspace_bytes bytes, 256-byte aligned, of any content.
+ * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, WORKSPACE, CUDA. */
+AF1_API int64_t af1_pages_workspace_bytes(const af1_page_table* table);
+AF1_API int af1_pages_reserve(const af1_page_table* table, const int32_t* first, const int32_t* counts,
+                              int32_t* copies, int32_t* lacking, void* workspace, int64_t workspace_bytes,
+                              void* stream);
+
+/* Give up the pages behind each sequence's first lens[s] slots (negative: 0):
+ * their entries become -1. lens: device int32 [sequences]. Errors: INVALID_ARG,
+ * BAD_POINTER, MISALIGNED, CUDA. */
+AF1_API int af1_pages_release(const af1_page_table* table, const int32_t* lens, void* stream);
+
 /* Message for the last error on the calling thread ("" if none). */
 AF1_API const char* af1_last_error(void);
 

@@ -645,3 +645,4 @@ class Step:
 # -- the step around the linears -------------------------------------------------------
 
 from .attention import KVCache, rope, rope_frequencies, rope_table, token_logprobs, tree_mask  # noqa: E402
+from .drafting import PageTable, kv_compact, kv_copy, token_probs, verify_tree  # noqa: E402
