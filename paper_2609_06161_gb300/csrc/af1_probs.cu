@@ -23,11 +23,14 @@ namespace cg = cooperative_groups;
 namespace af1 {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256, kBlocks = 5;  // blocks to an SM
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr int kListed = 1024;      // keys of a row that its CTAs list
+constexpr int kBins = 2048;
 constexpr int kMost = 100 * 1024 / 16;  // 16-byte accesses of a CTA's stretch in shared memory
 constexpr float kInf = __builtin_huge_valf();
+constexpr float kLeast = -1e4f;  // 2^d is 0 from far above on
 
 struct ProbsProblem {
   const void* logits;
@@ -62,22 +65,65 @@ __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
+__device__ __forceinline__ float sort_descending(float x, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+    for (int d = size / 2; d > 0; d >>= 1) {
+      const float other = __shfl_xor_sync(0xffffffffu, x, d);
+      const bool down = size == 32 || (lane & size) == 0;
+      x = ((lane & d) == 0) == down ? fmaxf(x, other) : fminf(x, other);
+    }
+  return x;
+}
+
 struct Settings {
   float temperature, min_p;
   int top_k;
 };
 
+// 16 bytes of entries as they lie.
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) probs_kernel(const __grid_constant__ ProbsProblem p) {
+struct Piece {
+  uint4 w;
+  __device__ __forceinline__ T at(int e) const { return reinterpret_cast<const T*>(&w)[e]; }
+  __device__ __forceinline__ float most() const {  // NaN if there is one
+    if constexpr (sizeof(T) == 2) {
+      const __half2* h = reinterpret_cast<const __half2*>(&w);
+      const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+      return __half2float(__hmax_nan(__low2half(m), __high2half(m)));
+    } else {
+      const float* f = reinterpret_cast<const float*>(&w);
+      return max_nan(max_nan(f[0], f[1]), max_nan(f[2], f[3]));
+    }
+  }
+};
+
+// What a CTA says of its stretch to the others.
+struct Said {
+  float top, bound, sum;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_constant__ ProbsProblem p) {
   constexpr int E = 16 / (int)sizeof(T);
   extern __shared__ uint4 stretch[];
-  // Read by the cluster's other CTAs, each written once for a purpose.
-  __shared__ Settings settings;
-  __shared__ float cta_top, cta_sum;
-  __shared__ int cta_first, cta_count, cta_equal, cta_last;
-  __shared__ int hist[4][256];
-  __shared__ float warp_f[kWarps];
-  __shared__ int warp_i[kWarps], counts[256], found[2];
+  // Written by the cluster's CTAs, each once for a purpose.
+  __shared__ Settings settings, here_settings;
+  __shared__ double cut;
+  __shared__ Said said[kMaxCluster];
+  __shared__ float all_sums[kMaxCluster];
+  __shared__ uint64_t kth_key;
+  __shared__ int all_first[kMaxCluster], all_listed[kMaxCluster], all_equal[kMaxCluster], all_last[kMaxCluster];
+  __shared__ alignas(16) uint64_t lists[kListed];  // of every CTA a part; later counts of digits
+  // The CTA's own.
+  __shared__ float warp_f[kWarps], tried[2 * kWarps];
+  __shared__ int warp_i[kWarps], found[3], here_listed, here_last;
+  __shared__ int reached[kWarps][2 * kWarps];
+  static_assert(2 * kWarps <= 32, "");
+  __shared__ double here_cut;
+  __shared__ float here_low;
+  __shared__ long long warp_mass[kWarps];
   cg::cluster_group cluster = cg::this_cluster();
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
@@ -85,265 +131,481 @@ __global__ void __launch_bounds__(kThreads, 2) probs_kernel(const __grid_constan
   const T* x = static_cast<const T*>(p.logits) + row * p.ld;
   float* out = p.probs + row * p.probs_ld;
 
-  // Entry v of the row is entry v + skew of 16-byte accesses from the boundary before the row on.
+  // Entry v of the row is entry v + skew of 16-byte pieces from the boundary before the row on; this CTA has the pieces
+  // `begin` .. begin + n - 1, numbered from 0, of which those from j0 up to j1 lie in the row as a whole.
   const int skew = (int)((uintptr_t)x / sizeof(T) % E);
   const int64_t all = ((int64_t)p.vocab + skew + E - 1) / E;
-  const int begin = (int)(all * rank / cs), end = (int)(all * (rank + 1) / cs);
-  auto fetch = [&](int i) -> uint4 {  // entries outside the row are -infinity, which changes nothing
-    const int64_t v = (int64_t)i * E - skew;
-    if (v >= 0 && v + E <= p.vocab) return __ldg(reinterpret_cast<const uint4*>(x + v));
-    alignas(16) T t[E];
+  const int begin = (int)(all * rank / cs), n = (int)(all * (rank + 1) / cs) - begin;
+  const int64_t first_entry = (int64_t)begin * E - skew;
+  const int j0 = first_entry < 0 ? 1 : 0, j1 = first_entry + (int64_t)n * E > p.vocab ? n - 1 : n;
+  const uint4* source = reinterpret_cast<const uint4*>(x + first_entry);
+  auto index_of = [&](int j) { return (int)(first_entry + (int64_t)j * E); };
+  auto fetch = [&](int j) {  // entries outside the row are -infinity, which changes nothing
+    Piece<T> y;
+    if (j >= j0 && j < j1) {
+      y.w = __ldg(source + j);
+    } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) t[e] = v + e >= 0 && v + e < p.vocab ? x[v + e] : (T)-kInf;
-    return *reinterpret_cast<const uint4*>(t);
+      for (int e = 0; e < E; ++e) {
+        const int64_t v = first_entry + (int64_t)j * E + e;
+        reinterpret_cast<T*>(&y.w)[e] = v >= 0 && v < p.vocab ? x[v] : (T)-kInf;
+      }
+    }
+    return y;
   };
   const bool held = p.held > 0;
-  auto entries = [&](int i, float (&f)[E]) {
-    const uint4 w = held ? stretch[i - begin] : fetch(i);
-#pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = (float)reinterpret_cast<const T*>(&w)[e];
+  auto piece = [&](int j) {
+    if (!held) return fetch(j);
+    Piece<T> y;
+    y.w = stretch[j];
+    return y;
   };
-
-  // -- the largest entry, and the row's settings
-  if (tid == 0) {
-    settings.temperature = p.temperature == nullptr ? p.all_temperature : p.temperature[row];
-    settings.min_p = p.min_p == nullptr ? p.all_min_p : p.min_p[row];
-    settings.top_k = p.top_k == nullptr ? p.all_top_k : p.top_k[row];
-  }
-  float top = -kInf;
-  constexpr int U = 4;
-  for (int i0 = begin + tid; i0 < end; i0 += U * kThreads) {
-    uint4 w[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i0 + u * kThreads < end) w[u] = fetch(i0 + u * kThreads);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i0 + u * kThreads >= end) break;
-      if (held) stretch[i0 + u * kThreads - begin] = w[u];
-#pragma unroll
-      for (int e = 0; e < E; ++e) top = max_nan(top, (float)reinterpret_cast<const T*>(&w[u])[e]);
-    }
-  }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
-  if (lane == 0) warp_f[warp] = top;
-  __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kWarps; ++w) top = max_nan(top, warp_f[w]);
-    cta_top = top;
-  }
-  cluster.sync();
-  for (int i = 0; i < cs; ++i) top = max_nan(i == 0 ? -kInf : top, *cluster.map_shared_rank(&cta_top, i));
-  const Settings set = *cluster.map_shared_rank(&settings, 0);
-
-  auto write = [&](auto&& f) {  // f(entry, index)
-    for (int i = begin + tid; i < end; i += kThreads) {
-      const int64_t v = (int64_t)i * E - skew;
+  float* const target = out + first_entry;
+  const bool wide = (uintptr_t)target % 16 == 0;
+  auto write = [&](auto&& f) {  // f(piece's number, results)
+    for (int j = tid; j < n; j += kThreads) {
       float y[E];
-      entries(i, y);
+      f(j, y);
+      if (wide && j >= j0 && j < j1) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = f(y[e], (int)(v + e));
-      if (v >= 0 && v + E <= p.vocab && (uintptr_t)(out + v) % 16 == 0) {
-#pragma unroll
-        for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(out + v + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+        for (int e = 0; e < E; e += 4)
+          *reinterpret_cast<float4*>(target + (int64_t)j * E + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
       } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (v + e >= 0 && v + e < p.vocab) out[v + e] = y[e];
+        for (int e = 0; e < E; ++e) {
+          const int64_t v = first_entry + (int64_t)j * E + e;
+          if (v >= 0 && v < p.vocab) out[v] = y[e];
+        }
       }
     }
   };
-  auto block_sum = [&](int n) {  // for all threads
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
-    __syncthreads();
-    if (lane == 0) warp_i[warp] = n;
-    __syncthreads();
-    n = 0;
-    for (int w = 0; w < kWarps; ++w) n += warp_i[w];
-    return n;
+
+  // -- the stretch: its largest entry; its sum, where nothing is cut; a bound that top_k entries of the row reach
+  cluster_arrive_relaxed();  // the others' memory is written to when they have begun
+  if (tid == 0) {
+    here_settings.temperature = p.temperature == nullptr ? p.all_temperature : p.temperature[row];
+    here_settings.min_p = p.min_p == nullptr ? p.all_min_p : p.min_p[row];
+    here_settings.top_k = p.top_k == nullptr ? p.all_top_k : p.top_k[row];
+    here_listed = 0, here_last = -1;
+  }
+  auto slow = [&] {  // FP64: by one thread, while its first entries are on their way
+    if (tid == 0 && here_settings.min_p > 0.f)
+      here_cut = (double)fminf(here_settings.temperature, 1e30f) * log((double)fminf(here_settings.min_p, 1.f));
   };
+  float top = -kInf;
+  if (held) {
+    for (int j = tid; j < n; j += kThreads) {  // each thread's own pieces
+      if (j >= j0 && j < j1)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&stretch[j])), "l"(source + j) : "memory");
+      else
+        stretch[j] = fetch(j).w;
+    }
+    slow();
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    for (int j = tid; j < n; j += kThreads) top = max_nan(top, piece(j).most());
+  } else {
+    constexpr int U = 4;
+    slow();
+    for (int at = tid; at < n; at += U * kThreads) {
+      Piece<T> w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (at + u * kThreads < n) w[u] = fetch(at + u * kThreads);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (at + u * kThreads < n) top = max_nan(top, w[u].most());
+    }
+  }
+  float most = top;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
+  if (lane == 0) warp_f[warp] = most;
+  __syncthreads();
+  Settings set = here_settings;
+  // Where `need` lanes of every CTA have an entry of at least some bound, top_k entries of the row have. Each warp puts
+  // its lanes' largest in order and gives two from about as far down as the bound lies; the largest of these that enough
+  // lanes reach is the CTA's, and the least of the CTAs' the row's.
+  const int whole = (int)min(all / cs, (int64_t)kThreads) / 32;  // warps whose lanes all have entries, in every CTA
+  const int need = (int)(((int64_t)max(set.top_k, 0) + cs - 1) / cs);
+  const int part = whole > 0 ? (int)(((int64_t)need + whole - 1) / whole) : 33;  // lanes of each
+  const bool bounded = set.top_k >= 1 && part <= 32;
+  if (bounded) {
+    const float sorted = sort_descending(top, lane);  // a row with a NaN has no use for it
+    const float near = __shfl_sync(0xffffffffu, sorted, lane == 0 ? part - 1 : max(part - 2, 0));
+    if (lane < 2) tried[warp * 2 + lane] = warp < whole ? near : kInf;
+    __syncthreads();
+    int reach = 0;
+#pragma unroll
+    for (int l = 0; l < 2 * kWarps; ++l) {
+      const int count = __popc(__ballot_sync(0xffffffffu, sorted >= tried[l]));
+      if (lane == l) reach = count;
+    }
+    if (lane < 2 * kWarps) reached[warp][lane] = reach;
+  }
+  top = warp_f[lane % kWarps];
+#pragma unroll
+  for (int d = kWarps / 2; d > 0; d >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
+
+  float c = 1.4426950408889634f / fminf(set.temperature, 1e30f);
+  auto weights = [&](const Piece<T>& w, float2 (&y)[E / 2], float over) {  // without cuts
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) {
+      float2 v;
+      if constexpr (sizeof(T) == 2)
+        v = __half22float2(reinterpret_cast<const __half2*>(&w.w)[e]);
+      else
+        v = reinterpret_cast<const float2*>(&w.w)[e];
+      const float2 d = mul2(add2(v, make_float2(-over, -over)), make_float2(c, c));
+      y[e] = make_float2(ex2(d.x), ex2(d.y));
+    }
+  };
+  auto uncut = [&] { return (set.top_k < 1 || set.top_k >= p.vocab) && !(set.min_p > 0.f); };
+  auto block_sum = [&](float sum) {  // for all threads
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    __syncthreads();
+    if (lane == 0) warp_f[warp] = sum;
+    __syncthreads();
+    sum = warp_f[lane % kWarps];
+#pragma unroll
+    for (int d = kWarps / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    return sum;
+  };
+  float sum = 0.f;
+  if (uncut() && set.temperature >= 1e-30f && top > -kInf && top < kInf) {
+    float2 sums = make_float2(0.f, 0.f);
+    for (int j = tid; j < n; j += kThreads) {
+      float2 y[E / 2];
+      weights(piece(j), y, top);
+#pragma unroll
+      for (int e = 0; e < E / 2; ++e) sums = add2(sums, y[e]);
+    }
+    sum = block_sum(sums.x + sums.y);
+  }
+  __syncthreads();
+  cluster_wait();
+  if (warp == 0) {
+    float bound = set.top_k < 1 ? kInf : -kInf;
+    if (bounded) {
+      if (lane < 2 * whole) {
+        int lanes = 0;
+        for (int w = 0; w < kWarps; ++w) lanes += reached[w][lane];
+        if (lanes >= need) bound = tried[lane];
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, d));
+    }
+    if (lane < cs) {
+      *cluster.map_shared_rank(&said[rank], lane) = {top, bound, sum};
+      // Everyone takes the first CTA's settings, and so the same way.
+      if (rank == 0) {
+        *cluster.map_shared_rank(&settings, lane) = set;
+        *cluster.map_shared_rank(&cut, lane) = here_cut;
+      }
+    }
+  }
+  cluster.sync();
+  set = settings;
+  Said one = said[lane % kMaxCluster < cs ? lane % kMaxCluster : 0];
+  top = one.top;
+  float bound = one.bound;
+#pragma unroll
+  for (int d = kMaxCluster / 2; d > 0; d >>= 1) {
+    top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
+    bound = fminf(bound, __shfl_xor_sync(0xffffffffu, bound, d));
+  }
 
   if (!(top < kInf) || top == -kInf) {
-    const float y = top == -kInf ? 0.f : __int_as_float(0x7fffffff);
-    write([&](float, int) { return y; });
-    cluster.sync();  // the CTAs' memory was read
+    const float fill = top == -kInf ? 0.f : __int_as_float(0x7fffffff);
+    write([&](int, float (&y)[E]) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = fill;
+    });
     return;
   }
   if (!(set.temperature >= 1e-30f)) {  // greedy: the first of the largest
     int first = 0x7fffffff;
-    for (int i = begin + tid; i < end && first == 0x7fffffff; i += kThreads) {
-      float f[E];
-      entries(i, f);
+    for (int j = tid; j < n && first == 0x7fffffff; j += kThreads) {
+      const Piece<T> w = piece(j);
 #pragma unroll
       for (int e = E - 1; e >= 0; --e)
-        if (f[e] == top) first = (int)((int64_t)i * E - skew + e);
+        if ((float)w.at(e) == top) first = index_of(j) + e;
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) first = min(first, __shfl_xor_sync(0xffffffffu, first, d));
     if (lane == 0) warp_i[warp] = first;
     __syncthreads();
-    if (tid == 0) {
-      for (int w = 1; w < kWarps; ++w) first = min(first, warp_i[w]);
-      cta_first = first;
+    if (tid < cs) {
+      for (int w = 0; w < kWarps; ++w) first = min(first, warp_i[w]);
+      *cluster.map_shared_rank(&all_first[rank], tid) = first;
     }
     cluster.sync();
-    for (int i = 0; i < cs; ++i) first = min(i == 0 ? 0x7fffffff : first, *cluster.map_shared_rank(&cta_first, i));
-    write([&](float, int v) { return v == first ? 1.f : 0.f; });
-    cluster.sync();
+    first = all_first[0];
+    for (int i = 1; i < cs; ++i) first = min(first, all_first[i]);
+    write([&](int j, float (&y)[E]) {
+      const int v = index_of(j);
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = v + e == first ? 1.f : 0.f;
+    });
+    return;
+  }
+  const float t = fminf(set.temperature, 1e30f);
+  c = 1.4426950408889634f / t;
+  if (uncut()) {
+    const float mine = lane < cs ? one.sum * ex2(fmaxf((one.top - top) * c, kLeast)) : 0.f;
+    sum = one.top > -kInf ? mine : 0.f;  // a stretch of -infinity alone has no sum
+#pragma unroll
+    for (int d = kMaxCluster / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    sum = __shfl_sync(0xffffffffu, sum, 0);
+    const float inverse = 1.f / sum;  // sum is at least about 1
+    write([&](int j, float (&y)[E]) {
+      float2 z[E / 2];
+      weights(piece(j), z, top);
+#pragma unroll
+      for (int e = 0; e < E / 2; ++e) {
+        z[e] = mul2(z[e], make_float2(inverse, inverse));
+        y[2 * e] = z[e].x, y[2 * e + 1] = z[e].y;
+      }
+    });
     return;
   }
 
   // -- what is kept: above `low`, or equal to it up to the index `last`
-  const float t = fminf(set.temperature, 1e30f), c = 1.4426950408889634f / t;
-  const float share = fminf(fmaxf(set.min_p, 0.f), 1.f);
-  // Entries are compared with the FP64 bound: the least FP32 that is not below it does the same.
-  float low = share > 0.f ? __double2float_ru((double)top + (double)t * log((double)share)) : -kInf;
+  float low = -kInf;
+  if (set.min_p > 0.f) {
+    // Entries are compared with the FP64 bound: the least FP32 that is not below it does the same.
+    if (tid == 0) here_low = __double2float_ru((double)top + cut);
+    __syncthreads();
+    low = here_low;
+  }
   int last = 0x7fffffff;
-  if (set.top_k >= 1 && set.top_k < p.vocab) {
-    int n = 0;
-    for (int i = begin + tid; i < end; i += kThreads) {
-      float f[E];
-      entries(i, f);
+  const int top_k = set.top_k < 1 || set.top_k >= p.vocab ? 0x7fffffff : set.top_k;
+  // The entries that reach both bounds, as keys that put them in order; everyone gets everyone's.
+  const int room = kListed / cs;
+  const float from = top_k < p.vocab ? fmaxf(low, bound) : low;
+  if (from > -kInf || p.vocab <= room) {
+    for (int j = tid; j < n; j += kThreads) {
+      const Piece<T> w = piece(j);
+      if (w.most() < from) continue;
 #pragma unroll
-      for (int e = 0; e < E; ++e) n += f[e] >= low ? 1 : 0;
-    }
-    n = block_sum(n);
-    if (tid == 0) cta_count = n;
-    cluster.sync();
-    int64_t kept = 0;
-    for (int i = 0; i < cs; ++i) kept += *cluster.map_shared_rank(&cta_count, i);
-    if (kept > set.top_k) {
-      // The k-th largest key, 8 bits at a time.
-      uint32_t prefix = 0;
-      int k = set.top_k, equal = 0;
-#pragma unroll
-      for (int level = 0; level < 4; ++level) {
-        const int shift = 24 - 8 * level;
-        if (tid < 256) hist[level][tid] = 0;
-        if (tid < 2) found[tid] = 0;
-        __syncthreads();
-        for (int i = begin + tid; i < end; i += kThreads) {
-          float f[E];
-          entries(i, f);
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const uint32_t key = order_key(f[e]);
-            if (f[e] >= low && (level == 0 || key >> (shift + 8) == prefix)) atomicAdd(&hist[level][key >> shift & 255], 1);
-          }
+      for (int e = 0; e < E; ++e) {
+        const float v = (float)w.at(e);
+        const int index = index_of(j) + e;
+        if (v >= from && index >= 0 && index < p.vocab) {
+          const int at = atomicAdd(&here_listed, 1);
+          if (at < room) lists[rank * room + at] = (uint64_t)order_key(v) << 32 | (uint32_t)~index;
         }
-        cluster.sync();
-        if (tid < 256) {
-          int sum = 0;
-          for (int i = 0; i < cs; ++i) sum += *cluster.map_shared_rank(&hist[level][tid], i);
-          counts[tid] = sum;
-        }
-        __syncthreads();
-        if (warp == 0) {  // 8 bins to a lane, the largest first
-          int sum = 0;
-          for (int b = 0; b < 8; ++b) sum += counts[255 - (lane * 8 + b)];
-          int upto = sum;
-#pragma unroll
-          for (int d = 1; d < 32; d <<= 1) {
-            const int other = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += other;
-          }
-          const int from = __ffs(__ballot_sync(0xffffffffu, upto >= k)) - 1;
-          if (lane == from) {
-            int left = k - (upto - sum), b = 255 - lane * 8;
-            while (b > 0 && left > counts[b]) left -= counts[b], --b;
-            found[0] = b, found[1] = left;
-          }
-        }
-        __syncthreads();
-        prefix = prefix << 8 | (uint32_t)found[0];
-        k = found[1];  // of the entries with this prefix
-        equal = counts[found[0]];
-        __syncthreads();
-      }
-      low = key_value(prefix);
-      if (k < equal) {  // the first k of the equal ones: their counts by stretches of warps
-        const int per = (end - begin + kWarps - 1) / kWarps;
-        const int from = begin + warp * per, to = min(end, from + per);
-        int mine = 0;
-        for (int i = from + lane; i < to; i += 32) {
-          float f[E];
-          entries(i, f);
-#pragma unroll
-          for (int e = 0; e < E; ++e) mine += f[e] == low ? 1 : 0;
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
-        if (lane == 0) warp_i[warp] = mine;
-        if (tid == 0) cta_last = -1;
-        __syncthreads();
-        if (tid == 0) {
-          int sum = 0;
-          for (int w = 0; w < kWarps; ++w) sum += warp_i[w];
-          cta_equal = sum;
-        }
-        cluster.sync();
-        for (int i = 0; i < rank; ++i) k -= *cluster.map_shared_rank(&cta_equal, i);
-        for (int w = 0; w < warp; ++w) k -= warp_i[w];
-        if (k >= 1 && k <= mine) {  // the k-th of this warp's
-          for (int i0 = from; i0 < to && k > 0; i0 += 32) {
-            const int i = i0 + lane;
-            float f[E];
-            unsigned same = 0;
-            if (i < to) {
-              entries(i, f);
-#pragma unroll
-              for (int e = 0; e < E; ++e) same |= f[e] == low ? 1u << e : 0u;
-            }
-            const int sum = __popc(same);
-            int upto = sum;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-              const int other = __shfl_up_sync(0xffffffffu, upto, d);
-              if (lane >= d) upto += other;
-            }
-            if (upto - sum < k && k <= upto) {
-              for (int left = k - (upto - sum); left > 1; --left) same &= same - 1;
-              cta_last = (int)((int64_t)i * E - skew) + __ffs(same) - 1;
-            }
-            k -= __shfl_sync(0xffffffffu, upto, 31);
-          }
-        }
-        cluster.sync();
-        last = -1;
-        for (int i = 0; i < cs; ++i) last = max(last, *cluster.map_shared_rank(&cta_last, i));
       }
     }
+    __syncthreads();
+  } else if (tid == 0) {
+    here_listed = room + 1;
   }
-
-  // -- the sum, and the row
-  auto weight = [&](float v, int index) {
-    const bool kept = v > low || (v == low && index <= last);
-    return kept ? ex2((v - top) * c) : 0.f;
-  };
-  float sum = 0.f;
-  for (int i = begin + tid; i < end; i += kThreads) {
-    float f[E];
-    entries(i, f);
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum += weight(f[e], (int)((int64_t)i * E - skew + e));
-  }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  if (lane == 0) warp_f[warp] = sum;
   __syncthreads();
-  if (tid == 0) {
-    sum = 0.f;
-    for (int w = 0; w < kWarps; ++w) sum += warp_f[w];
-    cta_sum = sum;
+  const int mine = here_listed;
+  for (int i = 0; i < cs; ++i) {
+    if (tid == 0) *cluster.map_shared_rank(&all_listed[rank], i) = mine;
+    if (i != rank && mine <= room)
+      for (int j = tid; j < mine; j += kThreads)
+        *cluster.map_shared_rank(&lists[rank * room + j], i) = lists[rank * room + j];
   }
   cluster.sync();
-  sum = 0.f;
-  for (int i = 0; i < cs; ++i) sum += *cluster.map_shared_rank(&cta_sum, i);
-  const float inverse = 1.f / sum;  // sum is at least 1
-  write([&](float v, int index) { return weight(v, index) * inverse; });
-  cluster.sync();  // the CTAs' memory was read
+  bool fits = true;
+  int listed = 0;
+  for (int i = 0; i < cs; ++i) fits = fits && all_listed[i] <= room, listed += min(all_listed[i], room);
+  float inverse;
+  if (fits) {
+    uint64_t least = 0;
+    if (listed > top_k) {
+      // The key that k - 1 others are above: a few threads compare one of this CTA's keys with all.
+      constexpr int kTeam = 8;
+      const int own = all_listed[rank];
+      for (int at = 0; at < own; at += kThreads / kTeam) {
+        const int j = at + tid / kTeam;
+        const uint64_t key = j < own ? lists[rank * room + j] : 0;
+        int above = 0;
+        for (int r = 0; r < cs; ++r)
+          for (int i = tid % kTeam; i < all_listed[r]; i += kTeam) above += lists[r * room + i] > key ? 1 : 0;
+#pragma unroll
+        for (int d = kTeam / 2; d > 0; d >>= 1) above += __shfl_xor_sync(0xffffffffu, above, d);
+        if (key != 0 && above == top_k - 1 && tid % kTeam < cs) *cluster.map_shared_rank(&kth_key, tid % kTeam) = key;
+      }
+      static_assert(kTeam == kMaxCluster, "");
+      cluster.sync();
+      least = kth_key;
+      low = key_value((uint32_t)(least >> 32)), last = (int)~(uint32_t)least;
+    } else {
+      low = from;  // these are all: at `low` or above, or as many as the k
+    }
+    // Lists are in no order, so that their weights are added up as whole multiples of 2^-40.
+    long long mass = 0;
+    for (int s = 0; s < cs; ++s)
+      for (int i = tid; i < all_listed[s]; i += kThreads) {
+        const uint64_t key = lists[s * room + i];
+        if (key >= least) mass += __float2ll_rn(ex2((key_value((uint32_t)(key >> 32)) - top) * c) * 1099511627776.f);
+      }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, d);
+    if (lane == 0) warp_mass[warp] = mass;
+    __syncthreads();
+    mass = warp_mass[lane % kWarps];
+#pragma unroll
+    for (int d = kWarps / 2; d > 0; d >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, d);
+    inverse = 1.f / ((float)mass * 9.094947017729282e-13f);
+  } else {
+    if (top_k < p.vocab) {
+      // The k-th largest key by counts of its digits: 11, 11 and 10 bits (FP16 has 22).
+      int* const counts = reinterpret_cast<int*>(lists);
+      static_assert(sizeof(lists) >= kBins * sizeof(int), "");
+      uint32_t prefix = 0;
+      int k = top_k, equal = 0;
+      bool cut = true;
+      constexpr int kLevels = sizeof(T) == 2 ? 2 : 3;
+#pragma unroll
+      for (int level = 0; level < kLevels; ++level) {
+        const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bins = level < 2 ? 2048 : 1024;
+        cluster.sync();  // what lies there was read
+        for (int i = tid; i < bins; i += kThreads) counts[i] = 0;
+        if (tid < 3) found[tid] = 0;
+        __syncthreads();
+        for (int j = tid; j < n; j += kThreads) {
+          const Piece<T> w = piece(j);
+          if (w.most() < low) continue;
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float v = (float)w.at(e);
+            const uint32_t key = order_key(v);
+            if (v >= low && (level == 0 || key >> (level == 1 ? 21 : 10) == prefix))
+              atomicAdd(&counts[key >> shift & (bins - 1)], 1);
+          }
+        }
+        cluster.sync();
+        // Each thread sums a few bins of all CTAs, the largest first.
+        const int per = bins / kThreads;
+        int some[kBins / kThreads], here = 0;
+#pragma unroll
+        for (int j = 0; j < kBins / kThreads; ++j) {
+          some[j] = 0;
+          if (j >= per) break;
+          for (int i = 0; i < cs; ++i) some[j] += *cluster.map_shared_rank(&counts[bins - 1 - (tid * per + j)], i);
+          here += some[j];
+        }
+        int upto = here;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int other = __shfl_up_sync(0xffffffffu, upto, d);
+          if (lane >= d) upto += other;
+        }
+        if (lane == 31) warp_i[warp] = upto;
+        __syncthreads();
+        int total = 0;
+        for (int w = 0; w < kWarps; ++w) {
+          if (w < warp) upto += warp_i[w];
+          total += warp_i[w];
+        }
+        if (level == 0 && total <= k) {
+          cut = false;  // all that reach `low`
+          break;
+        }
+        if (upto - here < k && k <= upto) {
+          int left = k - (upto - here);
+#pragma unroll
+          for (int j = 0; j < kBins / kThreads; ++j) {
+            if (j >= per) break;
+            if (left > 0 && left <= some[j]) found[0] = bins - 1 - (tid * per + j), found[1] = left, found[2] = some[j];
+            left -= some[j];
+          }
+        }
+        __syncthreads();
+        prefix = prefix << (level == 2 ? 10 : 11) | (uint32_t)found[0];
+        k = found[1];  // of the entries with this prefix
+        equal = found[2];
+      }
+      if (cut) {
+        // The bits that FP16 does not have are 0, and 1 in the keys of negative values.
+        low = key_value(sizeof(T) == 4 ? prefix : prefix << 10 | (prefix >> 21 & 1 ? 0u : 1023u));
+        if (k < equal) {  // the first k of the equal ones: their counts by stretches of warps
+          const int per = (n + kWarps - 1) / kWarps;
+          const int from_here = warp * per, to = min(n, from_here + per);
+          int same_here = 0;
+          for (int i = from_here + lane; i < to; i += 32) {
+            const Piece<T> w = piece(i);
+#pragma unroll
+            for (int e = 0; e < E; ++e) same_here += (float)w.at(e) == low ? 1 : 0;
+          }
+#pragma unroll
+          for (int d = 16; d > 0; d >>= 1) same_here += __shfl_xor_sync(0xffffffffu, same_here, d);
+          if (lane == 0) warp_i[warp] = same_here;
+          __syncthreads();
+          if (tid < cs) {
+            int sum_here = 0;
+            for (int w = 0; w < kWarps; ++w) sum_here += warp_i[w];
+            *cluster.map_shared_rank(&all_equal[rank], tid) = sum_here;
+          }
+          cluster.sync();
+          for (int i = 0; i < rank; ++i) k -= all_equal[i];
+          for (int w = 0; w < warp; ++w) k -= warp_i[w];
+          if (k >= 1 && k <= same_here) {  // the k-th of this warp's
+            for (int i0 = from_here; i0 < to && k > 0; i0 += 32) {
+              const int i = i0 + lane;
+              unsigned same = 0;
+              if (i < to) {
+                const Piece<T> w = piece(i);
+#pragma unroll
+                for (int e = 0; e < E; ++e) same |= (float)w.at(e) == low ? 1u << e : 0u;
+              }
+              const int have = __popc(same);
+              int upto = have;
+#pragma unroll
+              for (int d = 1; d < 32; d <<= 1) {
+                const int other = __shfl_up_sync(0xffffffffu, upto, d);
+                if (lane >= d) upto += other;
+              }
+              if (upto - have < k && k <= upto) {
+                for (int left = k - (upto - have); left > 1; --left) same &= same - 1;
+                here_last = index_of(i) + __ffs(same) - 1;
+              }
+              k -= __shfl_sync(0xffffffffu, upto, 31);
+            }
+          }
+          __syncthreads();
+          if (tid < cs) *cluster.map_shared_rank(&all_last[rank], tid) = here_last;
+          cluster.sync();
+          last = -1;
+          for (int i = 0; i < cs; ++i) last = max(last, all_last[i]);
+        }
+      }
+    }
+    sum = 0.f;
+    for (int j = tid; j < n; j += kThreads) {
+      const Piece<T> w = piece(j);
+      if (w.most() < low) continue;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float v = (float)w.at(e);
+        if (v > low || (v == low && index_of(j) + e <= last)) sum += ex2((v - top) * c);
+      }
+    }
+    sum = block_sum(sum);
+    if (tid < cs) *cluster.map_shared_rank(&all_sums[rank], tid) = sum;
+    cluster.sync();  // counts were read, too
+    sum = 0.f;
+    for (int i = 0; i < cs; ++i) sum += all_sums[i];
+    inverse = 1.f / sum;
+  }
+  write([&](int j, float (&y)[E]) {
+    const Piece<T> w = piece(j);
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = 0.f;
+    if (w.most() >= low) {
+      const int index = index_of(j);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float v = (float)w.at(e);
+        if (v > low || (v == low && index + e <= last)) y[e] = ex2((v - top) * c) * inverse;
+      }
+    }
+  });
 }
 
 int fail(int code, const std::string& msg) { return set_error(code, "af1_token_probs: " + msg); }
@@ -403,12 +665,12 @@ int af1_token_probs(const af1_probs_args* a, void* stream) {
   }
   ProbsProblem p = {a->logits, a->ld,    a->probs,           a->probs_ld,  (int)a->vocab,  a->temperature,
                     a->top_k,  a->min_p, a->all_temperature, a->all_min_p, a->all_top_k, 0};
-  // CTAs of a row: as many as give each a batch of accesses, while two of them
-  // to an SM hold all rows, or until a stretch fits in the 100 KB that leave two CTAs to an SM.
+  // CTAs of a row: as many as give each thread two accesses, while two to an SM
+  // take all rows, or until a stretch is at most 32 KB, so that three to an SM are in different passes.
   const int64_t accesses = (a->vocab * es + 15) / 16 + 1;
   int cluster = 1;
   while (cluster < kMaxCluster &&
-         ((a->rows * cluster * 2 <= 2 * sms && accesses >= 2 * cluster * kThreads) || accesses > kMost * cluster))
+         ((a->rows * cluster * 2 <= 2 * sms && accesses >= 2 * cluster * kThreads) || accesses > 2048 * cluster))
     cluster *= 2;
   const int64_t stretch = (accesses + cluster - 1) / cluster;
   p.held = stretch <= kMost ? (int)stretch : 0;

@@ -60,8 +60,6 @@ __device__ __forceinline__ float clamped(float p) { return fminf(fmaxf(p, 0.f), 
 __device__ __forceinline__ float residual(float p, float q, float c) {
   return fmaxf(__fsub_rn(p, __fmul_rn(c, q)), 0.f);
 }
-__device__ __forceinline__ long long mass_of(float r) { return __double2ll_rn((double)r * kUnit); }
-
 // Sums of masses of at most 16 entries each, until they are added up.
 struct Masses {
   float high = 0.f, low = 0.f;
@@ -77,6 +75,11 @@ struct Masses {
   }
 };
 
+__device__ __forceinline__ long long mass_of(float r) {
+  Masses m;
+  m.add(r);
+  return m.total();
+}
 __device__ __forceinline__ long long warp_sum(long long x) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
@@ -105,6 +108,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
   __shared__ Order order;
   __shared__ Gone gone[kMaxNodes];
   __shared__ long long warp_mass[kWarps], cta_mass[kMaxCluster];  // cta_mass: of all CTAs, written by each
+  __shared__ long long drawn;
   __shared__ int parent[kMaxNodes], token[kMaxNodes];
   __shared__ float u[kMaxNodes], px[kMaxNodes], qx[kMaxNodes];
   const float* probs = p.probs + seq * p.p_seq;
@@ -209,8 +213,12 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
       if (rank == 0 && tid == 0) p.following[seq] = -1;
       return;
     }
-    const float u1 = fminf(fmaxf(o.u, 0.f), 0.99999994f);  // 1 - 2^-24; NaN is 0
-    long long bound = __double2ll_rd(__dmul_rn((double)u1, (double)all));
+    if (tid == 0) {  // FP64 is slow: one thread's
+      const float u1 = fminf(fmaxf(o.u, 0.f), 0.99999994f);  // 1 - 2^-24; NaN is 0
+      drawn = __double2ll_rd(__dmul_rn((double)u1, (double)all));
+    }
+    __syncthreads();
+    long long bound = drawn;
     for (int i = 0; i < rank; ++i) bound -= cta_mass[i];
     if (bound < 0 || bound >= cta_mass[rank]) return;
     for (int w = 0; w < warp; ++w) bound -= warp_mass[w];
@@ -247,19 +255,22 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     }
   };
 
-  if (rank != 0) {
+  auto follow = [&] {
     for (;;) {
       const Order o = receive();
       if (o.what == 0) {
         cluster.sync();  // the first CTA's memory was read
-        break;
+        return;
       }
       if (o.what == 2) {
         draw(o);
-        break;
+        return;
       }
       total_mass(o);
     }
+  };
+  if (rank != 0) {
+    follow();
     return;
   }
 
@@ -275,7 +286,11 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     qx[tid] = DRAFT && real ? clamped(draft[up * p.q_node + x]) : 0.f;
   }
   __syncthreads();
-  // The walk: every thread of this CTA takes the same steps; the first writes.
+  // The walk is one warp's (FP64 is slow), whose lanes take the same steps; its first writes.
+  if (warp != 0) {
+    follow();
+    return;
+  }
   int at = 0, length = 1, n_gone = 0;
   double c = 0.0, z = 1.0, zq = 1.0;
   bool stale = false;  // z is of the residual before
@@ -291,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     if (stale) {
       if (tid == 0) order = {1, at, (float)c, 0.f, n_gone};
       const Order o = receive();
-      z = (double)total_mass(o) / kUnit;
+      z = (double)total_mass(o) * (1.0 / kUnit);
       stale = false;
     }
     const double r = again ? 0.f : DRAFT ? residual(px[child], qx[child], (float)c) : px[child];
@@ -310,15 +325,15 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     } else {
       z = __dsub_rn(z, r);
     }
-    __syncthreads();  // the list was read
+    __syncwarp();  // the list was read
     if (!again) {
       if (tid == 0) gone[n_gone] = {token[child], px[child], qx[child]};
       ++n_gone;
     }
-    __syncthreads();
+    __syncwarp();
   }
   if (n == 0) length = 0;
-  for (int i = length + tid; i < p.nodes; i += kThreads) p.path[seq * p.nodes + i] = -1;
+  for (int i = length + lane; i < p.nodes; i += 32) p.path[seq * p.nodes + i] = -1;
   if (tid == 0) {
     p.lengths[seq] = length;
     order = {n > 0 ? 2 : 0, at, (float)c, u[0], n_gone};
