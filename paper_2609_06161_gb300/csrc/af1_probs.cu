@@ -23,7 +23,8 @@ namespace cg = cooperative_groups;
 namespace af1 {
 namespace {
 
-constexpr int kThreads = 256, kBlocks = 5;  // blocks to an SM
+constexpr int kLogThreads = 8, kThreads = 1 << kLogThreads;
+constexpr int kBlocks = 5;  // blocks to an SM
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kListed = 1024;      // keys of a row that its CTAs list
@@ -113,14 +114,16 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   __shared__ double cut;
   __shared__ Said said[kMaxCluster];
   __shared__ float all_sums[kMaxCluster];
-  __shared__ uint64_t kth_key;
   __shared__ int all_first[kMaxCluster], all_listed[kMaxCluster], all_equal[kMaxCluster], all_last[kMaxCluster];
-  __shared__ alignas(16) uint64_t lists[kListed];  // of every CTA a part; later counts of digits
+  __shared__ alignas(16) uint64_t lists[kListed];  // of every CTA a part; later the few keys near the k-th, or counts of digits
   // The CTA's own.
   __shared__ float warp_f[kWarps], tried[2 * kWarps];
   __shared__ int warp_i[kWarps], found[3], here_listed, here_last;
   __shared__ int reached[kWarps][2 * kWarps];
   static_assert(2 * kWarps <= 32, "");
+  __shared__ uint64_t kth_key;
+  __shared__ int parts[kThreads], here_few;
+  uint64_t* const few = lists;
   __shared__ double here_cut;
   __shared__ float here_low;
   __shared__ long long warp_mass[kWarps];
@@ -415,23 +418,53 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   for (int i = 0; i < cs; ++i) fits = fits && all_listed[i] <= room, listed += min(all_listed[i], room);
   float inverse;
   if (fits) {
+    // All keys, a few to a thread (0: none).
+    constexpr int kOwn = kListed / kThreads;
+    uint64_t key[kOwn];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      const int slot = tid + i * kThreads, of = slot / room;
+      key[i] = of < cs && slot - of * room < all_listed[of] ? lists[slot] : 0;
+    }
     uint64_t least = 0;
     if (listed > top_k) {
-      // The key that k - 1 others are above: a few threads compare one of this CTA's keys with all.
-      constexpr int kTeam = 8;
-      const int own = all_listed[rank];
-      for (int at = 0; at < own; at += kThreads / kTeam) {
-        const int j = at + tid / kTeam;
-        const uint64_t key = j < own ? lists[rank * room + j] : 0;
-        int above = 0;
-        for (int r = 0; r < cs; ++r)
-          for (int i = tid % kTeam; i < all_listed[r]; i += kTeam) above += lists[r * room + i] > key ? 1 : 0;
+      // The key that k - 1 others are above: first the part of the range, one of kThreads, that it lies in, then its place
+      // among the keys of that part, which are few but for ties.
+      const uint32_t base = order_key(from), span = order_key(top) - base;
+      const int shift = max(0, 32 - __clz((int)span) - kLogThreads);
+      auto part_of = [&](uint64_t k) { return (int)(((uint32_t)(k >> 32) - base) >> shift); };
+      __syncthreads();
+      parts[tid] = 0;
+      if (tid == 0) here_few = 0;
+      __syncthreads();
 #pragma unroll
-        for (int d = kTeam / 2; d > 0; d >>= 1) above += __shfl_xor_sync(0xffffffffu, above, d);
-        if (key != 0 && above == top_k - 1 && tid % kTeam < cs) *cluster.map_shared_rank(&kth_key, tid % kTeam) = key;
+      for (int i = 0; i < kOwn; ++i)
+        if (key[i] != 0) atomicAdd(&parts[part_of(key[i])], 1);
+      __syncthreads();
+      const int have = parts[kThreads - 1 - tid];
+      int upto = have;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int other = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += other;
       }
-      static_assert(kTeam == kMaxCluster, "");
-      cluster.sync();
+      if (lane == 31) warp_i[warp] = upto;
+      __syncthreads();
+      for (int w = 0; w < warp; ++w) upto += warp_i[w];
+      if (upto - have < top_k && top_k <= upto) found[0] = kThreads - 1 - tid, found[1] = top_k - (upto - have);
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i)
+        if (key[i] != 0 && part_of(key[i]) == found[0]) few[atomicAdd(&here_few, 1)] = key[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i)
+        if (key[i] != 0 && part_of(key[i]) == found[0]) {
+          int above = 0;
+          for (int j = 0; j < here_few; ++j) above += few[j] > key[i] ? 1 : 0;
+          if (above == found[1] - 1) kth_key = key[i];
+        }
+      __syncthreads();
       least = kth_key;
       low = key_value((uint32_t)(least >> 32)), last = (int)~(uint32_t)least;
     } else {
@@ -439,11 +472,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
     }
     // Lists are in no order, so that their weights are added up as whole multiples of 2^-40.
     long long mass = 0;
-    for (int s = 0; s < cs; ++s)
-      for (int i = tid; i < all_listed[s]; i += kThreads) {
-        const uint64_t key = lists[s * room + i];
-        if (key >= least) mass += __float2ll_rn(ex2((key_value((uint32_t)(key >> 32)) - top) * c) * 1099511627776.f);
-      }
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      if (key[i] != 0 && key[i] >= least)
+        mass += __float2ll_rn(ex2((key_value((uint32_t)(key[i] >> 32)) - top) * c) * 1099511627776.f);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, d);
     if (lane == 0) warp_mass[warp] = mass;
