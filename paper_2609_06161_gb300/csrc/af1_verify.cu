@@ -31,6 +31,7 @@
 
 #include "af1_internal.h"
 #include "af1_kv.cuh"
+#include "af1_ptx.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -41,6 +42,7 @@ constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kMaxNodes = 64;
+constexpr int kMostHeld = 208 * 1024;  // bytes of shared memory beside the kernel's own 6 KB
 constexpr double kUnit = 1099511627776.0;  // 2^40
 
 struct VerifyProblem {
@@ -53,6 +55,7 @@ struct VerifyProblem {
   int32_t *path, *lengths, *following;
   int nodes, vocab;
   bool distinct;
+  int held;  // 16-byte pieces of a row's stretch that a CTA keeps in shared memory; 0: it is read again for every pass
 };
 
 // Probabilities as they count: 0 to 1, NaN as 0.
@@ -86,18 +89,14 @@ __device__ __forceinline__ long long warp_sum(long long x) {
   return x;
 }
 
-// What the cluster's CTAs are to do with a row.
+// What the CTA's warps are to do with a row.
 struct Order {
-  int what;   // 0: nothing more, 1: the mass of R, 2: draw from it
-  int node;   // whose row
+  int node;       // whose row
+  int draw;       // 0: the mass of R, 1: draw from it
   float c;
-  float u;    // of the draw
-  int gone;   // tokens rejected here
+  uint64_t gone;  // nodes whose tokens are rejected here, no token twice
 };
-struct Gone {
-  int token;
-  float p, q;
-};
+constexpr int kMarks = 32;  // sums of a warp's stretch that are kept for the search
 
 template <bool DRAFT>
 __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_constant__ VerifyProblem p) {
@@ -105,19 +104,50 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   const int64_t seq = blockIdx.x / cs;
+  extern __shared__ float4 held[];  // P's stretch, then Q's
   __shared__ Order order;
-  __shared__ Gone gone[kMaxNodes];
-  __shared__ long long warp_mass[kWarps], cta_mass[kMaxCluster];  // cta_mass: of all CTAs, written by each
-  __shared__ long long drawn;
-  __shared__ int parent[kMaxNodes], token[kMaxNodes];
+  __shared__ long long marks[kWarps][kMarks], warp_mass[kWarps], drawn;
+  // Written by the cluster's CTAs.
+  __shared__ long long cta_mass[2][kMaxCluster];
+  __shared__ int nodes, parent[kMaxNodes], token[kMaxNodes];
   __shared__ float u[kMaxNodes], px[kMaxNodes], qx[kMaxNodes];
   const float* probs = p.probs + seq * p.p_seq;
   const float* draft = DRAFT ? p.draft + seq * p.q_seq : nullptr;
+  cluster_arrive_relaxed();  // the others' memory is written to when they have begun
 
-  // One row's stretch of this warp, in 16-byte accesses from the boundary before the row on: entry `v` of the row is
-  // entry v + skew of these accesses, whose first and last may lie outside in part.
-  int begin = 0, end = 0;  // accesses
-  int skew = 0;
+  // What the walk needs of the nodes: read by the first CTA for all, so that all walk alike.
+  if (rank == 0) {
+    const int n = p.counts == nullptr ? p.nodes : max(0, min(p.nodes, p.counts[seq]));
+    int up = -1, x = 0;
+    float w = 0.f, a = 0.f, b = 0.f;
+    if (tid < n) {
+      const int64_t at = seq * p.nodes + tid;
+      up = p.parents[at], x = p.tokens[at], w = p.uniforms[at];
+      if (!(tid > 0 && up >= 0 && up < n && x >= 0 && x < p.vocab)) up = -1;
+      if (up >= 0) {
+        a = __ldg(probs + up * p.p_node + x);
+        if (DRAFT) b = __ldg(draft + up * p.q_node + x);
+      }
+    }
+    cluster_wait();
+    if (tid < kMaxNodes)
+      for (int i = 0; i < cs; ++i) {
+        *cluster.map_shared_rank(&parent[tid], i) = up;
+        *cluster.map_shared_rank(&token[tid], i) = x;
+        *cluster.map_shared_rank(&u[tid], i) = w;
+        *cluster.map_shared_rank(&px[tid], i) = clamped(a);
+        *cluster.map_shared_rank(&qx[tid], i) = clamped(b);
+        if (tid == 0) *cluster.map_shared_rank(&nodes, i) = n;
+      }
+  } else {
+    cluster_wait();
+  }
+  cluster.sync();
+  const int n = nodes;
+
+  // A row's stretch of this CTA in 16-byte pieces from the boundary before the row on: entry v of the row is entry v +
+  // skew of these pieces, whose first and last may lie outside in part. Each warp has a part of the stretch.
+  int skew = 0, first = 0, begin = 0, end = 0;
   bool together = false;  // P and Q lie alike
   const float *prow = nullptr, *qrow = nullptr;
   auto take_row = [&](int node) {
@@ -126,86 +156,114 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     skew = (int)((uintptr_t)prow / 4 % 4);
     together = !DRAFT || (uintptr_t)qrow / 4 % 4 == skew;
     const int all = (p.vocab + skew + 3) / 4;  // at most 2^20 + 1
-    const int parts = cs * kWarps, part = rank * kWarps + warp;  // at most 128
-    begin = all * part / parts, end = all * (part + 1) / parts;
+    const int parts = cs * kWarps;             // at most 128
+    first = all * (rank * kWarps) / parts;
+    begin = all * (rank * kWarps + warp) / parts, end = all * (rank * kWarps + warp + 1) / parts;
   };
-  auto load = [&](int i, float (&a)[4], float (&b)[4]) {  // entries outside the row are 0
+  auto load = [&](int i, float4& a, float4& b) {  // entries outside the row are 0
     const int v = 4 * i - skew;
     const bool whole = v >= 0 && v + 4 <= p.vocab;
-    if (whole) {
-      const float4 x = __ldg(reinterpret_cast<const float4*>(prow + v));
-      a[0] = x.x, a[1] = x.y, a[2] = x.z, a[3] = x.w;
-    }
-    if (DRAFT && whole && together) {
-      const float4 x = __ldg(reinterpret_cast<const float4*>(qrow + v));
-      b[0] = x.x, b[1] = x.y, b[2] = x.z, b[3] = x.w;
-    }
+    if (whole) a = __ldg(reinterpret_cast<const float4*>(prow + v));
+    if (DRAFT && whole && together) b = __ldg(reinterpret_cast<const float4*>(qrow + v));
+    if (whole && together) return;
+    float x[4], y[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const bool inside = v + e >= 0 && v + e < p.vocab;
-      if (!whole) a[e] = inside ? __ldg(prow + v + e) : 0.f;
-      if (DRAFT && !(whole && together)) b[e] = inside ? __ldg(qrow + v + e) : 0.f;
+      x[e] = inside ? __ldg(prow + v + e) : 0.f;
+      y[e] = DRAFT && inside ? __ldg(qrow + v + e) : 0.f;
+    }
+    a = make_float4(x[0], x[1], x[2], x[3]), b = make_float4(y[0], y[1], y[2], y[3]);
+  };
+  const bool keeps = p.held > 0;
+  int kept_node = -1;
+  // A row's stretch to shared memory, each warp's by itself.
+  auto keep_row = [&](int node) {
+    if (!keeps || node == kept_node) return;
+    kept_node = node;
+    for (int i = begin + lane; i < end; i += 32) {
+      const int v = 4 * i - skew;
+      if (v >= 0 && v + 4 <= p.vocab && together) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&held[i - first])), "l"(prow + v) : "memory");
+        if (DRAFT)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&held[p.held + i - first])), "l"(qrow + v)
+                       : "memory");
+      } else {
+        float4 a, b = make_float4(0.f, 0.f, 0.f, 0.f);
+        load(i, a, b);
+        held[i - first] = a;
+        if (DRAFT) held[p.held + i - first] = b;
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+  };
+  auto fetch = [&](int i, float4& a, float4& b) {
+    if (keeps) {
+      a = held[i - first];
+      if (DRAFT) b = held[p.held + i - first];
+    } else {
+      load(i, a, b);
     }
   };
   auto value = [&](float a, float b, float c) { return DRAFT ? residual(clamped(a), clamped(b), c) : clamped(a); };
-  // The mass of this warp's stretch of R.
-  auto warp_total = [&](float c, int n_gone) {
-    long long sum = 0;
+  // The masses of all CTAs' stretches of R, in cta_mass of this turn, and their sum. All threads of all CTAs. The warp's is
+  // in warp_mass; up to every so many pieces of its stretch, in marks.
+  int turn = 0, step = 32;
+  auto total_mass = [&](const Order& o) {
+    turn ^= 1;
+    take_row(o.node);
+    keep_row(o.node);
     constexpr int U = DRAFT ? 2 : 4;
-    for (int i = begin; i < end; i += 32 * U) {
-      float a[U][4], b[U][4];
+    step = (end - begin + 32 * U * kMarks - 1) / (32 * U * kMarks) * (32 * U);  // pieces from mark to mark
+    step = max(step, 32 * U);
+    long long upto = 0;
+    for (int from = begin, mark = 0; from < end; from += step, ++mark) {
+      long long sum = 0;
+      for (int i = from; i < min(end, from + step); i += 32 * U) {
+        float4 a[U], b[U];
 #pragma unroll
-      for (int k = 0; k < U; ++k) {
-        const int at = i + 32 * k + lane;
-        if (at < end) {
-          load(at, a[k], b[k]);
-        } else {
+        for (int k = 0; k < U; ++k) {
+          a[k] = b[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (i + 32 * k + lane < end) fetch(i + 32 * k + lane, a[k], b[k]);
+        }
+        Masses m;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) a[k][e] = b[k][e] = 0.f;
+        for (int k = 0; k < U; ++k) {
+          m.add(value(a[k].x, b[k].x, o.c));
+          m.add(value(a[k].y, b[k].y, o.c));
+          m.add(value(a[k].z, b[k].z, o.c));
+          m.add(value(a[k].w, b[k].w, o.c));
+        }
+        sum += m.total();
+      }
+      if (o.gone != 0) {
+        const int to = min(end, from + step);
+#pragma unroll
+        for (int k = 0; k < kMaxNodes; k += 32) {
+          const int at = (token[k + lane] + skew) / 4;
+          if ((o.gone >> (k + lane) & 1) != 0 && at >= from && at < to) sum -= mass_of(value(px[k + lane], qx[k + lane], o.c));
         }
       }
-      Masses m;
-#pragma unroll
-      for (int k = 0; k < U; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) m.add(value(a[k][e], b[k][e], c));
-      sum += m.total();
+      upto += warp_sum(sum);
+      if (lane == 0) marks[warp][mark] = upto;
     }
-    for (int g = lane; g < n_gone; g += 32) {
-      const int at = (gone[g].token + skew) / 4;
-      if (at >= begin && at < end) sum -= mass_of(value(gone[g].p, gone[g].q, c));
-    }
-    return warp_sum(sum);
-  };
-  // The masses of all CTAs, in cta_mass; the returned one is their sum. All threads of all CTAs.
-  auto total_mass = [&](const Order& o) {
-    take_row(o.node);
-    const long long mine = warp_total(o.c, o.gone);
-    if (lane == 0) warp_mass[warp] = mine;
+    if (lane == 0) warp_mass[warp] = upto;
     __syncthreads();
     if (tid < cs) {
       long long sum = 0;
       for (int w = 0; w < kWarps; ++w) sum += warp_mass[w];
-      *cluster.map_shared_rank(&cta_mass[rank], tid) = sum;
+      *cluster.map_shared_rank(&cta_mass[turn][rank], tid) = sum;
     }
     cluster.sync();
     long long sum = 0;
-    for (int i = 0; i < cs; ++i) sum += cta_mass[i];
+    for (int i = 0; i < cs; ++i) sum += cta_mass[turn][i];
     return sum;
   };
-  // Everyone gets the first CTA's order, and the tokens that it leaves out.
-  auto receive = [&] {
-    cluster.sync();  // it is written
-    const Order o = *cluster.map_shared_rank(&order, 0);
-    if (rank != 0 && tid < o.gone) gone[tid] = *cluster.map_shared_rank(&gone[tid], 0);
-    __syncthreads();
-    return o;
-  };
-  // Draws from R. The search is the CTA's whose stretch the bound falls in.
+  // Draws from R. The search is the warp's whose stretch the bound falls in.
   auto draw = [&](Order o) {
     long long all = total_mass(o);
     if (all <= 0) {  // nothing is left: from P
-      cluster.sync();  // cta_mass was read
       o.c = 0.f, o.gone = 0;
       all = total_mass(o);
     }
@@ -214,27 +272,31 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
       return;
     }
     if (tid == 0) {  // FP64 is slow: one thread's
-      const float u1 = fminf(fmaxf(o.u, 0.f), 0.99999994f);  // 1 - 2^-24; NaN is 0
+      const float u1 = fminf(fmaxf(u[0], 0.f), 0.99999994f);  // 1 - 2^-24; NaN is 0
       drawn = __double2ll_rd(__dmul_rn((double)u1, (double)all));
     }
     __syncthreads();
     long long bound = drawn;
-    for (int i = 0; i < rank; ++i) bound -= cta_mass[i];
-    if (bound < 0 || bound >= cta_mass[rank]) return;
+    for (int i = 0; i < rank; ++i) bound -= cta_mass[turn][i];
+    if (bound < 0 || bound >= cta_mass[turn][rank]) return;
     for (int w = 0; w < warp; ++w) bound -= warp_mass[w];
     if (bound < 0 || bound >= warp_mass[warp]) return;
-    for (int i = begin; i < end; i += 32) {
-      float a[4] = {0.f, 0.f, 0.f, 0.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
+    int from = begin;
+    for (int mark = 0; from + step < end && bound >= marks[warp][mark]; ++mark) from += step;
+    if (from > begin) bound -= marks[warp][(from - begin) / step - 1];
+    for (int i = from; i < end; i += 32) {
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
       const int at = i + lane;
-      if (at < end) load(at, a, b);
-      long long m[4], sum = 0;
+      if (at < end) fetch(at, a, b);
+      long long m[4] = {mass_of(value(a.x, b.x, o.c)), mass_of(value(a.y, b.y, o.c)), mass_of(value(a.z, b.z, o.c)),
+                        mass_of(value(a.w, b.w, o.c))};
+      for (uint64_t left = o.gone; left != 0; left &= left - 1) {
+        const int place = token[__ffsll((long long)left) - 1] + skew - 4 * at;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        m[e] = mass_of(value(a[e], b[e], o.c));
-        for (int g = 0; g < o.gone; ++g)
-          if (gone[g].token == 4 * at - skew + e) m[e] = 0;
-        sum += m[e];
+        for (int e = 0; e < 4; ++e)
+          if (place == e) m[e] = 0;
       }
+      const long long sum = m[0] + m[1] + m[2] + m[3];
       long long upto = sum;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
@@ -255,66 +317,53 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     }
   };
 
-  auto follow = [&] {
+  if (n == 0) {
+    if (rank == 0) {
+      for (int i = tid; i < p.nodes; i += kThreads) p.path[seq * p.nodes + i] = -1;
+      if (tid == 0) p.lengths[seq] = 0, p.following[seq] = -1;
+    }
+    return;
+  }
+  // The walk is the first warp's of every CTA (FP64 is slow), whose lanes take the same steps; the others do the rows.
+  if (warp != 0) {
     for (;;) {
-      const Order o = receive();
-      if (o.what == 0) {
-        cluster.sync();  // the first CTA's memory was read
-        return;
-      }
-      if (o.what == 2) {
+      __syncthreads();  // the order is given
+      const Order o = order;
+      if (o.draw != 0) {
         draw(o);
         return;
       }
       total_mass(o);
     }
+  }
+  // Each lane keeps two nodes.
+  const int parent0 = parent[lane], parent1 = parent[lane + 32], token0 = token[lane], token1 = token[lane + 32];
+  auto nodes_with = [&](int x0, int x1, int x) {
+    return (uint64_t)__ballot_sync(0xffffffffu, x1 == x) << 32 | __ballot_sync(0xffffffffu, x0 == x);
   };
-  if (rank != 0) {
-    follow();
-    return;
-  }
-
-  const int n = p.counts == nullptr ? p.nodes : max(0, min(p.nodes, p.counts[seq]));
-  if (tid < p.nodes) {
-    const int64_t at = seq * p.nodes + tid;
-    const int up = p.parents[at], x = p.tokens[at];
-    const bool real = tid > 0 && tid < n && up >= 0 && up < n && x >= 0 && x < p.vocab;
-    parent[tid] = real ? up : -1;
-    token[tid] = x;
-    u[tid] = p.uniforms[at];
-    px[tid] = real ? clamped(probs[up * p.p_node + x]) : 0.f;
-    qx[tid] = DRAFT && real ? clamped(draft[up * p.q_node + x]) : 0.f;
-  }
-  __syncthreads();
-  // The walk is one warp's (FP64 is slow), whose lanes take the same steps; its first writes.
-  if (warp != 0) {
-    follow();
-    return;
-  }
-  int at = 0, length = 1, n_gone = 0;
+  const bool writes = rank == 0 && lane == 0;
+  int at = 0, length = 1;
+  uint64_t left = nodes_with(parent0, parent1, 0), gone = 0;
   double c = 0.0, z = 1.0, zq = 1.0;
   bool stale = false;  // z is of the residual before
-  if (n > 0 && tid == 0) p.path[seq * p.nodes] = 0;
-  for (int i = 1; n > 0;) {
-    while (i < n && parent[i] != at) ++i;
-    if (i >= n) break;
-    const int child = i++;
-    int seen = 0;
-    while (seen < n_gone && gone[seen].token != token[child]) ++seen;
-    const bool again = seen < n_gone;
+  if (writes) p.path[seq * p.nodes] = 0;
+  while (left != 0) {
+    const int child = __ffsll((long long)left) - 1;
+    left &= left - 1;
+    const bool again = (nodes_with(token0, token1, token[child]) & gone) != 0;
     if (DRAFT && (!(zq > 0.0) || (again && p.distinct))) continue;
     if (stale) {
-      if (tid == 0) order = {1, at, (float)c, 0.f, n_gone};
-      const Order o = receive();
-      z = (double)total_mass(o) * (1.0 / kUnit);
+      if (lane == 0) order = {at, 0, (float)c, gone};
+      __syncthreads();
+      z = (double)total_mass(order) * (1.0 / kUnit);
       stale = false;
     }
     const double r = again ? 0.f : DRAFT ? residual(px[child], qx[child], (float)c) : px[child];
-    const double left = DRAFT ? __dmul_rn(__dmul_rn(u[child], qx[child]), z) : __dmul_rn(u[child], z);
-    if (left < (DRAFT ? __dmul_rn(r, zq) : r)) {
-      if (tid == 0) p.path[seq * p.nodes + length] = child;
+    const double reach = DRAFT ? __dmul_rn(__dmul_rn(u[child], qx[child]), z) : __dmul_rn(u[child], z);
+    if (reach < (DRAFT ? __dmul_rn(r, zq) : r)) {
+      if (writes) p.path[seq * p.nodes + length] = child;
       ++length;
-      at = child, i = 1, n_gone = 0;
+      at = child, left = nodes_with(parent0, parent1, at), gone = 0;
       c = 0.0, z = zq = 1.0;
       continue;
     }
@@ -325,25 +374,15 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     } else {
       z = __dsub_rn(z, r);
     }
-    __syncwarp();  // the list was read
-    if (!again) {
-      if (tid == 0) gone[n_gone] = {token[child], px[child], qx[child]};
-      ++n_gone;
-    }
-    __syncwarp();
+    if (!again) gone |= 1ull << child;
   }
-  if (n == 0) length = 0;
-  for (int i = length + lane; i < p.nodes; i += 32) p.path[seq * p.nodes + i] = -1;
-  if (tid == 0) {
-    p.lengths[seq] = length;
-    order = {n > 0 ? 2 : 0, at, (float)c, u[0], n_gone};
-    if (n == 0) p.following[seq] = -1;
+  if (rank == 0) {
+    for (int i = length + lane; i < p.nodes; i += 32) p.path[seq * p.nodes + i] = -1;
+    if (lane == 0) p.lengths[seq] = length;
   }
-  const Order o = receive();
-  if (o.what == 2)
-    draw(o);
-  else
-    cluster.sync();
+  if (lane == 0) order = {at, 1, (float)c, gone};
+  __syncthreads();
+  draw(order);
 }
 
 int fail(int code, const std::string& msg) { return set_error(code, "af1_verify_tree: " + msg); }
@@ -355,6 +394,10 @@ cudaError_t launch(const VerifyProblem& p, int64_t sequences, int cluster, cudaS
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(sequences * cluster));
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = p.held * 16 * (DRAFT ? 2 : 1);
+  // Always the most, so that calls of several threads do not lower each other's.
+  cudaError_t e = cudaFuncSetAttribute(verify_kernel<DRAFT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostHeld);
+  if (e != cudaSuccess) return e;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -402,10 +445,14 @@ int af1_verify_tree(const af1_verify_args* a, void* stream) {
   }
   VerifyProblem p = {a->probs,  a->probs_seq, a->probs_node, a->draft,   a->draft_seq,  a->draft_node, a->tokens,
                      a->parents, a->counts,   a->uniforms,   a->path,    a->lengths,    a->following,  (int)a->nodes,
-                     (int)a->vocab, (a->flags & AF1_VERIFY_DISTINCT) != 0};
+                     (int)a->vocab, (a->flags & AF1_VERIFY_DISTINCT) != 0, 0};
   // CTAs of a sequence: as many as two to an SM allow, while each of their warps has 128 entries.
   int cluster = 1;
   while (cluster < kMaxCluster && a->sequences * cluster * 2 <= 2 * sms && a->vocab >= 2 * cluster * kWarps * 128) cluster *= 2;
+  // A stretch is kept where all CTAs have room for theirs at once.
+  const int64_t pieces = ((a->vocab + 3 + 3) / 4 + cluster - 1) / cluster + 1, bytes = pieces * (draft ? 32 : 16);
+  const int64_t beside = (a->sequences * cluster + sms - 1) / sms;  // CTAs to an SM
+  if (beside * (bytes + 8192) <= kMostHeld) p.held = (int)pieces;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   e = draft ? launch<true>(p, a->sequences, cluster, st) : launch<false>(p, a->sequences, cluster, st);
   if (e != cudaSuccess) return fail(AF1_ERR_CUDA, std::string(cudaGetErrorName(e)) + " (" + cudaGetErrorString(e) + ")");
