@@ -18,7 +18,7 @@
 // numbers are FP64. A sum of whole numbers costs no wide arithmetic: an FP32
 // addition of 12 and back splits r into a multiple of 2^-20 and a rest, another
 // addition rounds the rest to a multiple of 2^-40, and 16 of either add up
-// exactly in FP32 before they go to 64-bit integers.
+// exactly in FP32 before they go to integers.
 //
 // A cluster of CTAs takes a sequence. The numbers that the walk needs (four to a
 // node) are fetched for all nodes at once; its first CTA walks, the
@@ -59,28 +59,32 @@ struct VerifyProblem {
 };
 
 // Probabilities as they count: 0 to 1, NaN as 0.
-__device__ __forceinline__ float clamped(float p) { return fminf(fmaxf(p, 0.f), 1.f); }
+__device__ __forceinline__ float clamped(float p) { return __saturatef(p); }
+// Of such, with c at least 0: at most 1.
 __device__ __forceinline__ float residual(float p, float q, float c) {
-  return fmaxf(__fsub_rn(p, __fmul_rn(c, q)), 0.f);
+  return __saturatef(__fsub_rn(p, __fmul_rn(c, q)));
 }
-// Sums of masses of at most 16 entries each, until they are added up.
+
+// Sums of masses of at most 16 pairs of entries, until they are added up.
 struct Masses {
-  float high = 0.f, low = 0.f;
-  __device__ __forceinline__ void add(float r) {
-    const float h = __fsub_rn(__fadd_rn(r, 12.f), 12.f);  // to 2^-20
-    constexpr float kFine = 1.52587890625e-05f * 0.75f;    // 1.5 * 2^-17, whose last place is 2^-40
-    const float l = __fsub_rn(__fadd_rn(__fsub_rn(r, h), kFine), kFine);
-    high = __fadd_rn(high, h);
-    low = __fadd_rn(low, l);
+  float2 high = make_float2(0.f, 0.f), low = make_float2(0.f, 0.f);
+  __device__ __forceinline__ void add(float x, float y) {
+    constexpr float kFine = 1.52587890625e-05f * 0.75f;  // 1.5 * 2^-17, whose last place is 2^-40
+    const float2 r = make_float2(x, y);
+    const float2 h = add2(add2(r, make_float2(12.f, 12.f)), make_float2(-12.f, -12.f));  // to 2^-20
+    const float2 l = fma2(h, make_float2(-1.f, -1.f), r);                                // exact
+    high = add2(high, h);
+    low = add2(low, add2(add2(l, make_float2(kFine, kFine)), make_float2(-kFine, -kFine)));
   }
-  __device__ __forceinline__ long long total() const {
-    return ((long long)__float2int_rn(high * 1048576.f) << 20) + __float2int_rn(low * 1099511627776.f);
+  __device__ __forceinline__ long long total() const {  // sums of 16 are exact, and those of both halves as integers
+    const int h = __float2int_rn(high.x * 1048576.f) + __float2int_rn(high.y * 1048576.f);
+    const int l = __float2int_rn(low.x * 1099511627776.f) + __float2int_rn(low.y * 1099511627776.f);
+    return ((long long)h << 20) + l;
   }
 };
-
 __device__ __forceinline__ long long mass_of(float r) {
   Masses m;
-  m.add(r);
+  m.add(r, 0.f);
   return m.total();
 }
 __device__ __forceinline__ long long warp_sum(long long x) {
@@ -96,7 +100,8 @@ struct Order {
   float c;
   uint64_t gone;  // nodes whose tokens are rejected here, no token twice
 };
-constexpr int kMarks = 32;  // sums of a warp's stretch that are kept for the search
+constexpr int kMarks = 32;       // sums of a warp's stretch that are kept for the search,
+constexpr int kMarkPieces = 128;  // of so many pieces at least
 
 template <bool DRAFT>
 __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_constant__ VerifyProblem p) {
@@ -207,16 +212,26 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     }
   };
   auto value = [&](float a, float b, float c) { return DRAFT ? residual(clamped(a), clamped(b), c) : clamped(a); };
+  // What the rejected tokens among these pieces would add.
+  auto gone_mass = [&](const Order& o, int from, int to) {
+    long long sum = 0;
+#pragma unroll
+    for (int k = 0; k < kMaxNodes; k += 32) {
+      const int at = (token[k + lane] + skew) / 4;
+      if ((o.gone >> (k + lane) & 1) != 0 && at >= from && at < to) sum += mass_of(value(px[k + lane], qx[k + lane], o.c));
+    }
+    return warp_sum(sum);
+  };
   // The masses of all CTAs' stretches of R, in cta_mass of this turn, and their sum. All threads of all CTAs. The warp's is
-  // in warp_mass; up to every so many pieces of its stretch, in marks.
+  // in warp_mass; up to every so many pieces of its stretch, with the rejected tokens, in marks.
   int turn = 0, step = 32;
   auto total_mass = [&](const Order& o) {
     turn ^= 1;
     take_row(o.node);
     keep_row(o.node);
-    constexpr int U = DRAFT ? 2 : 4;
-    step = (end - begin + 32 * U * kMarks - 1) / (32 * U * kMarks) * (32 * U);  // pieces from mark to mark
-    step = max(step, 32 * U);
+    constexpr int U = DRAFT ? 2 : 4;  // up to 16 entries of a lane
+    static_assert(kMarkPieces % (32 * U) == 0, "");
+    step = max(1, (end - begin + kMarkPieces * kMarks - 1) / (kMarkPieces * kMarks)) * kMarkPieces;  // from mark to mark
     long long upto = 0;
     for (int from = begin, mark = 0; from < end; from += step, ++mark) {
       long long sum = 0;
@@ -230,24 +245,15 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
         Masses m;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-          m.add(value(a[k].x, b[k].x, o.c));
-          m.add(value(a[k].y, b[k].y, o.c));
-          m.add(value(a[k].z, b[k].z, o.c));
-          m.add(value(a[k].w, b[k].w, o.c));
+          m.add(value(a[k].x, b[k].x, o.c), value(a[k].y, b[k].y, o.c));
+          m.add(value(a[k].z, b[k].z, o.c), value(a[k].w, b[k].w, o.c));
         }
         sum += m.total();
-      }
-      if (o.gone != 0) {
-        const int to = min(end, from + step);
-#pragma unroll
-        for (int k = 0; k < kMaxNodes; k += 32) {
-          const int at = (token[k + lane] + skew) / 4;
-          if ((o.gone >> (k + lane) & 1) != 0 && at >= from && at < to) sum -= mass_of(value(px[k + lane], qx[k + lane], o.c));
-        }
       }
       upto += warp_sum(sum);
       if (lane == 0) marks[warp][mark] = upto;
     }
+    if (o.gone != 0) upto -= gone_mass(o, begin, end);
     if (lane == 0) warp_mass[warp] = upto;
     __syncthreads();
     if (tid < cs) {
@@ -282,8 +288,13 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     for (int w = 0; w < warp; ++w) bound -= warp_mass[w];
     if (bound < 0 || bound >= warp_mass[warp]) return;
     int from = begin;
-    for (int mark = 0; from + step < end && bound >= marks[warp][mark]; ++mark) from += step;
-    if (from > begin) bound -= marks[warp][(from - begin) / step - 1];
+    long long before = 0;
+    for (int mark = 0; from + step < end; ++mark, from += step) {
+      const long long upto = marks[warp][mark] - (o.gone != 0 ? gone_mass(o, begin, from + step) : 0);
+      if (bound < upto) break;
+      before = upto;
+    }
+    bound -= before;
     for (int i = from; i < end; i += 32) {
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
       const int at = i + lane;
@@ -345,6 +356,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
   int at = 0, length = 1;
   uint64_t left = nodes_with(parent0, parent1, 0), gone = 0;
   double c = 0.0, z = 1.0, zq = 1.0;
+  float near_z = 1.f, near_zq = 1.f;
   bool stale = false;  // z is of the residual before
   if (writes) p.path[seq * p.nodes] = 0;
   while (left != 0) {
@@ -355,24 +367,32 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     if (stale) {
       if (lane == 0) order = {at, 0, (float)c, gone};
       __syncthreads();
-      z = (double)total_mass(order) * (1.0 / kUnit);
+      const long long mass = total_mass(order);
+      z = (double)mass * (1.0 / kUnit), near_z = (float)mass * (float)(1.0 / kUnit);
       stale = false;
     }
-    const double r = again ? 0.f : DRAFT ? residual(px[child], qx[child], (float)c) : px[child];
-    const double reach = DRAFT ? __dmul_rn(__dmul_rn(u[child], qx[child]), z) : __dmul_rn(u[child], z);
-    if (reach < (DRAFT ? __dmul_rn(r, zq) : r)) {
+    // Clear cases are decided in FP32, whose errors are far below these margins, without waiting for FP64, which is slow.
+    const float r = again ? 0.f : DRAFT ? residual(px[child], qx[child], (float)c) : px[child];
+    const float near_reach = DRAFT ? u[child] * qx[child] * near_z : u[child] * near_z, near_r = DRAFT ? r * near_zq : r;
+    const float margin = 2e-5f * (near_reach + near_r) + 1e-5f * (DRAFT ? r : u[child]) + 1e-35f;
+    bool accepted = near_r - near_reach > margin;
+    if (!accepted && !(near_reach - near_r > margin)) {
+      const double reach = DRAFT ? __dmul_rn(__dmul_rn(u[child], qx[child]), z) : __dmul_rn(u[child], z);
+      accepted = reach < (DRAFT ? __dmul_rn(r, zq) : (double)r);
+    }
+    if (accepted) {
       if (writes) p.path[seq * p.nodes + length] = child;
       ++length;
       at = child, left = nodes_with(parent0, parent1, at), gone = 0;
-      c = 0.0, z = zq = 1.0;
+      c = 0.0, z = zq = 1.0, near_z = near_zq = 1.f;
       continue;
     }
     if (DRAFT) {
-      c = __dadd_rn(c, __ddiv_rn(z, zq));
-      if (p.distinct) zq = __dsub_rn(zq, (double)qx[child]);
+      c = __dadd_rn(c, zq == 1.0 ? z : __ddiv_rn(z, zq));
+      if (p.distinct) zq = __dsub_rn(zq, (double)qx[child]), near_zq -= qx[child];
       stale = true;
     } else {
-      z = __dsub_rn(z, r);
+      z = __dsub_rn(z, (double)r), near_z -= r;
     }
     if (!again) gone |= 1ull << child;
   }
@@ -449,9 +469,11 @@ int af1_verify_tree(const af1_verify_args* a, void* stream) {
   // CTAs of a sequence: as many as two to an SM allow, while each of their warps has 128 entries.
   int cluster = 1;
   while (cluster < kMaxCluster && a->sequences * cluster * 2 <= 2 * sms && a->vocab >= 2 * cluster * kWarps * 128) cluster *= 2;
-  // A stretch is kept where all CTAs have room for theirs at once.
+  // A stretch is kept where all CTAs have room for theirs at once. Clusters of 8 lie in parts of the GPU that are no
+  // multiples of 8 SMs: 15 of them, not 19, have an SM to each CTA.
   const int64_t pieces = ((a->vocab + 3 + 3) / 4 + cluster - 1) / cluster + 1, bytes = pieces * (draft ? 32 : 16);
-  const int64_t beside = (a->sequences * cluster + sms - 1) / sms;  // CTAs to an SM
+  const int64_t room = cluster == 8 ? sms * 15 / 19 : cluster == 4 ? sms * 9 / 10 : sms;
+  const int64_t beside = (a->sequences * cluster + room - 1) / room;  // CTAs to an SM
   if (beside * (bytes + 8192) <= kMostHeld) p.held = (int)pieces;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   e = draft ? launch<true>(p, a->sequences, cluster, st) : launch<false>(p, a->sequences, cluster, st);
