@@ -39,10 +39,11 @@ namespace af1 {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
+constexpr int kLogWarps = 4, kWarps = 1 << kLogWarps;
+static_assert(kThreads == 32 * kWarps, "");
+constexpr int kMaxCluster = 16;
 constexpr int kMaxNodes = 64;
-constexpr int kMostHeld = 208 * 1024;  // bytes of shared memory beside the kernel's own 6 KB
+constexpr int kMostHeld = 208 * 1024;  // bytes of shared memory beside the kernel's own 6 KB; half where two CTAs share an SM
 constexpr double kUnit = 1099511627776.0;  // 2^40
 
 struct VerifyProblem {
@@ -55,7 +56,8 @@ struct VerifyProblem {
   int32_t *path, *lengths, *following;
   int nodes, vocab;
   bool distinct;
-  int held;  // 16-byte pieces of a row's stretch that a CTA keeps in shared memory; 0: it is read again for every pass
+  int log_cluster;
+  int held;  // 16-byte pieces of a row that a warp keeps in shared memory; 0: they are read again for every pass
 };
 
 // Probabilities as they count: 0 to 1, NaN as 0.
@@ -65,32 +67,51 @@ __device__ __forceinline__ float residual(float p, float q, float c) {
   return __saturatef(__fsub_rn(p, __fmul_rn(c, q)));
 }
 
-// Sums of masses of at most 16 pairs of entries, until they are added up.
+// Sums of masses: the bits of r + 12 and of what is left of r count multiples of 2^-20 and of 2^-40 in their low
+// parts, and the others add up to a known number. For up to 2048 entries, or 64 in each lane of a warp.
 struct Masses {
-  float2 high = make_float2(0.f, 0.f), low = make_float2(0.f, 0.f);
+  uint32_t high = 0, low = 0;
   __device__ __forceinline__ void add(float x, float y) {
-    constexpr float kFine = 1.52587890625e-05f * 0.75f;  // 1.5 * 2^-17, whose last place is 2^-40
     const float2 r = make_float2(x, y);
-    const float2 h = add2(add2(r, make_float2(12.f, 12.f)), make_float2(-12.f, -12.f));  // to 2^-20
-    const float2 l = fma2(h, make_float2(-1.f, -1.f), r);                                // exact
-    high = add2(high, h);
-    low = add2(low, add2(add2(l, make_float2(kFine, kFine)), make_float2(-kFine, -kFine)));
+    const float2 t = add2(r, make_float2(12.f, 12.f));
+    const float2 l = fma2(add2(t, make_float2(-12.f, -12.f)), make_float2(-1.f, -1.f), r);  // exact
+    const float2 f = add2(l, make_float2(kFine, kFine));
+    high += __float_as_uint(t.x) + __float_as_uint(t.y);
+    low += __float_as_uint(f.x) + __float_as_uint(f.y);
   }
-  __device__ __forceinline__ long long total() const {  // sums of 16 are exact, and those of both halves as integers
-    const int h = __float2int_rn(high.x * 1048576.f) + __float2int_rn(high.y * 1048576.f);
-    const int l = __float2int_rn(low.x * 1099511627776.f) + __float2int_rn(low.y * 1099511627776.f);
-    return ((long long)h << 20) + l;
+  static constexpr float kFine = 1.52587890625e-05f * 0.75f;  // 1.5 * 2^-17, whose last place is 2^-40
+  // Of n entries.
+  __device__ __forceinline__ long long total(uint32_t n) const {
+    return ((long long)(uint32_t)(high - n * 0x41400000u) << 20) + (int32_t)(low - n * 0x37400000u);
+  }
+  __device__ __forceinline__ long long warp_total(uint32_t n) const {  // n in all lanes
+    Masses all;
+    all.high = __reduce_add_sync(0xffffffffu, high), all.low = __reduce_add_sync(0xffffffffu, low);
+    return all.total(n);
   }
 };
 __device__ __forceinline__ long long mass_of(float r) {
   Masses m;
   m.add(r, 0.f);
-  return m.total();
+  return m.total(2);
 }
 __device__ __forceinline__ long long warp_sum(long long x) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
   return x;
+}
+
+// All threads of the cluster meet; what those that `wrote` wrote to the others' memory is seen there. (A release by every
+// thread costs them all a wait for their stores.)
+__device__ __forceinline__ void meet(int ctas, bool wrote) {
+  if (ctas == 1) {
+    __syncthreads();
+    return;
+  }
+  if (wrote) asm volatile("fence.acq_rel.cluster;" ::: "memory");
+  __syncwarp();
+  cluster_arrive_relaxed();
+  cluster_wait();
 }
 
 // What the CTA's warps are to do with a row.
@@ -109,8 +130,9 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   const int64_t seq = blockIdx.x / cs;
-  extern __shared__ float4 held[];  // P's stretch, then Q's
+  extern __shared__ float4 pieces[];
   __shared__ Order order;
+  __shared__ int walked[kMaxNodes];
   __shared__ long long marks[kWarps][kMarks], warp_mass[kWarps], drawn;
   // Written by the cluster's CTAs.
   __shared__ long long cta_mass[2][kMaxCluster];
@@ -147,23 +169,25 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
   } else {
     cluster_wait();
   }
-  cluster.sync();
+  meet(cs, rank == 0 && tid < kMaxNodes);
   const int n = nodes;
 
   // A row's stretch of this CTA in 16-byte pieces from the boundary before the row on: entry v of the row is entry v +
   // skew of these pieces, whose first and last may lie outside in part. Each warp has a part of the stretch.
-  int skew = 0, first = 0, begin = 0, end = 0;
+  int skew = 0, begin = 0, end = 0;
   bool together = false;  // P and Q lie alike
   const float *prow = nullptr, *qrow = nullptr;
+  int row_node = -1;
   auto take_row = [&](int node) {
+    if (node == row_node) return;
+    row_node = node;
     prow = probs + node * p.p_node;
     qrow = DRAFT ? draft + node * p.q_node : nullptr;
     skew = (int)((uintptr_t)prow / 4 % 4);
     together = !DRAFT || (uintptr_t)qrow / 4 % 4 == skew;
     const int all = (p.vocab + skew + 3) / 4;  // at most 2^20 + 1
-    const int parts = cs * kWarps;             // at most 128
-    first = all * (rank * kWarps) / parts;
-    begin = all * (rank * kWarps + warp) / parts, end = all * (rank * kWarps + warp + 1) / parts;
+    const int shift = p.log_cluster + kLogWarps;  // at most 8
+    begin = all * (rank * kWarps + warp) >> shift, end = all * (rank * kWarps + warp + 1) >> shift;
   };
   auto load = [&](int i, float4& a, float4& b) {  // entries outside the row are 0
     const int v = 4 * i - skew;
@@ -180,33 +204,35 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     }
     a = make_float4(x[0], x[1], x[2], x[3]), b = make_float4(y[0], y[1], y[2], y[3]);
   };
-  const bool keeps = p.held > 0;
+  float4* const held_p = pieces + warp * p.held;
+  float4* const held_q = pieces + (kWarps + warp) * p.held;
   int kept_node = -1;
-  // A row's stretch to shared memory, each warp's by itself.
+  // The warp's part to shared memory, each lane's own pieces.
   auto keep_row = [&](int node) {
-    if (!keeps || node == kept_node) return;
+    if (node == kept_node) return;
     kept_node = node;
     for (int i = begin + lane; i < end; i += 32) {
       const int v = 4 * i - skew;
       if (v >= 0 && v + 4 <= p.vocab && together) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&held[i - first])), "l"(prow + v) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&held_p[i - begin])), "l"(prow + v) : "memory");
         if (DRAFT)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&held[p.held + i - first])), "l"(qrow + v)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&held_q[i - begin])), "l"(qrow + v)
                        : "memory");
       } else {
         float4 a, b = make_float4(0.f, 0.f, 0.f, 0.f);
         load(i, a, b);
-        held[i - first] = a;
-        if (DRAFT) held[p.held + i - first] = b;
+        held_p[i - begin] = a;
+        if (DRAFT) held_q[i - begin] = b;
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncwarp();
   };
+  const bool keeps = p.held > 0;
   auto fetch = [&](int i, float4& a, float4& b) {
     if (keeps) {
-      a = held[i - first];
-      if (DRAFT) b = held[p.held + i - first];
+      a = held_p[i - begin];
+      if (DRAFT) b = held_q[i - begin];
     } else {
       load(i, a, b);
     }
@@ -228,29 +254,42 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
   auto total_mass = [&](const Order& o) {
     turn ^= 1;
     take_row(o.node);
-    keep_row(o.node);
-    constexpr int U = DRAFT ? 2 : 4;  // up to 16 entries of a lane
+    if (keeps) keep_row(o.node);
+    constexpr int U = DRAFT ? 2 : 4;
     static_assert(kMarkPieces % (32 * U) == 0, "");
     step = max(1, (end - begin + kMarkPieces * kMarks - 1) / (kMarkPieces * kMarks)) * kMarkPieces;  // from mark to mark
     long long upto = 0;
     for (int from = begin, mark = 0; from < end; from += step, ++mark) {
-      long long sum = 0;
-      for (int i = from; i < min(end, from + step); i += 32 * U) {
-        float4 a[U], b[U];
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-          a[k] = b[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (i + 32 * k + lane < end) fetch(i + 32 * k + lane, a[k], b[k]);
-        }
+      for (int at = from; at < min(end, from + step); at += kMarkPieces) {
         Masses m;
+        uint32_t entries = 0;
+        for (int i = at; i < min(end, at + kMarkPieces); i += 32 * U) {
+          entries += 32 * U * 4;
+          float4 a[U], b[U];
+          // All pieces in the stretch and, read from the row, in the row: no piece is looked at by itself.
+          if (i + 32 * U <= end && (keeps || (together && 4 * i >= skew && 4 * (i + 32 * U) - skew <= p.vocab))) {
+            const float4* x = keeps ? held_p + (i - begin) : reinterpret_cast<const float4*>(prow + 4 * i - skew);
+            const float4* y = keeps ? held_q + (i - begin) : reinterpret_cast<const float4*>(qrow + 4 * i - skew);
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-          m.add(value(a[k].x, b[k].x, o.c), value(a[k].y, b[k].y, o.c));
-          m.add(value(a[k].z, b[k].z, o.c), value(a[k].w, b[k].w, o.c));
+            for (int k = 0; k < U; ++k) {
+              a[k] = x[32 * k + lane];
+              b[k] = DRAFT ? y[32 * k + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+              a[k] = b[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (i + 32 * k + lane < end) fetch(i + 32 * k + lane, a[k], b[k]);
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < U; ++k) {
+            m.add(value(a[k].x, b[k].x, o.c), value(a[k].y, b[k].y, o.c));
+            m.add(value(a[k].z, b[k].z, o.c), value(a[k].w, b[k].w, o.c));
+          }
         }
-        sum += m.total();
+        upto += m.warp_total(entries);
       }
-      upto += warp_sum(sum);
       if (lane == 0) marks[warp][mark] = upto;
     }
     if (o.gone != 0) upto -= gone_mass(o, begin, end);
@@ -261,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
       for (int w = 0; w < kWarps; ++w) sum += warp_mass[w];
       *cluster.map_shared_rank(&cta_mass[turn][rank], tid) = sum;
     }
-    cluster.sync();
+    meet(cs, tid < cs);
     long long sum = 0;
     for (int i = 0; i < cs; ++i) sum += cta_mass[turn][i];
     return sum;
@@ -352,13 +391,12 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
   auto nodes_with = [&](int x0, int x1, int x) {
     return (uint64_t)__ballot_sync(0xffffffffu, x1 == x) << 32 | __ballot_sync(0xffffffffu, x0 == x);
   };
-  const bool writes = rank == 0 && lane == 0;
   int at = 0, length = 1;
   uint64_t left = nodes_with(parent0, parent1, 0), gone = 0;
   double c = 0.0, z = 1.0, zq = 1.0;
   float near_z = 1.f, near_zq = 1.f;
   bool stale = false;  // z is of the residual before
-  if (writes) p.path[seq * p.nodes] = 0;
+  if (lane == 0) walked[0] = 0;
   while (left != 0) {
     const int child = __ffsll((long long)left) - 1;
     left &= left - 1;
@@ -377,11 +415,15 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     const float margin = 2e-5f * (near_reach + near_r) + 1e-5f * (DRAFT ? r : u[child]) + 1e-35f;
     bool accepted = near_r - near_reach > margin;
     if (!accepted && !(near_reach - near_r > margin)) {
+      if (!DRAFT) {
+        z = 1.0;
+        for (uint64_t some = gone; some != 0; some &= some - 1) z = __dsub_rn(z, (double)px[__ffsll((long long)some) - 1]);
+      }
       const double reach = DRAFT ? __dmul_rn(__dmul_rn(u[child], qx[child]), z) : __dmul_rn(u[child], z);
       accepted = reach < (DRAFT ? __dmul_rn(r, zq) : (double)r);
     }
     if (accepted) {
-      if (writes) p.path[seq * p.nodes + length] = child;
+      if (lane == 0) walked[length] = child;
       ++length;
       at = child, left = nodes_with(parent0, parent1, at), gone = 0;
       c = 0.0, z = zq = 1.0, near_z = near_zq = 1.f;
@@ -392,17 +434,17 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
       if (p.distinct) zq = __dsub_rn(zq, (double)qx[child]), near_zq -= qx[child];
       stale = true;
     } else {
-      z = __dsub_rn(z, (double)r), near_z -= r;
+      near_z -= r;
     }
     if (!again) gone |= 1ull << child;
-  }
-  if (rank == 0) {
-    for (int i = length + lane; i < p.nodes; i += 32) p.path[seq * p.nodes + i] = -1;
-    if (lane == 0) p.lengths[seq] = length;
   }
   if (lane == 0) order = {at, 1, (float)c, gone};
   __syncthreads();
   draw(order);
+  if (rank == 0) {
+    for (int i = lane; i < p.nodes; i += 32) p.path[seq * p.nodes + i] = i < length ? walked[i] : -1;
+    if (lane == 0) p.lengths[seq] = length;
+  }
 }
 
 int fail(int code, const std::string& msg) { return set_error(code, "af1_verify_tree: " + msg); }
@@ -414,9 +456,10 @@ cudaError_t launch(const VerifyProblem& p, int64_t sequences, int cluster, cudaS
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(sequences * cluster));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = p.held * 16 * (DRAFT ? 2 : 1);
+  cfg.dynamicSmemBytes = p.held * kWarps * 16 * (DRAFT ? 2 : 1);
   // Always the most, so that calls of several threads do not lower each other's.
   cudaError_t e = cudaFuncSetAttribute(verify_kernel<DRAFT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostHeld);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(verify_kernel<DRAFT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -465,16 +508,19 @@ int af1_verify_tree(const af1_verify_args* a, void* stream) {
   }
   VerifyProblem p = {a->probs,  a->probs_seq, a->probs_node, a->draft,   a->draft_seq,  a->draft_node, a->tokens,
                      a->parents, a->counts,   a->uniforms,   a->path,    a->lengths,    a->following,  (int)a->nodes,
-                     (int)a->vocab, (a->flags & AF1_VERIFY_DISTINCT) != 0, 0};
-  // CTAs of a sequence: as many as two to an SM allow, while each of their warps has 128 entries.
-  int cluster = 1;
-  while (cluster < kMaxCluster && a->sequences * cluster * 2 <= 2 * sms && a->vocab >= 2 * cluster * kWarps * 128) cluster *= 2;
-  // A stretch is kept where all CTAs have room for theirs at once. Clusters of 8 lie in parts of the GPU that are no
-  // multiples of 8 SMs: 15 of them, not 19, have an SM to each CTA.
-  const int64_t pieces = ((a->vocab + 3 + 3) / 4 + cluster - 1) / cluster + 1, bytes = pieces * (draft ? 32 : 16);
-  const int64_t room = cluster == 8 ? sms * 15 / 19 : cluster == 4 ? sms * 9 / 10 : sms;
-  const int64_t beside = (a->sequences * cluster + room - 1) / room;  // CTAs to an SM
-  if (beside * (bytes + 8192) <= kMostHeld) p.held = (int)pieces;
+                     (int)a->vocab, (a->flags & AF1_VERIFY_DISTINCT) != 0, 0, 0};
+  // CTAs of a sequence: as many as two to an SM allow, while each of their warps has 128 entries. (Clusters lie within
+  // parts of the GPU, whose SMs are no multiple of theirs: at one CTA to an SM there is room for 7 clusters of 16, 15 of 8,
+  // 36 of 4 and 76 of 2.)
+  const int64_t alone[] = {sms, sms / 2, sms * 36 / 152, sms * 15 / 152, sms * 7 / 152};
+  int level = 0;
+  while (level < 4 && a->sequences <= 2 * alone[level + 1] && a->vocab >= (128 * kWarps << (level + 1))) ++level;
+  const int cluster = 1 << level;
+  p.log_cluster = level;
+  // A row that may be summed more than once is kept, where all CTAs have room for their parts at once.
+  const int64_t part = ((a->vocab + 3 + 3) / 4 + cluster * kWarps - 1) / (cluster * kWarps) + 1;
+  const int64_t room = a->sequences <= alone[level] ? kMostHeld : kMostHeld / 2;
+  if (draft && part * kWarps * 32 <= room) p.held = (int)part;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   e = draft ? launch<true>(p, a->sequences, cluster, st) : launch<false>(p, a->sequences, cluster, st);
   if (e != cudaSuccess) return fail(AF1_ERR_CUDA, std::string(cudaGetErrorName(e)) + " (" + cudaGetErrorString(e) + ")");
