@@ -159,7 +159,7 @@ struct TableView {
 __device__ __forceinline__ bool holds(const TableView& t, int page) { return page >= 0 && page < t.pages; }
 
 // A block takes a few columns of all rows: it reads them all before it writes.
-constexpr int kForkColumns = 8, kForkThreads = 256;
+constexpr int kForkColumns = 8, kForkThreads = 1024;
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(const TableView t, const int32_t* parents) {
   __shared__ int32_t old[kMaxSequences * kForkColumns];
   const int column = blockIdx.x * kForkColumns + threadIdx.x % kForkColumns;
@@ -193,11 +193,15 @@ __global__ void __launch_bounds__(kReleaseThreads) release_kernel(const TableVie
   if (page != -1) *entry = -1;
 }
 
-// One block. `flags` has a word for every entry of the table, `list` the entries
-// that need a page, in order.
+// One block. The entries that the slots lie in are numbered in order of sequences and columns; a thread takes every
+// 1024th. Up to kNear of them, what is noted of them lies in shared memory, and pages that several of them hold meet in a
+// hash table there; of more, in the workspace, and pages meet in refs. (With a warp to a sequence and all notes in the
+// workspace a step of 256 sequences, fork and release among it, took 34 us.)
 constexpr int kReserveThreads = 1024;
 constexpr int kReserveWarps = kReserveThreads / 32;
-enum : int32_t { kOwn = 0, kMissing = 1, kShared = 2, kLast = 3, kKeeps = 4 };  // below 0: page -1 - flag is to be replaced
+constexpr int kNear = 1024, kLogSlots = 11, kSlots = 1 << kLogSlots;
+// What is noted of an entry; below 0: page -1 - note is to be replaced.
+enum : int32_t { kOwn = 0, kMissing = 1, kShared = 2, kLast = 3, kKeeps = 4 };
 
 __device__ __forceinline__ int block_exclusive(int x, int* warps, int* total) {
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -226,77 +230,118 @@ __device__ __forceinline__ int block_exclusive(int x, int* warps, int* total) {
 
 __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(const TableView t, const int32_t* first,
                                                                   const int32_t* counts, int32_t* copies,
-                                                                  int32_t* lacking, int32_t* flags, int32_t* list) {
-  __shared__ int begin[kMaxSequences], end[kMaxSequences], needs[kMaxSequences], warps[kReserveWarps];
-  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+                                                                  int32_t* lacking, int32_t* far_notes, int32_t* far_list) {
+  __shared__ int begin[kMaxSequences], before[kMaxSequences + 1], warps[kReserveWarps];
+  __shared__ int near_notes[kNear], near_list[kNear];
+  __shared__ int slot_page[kSlots], slot_count[kSlots], slot_last[kSlots];
+  const int tid = threadIdx.x;
   const int page_mask = (1 << t.shift) - 1;
+  int columns = 0;
   if (tid < t.seqs) {
     const int64_t f = first[tid], n = counts[tid];
-    const bool any = f >= 0 && n >= 1;
-    begin[tid] = any ? (int)(f >> t.shift) : 0;
-    end[tid] = any ? (int)min((int64_t)t.columns, ((f + n - 1) >> t.shift) + 1) : 0;
+    if (f >= 0 && n >= 1)
+      columns = (int)max((int64_t)0, min((int64_t)t.columns, ((f + n - 1) >> t.shift) + 1) - (f >> t.shift));
+    begin[tid] = columns > 0 ? (int)(f >> t.shift) : 0;
     copies[tid * 3] = copies[tid * 3 + 1] = copies[tid * 3 + 2] = -1;
   }
+  for (int i = tid; i < kSlots; i += kReserveThreads) slot_page[i] = -1, slot_count[i] = 0, slot_last[i] = -1;
+  int entries;
+  const int own_before = block_exclusive(columns, warps, &entries);
+  if (tid < t.seqs) before[tid] = own_before;
+  if (tid == 0) before[t.seqs] = entries;
   __syncthreads();
-  // f(entry, its flag, its place in the table) for every entry that the slots lie in.
-  auto each = [&](auto&& f) {
-    for (int s = warp; s < t.seqs; s += kReserveWarps)
-      for (int c = begin[s] + lane; c < end[s]; c += 32) f((int64_t)s * t.columns + c, &t.table[s * t.ld + c]);
+  const bool near = entries <= kNear;
+  int32_t* const notes = near ? near_notes : far_notes;
+  int32_t* const list = near ? near_list : far_list;
+  auto sequence_of = [&](int i) {  // before[s] <= i < before[s + 1]
+    int s = 0;
+    for (int half = kMaxSequences / 2; half > 0; half /= 2)
+      if (s + half < t.seqs && before[s + half] <= i) s += half;
+    return s;
+  };
+  auto entry_of = [&](int i) {
+    const int s = sequence_of(i);
+    return &t.table[s * t.ld + begin[s] + (i - before[s])];
   };
   bool shared = false;
-  each([&](int64_t e, const int32_t* entry) {
-    const int page = *entry;
-    const int flag = !holds(t, page) ? kMissing : __ldcg(&t.refs[page]) > 1 ? kShared : kOwn;
-    shared = shared || flag == kShared;
-    flags[e] = flag;
-  });
+  int page0 = -1;  // of the thread's first entry, whose place and page are not looked up again
+  int32_t* entry0 = nullptr;
+  for (int i = tid; i < entries; i += kReserveThreads) {
+    int32_t* entry = entry_of(i);
+    const int page = *entry, count = holds(t, page) ? __ldcg(&t.refs[page]) : 0;
+    if (i == tid) entry0 = entry, page0 = page;
+    int note = !holds(t, page) ? kMissing : kOwn;
+    if (count > 1) {
+      note = kShared, shared = true;
+      if (near) {  // at most half of the slots are taken
+        int at = (int)((uint32_t)page * 2654435769u >> (32 - kLogSlots));
+        for (;;) {
+          const int found = atomicCAS(&slot_page[at], -1, page);
+          if (found == -1 || found == page) break;
+          at = (at + 1) % kSlots;
+        }
+        static_assert(kNear * 2 <= kSlots, "");
+        atomicAdd(&slot_count[at], 1);
+        atomicMax(&slot_last[at], i);
+        note = at << 3 | kShared;
+      }
+    }
+    notes[i] = note;
+  }
+  auto each = [&](auto&& f) {  // f(number, its place in the table, its page), of entries that a page is held by
+    for (int i = tid; i < entries; i += kReserveThreads) {
+      int32_t* entry = i == tid ? entry0 : entry_of(i);
+      f(i, entry, i == tid ? page0 : *entry);
+    }
+  };
   if (__syncthreads_or(shared)) {
-    // A page whose count comes to 0 is held by entries of this call alone: the last of them keeps it. Counts below 0
-    // stand for the largest entry for a moment.
-    each([&](int64_t e, const int32_t* entry) {
-      if (flags[e] == kShared) atomicSub(&t.refs[*entry], 1);
+    // Of the entries of a page that are no fewer than its count, the last keeps it.
+    if (near) {
+      each([&](int i, int32_t*, int page) {
+        if ((notes[i] & 7) != kShared) return;
+        const int at = notes[i] >> 3;
+        // A page that all of its holders write to has as many entries here as its count says.
+        const bool keeps = slot_last[at] == i && slot_count[at] >= __ldcg(&t.refs[page]);
+        notes[i] = keeps ? kKeeps : -1 - page;
+      });
+      __syncthreads();
+      each([&](int i, int32_t*, int page) {
+        if (notes[i] < 0) atomicSub(&t.refs[page], 1);
+      });
+      __syncthreads();
+    } else {
+      // By the count, which comes to 0 then, and stands for the largest number for a moment.
+      each([&](int i, int32_t*, int page) {
+        if (notes[i] == kShared) atomicSub(&t.refs[page], 1);
+      });
+      __syncthreads();
+      each([&](int i, int32_t*, int page) {
+        if (notes[i] == kShared) notes[i] = __ldcg(&t.refs[page]) <= 0 ? kLast : -1 - page;
+      });
+      __syncthreads();
+      each([&](int i, int32_t*, int page) {
+        if (notes[i] == kLast) atomicMin(&t.refs[page], -2 - i);
+      });
+      __syncthreads();
+      each([&](int i, int32_t*, int page) {
+        if (notes[i] == kLast) notes[i] = __ldcg(&t.refs[page]) == -2 - i ? kKeeps : -1 - page;
+      });
+      __syncthreads();
+    }
+    each([&](int i, int32_t*, int page) {
+      if (notes[i] == kKeeps) __stcg(&t.refs[page], 1);
     });
     __syncthreads();
-    each([&](int64_t e, const int32_t* entry) {
-      if (flags[e] == kShared) flags[e] = __ldcg(&t.refs[*entry]) <= 0 ? kLast : -1 - *entry;
-    });
-    __syncthreads();
-    each([&](int64_t e, const int32_t* entry) {
-      if (flags[e] == kLast) atomicMin(&t.refs[*entry], (int)(-2 - e));
-    });
-    __syncthreads();
-    each([&](int64_t e, const int32_t* entry) {
-      if (flags[e] == kLast) flags[e] = __ldcg(&t.refs[*entry]) == (int)(-2 - e) ? kKeeps : -1 - *entry;
-    });
-    __syncthreads();
-    each([&](int64_t e, const int32_t* entry) {
-      if (flags[e] == kKeeps) __stcg(&t.refs[*entry], 1);
-    });
   }
   // The list of entries that need a page.
-  for (int s = warp; s < t.seqs; s += kReserveWarps) {
-    int n = 0;
-    for (int c = begin[s]; c < end[s]; c += 32) {
-      const int flag = c + lane < end[s] ? flags[(int64_t)s * t.columns + c + lane] : kOwn;
-      n += __popc(__ballot_sync(0xffffffffu, flag < 0 || flag == kMissing));
-    }
-    if (lane == 0) needs[s] = n;
-  }
-  __syncthreads();
-  int total;
-  const int before = block_exclusive(tid < t.seqs ? needs[tid] : 0, warps, &total);
-  if (tid < t.seqs) needs[tid] = before;
-  __syncthreads();
-  for (int s = warp; s < t.seqs; s += kReserveWarps) {
-    int at = needs[s];
-    for (int c = begin[s]; c < end[s]; c += 32) {
-      const int64_t e = (int64_t)s * t.columns + c + lane;
-      const int flag = c + lane < end[s] ? flags[e] : kOwn;
-      const bool need = flag < 0 || flag == kMissing;
-      const unsigned all = __ballot_sync(0xffffffffu, need);
-      if (need) list[at + __popc(all & ((1u << lane) - 1))] = (int32_t)e;
-      at += __popc(all);
-    }
+  int total = 0;
+  for (int base = 0; base < entries; base += kReserveThreads) {
+    const int i = base + tid, note = i < entries ? notes[i] : kOwn;
+    const bool need = note < 0 || note == kMissing;
+    int here;
+    const int rank = block_exclusive(need ? 1 : 0, warps, &here);
+    if (need) list[total + rank] = i;
+    total += here;
   }
   __syncthreads();
   // Free pages, in order, to the list's entries.
@@ -312,13 +357,12 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(const TableVie
     int rank = found + block_exclusive(__popc(free), warps, &here);
     for (; free != 0 && rank < total; free &= free - 1, ++rank) {
       const int page = (int)(base + 4 * tid + __ffs(free) - 1);
-      const int64_t e = list[rank];
-      const int s = (int)(e / t.columns), c = (int)(e - (int64_t)s * t.columns);
+      const int i = list[rank], s = sequence_of(i), c = begin[s] + (i - before[s]);
       t.table[s * t.ld + c] = page;
       __stcg(&t.refs[page], 1);
-      const int f = first[s];
-      if (flags[e] < 0 && c == f >> t.shift && (f & page_mask) != 0) {
-        copies[s * 3] = -1 - flags[e];
+      const int note = notes[i], f = first[s];
+      if (note < 0 && c == f >> t.shift && (f & page_mask) != 0) {
+        copies[s * 3] = -1 - note;
         copies[s * 3 + 1] = page;
         copies[s * 3 + 2] = f & page_mask;
       }
@@ -327,17 +371,12 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(const TableVie
   }
   if (found < total) {  // all as it was
     __syncthreads();
-    for (int i = tid; i < total; i += kReserveThreads) {
-      const int64_t e = list[i];
-      const int s = (int)(e / t.columns), c = (int)(e - (int64_t)s * t.columns);
-      int32_t* entry = &t.table[s * t.ld + c];
-      if (i < found) __stcg(&t.refs[*entry], 0);
-      if (flags[e] < 0) {
-        *entry = -1 - flags[e];
-        atomicAdd(&t.refs[*entry], 1);
-      } else {
-        *entry = -1;
-      }
+    for (int k = tid; k < total; k += kReserveThreads) {
+      const int i = list[k], note = notes[i];
+      int32_t* entry = entry_of(i);
+      if (k < found) __stcg(&t.refs[*entry], 0);
+      *entry = note < 0 ? -1 - note : -1;
+      if (note < 0) atomicAdd(&t.refs[-1 - note], 1);
     }
     if (tid < t.seqs) copies[tid * 3] = copies[tid * 3 + 1] = copies[tid * 3 + 2] = -1;
   }
@@ -504,9 +543,9 @@ int af1_pages_reserve(const af1_page_table* table, const int32_t* first, const i
        (rc = check_words(counts, "counts", dev)) != AF1_OK || (rc = check_words(copies, "copies", dev)) != AF1_OK ||
        (rc = check_pointer(workspace, "workspace", dev)) != AF1_OK))
     return rc;
-  int32_t* flags = static_cast<int32_t*>(workspace);
+  int32_t* notes = static_cast<int32_t*>(workspace);
   reserve_kernel<<<1, kReserveThreads, 0, static_cast<cudaStream_t>(stream)>>>(
-      t, first, counts, copies, lacking, flags, flags + (int64_t)t.seqs * t.columns);
+      t, first, counts, copies, lacking, notes, notes + (int64_t)t.seqs * t.columns);
   return launched(who);
 }
 
