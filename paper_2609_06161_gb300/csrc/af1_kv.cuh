@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <string>
 
 #include "af1.h"
@@ -58,5 +59,17 @@ static __device__ __forceinline__ int64_t kv_row(const KvView& c, const PageTabl
 int check_pointer(const void* p, const char* name, int device);
 int check_align(const void* p, int bytes, const char* name);
 KvView view_of(const af1_kv_desc& d);
+// Sets a kernel's attributes once for each device (setting them takes longer than a launch): `done` has a bit for each
+// of the first 64, set by the first call that succeeds. They are the same for every call, so that threads may race.
+template <typename F>
+cudaError_t once_per_device(std::atomic<uint64_t>& done, F&& set) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (e != cudaSuccess || (done.load(std::memory_order_acquire) & bit) != 0) return e;
+  e = set();
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
 
 }  // namespace af1

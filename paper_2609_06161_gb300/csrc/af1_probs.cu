@@ -645,8 +645,9 @@ int fail(int code, const std::string& msg) { return set_error(code, "af1_token_p
 template <typename T>
 cudaError_t launch(const ProbsProblem& p, int64_t rows, int cluster, cudaStream_t st) {
   const int smem = p.held * 16;
-  // Always the most, so that calls of several threads do not lower each other's.
-  cudaError_t e = cudaFuncSetAttribute(probs_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost * 16);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = once_per_device(
+      done, [] { return cudaFuncSetAttribute(probs_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost * 16); });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows * cluster));

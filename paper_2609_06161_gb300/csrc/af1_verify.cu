@@ -457,9 +457,12 @@ cudaError_t launch(const VerifyProblem& p, int64_t sequences, int cluster, cudaS
   cfg.gridDim = dim3((unsigned)(sequences * cluster));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = p.held * kWarps * 16 * (DRAFT ? 2 : 1);
-  // Always the most, so that calls of several threads do not lower each other's.
-  cudaError_t e = cudaFuncSetAttribute(verify_kernel<DRAFT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostHeld);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(verify_kernel<DRAFT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = once_per_device(done, [] {
+    const cudaError_t first = cudaFuncSetAttribute(verify_kernel<DRAFT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostHeld);
+    if (first != cudaSuccess) return first;
+    return cudaFuncSetAttribute(verify_kernel<DRAFT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  });
   if (e != cudaSuccess) return e;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];

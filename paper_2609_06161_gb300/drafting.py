@@ -192,7 +192,7 @@ class PageTable:
         if size < 0:
             raise AF1Error(int(size), last_error())
         self.table, self.refs, self.page_size = table, refs, page_size
-        self._workspace_bytes = size
+        self._workspace_bytes, self._workspaces = size, {}  # a workspace for each stream that has had a call
 
     @classmethod
     def empty(cls, sequences: int, columns: int, pages: int, page_size: int, device=None):
@@ -221,10 +221,12 @@ class PageTable:
             copies = _empty(shape, _I32, self.table.device, stream)
         if lacking is None:
             lacking = _empty((1,), _I32, self.table.device, stream)
-        workspace = _empty((self._workspace_bytes,), torch.uint8, self.table.device, stream)
+        handle = _stream_handle(stream)
+        workspace = self._workspaces.get(handle)
+        if workspace is None:
+            workspace = self._workspaces[handle] = _empty((self._workspace_bytes,), torch.uint8, self.table.device, stream)
         _check(_pages_reserve(ctypes.byref(self._d), fp, cp, _index(copies, "copies", shape),
-                              _index(lacking, "lacking", (1,)), workspace.data_ptr(), self._workspace_bytes,
-                              _stream_handle(stream)))
+                              _index(lacking, "lacking", (1,)), workspace.data_ptr(), self._workspace_bytes, handle))
         return copies, lacking
 
     def release(self, lens: torch.Tensor, stream=None) -> None:
