@@ -27,7 +27,7 @@ constexpr int kLogThreads = 8, kThreads = 1 << kLogThreads;
 constexpr int kBlocks = 5;  // blocks to an SM
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kListed = 1024;      // keys of a row that its CTAs list
+constexpr int kLogListed = 10, kListed = 1 << kLogListed;  // keys of a row that its CTAs list
 constexpr int kBins = 2048;
 constexpr int kMost = 100 * 1024 / 16;  // 16-byte accesses of a CTA's stretch in shared memory
 constexpr float kInf = __builtin_huge_valf();
@@ -44,6 +44,7 @@ struct ProbsProblem {
   const float* min_p;
   float all_temperature, all_min_p;
   int all_top_k;
+  int log_cluster;
   int held;  // accesses that a CTA keeps in shared memory; 0: its stretch is read again for every pass
 };
 
@@ -100,6 +101,15 @@ struct Piece {
   }
 };
 
+// All threads of the cluster meet; what those that `wrote` wrote to the others' memory is seen there. (A release by every
+// thread costs them all a wait for their stores.)
+__device__ __forceinline__ void meet(bool wrote) {
+  if (wrote) asm volatile("fence.acq_rel.cluster;" ::: "memory");
+  __syncwarp();
+  cluster_arrive_relaxed();
+  cluster_wait();
+}
+
 // What a CTA says of its stretch to the others.
 struct Said {
   float top, bound, sum;
@@ -128,9 +138,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   __shared__ float here_low;
   __shared__ long long warp_mass[kWarps];
   cg::cluster_group cluster = cg::this_cluster();
-  const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int cs = 1 << p.log_cluster, rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
-  const int64_t row = blockIdx.x / cs;
+  const int64_t row = blockIdx.x >> p.log_cluster;
   const T* x = static_cast<const T*>(p.logits) + row * p.ld;
   float* out = p.probs + row * p.probs_ld;
 
@@ -138,7 +148,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   // `begin` .. begin + n - 1, numbered from 0, of which those from j0 up to j1 lie in the row as a whole.
   const int skew = (int)((uintptr_t)x / sizeof(T) % E);
   const int64_t all = ((int64_t)p.vocab + skew + E - 1) / E;
-  const int begin = (int)(all * rank / cs), n = (int)(all * (rank + 1) / cs) - begin;
+  const int begin = (int)(all * rank >> p.log_cluster), n = (int)(all * (rank + 1) >> p.log_cluster) - begin;
   const int64_t first_entry = (int64_t)begin * E - skew;
   const int j0 = first_entry < 0 ? 1 : 0, j1 = first_entry + (int64_t)n * E > p.vocab ? n - 1 : n;
   const uint4* source = reinterpret_cast<const uint4*>(x + first_entry);
@@ -228,9 +238,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   // Where `need` lanes of every CTA have an entry of at least some bound, top_k entries of the row have. Each warp puts
   // its lanes' largest in order and gives two from about as far down as the bound lies; the largest of these that enough
   // lanes reach is the CTA's, and the least of the CTAs' the row's.
-  const int whole = (int)min(all / cs, (int64_t)kThreads) / 32;  // warps whose lanes all have entries, in every CTA
-  const int need = (int)(((int64_t)max(set.top_k, 0) + cs - 1) / cs);
-  const int part = whole > 0 ? (int)(((int64_t)need + whole - 1) / whole) : 33;  // lanes of each
+  const int whole = min((int)(all >> p.log_cluster), kThreads) / 32;  // warps whose lanes all have entries, in every CTA
+  const int need = (int)(((int64_t)max(set.top_k, 0) + cs - 1) >> p.log_cluster);
+  const int part = whole == 0 || need > 32 * kWarps ? 33 : (need + whole - 1) / whole;  // lanes of each
   const bool bounded = set.top_k >= 1 && part <= 32;
   if (bounded) {
     const float sorted = sort_descending(top, lane);  // a row with a NaN has no use for it
@@ -307,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
       }
     }
   }
-  cluster.sync();
+  meet(tid < cs);
   set = settings;
   Said one = said[lane % kMaxCluster < cs ? lane % kMaxCluster : 0];
   top = one.top;
@@ -342,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
       for (int w = 0; w < kWarps; ++w) first = min(first, warp_i[w]);
       *cluster.map_shared_rank(&all_first[rank], tid) = first;
     }
-    cluster.sync();
+    meet(tid < cs);
     first = all_first[0];
     for (int i = 1; i < cs; ++i) first = min(first, all_first[i]);
     write([&](int j, float (&y)[E]) {
@@ -384,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   int last = 0x7fffffff;
   const int top_k = set.top_k < 1 || set.top_k >= p.vocab ? 0x7fffffff : set.top_k;
   // The entries that reach both bounds, as keys that put them in order; everyone gets everyone's.
-  const int room = kListed / cs;
+  const int room = kListed >> p.log_cluster;
   const float from = top_k < p.vocab ? fmaxf(low, bound) : low;
   if (from > -kInf || p.vocab <= room) {
     for (int j = tid; j < n; j += kThreads) {
@@ -412,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
       for (int j = tid; j < mine; j += kThreads)
         *cluster.map_shared_rank(&lists[rank * room + j], i) = lists[rank * room + j];
   }
-  cluster.sync();
+  meet(tid < mine || tid == 0);
   bool fits = true;
   int listed = 0;
   for (int i = 0; i < cs; ++i) fits = fits && all_listed[i] <= room, listed += min(all_listed[i], room);
@@ -423,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
     uint64_t key[kOwn];
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-      const int slot = tid + i * kThreads, of = slot / room;
+      const int slot = tid + i * kThreads, of = slot >> (kLogListed - p.log_cluster);
       key[i] = of < cs && slot - of * room < all_listed[of] ? lists[slot] : 0;
     }
     uint64_t least = 0;
@@ -643,7 +653,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
 int fail(int code, const std::string& msg) { return set_error(code, "af1_token_probs: " + msg); }
 
 template <typename T>
-cudaError_t launch(const ProbsProblem& p, int64_t rows, int cluster, cudaStream_t st) {
+cudaError_t launch(const ProbsProblem& p, int64_t rows, cudaStream_t st) {
+  const int cluster = 1 << p.log_cluster;
   const int smem = p.held * 16;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = once_per_device(
@@ -697,18 +708,17 @@ int af1_token_probs(const af1_probs_args* a, void* stream) {
     if ((rc = check_pointer(t.p, t.name, dev)) != AF1_OK || (rc = check_align(t.p, t.align, t.name)) != AF1_OK) return rc;
   }
   ProbsProblem p = {a->logits, a->ld,    a->probs,           a->probs_ld,  (int)a->vocab,  a->temperature,
-                    a->top_k,  a->min_p, a->all_temperature, a->all_min_p, a->all_top_k, 0};
+                    a->top_k,  a->min_p, a->all_temperature, a->all_min_p, a->all_top_k, 0, 0};
   // CTAs of a row: as many as give each thread two accesses, while two to an SM
   // take all rows, or until a stretch is at most 32 KB, so that three to an SM are in different passes.
-  const int64_t accesses = (a->vocab * es + 15) / 16 + 1;
-  int cluster = 1;
-  while (cluster < kMaxCluster &&
-         ((a->rows * cluster * 2 <= 2 * sms && accesses >= 2 * cluster * kThreads) || accesses > 2048 * cluster))
-    cluster *= 2;
-  const int64_t stretch = (accesses + cluster - 1) / cluster;
-  p.held = stretch <= kMost ? (int)stretch : 0;
+  const int64_t pieces = (a->vocab * es + 15) / 16 + 1;
+  while (p.log_cluster < 3 && (((a->rows << p.log_cluster) <= sms && pieces >= (int64_t)4 * kThreads << p.log_cluster) ||
+                               pieces > (int64_t)2048 << p.log_cluster))
+    ++p.log_cluster;
+  const int64_t part = (pieces + (1 << p.log_cluster) - 1) >> p.log_cluster;
+  p.held = part <= kMost ? (int)part : 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  e = a->dtype == AF1_F16 ? launch<__half>(p, a->rows, cluster, st) : launch<float>(p, a->rows, cluster, st);
+  e = a->dtype == AF1_F16 ? launch<__half>(p, a->rows, st) : launch<float>(p, a->rows, st);
   if (e != cudaSuccess) return fail(AF1_ERR_CUDA, std::string(cudaGetErrorName(e)) + " (" + cudaGetErrorString(e) + ")");
   set_error(AF1_OK, "");
   return AF1_OK;
