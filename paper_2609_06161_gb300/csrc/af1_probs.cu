@@ -175,8 +175,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   };
   float* const target = out + first_entry;
   const bool wide = (uintptr_t)target % 16 == 0;
-  auto write = [&](auto&& f) {  // f(piece's number, results)
-    for (int j = tid; j < n; j += kThreads) {
+  auto write_some = [&](int from, int step, auto&& f) {  // f(piece's number, results)
+#pragma unroll 2
+    for (int j = from; j < n; j += step) {
       float y[E];
       f(j, y);
       if (wide && j >= j0 && j < j1) {
@@ -193,17 +194,29 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
     }
   };
 
+  auto write = [&](auto&& f) { write_some(tid, kThreads, f); };
+
   // -- the stretch: its largest entry; its sum, where nothing is cut; a bound that top_k entries of the row reach
   cluster_arrive_relaxed();  // the others' memory is written to when they have begun
-  if (tid == 0) {
-    here_settings.temperature = p.temperature == nullptr ? p.all_temperature : p.temperature[row];
-    here_settings.min_p = p.min_p == nullptr ? p.all_min_p : p.min_p[row];
-    here_settings.top_k = p.top_k == nullptr ? p.all_top_k : p.top_k[row];
-    here_listed = 0, here_last = -1;
-  }
-  auto slow = [&] {  // FP64: by one thread, while its first entries are on their way
-    if (tid == 0 && here_settings.min_p > 0.f)
-      here_cut = (double)fminf(here_settings.temperature, 1e30f) * log((double)fminf(here_settings.min_p, 1.f));
+  Settings set = {};
+  auto uncut = [&] { return (set.top_k < 1 || set.top_k >= p.vocab) && !(set.min_p > 0.f); };
+  // While the first entries are on their way: the settings; the cut in FP64, which is slow, by one thread; zeros, where few
+  // entries will be kept, which are then all that is left to write.
+  bool zeroed = false;
+  auto meanwhile = [&] {
+    set.temperature = p.temperature == nullptr ? p.all_temperature : __ldg(p.temperature + row);
+    set.min_p = p.min_p == nullptr ? p.all_min_p : __ldg(p.min_p + row);
+    set.top_k = p.top_k == nullptr ? p.all_top_k : __ldg(p.top_k + row);
+    zeroed = !uncut() || !(set.temperature >= 1e-30f);
+    if (zeroed && warp != 0)  // not by the warp whose stores the others wait for
+      write_some(tid - 32, kThreads - 32, [&](int, float (&y)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = 0.f;
+      });
+    if (tid == 0) {
+      here_settings = set, here_listed = 0, here_last = -1;
+      if (set.min_p > 0.f) here_cut = (double)fminf(set.temperature, 1e30f) * log((double)fminf(set.min_p, 1.f));
+    }
   };
   float top = -kInf;
   if (held) {
@@ -213,12 +226,13 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
       else
         stretch[j] = fetch(j).w;
     }
-    slow();
+    meanwhile();
     asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 4
     for (int j = tid; j < n; j += kThreads) top = max_nan(top, piece(j).most());
   } else {
     constexpr int U = 4;
-    slow();
+    meanwhile();
     for (int at = tid; at < n; at += U * kThreads) {
       Piece<T> w[U];
 #pragma unroll
@@ -234,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   for (int d = 16; d > 0; d >>= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
   if (lane == 0) warp_f[warp] = most;
   __syncthreads();
-  Settings set = here_settings;
+  set = here_settings;
   // Where `need` lanes of every CTA have an entry of at least some bound, top_k entries of the row have. Each warp puts
   // its lanes' largest in order and gives two from about as far down as the bound lies; the largest of these that enough
   // lanes reach is the CTA's, and the least of the CTAs' the row's.
@@ -272,7 +286,6 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
       y[e] = make_float2(ex2(d.x), ex2(d.y));
     }
   };
-  auto uncut = [&] { return (set.top_k < 1 || set.top_k >= p.vocab) && !(set.min_p > 0.f); };
   auto block_sum = [&](float sum) {  // for all threads
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -355,6 +368,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
     meet(tid < cs);
     first = all_first[0];
     for (int i = 1; i < cs; ++i) first = min(first, all_first[i]);
+    if (zeroed) {
+      if (tid == 0 && first >= first_entry && first < first_entry + (int64_t)n * E) out[first] = 1.f;
+      return;
+    }
     write([&](int j, float (&y)[E]) {
       const int v = index_of(j);
 #pragma unroll
@@ -494,6 +511,13 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
 #pragma unroll
     for (int d = kWarps / 2; d > 0; d >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, d);
     inverse = 1.f / ((float)mass * 9.094947017729282e-13f);
+    if (zeroed) {  // this CTA's entries to their places
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i)
+        if (key[i] != 0 && key[i] >= least && (tid + i * kThreads) >> (kLogListed - p.log_cluster) == rank)
+          out[(int)~(uint32_t)key[i]] = ex2((key_value((uint32_t)(key[i] >> 32)) - top) * c) * inverse;
+      return;
+    }
   } else {
     if (top_k < p.vocab) {
       // The k-th largest key by counts of its digits: 11, 11 and 10 bits (FP16 has 22).
