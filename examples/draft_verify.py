@@ -1,7 +1,7 @@
 """Drafted tokens verified in one pass: a small decoder of AF1 layers with a
 paged, quantised cache.
 
-    python examples/draft_verify.py [--kind int8] [--tokens 48]
+    python examples/draft_verify.py [--kind int8] [--tokens 48] [--temperature 0.8]
 
 A decoder with random weights generates greedily. Each step drafts a tree of
 tokens (here: the true continuation, found by a plain decoder for the
@@ -9,6 +9,11 @@ demonstration, beside wrong guesses), runs the whole tree through the layers
 at once, scores every node, and accepts the longest path that greedy decoding
 would have taken. The accepted keys and values are written again to the slots
 behind the prefix, where the next step expects them.
+
+With a temperature it samples: the tree is verified against the target's
+probabilities with random numbers, the accepted slots move behind the prefix
+as they are, and the cache's pages are reserved and released step by step.
+Nothing but the tokens comes back to the host.
 """
 from __future__ import annotations
 
@@ -165,9 +170,60 @@ def run(kind="int8", steps=48, drafted=5, prompt=9, seed=0, say=print):
     return plain[:steps], found[:steps], passes, off
 
 
+def sample(kind="int8", steps=48, drafted=5, prompt=9, seed=0, temperature=0.8, top_k=50, say=print):
+    """(tokens by plain greedy decoding, sampled tokens, passes): guesses around the greedy text, verified at this
+    temperature (0: what comes out is the greedy text)."""
+    decoder = Decoder(kind=kind, seed=seed)
+    g = torch.Generator().manual_seed(seed)
+    start = torch.randint(0, decoder.vocab, (prompt,), generator=g).cuda()
+    logits, _ = decoder.forward(start, 0, torch.arange(prompt, device="cuda"))
+    first = int(logits[-1].argmax())
+    plain = [first] + greedy(decoder, first, prompt, steps + drafted)
+
+    # The same cache, now through a table of pages that grows with the text.
+    one = lambda x: torch.tensor([x], dtype=torch.int32, device="cuda")  # noqa: E731
+    cache = decoder.caches[0]
+    table = af1.PageTable.empty(1, decoder.pages.shape[1], cache.pages, cache.page_size)
+    decoder.pages = table.table
+    lens = one(0)
+    table.reserve(lens, one(prompt))
+    decoder.forward(start, 0, torch.arange(prompt, device="cuda"))
+    lens += prompt
+    found, length, passes = [first], prompt, 0
+    while len(found) <= steps:
+        at = len(found) - 1
+        tokens, parents = draft([found[-1]] + plain[at + 1: at + drafted], decoder.vocab, g)
+        n = len(tokens)
+        depth = torch.zeros(n, dtype=torch.int64)
+        for i in range(1, n):
+            depth[i] = depth[parents[i]] + 1
+        tokens = torch.tensor(tokens, dtype=torch.int32, device="cuda")
+        parents = torch.tensor(parents, dtype=torch.int32, device="cuda")[None]
+        copies, lacking = table.reserve(lens, one(n))
+        af1.kv_copy(decoder.caches, copies)  # of pages that other sequences hold, too: there are none here
+        logits, _ = decoder.forward(tokens.long(), length, depth.cuda(), mask=af1.tree_mask(parents))
+        probs = af1.token_probs(logits, temperature=temperature, top_k=top_k)
+        path, lengths, following = af1.verify_tree(probs[None], tokens[None], parents, torch.rand((1, n), generator=g).cuda())
+        af1.kv_compact(decoder.caches, table.table, lens, path, lengths)
+        lens += lengths
+        table.release(lens)
+        passes += 1
+        accepted = path[0, 1: int(lengths[0])].long()
+        found += tokens[accepted].tolist() + [int(following[0])]
+        length += int(lengths[0])
+        assert int(lacking[0]) == 0, "no pages are left"
+    say(f"{kind} at temperature {temperature}: {len(found) - 1} tokens in {passes} passes of drafts "
+        f"({(len(found) - 1) / passes:.2f} a pass)")
+    return plain[:steps], found[:steps], passes
+
+
 if __name__ == "__main__":
     p = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     p.add_argument("--kind", choices=["f16", "int8", "e4m3", "int4"], default="int8")
     p.add_argument("--tokens", type=int, default=48)
+    p.add_argument("--temperature", type=float, default=None, help="sample at this temperature")
     a = p.parse_args()
-    run(a.kind, a.tokens)
+    if a.temperature is None:
+        run(a.kind, a.tokens)
+    else:
+        sample(a.kind, a.tokens, temperature=a.temperature)

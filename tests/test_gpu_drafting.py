@@ -270,7 +270,8 @@ def drawn_tokens(g, draft, parents, distinct):
 
 @pytest.mark.parametrize("mode", ["drawn", "distinct", "guessed"])
 @pytest.mark.parametrize("b,n,vocab", [(1, 1, 1), (3, 2, 1), (2, 5, 2), (4, 8, 5), (6, 64, 37), (5, 6, 1000), (3, 7, 4096),
-                                       (2, 12, 32001), (40, 4, 515), (1, 6, 128001), (400, 3, 130)])
+                                       (2, 12, 32001), (40, 4, 515), (1, 6, 128001), (400, 3, 130), (20, 3, 70001),
+                                       (320, 2, 3001), (1, 3, 1 << 22), (9, 2, 300007)])
 def test_verify_sizes(P, mode, b, n, vocab):
     g, rng = gen(b * 1000 + n), np.random.default_rng(n)
     probs, draft = distributions(g, b, n, vocab, 0.7)
@@ -816,3 +817,23 @@ def test_compacted_path_attends_like_appended_tokens(P):
         z.append(k[path], v[path], pages, seq(4), slots(4), rope=rope)
         for x, y in zip(a.read(pages, one(first + 4)), z.read(pages, one(first + 4))):
             assert torch.equal(x[:, first:], y[:, first:])
+
+
+@pytest.mark.parametrize("kind", ["int8", "f16"])
+@pytest.mark.parametrize("temperature", [0.0, 1.0])
+def test_the_example_samples(kind, temperature):
+    """At temperature 0 the verified text is the greedy one, until a near tie parts them (as for the example's greedy
+    drafts); at another it runs."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    try:
+        import draft_verify
+    finally:
+        sys.path.pop(0)
+    plain, found, passes = draft_verify.sample(kind, steps=30, temperature=temperature, say=lambda _: None)
+    assert len(found) == 30 and all(0 <= t < 1000 for t in found)
+    if temperature == 0.0:
+        same = next((i for i, (a, b) in enumerate(zip(plain, found)) if a != b), len(plain))
+        assert same >= 20, (plain, found)
+        assert passes < 30  # drafts were accepted
