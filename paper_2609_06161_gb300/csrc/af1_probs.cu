@@ -26,7 +26,7 @@ namespace {
 constexpr int kLogThreads = 8, kThreads = 1 << kLogThreads;
 constexpr int kBlocks = 5;  // blocks to an SM
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;
 constexpr int kLogListed = 10, kListed = 1 << kLogListed;  // keys of a row that its CTAs list
 constexpr int kBins = 2048;
 constexpr int kMost = 100 * 1024 / 16;  // 16-byte accesses of a CTA's stretch in shared memory
@@ -433,13 +433,13 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   }
   __syncthreads();
   const int mine = here_listed;
-  for (int i = 0; i < cs; ++i) {
-    if (tid == 0) *cluster.map_shared_rank(&all_listed[rank], i) = mine;
-    if (i != rank && mine <= room)
-      for (int j = tid; j < mine; j += kThreads)
-        *cluster.map_shared_rank(&lists[rank * room + j], i) = lists[rank * room + j];
-  }
-  meet(tid < mine || tid == 0);
+  if (tid < cs) *cluster.map_shared_rank(&all_listed[rank], tid) = mine;
+  if (mine <= room)
+    for (int i = tid; i < mine << p.log_cluster; i += kThreads) {  // key i / cs to CTA i % cs
+      uint64_t* key = &lists[rank * room + (i >> p.log_cluster)];
+      if ((i & (cs - 1)) != rank) *cluster.map_shared_rank(key, i & (cs - 1)) = *key;
+    }
+  meet(tid < max(cs, min(mine, room + 1) << p.log_cluster));
   bool fits = true;
   int listed = 0;
   for (int i = 0; i < cs; ++i) fits = fits && all_listed[i] <= room, listed += min(all_listed[i], room);
@@ -681,8 +681,11 @@ cudaError_t launch(const ProbsProblem& p, int64_t rows, cudaStream_t st) {
   const int cluster = 1 << p.log_cluster;
   const int smem = p.held * 16;
   static std::atomic<uint64_t> done{0};
-  const cudaError_t e = once_per_device(
-      done, [] { return cudaFuncSetAttribute(probs_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost * 16); });
+  const cudaError_t e = once_per_device(done, [] {
+    const cudaError_t first = cudaFuncSetAttribute(probs_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost * 16);
+    if (first != cudaSuccess) return first;
+    return cudaFuncSetAttribute(probs_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows * cluster));
@@ -736,7 +739,7 @@ int af1_token_probs(const af1_probs_args* a, void* stream) {
   // CTAs of a row: as many as give each thread two accesses, while two to an SM
   // take all rows, or until a stretch is at most 32 KB, so that three to an SM are in different passes.
   const int64_t pieces = (a->vocab * es + 15) / 16 + 1;
-  while (p.log_cluster < 3 && (((a->rows << p.log_cluster) <= sms && pieces >= (int64_t)4 * kThreads << p.log_cluster) ||
+  while ((1 << p.log_cluster) < kMaxCluster && (((a->rows << p.log_cluster) <= sms && pieces >= (int64_t)4 * kThreads << p.log_cluster) ||
                                pieces > (int64_t)2048 << p.log_cluster))
     ++p.log_cluster;
   const int64_t part = (pieces + (1 << p.log_cluster) - 1) >> p.log_cluster;
