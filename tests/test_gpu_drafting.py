@@ -496,6 +496,28 @@ def test_compact_bad_slots(P):
             assert np.array_equal(got.cpu().numpy(), x)
 
 
+@pytest.mark.parametrize("order", ["path", "any"])
+@pytest.mark.parametrize("layers,heads", [(12, 7), (40, 7), (40, 8)])
+def test_compact_many_layers(P, layers, heads, order):
+    """A model's layers, of different heads, in one call."""
+    g, rng = gen(layers), np.random.default_rng(layers)
+    b, nodes, columns = 60, 21, 5
+    caches = [filled(P, g, KINDS[i % 4], b * columns, 16, heads - 4 * (i % 5 == 3), 64) for i in range(layers)]
+    pages = torch.tensor(rng.permutation(b * columns).reshape(b, columns), dtype=I32, device="cuda")
+    first = torch.tensor(rng.integers(0, 55, b), dtype=I32, device="cuda")
+    index = np.sort(rng.permuted(np.tile(np.arange(1, nodes), (b, 1)), axis=1)[:, :9], axis=1)
+    index = np.concatenate((np.zeros((b, 1), np.int64), index, np.full((b, nodes - 10), -1)), 1)
+    if order == "any":
+        index[::2, :10] = index[::2, 9::-1]
+    index = torch.tensor(index, dtype=I32, device="cuda")
+    counts = torch.tensor(rng.integers(0, 11, b), dtype=I32, device="cuda")
+    want = [compact_oracle(c, pages, first, index, counts) for c in caches]
+    P.kv_compact(caches, pages, first, index, counts)
+    for c, w in zip(caches, want):
+        for got, x in zip(parts(c), w):
+            assert np.array_equal(got.cpu().numpy(), x)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("dim,page,heads", [(64, 16, 1), (128, 16, 8), (64, 64, 3), (128, 256, 2)])
 def test_copy(P, kind, dim, page, heads):
