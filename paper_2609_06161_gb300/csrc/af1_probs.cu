@@ -119,6 +119,7 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_constant__ ProbsProblem p) {
   constexpr int E = 16 / (int)sizeof(T);
   extern __shared__ uint4 stretch[];
+  __shared__ alignas(16) uint4 zeros[64];
   // Written by the cluster's CTAs, each once for a purpose.
   __shared__ Settings settings, here_settings;
   __shared__ double cut;
@@ -200,19 +201,43 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   cluster_arrive_relaxed();  // the others' memory is written to when they have begun
   Settings set = {};
   auto uncut = [&] { return (set.top_k < 1 || set.top_k >= p.vocab) && !(set.min_p > 0.f); };
+  auto few_kept = [&] { return !uncut() || !(set.temperature >= 1e-30f); };
   // While the first entries are on their way: the settings; the cut in FP64, which is slow, by one thread; zeros, where few
   // entries will be kept, which are then all that is left to write.
   bool zeroed = false;
+  auto zeros_are_there = [&] {  // before anything else is written to their places, or the CTA ends
+    if (warp == 1) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    if (zeroed) __syncthreads();
+  };
   auto meanwhile = [&] {
     set.temperature = p.temperature == nullptr ? p.all_temperature : __ldg(p.temperature + row);
     set.min_p = p.min_p == nullptr ? p.all_min_p : __ldg(p.min_p + row);
     set.top_k = p.top_k == nullptr ? p.all_top_k : __ldg(p.top_k + row);
-    zeroed = !uncut() || !(set.temperature >= 1e-30f);
-    if (zeroed && warp != 0)  // not by the warp whose stores the others wait for
+    zeroed = few_kept();
+    if (zeroed && wide) {
+      // One warp has 1 KB of zeros copied to all of them; the ends are written one by one.
+      if (warp == 1) {
+        zeros[lane] = zeros[32 + lane] = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        const int bytes = max(0, j1 - j0) * E * 4;
+        for (int at = lane * (int)sizeof(zeros); at < bytes; at += 32 * (int)sizeof(zeros))
+          asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(
+                           reinterpret_cast<uint8_t*>(target + (int64_t)j0 * E) + at),
+                       "r"(smem_u32(zeros)), "r"(min((int)sizeof(zeros), bytes - at))
+                       : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      } else if (warp == 2 && lane < 2 * E) {
+        const int j = lane < E ? 0 : n - 1;
+        const int64_t v = first_entry + (int64_t)j * E + lane % E;
+        if (!(j >= j0 && j < j1) && v >= 0 && v < p.vocab) out[v] = 0.f;
+      }
+    } else if (zeroed && warp != 0) {  // not by the warp whose stores the others wait for
       write_some(tid - 32, kThreads - 32, [&](int, float (&y)[E]) {
 #pragma unroll
         for (int e = 0; e < E; ++e) y[e] = 0.f;
       });
+    }
     if (tid == 0) {
       here_settings = set, here_listed = 0, here_last = -1;
       if (set.min_p > 0.f) here_cut = (double)fminf(set.temperature, 1e30f) * log((double)fminf(set.min_p, 1.f));
@@ -248,7 +273,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   for (int d = 16; d > 0; d >>= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
   if (lane == 0) warp_f[warp] = most;
   __syncthreads();
-  set = here_settings;
+  set = here_settings;  // every thread the first one's
+  zeroed = few_kept();
   // Where `need` lanes of every CTA have an entry of at least some bound, top_k entries of the row have. Each warp puts
   // its lanes' largest in order and gives two from about as far down as the bound lies; the largest of these that enough
   // lanes reach is the CTA's, and the least of the CTAs' the row's.
@@ -342,6 +368,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   }
 
   if (!(top < kInf) || top == -kInf) {
+    zeros_are_there();
     const float fill = top == -kInf ? 0.f : __int_as_float(0x7fffffff);
     write([&](int, float (&y)[E]) {
 #pragma unroll
@@ -368,6 +395,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
     meet(tid < cs);
     first = all_first[0];
     for (int i = 1; i < cs; ++i) first = min(first, all_first[i]);
+    zeros_are_there();
     if (zeroed) {
       if (tid == 0 && first >= first_entry && first < first_entry + (int64_t)n * E) out[first] = 1.f;
       return;
@@ -382,6 +410,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   const float t = fminf(set.temperature, 1e30f);
   c = 1.4426950408889634f / t;
   if (uncut()) {
+    zeros_are_there();
     const float mine = lane < cs ? one.sum * ex2(fmaxf((one.top - top) * c, kLeast)) : 0.f;
     sum = one.top > -kInf ? mine : 0.f;  // a stretch of -infinity alone has no sum
 #pragma unroll
@@ -511,6 +540,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
 #pragma unroll
     for (int d = kWarps / 2; d > 0; d >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, d);
     inverse = 1.f / ((float)mass * 9.094947017729282e-13f);
+    zeros_are_there();
     if (zeroed) {  // this CTA's entries to their places
 #pragma unroll
       for (int i = 0; i < kOwn; ++i)
@@ -658,6 +688,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
     sum = 0.f;
     for (int i = 0; i < cs; ++i) sum += all_sums[i];
     inverse = 1.f / sum;
+    zeros_are_there();
   }
   write([&](int j, float (&y)[E]) {
     const Piece<T> w = piece(j);
