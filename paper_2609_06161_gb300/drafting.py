@@ -96,7 +96,7 @@ def token_probs(logits: torch.Tensor, temperature=1.0, top_k=0, min_p=0.0, out: 
 
 def verify_tree(probs: torch.Tensor, tokens: torch.Tensor, parents: torch.Tensor, uniforms: torch.Tensor,
                 draft: torch.Tensor | None = None, counts: torch.Tensor | None = None, distinct: bool = False,
-                stream=None):
+                out=None, stream=None):
     """(path, lengths, following) of drafted trees (af1_verify_tree): the
     accepted nodes of every sequence from node 0 on, then -1 (sequences, nodes);
     how many they are; the token that follows.
@@ -106,7 +106,9 @@ def verify_tree(probs: torch.Tensor, tokens: torch.Tensor, parents: torch.Tensor
     token and the root. uniforms: float32 (sequences, nodes), number 0 for the
     token that follows. draft: the probabilities that every node's children were
     drawn from, like probs; None: the children are guesses. distinct: siblings
-    were drawn without repetition. counts: nodes of each sequence's tree."""
+    were drawn without repetition. counts: nodes of each sequence's tree. out:
+    three contiguous int32 tensors for the results; without them a call takes
+    the host 10 us more."""
     ps = _steps(probs, "probs", 3)
     sequences, nodes, vocab = probs.shape
     if probs.dtype is not _F32:
@@ -122,9 +124,15 @@ def verify_tree(probs: torch.Tensor, tokens: torch.Tensor, parents: torch.Tensor
         raise ValueError(f"uniforms must be a contiguous float32 tensor of shape {(sequences, nodes)}")
     tp, pp = _index(tokens, "tokens", (sequences, nodes)), _index(parents, "parents", (sequences, nodes))
     cp = _index(counts, "counts", (sequences,))
-    device = probs.device
-    path = _empty((sequences, nodes), _I32, device, stream)
-    lengths, following = _empty((sequences,), _I32, device, stream), _empty((sequences,), _I32, device, stream)
+    if out is None:
+        device = probs.device
+        path = _empty((sequences, nodes), _I32, device, stream)
+        lengths, following = _empty((sequences,), _I32, device, stream), _empty((sequences,), _I32, device, stream)
+    else:
+        path, lengths, following = out
+        _index(path, "out[0]", (sequences, nodes))
+        _index(lengths, "out[1]", (sequences,))
+        _index(following, "out[2]", (sequences,))
     if sequences == 0:
         return path, lengths, following
     a = _VerifyArgs(probs.data_ptr(), ps[0], ps[1], _ptr(draft), qs[0], qs[1], tp, pp, cp, uniforms.data_ptr(),
@@ -193,6 +201,8 @@ class PageTable:
             raise AF1Error(int(size), last_error())
         self.table, self.refs, self.page_size = table, refs, page_size
         self._workspace_bytes, self._workspaces = size, {}  # a workspace for each stream that has had a call
+        self._copies = torch.full((sequences, 3), -1, dtype=_I32, device=table.device)
+        self._lacking = torch.zeros(1, dtype=_I32, device=table.device)
 
     @classmethod
     def empty(cls, sequences: int, columns: int, pages: int, page_size: int, device=None):
@@ -214,19 +224,18 @@ class PageTable:
         """Pages of the sequences' own for counts slots from `first` on
         (af1_pages_reserve). Returns (copies, lacking): what kv_copy has to copy
         before these slots are written, (sequences, 3), and the number of pages
-        that were lacking, (1,); if it is not 0, no page has changed hands."""
+        that were lacking, (1,); if it is not 0, no page has changed hands. Where
+        they are not given they are the table's own, as table and refs are, and
+        hold until the next call."""
         fp, cp = self._per_sequence(first, "first"), self._per_sequence(counts, "counts")
-        shape = (self.table.shape[0], 3)
-        if copies is None:
-            copies = _empty(shape, _I32, self.table.device, stream)
-        if lacking is None:
-            lacking = _empty((1,), _I32, self.table.device, stream)
+        copies = self._copies if copies is None else copies
+        lacking = self._lacking if lacking is None else lacking
+        op, lp = _index(copies, "copies", (self.table.shape[0], 3)), _index(lacking, "lacking", (1,))
         handle = _stream_handle(stream)
         workspace = self._workspaces.get(handle)
         if workspace is None:
             workspace = self._workspaces[handle] = _empty((self._workspace_bytes,), torch.uint8, self.table.device, stream)
-        _check(_pages_reserve(ctypes.byref(self._d), fp, cp, _index(copies, "copies", shape),
-                              _index(lacking, "lacking", (1,)), workspace.data_ptr(), self._workspace_bytes, handle))
+        _check(_pages_reserve(ctypes.byref(self._d), fp, cp, op, lp, workspace.data_ptr(), self._workspace_bytes, handle))
         return copies, lacking
 
     def release(self, lens: torch.Tensor, stream=None) -> None:

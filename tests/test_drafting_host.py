@@ -89,7 +89,9 @@ def test_verify_arguments(P):
                dict(tokens=torch.zeros(b, n, dtype=torch.int64)), dict(parents=torch.zeros(b, n + 1, dtype=I32)),
                dict(uniforms=torch.zeros(b, n, dtype=torch.float64)), dict(uniforms=torch.zeros(b, 2 * n)[:, ::2]),
                dict(draft=torch.zeros(b, n, v + 1)), dict(draft=torch.zeros(b, n, v, dtype=F16)),
-               dict(draft=torch.zeros(b, n, 2 * v)[..., ::2]), dict(counts=torch.zeros(3, dtype=I32)), dict(distinct=True)):
+               dict(draft=torch.zeros(b, n, 2 * v)[..., ::2]), dict(counts=torch.zeros(3, dtype=I32)), dict(distinct=True),
+               dict(out=(torch.zeros(b, n, dtype=I32), torch.zeros(b, dtype=I32), torch.zeros(b))),
+               dict(out=(torch.zeros(b, n + 1, dtype=I32), torch.zeros(b, dtype=I32), torch.zeros(b, dtype=I32)))):
         with pytest.raises(ValueError):
             P.verify_tree(**{**good, **kw})
     with pytest.raises((P.AF1Error, RuntimeError)):

@@ -400,6 +400,9 @@ def test_verify_greedy(P):
     tokens[:, ::2] = torch.randint(0, vocab, (b, n // 2), generator=g, device="cuda", dtype=I32)
     u = torch.rand((b, n), generator=g, device="cuda")
     path, lengths, following = check_verify(P, probs, tokens, parents, u)
+    given = tuple(torch.full_like(t, 7) for t in (path, lengths, following))
+    assert all(a is z for a, z in zip(P.verify_tree(probs, tokens, parents, u, out=given), given))
+    assert all(torch.equal(a, z) for a, z in zip(given, (path, lengths, following)))
     last = path.gather(1, (lengths[:, None] - 1).long())
     assert torch.equal(following, best.gather(1, last.long())[:, 0].to(I32))
 
