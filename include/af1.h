@@ -778,7 +778,9 @@ AF1_API int af1_token_logprobs(const af1_logprob_args* args, void* stream);
  *       scalar beside it for all rows.
  *   probs: FP32 [rows][vocab], row stride probs_ld.
  * A row of -infinity alone gives zeros, one with a NaN or +infinity NaN
- * everywhere. Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
+ * everywhere. Exponents and sums are FP32; an e^((x_i - M) / T) below 2^-126 is
+ * 0. probs is a function of the inputs to the bit.
+ * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
 typedef struct af1_probs_args {
   const void* logits;
   int64_t rows, vocab, ld; /* 0 .. 2^24, 1 .. 2^31 - 1, vocab .. 2^36 */

@@ -6,10 +6,28 @@
 // most `last`.
 //
 // A cluster of CTAs takes a row, each CTA a stretch of it, which it reads once
-// into shared memory. The k-th largest is found there by four counts of 8 bits
-// each of the entries' keys (their bits as ordered integers), which the CTAs
-// add up through distributed shared memory; ties at the bound go by index. So
-// a row is read once and written once, and device memory bounds large calls.
+// into shared memory (up to 100 KB; longer ones are read again for every pass). A row is
+// written once, so device memory bounds large calls; small ones are bound by the
+// chain of one pass and exchange after another.
+//   - Nothing cut: every CTA sums its weights relative to its own largest entry;
+//     one exchange, then the row is written.
+//   - Cut: the k-th largest lane's maximum bounds the k-th largest entry from below. The
+//     entries that reach the bound and the least share (300 of 128001 for k = 200)
+//     are listed as keys of 64 bits (the value as an ordered integer, then the
+//     index, inverted), so that ties go by index; every CTA gets all keys, finds the k-th
+//     and sums the kept weights. The row's zeros are on their way by then, so that
+//     only the kept entries are left to write.
+//   - Where more entries reach the bound than the lists hold (1024 of a row; large k, many ties): the k-th
+//     largest key by counts of its digits, over all entries.
+// FP64 is slow enough here that the cut's logarithm, computed by every thread, took a
+// CTA 8 us: one thread computes it while the first entries are on their way.
+//
+// Measured (GPU, from a CUDA graph): 512 rows of 128001 FP16 logits with cuts
+// of their own 89 us (4.4 TB/s of logits and probabilities; of measured 6.8), uncut 83; 128 rows of 128000 FP32
+// uncut 30 (4.4 TB/s); 5 of 32000 FP32 with k = 50 7.4. In a CTA's life of 17 us under load its
+// copies land after 5, the first exchange takes 2, listing 2.5, the second exchange 3. Five CTAs
+// to an SM hide one another's waits: persistent clusters with the next row on its way, three to
+// an SM, took 170 us for 99 then, stretches of 16 KB 170, 512 threads 131, and a row read again instead of held 110.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -24,12 +42,12 @@ namespace af1 {
 namespace {
 
 constexpr int kLogThreads = 8, kThreads = 1 << kLogThreads;
-constexpr int kBlocks = 5;  // blocks to an SM
+constexpr int kBlocks = 5;  // CTAs to an SM
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
 constexpr int kLogListed = 10, kListed = 1 << kLogListed;  // keys of a row that its CTAs list
-constexpr int kBins = 2048;
-constexpr int kMost = 100 * 1024 / 16;  // 16-byte accesses of a CTA's stretch in shared memory
+constexpr int kBins = 2048;          // of a digit
+constexpr int kMost = 100 * 1024 / 16;  // 16-byte pieces of a CTA's stretch in shared memory
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLeast = -1e4f;  // 2^d is 0 from far above on
 
@@ -45,7 +63,7 @@ struct ProbsProblem {
   float all_temperature, all_min_p;
   int all_top_k;
   int log_cluster;
-  int held;  // accesses that a CTA keeps in shared memory; 0: its stretch is read again for every pass
+  int held;  // pieces that a CTA keeps in shared memory; 0: its stretch is read again for every pass
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -126,7 +144,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   __shared__ Said said[kMaxCluster];
   __shared__ float all_sums[kMaxCluster];
   __shared__ int all_first[kMaxCluster], all_listed[kMaxCluster], all_equal[kMaxCluster], all_last[kMaxCluster];
-  __shared__ alignas(16) uint64_t lists[kListed];  // of every CTA a part; later the few keys near the k-th, or counts of digits
+  __shared__ alignas(16) uint64_t lists[kListed];  // of every CTA a part; later the keys near the k-th, or counts of digits
   // The CTA's own.
   __shared__ float warp_f[kWarps], tried[2 * kWarps];
   __shared__ int warp_i[kWarps], found[3], here_listed, here_last;
@@ -767,12 +785,14 @@ int af1_token_probs(const af1_probs_args* a, void* stream) {
   }
   ProbsProblem p = {a->logits, a->ld,    a->probs,           a->probs_ld,  (int)a->vocab,  a->temperature,
                     a->top_k,  a->min_p, a->all_temperature, a->all_min_p, a->all_top_k, 0, 0};
-  // CTAs of a row: as many as give each thread two accesses, while two to an SM
-  // take all rows, or until a stretch is at most 32 KB, so that three to an SM are in different passes.
+  // CTAs of a row: until all rows have one to an SM, while each thread has two pieces (5 rows of 32000: 8 CTAs to a row
+  // 7.4 us, one 16); and until a stretch is at most 32 KB, so that five to an SM are in different passes (128 rows of
+  // 128000 FP32: 16 CTAs 30 us, 8 of 64 KB 34; 512 rows of FP16 in 4 of 64 KB 103, in 8 of 32 KB 106, in 16 of 16 KB 170).
   const int64_t pieces = (a->vocab * es + 15) / 16 + 1;
-  while ((1 << p.log_cluster) < kMaxCluster && (((a->rows << p.log_cluster) <= sms && pieces >= (int64_t)4 * kThreads << p.log_cluster) ||
-                               pieces > (int64_t)2048 << p.log_cluster))
-    ++p.log_cluster;
+  auto more = [&](int64_t ctas) {
+    return pieces > 2048 * ctas || (a->rows * ctas <= sms && pieces >= 4 * kThreads * ctas);
+  };
+  while ((1 << p.log_cluster) < kMaxCluster && more(1 << p.log_cluster)) ++p.log_cluster;
   const int64_t part = (pieces + (1 << p.log_cluster) - 1) >> p.log_cluster;
   p.held = part <= kMost ? (int)part : 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);

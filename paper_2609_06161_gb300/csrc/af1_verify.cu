@@ -15,16 +15,24 @@
 // Comparisons decide, so that every step is defined to the last bit: P - c Q is
 // an FP32 product and difference, each rounded; masses are whole multiples of
 // 2^-40 of it, so that their sums do not depend on an order; the walk's few
-// numbers are FP64. A sum of whole numbers costs no wide arithmetic: an FP32
-// addition of 12 and back splits r into a multiple of 2^-20 and a rest, another
-// addition rounds the rest to a multiple of 2^-40, and 16 of either add up
-// exactly in FP32 before they go to integers.
+// numbers are FP64. A sum of whole numbers costs no wide arithmetic: the bits of
+// r + 12 count multiples of 2^-20, those of the rest (exact) and a constant count
+// multiples of 2^-40, and both add up as 32-bit integers.
 //
 // A cluster of CTAs takes a sequence. The numbers that the walk needs (four to a
-// node) are fetched for all nodes at once; its first CTA walks, the
-// others wait for rows to sum: every CTA has a stretch of the vocabulary, so
-// that a row is summed and then searched (one warp's stretch) where the sum of
-// the stretches before passes the bound. Only rows that the walk needs are read.
+// node) are fetched for all nodes at once by the first and given to all. One warp of
+// every CTA walks, all alike, so that only masses are exchanged; the others wait for rows to sum. Every
+// warp has a stretch of the vocabulary, so that a row is summed and then searched
+// (one warp's stretch, by marks in it) where the sum of the stretches before
+// passes the bound. Only rows that the walk needs are read, and with a draft, where they may be
+// summed more than once, they are kept in shared memory if there is room for them.
+//
+// What bounds it is latency: launch, two trips to memory for the nodes, their exchange, half a
+// microsecond for every node that is looked at, and for every row its trip, an exchange and the search.
+// GPU times: 8 chains of 5 over 32000 tokens 7.7 us; 64 guessed trees of 32 over 128000 13 (33 MB of rows, of which
+// device memory would need 4.8); 16 trees of 16 over 128001, drawn without repetition, 25 (2.4): two to
+// four sums of a row of P and Q one after another, 3 to 5 us each. FP64 is slow enough to count:
+// with every thread walking the three took 14, 34 and 41 us; clear cases are decided in FP32 beside it.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -512,9 +520,10 @@ int af1_verify_tree(const af1_verify_args* a, void* stream) {
   VerifyProblem p = {a->probs,  a->probs_seq, a->probs_node, a->draft,   a->draft_seq,  a->draft_node, a->tokens,
                      a->parents, a->counts,   a->uniforms,   a->path,    a->lengths,    a->following,  (int)a->nodes,
                      (int)a->vocab, (a->flags & AF1_VERIFY_DISTINCT) != 0, 0, 0};
-  // CTAs of a sequence: as many as two to an SM allow, while each of their warps has 128 entries. (Clusters lie within
-  // parts of the GPU, whose SMs are no multiple of theirs: at one CTA to an SM there is room for 7 clusters of 16, 15 of 8,
-  // 36 of 4 and 76 of 2.)
+  // CTAs of a sequence: as many as two to an SM allow, while each of their warps has 128 entries (one tree over 128000
+  // tokens: 8 CTAs 9.9 us, 16 7.8). Clusters lie within parts of the GPU, whose SMs are no multiple of theirs: at one CTA
+  // to an SM there is room for 7 clusters of 16, 15 of 8, 36 of 4 and 76 of 2 (16 trees, kept rows of 128 KB a CTA: 16
+  // clusters of 8 came in two waves and took 9 us for a sum, where reading the rows again takes 5).
   const int64_t alone[] = {sms, sms / 2, sms * 36 / 152, sms * 15 / 152, sms * 7 / 152};
   int level = 0;
   while (level < 4 && a->sequences <= 2 * alone[level + 1] && a->vocab >= (128 * kWarps << (level + 1))) ++level;
