@@ -46,7 +46,8 @@ constexpr int kBlocks = 5;  // CTAs to an SM
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
 constexpr int kLogListed = 10, kListed = 1 << kLogListed;  // keys of a row that its CTAs list
-constexpr int kBins = 2048;          // of a digit
+constexpr int kFew = 768;            // a top_k that the lists mostly have room for
+constexpr int kBins = 2048;
 constexpr int kMost = 100 * 1024 / 16;  // 16-byte pieces of a CTA's stretch in shared memory
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLeast = -1e4f;  // 2^d is 0 from far above on
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   cluster_arrive_relaxed();  // the others' memory is written to when they have begun
   Settings set = {};
   auto uncut = [&] { return (set.top_k < 1 || set.top_k >= p.vocab) && !(set.min_p > 0.f); };
-  auto few_kept = [&] { return !uncut() || !(set.temperature >= 1e-30f); };
+  auto few_kept = [&] { return !(set.temperature >= 1e-30f) || set.min_p > 0.f || (!uncut() && set.top_k <= kFew); };
   // While the first entries are on their way: the settings; the cut in FP64, which is slow, by one thread; zeros, where few
   // entries will be kept, which are then all that is left to write.
   bool zeroed = false;
@@ -457,90 +458,109 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   }
   int last = 0x7fffffff;
   const int top_k = set.top_k < 1 || set.top_k >= p.vocab ? 0x7fffffff : set.top_k;
-  // The entries that reach both bounds, as keys that put them in order; everyone gets everyone's.
+  // The entries from `least_value` on that `is_one` takes, as keys that put them in order; everyone gets everyone's.
+  // Whether the lists hold them all; `listed` of them.
   const int room = kListed >> p.log_cluster;
-  const float from = top_k < p.vocab ? fmaxf(low, bound) : low;
-  if (from > -kInf || p.vocab <= room) {
-    for (int j = tid; j < n; j += kThreads) {
+  int listed = 0;
+  auto list_entries = [&](float least_value, bool some, auto&& is_one) {
+    for (int j = tid; some && j < n; j += kThreads) {
       const Piece<T> w = piece(j);
-      if (w.most() < from) continue;
+      if (w.most() < least_value) continue;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float v = (float)w.at(e);
         const int index = index_of(j) + e;
-        if (v >= from && index >= 0 && index < p.vocab) {
+        if (v >= least_value && index >= 0 && index < p.vocab && is_one(v)) {
           const int at = atomicAdd(&here_listed, 1);
           if (at < room) lists[rank * room + at] = (uint64_t)order_key(v) << 32 | (uint32_t)~index;
         }
       }
     }
     __syncthreads();
-  } else if (tid == 0) {
-    here_listed = room + 1;
-  }
-  __syncthreads();
-  const int mine = here_listed;
-  if (tid < cs) *cluster.map_shared_rank(&all_listed[rank], tid) = mine;
-  if (mine <= room)
-    for (int i = tid; i < mine << p.log_cluster; i += kThreads) {  // key i / cs to CTA i % cs
-      uint64_t* key = &lists[rank * room + (i >> p.log_cluster)];
-      if ((i & (cs - 1)) != rank) *cluster.map_shared_rank(key, i & (cs - 1)) = *key;
-    }
-  meet(tid < max(cs, min(mine, room + 1) << p.log_cluster));
-  bool fits = true;
-  int listed = 0;
-  for (int i = 0; i < cs; ++i) fits = fits && all_listed[i] <= room, listed += min(all_listed[i], room);
-  float inverse;
-  if (fits) {
-    // All keys, a few to a thread (0: none).
-    constexpr int kOwn = kListed / kThreads;
-    uint64_t key[kOwn];
+    const int mine = some ? here_listed : room + 1;
+    if (tid < cs) *cluster.map_shared_rank(&all_listed[rank], tid) = mine;
+    if (mine <= room)
+      for (int i = tid; i < mine << p.log_cluster; i += kThreads) {  // key i / cs to CTA i % cs
+        uint64_t* key = &lists[rank * room + (i >> p.log_cluster)];
+        if ((i & (cs - 1)) != rank) *cluster.map_shared_rank(key, i & (cs - 1)) = *key;
+      }
+    meet(tid < max(cs, min(mine, room + 1) << p.log_cluster));
+    bool fits = true;
+    listed = 0;
+    for (int i = 0; i < cs; ++i) fits = fits && all_listed[i] <= room, listed += min(all_listed[i], room);
+    return fits;
+  };
+  // All listed keys, a few to a thread (0: none).
+  constexpr int kOwn = kListed / kThreads;
+  uint64_t key[kOwn];
+  auto take_keys = [&] {
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
       const int slot = tid + i * kThreads, of = slot >> (kLogListed - p.log_cluster);
       key[i] = of < cs && slot - of * room < all_listed[of] ? lists[slot] : 0;
     }
+  };
+  auto value_of = [&](uint64_t k) { return key_value((uint32_t)(k >> 32)); };
+  // The key that k - 1 others are above: first the part of the range, one of kThreads equal ones, that it lies in, then its
+  // place among the keys of that part, which are few but for ties. `lowest`: -infinity if it is not known.
+  auto kth_of_keys = [&](int k, float lowest) {
+    __syncthreads();
+    parts[tid] = 0;
+    if (tid == 0) here_few = 0;
+    if (lowest == -kInf) {
+      lowest = kInf;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i)
+        if (key[i] != 0 && value_of(key[i]) > -kInf) lowest = fminf(lowest, value_of(key[i]));
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) lowest = fminf(lowest, __shfl_xor_sync(0xffffffffu, lowest, d));
+      if (lane == 0) warp_f[warp] = lowest;
+      __syncthreads();
+      for (int w = 0; w < kWarps; ++w) lowest = fminf(lowest, warp_f[w]);
+    }
+    // (Differences, products and minima keep the order of values, however they are rounded.)
+    const float scale = top > lowest ? (float)kThreads / (top - lowest) : 0.f;
+    auto part_of = [&](uint64_t one) { return (int)fminf((top - value_of(one)) * scale, (float)(kThreads - 1)); };
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      if (key[i] != 0) atomicAdd(&parts[part_of(key[i])], 1);
+    __syncthreads();
+    const int have = parts[tid];
+    int upto = have;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int other = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += other;
+    }
+    if (lane == 31) warp_i[warp] = upto;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) upto += warp_i[w];
+    if (upto - have < k && k <= upto) found[0] = tid, found[1] = k - (upto - have);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      if (key[i] != 0 && part_of(key[i]) == found[0]) few[atomicAdd(&here_few, 1)] = key[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      if (key[i] != 0 && part_of(key[i]) == found[0]) {
+        int above = 0;
+        for (int j = 0; j < here_few; ++j) above += few[j] > key[i] ? 1 : 0;
+        if (above == found[1] - 1) kth_key = key[i];
+      }
+    __syncthreads();
+    return kth_key;
+  };
+  const float from = top_k < p.vocab ? fmaxf(low, bound) : low;
+  const bool fits = list_entries(from, from > -kInf || p.vocab <= room, [](float) { return true; });
+  float inverse;
+  if (fits) {
+    take_keys();
     uint64_t least = 0;
     if (listed > top_k) {
-      // The key that k - 1 others are above: first the part of the range, one of kThreads, that it lies in, then its place
-      // among the keys of that part, which are few but for ties.
-      const uint32_t base = order_key(from), span = order_key(top) - base;
-      const int shift = max(0, 32 - __clz((int)span) - kLogThreads);
-      auto part_of = [&](uint64_t k) { return (int)(((uint32_t)(k >> 32) - base) >> shift); };
-      __syncthreads();
-      parts[tid] = 0;
-      if (tid == 0) here_few = 0;
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kOwn; ++i)
-        if (key[i] != 0) atomicAdd(&parts[part_of(key[i])], 1);
-      __syncthreads();
-      const int have = parts[kThreads - 1 - tid];
-      int upto = have;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int other = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += other;
-      }
-      if (lane == 31) warp_i[warp] = upto;
-      __syncthreads();
-      for (int w = 0; w < warp; ++w) upto += warp_i[w];
-      if (upto - have < top_k && top_k <= upto) found[0] = kThreads - 1 - tid, found[1] = top_k - (upto - have);
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kOwn; ++i)
-        if (key[i] != 0 && part_of(key[i]) == found[0]) few[atomicAdd(&here_few, 1)] = key[i];
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kOwn; ++i)
-        if (key[i] != 0 && part_of(key[i]) == found[0]) {
-          int above = 0;
-          for (int j = 0; j < here_few; ++j) above += few[j] > key[i] ? 1 : 0;
-          if (above == found[1] - 1) kth_key = key[i];
-        }
-      __syncthreads();
-      least = kth_key;
-      low = key_value((uint32_t)(least >> 32)), last = (int)~(uint32_t)least;
+      least = kth_of_keys(top_k, from);
+      low = value_of(least), last = (int)~(uint32_t)least;
     } else {
       low = from;  // these are all: at `low` or above, or as many as the k
     }
@@ -548,8 +568,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
     long long mass = 0;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i)
-      if (key[i] != 0 && key[i] >= least)
-        mass += __float2ll_rn(ex2((key_value((uint32_t)(key[i] >> 32)) - top) * c) * 1099511627776.f);
+      if (key[i] != 0 && key[i] >= least) mass += __float2ll_rn(ex2((value_of(key[i]) - top) * c) * 1099511627776.f);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, d);
     if (lane == 0) warp_mass[warp] = mass;
@@ -563,47 +582,44 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
 #pragma unroll
       for (int i = 0; i < kOwn; ++i)
         if (key[i] != 0 && key[i] >= least && (tid + i * kThreads) >> (kLogListed - p.log_cluster) == rank)
-          out[(int)~(uint32_t)key[i]] = ex2((key_value((uint32_t)(key[i] >> 32)) - top) * c) * inverse;
+          out[(int)~(uint32_t)key[i]] = ex2((value_of(key[i]) - top) * c) * inverse;
       return;
     }
   } else {
     if (top_k < p.vocab) {
-      // The k-th largest key by counts of its digits: 11, 11 and 10 bits (FP16 has 22).
+      // Counts of all entries in bins, the largest entries in the first, where the lists lay. A CTA adds up its share of
+      // the bins and gives the sums to all.
       int* const counts = reinterpret_cast<int*>(lists);
       static_assert(sizeof(lists) >= kBins * sizeof(int), "");
-      uint32_t prefix = 0;
-      int k = top_k, equal = 0;
-      bool cut = true;
-      constexpr int kLevels = sizeof(T) == 2 ? 2 : 3;
-#pragma unroll
-      for (int level = 0; level < kLevels; ++level) {
-        const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bins = level < 2 ? 2048 : 1024;
+      auto count_bins = [&](int bins, auto&& bin_of) {  // bin_of(value): below 0 for none
         cluster.sync();  // what lies there was read
         for (int i = tid; i < bins; i += kThreads) counts[i] = 0;
-        if (tid < 3) found[tid] = 0;
         __syncthreads();
         for (int j = tid; j < n; j += kThreads) {
           const Piece<T> w = piece(j);
-          if (w.most() < low) continue;
+          if (w.most() < from) continue;
 #pragma unroll
           for (int e = 0; e < E; ++e) {
             const float v = (float)w.at(e);
-            const uint32_t key = order_key(v);
-            if (v >= low && (level == 0 || key >> (level == 1 ? 21 : 10) == prefix))
-              atomicAdd(&counts[key >> shift & (bins - 1)], 1);
+            const int bin = v >= from ? bin_of(v) : -1;
+            if (bin >= 0) atomicAdd(&counts[bin], 1);
           }
         }
         cluster.sync();
-        // Each thread sums a few bins of all CTAs, the largest first.
+        const int share = bins >> p.log_cluster;
+        for (int i = rank * share + tid; i < (rank + 1) * share; i += kThreads) {
+          int sum_of = 0;
+          for (int r = 0; r < cs; ++r) sum_of += *cluster.map_shared_rank(&counts[i], r);
+          for (int r = 0; r < cs; ++r) *cluster.map_shared_rank(&counts[i], r) = sum_of;
+        }
+        cluster.sync();
+      };
+      // The bin of the k-th entry, its place there and how many are there, in `found`; the number of all.
+      auto find_bin = [&](int bins, int k) {
         const int per = bins / kThreads;
         int some[kBins / kThreads], here = 0;
 #pragma unroll
-        for (int j = 0; j < kBins / kThreads; ++j) {
-          some[j] = 0;
-          if (j >= per) break;
-          for (int i = 0; i < cs; ++i) some[j] += *cluster.map_shared_rank(&counts[bins - 1 - (tid * per + j)], i);
-          here += some[j];
-        }
+        for (int j = 0; j < kBins / kThreads; ++j) here += some[j] = j < per ? counts[tid * per + j] : 0;
         int upto = here;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -617,21 +633,70 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
           if (w < warp) upto += warp_i[w];
           total += warp_i[w];
         }
-        if (level == 0 && total <= k) {
-          cut = false;  // all that reach `low`
-          break;
-        }
         if (upto - here < k && k <= upto) {
           int left = k - (upto - here);
 #pragma unroll
           for (int j = 0; j < kBins / kThreads; ++j) {
-            if (j >= per) break;
-            if (left > 0 && left <= some[j]) found[0] = bins - 1 - (tid * per + j), found[1] = left, found[2] = some[j];
+            if (j < per && left > 0 && left <= some[j]) found[0] = tid * per + j, found[1] = left, found[2] = some[j];
             left -= some[j];
           }
         }
         __syncthreads();
-        prefix = prefix << (level == 2 ? 10 : 11) | (uint32_t)found[0];
+        return total;
+      };
+      // Bins of equal width first: what is in the k-th's bin mostly fits the lists.
+      float lowest = from;
+      if (from == -kInf) {
+        lowest = kInf;
+        for (int j = tid; j < n; j += kThreads) {
+          const Piece<T> w = piece(j);
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if ((float)w.at(e) > -kInf) lowest = fminf(lowest, (float)w.at(e));
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) lowest = fminf(lowest, __shfl_xor_sync(0xffffffffu, lowest, d));
+        __syncthreads();
+        if (lane == 0) warp_f[warp] = lowest;
+        __syncthreads();
+        if (tid < cs) {
+          for (int w = 0; w < kWarps; ++w) lowest = fminf(lowest, warp_f[w]);
+          *cluster.map_shared_rank(&all_sums[rank], tid) = lowest;
+        }
+        meet(tid < cs);
+        lowest = all_sums[0];
+        for (int i = 1; i < cs; ++i) lowest = fminf(lowest, all_sums[i]);
+      }
+      const float scale = top > lowest ? (float)kBins / (top - lowest) : 0.f;
+      auto wide_bin = [&](float v) { return (int)fminf((top - v) * scale, (float)(kBins - 1)); };
+      count_bins(kBins, wide_bin);
+      bool cut = find_bin(kBins, top_k) > top_k;
+      if (!cut) {
+        low = from;  // all that reach it
+      } else {
+        const int bin = found[0], place = found[1];
+        const bool try_lists = found[2] <= kListed;
+        if (tid == 0) here_listed = 0;
+        cluster.sync();  // counts were read
+        if (list_entries(from, try_lists, [&](float v) { return wide_bin(v) == bin; })) {
+          take_keys();
+          const uint64_t least = kth_of_keys(place, -kInf);
+          low = value_of(least), last = (int)~(uint32_t)least;
+          cut = false;
+        }
+      }
+      // Many of nearly the same value: by digits of their keys, 11, 11 and 10 bits (FP16 has 22).
+      uint32_t prefix = 0;
+      int k = top_k, equal = 0;
+      constexpr int kLevels = sizeof(T) == 2 ? 2 : 3;
+      for (int level = 0; cut && level < kLevels; ++level) {
+        const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level < 2 ? 11 : 10, bins = 1 << bits;
+        count_bins(bins, [&](float v) {
+          const uint32_t one = order_key(v);
+          return level == 0 || one >> (shift + bits) == prefix ? bins - 1 - (int)(one >> shift & (bins - 1)) : -1;
+        });
+        find_bin(bins, k);
+        prefix = prefix << bits | (uint32_t)(bins - 1 - found[0]);
         k = found[1];  // of the entries with this prefix
         equal = found[2];
       }

@@ -154,6 +154,25 @@ def test_probs_strides(P, dtype, shift, out_shift):
     assert (out[:, :out_shift] == -7).all() and (out[:, out_shift + vocab:] == -7).all()
 
 
+@pytest.mark.parametrize("dtype", [F16, F32])
+@pytest.mark.parametrize("vocab", [700, 3000, 20011, 128001, 700001])
+def test_probs_large_k(P, dtype, vocab):
+    """More entries than the lists hold: among spread values, values that crowd in one place of a wide range, many equal
+    ones, and rows with few entries that are not banned."""
+    g = gen(vocab)
+    x = draw_logits(g, 6, vocab, F32)
+    x[1] = torch.where(x[1] > 2, 1e4 * x[1], 1e-3 * x[1])
+    x[2] = (x[2] * 2).round() / 2
+    x[3, torch.rand(vocab, generator=g, device="cuda") < 0.9] = -INF
+    x[4] = 0.25
+    x[4, 5], x[4, vocab - 2] = 30.0, -1e4
+    x[5] = torch.where(x[5] > 0, 3e38, -3e38) if dtype == F32 else torch.where(x[5] > 0, 6e4, -6e4)
+    x = x.to(dtype)
+    for k in (257, vocab // 3, vocab // 2, vocab - 1):
+        for m in (0.0, 1e-3):
+            check_probs(P.token_probs(x, 1.1, k, m), x, 1.1, k, m)
+
+
 def test_probs_cut_next_to_an_entry(P):
     """The bound of min_p in 64 bits: entries a unit in the last place above and below it."""
     t, m = 0.75, 0.05
