@@ -779,7 +779,8 @@ AF1_API int af1_token_logprobs(const af1_logprob_args* args, void* stream);
  *   probs: FP32 [rows][vocab], row stride probs_ld.
  * A row of -infinity alone gives zeros, one with a NaN or +infinity NaN
  * everywhere. Exponents and sums are FP32; an e^((x_i - M) / T) below 2^-126 is
- * 0. probs is a function of the inputs to the bit.
+ * 0. The same call gives the same bits (a row among others may be summed in
+ * another order).
  * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
 typedef struct af1_probs_args {
   const void* logits;

@@ -17,8 +17,11 @@
 //     index, inverted), so that ties go by index; every CTA gets all keys, finds the k-th
 //     and sums the kept weights. The row's zeros are on their way by then, so that
 //     only the kept entries are left to write.
-//   - Where more entries reach the bound than the lists hold (1024 of a row; large k, many ties): the k-th
-//     largest key by counts of its digits, over all entries.
+//   - Where more entries reach the bound than the lists hold (1024 of a row; large k): the
+//     k-th's bin, of 2048 of equal width, by a count of all entries, and then its entries
+//     listed; where these are too many, too (ties), the k-th key by counts of its digits.
+//     A CTA adds up its share of all CTAs' counts (every CTA adding up all of them: 2.3 ms
+//     for 200 rows of 128001 FP32, k = 900, that take 0.15).
 // FP64 is slow enough here that the cut's logarithm, computed by every thread, took a
 // CTA 8 us: one thread computes it while the first entries are on their way.
 //
@@ -851,11 +854,14 @@ int af1_token_probs(const af1_probs_args* a, void* stream) {
   ProbsProblem p = {a->logits, a->ld,    a->probs,           a->probs_ld,  (int)a->vocab,  a->temperature,
                     a->top_k,  a->min_p, a->all_temperature, a->all_min_p, a->all_top_k, 0, 0};
   // CTAs of a row: until all rows have one to an SM, while each thread has two pieces (5 rows of 32000: 8 CTAs to a row
-  // 7.4 us, one 16); and until a stretch is at most 32 KB, so that five to an SM are in different passes (128 rows of
-  // 128000 FP32: 16 CTAs 30 us, 8 of 64 KB 34; 512 rows of FP16 in 4 of 64 KB 103, in 8 of 32 KB 106, in 16 of 16 KB 170).
-  const int64_t pieces = (a->vocab * es + 15) / 16 + 1;
+  // 7.4 us, one 16); and until a stretch is at most 64 KB where entries are cut, and 40 KB where not. Cuts cost a CTA as
+  // much as 30 KB, whatever its stretch, and write little at its end (200 rows of 128001 FP32, k = 300: 70 us in 8 CTAs, 83
+  // in 16); without them more CTAs to an SM, in different passes, are faster (200 rows of 128001 FP16: 38 us in 8, 43 in 4;
+  // 512 in 16, of 16 KB: 108 for 83).
+  const bool cuts = a->top_k != nullptr || a->min_p != nullptr || a->all_top_k > 0 || a->all_min_p > 0.f;
+  const int64_t most = cuts ? 4096 : 2560, pieces = (a->vocab * es + 15) / 16 + 1;
   auto more = [&](int64_t ctas) {
-    return pieces > 2048 * ctas || (a->rows * ctas <= sms && pieces >= 4 * kThreads * ctas);
+    return pieces > most * ctas || (a->rows * ctas <= sms && pieces >= 4 * kThreads * ctas);
   };
   while ((1 << p.log_cluster) < kMaxCluster && more(1 << p.log_cluster)) ++p.log_cluster;
   const int64_t part = (pieces + (1 << p.log_cluster) - 1) >> p.log_cluster;
