@@ -4,9 +4,12 @@
 //
 // Nothing is computed on keys and values: rows of codes and scales move as they
 // are, those of all layers in one launch (a launch for each of 32 layers would
-// take longer than their rows). Device memory bounds large calls, and latency
-// the others. The table's calls decide on the device, so that the lengths
-// that verification gives need not reach the host.
+// take longer than their rows). Device memory bounds large calls (100 INT4
+// pages of 128 slots in 16 layers, 525 MB: 79 us, 6.6 TB/s; 64 paths of 7 moved
+// rows in 32 FP16 layers, 117 MB in pieces of 256 bytes: 19 us, 25 from a cold
+// cache), and latency the others (2 to 4 us). The table's calls decide on the device, so that the lengths
+// that verification gives need not reach the host: fork, reserve and release take
+// 12.8 us for 256 sequences over 131072 pages, 9.6 for 16 over 1000.
 #include <algorithm>
 
 #include "af1_internal.h"
