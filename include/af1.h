@@ -784,7 +784,7 @@ AF1_API int af1_token_logprobs(const af1_logprob_args* args, void* stream);
  * Errors: INVALID_ARG, BAD_POINTER, MISALIGNED, CUDA. */
 typedef struct af1_probs_args {
   const void* logits;
-  int64_t rows, vocab, ld; /* 0 .. 2^24, 1 .. 2^31 - 1, vocab .. 2^36 */
+  int64_t rows, vocab, ld; /* 0 .. 2^24, 1 .. 2^30, vocab .. 2^36 */
   float* probs;
   int64_t probs_ld;        /* vocab .. 2^36 */
   const float* temperature;

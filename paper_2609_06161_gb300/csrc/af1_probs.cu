@@ -826,9 +826,9 @@ using namespace af1;
 
 int af1_token_probs(const af1_probs_args* a, void* stream) {
   if (a == nullptr) return fail(AF1_ERR_INVALID_ARG, "args is NULL");
-  if (a->rows < 0 || a->rows > (1 << 24) || a->vocab < 1 || a->vocab > 0x7fffffff || a->ld < a->vocab ||
+  if (a->rows < 0 || a->rows > (1 << 24) || a->vocab < 1 || a->vocab > (1 << 30) || a->ld < a->vocab ||
       a->ld > ((int64_t)1 << 36) || a->probs_ld < a->vocab || a->probs_ld > ((int64_t)1 << 36))
-    return fail(AF1_ERR_INVALID_ARG, "need rows 0..2^24, vocab 1..2^31 - 1, vocab <= ld, probs_ld <= 2^36");
+    return fail(AF1_ERR_INVALID_ARG, "need rows 0..2^24, vocab 1..2^30, vocab <= ld, probs_ld <= 2^36");
   if (a->dtype != AF1_F16 && a->dtype != AF1_F32) return fail(AF1_ERR_INVALID_ARG, "dtype must be AF1_F16 or AF1_F32");
   if (a->rows == 0) return AF1_OK;
   int dev = 0, sms = 0;

@@ -56,7 +56,7 @@ _pages_release = _declare("af1_pages_release", _P(_TableDesc), _vp, _vp)
 def _setting(value, what: str, rows: int, dtype):
     """(pointer, value for all rows) of a number or of a tensor of the rows' own."""
     if not isinstance(value, torch.Tensor):
-        return 0, value
+        return 0, float(value)
     if value.dtype is not dtype or value.shape != (rows,) or not value.is_contiguous():
         raise ValueError(f"{what} must be a number or a contiguous {dtype} tensor of shape {(rows,)}")
     return value.data_ptr(), 0

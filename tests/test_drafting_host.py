@@ -31,7 +31,7 @@ def refused(P, code, call, *args):
 
 
 @pytest.mark.parametrize("change", [
-    dict(rows=-1), dict(rows=(1 << 24) + 1), dict(vocab=0), dict(vocab=1 << 31), dict(ld=99), dict(ld=(1 << 36) + 1),
+    dict(rows=-1), dict(rows=(1 << 24) + 1), dict(vocab=0), dict(vocab=(1 << 30) + 1, ld=1 << 32, probs_ld=1 << 32), dict(ld=99), dict(ld=(1 << 36) + 1),
     dict(probs_ld=99), dict(probs_ld=(1 << 36) + 1), dict(dtype=2), dict(dtype=-1)])
 def test_probs_refusals(P, change):
     from paper_2609_06161_gb300 import drafting as D
