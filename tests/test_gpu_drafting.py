@@ -155,6 +155,34 @@ def test_probs_strides(P, dtype, shift, out_shift):
 
 
 @pytest.mark.parametrize("dtype", [F16, F32])
+@pytest.mark.parametrize("vocab", [16500, 34000, 50001, 128001])
+@pytest.mark.parametrize("order", ["any", "rising", "falling"])
+def test_probs_many_rows(P, dtype, vocab, order):
+    """Calls of more rows than the GPU takes at once in parts, each with its settings; largest entries early and late; ties,
+    infinities and rows of few entries among them."""
+    g = gen(vocab)
+    rows = 320
+    x = draw_logits(g, rows, vocab, F32)
+    if order != "any":
+        x[::2] = x[::2].sort(dim=-1, descending=order == "falling").values
+    x[3::16] = (x[3::16] * 2).round() / 2
+    x[5::16] = torch.where(torch.rand(x[5::16].shape, generator=g, device="cuda") < 0.997, -INF, x[5::16])
+    x[6, vocab // 2], x[7, 3], x[8], x[9, 1:] = NAN, INF, -INF, -INF
+    x[10] = 1.0
+    x = x.to(dtype)
+    t = torch.where(torch.rand(rows, generator=g, device="cuda") < 0.1, 0.0, 0.5 + torch.rand(rows, generator=g, device="cuda"))
+    k = torch.tensor([0, 1, 7, 50, 200, 255, 256, 257, 400, 700, 1000, 1023, 1024, 1500, vocab // 2, vocab - 1], dtype=I32,
+                     device="cuda")[torch.randint(0, 16, (rows,), generator=g, device="cuda")]
+    m = torch.tensor([0.0, 0.0, 0.5, 0.05, 1e-3, 1e-8], device="cuda")[torch.randint(0, 6, (rows,), generator=g, device="cuda")]
+    out = torch.full((rows, vocab + 3), -7.0, device="cuda")
+    y = P.token_probs(x, t, k, m, out=out[:, 1: vocab + 1])
+    check_probs(y, x, t, k, m)
+    assert (out[:, 0] == -7).all() and (out[:, vocab + 1:] == -7).all()
+    again = P.token_probs(x, t, k, m)
+    assert torch.equal(again.nan_to_num(7), y.nan_to_num(7))
+
+
+@pytest.mark.parametrize("dtype", [F16, F32])
 @pytest.mark.parametrize("vocab", [700, 3000, 20011, 128001, 700001])
 def test_probs_large_k(P, dtype, vocab):
     """More entries than the lists hold: among spread values, values that crowd in one place of a wide range, many equal
