@@ -784,6 +784,34 @@ def test_other_devices_and_streams(P):
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(y, plain)
 
+    # A chain of calls on two streams at once, each on tensors of its own.
+    def chain(stream):
+        one = lambda *v: torch.tensor(v, dtype=I32, device="cuda")  # noqa: E731
+        cache = filled(P, gen(3), "int8", 12, 16, 2, 64)
+        table = P.PageTable.empty(2, 5, 12, 16)
+        probs, parents, tokens = y[:6].view(2, 3, -1), one(-1, 0, 0, -1, 0, 1).view(2, 3), one(0, 5, 9, 0, 7, 3).view(2, 3)
+        u, first, n = torch.full((2, 3), 0.4, device="cuda"), one(0, 0), one(30, 20)
+        back = one(0, 0)
+        made = torch.cuda.Event()
+        made.record()
+        if stream is not None:
+            stream.wait_event(made)
+        table.reserve(first, n, stream=stream)
+        table.fork(back, stream=stream)
+        copies, _ = table.reserve(n, n, stream=stream)
+        P.kv_copy(cache, copies, stream=stream)
+        path, lengths, following = P.verify_tree(probs, tokens, parents, u, stream=stream)
+        P.kv_compact(cache, table.table, n, path, lengths, stream=stream)
+        table.release(n, stream=stream)
+        return [path, lengths, following, table.table, table.refs, copies] + parts(cache)
+
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    runs = [chain(s) for s in (side, other, None)]
+    torch.cuda.synchronize()
+    for a, b, c in zip(*runs):
+        assert torch.equal(a, c) and torch.equal(b, c)
+
 
 def test_a_step_in_a_graph(P):
     """Reserve, append, attend, probabilities, verification, compaction, release: captured once, replayed on new inputs,
@@ -909,3 +937,53 @@ def test_the_example_samples(kind, temperature):
         same = next((i for i, (a, b) in enumerate(zip(plain, found)) if a != b), len(plain))
         assert same >= 20, (plain, found)
         assert passes < 30  # drafts were accepted
+
+
+# -- offsets beyond 32 bits ------------------------------------------------------------
+
+
+def test_far_rows(P):
+    """Rows of logits and of probabilities more than 2^31 entries apart."""
+    g, rng = gen(20), np.random.default_rng(20)
+    far, vocab = (1 << 31) + 8, 3001
+    big = torch.empty(far + 4 * vocab, device="cuda")
+    x = big.as_strided((2, vocab), (far, 1))
+    x.copy_(draw_logits(g, 2, vocab, F32))
+    kw = dict(temperature=0.9, top_k=30, min_p=0.001)
+    check_probs(P.token_probs(x, **kw), x, **kw)
+    want = P.token_probs(x.contiguous(), **kw)
+    x.copy_(x.clone())
+    y = big.as_strided((2, vocab), (far, 1), vocab)
+    assert torch.equal(P.token_probs(x, out=y, **kw), want)
+
+    n = 4
+    probs, draft = distributions(g, 2, n, vocab // 4, 0.7)
+    parents = trees(rng, 2, n)
+    tokens = drawn_tokens(g, draft, parents, False)
+    u = torch.rand((2, n), generator=g, device="cuda")
+    p = big.as_strided((2, n, vocab // 4), (far, vocab // 4, 1))
+    p.copy_(probs)
+    check_verify(P, p, tokens, parents, u, draft)
+
+
+def test_far_pages(P):
+    """A cache of more than 2^31 bytes of keys."""
+    pages, page, heads = 20000, 64, 8
+    c = P.KVCache.empty(pages, page, heads, 128, "f16")
+    assert c.k.numel() * 2 > 1 << 31
+    near = [pages - 1, pages - 2, 0]
+    g = gen(21)
+    for t in (c.k, c.v):
+        for i in near:
+            t[i] = torch.randn(t.shape[1:], generator=g, device="cuda").half()
+    one = lambda *v: torch.tensor(v, dtype=I32, device="cuda")  # noqa: E731
+    want = [t[near].clone() for t in (c.k, c.v)]
+    P.kv_copy(c, one(pages - 1, 0, 40).view(1, 3))
+    for w in want:
+        w[2, :, :40] = w[0, :, :40]
+    P.kv_compact(c, one(pages - 1, pages - 2).view(1, 2), one(60), one(0, 2, 9, 5).view(1, 4), one(4))
+    for t, w in zip((c.k, c.v), want):
+        was = w.clone()
+        w[0, :, 61], w[0, :, 62], w[0, :, 63] = was[0, :, 62], was[1, :, 5], was[1, :, 1]
+        assert torch.equal(t[near], w)
+        assert float(t[1: pages - 2].abs().max()) == 0
