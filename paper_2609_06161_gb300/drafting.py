@@ -200,13 +200,15 @@ class PageTable:
         if size < 0:
             raise AF1Error(int(size), last_error())
         self.table, self.refs, self.page_size = table, refs, page_size
-        self._workspace_bytes, self._workspaces = size, {}  # a workspace for each stream that has had a call
-        self._copies = torch.full((sequences, 3), -1, dtype=_I32, device=table.device)
-        self._lacking = torch.zeros(1, dtype=_I32, device=table.device)
+        self._workspace_bytes = size
+        # (workspace, copies, lacking) for each stream that has had a reserve call, which writes them before it reads them:
+        # made at the first one, in that stream's order, and filled by nothing else.
+        self._buffers = {}
 
     @classmethod
     def empty(cls, sequences: int, columns: int, pages: int, page_size: int, device=None):
-        """A table without pages, over tensors of its own."""
+        """A table without pages, over tensors of its own, which are filled in
+        the order of the current stream."""
         device = device or torch.device("cuda", torch.cuda.current_device())
         return cls(torch.full((sequences, columns), -1, dtype=_I32, device=device),
                    torch.zeros(pages, dtype=_I32, device=device), page_size)
@@ -225,16 +227,23 @@ class PageTable:
         (af1_pages_reserve). Returns (copies, lacking): what kv_copy has to copy
         before these slots are written, (sequences, 3), and the number of pages
         that were lacking, (1,); if it is not 0, no page has changed hands. Where
-        they are not given they are the table's own, as table and refs are, and
-        hold until the next call."""
+        they are not given they are tensors that the table has for this stream,
+        and hold until the next call on it."""
         fp, cp = self._per_sequence(first, "first"), self._per_sequence(counts, "counts")
-        copies = self._copies if copies is None else copies
-        lacking = self._lacking if lacking is None else lacking
-        op, lp = _index(copies, "copies", (self.table.shape[0], 3)), _index(lacking, "lacking", (1,))
+        sequences, device = self.table.shape[0], self.table.device
+        op, lp = _index(copies, "copies", (sequences, 3)), _index(lacking, "lacking", (1,))
         handle = _stream_handle(stream)
-        workspace = self._workspaces.get(handle)
-        if workspace is None:
-            workspace = self._workspaces[handle] = _empty((self._workspace_bytes,), torch.uint8, self.table.device, stream)
+        own = self._buffers.get(handle)
+        if own is None:
+            own = self._buffers[handle] = (_empty((self._workspace_bytes,), torch.uint8, device, stream),
+                                           _empty((sequences, 3), _I32, device, stream), _empty((1,), _I32, device, stream))
+        workspace = own[0]
+        if copies is None:
+            copies = own[1]
+            op = copies.data_ptr()
+        if lacking is None:
+            lacking = own[2]
+            lp = lacking.data_ptr()
         _check(_pages_reserve(ctypes.byref(self._d), fp, cp, op, lp, workspace.data_ptr(), self._workspace_bytes, handle))
         return copies, lacking
 

@@ -813,6 +813,28 @@ def test_other_devices_and_streams(P):
         assert torch.equal(a, c) and torch.equal(b, c)
 
 
+def test_a_table_made_while_the_current_stream_is_busy(P):
+    """Tables made behind work that the current stream still has to do, and used on another stream, which table and refs
+    are ordered with: nothing that the table allocates for itself waits for the current stream."""
+    one = lambda *v: torch.tensor(v, dtype=I32, device="cuda")  # noqa: E731
+    side = torch.cuda.Stream()
+    big = torch.zeros(1 << 28, device="cuda")
+    first, n = one(3, 5, 2), one(1, 1, 20)
+    for work in (0, 100):  # once for what is done at first use
+        tables = [one(0, -1, 0, -1, 1, -1).view(3, 2) for _ in range(2)]
+        refs = [counted(t, pages) for t, pages in zip(tables, (6, 2))]
+        torch.cuda.synchronize()
+        for _ in range(work):
+            big.mul_(1.0)
+        got = [P.PageTable(t, r, 16).reserve(first, n, stream=side) for t, r in zip(tables, refs)]
+        torch.cuda.synchronize()
+        (copies, lacking), (no_copies, short) = got
+        assert copies.tolist() == [[0, 2, 3], [-1] * 3, [-1] * 3] and lacking.tolist() == [0]
+        assert tables[0].tolist() == [[2, -1], [0, -1], [1, 3]]
+        assert no_copies.tolist() == [[-1] * 3] * 3 and short.tolist() == [2]
+        assert tables[1].tolist() == [[0, -1], [0, -1], [1, -1]]
+
+
 def test_a_step_in_a_graph(P):
     """Reserve, append, attend, probabilities, verification, compaction, release: captured once, replayed on new inputs,
     with the lengths on the device throughout; against the same calls made one by one."""
