@@ -776,7 +776,9 @@ AF1_API int af1_token_logprobs(const af1_logprob_args* args, void* stream);
  *   logits: [rows][vocab] of `dtype`, row stride ld; -infinity bans a token.
  *   temperature, top_k, min_p: device [rows], each row's own, or NULL: the
  *       scalar beside it for all rows.
- *   probs: FP32 [rows][vocab], row stride probs_ld.
+ *   probs: FP32 [rows][vocab], row stride probs_ld. May be logits, if these are
+ *       FP32 with the same stride; otherwise no row of one overlaps a row of the
+ *       other (INVALID_ARG).
  * A row of -infinity alone gives zeros, one with a NaN or +infinity NaN
  * everywhere. Exponents and sums are FP32; an e^((x_i - M) / T) below 2^-126 is
  * 0. The same call gives the same bits (a row among others may be summed in

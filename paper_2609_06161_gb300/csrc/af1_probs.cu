@@ -80,6 +80,12 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
   return d;
 }
+// Not by way of the read-only cache: the row is written later.
+__device__ __forceinline__ uint4 load_plain(const uint4* at) {
+  uint4 w;
+  asm("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "l"(at));
+  return w;
+}
 // Larger for larger values, -0 as 0.
 __device__ __forceinline__ uint32_t order_key(float x) {
   const int32_t b = __float_as_int(x + 0.f);
@@ -137,7 +143,9 @@ struct Said {
   float top, bound, sum;
 };
 
-template <typename T>
+// IN_PLACE: probs is logits. A piece that is not held is written by the thread that read it last. (A kernel of its own:
+// with both ways in one 20 rows of 1000003 FP32, beside their logits, took 82 us for 78.)
+template <typename T, bool IN_PLACE>
 __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_constant__ ProbsProblem p) {
   constexpr int E = 16 / (int)sizeof(T);
   extern __shared__ uint4 stretch[];
@@ -179,7 +187,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   auto fetch = [&](int j) {  // entries outside the row are -infinity, which changes nothing
     Piece<T> y;
     if (j >= j0 && j < j1) {
-      y.w = __ldg(source + j);
+      y.w = IN_PLACE ? load_plain(source + j) : __ldg(source + j);
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -223,9 +231,11 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
   cluster_arrive_relaxed();  // the others' memory is written to when they have begun
   Settings set = {};
   auto uncut = [&] { return (set.top_k < 1 || set.top_k >= p.vocab) && !(set.min_p > 0.f); };
-  auto few_kept = [&] { return !(set.temperature >= 1e-30f) || set.min_p > 0.f || (!uncut() && set.top_k <= kFew); };
+  auto few_kept = [&] {
+    return !IN_PLACE && (!(set.temperature >= 1e-30f) || set.min_p > 0.f || (!uncut() && set.top_k <= kFew));
+  };
   // While the first entries are on their way: the settings; the cut in FP64, which is slow, by one thread; zeros, where few
-  // entries will be kept, which are then all that is left to write.
+  // entries will be kept, which are then all that is left to write (not in place: they would overtake the entries).
   bool zeroed = false;
   auto zeros_are_there = [&] {  // before anything else is written to their places, or the CTA ends
     if (warp == 1) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -793,15 +803,31 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
 
 int fail(int code, const std::string& msg) { return set_error(code, "af1_token_probs: " + msg); }
 
-template <typename T>
+// Whether a row of one matrix overlaps a row of another; bytes, and strides of at least a row.
+bool rows_overlap(const void* x, int64_t width, int64_t ld, const void* y, int64_t y_width, int64_t y_ld, int64_t rows) {
+  const int64_t a = (int64_t)(uintptr_t)x, b = (int64_t)(uintptr_t)y;
+  if (a + (rows - 1) * ld + width <= b || b + (rows - 1) * y_ld + y_width <= a) return false;
+  for (int64_t i = 0, j = 0; i < rows && j < rows;) {  // the one that ends first overlaps no later row
+    if (a + i * ld + width <= b + j * y_ld)
+      ++i;
+    else if (b + j * y_ld + y_width <= a + i * ld)
+      ++j;
+    else
+      return true;
+  }
+  return false;
+}
+
+template <typename T, bool IN_PLACE>
 cudaError_t launch(const ProbsProblem& p, int64_t rows, cudaStream_t st) {
   const int cluster = 1 << p.log_cluster;
   const int smem = p.held * 16;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = once_per_device(done, [] {
-    const cudaError_t first = cudaFuncSetAttribute(probs_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost * 16);
+    const cudaError_t first =
+        cudaFuncSetAttribute(probs_kernel<T, IN_PLACE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost * 16);
     if (first != cudaSuccess) return first;
-    return cudaFuncSetAttribute(probs_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return cudaFuncSetAttribute(probs_kernel<T, IN_PLACE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -816,7 +842,7 @@ cudaError_t launch(const ProbsProblem& p, int64_t rows, cudaStream_t st) {
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, probs_kernel<T>, p);
+  return cudaLaunchKernelEx(&cfg, probs_kernel<T, IN_PLACE>, p);
 }
 
 }  // namespace
@@ -831,11 +857,14 @@ int af1_token_probs(const af1_probs_args* a, void* stream) {
     return fail(AF1_ERR_INVALID_ARG, "need rows 0..2^24, vocab 1..2^30, vocab <= ld, probs_ld <= 2^36");
   if (a->dtype != AF1_F16 && a->dtype != AF1_F32) return fail(AF1_ERR_INVALID_ARG, "dtype must be AF1_F16 or AF1_F32");
   if (a->rows == 0) return AF1_OK;
+  const int es = a->dtype == AF1_F16 ? 2 : 4;
+  const bool in_place = a->logits == a->probs && es == 4 && (a->rows == 1 || a->ld == a->probs_ld);
+  if (!in_place && rows_overlap(a->logits, a->vocab * es, a->ld * es, a->probs, a->vocab * 4, a->probs_ld * 4, a->rows))
+    return fail(AF1_ERR_INVALID_ARG, "rows of probs overlap rows of logits (in place: FP32, with one stride)");
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return fail(AF1_ERR_CUDA, cudaGetErrorString(e));
-  const int es = a->dtype == AF1_F16 ? 2 : 4;
   struct {
     const void* p;
     const char* name;
@@ -867,7 +896,9 @@ int af1_token_probs(const af1_probs_args* a, void* stream) {
   const int64_t part = (pieces + (1 << p.log_cluster) - 1) >> p.log_cluster;
   p.held = part <= kMost ? (int)part : 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  e = a->dtype == AF1_F16 ? launch<__half>(p, a->rows, st) : launch<float>(p, a->rows, st);
+  e = a->dtype == AF1_F16 ? launch<__half, false>(p, a->rows, st)
+      : in_place          ? launch<float, true>(p, a->rows, st)
+                          : launch<float, false>(p, a->rows, st);
   if (e != cudaSuccess) return fail(AF1_ERR_CUDA, std::string(cudaGetErrorName(e)) + " (" + cudaGetErrorString(e) + ")");
   set_error(AF1_OK, "");
   return AF1_OK;

@@ -68,7 +68,7 @@ def token_probs(logits: torch.Tensor, temperature=1.0, top_k=0, min_p=0.0, out: 
     float32, after the temperature (0: greedy), of the top_k largest (0: all)
     that are at least min_p times as likely as the largest (af1_token_probs).
     Each setting is a number, or a tensor (rows,) of the rows' own: float32,
-    top_k int32."""
+    top_k int32. out: float32, with rows of its own, or float32 logits themselves."""
     ld = _steps(logits, "logits", 2)[0]
     dt = _dtype(logits, "logits")
     rows, vocab = logits.shape

@@ -63,6 +63,29 @@ def test_probs_arguments(P):
         P.token_probs(x)  # not on a GPU
 
 
+def test_probs_overlap(P):
+    """Rows of probabilities on rows of logits are refused, unless they are the same ones; between them they are not."""
+    from paper_2609_06161_gb300 import drafting as D
+    at = 1 << 20  # rows of 100 entries
+
+    def call(**change):
+        a = dict(logits=at, rows=3, vocab=100, ld=100, probs=at, probs_ld=100, all_temperature=1.0, dtype=1) | change
+        return D._token_probs(ctypes.byref(D._ProbsArgs(**a)), None)
+
+    for change in (dict(dtype=0), dict(probs=at + 4), dict(probs=at - 4), dict(probs_ld=101), dict(probs=at + 1196),
+                   dict(probs=at - 1196), dict(ld=200, probs=at + 396, probs_ld=200), dict(ld=1000, probs_ld=500),
+                   dict(ld=1000, probs=at + 4396 - 500 * 4, probs_ld=500), dict(ld=1 << 36, probs=at + (2 << 38), rows=1 << 24),
+                   dict(dtype=0, probs=at + 196), dict(dtype=0, rows=1), dict(rows=1, ld=200, probs=at + 396)):
+        refused(P, -1, lambda: call(**change))
+        assert "overlap" in P.last_error(), change
+    for change in (dict(), dict(ld=200, probs_ld=200), dict(rows=1, ld=200), dict(probs=at + 1200), dict(probs=at - 1200),
+                   dict(ld=200, probs=at + 400, probs_ld=200), dict(ld=200, probs=at - 400, probs_ld=200),
+                   dict(ld=1000, probs=at + 400, probs_ld=500), dict(dtype=0, probs=at + 600),
+                   dict(dtype=0, ld=400, probs=at + 200, probs_ld=200), dict(rows=1, ld=200, probs=at + 400)):
+        call(**change)
+        assert "overlap" not in P.last_error(), change
+
+
 # -- verification --------------------------------------------------------------------
 
 

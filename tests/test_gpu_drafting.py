@@ -201,6 +201,28 @@ def test_probs_large_k(P, dtype, vocab):
             check_probs(P.token_probs(x, 1.1, k, m), x, 1.1, k, m)
 
 
+@pytest.mark.parametrize("rows,vocab", [(3, 5), (24, 1003), (320, 40000), (48, 128001), (6, 500003)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_probs_in_place(P, rows, vocab, shift):
+    """out may be logits: the same results as beside them, whatever is cut; what lies between rows stays."""
+    g = gen(vocab)
+    big = torch.full((rows, vocab + 3), -7.0, device="cuda")
+    x = big[:, shift: shift + vocab]
+    start = draw_logits(g, rows, vocab, F32)
+    start[-1, vocab // 2:] = -INF
+    start[-2, 1] = NAN
+    pick = lambda *v: torch.tensor(v, device="cuda")[torch.randint(0, len(v), (rows,), generator=g, device="cuda")]  # noqa: E731
+    own = dict(temperature=pick(0.0, 0.7, 1.0, 1.5), top_k=pick(0, 1, 50, 900, vocab // 2).to(I32), min_p=pick(0.0, 0.0, 1e-3, 0.1))
+    beside = big.clone()[:, shift: shift + vocab]  # lies as x does, so that its sums are added up in the same order
+    for kw in (own, dict(temperature=1.0, top_k=0, min_p=0.0), dict(temperature=0.8, top_k=50, min_p=0.0),
+               dict(temperature=0.0, top_k=0, min_p=0.0)):
+        x.copy_(start), beside.copy_(start)
+        assert P.token_probs(x, out=x, **kw) is x
+        check_probs(x, start, **kw)
+        assert torch.equal(x.nan_to_num(7), P.token_probs(beside, **kw).nan_to_num(7))
+        assert (big[:, :shift] == -7).all() and (big[:, shift + vocab:] == -7).all()
+
+
 def test_probs_cut_next_to_an_entry(P):
     """The bound of min_p in 64 bits: entries a unit in the last place above and below it."""
     t, m = 0.75, 0.05
