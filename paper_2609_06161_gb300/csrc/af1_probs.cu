@@ -45,13 +45,16 @@ namespace af1 {
 namespace {
 
 constexpr int kLogThreads = 8, kThreads = 1 << kLogThreads;
-constexpr int kBlocks = 5;  // CTAs to an SM
+// CTAs to an SM; of rows that are not held four, whose 64 registers each spare spills (20 rows of 1000003 FP32, uncut: 84.3
+// us, with five 86.4).
+constexpr int kBlocks = 5, kLongBlocks = 4;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
 constexpr int kLogListed = 10, kListed = 1 << kLogListed;  // keys of a row that its CTAs list
 constexpr int kFew = 768;            // a top_k that the lists mostly have room for
 constexpr int kBins = 2048;
 constexpr int kMost = 100 * 1024 / 16;  // 16-byte pieces of a CTA's stretch in shared memory
+constexpr int kPart = 32;  // pieces whose weights a thread adds up one after another
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLeast = -1e4f;  // 2^d is 0 from far above on
 
@@ -138,15 +141,27 @@ __device__ __forceinline__ void meet(bool wrote) {
   cluster_wait();
 }
 
+// A sum of parts that carries what its roundings lose. One FP32 sum of all of a thread's weights was off by 2^-13 for a row of
+// 2^26 nearly equal entries, whose roundings go one way, and would be by more for longer ones.
+struct LongSum {
+  float sum = 0.f, over = 0.f;
+  __device__ __forceinline__ void add(float part) {
+    const float y = part - over, t = sum + y;
+    over = (t - sum) - y;
+    sum = t;
+  }
+};
+
 // What a CTA says of its stretch to the others.
 struct Said {
   float top, bound, sum;
 };
 
-// IN_PLACE: probs is logits. A piece that is not held is written by the thread that read it last. (A kernel of its own:
-// with both ways in one 20 rows of 1000003 FP32, beside their logits, took 82 us for 78.)
-template <typename T, bool IN_PLACE>
-__global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_constant__ ProbsProblem p) {
+// IN_PLACE: probs is logits. HELD: a CTA keeps its stretch in shared memory; otherwise it reads it again for every pass, and
+// the thread that read a piece last writes it. Kernels of their own: with both ways of a choice in one, registers did not
+// suffice (sums in parts beside short ones: 128 rows of 128000 FP32, uncut, 34.8 us for 30.4 before and 28.7 so).
+template <typename T, bool IN_PLACE, bool HELD>
+__global__ void __launch_bounds__(kThreads, HELD ? kBlocks : kLongBlocks) probs_kernel(const __grid_constant__ ProbsProblem p) {
   constexpr int E = 16 / (int)sizeof(T);
   extern __shared__ uint4 stretch[];
   __shared__ alignas(16) uint4 zeros[64];
@@ -197,9 +212,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
     }
     return y;
   };
-  const bool held = p.held > 0;
   auto piece = [&](int j) {
-    if (!held) return fetch(j);
+    if constexpr (!HELD) return fetch(j);
     Piece<T> y;
     y.w = stretch[j];
     return y;
@@ -276,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
     }
   };
   float top = -kInf;
-  if (held) {
+  if constexpr (HELD) {
     for (int j = tid; j < n; j += kThreads) {  // each thread's own pieces
       if (j >= j0 && j < j1)
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&stretch[j])), "l"(source + j) : "memory");
@@ -355,16 +369,25 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
     for (int d = kWarps / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     return sum;
   };
+  // part(from, to): the sum of the thread's weights among these pieces.
+  auto sum_parts = [&](auto&& part) {
+    if constexpr (HELD) return part(0, n);  // at most 25 pieces of a thread
+    LongSum sums;
+    for (int from = 0; from < n; from += kPart * kThreads) sums.add(part(from, min(n, from + kPart * kThreads)));
+    return sums.sum;
+  };
   float sum = 0.f;
   if (uncut() && set.temperature >= 1e-30f && top > -kInf && top < kInf) {
-    float2 sums = make_float2(0.f, 0.f);
-    for (int j = tid; j < n; j += kThreads) {
-      float2 y[E / 2];
-      weights(piece(j), y, top);
+    sum = block_sum(sum_parts([&](int from, int to) {
+      float2 sums = make_float2(0.f, 0.f);
+      for (int j = from + tid; j < to; j += kThreads) {
+        float2 y[E / 2];
+        weights(piece(j), y, top);
 #pragma unroll
-      for (int e = 0; e < E / 2; ++e) sums = add2(sums, y[e]);
-    }
-    sum = block_sum(sums.x + sums.y);
+        for (int e = 0; e < E / 2; ++e) sums = add2(sums, y[e]);
+      }
+      return sums.x + sums.y;
+    }));
   }
   __syncthreads();
   cluster_wait();
@@ -768,17 +791,19 @@ __global__ void __launch_bounds__(kThreads, kBlocks) probs_kernel(const __grid_c
         }
       }
     }
-    sum = 0.f;
-    for (int j = tid; j < n; j += kThreads) {
-      const Piece<T> w = piece(j);
-      if (w.most() < low) continue;
+    sum = block_sum(sum_parts([&](int start, int to) {
+      float some = 0.f;
+      for (int j = start + tid; j < to; j += kThreads) {
+        const Piece<T> w = piece(j);
+        if (w.most() < low) continue;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float v = (float)w.at(e);
-        if (v > low || (v == low && index_of(j) + e <= last)) sum += ex2((v - top) * c);
+        for (int e = 0; e < E; ++e) {
+          const float v = (float)w.at(e);
+          if (v > low || (v == low && index_of(j) + e <= last)) some += ex2((v - top) * c);
+        }
       }
-    }
-    sum = block_sum(sum);
+      return some;
+    }));
     if (tid < cs) *cluster.map_shared_rank(&all_sums[rank], tid) = sum;
     cluster.sync();  // counts were read, too
     sum = 0.f;
@@ -818,16 +843,16 @@ bool rows_overlap(const void* x, int64_t width, int64_t ld, const void* y, int64
   return false;
 }
 
-template <typename T, bool IN_PLACE>
+template <typename T, bool IN_PLACE, bool HELD>
 cudaError_t launch(const ProbsProblem& p, int64_t rows, cudaStream_t st) {
   const int cluster = 1 << p.log_cluster;
   const int smem = p.held * 16;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = once_per_device(done, [] {
     const cudaError_t first =
-        cudaFuncSetAttribute(probs_kernel<T, IN_PLACE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost * 16);
+        cudaFuncSetAttribute(probs_kernel<T, IN_PLACE, HELD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost * 16);
     if (first != cudaSuccess) return first;
-    return cudaFuncSetAttribute(probs_kernel<T, IN_PLACE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return cudaFuncSetAttribute(probs_kernel<T, IN_PLACE, HELD>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -842,7 +867,7 @@ cudaError_t launch(const ProbsProblem& p, int64_t rows, cudaStream_t st) {
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, probs_kernel<T, IN_PLACE>, p);
+  return cudaLaunchKernelEx(&cfg, probs_kernel<T, IN_PLACE, HELD>, p);
 }
 
 }  // namespace
@@ -896,9 +921,14 @@ int af1_token_probs(const af1_probs_args* a, void* stream) {
   const int64_t part = (pieces + (1 << p.log_cluster) - 1) >> p.log_cluster;
   p.held = part <= kMost ? (int)part : 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  e = a->dtype == AF1_F16 ? launch<__half, false>(p, a->rows, st)
-      : in_place          ? launch<float, true>(p, a->rows, st)
-                          : launch<float, false>(p, a->rows, st);
+  if (p.held > 0)
+    e = a->dtype == AF1_F16 ? launch<__half, false, true>(p, a->rows, st)
+        : in_place          ? launch<float, true, true>(p, a->rows, st)
+                            : launch<float, false, true>(p, a->rows, st);
+  else
+    e = a->dtype == AF1_F16 ? launch<__half, false, false>(p, a->rows, st)
+        : in_place          ? launch<float, true, false>(p, a->rows, st)
+                            : launch<float, false, false>(p, a->rows, st);
   if (e != cudaSuccess) return fail(AF1_ERR_CUDA, std::string(cudaGetErrorName(e)) + " (" + cudaGetErrorString(e) + ")");
   set_error(AF1_OK, "");
   return AF1_OK;

@@ -223,6 +223,25 @@ def test_probs_in_place(P, rows, vocab, shift):
         assert (big[:, :shift] == -7).all() and (big[:, shift + vocab:] == -7).all()
 
 
+@pytest.mark.parametrize("dtype", [F16, F32])
+@pytest.mark.parametrize("k", [0, 40000000])
+def test_probs_sums_of_long_rows(P, dtype, k):
+    """16000 nearly equal weights for every thread, whose roundings in one long sum would all go one way: that sum would be
+    off by 2^-14 or more."""
+    vocab, low = (1 << 26) + 3, -0.30859375
+    x = torch.full((1, vocab), low, device="cuda").to(dtype)
+    x[0, ::1 << 20] = 0.0  # in every stretch of the row
+    got = P.token_probs(x, top_k=k)[0]
+    kept, tops, rest = k or vocab, 65, math.exp(low)
+    top = 1.0 / (tops + (kept - tops) * rest)
+    # Three roundings of the exponent d = 0.45 and 2^-22 for its power, of the weight and of the sum's weights; up to 256
+    # weights one after another, 2^-24 each, and 60 more for the sums of these, 1 / S and the product.
+    tol = 2 * (3 * 2.0 ** -24 * 0.6932 * 0.45 + 2.0 ** -22) + (256 + 60) * 2.0 ** -24
+    assert int((got > 0).sum()) == kept
+    assert abs(float(got[0]) / top - 1) <= tol
+    assert abs(float(got[1]) / (top * rest) - 1) <= tol
+
+
 def test_probs_cut_next_to_an_entry(P):
     """The bound of min_p in 64 bits: entries a unit in the last place above and below it."""
     t, m = 0.75, 0.05
