@@ -817,7 +817,8 @@ AF1_API int af1_token_probs(const af1_probs_args* args, void* stream);
  * sum of R. (Of P where R has no mass; -1 where P has none, and where a tree has no node.)
  *   probs, draft: FP32 [sequences][nodes][vocab] with strides, rows that sum to 1;
  *       entries count as 0 .. 1 (NaN: 0). draft NULL: guesses. Rows of nodes that
- *       the walk does not come to are not read.
+ *       the walk does not come to change nothing, but their entries at their
+ *       children's tokens are read: the rows of all parents must be there.
  *   tokens, parents: device int32 [sequences][nodes]; node 0's own are not
  *       read, nor are nodes at counts and after. A node whose parent is no node, or
  *       whose token is outside the vocabulary, is never looked at, nor, with

@@ -447,6 +447,23 @@ def test_verify_strides(P, pad, draft_pad, shift, draft_shift):
 
 
 @pytest.mark.parametrize("mode", ["drawn", "distinct", "guessed"])
+def test_verify_rows_off_the_path(P, mode):
+    """What lies in rows of nodes that the walk does not come to changes nothing."""
+    g, rng = gen(16), np.random.default_rng(16)
+    b, n, vocab = 12, 14, 700
+    probs, draft = distributions(g, b, n, vocab, 0.7)
+    parents = trees(rng, b, n)
+    tokens = drawn_tokens(g, draft, parents, mode == "distinct")
+    u = torch.rand((b, n), generator=g, device="cuda")
+    kw = dict(draft=None if mode == "guessed" else draft, distinct=mode == "distinct")
+    want = P.verify_tree(probs, tokens, parents, u, **kw)
+    on = torch.zeros((b, n + 1), dtype=torch.bool, device="cuda").scatter_(1, torch.where(want[0] < 0, n, want[0]).long(), True)
+    for t, other in ((probs, NAN), (draft, INF), (probs, 1.0), (draft, -INF)):
+        t[~on[:, :n]] = other
+        assert all(torch.equal(a, z) for a, z in zip(P.verify_tree(probs, tokens, parents, u, **kw), want))
+
+
+@pytest.mark.parametrize("mode", ["drawn", "distinct", "guessed"])
 def test_verified_tokens_have_the_targets_distribution(P, mode):
     """Many sequences with one target and one draft: the first token that comes out (an accepted child's or the one that
     follows) has the target's probabilities, within 6 standard deviations."""
