@@ -13,7 +13,7 @@ behind the prefix, where the next step expects them.
 With a temperature it samples: the tree is verified against the target's
 probabilities with random numbers, the accepted slots move behind the prefix
 as they are, and the cache's pages are reserved and released step by step.
-Nothing but the tokens comes back to the host.
+Nothing but the tokens, and how many they are, comes back to the host.
 """
 from __future__ import annotations
 

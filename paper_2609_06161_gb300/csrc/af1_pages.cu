@@ -9,7 +9,9 @@
 // rows in 32 FP16 layers, 117 MB in pieces of 256 bytes: 19 us, 25 from a cold
 // cache), and latency the others (2 to 4 us). The table's calls decide on the device, so that the lengths
 // that verification gives need not reach the host: fork, reserve and release take
-// 12.8 us for 256 sequences over 131072 pages, 9.6 for 16 over 1000.
+// 12.7 us for 256 sequences over 131072 pages, 9.7 for 16 over 1000. Reserve's one block looks
+// for free pages 4096 at a time: 6.4 us for 512 of 131072 free ones, 34 where only the last 1 percent
+// are free, 215 of 1000000.
 #include <algorithm>
 
 #include "af1_internal.h"

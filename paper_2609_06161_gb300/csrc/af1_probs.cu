@@ -17,19 +17,23 @@
 //     index, inverted), so that ties go by index; every CTA gets all keys, finds the k-th
 //     and sums the kept weights. The row's zeros are on their way by then, so that
 //     only the kept entries are left to write.
-//   - Where more entries reach the bound than the lists hold (1024 of a row; large k): the
+//   - Where more entries reach the bound than the lists hold (1024 of a row, each CTA its share
+//     of them; large k, and ordinary k where likely tokens lie close together): the
 //     k-th's bin, of 2048 of equal width, by a count of all entries, and then its entries
 //     listed; where these are too many, too (ties), the k-th key by counts of its digits.
 //     A CTA adds up its share of all CTAs' counts (every CTA adding up all of them: 2.3 ms
-//     for 200 rows of 128001 FP32, k = 900, that take 0.15).
+//     for 200 rows of 128001 FP32, k = 900, that took 0.15 so). 200 such rows with k = 300 take 66 us
+//     where likely tokens are spread evenly, 135 where the mean falls by half a unit an octave of ids.
 // FP64 is slow enough here that the cut's logarithm, computed by every thread, took a
 // CTA 8 us: one thread computes it while the first entries are on their way.
 //
 // Measured (GPU, from a CUDA graph): 512 rows of 128001 FP16 logits with cuts
-// of their own 89 us (4.4 TB/s of logits and probabilities; of measured 6.8), uncut 83; 128 rows of 128000 FP32
-// uncut 30 (4.4 TB/s); 5 of 32000 FP32 with k = 50 7.4. In a CTA's life of 17 us under load its
-// copies land after 5, the first exchange takes 2, listing 2.5, the second exchange 3. Five CTAs
-// to an SM hide one another's waits: persistent clusters with the next row on its way, three to
+// of their own 88 us (4.5 TB/s of logits and probabilities; of measured 6.8), uncut 81; 128 rows of 128000 FP32
+// uncut 29 (4.5 TB/s); 5 of 32000 FP32 with k = 50 7.0. Waits bound large calls: a warp that is issued has waited 7 cycles
+// at barriers. The 512 rows have 64 KB stretches with cuts, three CTAs or 24 warps to an SM, and 32 KB without, five
+// CTAs; with cuts 32 KB take as long (88.5).
+// Earlier steps with cuts had 32 KB: there a CTA's life under load was 17 us, of which its copies landed after 5, the first
+// exchange took 2, listing 2.5, the second exchange 3. Persistent clusters with the next row on its way, three to
 // an SM, took 170 us for 99 then, stretches of 16 KB 170, 512 threads 131, and a row read again instead of held 110.
 #include <cooperative_groups.h>
 
@@ -907,11 +911,11 @@ int af1_token_probs(const af1_probs_args* a, void* stream) {
   }
   ProbsProblem p = {a->logits, a->ld,    a->probs,           a->probs_ld,  (int)a->vocab,  a->temperature,
                     a->top_k,  a->min_p, a->all_temperature, a->all_min_p, a->all_top_k, 0, 0};
-  // CTAs of a row: until all rows have one to an SM, while each thread has two pieces (5 rows of 32000: 8 CTAs to a row
-  // 7.4 us, one 16); and until a stretch is at most 64 KB where entries are cut, and 40 KB where not. Cuts cost a CTA as
-  // much as 30 KB, whatever its stretch, and write little at its end (200 rows of 128001 FP32, k = 300: 70 us in 8 CTAs, 83
-  // in 16); without them more CTAs to an SM, in different passes, are faster (200 rows of 128001 FP16: 38 us in 8, 43 in 4;
-  // 512 in 16, of 16 KB: 108 for 83).
+  // CTAs of a row: until all rows have one to an SM, while each thread has two pieces (5 rows of 32000 FP32: 8 CTAs to a row
+  // 7.0 us, two 9.5); and until a stretch is at most 64 KB where entries are cut, and 40 KB where not. Cuts cost a CTA as
+  // much as 30 KB, whatever its stretch, and write little at its end (200 rows of 128001 FP32, k = 300: 67 us in 8 CTAs, 81
+  // in 16; FP16 takes as long in 4 as in 8); without them more CTAs to an SM, in different passes, are faster (200 rows of
+  // 128001 FP16: 37 us in 8, 40 in 4; 512 in 16, of 16 KB: 106 for 81).
   const bool cuts = a->top_k != nullptr || a->min_p != nullptr || a->all_top_k > 0 || a->all_min_p > 0.f;
   const int64_t most = cuts ? 4096 : 2560, pieces = (a->vocab * es + 15) / 16 + 1;
   auto more = [&](int64_t ctas) {

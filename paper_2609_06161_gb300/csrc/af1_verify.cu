@@ -24,14 +24,16 @@
 // every CTA walks, all alike, so that only masses are exchanged; the others wait for rows to sum. Every
 // warp has a stretch of the vocabulary, so that a row is summed and then searched
 // (one warp's stretch, by marks in it) where the sum of the stretches before
-// passes the bound. Only rows that the walk needs are read, and with a draft, where they may be
-// summed more than once, they are kept in shared memory if there is room for them.
+// passes the bound. Only rows that the walk needs are summed, and with a draft, where they may be
+// summed more than once, they are kept in shared memory if all sequences' have room there at once (of 16
+// sequences over 128001 tokens they have not, of 15 they have).
 //
 // What bounds it is latency: launch, two trips to memory for the nodes, their exchange, half a
 // microsecond for every node that is looked at, and for every row its trip, an exchange and the search.
 // GPU times: 8 chains of 5 over 32000 tokens 7.7 us; 64 guessed trees of 32 over 128000 13 (33 MB of rows, of which
 // device memory would need 4.8); 16 trees of 16 over 128001, drawn without repetition, 25 (2.4): two to
-// four sums of a row of P and Q one after another, 3 to 5 us each. FP64 is slow enough to count:
+// four sums of a row of P and Q one after another, 3 to 5 us each, at the 64 registers of two CTAs to an SM,
+// which spill 44 bytes. FP64 is slow enough to count:
 // with every thread walking the three took 14, 34 and 41 us; clear cases are decided in FP32 beside it.
 #include <cooperative_groups.h>
 
